@@ -369,20 +369,23 @@ def _step(s):
 
 
 def _held(s, x, r, top):
-    """`x` in 8 bits: the largest of a block is 1.875 * 2^`top` steps of exponent up, 3 bits follow the leading one, and
-    the rest is rounded up with the probability r / 65536 says.  (codes with the sign of x, scales)"""
+    """`x` in 8 bits: relative to the power of two that brings a block's largest into (0.9375, 1.875], 3 bits follow the
+    leading one of a float with exponents from 0 to `top`, and the rest is rounded up with the probability r / 65536
+    says.  (codes with the sign of x, scales)"""
     block = s["block"]
     most = torch.zeros((x.shape[0], s["blocks"]), device="cuda").scatter_reduce_(1, block.expand(x.shape), x.abs(), "amax")
-    up = torch.where(most > 0, 1.875 / most, 0.0)
+    bits = most.view(torch.int32)
+    power = (bits & 0x7F800000) + torch.where((bits & 0x7FFFFF) > 0x700000, 1 << 23, 0).int()
+    up = ((254 << 23) - power).view(torch.float32)
     y = x.abs() * up[:, block]
     low = y * 2.0 ** (top - 127)                  # exponents below the format's come out as denormal numbers
     bits = low.view(torch.int32) + (r << 4).int()
     code = torch.clamp(bits >> 20, max=8 * top + 7).short()
-    return torch.where(x < 0, -code, code), most * (1 / 1.875)
+    return torch.where(x < 0, -code, code), power.view(torch.float32)
 
 
 def _value(code, top):
-    """What a code of _held stands for, the largest being 1.875."""
+    """What a code of _held stands for, relative to its block's scale: at most 1.875."""
     size = (code.abs().int() << 20).view(torch.float32) * 2.0 ** (127 - top)
     return torch.where(code < 0, -size, size)
 
@@ -543,17 +546,20 @@ def _exact_adamw(c, seed):
 
 
 def _exact_held(x, r, exponent_bits):
-    """`x` as 8 bits hold it: a float of 3 mantissa and so many exponent bits with gradual underflow, as a share of the
-    block's largest value, rounded up where its distance to the next lower one and r add up to a whole step."""
+    """`x` as 8 bits hold it: a float of 3 mantissa and so many exponent bits with gradual underflow, relative to a power of
+    two (the block's largest: above a half of 1.875, at most that), rounded up where its distance to the next lower
+    one and r add up to a whole step."""
     n, long = x.shape
     whole = -(-long // BLOCK) * BLOCK
     y = torch.nn.functional.pad(x.abs(), (0, whole - long)).view(n, -1, BLOCK)
     most = y.amax(2, keepdim=True)
-    y = torch.where(most > 0, y / most * 1.875, 0.0).view(n, -1)[:, :long]
+    share, exponent = torch.frexp(most / 1.875)      # share in [0.5, 1), exactly 0.5 for a power of two
+    scale = torch.where(share > 0.5, torch.exp2(exponent.double()), torch.exp2(exponent.double() - 1))
+    y = (y / scale).view(n, -1)[:, :long]
     exponent = torch.frexp(y)[1].sub(1).clamp(min=2 - 2 ** exponent_bits).double()
     step = torch.exp2(exponent - 3)
     size = torch.floor(y / step + r) * step
     if exponent_bits == 5:
         size = torch.where((y > 0) & (size == 0), step, size)
-    back = size.clamp(max=1.875) * (most.expand(n, -1, BLOCK).reshape(n, -1)[:, :long] / 1.875)
+    back = size.clamp(max=1.875) * scale.expand(n, -1, BLOCK).reshape(n, -1)[:, :long]
     return torch.where(x < 0, -back, back)
