@@ -2,6 +2,7 @@
 
 The compute lives in the HIP shared library built from csrc/; `binding`
 marshals arguments into its C ABI and raises if the library is missing.
+`train` binds the operators of a language model's local step around it.
 `synth` makes seeded synthetic inputs and has no dependency on the library.
 """
-__all__ = ["binding", "synth", "build"]
+__all__ = ["binding", "train", "synth", "build"]

@@ -1,0 +1,507 @@
+// Host side of the C ABI declared in include/choco_train.h: argument checks, workspace layout, kernel
+// launches.  No device memory is allocated here; only choco_adamw_init waits for the device.
+
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+#include <new>
+#include <vector>
+
+#include "choco_train.h"
+#include "choco_adamw.h"
+#include "choco_embed.h"
+#include "choco_recur.h"
+
+using namespace choco;
+
+namespace {
+
+thread_local int g_last_hip_error = 0;
+
+#define TRY_HIP(expr)                        \
+  do {                                       \
+    const hipError_t e_ = (expr);            \
+    if (e_ != hipSuccess) {                  \
+      g_last_hip_error = (int)e_;            \
+      return CHOCO_E_HIP;                    \
+    }                                        \
+  } while (0)
+
+constexpr int64_t kMaxIndex = (int64_t)1 << 31;
+constexpr int64_t kMaxExtent = (int64_t)1 << 60;   // entries of any array, strides included
+
+int type_bytes(int type) { return type == CHOCO_F32 ? 4 : type == CHOCO_BF16 || type == CHOCO_F16 ? 2 : 0; }
+bool aligned_to(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
+uint32_t blocks_of(int64_t items, int64_t per_block) { return (uint32_t)((items + per_block - 1) / per_block); }
+
+// calls FN.operator()<T>() for the C++ type of a CHOCO_F32 / BF16 / F16
+template <class Fn>
+void with_type(int type, Fn&& fn) {
+  if (type == CHOCO_F32) fn(float{});
+  else if (type == CHOCO_BF16) fn(bf16_t{});
+  else fn(f16_t{});
+}
+
+// ---- embedding ----
+
+int check_embed(const choco_embed_config* c) {
+  if (!c) return CHOCO_E_INVAL;
+  if (c->n < 0 || c->n > 65535 || c->tokens < 0 || c->tokens >= kMaxIndex || c->vocab < 1 || c->vocab >= kMaxIndex ||
+      c->dim < 0 || c->dim >= kMaxIndex)
+    return CHOCO_E_INVAL;
+  if ((c->token_type != CHOCO_I32 && c->token_type != CHOCO_I64) || !type_bytes(c->table_type) || !type_bytes(c->row_type))
+    return CHOCO_E_INVAL;
+  if (c->token_stride < c->tokens || c->row_ld < c->dim || c->row_ld >= kMaxIndex || c->table_stride < c->vocab * c->dim ||
+      c->row_stride < c->tokens * c->row_ld)
+    return CHOCO_E_INVAL;
+  const int64_t most = kMaxExtent / (c->n > 0 ? c->n : 1);
+  if (c->token_stride > most || c->table_stride > most || c->row_stride > most) return CHOCO_E_INVAL;
+  return CHOCO_OK;
+}
+
+EmbedArgs embed_args(const choco_embed_config& c, const void* tokens) {
+  EmbedArgs A{};
+  A.tokens = tokens;
+  A.ntokens = c.tokens;
+  A.vocab = c.vocab;
+  A.dim = c.dim;
+  A.token_stride = c.token_stride;
+  A.table_stride = c.table_stride;
+  A.row_stride = c.row_stride;
+  A.row_ld = c.row_ld;
+  A.scale = c.scale;
+  return A;
+}
+
+// ---- recurrence ----
+
+bool strides_ok(const choco_recur_config& c, const int64_t s[2], bool output) {
+  if (s[0] < 0 || s[1] < 0 || s[0] > kMaxExtent || s[1] > kMaxExtent) return false;
+  const double extent = (double)s[0] * (double)(c.batch - 1) + (double)s[1] * (double)(c.steps - 1) + (double)c.dim;
+  if (extent > (double)kMaxExtent) return false;
+  if (!output) return true;
+  // entries of an output apart: sequence after sequence, or step after step
+  const bool one_seq = c.batch <= 1, one_step = c.steps <= 1;
+  const bool by_seq = (one_step || s[1] >= c.dim) && (one_seq || (double)s[0] >= (double)s[1] * (double)(c.steps - 1) + (double)c.dim);
+  const bool by_step = (one_seq || s[0] >= c.dim) && (one_step || (double)s[1] >= (double)s[0] * (double)(c.batch - 1) + (double)c.dim);
+  return by_seq || by_step;
+}
+
+int check_recur(const choco_recur_config* c) {
+  if (!c) return CHOCO_E_INVAL;
+  if (c->batch < 0 || c->steps < 0 || c->dim < 0 || c->batch >= kMaxIndex || c->steps >= kMaxIndex || c->dim >= kMaxIndex)
+    return CHOCO_E_INVAL;
+  const int64_t most = (int64_t)1 << 40;
+  if (c->batch * c->dim >= most || c->batch * c->steps >= most) return CHOCO_E_INVAL;
+  if (!type_bytes(c->type)) return CHOCO_E_INVAL;
+  return CHOCO_OK;
+}
+
+RecurArgs recur_args(const choco_recur_config& c, const void* f, const void* u, const void* o, const int32_t* lengths) {
+  RecurArgs A{};
+  A.f = f; A.u = u; A.o = o;
+  A.lengths = lengths;
+  A.batch = c.batch; A.steps = c.steps; A.dim = c.dim;
+  A.f_seq = c.f_stride[0]; A.f_step = c.f_stride[1];
+  A.u_seq = c.u_stride[0]; A.u_step = c.u_stride[1];
+  A.o_seq = c.o_stride[0]; A.o_step = c.o_stride[1];
+  A.y_seq = c.y_stride[0]; A.y_step = c.y_stride[1];
+  A.df_seq = c.df_stride[0]; A.df_step = c.df_stride[1];
+  A.du_seq = c.du_stride[0]; A.du_step = c.du_stride[1];
+  A.do_seq = c.do_stride[0]; A.do_step = c.do_stride[1];
+  return A;
+}
+
+int64_t saved_floats(const choco_recur_config& c) {
+  return (c.steps + CHOCO_RECUR_SAVE_STEPS - 1) / CHOCO_RECUR_SAVE_STEPS * c.batch * c.dim;
+}
+
+// ---- AdamW ----
+
+struct AdamwLayout {
+  size_t state, m, v, m_scale, v_scale, state_end, tiles, total;
+  int32_t ntiles, nblocks, ngaps;
+};
+
+int64_t resolve_adamw_ld(const choco_adamw_config& c) { return c.ld == 0 ? (c.d + 3) / 4 * 4 : c.ld; }
+
+int check_adamw(const choco_adamw_config* c) {
+  if (!c) return CHOCO_E_INVAL;
+  if (c->n < 1 || c->n > 65535 || c->d < 1 || c->d > CHOCO_MAX_D) return CHOCO_E_INVAL;
+  const int64_t ld = resolve_adamw_ld(*c);
+  if (ld < c->d || (ld & 3) != 0 || ld > kMaxIndex) return CHOCO_E_INVAL;
+  if (!(c->beta1 >= 0.0 && c->beta1 < 1.0) || !(c->beta2 >= 0.0 && c->beta2 < 1.0)) return CHOCO_E_INVAL;
+  if ((float)c->beta1 >= 1.0f || (float)c->beta2 >= 1.0f) return CHOCO_E_INVAL;
+  if (!((float)c->eps > 0.0f) || !std::isfinite((float)c->eps)) return CHOCO_E_INVAL;
+  if (c->state_bits != 32 && c->state_bits != 8) return CHOCO_E_INVAL;
+  if (c->ntensors < 0 || (c->ntensors > 0 && (!c->start_host || !c->len_host))) return CHOCO_E_INVAL;
+  const int32_t rows = c->ntensors > 0 ? c->ntensors : 1;
+  int64_t end = 0;
+  for (int32_t t = 0; t < c->ntensors; ++t) {
+    const int64_t start = c->start_host[t], len = c->len_host[t];
+    if (start < end || len < 0 || start > c->d || len > c->d - start) return CHOCO_E_INVAL;
+    end = start + len;
+  }
+  for (int32_t t = 0; t < rows; ++t) {
+    if (c->weight_decay_host && !(c->weight_decay_host[t] >= 0.0f && std::isfinite(c->weight_decay_host[t]))) return CHOCO_E_INVAL;
+    if (c->lr_scale_host && !std::isfinite(c->lr_scale_host[t])) return CHOCO_E_INVAL;
+  }
+  return CHOCO_OK;
+}
+
+// calls fn(tensor, start, len) for every tensor
+template <class Fn>
+void for_tensors(const choco_adamw_config& c, Fn&& fn) {
+  if (c.ntensors == 0) fn(0, (int64_t)0, c.d);
+  for (int32_t t = 0; t < c.ntensors; ++t) fn(t, c.start_host[t], c.len_host[t]);
+}
+
+AdamwLayout adamw_layout(const choco_adamw_config& c) {
+  AdamwLayout L{};
+  int64_t tiles = 0, blocks = 0, gaps = 0, end = 0;   // (at most ld of each: 32 bits hold them)
+  for_tensors(c, [&](int32_t, int64_t start, int64_t len) {
+    tiles += (len + kTile - 1) / kTile;
+    blocks += (len + kMomentBlock - 1) / kMomentBlock;
+    gaps += (start - end + kTile - 1) / kTile;
+    end = start + len;
+  });
+  L.ngaps = (int32_t)(gaps + (resolve_adamw_ld(c) - end + kTile - 1) / kTile);
+  L.ntiles = (int32_t)tiles;
+  L.nblocks = (int32_t)blocks;
+  const size_t entries = (size_t)c.n * (size_t)resolve_adamw_ld(c);
+  size_t at = 0;
+  const auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at = (at + bytes + 255) / 256 * 256;
+    return here;
+  };
+  L.m = take(entries * (c.state_bits / 8));
+  L.v = take(entries * (c.state_bits / 8));
+  if (c.state_bits == 8) {
+    L.m_scale = take((size_t)c.n * L.nblocks * sizeof(float));
+    L.v_scale = take((size_t)c.n * L.nblocks * sizeof(float));
+  }
+  L.state_end = at;
+  L.tiles = take(((size_t)L.ntiles + L.ngaps) * sizeof(AdamwTile));
+  L.total = at;
+  return L;
+}
+
+}  // namespace
+
+struct choco_adamw {
+  AdamwArgs args;
+  AdamwLayout layout;
+  char* workspace;
+  hipStream_t stream;
+  double beta1, beta2;
+  int32_t n, state_bits;
+  uint64_t seed, t;
+};
+
+extern "C" {
+
+int choco_train_last_hip_error(void) { return g_last_hip_error; }
+
+int choco_embed_workspace_bytes(const choco_embed_config* cfg, size_t* bytes_host) {
+  if (!bytes_host) return CHOCO_E_INVAL;
+  if (const int rc = check_embed(cfg)) return rc;
+  *bytes_host = 0;
+  return CHOCO_OK;
+}
+
+int choco_embed_forward(const choco_embed_config* cfg, const void* tokens_dev, const void* table_dev, void* y_dev) {
+  if (const int rc = check_embed(cfg)) return rc;
+  const choco_embed_config& c = *cfg;
+  if (c.n == 0 || c.tokens == 0 || c.dim == 0) return CHOCO_OK;
+  if (!tokens_dev || !table_dev || !y_dev) return CHOCO_E_INVAL;
+  if (!aligned_to(tokens_dev, c.token_type == CHOCO_I32 ? 4 : 8) || !aligned_to(table_dev, type_bytes(c.table_type)) ||
+      !aligned_to(y_dev, type_bytes(c.row_type)))
+    return CHOCO_E_INVAL;
+  EmbedArgs A = embed_args(c, tokens_dev);
+  A.table = table_dev;
+  A.rows = y_dev;
+  const int lanes_log2 = 6;
+  const dim3 grid(blocks_of(c.tokens, 256 >> lanes_log2), (uint32_t)c.n);
+  with_type(c.table_type, [&](auto tab) {
+    with_type(c.row_type, [&](auto row) {
+      using Tab = decltype(tab);
+      using Row = decltype(row);
+      if (c.token_type == CHOCO_I32) k_embed<int32_t, Tab, Row, 1><<<grid, 256, 0, (hipStream_t)c.stream>>>(A, lanes_log2);
+      else k_embed<int64_t, Tab, Row, 1><<<grid, 256, 0, (hipStream_t)c.stream>>>(A, lanes_log2);
+    });
+  });
+  TRY_HIP(hipGetLastError());
+  return CHOCO_OK;
+}
+
+int choco_embed_backward(const choco_embed_config* cfg, const void* tokens_dev, const void* dy_dev, float* dtable_dev,
+                         int accumulate, void* workspace_dev, size_t workspace_bytes) {
+  if (const int rc = check_embed(cfg)) return rc;
+  const choco_embed_config& c = *cfg;
+  if (c.n == 0 || c.dim == 0 || (c.tokens == 0 && accumulate)) return CHOCO_OK;
+  if (!dtable_dev || (c.tokens > 0 && (!tokens_dev || !dy_dev))) return CHOCO_E_INVAL;
+  if (!aligned_to(tokens_dev, c.token_type == CHOCO_I32 ? 4 : 8) || !aligned_to(dtable_dev, 4) || !aligned_to(dy_dev, type_bytes(c.row_type)))
+    return CHOCO_E_INVAL;
+  if (c.vocab * c.dim >= (int64_t)1 << 38) return CHOCO_E_UNSUPPORTED;   // 2^31 workgroups of the pass that clears it
+  (void)workspace_dev;
+  (void)workspace_bytes;
+  EmbedArgs A = embed_args(c, tokens_dev);
+  A.rows = dy_dev;
+  A.dtable = dtable_dev;
+  const hipStream_t stream = (hipStream_t)c.stream;
+  if (!accumulate) {
+    k_embed_zero<<<dim3(blocks_of(c.vocab * c.dim, 256), (uint32_t)c.n), 256, 0, stream>>>(A);
+    TRY_HIP(hipGetLastError());
+  }
+  if (c.tokens == 0) return CHOCO_OK;
+  const dim3 grid((uint32_t)c.tokens, (uint32_t)c.n);
+  with_type(c.row_type, [&](auto row) {
+    using Row = decltype(row);
+    if (c.token_type == CHOCO_I32) k_embed_sum<int32_t, Row><<<grid, 64, 0, stream>>>(A);
+    else k_embed_sum<int64_t, Row><<<grid, 64, 0, stream>>>(A);
+  });
+  TRY_HIP(hipGetLastError());
+  return CHOCO_OK;
+}
+
+int choco_recur_saved_bytes(const choco_recur_config* cfg, size_t* bytes_host) {
+  if (!bytes_host) return CHOCO_E_INVAL;
+  if (const int rc = check_recur(cfg)) return rc;
+  *bytes_host = (size_t)saved_floats(*cfg) * sizeof(float);
+  return CHOCO_OK;
+}
+
+int choco_recur_workspace_bytes(const choco_recur_config* cfg, size_t* bytes_host) {
+  if (!bytes_host) return CHOCO_E_INVAL;
+  if (const int rc = check_recur(cfg)) return rc;
+  *bytes_host = 0;
+  return CHOCO_OK;
+}
+
+int choco_recur_forward(const choco_recur_config* cfg, const void* f_dev, const void* u_dev, const void* o_dev,
+                        const float* h0_dev, const int32_t* lengths_dev, void* y_dev, float* h_last_dev, float* saved_dev,
+                        void* workspace_dev, size_t workspace_bytes) {
+  if (const int rc = check_recur(cfg)) return rc;
+  const choco_recur_config& c = *cfg;
+  if (c.batch == 0 || c.dim == 0) return CHOCO_OK;
+  const size_t size = type_bytes(c.type);
+  if (c.steps > 0) {
+    if (!f_dev || !u_dev || !y_dev) return CHOCO_E_INVAL;
+    if (!strides_ok(c, c.f_stride, false) || !strides_ok(c, c.u_stride, false) || (o_dev && !strides_ok(c, c.o_stride, false)) ||
+        !strides_ok(c, c.y_stride, true))
+      return CHOCO_E_INVAL;
+  }
+  if (!aligned_to(f_dev, size) || !aligned_to(u_dev, size) || !aligned_to(o_dev, size) || !aligned_to(y_dev, size) ||
+      !aligned_to(h0_dev, 4) || !aligned_to(lengths_dev, 4) || !aligned_to(h_last_dev, 4) || !aligned_to(saved_dev, 4))
+    return CHOCO_E_INVAL;
+  if (c.batch * ((c.dim + 255) / 256) >= kMaxIndex) return CHOCO_E_UNSUPPORTED;   // (a grid's first dimension)
+  (void)workspace_dev;
+  (void)workspace_bytes;
+  RecurArgs A = recur_args(c, f_dev, u_dev, o_dev, lengths_dev);
+  A.h0 = h0_dev;
+  A.y = y_dev;
+  A.h_last = h_last_dev;
+  A.saved = saved_dev;
+  const dim3 grid((uint32_t)(c.batch * ((c.dim + 255) / 256)));
+  with_type(c.type, [&](auto x) {
+    using T = decltype(x);
+    if (o_dev) k_recur<T, true><<<grid, 256, 0, (hipStream_t)c.stream>>>(A);
+    else k_recur<T, false><<<grid, 256, 0, (hipStream_t)c.stream>>>(A);
+  });
+  TRY_HIP(hipGetLastError());
+  return CHOCO_OK;
+}
+
+int choco_recur_backward(const choco_recur_config* cfg, const void* f_dev, const void* u_dev, const void* o_dev,
+                         const int32_t* lengths_dev, const float* saved_dev, const void* dy_dev, const float* dlast_dev,
+                         void* df_dev, void* du_dev, void* do_dev, float* dh0_dev, void* workspace_dev, size_t workspace_bytes) {
+  if (const int rc = check_recur(cfg)) return rc;
+  const choco_recur_config& c = *cfg;
+  if (c.batch == 0 || c.dim == 0) return CHOCO_OK;
+  const size_t size = type_bytes(c.type);
+  if (c.steps > 0) {
+    if (!f_dev || !u_dev || !saved_dev || !dy_dev || !df_dev || !du_dev || (o_dev && !do_dev)) return CHOCO_E_INVAL;
+    if (!strides_ok(c, c.f_stride, false) || !strides_ok(c, c.u_stride, false) || (o_dev && !strides_ok(c, c.o_stride, false)) ||
+        !strides_ok(c, c.y_stride, false) || !strides_ok(c, c.df_stride, true) || !strides_ok(c, c.du_stride, true) ||
+        (o_dev && !strides_ok(c, c.do_stride, true)))
+      return CHOCO_E_INVAL;
+  }
+  if (!aligned_to(f_dev, size) || !aligned_to(u_dev, size) || !aligned_to(o_dev, size) || !aligned_to(dy_dev, size) ||
+      !aligned_to(df_dev, size) || !aligned_to(du_dev, size) || !aligned_to(do_dev, size) || !aligned_to(lengths_dev, 4) ||
+      !aligned_to(saved_dev, 4) || !aligned_to(dlast_dev, 4) || !aligned_to(dh0_dev, 4))
+    return CHOCO_E_INVAL;
+  if (c.batch * ((c.dim + 255) / 256) >= kMaxIndex) return CHOCO_E_UNSUPPORTED;   // (a grid's first dimension)
+  (void)workspace_dev;
+  (void)workspace_bytes;
+  RecurArgs A = recur_args(c, f_dev, u_dev, o_dev, lengths_dev);
+  A.saved = const_cast<float*>(saved_dev);
+  A.dy = dy_dev;
+  A.dlast = dlast_dev;
+  A.df = df_dev;
+  A.du = du_dev;
+  A.dout = do_dev;
+  A.dh0 = dh0_dev;
+  const dim3 grid((uint32_t)(c.batch * ((c.dim + 255) / 256)));
+  with_type(c.type, [&](auto x) {
+    using T = decltype(x);
+    if (o_dev) k_recur_back<T, true><<<grid, 256, 0, (hipStream_t)c.stream>>>(A);
+    else k_recur_back<T, false><<<grid, 256, 0, (hipStream_t)c.stream>>>(A);
+  });
+  TRY_HIP(hipGetLastError());
+  return CHOCO_OK;
+}
+
+int choco_adamw_workspace_bytes(const choco_adamw_config* cfg, size_t* bytes_host) {
+  if (!bytes_host) return CHOCO_E_INVAL;
+  if (const int rc = check_adamw(cfg)) return rc;
+  *bytes_host = adamw_layout(*cfg).total;
+  return CHOCO_OK;
+}
+
+int choco_adamw_init(const choco_adamw_config* cfg, float* x_dev, void* workspace_dev, size_t workspace_bytes,
+                     choco_adamw** out) {
+  if (!out) return CHOCO_E_INVAL;
+  *out = nullptr;
+  if (const int rc = check_adamw(cfg)) return rc;
+  if (!x_dev || !workspace_dev || !aligned_to(x_dev, 16) || !aligned_to(workspace_dev, 256)) return CHOCO_E_INVAL;
+  const choco_adamw_config& c = *cfg;
+  const AdamwLayout L = adamw_layout(c);
+  if (workspace_bytes < L.total) return CHOCO_E_NOMEM;
+  try {
+    std::vector<AdamwTile> tiles;
+    tiles.reserve((size_t)L.ntiles + L.ngaps);
+    const auto gap = [&](int64_t at, int64_t end) {   // entries of no tensor, behind the tensors' tiles
+      for (; at < end; at += kTile) {
+        AdamwTile tile{};
+        tile.start = (int32_t)at;
+        tile.len = (int32_t)(end - at < kTile ? end - at : kTile);
+        tile.block = -1;
+        tiles.push_back(tile);
+      }
+    };
+    int32_t block = 0;
+    for_tensors(c, [&](int32_t t, int64_t start, int64_t len) {
+      for (int64_t at = 0; at < len; at += kTile) {
+        AdamwTile tile{};
+        tile.start = (int32_t)(start + at);
+        tile.len = (int32_t)(len - at < kTile ? len - at : kTile);
+        tile.block = block;
+        tile.lr_scale = c.lr_scale_host ? c.lr_scale_host[t] : 1.0f;
+        tile.weight_decay = c.weight_decay_host ? c.weight_decay_host[t] : 0.0f;
+        block += (tile.len + kMomentBlock - 1) / kMomentBlock;
+        tiles.push_back(tile);
+      }
+    });
+    int64_t end = 0;
+    for_tensors(c, [&](int32_t, int64_t start, int64_t len) {
+      gap(end, start);
+      end = start + len;
+    });
+    gap(end, resolve_adamw_ld(c));
+    char* ws = (char*)workspace_dev;
+    const hipStream_t stream = (hipStream_t)c.stream;
+    TRY_HIP(hipMemsetAsync(ws, 0, L.state_end, stream));
+    if (!tiles.empty())
+      TRY_HIP(hipMemcpyAsync(ws + L.tiles, tiles.data(), tiles.size() * sizeof(AdamwTile), hipMemcpyHostToDevice, stream));
+    TRY_HIP(hipStreamSynchronize(stream));   // `tiles` goes
+    choco_adamw* a = new choco_adamw{};
+    a->layout = L;
+    a->workspace = ws;
+    a->stream = stream;
+    a->beta1 = c.beta1;
+    a->beta2 = c.beta2;
+    a->n = c.n;
+    a->state_bits = c.state_bits;
+    a->seed = c.seed;
+    AdamwArgs& A = a->args;
+    A.x = x_dev;
+    A.m = ws + L.m;
+    A.v = ws + L.v;
+    A.m_scale = (float*)(ws + L.m_scale);
+    A.v_scale = (float*)(ws + L.v_scale);
+    A.tiles = (const AdamwTile*)(ws + L.tiles);
+    A.ntiles = L.ntiles;
+    A.nblocks = L.nblocks;
+    A.ld = resolve_adamw_ld(c);
+    A.beta1 = (float)c.beta1;
+    A.one_minus_beta1 = (float)(1.0 - c.beta1);
+    A.beta2 = (float)c.beta2;
+    A.one_minus_beta2 = (float)(1.0 - c.beta2);
+    A.eps = (float)c.eps;
+    A.seed_lo = (uint32_t)c.seed;
+    A.seed_hi = (uint32_t)(c.seed >> 32);
+    *out = a;
+  } catch (const std::bad_alloc&) {
+    return CHOCO_E_NOMEM;
+  }
+  return CHOCO_OK;
+}
+
+int choco_adamw_step(choco_adamw* a, const void* g_dev, int32_t grad_type, float lr, const float* grad_scale_dev) {
+  if (!a || !g_dev || !aligned_to(g_dev, 16) || !aligned_to(grad_scale_dev, 4)) return CHOCO_E_INVAL;
+  if ((grad_type != CHOCO_F32 && grad_type != CHOCO_BF16) || !std::isfinite(lr)) return CHOCO_E_INVAL;
+  AdamwArgs A = a->args;
+  A.g = g_dev;
+  A.grad_scale = grad_scale_dev;
+  // the words of step t are keyed by the steps before it; its corrections are those of the (t + 1)-th
+  A.t_lo = (uint32_t)a->t;
+  A.t_hi = (uint32_t)(a->t >> 32);
+  const double t = (double)a->t + 1.0;
+  A.lr = lr;
+  A.rate = (float)((double)lr / (1.0 - std::pow(a->beta1, t)));
+  A.root_scale = (float)(1.0 / std::sqrt(1.0 - std::pow(a->beta2, t)));
+  if (A.ntiles > 0) {
+    const dim3 grid(blocks_of(A.ntiles, 4), (uint32_t)a->n);
+    if (grad_type == CHOCO_F32) {
+      if (a->state_bits == 32) k_adamw<float, 32><<<grid, 256, 0, a->stream>>>(A);
+      else k_adamw<float, 8><<<grid, 256, 0, a->stream>>>(A);
+    } else {
+      if (a->state_bits == 32) k_adamw<bf16_t, 32><<<grid, 256, 0, a->stream>>>(A);
+      else k_adamw<bf16_t, 8><<<grid, 256, 0, a->stream>>>(A);
+    }
+    TRY_HIP(hipGetLastError());
+  }
+  ++a->t;
+  return CHOCO_OK;
+}
+
+int choco_adamw_moments(choco_adamw* a, float* m_dev, float* v_dev) {
+  if (!a || !m_dev || !v_dev || !aligned_to(m_dev, 16) || !aligned_to(v_dev, 16)) return CHOCO_E_INVAL;
+  AdamwArgs A = a->args;
+  A.m_out = m_dev;
+  A.v_out = v_dev;
+  A.ntiles += a->layout.ngaps;
+  const dim3 grid(blocks_of(A.ntiles, 4), (uint32_t)a->n);
+  if (a->state_bits == 32) k_adamw_moments<32><<<grid, 256, 0, a->stream>>>(A);
+  else k_adamw_moments<8><<<grid, 256, 0, a->stream>>>(A);
+  TRY_HIP(hipGetLastError());
+  return CHOCO_OK;
+}
+
+int choco_adamw_state(choco_adamw* a, void** state_dev, size_t* bytes_host) {
+  if (!a || !state_dev || !bytes_host) return CHOCO_E_INVAL;
+  *state_dev = a->workspace;
+  *bytes_host = a->layout.state_end;
+  return CHOCO_OK;
+}
+
+int choco_adamw_get_step(choco_adamw* a, uint64_t* t_host) {
+  if (!a || !t_host) return CHOCO_E_INVAL;
+  *t_host = a->t;
+  return CHOCO_OK;
+}
+
+int choco_adamw_set_step(choco_adamw* a, uint64_t t) {
+  if (!a) return CHOCO_E_INVAL;
+  a->t = t;
+  return CHOCO_OK;
+}
+
+int choco_adamw_destroy(choco_adamw* a) {
+  delete a;
+  return CHOCO_OK;
+}
+
+}  // extern "C"

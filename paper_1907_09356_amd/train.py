@@ -1,0 +1,284 @@
+"""ctypes binding of include/choco_train.h: embedding lookup and gradient, gated linear recurrence, AdamW.
+
+Argument marshalling only, like `binding`: torch provides device memory and the stream (the current one of the
+tensors' device unless `stream` is given), every computation runs in the HIP library.  A tensor that is used on
+another stream than the one it was made on has to be kept by the caller until that stream is done with it.
+"""
+import ctypes
+
+import numpy as np
+import torch
+
+from . import binding
+from .binding import _check
+
+F32, BF16, F16 = 0, 1, 2
+I32, I64 = 0, 1
+SAVE_STEPS, BLOCK = 16, 256
+TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+
+EXPORTS = [
+    "choco_embed_workspace_bytes", "choco_embed_forward", "choco_embed_backward", "choco_recur_saved_bytes",
+    "choco_recur_workspace_bytes", "choco_recur_forward", "choco_recur_backward", "choco_adamw_workspace_bytes",
+    "choco_adamw_init", "choco_adamw_step", "choco_adamw_moments", "choco_adamw_state", "choco_adamw_get_step",
+    "choco_adamw_set_step", "choco_adamw_destroy", "choco_train_last_hip_error",
+]
+
+_i32, _i64, _u64, _f32, _f64 = ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64, ctypes.c_float, ctypes.c_double
+_vp, _size = ctypes.c_void_p, ctypes.c_size_t
+
+
+class EmbedConfig(ctypes.Structure):
+    _fields_ = [("n", _i32), ("tokens", _i64), ("vocab", _i64), ("dim", _i64), ("token_type", _i32), ("table_type", _i32),
+                ("row_type", _i32), ("token_stride", _i64), ("table_stride", _i64), ("row_stride", _i64), ("row_ld", _i64),
+                ("scale", _f32), ("stream", _vp)]
+
+
+class RecurConfig(ctypes.Structure):
+    _fields_ = [("batch", _i64), ("steps", _i64), ("dim", _i64), ("type", _i32)] + [
+        (name + "_stride", _i64 * 2) for name in ("f", "u", "o", "y", "df", "du", "do")] + [("stream", _vp)]
+
+
+class AdamwConfig(ctypes.Structure):
+    _fields_ = [("n", _i32), ("d", _i64), ("ld", _i64), ("ntensors", _i32), ("start_host", ctypes.POINTER(_i64)),
+                ("len_host", ctypes.POINTER(_i64)), ("weight_decay_host", ctypes.POINTER(_f32)),
+                ("lr_scale_host", ctypes.POINTER(_f32)), ("beta1", _f64), ("beta2", _f64), ("eps", _f64),
+                ("state_bits", _i32), ("seed", _u64), ("stream", _vp)]
+
+
+_lib = None
+
+
+def lib():
+    """The loaded HIP library.  Raises if it has not been built."""
+    global _lib
+    if _lib is None:
+        L = binding.lib()
+        embed, recur, adamw, size = (ctypes.POINTER(t) for t in (EmbedConfig, RecurConfig, AdamwConfig, _size))
+        L.choco_embed_workspace_bytes.argtypes = [embed, size]
+        L.choco_embed_forward.argtypes = [embed, _vp, _vp, _vp]
+        L.choco_embed_backward.argtypes = [embed, _vp, _vp, _vp, ctypes.c_int, _vp, _size]
+        L.choco_recur_saved_bytes.argtypes = [recur, size]
+        L.choco_recur_workspace_bytes.argtypes = [recur, size]
+        L.choco_recur_forward.argtypes = [recur] + [_vp] * 9 + [_size]
+        L.choco_recur_backward.argtypes = [recur] + [_vp] * 12 + [_size]
+        L.choco_adamw_workspace_bytes.argtypes = [adamw, size]
+        L.choco_adamw_init.argtypes = [adamw, _vp, _vp, _size, ctypes.POINTER(_vp)]
+        L.choco_adamw_step.argtypes = [_vp, _vp, _i32, _f32, _vp]
+        L.choco_adamw_moments.argtypes = [_vp, _vp, _vp]
+        L.choco_adamw_state.argtypes = [_vp, ctypes.POINTER(_vp), size]
+        L.choco_adamw_get_step.argtypes = [_vp, ctypes.POINTER(_u64)]
+        L.choco_adamw_set_step.argtypes = [_vp, _u64]
+        L.choco_adamw_destroy.argtypes = [_vp]
+        L.choco_train_last_hip_error.argtypes = []
+        for name in EXPORTS:
+            getattr(L, name).restype = ctypes.c_int
+        _lib = L
+    return _lib
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _stream(t, stream):
+    return torch.cuda.current_stream(t.device).cuda_stream if stream is None else stream
+
+
+def _workspace(query, cfg, like):
+    """Scratch of the size that `query` asks for, and that size."""
+    need = _size()
+    _check(query(ctypes.byref(cfg), ctypes.byref(need)), query.__name__)
+    return (torch.empty(need.value, dtype=torch.uint8, device=like.device) if need.value else None), need.value
+
+
+# ---- embedding ------------------------------------------------------------------------------------
+def _embed_config(tokens, table, rows, scale, stream):
+    assert tokens.dim() == 2 and table.dim() == 3 and rows.dim() == 3
+    assert tokens.is_cuda and table.device == tokens.device and rows.device == tokens.device
+    assert tokens.dtype in (torch.int32, torch.int64) and table.dtype in TYPES and rows.dtype in TYPES
+    (n, count), (_, vocab, dim) = tokens.shape, table.shape
+    assert table.shape[0] == n and rows.shape == (n, count, dim)
+    assert count <= 1 or tokens.stride(1) == 1
+    assert (dim <= 1 or table.stride(2) == 1) and (vocab <= 1 or table.stride(1) == dim)   # rows of a table lie one behind the other
+    assert dim <= 1 or rows.stride(2) == 1
+    row_ld = rows.stride(1) if count > 1 else dim
+    return EmbedConfig(n=n, tokens=count, vocab=vocab, dim=dim, token_type=I32 if tokens.dtype == torch.int32 else I64,
+                       table_type=TYPES[table.dtype], row_type=TYPES[rows.dtype],
+                       token_stride=tokens.stride(0) if n > 1 else count, table_stride=table.stride(0) if n > 1 else vocab * dim,
+                       row_stride=rows.stride(0) if n > 1 else count * row_ld, row_ld=row_ld, scale=scale,
+                       stream=_stream(tokens, stream))
+
+
+def embed(tokens, table, scale=1.0, out_dtype=None, out=None, stream=None):
+    """scale * table[w, tokens[w, r]] for every worker w: (n, R, dim).
+
+    tokens (n, R) of int32 or int64, zero rows for those outside [0, vocab); table (n, vocab, dim), e.g. a tensor's slice of the
+    workers' rows, `X[:, a:a + vocab * dim].view(n, vocab, dim)`."""
+    if out is None:
+        out = torch.empty(tokens.shape + table.shape[2:], dtype=out_dtype or table.dtype, device=table.device)
+    cfg = _embed_config(tokens, table, out, float(scale), stream)
+    _check(lib().choco_embed_forward(ctypes.byref(cfg), _ptr(tokens), _ptr(table), _ptr(out)), "choco_embed_forward")
+    return out
+
+
+def embed_grad(tokens, dout, dtable, scale=1.0, accumulate=False, stream=None):
+    """The gradient of `embed` with respect to its table, written (or added) to dtable (n, vocab, dim) of float32,
+    e.g. a tensor's slice of the workers' gradient rows."""
+    assert dtable.dtype == torch.float32
+    cfg = _embed_config(tokens, dtable, dout, float(scale), stream)
+    ws, nbytes = _workspace(lib().choco_embed_workspace_bytes, cfg, dtable)
+    _check(lib().choco_embed_backward(ctypes.byref(cfg), _ptr(tokens), _ptr(dout), _ptr(dtable), 1 if accumulate else 0,
+                                      _ptr(ws), nbytes), "choco_embed_backward")
+    return dtable
+
+
+# ---- gated linear recurrence ----------------------------------------------------------------------
+def _recur_config(f, stream, tensors):
+    B, T, C = f.shape
+    cfg = RecurConfig(batch=B, steps=T, dim=C, type=TYPES[f.dtype], stream=_stream(f, stream))
+    for name, t in tensors.items():
+        if t is None:
+            continue
+        assert t.device == f.device and t.dtype == f.dtype and t.shape == f.shape and (C <= 1 or t.stride(2) == 1), name
+        getattr(cfg, name + "_stride")[:] = t.stride()[:2]
+    return cfg
+
+
+def _state(t, f):
+    assert t is None or (t.device == f.device and t.dtype == torch.float32 and t.is_contiguous()
+                         and t.shape == (f.shape[0], f.shape[2]))
+    return t
+
+
+def _lengths(t, f):
+    assert t is None or (t.device == f.device and t.dtype == torch.int32 and t.is_contiguous() and t.shape == f.shape[:1])
+    return t
+
+
+def recurrence(f, u, o=None, h0=None, lengths=None, save=False, out=None, h_last=None, stream=None):
+    """h_t = a_t h_{t-1} + (1 - a_t) u_t with a = sigmoid(f), y = sigmoid(o) h (or h): (y, last states, saved).
+
+    f, u, o (batch, steps, dim) of one type, strided as they come (columns of one projection); h0 (batch, dim) of
+    float32, zero without; lengths (batch,) of int32.  save: keep what `recurrence_grad` needs (else None is returned).
+    h_last may be h0 itself, as in token by token generation."""
+    assert f.is_cuda and f.dim() == 3 and f.dtype in TYPES
+    B, T, C = f.shape
+    y = torch.empty((B, T, C), dtype=f.dtype, device=f.device) if out is None else out
+    if h_last is None:
+        h_last = torch.empty((B, C), dtype=torch.float32, device=f.device)
+    saved = None
+    if save:
+        saved = torch.empty(((T + SAVE_STEPS - 1) // SAVE_STEPS, B, C), dtype=torch.float32, device=f.device)
+    cfg = _recur_config(f, stream, dict(f=f, u=u, o=o, y=y))
+    ws, nbytes = _workspace(lib().choco_recur_workspace_bytes, cfg, f)
+    _check(lib().choco_recur_forward(ctypes.byref(cfg), _ptr(f), _ptr(u), _ptr(o), _ptr(_state(h0, f)),
+                                     _ptr(_lengths(lengths, f)), _ptr(y), _ptr(_state(h_last, f)), _ptr(saved), _ptr(ws),
+                                     nbytes), "choco_recur_forward")
+    return y, h_last, saved
+
+
+def recurrence_grad(f, u, saved, dy, o=None, lengths=None, dlast=None, stream=None):
+    """Backward pass of `recurrence`: (df, du, do or None, dh0), the first three columns of one matrix.
+
+    saved as `recurrence(..., save=True)` returned it; dlast the gradient of the last states, zero without."""
+    assert f.is_cuda and f.dim() == 3 and f.dtype in TYPES
+    B, T, C = f.shape
+    assert saved.device == f.device and saved.dtype == torch.float32 and saved.is_contiguous()
+    assert saved.shape == ((T + SAVE_STEPS - 1) // SAVE_STEPS, B, C)
+    parts = 2 if o is None else 3
+    grads = torch.empty((B, T, parts * C), dtype=f.dtype, device=f.device).split(C, 2) if C else [torch.empty_like(f)] * parts
+    df, du, do = grads[0], grads[1], None if o is None else grads[2]
+    dh0 = torch.empty((B, C), dtype=torch.float32, device=f.device)
+    cfg = _recur_config(f, stream, dict(f=f, u=u, o=o, y=dy, df=df, du=du, do=do))
+    ws, nbytes = _workspace(lib().choco_recur_workspace_bytes, cfg, f)
+    _check(lib().choco_recur_backward(ctypes.byref(cfg), _ptr(f), _ptr(u), _ptr(o), _ptr(_lengths(lengths, f)), _ptr(saved),
+                                      _ptr(dy), _ptr(_state(dlast, f)), _ptr(df), _ptr(du), _ptr(do), _ptr(dh0), _ptr(ws),
+                                      nbytes), "choco_recur_backward")
+    return df, du, do, dh0
+
+
+# ---- AdamW ----------------------------------------------------------------------------------------
+def make_adamw_config(n, d, ld=0, tensors=None, weight_decay=None, lr_scale=None, betas=(0.9, 0.999), eps=1e-8, state_bits=32,
+                      seed=0, stream=None):
+    """Fill a choco_adamw_config.  Returns (config, keepalive) as `binding.make_config` does.  tensors = (start, length)
+    arrays; weight_decay and lr_scale a number or one per tensor."""
+    cfg = AdamwConfig(n=int(n), d=int(d), ld=int(ld), beta1=float(betas[0]), beta2=float(betas[1]), eps=float(eps),
+                      state_bits=int(state_bits), seed=int(seed), stream=stream)
+    keep = []
+
+    def array(values, dtype, kind):
+        a = np.ascontiguousarray(values, dtype=dtype)
+        keep.append(a)
+        return a.ctypes.data_as(ctypes.POINTER(kind))
+
+    count = 1
+    if tensors is not None:
+        start, length = tensors[0], tensors[1]
+        assert len(start) == len(length)
+        cfg.ntensors = count = len(start)
+        cfg.start_host, cfg.len_host = array(start, np.int64, _i64), array(length, np.int64, _i64)
+    if weight_decay is not None:
+        cfg.weight_decay_host = array(np.broadcast_to(weight_decay, (count,)), np.float32, _f32)
+    if lr_scale is not None:
+        cfg.lr_scale_host = array(np.broadcast_to(lr_scale, (count,)), np.float32, _f32)
+    return cfg, tuple(keep)
+
+
+class AdamW:
+    """AdamW on the parameter rows X (n, ld) of all workers, in place: `step` takes the place of a local update, a gossip
+    step of `binding.Choco` on the same X may follow.  tensors: (start, length) arrays, e.g. the first two of a layer table;
+    the whole row is one without."""
+
+    def __init__(self, X, d, tensors=None, stream=None, **kw):
+        assert X.is_cuda and X.dtype == torch.float32 and X.is_contiguous() and X.dim() == 2
+        self.X, self.d = X, int(d)
+        self.cfg, keep = make_adamw_config(X.shape[0], d, X.shape[1], tensors, stream=_stream(X, stream), **kw)
+        need, a = _size(), _vp()
+        _check(lib().choco_adamw_workspace_bytes(ctypes.byref(self.cfg), ctypes.byref(need)), "choco_adamw_workspace_bytes")
+        self.workspace = torch.empty(need.value + 256, dtype=torch.uint8, device=X.device)
+        base = (self.workspace.data_ptr() + 255) // 256 * 256
+        _check(lib().choco_adamw_init(ctypes.byref(self.cfg), _ptr(X), base, need.value, ctypes.byref(a)), "choco_adamw_init")
+        del keep
+        self.handle = a
+
+    def close(self):
+        if getattr(self, "handle", None):
+            lib().choco_adamw_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def step(self, G, lr, grad_scale=None):
+        """G: gradients (n, ld) of float32 or bfloat16; grad_scale: (n,) of float32 on the device, a factor for each
+        worker's gradient (one that is not finite leaves the worker as it is)."""
+        assert G.device == self.X.device and G.is_contiguous() and G.shape == self.X.shape and G.dtype in (torch.float32, torch.bfloat16)
+        if grad_scale is not None:
+            assert grad_scale.device == G.device and grad_scale.dtype == torch.float32
+            assert grad_scale.is_contiguous() and grad_scale.shape == G.shape[:1]
+        _check(lib().choco_adamw_step(self.handle, _ptr(G), TYPES[G.dtype], float(lr), _ptr(grad_scale)), "choco_adamw_step")
+
+    def moments(self):
+        """(m, v), float32 of (n, d): what is held stands for."""
+        m, v = torch.empty_like(self.X), torch.empty_like(self.X)
+        _check(lib().choco_adamw_moments(self.handle, _ptr(m), _ptr(v)), "choco_adamw_moments")
+        return m[:, :self.d], v[:, :self.d]
+
+    def state(self):
+        """The moments as they are held, a view of bytes: copy it (and `get_step`) to save a run, copy back to resume it."""
+        p, count = _vp(), _size()
+        _check(lib().choco_adamw_state(self.handle, ctypes.byref(p), ctypes.byref(count)), "choco_adamw_state")
+        at = p.value - self.workspace.data_ptr()
+        return self.workspace[at:at + count.value]
+
+    def get_step(self):
+        t = _u64()
+        _check(lib().choco_adamw_get_step(self.handle, ctypes.byref(t)), "choco_adamw_get_step")
+        return t.value
+
+    def set_step(self, t):
+        _check(lib().choco_adamw_set_step(self.handle, int(t)), "choco_adamw_set_step")
