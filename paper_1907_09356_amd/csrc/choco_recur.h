@@ -8,6 +8,9 @@ namespace choco {
 
 constexpr int kSaveSteps = 16;   // the forward pass keeps the state before every so many steps
 
+constexpr int kRecurWaves = 8;   // most waves of a workgroup
+constexpr int kMaxSegments = 64; // most pieces that a sequence is split into
+
 struct RecurArgs {
   const void *f, *u, *o, *dy;
   void *y, *df, *du, *dout;
@@ -18,16 +21,20 @@ struct RecurArgs {
   int64_t batch, steps, dim;
   int64_t f_seq, f_step, u_seq, u_step, o_seq, o_step, y_seq, y_step;
   int64_t df_seq, df_step, du_seq, du_step, do_seq, do_step;
+  float2* parts;            // [segments][batch][dim], see k_recur_part; null: one segment
+  int64_t segment_steps;    // a multiple of kSaveSteps * (waves of a workgroup)
+  uint32_t strips, segments;
 };
 
-// sigmoid(x) and sigmoid(-x) = 1 - sigmoid(x), neither by a difference: exp(-|x|) <= 1 cannot overflow and the
-// smaller of the two keeps its relative accuracy (about 2^-22).
+// sigmoid(x) and 1 - sigmoid(x), the smaller of the two not by a difference: the exponential's argument is rounded to
+// |x| 2^-24, the rest is good to a few 2^-24.  exp(-x) may overflow: up is then 0 and down 1.
 __device__ __forceinline__ void gate(float x, float& up, float& down) {
-  const float e = __expf(-fabsf(x));
-  const float r = __builtin_amdgcn_rcpf(1.0f + e);
-  up = x >= 0.0f ? r : e * r;
-  down = x >= 0.0f ? e * r : r;
-  if (x != x) up = down = x;
+  const float e = __builtin_amdgcn_exp2f(x * -1.44269504f);
+  up = __builtin_amdgcn_rcpf(1.0f + e);
+  down = x >= 0.0f ? e * up : 1.0f - up;
+}
+__device__ __forceinline__ float gate(float x) {
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * -1.44269504f));
 }
 
 __device__ __forceinline__ int64_t steps_of(const RecurArgs& A, int64_t b) {
@@ -36,87 +43,369 @@ __device__ __forceinline__ int64_t steps_of(const RecurArgs& A, int64_t b) {
   return n < 0 ? 0 : n > A.steps ? A.steps : n;
 }
 
-// A lane per channel, step after step.
-template <class T, bool GATED>
-__global__ __launch_bounds__(256) void k_recur(RecurArgs A) {
-  const uint32_t strips = (uint32_t)((A.dim + 255) / 256);
-  const int64_t b = blockIdx.x / strips, c = (int64_t)(blockIdx.x % strips) * 256 + threadIdx.x;
-  if (c >= A.dim) return;
-  const int64_t len = steps_of(A, b);
-  const T* f = (const T*)A.f + b * A.f_seq + c;
-  const T* u = (const T*)A.u + b * A.u_seq + c;
-  const T* o = GATED ? (const T*)A.o + b * A.o_seq + c : nullptr;
-  T* y = (T*)A.y + b * A.y_seq + c;
-  float h = A.h0 ? A.h0[b * A.dim + c] : 0.0f;
-  for (int64_t t = 0; t < A.steps; ++t) {
-    if (A.saved && t % kSaveSteps == 0) A.saved[((t / kSaveSteps) * A.batch + b) * A.dim + c] = h;
-    float out = 0.0f;
-    if (t < len) {
-      float a, i;
-      gate(to_float(f[t * A.f_step]), a, i);
-      h = a * h + i * to_float(u[t * A.u_step]);
-      out = h;
-      if (GATED) {
-        float s, r;
-        gate(to_float(o[t * A.o_step]), s, r);
-        out = s * h;
-      }
-    }
-    y[t * A.y_step] = from_float<T>(out);
-  }
-  if (A.h_last) A.h_last[b * A.dim + c] = h;
+// How the work is split.  A strip is 64 * V channels of one sequence, V channels a lane.  A workgroup takes a strip (of
+// one segment of the sequence) and goes through its steps in rounds, kSaveSteps of a round for each wave: a wave loads
+// its steps at once, reduces them to the map h -> A h + H, the waves exchange these maps through LDS, and each applies
+// the maps before its own to the state and goes through its steps, which are still in registers, once more.  Everything
+// is read once, and the chain from step to step is as long as a round has waves, not steps.
+// Sequences with too few strips to fill the chip are split into segments, whose maps a first kernel (k_recur_part)
+// computes: f and u (backward: f, o and dy) are then read twice.
+struct RecurPlace {
+  int64_t b, c, len, begin, end;   // sequence, first channel of the lane, its length, the segment's steps
+  uint32_t segment;
+  bool in;                         // the lane has channels (one that has none works on the first ones and writes nothing)
+};
+
+template <int V>
+__device__ __forceinline__ RecurPlace recur_place(const RecurArgs& A) {
+  RecurPlace P;
+  const uint32_t rest = blockIdx.x / A.strips, strip = blockIdx.x % A.strips;
+  P.segment = rest / (uint32_t)A.batch;
+  P.b = rest % (uint32_t)A.batch;
+  P.c = (int64_t)strip * (64 * V) + (threadIdx.x & 63) * V;
+  P.in = P.c < A.dim;
+  if (!P.in) P.c = 0;
+  P.len = steps_of(A, P.b);
+  P.begin = P.segment * A.segment_steps;
+  P.end = P.begin + A.segment_steps < A.steps ? P.begin + A.segment_steps : A.steps;
+  return P;
 }
 
-// A lane per channel; from the last steps back, kSaveSteps at a time, whose states are computed again.
-template <class T, bool GATED>
-__global__ __launch_bounds__(256) void k_recur_back(RecurArgs A) {
-  const uint32_t strips = (uint32_t)((A.dim + 255) / 256);
-  const int64_t b = blockIdx.x / strips, c = (int64_t)(blockIdx.x % strips) * 256 + threadIdx.x;
-  if (c >= A.dim) return;
-  const int64_t len = steps_of(A, b);
-  const T* f = (const T*)A.f + b * A.f_seq + c;
-  const T* u = (const T*)A.u + b * A.u_seq + c;
-  const T* o = GATED ? (const T*)A.o + b * A.o_seq + c : nullptr;
-  const T* dy = (const T*)A.dy + b * A.y_seq + c;
-  T* df = (T*)A.df + b * A.df_seq + c;
-  T* du = (T*)A.du + b * A.du_seq + c;
-  T* dout = GATED ? (T*)A.dout + b * A.do_seq + c : nullptr;
-  float e = A.dlast ? A.dlast[b * A.dim + c] : 0.0f;   // a_{t+1} e_{t+1}
-  for (int64_t k = (A.steps + kSaveSteps - 1) / kSaveSteps - 1; k >= 0; --k) {
-    const int64_t t0 = k * kSaveSteps;
-    float h[kSaveSteps + 1];
-    h[0] = A.saved[(k * A.batch + b) * A.dim + c];
+// Rows t .. t + kSaveSteps - 1 of a lane's V channels; rows from `n` on repeat the last one before (n >= 1).
+template <class T, int V>
+__device__ __forceinline__ void load_steps(const void* base, int64_t seq, int64_t step, int64_t b, int64_t t, int64_t c, int n,
+                                           Pack<T, V> (&x)[kSaveSteps]) {
+  const T* p = (const T*)base + b * seq + t * step;
+#pragma unroll
+  for (int j = 0; j < kSaveSteps; ++j) {
+    x[j] = *reinterpret_cast<const Pack<T, V>*>(p + c);
+    p += j + 1 < n ? step : 0;
+  }
+}
+
+template <class T, int V>
+__device__ __forceinline__ void store_steps(void* base, int64_t seq, int64_t step, int64_t b, int64_t t, int64_t c, int j,
+                                            const float (&x)[V]) {
+  store_floats<T, V>((T*)base + b * seq + (t + j) * step + c, x);
+}
+
+__device__ __forceinline__ int steps_left(int64_t end, int64_t t) {
+  return end <= t ? 0 : end - t < kSaveSteps ? (int)(end - t) : kSaveSteps;
+}
+
+// (a, b) of the steps of a wave; steps that are not in the sequence pass the state on.
+template <class T, int V>
+__device__ __forceinline__ void step_maps(const Pack<T, V> (&f)[kSaveSteps], const Pack<T, V> (&u)[kSaveSteps], int n,
+                                          float (&a)[kSaveSteps][V], float (&b)[kSaveSteps][V]) {
+#pragma unroll
+  for (int j = 0; j < kSaveSteps; ++j)
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      float down;
+      gate(to_float(f[j].e[i]), a[j][i], down);
+      b[j][i] = down * to_float(u[j].e[i]);
+      if (j >= n) {
+        a[j][i] = 1.0f;
+        b[j][i] = 0.0f;
+      }
+    }
+}
+
+// The waves' maps in LDS, two rounds in turn (so that one barrier a round is enough).
+template <int V>
+struct RecurMaps {
+  float a[2][kRecurWaves][64][V], h[2][kRecurWaves][64][V];
+};
+
+template <class T, int V, bool GATED>
+__global__ __launch_bounds__(64 * kRecurWaves) void k_recur(RecurArgs A) {
+  __shared__ RecurMaps<V> S;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  const RecurPlace P = recur_place<V>(A);
+  float h[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) h[i] = A.parts || !A.h0 ? 0.0f : A.h0[P.b * A.dim + P.c + i];
+  if (A.parts)
+    for (uint32_t s = 0; s <= P.segment; ++s)
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const float2 m = A.parts[((int64_t)s * A.batch + P.b) * A.dim + P.c + i];
+        h[i] = fmaf(m.x, h[i], m.y);
+      }
+  int turn = 0;
+  for (int64_t t = P.begin; t < P.end; t += kSaveSteps * waves, turn ^= 1) {
+    const int64_t t0 = t + kSaveSteps * wave;
+    const int n = __builtin_amdgcn_readfirstlane(steps_left(P.len, t0)), all = __builtin_amdgcn_readfirstlane(steps_left(P.end, t0));
+    float a[kSaveSteps][V], b[kSaveSteps][V];
+    Pack<T, V> o[kSaveSteps];
+    float ma[V], mh[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      ma[i] = 1.0f;
+      mh[i] = 0.0f;
+    }
+    if (n > 0) {
+      Pack<T, V> f[kSaveSteps], u[kSaveSteps];
+      load_steps<T, V>(A.f, A.f_seq, A.f_step, P.b, t0, P.c, n, f);
+      load_steps<T, V>(A.u, A.u_seq, A.u_step, P.b, t0, P.c, n, u);
+      if (GATED) load_steps<T, V>(A.o, A.o_seq, A.o_step, P.b, t0, P.c, n, o);
+      step_maps<T, V>(f, u, n, a, b);
+#pragma unroll
+      for (int j = 0; j < kSaveSteps; ++j)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          mh[i] = fmaf(a[j][i], mh[i], b[j][i]);
+          ma[i] *= a[j][i];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      S.a[turn][wave][lane][i] = ma[i];
+      S.h[turn][wave][lane][i] = mh[i];
+    }
+    __syncthreads();
+    float g[V];
+    for (int w = 0; w < waves; ++w)
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        if (w == wave) g[i] = h[i];
+        h[i] = fmaf(S.a[turn][w][lane][i], h[i], S.h[turn][w][lane][i]);
+      }
+    if (!P.in || all == 0) continue;
+    if (A.saved) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) A.saved[((t0 / kSaveSteps) * A.batch + P.b) * A.dim + P.c + i] = g[i];
+    }
 #pragma unroll
     for (int j = 0; j < kSaveSteps; ++j) {
-      h[j + 1] = h[j];
-      if (t0 + j < len) {
-        float a, i;
-        gate(to_float(f[(t0 + j) * A.f_step]), a, i);
-        h[j + 1] = a * h[j] + i * to_float(u[(t0 + j) * A.u_step]);
-      }
-    }
+      float out[V];
+      if (j >= all) break;
 #pragma unroll
-    for (int j = kSaveSteps - 1; j >= 0; --j) {
-      const int64_t t = t0 + j;
-      if (t >= A.steps) continue;
-      float gf = 0.0f, gu = 0.0f, go = 0.0f;
-      if (t < len) {
-        float a, i, s = 1.0f, r = 0.0f;
-        gate(to_float(f[t * A.f_step]), a, i);
-        const float d = to_float(dy[t * A.y_step]);
-        if (GATED) gate(to_float(o[t * A.o_step]), s, r);
-        e += d * s;
-        go = d * h[j + 1] * s * r;
-        gu = e * i;
-        gf = e * (h[j] - to_float(u[t * A.u_step])) * a * i;
-        e *= a;
+      for (int i = 0; i < V; ++i) {
+        out[i] = 0.0f;
+        if (j < n) {
+          g[i] = fmaf(a[j][i], g[i], b[j][i]);
+          out[i] = GATED ? gate(to_float(o[j].e[i])) * g[i] : g[i];
+        }
       }
-      df[t * A.df_step] = from_float<T>(gf);
-      du[t * A.du_step] = from_float<T>(gu);
-      if (GATED) dout[t * A.do_step] = from_float<T>(go);
+      store_steps<T, V>(A.y, A.y_seq, A.y_step, P.b, t0, P.c, j, out);
     }
   }
-  if (A.dh0) A.dh0[b * A.dim + c] = e;
+  if (A.h_last && P.in && wave == 0 && P.segment + 1 == A.segments)
+#pragma unroll
+    for (int i = 0; i < V; ++i) A.h_last[P.b * A.dim + P.c + i] = h[i];
+}
+
+// The maps of the segments: parts[0] = (0, h0), parts[s + 1] = that of segment s; the last one's is not needed.  A wave
+// takes a piece of the segment in one go.
+template <class T, int V>
+__global__ __launch_bounds__(64 * kRecurWaves) void k_recur_part(RecurArgs A) {
+  __shared__ RecurMaps<V> S;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  const RecurPlace P = recur_place<V>(A);
+  const int64_t piece = A.segment_steps / waves;
+  float ma[V], mh[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    ma[i] = 1.0f;
+    mh[i] = 0.0f;
+  }
+  for (int64_t t0 = P.begin + wave * piece; t0 < P.begin + (wave + 1) * piece; t0 += kSaveSteps) {
+    const int n = __builtin_amdgcn_readfirstlane(steps_left(P.len, t0));
+    if (n == 0) break;
+    Pack<T, V> f[kSaveSteps], u[kSaveSteps];
+    load_steps<T, V>(A.f, A.f_seq, A.f_step, P.b, t0, P.c, n, f);
+    load_steps<T, V>(A.u, A.u_seq, A.u_step, P.b, t0, P.c, n, u);
+    float a[kSaveSteps][V], b[kSaveSteps][V];
+    step_maps<T, V>(f, u, n, a, b);
+#pragma unroll
+    for (int j = 0; j < kSaveSteps; ++j)
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        mh[i] = fmaf(a[j][i], mh[i], b[j][i]);
+        ma[i] *= a[j][i];
+      }
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    S.a[0][wave][lane][i] = ma[i];
+    S.h[0][wave][lane][i] = mh[i];
+  }
+  __syncthreads();
+  if (wave != 0 || !P.in) return;
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    for (int w = 1; w < waves; ++w) {
+      mh[i] = fmaf(S.a[0][w][lane][i], mh[i], S.h[0][w][lane][i]);
+      ma[i] *= S.a[0][w][lane][i];
+    }
+    const int64_t at = P.b * A.dim + P.c + i;
+    A.parts[(int64_t)(P.segment + 1) * A.batch * A.dim + at] = make_float2(ma[i], mh[i]);
+    if (P.segment == 0) A.parts[at] = make_float2(0.0f, A.h0 ? A.h0[at] : 0.0f);
+  }
+}
+
+// Backward: the same from the last steps back, with the map of a step on a_{t+1} e_{t+1}: e -> a (e + dy s).  The states
+// before each wave's steps are those that the forward pass kept.
+template <class T, int V, bool GATED>
+__global__ __launch_bounds__(64 * kRecurWaves) void k_recur_back(RecurArgs A) {
+  __shared__ RecurMaps<V> S;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  const RecurPlace P = recur_place<V>(A);
+  float e[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) e[i] = A.dlast ? A.dlast[P.b * A.dim + P.c + i] : 0.0f;
+  if (A.parts)
+    for (uint32_t s = A.segments - 1; s > P.segment; --s)
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const float2 m = A.parts[((int64_t)s * A.batch + P.b) * A.dim + P.c + i];
+        e[i] = fmaf(m.x, e[i], m.y);
+      }
+  const int64_t round = kSaveSteps * waves;
+  int turn = 0;
+  for (int64_t t = P.begin + (P.end - P.begin + round - 1) / round * round - round; t >= P.begin; t -= round, turn ^= 1) {
+    const int64_t t0 = t + kSaveSteps * wave;
+    const int n = __builtin_amdgcn_readfirstlane(steps_left(P.len, t0)), all = __builtin_amdgcn_readfirstlane(steps_left(P.end, t0));
+    // of each step: a, dy s, 1 - a, (h_{t-1} - u) a
+    float a[kSaveSteps][V], into[kSaveSteps][V], down[kSaveSteps][V], off[kSaveSteps][V];
+    float ma[V], me[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      ma[i] = 1.0f;
+      me[i] = 0.0f;
+    }
+    if (n > 0) {
+      Pack<T, V> f[kSaveSteps], u[kSaveSteps], o[kSaveSteps], d[kSaveSteps];
+      load_steps<T, V>(A.f, A.f_seq, A.f_step, P.b, t0, P.c, n, f);
+      load_steps<T, V>(A.u, A.u_seq, A.u_step, P.b, t0, P.c, n, u);
+      load_steps<T, V>(A.dy, A.y_seq, A.y_step, P.b, t0, P.c, n, d);
+      if (GATED) load_steps<T, V>(A.o, A.o_seq, A.o_step, P.b, t0, P.c, n, o);
+      float h[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) h[i] = A.saved[((t0 / kSaveSteps) * A.batch + P.b) * A.dim + P.c + i];
+#pragma unroll
+      for (int j = 0; j < kSaveSteps; ++j) {
+        float go[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          const float x = to_float(u[j].e[i]), dy = to_float(d[j].e[i]);
+          gate(to_float(f[j].e[i]), a[j][i], down[j][i]);
+          off[j][i] = (h[i] - x) * a[j][i];
+          h[i] = fmaf(a[j][i], h[i], down[j][i] * x);
+          into[j][i] = dy;
+          if (GATED) {
+            float s, r;
+            gate(to_float(o[j].e[i]), s, r);
+            into[j][i] = dy * s;
+            go[i] = dy * h[i] * s * r;
+          }
+          if (j >= n) {
+            a[j][i] = 1.0f;
+            into[j][i] = 0.0f;
+            go[i] = 0.0f;
+          }
+        }
+        if (GATED && P.in && j < all) store_steps<T, V>(A.dout, A.do_seq, A.do_step, P.b, t0, P.c, j, go);
+      }
+#pragma unroll
+      for (int j = kSaveSteps - 1; j >= 0; --j)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          me[i] = (me[i] + into[j][i]) * a[j][i];
+          ma[i] *= a[j][i];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      S.a[turn][wave][lane][i] = ma[i];
+      S.h[turn][wave][lane][i] = me[i];
+    }
+    __syncthreads();
+    float g[V];
+    for (int w = waves - 1; w >= 0; --w)
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        if (w == wave) g[i] = e[i];
+        e[i] = fmaf(S.a[turn][w][lane][i], e[i], S.h[turn][w][lane][i]);
+      }
+    if (!P.in || all == 0) continue;
+#pragma unroll
+    for (int j = kSaveSteps - 1; j >= 0; --j) {
+      if (j >= all) continue;
+      float gf[V], gu[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        gf[i] = gu[i] = 0.0f;
+        if (j < n) {
+          g[i] += into[j][i];
+          gu[i] = g[i] * down[j][i];
+          gf[i] = gu[i] * off[j][i];
+          g[i] *= a[j][i];
+        }
+      }
+      store_steps<T, V>(A.df, A.df_seq, A.df_step, P.b, t0, P.c, j, gf);
+      store_steps<T, V>(A.du, A.du_seq, A.du_step, P.b, t0, P.c, j, gu);
+      if (GATED && n == 0) {
+        const float zero[V] = {};
+        store_steps<T, V>(A.dout, A.do_seq, A.do_step, P.b, t0, P.c, j, zero);
+      }
+    }
+  }
+  if (A.dh0 && P.in && wave == 0 && P.segment == 0)
+#pragma unroll
+    for (int i = 0; i < V; ++i) A.dh0[P.b * A.dim + P.c + i] = e[i];
+}
+
+// parts[s] = the map of segment s; the first one's is not needed.
+template <class T, int V, bool GATED>
+__global__ __launch_bounds__(64 * kRecurWaves) void k_recur_back_part(RecurArgs A) {
+  __shared__ RecurMaps<V> S;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  RecurPlace P = recur_place<V>(A);
+  P.begin += A.segment_steps;     // from the second segment on
+  const int64_t piece = A.segment_steps / waves;
+  float ma[V], me[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    ma[i] = 1.0f;
+    me[i] = 0.0f;
+  }
+  for (int64_t t0 = P.begin + (wave + 1) * piece - kSaveSteps; t0 >= P.begin + wave * piece; t0 -= kSaveSteps) {
+    const int n = __builtin_amdgcn_readfirstlane(steps_left(P.len, t0));
+    if (n == 0) continue;
+    Pack<T, V> f[kSaveSteps], o[kSaveSteps], d[kSaveSteps];
+    load_steps<T, V>(A.f, A.f_seq, A.f_step, P.b, t0, P.c, n, f);
+    load_steps<T, V>(A.dy, A.y_seq, A.y_step, P.b, t0, P.c, n, d);
+    if (GATED) load_steps<T, V>(A.o, A.o_seq, A.o_step, P.b, t0, P.c, n, o);
+#pragma unroll
+    for (int j = kSaveSteps - 1; j >= 0; --j)
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const float a = gate(to_float(f[j].e[i]));
+        float into = to_float(d[j].e[i]);
+        if (GATED) into *= gate(to_float(o[j].e[i]));
+        if (j < n) {
+          me[i] = (me[i] + into) * a;
+          ma[i] *= a;
+        }
+      }
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    S.a[0][wave][lane][i] = ma[i];
+    S.h[0][wave][lane][i] = me[i];
+  }
+  __syncthreads();
+  if (wave != waves - 1 || !P.in) return;
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    for (int w = waves - 2; w >= 0; --w) {
+      me[i] = fmaf(S.a[0][w][lane][i], me[i], S.h[0][w][lane][i]);
+      ma[i] *= S.a[0][w][lane][i];
+    }
+    A.parts[((int64_t)(P.segment + 1) * A.batch + P.b) * A.dim + P.c + i] = make_float2(ma[i], me[i]);
+  }
 }
 
 }  // namespace choco

@@ -3,8 +3,10 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <initializer_list>
 #include <new>
 #include <vector>
 
@@ -29,6 +31,7 @@ thread_local int g_last_hip_error = 0;
   } while (0)
 
 constexpr int64_t kMaxIndex = (int64_t)1 << 31;
+constexpr int64_t kFewGroups = 512, kWantedGroups = 1024;
 constexpr int64_t kMaxExtent = (int64_t)1 << 60;   // entries of any array, strides included
 
 int type_bytes(int type) { return type == CHOCO_F32 ? 4 : type == CHOCO_BF16 || type == CHOCO_F16 ? 2 : 0; }
@@ -111,6 +114,75 @@ RecurArgs recur_args(const choco_recur_config& c, const void* f, const void* u, 
   A.du_seq = c.du_stride[0]; A.du_step = c.du_stride[1];
   A.do_seq = c.do_stride[0]; A.do_step = c.do_stride[1];
   return A;
+}
+
+// Channels a lane takes at once: two of 16 bits where everything is aligned to that.
+bool recur_pairs(const choco_recur_config& c, bool gated, bool back, std::initializer_list<const void*> pointers) {
+  if (c.type == CHOCO_F32 || c.dim % 2) return false;
+  uint64_t all = (uint64_t)(c.f_stride[0] | c.f_stride[1] | c.u_stride[0] | c.u_stride[1] | c.y_stride[0] | c.y_stride[1]);
+  if (gated) all |= (uint64_t)(c.o_stride[0] | c.o_stride[1]);
+  if (back) all |= (uint64_t)(c.df_stride[0] | c.df_stride[1] | c.du_stride[0] | c.du_stride[1]);
+  if (back && gated) all |= (uint64_t)(c.do_stride[0] | c.do_stride[1]);
+  if (all & 1) return false;
+  for (const void* p : pointers)
+    if (!aligned_to(p, 4)) return false;
+  return true;
+}
+
+// Waves of a workgroup, segments of a sequence and their steps, for strips of `width` channels.
+struct RecurPlan {
+  int64_t strips, segments, segment_steps;
+  int waves;
+};
+
+RecurPlan plan_recur(const choco_recur_config& c, int width) {
+  RecurPlan P{};
+  P.strips = (c.dim + width - 1) / width;
+  P.waves = (int)std::max<int64_t>(1, std::min<int64_t>(kRecurWaves, (c.steps + kSaveSteps - 1) / kSaveSteps));
+  const int64_t round = (int64_t)kSaveSteps * P.waves, rounds = std::max<int64_t>(1, (c.steps + round - 1) / round);
+  const int64_t groups = P.strips * c.batch;
+  P.segments = 1;
+  if (groups < kFewGroups && rounds >= 4) {
+    P.segments = std::min<int64_t>(std::min<int64_t>(kMaxSegments, rounds / 2), (kWantedGroups + groups - 1) / groups);
+  }
+  const int64_t each = (rounds + P.segments - 1) / P.segments;
+  P.segments = std::max<int64_t>(1, (rounds + each - 1) / each);
+  P.segment_steps = each * round;
+  return P;
+}
+
+size_t recur_workspace(const choco_recur_config& c) {
+  // (a call takes the wide strips or the narrow ones, whatever its pointers allow: room for either)
+  size_t most = 0;
+  for (int width : {64, 128}) {
+    const RecurPlan P = plan_recur(c, width);
+    if (P.segments > 1) most = std::max(most, (size_t)P.segments * c.batch * c.dim * sizeof(float2));
+  }
+  return most;
+}
+
+// The launches of a call: false where a grid's first dimension does not hold them.
+bool place_recur(const choco_recur_config& c, bool pairs, void* workspace, RecurArgs& A, dim3& grid, dim3& part, int& threads) {
+  const RecurPlan P = plan_recur(c, pairs ? 128 : 64);
+  const double groups = (double)P.strips * (double)c.batch;
+  if (groups * (double)P.segments >= (double)kMaxIndex) return false;
+  A.strips = (uint32_t)P.strips;
+  A.segments = (uint32_t)P.segments;
+  A.segment_steps = P.segment_steps;
+  A.parts = P.segments > 1 ? (float2*)workspace : nullptr;
+  threads = 64 * P.waves;
+  grid = dim3((uint32_t)(P.strips * c.batch * P.segments));
+  part = dim3((uint32_t)(P.strips * c.batch * (P.segments - 1)));
+  return true;
+}
+
+// calls fn with the channels a lane takes (a type's only where it can be two)
+template <class T, class Fn>
+void with_width(bool pairs, Fn&& fn) {
+  if constexpr (sizeof(T) == 2) {
+    if (pairs) return fn(std::integral_constant<int, 2>{});
+  }
+  fn(std::integral_constant<int, 1>{});
 }
 
 int64_t saved_floats(const choco_recur_config& c) {
@@ -276,7 +348,7 @@ int choco_recur_saved_bytes(const choco_recur_config* cfg, size_t* bytes_host) {
 int choco_recur_workspace_bytes(const choco_recur_config* cfg, size_t* bytes_host) {
   if (!bytes_host) return CHOCO_E_INVAL;
   if (const int rc = check_recur(cfg)) return rc;
-  *bytes_host = 0;
+  *bytes_host = recur_workspace(*cfg);
   return CHOCO_OK;
 }
 
@@ -296,19 +368,27 @@ int choco_recur_forward(const choco_recur_config* cfg, const void* f_dev, const 
   if (!aligned_to(f_dev, size) || !aligned_to(u_dev, size) || !aligned_to(o_dev, size) || !aligned_to(y_dev, size) ||
       !aligned_to(h0_dev, 4) || !aligned_to(lengths_dev, 4) || !aligned_to(h_last_dev, 4) || !aligned_to(saved_dev, 4))
     return CHOCO_E_INVAL;
-  if (c.batch * ((c.dim + 255) / 256) >= kMaxIndex) return CHOCO_E_UNSUPPORTED;   // (a grid's first dimension)
-  (void)workspace_dev;
-  (void)workspace_bytes;
+  const size_t need = recur_workspace(c);
+  if (need > 0 && (!workspace_dev || !aligned_to(workspace_dev, 16))) return CHOCO_E_INVAL;
+  if (need > workspace_bytes) return CHOCO_E_NOMEM;
   RecurArgs A = recur_args(c, f_dev, u_dev, o_dev, lengths_dev);
   A.h0 = h0_dev;
   A.y = y_dev;
   A.h_last = h_last_dev;
   A.saved = saved_dev;
-  const dim3 grid((uint32_t)(c.batch * ((c.dim + 255) / 256)));
+  const bool pairs = recur_pairs(c, o_dev, false, {f_dev, u_dev, o_dev, y_dev});
+  dim3 grid, part;
+  int threads;
+  if (!place_recur(c, pairs, workspace_dev, A, grid, part, threads)) return CHOCO_E_UNSUPPORTED;
+  const hipStream_t stream = (hipStream_t)c.stream;
   with_type(c.type, [&](auto x) {
     using T = decltype(x);
-    if (o_dev) k_recur<T, true><<<grid, 256, 0, (hipStream_t)c.stream>>>(A);
-    else k_recur<T, false><<<grid, 256, 0, (hipStream_t)c.stream>>>(A);
+    with_width<T>(pairs, [&](auto width) {
+      constexpr int V = decltype(width)::value;
+      if (A.parts) k_recur_part<T, V><<<part, threads, 0, stream>>>(A);
+      if (o_dev) k_recur<T, V, true><<<grid, threads, 0, stream>>>(A);
+      else k_recur<T, V, false><<<grid, threads, 0, stream>>>(A);
+    });
   });
   TRY_HIP(hipGetLastError());
   return CHOCO_OK;
@@ -332,9 +412,9 @@ int choco_recur_backward(const choco_recur_config* cfg, const void* f_dev, const
       !aligned_to(df_dev, size) || !aligned_to(du_dev, size) || !aligned_to(do_dev, size) || !aligned_to(lengths_dev, 4) ||
       !aligned_to(saved_dev, 4) || !aligned_to(dlast_dev, 4) || !aligned_to(dh0_dev, 4))
     return CHOCO_E_INVAL;
-  if (c.batch * ((c.dim + 255) / 256) >= kMaxIndex) return CHOCO_E_UNSUPPORTED;   // (a grid's first dimension)
-  (void)workspace_dev;
-  (void)workspace_bytes;
+  const size_t need = recur_workspace(c);
+  if (need > 0 && (!workspace_dev || !aligned_to(workspace_dev, 16))) return CHOCO_E_INVAL;
+  if (need > workspace_bytes) return CHOCO_E_NOMEM;
   RecurArgs A = recur_args(c, f_dev, u_dev, o_dev, lengths_dev);
   A.saved = const_cast<float*>(saved_dev);
   A.dy = dy_dev;
@@ -343,11 +423,23 @@ int choco_recur_backward(const choco_recur_config* cfg, const void* f_dev, const
   A.du = du_dev;
   A.dout = do_dev;
   A.dh0 = dh0_dev;
-  const dim3 grid((uint32_t)(c.batch * ((c.dim + 255) / 256)));
+  const bool pairs = recur_pairs(c, o_dev, true, {f_dev, u_dev, o_dev, dy_dev, df_dev, du_dev, do_dev});
+  dim3 grid, part;
+  int threads;
+  if (!place_recur(c, pairs, workspace_dev, A, grid, part, threads)) return CHOCO_E_UNSUPPORTED;
+  const hipStream_t stream = (hipStream_t)c.stream;
   with_type(c.type, [&](auto x) {
     using T = decltype(x);
-    if (o_dev) k_recur_back<T, true><<<grid, 256, 0, (hipStream_t)c.stream>>>(A);
-    else k_recur_back<T, false><<<grid, 256, 0, (hipStream_t)c.stream>>>(A);
+    with_width<T>(pairs, [&](auto width) {
+      constexpr int V = decltype(width)::value;
+      if (o_dev) {
+        if (A.parts) k_recur_back_part<T, V, true><<<part, threads, 0, stream>>>(A);
+        k_recur_back<T, V, true><<<grid, threads, 0, stream>>>(A);
+      } else {
+        if (A.parts) k_recur_back_part<T, V, false><<<part, threads, 0, stream>>>(A);
+        k_recur_back<T, V, false><<<grid, threads, 0, stream>>>(A);
+      }
+    });
   });
   TRY_HIP(hipGetLastError());
   return CHOCO_OK;

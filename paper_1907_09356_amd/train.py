@@ -5,6 +5,7 @@ tensors' device unless `stream` is given), every computation runs in the HIP lib
 another stream than the one it was made on has to be kept by the caller until that stream is done with it.
 """
 import ctypes
+import functools
 
 import numpy as np
 import torch
@@ -16,6 +17,7 @@ F32, BF16, F16 = 0, 1, 2
 I32, I64 = 0, 1
 SAVE_STEPS, BLOCK = 16, 256
 TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+TOKEN_TYPES = {torch.int32: I32, torch.int64: I64}
 
 EXPORTS = [
     "choco_embed_workspace_bytes", "choco_embed_forward", "choco_embed_backward", "choco_recur_saved_bytes",
@@ -85,29 +87,42 @@ def _stream(t, stream):
     return torch.cuda.current_stream(t.device).cuda_stream if stream is None else stream
 
 
-def _workspace(query, cfg, like):
-    """Scratch of the size that `query` asks for, and that size."""
+def _scratch(nbytes, like):
+    return torch.empty(nbytes, dtype=torch.uint8, device=like.device) if nbytes else None
+
+
+def _planned(cfg, query):
+    """A configuration by reference, and the bytes of workspace that `query` asks for it."""
     need = _size()
     _check(query(ctypes.byref(cfg), ctypes.byref(need)), query.__name__)
-    return (torch.empty(need.value, dtype=torch.uint8, device=like.device) if need.value else None), need.value
+    return ctypes.byref(cfg), need.value
 
 
 # ---- embedding ------------------------------------------------------------------------------------
+@functools.lru_cache(maxsize=512)
+def _embed_plan(token_shape, token_stride, token_type, table_shape, table_stride, table_type, row_shape, row_stride, row_type,
+                scale, stream):
+    """The configuration of a call, by what of its tensors goes into it."""
+    (n, count), (tables, vocab, dim) = token_shape, table_shape
+    assert tables == n and row_shape == (n, count, dim)
+    assert count <= 1 or token_stride[1] == 1
+    assert (dim <= 1 or table_stride[2] == 1) and (vocab <= 1 or table_stride[1] == dim)   # rows of a table lie one behind the other
+    assert dim <= 1 or row_stride[2] == 1
+    row_ld = row_stride[1] if count > 1 else dim
+    return _planned(EmbedConfig(n=n, tokens=count, vocab=vocab, dim=dim, token_type=TOKEN_TYPES[token_type],
+                                table_type=TYPES[table_type], row_type=TYPES[row_type],
+                                token_stride=token_stride[0] if n > 1 else count,
+                                table_stride=table_stride[0] if n > 1 else vocab * dim,
+                                row_stride=row_stride[0] if n > 1 else count * row_ld, row_ld=row_ld, scale=scale,
+                                stream=stream), lib().choco_embed_workspace_bytes)
+
+
 def _embed_config(tokens, table, rows, scale, stream):
-    assert tokens.dim() == 2 and table.dim() == 3 and rows.dim() == 3
     assert tokens.is_cuda and table.device == tokens.device and rows.device == tokens.device
-    assert tokens.dtype in (torch.int32, torch.int64) and table.dtype in TYPES and rows.dtype in TYPES
-    (n, count), (_, vocab, dim) = tokens.shape, table.shape
-    assert table.shape[0] == n and rows.shape == (n, count, dim)
-    assert count <= 1 or tokens.stride(1) == 1
-    assert (dim <= 1 or table.stride(2) == 1) and (vocab <= 1 or table.stride(1) == dim)   # rows of a table lie one behind the other
-    assert dim <= 1 or rows.stride(2) == 1
-    row_ld = rows.stride(1) if count > 1 else dim
-    return EmbedConfig(n=n, tokens=count, vocab=vocab, dim=dim, token_type=I32 if tokens.dtype == torch.int32 else I64,
-                       table_type=TYPES[table.dtype], row_type=TYPES[rows.dtype],
-                       token_stride=tokens.stride(0) if n > 1 else count, table_stride=table.stride(0) if n > 1 else vocab * dim,
-                       row_stride=rows.stride(0) if n > 1 else count * row_ld, row_ld=row_ld, scale=scale,
-                       stream=_stream(tokens, stream))
+    assert tokens.dim() == 2 and table.dim() == 3 and rows.dim() == 3
+    assert tokens.dtype in TOKEN_TYPES and table.dtype in TYPES and rows.dtype in TYPES
+    return _embed_plan(tokens.shape, tokens.stride(), tokens.dtype, table.shape, table.stride(), table.dtype, rows.shape,
+                       rows.stride(), rows.dtype, scale, _stream(tokens, stream))
 
 
 def embed(tokens, table, scale=1.0, out_dtype=None, out=None, stream=None):
@@ -117,8 +132,8 @@ def embed(tokens, table, scale=1.0, out_dtype=None, out=None, stream=None):
     workers' rows, `X[:, a:a + vocab * dim].view(n, vocab, dim)`."""
     if out is None:
         out = torch.empty(tokens.shape + table.shape[2:], dtype=out_dtype or table.dtype, device=table.device)
-    cfg = _embed_config(tokens, table, out, float(scale), stream)
-    _check(lib().choco_embed_forward(ctypes.byref(cfg), _ptr(tokens), _ptr(table), _ptr(out)), "choco_embed_forward")
+    cfg, _ = _embed_config(tokens, table, out, float(scale), stream)
+    _check(lib().choco_embed_forward(cfg, tokens.data_ptr(), table.data_ptr(), out.data_ptr()), "choco_embed_forward")
     return out
 
 
@@ -126,23 +141,32 @@ def embed_grad(tokens, dout, dtable, scale=1.0, accumulate=False, stream=None):
     """The gradient of `embed` with respect to its table, written (or added) to dtable (n, vocab, dim) of float32,
     e.g. a tensor's slice of the workers' gradient rows."""
     assert dtable.dtype == torch.float32
-    cfg = _embed_config(tokens, dtable, dout, float(scale), stream)
-    ws, nbytes = _workspace(lib().choco_embed_workspace_bytes, cfg, dtable)
-    _check(lib().choco_embed_backward(ctypes.byref(cfg), _ptr(tokens), _ptr(dout), _ptr(dtable), 1 if accumulate else 0,
+    cfg, nbytes = _embed_config(tokens, dtable, dout, float(scale), stream)
+    ws = _scratch(nbytes, dtable)
+    _check(lib().choco_embed_backward(cfg, tokens.data_ptr(), dout.data_ptr(), dtable.data_ptr(), 1 if accumulate else 0,
                                       _ptr(ws), nbytes), "choco_embed_backward")
     return dtable
 
 
 # ---- gated linear recurrence ----------------------------------------------------------------------
-def _recur_config(f, stream, tensors):
-    B, T, C = f.shape
-    cfg = RecurConfig(batch=B, steps=T, dim=C, type=TYPES[f.dtype], stream=_stream(f, stream))
-    for name, t in tensors.items():
-        if t is None:
-            continue
-        assert t.device == f.device and t.dtype == f.dtype and t.shape == f.shape and (C <= 1 or t.stride(2) == 1), name
-        getattr(cfg, name + "_stride")[:] = t.stride()[:2]
-    return cfg
+@functools.lru_cache(maxsize=512)
+def _recur_plan(shape, dtype, strides, stream):
+    """The configuration of a call: strides of f, u, o, y (backward: dy), df, du, do, None for one that is not there."""
+    assert shape[2] <= 1 or all(s is None or s[2] == 1 for s in strides)
+    cfg = RecurConfig(batch=shape[0], steps=shape[1], dim=shape[2], type=TYPES[dtype], stream=stream)
+    for name, s in zip(("f", "u", "o", "y", "df", "du", "do"), strides):
+        if s is not None:
+            getattr(cfg, name + "_stride")[:] = s[:2]
+    return _planned(cfg, lib().choco_recur_workspace_bytes)
+
+
+def _recur_config(f, stream, *tensors):
+    device, dtype, shape = f.device, f.dtype, f.shape
+    strides = [f.stride()]
+    for t in tensors:
+        assert t is None or (t.device == device and t.dtype == dtype and t.shape == shape)
+        strides.append(None if t is None else t.stride())
+    return _recur_plan(shape, dtype, tuple(strides), _stream(f, stream))
 
 
 def _state(t, f):
@@ -170,9 +194,9 @@ def recurrence(f, u, o=None, h0=None, lengths=None, save=False, out=None, h_last
     saved = None
     if save:
         saved = torch.empty(((T + SAVE_STEPS - 1) // SAVE_STEPS, B, C), dtype=torch.float32, device=f.device)
-    cfg = _recur_config(f, stream, dict(f=f, u=u, o=o, y=y))
-    ws, nbytes = _workspace(lib().choco_recur_workspace_bytes, cfg, f)
-    _check(lib().choco_recur_forward(ctypes.byref(cfg), _ptr(f), _ptr(u), _ptr(o), _ptr(_state(h0, f)),
+    cfg, nbytes = _recur_config(f, stream, u, o, y)
+    ws = _scratch(nbytes, f)
+    _check(lib().choco_recur_forward(cfg, _ptr(f), _ptr(u), _ptr(o), _ptr(_state(h0, f)),
                                      _ptr(_lengths(lengths, f)), _ptr(y), _ptr(_state(h_last, f)), _ptr(saved), _ptr(ws),
                                      nbytes), "choco_recur_forward")
     return y, h_last, saved
@@ -190,9 +214,9 @@ def recurrence_grad(f, u, saved, dy, o=None, lengths=None, dlast=None, stream=No
     grads = torch.empty((B, T, parts * C), dtype=f.dtype, device=f.device).split(C, 2) if C else [torch.empty_like(f)] * parts
     df, du, do = grads[0], grads[1], None if o is None else grads[2]
     dh0 = torch.empty((B, C), dtype=torch.float32, device=f.device)
-    cfg = _recur_config(f, stream, dict(f=f, u=u, o=o, y=dy, df=df, du=du, do=do))
-    ws, nbytes = _workspace(lib().choco_recur_workspace_bytes, cfg, f)
-    _check(lib().choco_recur_backward(ctypes.byref(cfg), _ptr(f), _ptr(u), _ptr(o), _ptr(_lengths(lengths, f)), _ptr(saved),
+    cfg, nbytes = _recur_config(f, stream, u, o, dy, df, du, do)
+    ws = _scratch(nbytes, f)
+    _check(lib().choco_recur_backward(cfg, _ptr(f), _ptr(u), _ptr(o), _ptr(_lengths(lengths, f)), _ptr(saved),
                                       _ptr(dy), _ptr(_state(dlast, f)), _ptr(df), _ptr(du), _ptr(do), _ptr(dh0), _ptr(ws),
                                       nbytes), "choco_recur_backward")
     return df, du, do, dh0

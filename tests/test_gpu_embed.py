@@ -3,8 +3,6 @@
 Tolerances: a looked-up row is one fp32 product, rounded once: bit for bit.  A sum of k rows in fp32, in whatever order, is
 off by at most k + 1 roundings (one of them the scale's) of 2^-24 of the sum of magnitudes, the first order of the
 standard bound; 2 more are allowed for the second order and, accumulating, for what was there."""
-import ctypes
-
 import numpy as np
 import pytest
 import torch
@@ -227,6 +225,5 @@ def test_arguments_are_checked():
                 lambda: T.embed_grad(tokens, table, table), lambda: T.embed_grad(tokens, table[:, :3], table.bfloat16())):
         with pytest.raises(AssertionError):
             bad()
-    cfg = T._embed_config(tokens, table, table[:, :3], 1.0, None)
-    cfg.vocab = 0
-    assert T.lib().choco_embed_forward(ctypes.byref(cfg), tokens.data_ptr(), table.data_ptr(), table.data_ptr()) == B.E_INVAL
+    with pytest.raises(B.ChocoError):
+        T.embed(tokens[:, :1].expand(2, 3).contiguous(), table, out=torch.zeros((2, 1, 4), device="cuda").expand(2, 3, 4))
