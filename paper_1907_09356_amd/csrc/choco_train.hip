@@ -8,6 +8,8 @@
 #include <cstdint>
 #include <initializer_list>
 #include <new>
+#include <type_traits>
+#include <utility>
 #include <vector>
 
 #include "choco_train.h"
@@ -36,6 +38,8 @@ constexpr int64_t kMaxExtent = (int64_t)1 << 60;   // entries of any array, stri
 
 int type_bytes(int type) { return type == CHOCO_F32 ? 4 : type == CHOCO_BF16 || type == CHOCO_F16 ? 2 : 0; }
 bool aligned_to(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
+// A grid's first dimension holds less than 2^32 threads.
+bool launch_fits(double blocks, int threads) { return blocks * threads < 4294967296.0; }
 uint32_t blocks_of(int64_t items, int64_t per_block) { return (uint32_t)((items + per_block - 1) / per_block); }
 
 // calls FN.operator()<T>() for the C++ type of a CHOCO_F32 / BF16 / F16
@@ -75,6 +79,67 @@ EmbedArgs embed_args(const choco_embed_config& c, const void* tokens) {
   A.row_ld = c.row_ld;
   A.scale = c.scale;
   return A;
+}
+
+// How the gradient's tokens are put in order, and where its workspace lies.
+struct EmbedLayout {
+  size_t keys, places, keys_next, places_next, counts, partial, total;
+  int64_t pieces, partial_ld;
+  uint32_t chunks;
+  int digit_bits, passes;
+  bool one;    // a workgroup orders all of a worker's tokens
+};
+
+EmbedLayout embed_layout(const choco_embed_config& c) {
+  EmbedLayout L{};
+  if (c.n == 0 || c.tokens == 0 || c.dim == 0) return L;
+  L.one = c.tokens <= kSortOne;
+  int bits = 1;
+  while (c.vocab >> bits) ++bits;    // keys go up to vocab itself
+  const int most = L.one ? kSortDigit : kChunkDigit;
+  L.passes = (bits + most - 1) / most;
+  L.digit_bits = (bits + L.passes - 1) / L.passes;
+  L.chunks = blocks_of(c.tokens, kChunkTokens);
+  L.pieces = (c.tokens + kPiece - 1) / kPiece;
+  L.partial_ld = (c.dim + 7) / 8 * 8;
+  size_t at = 0;
+  const auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at = (at + bytes + 255) / 256 * 256;
+    return here;
+  };
+  const size_t list = (size_t)c.n * (size_t)c.tokens * sizeof(uint32_t);
+  L.keys = take(list);
+  L.places = take(list);
+  if (!L.one) {
+    L.keys_next = take(list);
+    L.places_next = take(list);
+    L.counts = take(((size_t)c.n * L.chunks << L.digit_bits) * sizeof(uint32_t));
+  }
+  L.partial = take((size_t)c.n * (size_t)L.pieces * 2 * (size_t)L.partial_ld * sizeof(float));
+  L.total = at;
+  return L;
+}
+
+// Entries that a lane moves at once: most, most / 2, ... or 1, as rows and strides are aligned.
+int embed_width(int most, int64_t dim, std::initializer_list<std::pair<const void*, size_t>> pointers,
+                std::initializer_list<std::pair<int64_t, size_t>> strides) {
+  for (int v = most; v > 1; v /= 2) {
+    bool ok = dim % v == 0;
+    for (const auto& p : pointers) ok = ok && aligned_to(p.first, std::min<size_t>(v * p.second, 16));
+    for (const auto& s : strides) ok = ok && (size_t)s.first * s.second % std::min<size_t>(v * s.second, 16) == 0;
+    if (ok) return v;
+  }
+  return 1;
+}
+
+// calls fn with the width as a type's value
+template <class Fn>
+void with_vector(int v, Fn&& fn) {
+  if (v == 8) fn(std::integral_constant<int, 8>{});
+  else if (v == 4) fn(std::integral_constant<int, 4>{});
+  else if (v == 2) fn(std::integral_constant<int, 2>{});
+  else fn(std::integral_constant<int, 1>{});
 }
 
 // ---- recurrence ----
@@ -161,11 +226,11 @@ size_t recur_workspace(const choco_recur_config& c) {
   return most;
 }
 
-// The launches of a call: false where a grid's first dimension does not hold them.
+// The launches of a call: false where a grid does not hold them.
 bool place_recur(const choco_recur_config& c, bool pairs, void* workspace, RecurArgs& A, dim3& grid, dim3& part, int& threads) {
   const RecurPlan P = plan_recur(c, pairs ? 128 : 64);
   const double groups = (double)P.strips * (double)c.batch;
-  if (groups * (double)P.segments >= (double)kMaxIndex) return false;
+  if (!launch_fits(groups * (double)P.segments, 64 * P.waves)) return false;
   A.strips = (uint32_t)P.strips;
   A.segments = (uint32_t)P.segments;
   A.segment_steps = P.segment_steps;
@@ -279,7 +344,7 @@ int choco_train_last_hip_error(void) { return g_last_hip_error; }
 int choco_embed_workspace_bytes(const choco_embed_config* cfg, size_t* bytes_host) {
   if (!bytes_host) return CHOCO_E_INVAL;
   if (const int rc = check_embed(cfg)) return rc;
-  *bytes_host = 0;
+  *bytes_host = embed_layout(*cfg).total;
   return CHOCO_OK;
 }
 
@@ -294,14 +359,25 @@ int choco_embed_forward(const choco_embed_config* cfg, const void* tokens_dev, c
   EmbedArgs A = embed_args(c, tokens_dev);
   A.table = table_dev;
   A.rows = y_dev;
-  const int lanes_log2 = 6;
-  const dim3 grid(blocks_of(c.tokens, 256 >> lanes_log2), (uint32_t)c.n);
+  const size_t tab_size = type_bytes(c.table_type), row_size = type_bytes(c.row_type);
+  const int v = embed_width((int)(16 / std::max(tab_size, row_size)), c.dim, {{table_dev, tab_size}, {y_dev, row_size}},
+                            {{c.table_stride, tab_size}, {c.row_ld, row_size}, {c.row_stride, row_size}});
+  int lanes_log2 = 2;
+  while (lanes_log2 < 6 && ((int64_t)v << lanes_log2) < c.dim) ++lanes_log2;
+  const int64_t blocks = (c.tokens + (256 >> lanes_log2) - 1) / (256 >> lanes_log2);
+  if (!launch_fits(blocks, 256)) return CHOCO_E_UNSUPPORTED;
+  const dim3 grid((uint32_t)blocks, (uint32_t)c.n);
   with_type(c.table_type, [&](auto tab) {
     with_type(c.row_type, [&](auto row) {
-      using Tab = decltype(tab);
-      using Row = decltype(row);
-      if (c.token_type == CHOCO_I32) k_embed<int32_t, Tab, Row, 1><<<grid, 256, 0, (hipStream_t)c.stream>>>(A, lanes_log2);
-      else k_embed<int64_t, Tab, Row, 1><<<grid, 256, 0, (hipStream_t)c.stream>>>(A, lanes_log2);
+      with_vector(v, [&](auto width) {
+        using Tab = decltype(tab);
+        using Row = decltype(row);
+        constexpr int V = decltype(width)::value;
+        if constexpr (V * std::max(sizeof(Tab), sizeof(Row)) <= 16) {
+          if (c.token_type == CHOCO_I32) k_embed<int32_t, Tab, Row, V><<<grid, 256, 0, (hipStream_t)c.stream>>>(A, lanes_log2);
+          else k_embed<int64_t, Tab, Row, V><<<grid, 256, 0, (hipStream_t)c.stream>>>(A, lanes_log2);
+        }
+      });
     });
   });
   TRY_HIP(hipGetLastError());
@@ -316,23 +392,73 @@ int choco_embed_backward(const choco_embed_config* cfg, const void* tokens_dev, 
   if (!dtable_dev || (c.tokens > 0 && (!tokens_dev || !dy_dev))) return CHOCO_E_INVAL;
   if (!aligned_to(tokens_dev, c.token_type == CHOCO_I32 ? 4 : 8) || !aligned_to(dtable_dev, 4) || !aligned_to(dy_dev, type_bytes(c.row_type)))
     return CHOCO_E_INVAL;
-  if (c.vocab * c.dim >= (int64_t)1 << 38) return CHOCO_E_UNSUPPORTED;   // 2^31 workgroups of the pass that clears it
-  (void)workspace_dev;
-  (void)workspace_bytes;
+  const EmbedLayout L = embed_layout(c);
+  if (L.total > 0 && (!workspace_dev || !aligned_to(workspace_dev, 16))) return CHOCO_E_INVAL;
+  if (L.total > workspace_bytes) return CHOCO_E_NOMEM;
   EmbedArgs A = embed_args(c, tokens_dev);
   A.rows = dy_dev;
   A.dtable = dtable_dev;
+  A.accumulate = accumulate ? 1 : 0;
   const hipStream_t stream = (hipStream_t)c.stream;
-  if (!accumulate) {
-    k_embed_zero<<<dim3(blocks_of(c.vocab * c.dim, 256), (uint32_t)c.n), 256, 0, stream>>>(A);
+  const int64_t zero_blocks = accumulate ? 0 : (c.vocab * c.dim + kZeroFloats - 1) / kZeroFloats;
+  if (!launch_fits((double)zero_blocks * c.n + c.n, kSortThreads)) return CHOCO_E_UNSUPPORTED;
+  A.zero_blocks = (uint32_t)zero_blocks;
+  if (c.tokens == 0) {   // nothing but zeros
+    k_embed_count<int32_t, true><<<dim3(A.zero_blocks, (uint32_t)c.n), kChunkThreads, 0, stream>>>(A, 0);
     TRY_HIP(hipGetLastError());
+    return CHOCO_OK;
   }
-  if (c.tokens == 0) return CHOCO_OK;
-  const dim3 grid((uint32_t)c.tokens, (uint32_t)c.n);
+  char* ws = (char*)workspace_dev;
+  A.keys = (uint32_t*)(ws + L.keys);
+  A.places = (uint32_t*)(ws + L.places);
+  A.partial = (float*)(ws + L.partial);
+  A.partial_ld = L.partial_ld;
+  A.pieces = L.pieces;
+  A.digit_bits = L.digit_bits;
+  A.passes = L.passes;
+  const size_t size = type_bytes(c.row_type);
+  const int v = embed_width(size == 2 ? 8 : 4, c.dim, {{dy_dev, size}, {dtable_dev, 4}},
+                            {{c.row_ld, size}, {c.row_stride, size}, {c.table_stride, 4}});
+  A.column_chunks = (c.dim + 64 * v - 1) / (64 * v);
+  if (!launch_fits((double)A.pieces * (double)A.column_chunks, 64 * kJoinWaves) || !launch_fits((double)L.chunks + zero_blocks, kChunkThreads))
+    return CHOCO_E_UNSUPPORTED;
+  const auto order = [&](auto token) {
+    using Tok = decltype(token);
+    if (L.one) {
+      k_embed_sort<Tok><<<dim3((uint32_t)(c.n + zero_blocks * c.n)), kSortThreads, 0, stream>>>(A, c.n);
+      return;
+    }
+    A.counts = (uint32_t*)(ws + L.counts);
+    A.keys_next = (uint32_t*)(ws + L.keys_next);
+    A.places_next = (uint32_t*)(ws + L.places_next);
+    A.chunks = L.chunks;
+    const dim3 grid(L.chunks, (uint32_t)c.n), grid_and_zeros(L.chunks + A.zero_blocks, (uint32_t)c.n);
+    for (int pass = 0; pass < L.passes; ++pass) {
+      const int shift = pass * L.digit_bits;
+      if (pass == 0) {
+        k_embed_count<Tok, true><<<grid_and_zeros, kChunkThreads, 0, stream>>>(A, shift);
+        k_embed_scatter<Tok, true><<<grid, kChunkThreads, 0, stream>>>(A, shift);
+      } else {
+        k_embed_count<Tok, false><<<grid, kChunkThreads, 0, stream>>>(A, shift);
+        k_embed_scatter<Tok, false><<<grid, kChunkThreads, 0, stream>>>(A, shift);
+      }
+      std::swap(A.keys, A.keys_next);
+      std::swap(A.places, A.places_next);
+    }
+  };
+  if (c.token_type == CHOCO_I32) order(int32_t{});
+  else order(int64_t{});
+  TRY_HIP(hipGetLastError());
+  const int64_t units = A.pieces * A.column_chunks;
   with_type(c.row_type, [&](auto row) {
-    using Row = decltype(row);
-    if (c.token_type == CHOCO_I32) k_embed_sum<int32_t, Row><<<grid, 64, 0, stream>>>(A);
-    else k_embed_sum<int64_t, Row><<<grid, 64, 0, stream>>>(A);
+    with_vector(v, [&](auto width) {
+      using Row = decltype(row);
+      constexpr int V = decltype(width)::value;
+      if constexpr (V * sizeof(Row) <= 16) {
+        k_embed_sum<Row, V><<<dim3(blocks_of(units, 4), (uint32_t)c.n), 256, 0, stream>>>(A);
+        if (A.pieces > 1) k_embed_join<V><<<dim3((uint32_t)units, (uint32_t)c.n), 64 * kJoinWaves, 0, stream>>>(A);
+      }
+    });
   });
   TRY_HIP(hipGetLastError());
   return CHOCO_OK;
