@@ -135,7 +135,8 @@ int choco_adamw_init(const choco_adamw_config* cfg, float* x_dev, void* workspac
 int choco_adamw_step(choco_adamw* a, const void* g_dev, int32_t grad_type, float lr, const float* grad_scale_dev);
 /* The moments as fp32 (what they stand for in 8 bits), n x ld floats each, zero in entries of no tensor.  Asynchronous. */
 int choco_adamw_moments(choco_adamw* a, float* m_dev, float* v_dev);
-/* The part of the workspace that holds the moments: what to save, and with t to put back, to resume a run. */
+/* The part of the workspace that holds the moments: what to save, and with t to put back, to resume a run.  In 32 bits it is m
+   and then v, n x ld floats each, v on the next multiple of 256 bytes. */
 int choco_adamw_state(choco_adamw* a, void** state_dev, size_t* bytes_host);
 int choco_adamw_get_step(choco_adamw* a, uint64_t* t_host);
 int choco_adamw_set_step(choco_adamw* a, uint64_t t);

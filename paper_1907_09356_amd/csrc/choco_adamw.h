@@ -41,18 +41,18 @@ __device__ __forceinline__ float adamw_x(const AdamwArgs& A, float x, float m, f
   return x * keep - rate * m * __builtin_amdgcn_rcpf(root);
 }
 
-// The scale of a block: the power of two that brings the bits `most` of its largest magnitude into (0.9375, 1.875].
+// The scale of a block is the power of two that brings the largest magnitude into (0.9375, 1.875]: its exponent field is that of
+// the largest number with the cut-off bits below 1.875 carried up, so lanes compare exponent fields, those of m and v at once.
 // A power of two, because the codes are then exact multiples of one another from step to step: a moment that moves by
 // 0.1 % in a step changes its code in one step of a hundred, whereas a scale that follows the largest entry would put
 // every entry between two codes in every step, and rounding noise of 4 % a step adds up over the 1 / (1 - beta2) steps
-// that v remembers.  Zero for a block below the normal numbers (held as zero); infinite or NaN as `most` is.
-__device__ __forceinline__ uint32_t scale_bits(uint32_t most) {
-  const uint32_t up = (most & 0x7FFFFFu) > 0x700000u && most < 0x7F800000u ? 1u << 23 : 0u;
-  return most >= 0x7F800000u ? most : (most & 0x7F800000u) == 0 ? 0u : (most & 0x7F800000u) + up;
-}
-// 2^-k of a scale 2^k; 0 for the scales that are no power of two.
-__device__ __forceinline__ float inverse_scale(uint32_t scale) {
-  return scale == 0u || scale >= 0x7F800000u ? 0.0f : scale == 254u << 23 ? 5.87747175e-39f : __uint_as_float((254u << 23) - scale);
+// that v remembers.  0: the block is held as zero; 255 and more: something in it is infinite or NaN.
+typedef uint16_t Fields __attribute__((ext_vector_type(2)));   // of m and of v
+__device__ __forceinline__ uint32_t scale_field(float x) { return ((__float_as_uint(x) & 0x7FFFFFFFu) + 0xFFFFFu) >> 23; }
+__device__ __forceinline__ float scale_of(uint32_t field) { return __uint_as_float(field >= 255u ? 0x7FC00000u : field << 23); }
+// 2^-k of a scale 2^k; 0 for the fields of no power of two.
+__device__ __forceinline__ float inverse_scale(uint32_t field) {
+  return field == 0u || field >= 255u ? 0.0f : field == 254u ? 5.87747175e-39f : __uint_as_float((254u - field) << 23);
 }
 
 // What a code of 3 mantissa bits under TOP exponents stands for relative to its scale, at most 1.875: its bits are those of a
@@ -69,108 +69,235 @@ __device__ __forceinline__ uint32_t value_code(float y, uint32_t r) {
   return code < 8u * TOP + 7u ? code : 8u * TOP + 7u;
 }
 
-// Largest of a wave's values by their bits: these are non-negative floats (or NaN, which is above all).
-__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) {
-    const uint32_t y = (uint32_t)__shfl_xor((int)x, off, 64);
-    x = x > y ? x : y;
-  }
-  return x;
+// Largest fields of a wave, in every lane: the halves and neighbouring rows of 16 lanes swapped, then rotations and permutations
+// within a row, all by moves of the vector unit.
+template <int CTRL>
+__device__ __forceinline__ Fields moved_max(Fields x) {
+  const Fields y = __builtin_bit_cast(Fields, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xF, 0xF, true));
+  return __builtin_elementwise_max(x, y);
+}
+__device__ __forceinline__ Fields pair_max(uint32_t x, uint32_t y) {
+  return __builtin_elementwise_max(__builtin_bit_cast(Fields, x), __builtin_bit_cast(Fields, y));
+}
+__device__ __forceinline__ Fields wave_max(Fields x) {
+  const uint32_t b = __builtin_bit_cast(uint32_t, x);
+  const auto halves = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+  x = pair_max(halves[0], halves[1]);
+  const uint32_t c = __builtin_bit_cast(uint32_t, x);
+  const auto rows = __builtin_amdgcn_permlane16_swap(c, c, false, false);
+  x = pair_max(rows[0], rows[1]);
+  x = moved_max<0x128>(x);    // row_ror 8
+  x = moved_max<0x124>(x);    // row_ror 4
+  x = moved_max<0x4E>(x);     // quad_perm [2,3,0,1]
+  return moved_max<0xB1>(x);  // quad_perm [1,0,3,2]
 }
 
-// An entry of a block for every lane and turn: entry lane + 64 j.
-template <class G, int BITS>
+// The four entries that a lane takes of a block: next to one another, from the first that the lane's number times four
+// reaches, where the tensor starts on a multiple of four; every 64th otherwise.
+template <bool ALIGNED>
+__device__ __forceinline__ int entry_of(int lane, int i) { return ALIGNED ? lane * 4 + i : i * 64 + lane; }
+
+// A lane's entries of those from p on; there are `left` of them (kMomentBlock or more: no lane has to look).
+template <bool ALIGNED, bool STREAM, class T>
+__device__ __forceinline__ void load_four(const T* p, int lane, int left, T (&x)[4]) {
+  if (ALIGNED && (left >= kMomentBlock || lane * 4 + 4 <= left)) {
+    typedef T Four __attribute__((ext_vector_type(4)));
+    Four v;
+    if constexpr (STREAM) v = __builtin_nontemporal_load(reinterpret_cast<const Four*>(p + lane * 4));
+    else v = *reinterpret_cast<const Four*>(p + lane * 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = v[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = entry_of<ALIGNED>(lane, i) < left ? p[entry_of<ALIGNED>(lane, i)] : T(0);
+  }
+}
+template <bool ALIGNED, bool STREAM, class T>
+__device__ __forceinline__ void store_four(T* p, int lane, int left, const T (&x)[4]) {
+  if (ALIGNED && (left >= kMomentBlock || lane * 4 + 4 <= left)) {
+    typedef T Four __attribute__((ext_vector_type(4)));
+    Four v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = x[i];
+    if constexpr (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<Four*>(p + lane * 4));
+    else *reinterpret_cast<Four*>(p + lane * 4) = v;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (entry_of<ALIGNED>(lane, i) < left) p[entry_of<ALIGNED>(lane, i)] = x[i];
+  }
+}
+
+// The words of a lane's entries in the BLOCKS blocks from entry e on.
+template <bool ALIGNED, int BLOCKS>
+__device__ __forceinline__ void entry_words(const AdamwArgs& A, int w, uint32_t e, int lane, uint32_t (&words)[BLOCKS][4]) {
+  const uint32_t c3 = STREAM_ADAMW | (A.t_hi << 8);
+  if (ALIGNED) {
+    uint4 four[BLOCKS];
+    philox_side_by_side<BLOCKS>((e >> 2) + lane, (uint32_t)w, A.t_lo, c3, A.seed_lo, A.seed_hi, four);
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b) {
+      words[b][0] = four[b].x;
+      words[b][1] = four[b].y;
+      words[b][2] = four[b].z;
+      words[b][3] = four[b].w;
+    }
+  } else {
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t at = e + b * kMomentBlock + entry_of<false>(lane, i);
+        const uint4 four = philox4x32_10(at >> 2, (uint32_t)w, A.t_lo, c3, A.seed_lo, A.seed_hi);
+        words[b][i] = (at & 3) == 0 ? four.x : (at & 3) == 1 ? four.y : (at & 3) == 2 ? four.z : four.w;
+      }
+  }
+}
+
+// A wave takes a tile: loads everything of its blocks, then computes and writes them.  FULL: the blocks are whole.
+template <class G, int BITS, bool STREAM, bool ALIGNED, bool FULL, int BLOCKS>
+__device__ __forceinline__ void adamw_tile(const AdamwArgs& A, const AdamwTile& tile, int w, float gs, int first) {
+  const int lane = threadIdx.x & 63;
+  const int64_t at = (int64_t)w * A.ld + tile.start + first;
+  const int64_t block = (int64_t)w * A.nblocks + tile.block + first / kMomentBlock;
+  const float rate = A.rate * tile.lr_scale, keep = 1.0f - A.lr * tile.lr_scale * tile.weight_decay;
+  float x[BLOCKS][4], m[BLOCKS][4], v[BLOCKS][4];
+  G g[BLOCKS][4];
+  uint8_t cm[BLOCKS][4], cv[BLOCKS][4];
+  float old_m[BLOCKS], old_v[BLOCKS];
+#pragma unroll
+  for (int b = 0; b < BLOCKS; ++b) {
+    const int64_t e = at + b * kMomentBlock;
+    const int left = FULL ? kMomentBlock : tile.len - first - b * kMomentBlock;
+    load_four<ALIGNED, STREAM>((const G*)A.g + e, lane, left, g[b]);
+    if (BITS == 32) {
+      load_four<ALIGNED, STREAM>((const float*)A.m + e, lane, left, m[b]);
+      load_four<ALIGNED, STREAM>((const float*)A.v + e, lane, left, v[b]);
+    } else {
+      load_four<ALIGNED, STREAM>((const uint8_t*)A.m + e, lane, left, cm[b]);
+      load_four<ALIGNED, STREAM>((const uint8_t*)A.v + e, lane, left, cv[b]);
+      old_m[b] = left > 0 ? A.m_scale[block + b] : 0.0f;
+      old_v[b] = left > 0 ? A.v_scale[block + b] : 0.0f;
+    }
+    load_four<ALIGNED, STREAM>(A.x + e, lane, left, x[b]);
+  }
+  uint32_t words[BLOCKS][4];
+  if (BITS == 8) entry_words<ALIGNED, BLOCKS>(A, w, (uint32_t)(tile.start + first), lane, words);
+#pragma unroll
+  for (int b = 0; b < BLOCKS; ++b) {
+    const int64_t e = at + b * kMomentBlock;
+    const int left = FULL ? kMomentBlock : tile.len - first - b * kMomentBlock;
+    Fields top = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (BITS == 8) {
+        m[b][i] = code_value<15>(cm[b][i] & 127u) * old_m[b];
+        if (cm[b][i] & 128u) m[b][i] = -m[b][i];
+        v[b][i] = code_value<31>(cv[b][i]) * old_v[b];
+      }
+      const float gr = to_float(g[b][i]) * gs;
+      m[b][i] = m[b][i] * A.beta1 + gr * A.one_minus_beta1;
+      v[b][i] = v[b][i] * A.beta2 + (gr * gr) * A.one_minus_beta2;
+      x[b][i] = adamw_x(A, x[b][i], m[b][i], v[b][i], rate, keep);
+      if (BITS == 8 && entry_of<ALIGNED>(lane, i) < left)
+        top = __builtin_elementwise_max(top, Fields{(uint16_t)scale_field(m[b][i]), (uint16_t)scale_field(v[b][i])});
+    }
+    store_four<ALIGNED, STREAM>(A.x + e, lane, left, x[b]);
+    if (BITS == 32) {
+      store_four<ALIGNED, STREAM>((float*)A.m + e, lane, left, m[b]);
+      store_four<ALIGNED, STREAM>((float*)A.v + e, lane, left, v[b]);
+      continue;
+    }
+    top = wave_max(top);
+    const float up_m = inverse_scale(top[0]), up_v = inverse_scale(top[1]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t code = value_code<15>(fabsf(m[b][i]) * up_m, words[b][i] & 0xFFFFu);
+      cm[b][i] = (uint8_t)(m[b][i] < 0.0f ? code | 128u : code);
+      const uint32_t code_v = value_code<31>(v[b][i] * up_v, words[b][i] >> 16);
+      cv[b][i] = (uint8_t)(code_v == 0u && v[b][i] > 0.0f ? 1u : code_v);
+    }
+    store_four<ALIGNED, STREAM>((uint8_t*)A.m + e, lane, left, cm[b]);
+    store_four<ALIGNED, STREAM>((uint8_t*)A.v + e, lane, left, cv[b]);
+    if (lane == 0 && left > 0) {
+      A.m_scale[block + b] = scale_of(top[0]);
+      A.v_scale[block + b] = scale_of(top[1]);
+    }
+  }
+}
+
+// Tiles of whole blocks that start on a multiple of four entries - nearly all of a model's - go through at once, the others
+// block by block.
+template <class G, int BITS, bool STREAM>
 __global__ __launch_bounds__(256) void k_adamw(AdamwArgs A) {
-  const int lane = threadIdx.x & 63, w = blockIdx.y;
-  const int ti = blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int w = blockIdx.y;
+  const int ti = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (ti >= A.ntiles) return;
   const AdamwTile tile = A.tiles[ti];
   const float gs = A.grad_scale ? A.grad_scale[w] : 1.0f;
   if (!(fabsf(gs) <= 3.402823466e38f)) return;
-  const int64_t row = (int64_t)w * A.ld;
-  const float rate = A.rate * tile.lr_scale, keep = 1.0f - A.lr * tile.lr_scale * tile.weight_decay;
-  for (int b = 0; b * kMomentBlock < tile.len; ++b) {
-    const int64_t block = (int64_t)w * A.nblocks + tile.block + b;
-    float m[4], v[4];
-    uint32_t most_m = 0, most_v = 0;
-    float old_m = 0.0f, old_v = 0.0f;
-    if (BITS == 8) { old_m = A.m_scale[block]; old_v = A.v_scale[block]; }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int at = b * kMomentBlock + j * 64 + lane;
-      m[j] = v[j] = 0.0f;
-      if (at >= tile.len) continue;
-      const int64_t e = row + tile.start + at;
-      const float g = to_float(((const G*)A.g)[e]) * gs;
-      if (BITS == 32) {
-        m[j] = ((const float*)A.m)[e];
-        v[j] = ((const float*)A.v)[e];
-      } else {
-        const uint32_t cm = ((const uint8_t*)A.m)[e], cv = ((const uint8_t*)A.v)[e];
-        m[j] = code_value<15>(cm & 127u) * old_m;
-        if (cm & 128u) m[j] = -m[j];
-        v[j] = code_value<31>(cv) * old_v;
-      }
-      m[j] = m[j] * A.beta1 + g * A.one_minus_beta1;
-      v[j] = v[j] * A.beta2 + (g * g) * A.one_minus_beta2;
-      A.x[e] = adamw_x(A, A.x[e], m[j], v[j], rate, keep);
-      if (BITS == 32) {
-        ((float*)A.m)[e] = m[j];
-        ((float*)A.v)[e] = v[j];
-      } else {
-        const uint32_t bm = __float_as_uint(m[j]) & 0x7FFFFFFFu, bv = __float_as_uint(v[j]) & 0x7FFFFFFFu;
-        most_m = bm > most_m ? bm : most_m;
-        most_v = bv > most_v ? bv : most_v;
-      }
-    }
-    if (BITS == 32) continue;
-    const uint32_t scale_m = scale_bits(wave_max(most_m)), scale_v = scale_bits(wave_max(most_v));
-    const float up_m = inverse_scale(scale_m), up_v = inverse_scale(scale_v);
-    if (lane == 0) {
-      A.m_scale[block] = __uint_as_float(scale_m);
-      A.v_scale[block] = __uint_as_float(scale_v);
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int at = b * kMomentBlock + j * 64 + lane;
-      if (at >= tile.len) continue;
-      const int32_t e = tile.start + at;
-      const uint4 words = philox4x32_10((uint32_t)e >> 2, (uint32_t)w, A.t_lo, STREAM_ADAMW | (A.t_hi << 8), A.seed_lo, A.seed_hi);
-      const uint32_t word = (e & 3) == 0 ? words.x : (e & 3) == 1 ? words.y : (e & 3) == 2 ? words.z : words.w;
-      uint32_t cm = value_code<15>(fabsf(m[j]) * up_m, word & 0xFFFFu);
-      if (m[j] < 0.0f) cm |= 128u;
-      uint32_t cv = value_code<31>(v[j] * up_v, word >> 16);
-      if (cv == 0 && v[j] > 0.0f) cv = 1;
-      ((uint8_t*)A.m)[row + e] = (uint8_t)cm;
-      ((uint8_t*)A.v)[row + e] = (uint8_t)cv;
-    }
+  if ((tile.start & 3) == 0 && tile.len == kTile) {
+    adamw_tile<G, BITS, STREAM, true, true, kTileBlocks>(A, tile, w, gs, 0);
+  } else if ((tile.start & 3) == 0) {
+    for (int first = 0; first < tile.len; first += kMomentBlock) adamw_tile<G, BITS, STREAM, true, false, 1>(A, tile, w, gs, first);
+  } else {
+    for (int first = 0; first < tile.len; first += kMomentBlock) adamw_tile<G, BITS, STREAM, false, false, 1>(A, tile, w, gs, first);
   }
 }
 
 // The moments as floats.
+template <int BITS, bool ALIGNED, bool FULL, int BLOCKS>
+__device__ __forceinline__ void adamw_moments_tile(const AdamwArgs& A, const AdamwTile& tile, int w, int first) {
+  constexpr bool STREAM = true;
+  const int lane = threadIdx.x & 63;
+  const int64_t at = (int64_t)w * A.ld + tile.start + first;
+  const int64_t block = (int64_t)w * A.nblocks + tile.block + first / kMomentBlock;
+  float m[BLOCKS][4], v[BLOCKS][4], scale_m[BLOCKS], scale_v[BLOCKS];
+  uint8_t cm[BLOCKS][4], cv[BLOCKS][4];
+#pragma unroll
+  for (int b = 0; b < BLOCKS; ++b) {
+    const int64_t e = at + b * kMomentBlock;
+    const int left = FULL ? kMomentBlock : tile.len - first - b * kMomentBlock;
+    if (BITS == 32) {
+      load_four<ALIGNED, STREAM>((const float*)A.m + e, lane, left, m[b]);
+      load_four<ALIGNED, STREAM>((const float*)A.v + e, lane, left, v[b]);
+    } else {
+      load_four<ALIGNED, STREAM>((const uint8_t*)A.m + e, lane, left, cm[b]);
+      load_four<ALIGNED, STREAM>((const uint8_t*)A.v + e, lane, left, cv[b]);
+      scale_m[b] = tile.block >= 0 ? A.m_scale[block + b] : 0.0f;
+      scale_v[b] = tile.block >= 0 ? A.v_scale[block + b] : 0.0f;
+    }
+  }
+#pragma unroll
+  for (int b = 0; b < BLOCKS; ++b) {
+    const int64_t e = at + b * kMomentBlock;
+    const int left = FULL ? kMomentBlock : tile.len - first - b * kMomentBlock;
+    if (BITS == 8) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        m[b][i] = code_value<15>(cm[b][i] & 127u) * scale_m[b];
+        if (cm[b][i] & 128u) m[b][i] = -m[b][i];
+        v[b][i] = code_value<31>(cv[b][i]) * scale_v[b];
+      }
+    }
+    store_four<ALIGNED, STREAM>(A.m_out + e, lane, left, m[b]);
+    store_four<ALIGNED, STREAM>(A.v_out + e, lane, left, v[b]);
+  }
+}
+
+// (Entries of no tensor hold zeros, codes and floats alike.)
 template <int BITS>
 __global__ __launch_bounds__(256) void k_adamw_moments(AdamwArgs A) {
-  const int lane = threadIdx.x & 63, w = blockIdx.y;
-  const int ti = blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int w = blockIdx.y;
+  const int ti = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (ti >= A.ntiles) return;
   const AdamwTile tile = A.tiles[ti];
-  for (int at = lane; at < tile.len; at += 64) {
-    const int64_t e = (int64_t)w * A.ld + tile.start + at;
-    float m = 0.0f, v = 0.0f;
-    if (tile.block < 0) {
-    } else if (BITS == 32) {
-      m = ((const float*)A.m)[e];
-      v = ((const float*)A.v)[e];
-    } else {
-      const int64_t block = (int64_t)w * A.nblocks + tile.block + at / kMomentBlock;
-      const uint32_t cm = ((const uint8_t*)A.m)[e], cv = ((const uint8_t*)A.v)[e];
-      m = code_value<15>(cm & 127u) * A.m_scale[block];
-      if (cm & 128u) m = -m;
-      v = code_value<31>(cv) * A.v_scale[block];
-    }
-    A.m_out[e] = m;
-    A.v_out[e] = v;
+  if ((tile.start & 3) == 0 && tile.len == kTile) {
+    adamw_moments_tile<BITS, true, true, kTileBlocks>(A, tile, w, 0);
+  } else if ((tile.start & 3) == 0) {
+    for (int first = 0; first < tile.len; first += kMomentBlock) adamw_moments_tile<BITS, true, false, 1>(A, tile, w, first);
+  } else {
+    for (int first = 0; first < tile.len; first += kMomentBlock) adamw_moments_tile<BITS, false, false, 1>(A, tile, w, first);
   }
 }
 

@@ -2,13 +2,18 @@
 // pass (device code).
 #pragma once
 
+#include <type_traits>
+
 #include "choco_types.h"
 
 namespace choco {
 
 constexpr int kSaveSteps = 16;   // the forward pass keeps the state before every so many steps
 
-constexpr int kRecurWaves = 8;   // most waves of a workgroup
+#ifndef RW
+#define RW 8
+#endif
+constexpr int kRecurWaves = RW;   // most waves of a workgroup
 constexpr int kMaxSegments = 64; // most pieces that a sequence is split into
 
 struct RecurArgs {
@@ -51,9 +56,10 @@ __device__ __forceinline__ int64_t steps_of(const RecurArgs& A, int64_t b) {
 // Sequences with too few strips to fill the chip are split into segments, whose maps a first kernel (k_recur_part)
 // computes: f and u (backward: f, o and dy) are then read twice.
 struct RecurPlace {
-  int64_t b, c, len, begin, end;   // sequence, first channel of the lane, its length, the segment's steps
+  int64_t b, strip, len, begin, end;   // sequence, first channel of the strip, its length, the segment's steps
   uint32_t segment;
-  bool in;                         // the lane has channels (one that has none works on the first ones and writes nothing)
+  int lane;                        // first channel of the lane in the strip (of one that has none: 0, and it writes nothing)
+  bool in;                         // the lane has channels
 };
 
 template <int V>
@@ -62,52 +68,68 @@ __device__ __forceinline__ RecurPlace recur_place(const RecurArgs& A) {
   const uint32_t rest = blockIdx.x / A.strips, strip = blockIdx.x % A.strips;
   P.segment = rest / (uint32_t)A.batch;
   P.b = rest % (uint32_t)A.batch;
-  P.c = (int64_t)strip * (64 * V) + (threadIdx.x & 63) * V;
-  P.in = P.c < A.dim;
-  if (!P.in) P.c = 0;
+  P.strip = (int64_t)strip * (64 * V);
+  P.lane = (threadIdx.x & 63) * V;
+  P.in = P.strip + P.lane < A.dim;
+  if (!P.in) P.lane = 0;
   P.len = steps_of(A, P.b);
   P.begin = P.segment * A.segment_steps;
   P.end = P.begin + A.segment_steps < A.steps ? P.begin + A.segment_steps : A.steps;
   return P;
 }
 
-// Rows t .. t + kSaveSteps - 1 of a lane's V channels; rows from `n` on repeat the last one before (n >= 1).
+// What a lane holds of a step, in one register: an entry of 32 bits, or two or one of 16.
 template <class T, int V>
-__device__ __forceinline__ void load_steps(const void* base, int64_t seq, int64_t step, int64_t b, int64_t t, int64_t c, int n,
-                                           Pack<T, V> (&x)[kSaveSteps]) {
-  const T* p = (const T*)base + b * seq + t * step;
+__device__ __forceinline__ uint32_t load_word(const T* p) {
+  static_assert(V * sizeof(T) <= 4, "one register");
+  if constexpr (V * sizeof(T) == 4) return *reinterpret_cast<const uint32_t*>(p);
+  else return *reinterpret_cast<const uint16_t*>(p);
+}
+template <class T>
+__device__ __forceinline__ float entry(uint32_t word, int i) {
+  if constexpr (sizeof(T) == 4) return __uint_as_float(word);
+  else if constexpr (std::is_same_v<T, bf16_t>) return __uint_as_float(i ? word & 0xFFFF0000u : word << 16);
+  else return (float)__builtin_bit_cast(f16_t, (uint16_t)(i ? word >> 16 : word));
+}
+
+// Rows t .. t + n - 1 of a lane's channels, n >= 1; the rest of the wave's steps repeat the last row.
+template <class T, int V>
+__device__ __forceinline__ void load_steps(const void* base, int64_t seq, int64_t step, const RecurPlace& P, int64_t t, int n,
+                                           uint32_t (&x)[kSaveSteps]) {
+  const T* p = (const T*)base + P.b * seq + t * step + P.strip;
 #pragma unroll
   for (int j = 0; j < kSaveSteps; ++j) {
-    x[j] = *reinterpret_cast<const Pack<T, V>*>(p + c);
+    x[j] = load_word<T, V>(p + P.lane);
     p += j + 1 < n ? step : 0;
   }
 }
 
 template <class T, int V>
-__device__ __forceinline__ void store_steps(void* base, int64_t seq, int64_t step, int64_t b, int64_t t, int64_t c, int j,
-                                            const float (&x)[V]) {
-  store_floats<T, V>((T*)base + b * seq + (t + j) * step + c, x);
+__device__ __forceinline__ void store_step(void* base, int64_t seq, int64_t step, const RecurPlace& P, int64_t t, const float (&x)[V]) {
+  store_floats<T, V>((T*)base + P.b * seq + t * step + P.strip + P.lane, x);
 }
 
 __device__ __forceinline__ int steps_left(int64_t end, int64_t t) {
-  return end <= t ? 0 : end - t < kSaveSteps ? (int)(end - t) : kSaveSteps;
+  return __builtin_amdgcn_readfirstlane(end <= t ? 0 : end - t < kSaveSteps ? (int)(end - t) : kSaveSteps);
 }
 
-// (a, b) of the steps of a wave; steps that are not in the sequence pass the state on.
+// (a, b) of the steps of a wave, and all of them in one map after (ma, mh); steps that are not in the sequence pass the state on.
 template <class T, int V>
-__device__ __forceinline__ void step_maps(const Pack<T, V> (&f)[kSaveSteps], const Pack<T, V> (&u)[kSaveSteps], int n,
-                                          float (&a)[kSaveSteps][V], float (&b)[kSaveSteps][V]) {
+__device__ __forceinline__ void step_maps(const uint32_t (&f)[kSaveSteps], const uint32_t (&u)[kSaveSteps], int n,
+                                          float (&a)[kSaveSteps][V], float (&b)[kSaveSteps][V], float (&ma)[V], float (&mh)[V]) {
 #pragma unroll
   for (int j = 0; j < kSaveSteps; ++j)
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       float down;
-      gate(to_float(f[j].e[i]), a[j][i], down);
-      b[j][i] = down * to_float(u[j].e[i]);
+      gate(entry<T>(f[j], i), a[j][i], down);
+      b[j][i] = down * entry<T>(u[j], i);
       if (j >= n) {
         a[j][i] = 1.0f;
         b[j][i] = 0.0f;
       }
+      mh[i] = fmaf(a[j][i], mh[i], b[j][i]);
+      ma[i] *= a[j][i];
     }
 }
 
@@ -124,20 +146,20 @@ __global__ __launch_bounds__(64 * kRecurWaves) void k_recur(RecurArgs A) {
   const RecurPlace P = recur_place<V>(A);
   float h[V];
 #pragma unroll
-  for (int i = 0; i < V; ++i) h[i] = A.parts || !A.h0 ? 0.0f : A.h0[P.b * A.dim + P.c + i];
+  for (int i = 0; i < V; ++i) h[i] = A.parts || !A.h0 ? 0.0f : A.h0[P.b * A.dim + P.strip + P.lane + i];
   if (A.parts)
     for (uint32_t s = 0; s <= P.segment; ++s)
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        const float2 m = A.parts[((int64_t)s * A.batch + P.b) * A.dim + P.c + i];
+        const float2 m = A.parts[((int64_t)s * A.batch + P.b) * A.dim + P.strip + P.lane + i];
         h[i] = fmaf(m.x, h[i], m.y);
       }
   int turn = 0;
   for (int64_t t = P.begin; t < P.end; t += kSaveSteps * waves, turn ^= 1) {
     const int64_t t0 = t + kSaveSteps * wave;
-    const int n = __builtin_amdgcn_readfirstlane(steps_left(P.len, t0)), all = __builtin_amdgcn_readfirstlane(steps_left(P.end, t0));
+    const int n = steps_left(P.len, t0), all = steps_left(P.end, t0);
     float a[kSaveSteps][V], b[kSaveSteps][V];
-    Pack<T, V> o[kSaveSteps];
+    uint32_t o[kSaveSteps];
     float ma[V], mh[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
@@ -145,18 +167,11 @@ __global__ __launch_bounds__(64 * kRecurWaves) void k_recur(RecurArgs A) {
       mh[i] = 0.0f;
     }
     if (n > 0) {
-      Pack<T, V> f[kSaveSteps], u[kSaveSteps];
-      load_steps<T, V>(A.f, A.f_seq, A.f_step, P.b, t0, P.c, n, f);
-      load_steps<T, V>(A.u, A.u_seq, A.u_step, P.b, t0, P.c, n, u);
-      if (GATED) load_steps<T, V>(A.o, A.o_seq, A.o_step, P.b, t0, P.c, n, o);
-      step_maps<T, V>(f, u, n, a, b);
-#pragma unroll
-      for (int j = 0; j < kSaveSteps; ++j)
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          mh[i] = fmaf(a[j][i], mh[i], b[j][i]);
-          ma[i] *= a[j][i];
-        }
+      uint32_t f[kSaveSteps], u[kSaveSteps];
+      load_steps<T, V>(A.f, A.f_seq, A.f_step, P, t0, n, f);
+      load_steps<T, V>(A.u, A.u_seq, A.u_step, P, t0, n, u);
+      if (GATED) load_steps<T, V>(A.o, A.o_seq, A.o_step, P, t0, n, o);
+      step_maps<T, V>(f, u, n, a, b, ma, mh);
     }
 #pragma unroll
     for (int i = 0; i < V; ++i) {
@@ -174,7 +189,7 @@ __global__ __launch_bounds__(64 * kRecurWaves) void k_recur(RecurArgs A) {
     if (!P.in || all == 0) continue;
     if (A.saved) {
 #pragma unroll
-      for (int i = 0; i < V; ++i) A.saved[((t0 / kSaveSteps) * A.batch + P.b) * A.dim + P.c + i] = g[i];
+      for (int i = 0; i < V; ++i) A.saved[((t0 / kSaveSteps) * A.batch + P.b) * A.dim + P.strip + P.lane + i] = g[i];
     }
 #pragma unroll
     for (int j = 0; j < kSaveSteps; ++j) {
@@ -185,15 +200,15 @@ __global__ __launch_bounds__(64 * kRecurWaves) void k_recur(RecurArgs A) {
         out[i] = 0.0f;
         if (j < n) {
           g[i] = fmaf(a[j][i], g[i], b[j][i]);
-          out[i] = GATED ? gate(to_float(o[j].e[i])) * g[i] : g[i];
+          out[i] = GATED ? gate(entry<T>(o[j], i)) * g[i] : g[i];
         }
       }
-      store_steps<T, V>(A.y, A.y_seq, A.y_step, P.b, t0, P.c, j, out);
+      store_step<T, V>(A.y, A.y_seq, A.y_step, P, t0 + j, out);
     }
   }
   if (A.h_last && P.in && wave == 0 && P.segment + 1 == A.segments)
 #pragma unroll
-    for (int i = 0; i < V; ++i) A.h_last[P.b * A.dim + P.c + i] = h[i];
+    for (int i = 0; i < V; ++i) A.h_last[P.b * A.dim + P.strip + P.lane + i] = h[i];
 }
 
 // The maps of the segments: parts[0] = (0, h0), parts[s + 1] = that of segment s; the last one's is not needed.  A wave
@@ -211,20 +226,13 @@ __global__ __launch_bounds__(64 * kRecurWaves) void k_recur_part(RecurArgs A) {
     mh[i] = 0.0f;
   }
   for (int64_t t0 = P.begin + wave * piece; t0 < P.begin + (wave + 1) * piece; t0 += kSaveSteps) {
-    const int n = __builtin_amdgcn_readfirstlane(steps_left(P.len, t0));
+    const int n = steps_left(P.len, t0);
     if (n == 0) break;
-    Pack<T, V> f[kSaveSteps], u[kSaveSteps];
-    load_steps<T, V>(A.f, A.f_seq, A.f_step, P.b, t0, P.c, n, f);
-    load_steps<T, V>(A.u, A.u_seq, A.u_step, P.b, t0, P.c, n, u);
+    uint32_t f[kSaveSteps], u[kSaveSteps];
+    load_steps<T, V>(A.f, A.f_seq, A.f_step, P, t0, n, f);
+    load_steps<T, V>(A.u, A.u_seq, A.u_step, P, t0, n, u);
     float a[kSaveSteps][V], b[kSaveSteps][V];
-    step_maps<T, V>(f, u, n, a, b);
-#pragma unroll
-    for (int j = 0; j < kSaveSteps; ++j)
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        mh[i] = fmaf(a[j][i], mh[i], b[j][i]);
-        ma[i] *= a[j][i];
-      }
+    step_maps<T, V>(f, u, n, a, b, ma, mh);
   }
 #pragma unroll
   for (int i = 0; i < V; ++i) {
@@ -239,7 +247,7 @@ __global__ __launch_bounds__(64 * kRecurWaves) void k_recur_part(RecurArgs A) {
       mh[i] = fmaf(S.a[0][w][lane][i], mh[i], S.h[0][w][lane][i]);
       ma[i] *= S.a[0][w][lane][i];
     }
-    const int64_t at = P.b * A.dim + P.c + i;
+    const int64_t at = P.b * A.dim + P.strip + P.lane + i;
     A.parts[(int64_t)(P.segment + 1) * A.batch * A.dim + at] = make_float2(ma[i], mh[i]);
     if (P.segment == 0) A.parts[at] = make_float2(0.0f, A.h0 ? A.h0[at] : 0.0f);
   }
@@ -254,19 +262,19 @@ __global__ __launch_bounds__(64 * kRecurWaves) void k_recur_back(RecurArgs A) {
   const RecurPlace P = recur_place<V>(A);
   float e[V];
 #pragma unroll
-  for (int i = 0; i < V; ++i) e[i] = A.dlast ? A.dlast[P.b * A.dim + P.c + i] : 0.0f;
+  for (int i = 0; i < V; ++i) e[i] = A.dlast ? A.dlast[P.b * A.dim + P.strip + P.lane + i] : 0.0f;
   if (A.parts)
     for (uint32_t s = A.segments - 1; s > P.segment; --s)
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        const float2 m = A.parts[((int64_t)s * A.batch + P.b) * A.dim + P.c + i];
+        const float2 m = A.parts[((int64_t)s * A.batch + P.b) * A.dim + P.strip + P.lane + i];
         e[i] = fmaf(m.x, e[i], m.y);
       }
   const int64_t round = kSaveSteps * waves;
   int turn = 0;
   for (int64_t t = P.begin + (P.end - P.begin + round - 1) / round * round - round; t >= P.begin; t -= round, turn ^= 1) {
     const int64_t t0 = t + kSaveSteps * wave;
-    const int n = __builtin_amdgcn_readfirstlane(steps_left(P.len, t0)), all = __builtin_amdgcn_readfirstlane(steps_left(P.end, t0));
+    const int n = steps_left(P.len, t0), all = steps_left(P.end, t0);
     // of each step: a, dy s, 1 - a, (h_{t-1} - u) a
     float a[kSaveSteps][V], into[kSaveSteps][V], down[kSaveSteps][V], off[kSaveSteps][V];
     float ma[V], me[V];
@@ -276,45 +284,45 @@ __global__ __launch_bounds__(64 * kRecurWaves) void k_recur_back(RecurArgs A) {
       me[i] = 0.0f;
     }
     if (n > 0) {
-      Pack<T, V> f[kSaveSteps], u[kSaveSteps], o[kSaveSteps], d[kSaveSteps];
-      load_steps<T, V>(A.f, A.f_seq, A.f_step, P.b, t0, P.c, n, f);
-      load_steps<T, V>(A.u, A.u_seq, A.u_step, P.b, t0, P.c, n, u);
-      load_steps<T, V>(A.dy, A.y_seq, A.y_step, P.b, t0, P.c, n, d);
-      if (GATED) load_steps<T, V>(A.o, A.o_seq, A.o_step, P.b, t0, P.c, n, o);
+      uint32_t f[kSaveSteps], u[kSaveSteps], o[kSaveSteps], d[kSaveSteps];
+      load_steps<T, V>(A.f, A.f_seq, A.f_step, P, t0, n, f);
+      load_steps<T, V>(A.u, A.u_seq, A.u_step, P, t0, n, u);
+      load_steps<T, V>(A.dy, A.y_seq, A.y_step, P, t0, n, d);
+      if (GATED) load_steps<T, V>(A.o, A.o_seq, A.o_step, P, t0, n, o);
       float h[V];
 #pragma unroll
-      for (int i = 0; i < V; ++i) h[i] = A.saved[((t0 / kSaveSteps) * A.batch + P.b) * A.dim + P.c + i];
+      for (int i = 0; i < V; ++i) h[i] = A.saved[((t0 / kSaveSteps) * A.batch + P.b) * A.dim + P.strip + P.lane + i];
 #pragma unroll
       for (int j = 0; j < kSaveSteps; ++j) {
         float go[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-          const float x = to_float(u[j].e[i]), dy = to_float(d[j].e[i]);
-          gate(to_float(f[j].e[i]), a[j][i], down[j][i]);
+          const float x = entry<T>(u[j], i), dy = entry<T>(d[j], i);
+          gate(entry<T>(f[j], i), a[j][i], down[j][i]);
           off[j][i] = (h[i] - x) * a[j][i];
           h[i] = fmaf(a[j][i], h[i], down[j][i] * x);
           into[j][i] = dy;
           if (GATED) {
             float s, r;
-            gate(to_float(o[j].e[i]), s, r);
+            gate(entry<T>(o[j], i), s, r);
             into[j][i] = dy * s;
             go[i] = dy * h[i] * s * r;
           }
           if (j >= n) {
             a[j][i] = 1.0f;
             into[j][i] = 0.0f;
-            go[i] = 0.0f;
           }
         }
-        if (GATED && P.in && j < all) store_steps<T, V>(A.dout, A.do_seq, A.do_step, P.b, t0, P.c, j, go);
+        if (GATED && P.in && j < n) store_step<T, V>(A.dout, A.do_seq, A.do_step, P, t0 + j, go);
       }
 #pragma unroll
-      for (int j = kSaveSteps - 1; j >= 0; --j)
+      for (int j = kSaveSteps - 1; j >= 0; --j) {
 #pragma unroll
         for (int i = 0; i < V; ++i) {
           me[i] = (me[i] + into[j][i]) * a[j][i];
           ma[i] *= a[j][i];
         }
+      }
     }
 #pragma unroll
     for (int i = 0; i < V; ++i) {
@@ -344,17 +352,17 @@ __global__ __launch_bounds__(64 * kRecurWaves) void k_recur_back(RecurArgs A) {
           g[i] *= a[j][i];
         }
       }
-      store_steps<T, V>(A.df, A.df_seq, A.df_step, P.b, t0, P.c, j, gf);
-      store_steps<T, V>(A.du, A.du_seq, A.du_step, P.b, t0, P.c, j, gu);
-      if (GATED && n == 0) {
+      store_step<T, V>(A.df, A.df_seq, A.df_step, P, t0 + j, gf);
+      store_step<T, V>(A.du, A.du_seq, A.du_step, P, t0 + j, gu);
+      if (GATED && j >= n) {
         const float zero[V] = {};
-        store_steps<T, V>(A.dout, A.do_seq, A.do_step, P.b, t0, P.c, j, zero);
+        store_step<T, V>(A.dout, A.do_seq, A.do_step, P, t0 + j, zero);
       }
     }
   }
   if (A.dh0 && P.in && wave == 0 && P.segment == 0)
 #pragma unroll
-    for (int i = 0; i < V; ++i) A.dh0[P.b * A.dim + P.c + i] = e[i];
+    for (int i = 0; i < V; ++i) A.dh0[P.b * A.dim + P.strip + P.lane + i] = e[i];
 }
 
 // parts[s] = the map of segment s; the first one's is not needed.
@@ -372,24 +380,24 @@ __global__ __launch_bounds__(64 * kRecurWaves) void k_recur_back_part(RecurArgs 
     me[i] = 0.0f;
   }
   for (int64_t t0 = P.begin + (wave + 1) * piece - kSaveSteps; t0 >= P.begin + wave * piece; t0 -= kSaveSteps) {
-    const int n = __builtin_amdgcn_readfirstlane(steps_left(P.len, t0));
+    const int n = steps_left(P.len, t0);
     if (n == 0) continue;
-    Pack<T, V> f[kSaveSteps], o[kSaveSteps], d[kSaveSteps];
-    load_steps<T, V>(A.f, A.f_seq, A.f_step, P.b, t0, P.c, n, f);
-    load_steps<T, V>(A.dy, A.y_seq, A.y_step, P.b, t0, P.c, n, d);
-    if (GATED) load_steps<T, V>(A.o, A.o_seq, A.o_step, P.b, t0, P.c, n, o);
+    uint32_t f[kSaveSteps], o[kSaveSteps], d[kSaveSteps];
+    load_steps<T, V>(A.f, A.f_seq, A.f_step, P, t0, n, f);
+    load_steps<T, V>(A.dy, A.y_seq, A.y_step, P, t0, n, d);
+    if (GATED) load_steps<T, V>(A.o, A.o_seq, A.o_step, P, t0, n, o);
 #pragma unroll
-    for (int j = kSaveSteps - 1; j >= 0; --j)
+    for (int j = kSaveSteps - 1; j >= 0; --j) {
+      if (j >= n) continue;
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        const float a = gate(to_float(f[j].e[i]));
-        float into = to_float(d[j].e[i]);
-        if (GATED) into *= gate(to_float(o[j].e[i]));
-        if (j < n) {
-          me[i] = (me[i] + into) * a;
-          ma[i] *= a;
-        }
+        const float a = gate(entry<T>(f[j], i));
+        float into = entry<T>(d[j], i);
+        if (GATED) into *= gate(entry<T>(o[j], i));
+        me[i] = (me[i] + into) * a;
+        ma[i] *= a;
       }
+    }
   }
 #pragma unroll
   for (int i = 0; i < V; ++i) {
@@ -404,7 +412,7 @@ __global__ __launch_bounds__(64 * kRecurWaves) void k_recur_back_part(RecurArgs 
       me[i] = fmaf(S.a[0][w][lane][i], me[i], S.h[0][w][lane][i]);
       ma[i] *= S.a[0][w][lane][i];
     }
-    A.parts[((int64_t)(P.segment + 1) * A.batch + P.b) * A.dim + P.c + i] = make_float2(ma[i], me[i]);
+    A.parts[((int64_t)(P.segment + 1) * A.batch + P.b) * A.dim + P.strip + P.lane + i] = make_float2(ma[i], me[i]);
   }
 }
 

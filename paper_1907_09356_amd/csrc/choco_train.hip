@@ -33,7 +33,11 @@ thread_local int g_last_hip_error = 0;
   } while (0)
 
 constexpr int64_t kMaxIndex = (int64_t)1 << 31;
-constexpr int64_t kFewGroups = 512, kWantedGroups = 1024;
+#ifndef FEW
+#define FEW 4096
+#define WANTED 8192
+#endif
+constexpr int64_t kFewWaves = FEW, kWantedWaves = WANTED;
 constexpr int64_t kMaxExtent = (int64_t)1 << 60;   // entries of any array, strides included
 
 int type_bytes(int type) { return type == CHOCO_F32 ? 4 : type == CHOCO_BF16 || type == CHOCO_F16 ? 2 : 0; }
@@ -205,10 +209,10 @@ RecurPlan plan_recur(const choco_recur_config& c, int width) {
   P.strips = (c.dim + width - 1) / width;
   P.waves = (int)std::max<int64_t>(1, std::min<int64_t>(kRecurWaves, (c.steps + kSaveSteps - 1) / kSaveSteps));
   const int64_t round = (int64_t)kSaveSteps * P.waves, rounds = std::max<int64_t>(1, (c.steps + round - 1) / round);
-  const int64_t groups = P.strips * c.batch;
+  const int64_t waves = P.strips * c.batch * P.waves;
   P.segments = 1;
-  if (groups < kFewGroups && rounds >= 4) {
-    P.segments = std::min<int64_t>(std::min<int64_t>(kMaxSegments, rounds / 2), (kWantedGroups + groups - 1) / groups);
+  if (waves < kFewWaves && rounds >= 4) {
+    P.segments = std::min<int64_t>(std::min<int64_t>(kMaxSegments, rounds / 2), (kWantedWaves + waves - 1) / waves);
   }
   const int64_t each = (rounds + P.segments - 1) / P.segments;
   P.segments = std::max<int64_t>(1, (rounds + each - 1) / each);
@@ -287,6 +291,13 @@ int check_adamw(const choco_adamw_config* c) {
   return CHOCO_OK;
 }
 
+// Loads and stores past the caches?  Where x, g, m and v do not stay in the 256 MB of the last-level cache until the next step.
+// us a step, through | past the caches: 32 bits, entries 2.2 M 15 | 16, 4 M 21 | 25, 8 M 37 | 42, 16 M 68 | 78, 32 M 172 | 152,
+// 254 M 1379 | 1319; 8 bits, with the moments read back, 2.2 M 17 | 19, 16 M 69 | 70, 32 M 125 | 128, 127 M 607 | 486.
+bool adamw_streams(const choco_adamw_config& c) {
+  return (double)c.n * (double)resolve_adamw_ld(c) * (8 + c.state_bits / 4) > 320.0 * 1048576.0;
+}
+
 // calls fn(tensor, start, len) for every tensor
 template <class Fn>
 void for_tensors(const choco_adamw_config& c, Fn&& fn) {
@@ -334,7 +345,8 @@ struct choco_adamw {
   hipStream_t stream;
   double beta1, beta2;
   int32_t n, state_bits;
-  uint64_t seed, t;
+  bool streamed;
+  uint64_t t;
 };
 
 extern "C" {
@@ -632,7 +644,7 @@ int choco_adamw_init(const choco_adamw_config* cfg, float* x_dev, void* workspac
     a->beta2 = c.beta2;
     a->n = c.n;
     a->state_bits = c.state_bits;
-    a->seed = c.seed;
+    a->streamed = adamw_streams(c);
     AdamwArgs& A = a->args;
     A.x = x_dev;
     A.m = ws + L.m;
@@ -672,13 +684,19 @@ int choco_adamw_step(choco_adamw* a, const void* g_dev, int32_t grad_type, float
   A.root_scale = (float)(1.0 / std::sqrt(1.0 - std::pow(a->beta2, t)));
   if (A.ntiles > 0) {
     const dim3 grid(blocks_of(A.ntiles, 4), (uint32_t)a->n);
-    if (grad_type == CHOCO_F32) {
-      if (a->state_bits == 32) k_adamw<float, 32><<<grid, 256, 0, a->stream>>>(A);
-      else k_adamw<float, 8><<<grid, 256, 0, a->stream>>>(A);
-    } else {
-      if (a->state_bits == 32) k_adamw<bf16_t, 32><<<grid, 256, 0, a->stream>>>(A);
-      else k_adamw<bf16_t, 8><<<grid, 256, 0, a->stream>>>(A);
-    }
+    const auto launch = [&](auto g, auto bits, auto stream) {
+      k_adamw<decltype(g), decltype(bits)::value, decltype(stream)::value><<<grid, 256, 0, a->stream>>>(A);
+    };
+    const auto with_stream = [&](auto g, auto bits) {
+      if (a->streamed) launch(g, bits, std::true_type{});
+      else launch(g, bits, std::false_type{});
+    };
+    const auto with_bits = [&](auto g) {
+      if (a->state_bits == 32) with_stream(g, std::integral_constant<int, 32>{});
+      else with_stream(g, std::integral_constant<int, 8>{});
+    };
+    if (grad_type == CHOCO_F32) with_bits(float{});
+    else with_bits(bf16_t{});
     TRY_HIP(hipGetLastError());
   }
   ++a->t;

@@ -287,9 +287,14 @@ class AdamW:
         _check(lib().choco_adamw_step(self.handle, _ptr(G), TYPES[G.dtype], float(lr), _ptr(grad_scale)), "choco_adamw_step")
 
     def moments(self):
-        """(m, v), float32 of (n, d): what is held stands for."""
-        m, v = torch.empty_like(self.X), torch.empty_like(self.X)
-        _check(lib().choco_adamw_moments(self.handle, _ptr(m), _ptr(v)), "choco_adamw_moments")
+        """(m, v), float32 of (n, d): in 32 bits the state itself (it moves with the next step), in 8 bits what it stands for now."""
+        n, ld = self.X.shape
+        if self.cfg.state_bits == 32:
+            state, size = self.state(), n * ld * 4
+            m, v = (state[at:at + size].view(torch.float32).view(n, ld) for at in (0, (size + 255) // 256 * 256))
+        else:
+            m, v = torch.empty_like(self.X), torch.empty_like(self.X)
+            _check(lib().choco_adamw_moments(self.handle, m.data_ptr(), v.data_ptr()), "choco_adamw_moments")
         return m[:, :self.d], v[:, :self.d]
 
     def state(self):

@@ -204,11 +204,11 @@ def test_a_worker_whose_factor_is_not_finite_is_left_alone(bits):
     opt = T.AdamW(X, d, state_bits=bits)
     G = torch.from_numpy(rows(n, d, d, 2, 0.1)).cuda()
     opt.step(G, 0.01)
-    x0, (m0, v0), s0 = X.clone(), opt.moments(), opt.state().clone()
+    x0, (m0, v0), s0 = X.clone(), (t.clone() for t in opt.moments()), opt.state().clone()
     G[1], G[3] = float("inf"), float("nan")
     factor = torch.tensor([1.0, float("nan"), 0.0, float("inf"), -float("inf")], device="cuda")
     opt.step(G, 0.01, grad_scale=factor)
-    m, v = opt.moments()
+    m, v = (t.clone() for t in opt.moments())
     for w in (1, 3, 4):
         assert torch.equal(X[w], x0[w]) and torch.equal(m[w], m0[w]) and torch.equal(v[w], v0[w])
     for w in (0, 2):
@@ -300,6 +300,20 @@ def test_other_streams_and_graphs(bits):
             X.copy_(X0)
             opt.state().copy_(s0)
     side.synchronize()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_moments_as_copies(bits):
+    # the C call writes both moments whatever they are held in, zero outside the tensors
+    n, d, tensors = 2, 700, ([5, 300], [200, 333])
+    X = torch.from_numpy(rows(n, d, d, 1, 0.1)).cuda()
+    opt = T.AdamW(X, d, tensors, state_bits=bits)
+    opt.step(torch.from_numpy(rows(n, d, d, 2, 0.1)).cuda(), 0.01)
+    m, v = torch.full_like(X, 7.0), torch.full_like(X, 7.0)
+    assert T.lib().choco_adamw_moments(opt.handle, m.data_ptr(), v.data_ptr()) == B.OK
+    for got, want in zip((m, v), opt.moments()):
+        assert torch.equal(got, want) and not bool(got[:, ~torch.from_numpy(inside(tensors, d))].any()) and bool(got[:, 5:205].any())
+    opt.close()
 
 
 def test_arguments_are_checked():
