@@ -20,20 +20,22 @@ struct EmbedArgs {
   float* partial;                    // [workers][pieces][2][partial_ld]
   int64_t partial_ld, pieces, column_chunks;
   uint32_t chunks, zero_blocks;      // zero_blocks: per worker, of kZeroFloats each
-  int digit_bits, passes, accumulate;
+  int digit_bits, passes;
 };
 
 constexpr int kSortThreads = 1024;                     // a workgroup that orders all of a worker's tokens in LDS ...
 constexpr int kSortRounds = 8;
 constexpr int kSortOne = kSortThreads * kSortRounds;   // ... of which there are no more than this
 constexpr int kSortDigit = 9;                          // bits of the key in one pass, at most
-constexpr int kChunkThreads = 256;                     // otherwise: a workgroup for each so many tokens
-constexpr int kChunkRounds = 16;
-constexpr int kChunkTokens = kChunkThreads * kChunkRounds;
+constexpr int kChunkThreads = 256;                     // otherwise: a workgroup for each so many tokens ...
+constexpr int kShortRounds = 4, kLongRounds = 16;      // ... times this
+constexpr int64_t kLongLists = 1 << 17;                // (kLongRounds from so many tokens on)
 constexpr int kChunkDigit = 10;
-constexpr int kPiece = 32;                             // ordered tokens that a wave adds up
+constexpr int kPiece = 32;                             // ordered tokens that a wave adds up ...
+constexpr int kAhead = 8;                              // ... asking for so many rows at once
 constexpr int kZeroFloats = 1 << 16;                   // floats that a workgroup clears
-constexpr int kJoinWaves = 8;
+constexpr int kJoinWaves = 4;
+constexpr int64_t kJoinAlone = 16;                     // partial sums that a wave adds up by itself
 
 // A token, or -1 for one outside the table.
 template <class Tok>
@@ -104,10 +106,11 @@ __device__ __forceinline__ uint32_t key_at(const EmbedArgs& A, int worker, int64
 // counters in LDS, starts at zero and ends as the digits' numbers.  Lanes of one digit find each other by a ballot for each of its bits.
 template <int ROUNDS>
 __device__ __forceinline__ void rank_digits(volatile uint32_t* count, const uint32_t (&key)[ROUNDS], const bool (&there)[ROUNDS],
-                                            int shift, int bits, uint32_t (&rank)[ROUNDS]) {
+                                            int rounds, int shift, int bits, uint32_t (&rank)[ROUNDS]) {
   const uint64_t before = ((uint64_t)1 << (threadIdx.x & 63)) - 1;
 #pragma unroll
   for (int j = 0; j < ROUNDS; ++j) {
+    if (j >= rounds) break;
     const uint32_t digit = (key[j] >> shift) & ((1u << bits) - 1u);
     uint64_t same = __ballot(there[j]);
     for (int b = 0; b < bits; ++b) {
@@ -141,39 +144,46 @@ __device__ __forceinline__ uint32_t sum_before(uint32_t x, uint32_t* waves) {
   return base + sum - x;
 }
 
+inline size_t sort_lds(int64_t tokens, int digit_bits) {
+  const size_t rounds = (size_t)((tokens + kSortThreads - 1) / kSortThreads), waves = kSortThreads / 64;
+  return (2 * rounds * kSortThreads + waves + ((1 + waves) << digit_bits)) * sizeof(uint32_t);
+}
+
 // All of a worker's tokens (no more than kSortOne) in order, in LDS.  Workgroups from the n-th on clear the gradient.
 template <class Tok>
 __global__ __launch_bounds__(kSortThreads) void k_embed_sort(EmbedArgs A, int workers) {
-  constexpr int kWaves = kSortThreads / 64, kBins = 1 << kSortDigit;
-  __shared__ uint32_t count[kWaves][kBins], base[kBins], sums[kWaves];
-  __shared__ uint32_t keys[kSortOne], places[kSortOne];
+  constexpr int kWaves = kSortThreads / 64;
+  extern __shared__ uint32_t lds[];     // as much as sort_lds says
   if ((int)blockIdx.x >= workers) {
     const uint32_t z = blockIdx.x - workers;
     zero_part(A, z / A.zero_blocks, z % A.zero_blocks);
     return;
   }
   const int w = blockIdx.x, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, total = (int)A.ntokens;
+  const int rounds = (total + kSortThreads - 1) / kSortThreads;
+  const uint32_t bins = 1u << A.digit_bits;
+  uint32_t *keys = lds, *places = keys + rounds * kSortThreads, *base = places + rounds * kSortThreads, *sums = base + bins,
+           *counts = sums + kWaves, *count = counts + wave * bins;
   uint32_t key[kSortRounds], place[kSortRounds], rank[kSortRounds];
   bool there[kSortRounds];
 #pragma unroll
   for (int j = 0; j < kSortRounds; ++j) {
-    const int r = (wave * kSortRounds + j) * 64 + lane;
-    there[j] = r < total;
+    const int r = (wave * rounds + j) * 64 + lane;
+    there[j] = j < rounds && r < total;
     key[j] = there[j] ? key_at<Tok>(A, w, r) : 0u;
     place[j] = (uint32_t)r;
   }
-  const uint32_t bins = 1u << A.digit_bits;
   for (int pass = 0; pass < A.passes; ++pass) {
     const int shift = pass * A.digit_bits;
-    for (uint32_t d = lane; d < bins; d += 64) count[wave][d] = 0;
-    rank_digits<kSortRounds>(count[wave], key, there, shift, A.digit_bits, rank);
+    for (uint32_t d = lane; d < bins; d += 64) count[d] = 0;
+    rank_digits<kSortRounds>(count, key, there, rounds, shift, A.digit_bits, rank);
     __syncthreads();
     // counters of a wave -> tokens of that digit in the waves before it; base -> tokens of lower digits
     uint32_t sum = 0;
     if (threadIdx.x < bins)
       for (int v = 0; v < kWaves; ++v) {
-        const uint32_t c = count[v][threadIdx.x];
-        count[v][threadIdx.x] = sum;
+        const uint32_t c = counts[v * bins + threadIdx.x];
+        counts[v * bins + threadIdx.x] = sum;
         sum += c;
       }
     const uint32_t lower = sum_before<kSortThreads>(sum, sums);
@@ -182,14 +192,14 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort(EmbedArgs A, int wo
 #pragma unroll
     for (int j = 0; j < kSortRounds; ++j)
       if (there[j]) {
-        const uint32_t digit = (key[j] >> shift) & (bins - 1u), at = base[digit] + count[wave][digit] + rank[j];
+        const uint32_t digit = (key[j] >> shift) & (bins - 1u), at = base[digit] + count[digit] + rank[j];
         keys[at] = key[j];
         places[at] = place[j];
       }
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < kSortRounds; ++j) {
-      const int r = (wave * kSortRounds + j) * 64 + lane;
+      const int r = (wave * rounds + j) * 64 + lane;
       if (there[j]) {
         key[j] = keys[r];
         place[j] = places[r];
@@ -199,7 +209,7 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort(EmbedArgs A, int wo
   }
 #pragma unroll
   for (int j = 0; j < kSortRounds; ++j) {
-    const int r = (wave * kSortRounds + j) * 64 + lane;
+    const int r = (wave * rounds + j) * 64 + lane;
     if (there[j]) {
       A.keys[(int64_t)w * A.ntokens + r] = key[j];
       A.places[(int64_t)w * A.ntokens + r] = place[j];
@@ -209,7 +219,7 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort(EmbedArgs A, int wo
 
 // One pass over longer lists, first half: how many tokens of a chunk hold each digit.  Workgroups from the last chunk's on clear
 // the gradient.  The first pass reads the tokens, later ones what the one before wrote.
-template <class Tok, bool FIRST>
+template <class Tok, bool FIRST, int ROUNDS>
 __global__ __launch_bounds__(kChunkThreads) void k_embed_count(EmbedArgs A, int shift) {
   __shared__ uint32_t count[1 << kChunkDigit];
   const int w = blockIdx.y;
@@ -221,8 +231,8 @@ __global__ __launch_bounds__(kChunkThreads) void k_embed_count(EmbedArgs A, int 
   for (uint32_t d = threadIdx.x; d < bins; d += kChunkThreads) count[d] = 0;
   __syncthreads();
 #pragma unroll
-  for (int j = 0; j < kChunkRounds; ++j) {
-    const int64_t r = (int64_t)blockIdx.x * kChunkTokens + j * kChunkThreads + threadIdx.x;
+  for (int j = 0; j < ROUNDS; ++j) {
+    const int64_t r = ((int64_t)blockIdx.x * ROUNDS + j) * kChunkThreads + threadIdx.x;
     if (r < A.ntokens) {
       const uint32_t key = FIRST ? key_at<Tok>(A, w, r) : A.keys[(int64_t)w * A.ntokens + r];
       atomicAdd(&count[(key >> shift) & (bins - 1u)], 1u);
@@ -233,57 +243,78 @@ __global__ __launch_bounds__(kChunkThreads) void k_embed_count(EmbedArgs A, int 
   for (uint32_t d = threadIdx.x; d < bins; d += kChunkThreads) out[d] = count[d];
 }
 
-// ... second half: the chunk's tokens to their places of the pass.
-template <class Tok, bool FIRST>
+// ... second half: the tokens of a chunk to their places.  Each workgroup adds up the counts of all chunks for itself, four digits a
+// thread and eight chunks at once, where the threads are more than a quarter of the digits groups of them a share of the chunks.
+template <class Tok, bool FIRST, int ROUNDS>
 __global__ __launch_bounds__(kChunkThreads) void k_embed_scatter(EmbedArgs A, int shift) {
-  constexpr int kWaves = kChunkThreads / 64, kBins = 1 << kChunkDigit, kEach = kBins / kChunkThreads;
+  constexpr int kWaves = kChunkThreads / 64, kBins = 1 << kChunkDigit, kAtOnce = 8;
+  static_assert(kBins == 4 * kChunkThreads, "four digits a thread");
   __shared__ uint32_t count[kWaves][kBins], sums[kWaves];
+  __shared__ uint4 all[kChunkThreads], before[kChunkThreads];
   const int w = blockIdx.y, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const uint32_t bins = 1u << A.digit_bits, chunk = blockIdx.x;
+  const uint32_t bins = 1u << A.digit_bits, chunk = blockIdx.x, quads = bins / 4;
   const int64_t row = (int64_t)w * A.ntokens;
-  uint32_t key[kChunkRounds], place[kChunkRounds], rank[kChunkRounds];
-  bool there[kChunkRounds];
+  uint32_t key[ROUNDS], place[ROUNDS], rank[ROUNDS];
+  bool there[ROUNDS];
 #pragma unroll
-  for (int j = 0; j < kChunkRounds; ++j) {
-    const int64_t r = (int64_t)chunk * kChunkTokens + (wave * kChunkRounds + j) * 64 + lane;
+  for (int j = 0; j < ROUNDS; ++j) {
+    const int64_t r = (int64_t)chunk * (ROUNDS * kChunkThreads) + (wave * ROUNDS + j) * 64 + lane;
     there[j] = r < A.ntokens;
     key[j] = !there[j] ? 0u : FIRST ? key_at<Tok>(A, w, r) : A.keys[row + r];
     place[j] = FIRST ? (uint32_t)r : there[j] ? A.places[row + r] : 0u;
   }
+  const uint32_t group = threadIdx.x / quads, groups = kChunkThreads / quads;
+  const uint4* counts = reinterpret_cast<const uint4*>(A.counts + (int64_t)w * A.chunks * bins) + threadIdx.x % quads;
+  uint4 sum_all = make_uint4(0, 0, 0, 0), sum_earlier = sum_all;
+  for (uint32_t c = group; c < A.chunks; c += kAtOnce * groups) {
+    uint4 x[kAtOnce];
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const uint32_t from = c + k * groups;
+      x[k] = counts[(int64_t)(from < A.chunks ? from : A.chunks - 1) * quads];
+    }
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const uint32_t from = c + k * groups;
+      const uint32_t mask = from < A.chunks ? 0xFFFFFFFFu : 0u, mask_before = from < chunk ? 0xFFFFFFFFu : 0u;
+      sum_all.x += x[k].x & mask;
+      sum_all.y += x[k].y & mask;
+      sum_all.z += x[k].z & mask;
+      sum_all.w += x[k].w & mask;
+      sum_earlier.x += x[k].x & mask_before;
+      sum_earlier.y += x[k].y & mask_before;
+      sum_earlier.z += x[k].z & mask_before;
+      sum_earlier.w += x[k].w & mask_before;
+    }
+  }
+  all[threadIdx.x] = sum_all;
+  before[threadIdx.x] = sum_earlier;
   for (uint32_t d = lane; d < bins; d += 64) count[wave][d] = 0;
-  rank_digits<kChunkRounds>(count[wave], key, there, shift, A.digit_bits, rank);
-  // of a thread's digits (next to one another): tokens in all chunks, and in those before this one
-  const uint32_t* counts = A.counts + (int64_t)w * A.chunks * bins;
-  const uint32_t each = bins >= (uint32_t)kChunkThreads ? bins / kChunkThreads : 1u;
-  uint32_t all[kEach] = {}, before[kEach] = {};
-  if (threadIdx.x * each < bins)
-    for (uint32_t c = 0; c < A.chunks; ++c)
+  rank_digits<ROUNDS>(count[wave], key, there, ROUNDS, shift, A.digit_bits, rank);
+  __syncthreads();
+  uint32_t mine[4] = {}, earlier[4] = {};     // of digits 4 t ... 4 t + 3
+  if (threadIdx.x < quads)
+    for (uint32_t g = 0; g < groups; ++g) {
+      const uint4 a = all[g * quads + threadIdx.x], b = before[g * quads + threadIdx.x];
+      mine[0] += a.x, mine[1] += a.y, mine[2] += a.z, mine[3] += a.w;
+      earlier[0] += b.x, earlier[1] += b.y, earlier[2] += b.z, earlier[3] += b.w;
+    }
+  uint32_t lower = sum_before<kChunkThreads>(mine[0] + mine[1] + mine[2] + mine[3], sums);
+  if (threadIdx.x < quads)
 #pragma unroll
-      for (int i = 0; i < kEach; ++i)
-        if ((uint32_t)i < each) {
-          const uint32_t x = counts[(int64_t)c * bins + threadIdx.x * each + i];
-          all[i] += x;
-          before[i] += c < chunk ? x : 0u;
-        }
-  uint32_t sum = 0;
+    for (int i = 0; i < 4; ++i) {
+      uint32_t at = lower + earlier[i];
+      lower += mine[i];
 #pragma unroll
-  for (int i = 0; i < kEach; ++i) sum += all[i];
-  uint32_t lower = sum_before<kChunkThreads>(sum, sums);   // (its barriers also close the ranking)
-  if (threadIdx.x * each < bins)
-#pragma unroll
-    for (int i = 0; i < kEach; ++i)
-      if ((uint32_t)i < each) {
-        uint32_t at = lower + before[i];
-        lower += all[i];
-        for (int v = 0; v < kWaves; ++v) {
-          const uint32_t c = count[v][threadIdx.x * each + i];
-          count[v][threadIdx.x * each + i] = at;
-          at += c;
-        }
+      for (int v = 0; v < kWaves; ++v) {
+        const uint32_t c = count[v][threadIdx.x * 4 + i];
+        count[v][threadIdx.x * 4 + i] = at;
+        at += c;
       }
+    }
   __syncthreads();
 #pragma unroll
-  for (int j = 0; j < kChunkRounds; ++j)
+  for (int j = 0; j < ROUNDS; ++j)
     if (there[j]) {
       const int64_t at = row + count[wave][(key[j] >> shift) & (bins - 1u)] + rank[j];
       A.keys_next[at] = key[j];
@@ -313,25 +344,21 @@ __device__ __forceinline__ void store_sums(float* p, const float (&x)[V]) {
     *reinterpret_cast<Pack<float, S>*>(p + i) = v;
   }
 }
-// scale * sum to (or onto) the gradient.
-template <int V>
-__device__ __forceinline__ void put_sums(const EmbedArgs& A, int w, uint32_t token, int64_t c, const float (&sum)[V]) {
-  float* p = A.dtable + (int64_t)w * A.table_stride + (int64_t)token * A.dim + c;
+__device__ __forceinline__ float* sums_of(const EmbedArgs& A, int w, uint32_t token, int64_t c) {
+  return A.dtable + (int64_t)w * A.table_stride + (int64_t)token * A.dim + c;
+}
+// scale * sum to (ADD: onto `old`, what is there) the gradient.
+template <bool ADD, int V>
+__device__ __forceinline__ void put_sums(const EmbedArgs& A, float* p, const float (&sum)[V], const float (&old)[V]) {
   float x[V];
 #pragma unroll
-  for (int i = 0; i < V; ++i) x[i] = sum[i] * A.scale;
-  if (A.accumulate) {
-    float old[V];
-    load_sums<V>(p, old);
-#pragma unroll
-    for (int i = 0; i < V; ++i) x[i] += old[i];
-  }
+  for (int i = 0; i < V; ++i) x[i] = ADD ? sum[i] * A.scale + old[i] : sum[i] * A.scale;
   store_sums<V>(p, x);
 }
 
 // A wave adds up the rows of a piece, for 64 * V columns.  Partial sums: slot 0 of a piece, its first token, where that is also the
 // last of the piece before; slot 1, its last token, where that goes on in the next piece (and is not in slot 0).
-template <class Row, int V>
+template <class Row, int V, bool ADD>
 __global__ __launch_bounds__(256) void k_embed_sum(EmbedArgs A) {
   const int lane = threadIdx.x & 63, w = blockIdx.y;
   const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -340,109 +367,134 @@ __global__ __launch_bounds__(256) void k_embed_sum(EmbedArgs A) {
   const uint32_t* keys = A.keys + (int64_t)w * A.ntokens;
   const int64_t first = piece * kPiece;
   const int count = __builtin_amdgcn_readfirstlane((int)(A.ntokens - first < kPiece ? A.ntokens - first : kPiece));
-  // lane l: the l-th token of the piece; lanes kPiece and kPiece + 1: the tokens around it
+  // lane l: the (l - 1)-th token of the piece; lanes 0 and count + 1: those around it
   const uint32_t none = 0xFFFFFFFFu, vocab = (uint32_t)A.vocab;
-  uint32_t key = none, place = 0;
-  if (lane < count) {
-    key = keys[first + lane];
-    place = A.places[(int64_t)w * A.ntokens + first + lane];
-  } else if (lane == kPiece && first > 0) {
-    key = keys[first - 1];
-  } else if (lane == kPiece + 1 && first + count < A.ntokens) {
-    key = keys[first + count];
-  }
-  const uint32_t left = (uint32_t)__builtin_amdgcn_readlane((int)key, kPiece), right = (uint32_t)__builtin_amdgcn_readlane((int)key, kPiece + 1);
+  const int64_t r = first + lane - 1;
+  const uint32_t key = lane <= count + 1 && r >= 0 && r < A.ntokens ? keys[r] : none;
+  const uint32_t place = lane >= 1 && lane <= count ? A.places[(int64_t)w * A.ntokens + r] : 0u;
+  const uint32_t after = (uint32_t)__shfl_down((int)key, 1, 64), ahead = (uint32_t)__shfl_up((int)key, 1, 64);
+  // tokens after which another one begins (or the piece ends); those, of these, whose sum is complete
+  const uint64_t ends = __ballot(lane >= 1 && lane <= count && (key != after || lane == count));
+  const uint64_t starts = __ballot(lane >= 1 && lane <= count && key != ahead);
+  const int here = __builtin_amdgcn_readfirstlane(__popcll(__ballot(lane >= 1 && lane <= count && key != vocab)));   // in the table
+  if (here == 0) return;
   const bool in = c < A.dim;
-  const Row* rows = (const Row*)A.rows + (int64_t)w * A.row_stride + (in ? c : 0);
-  float* partial = A.partial + ((int64_t)w * A.pieces + piece) * 2 * A.partial_ld + c;
+  const int64_t column = in ? c : 0;
+  const Row* rows = (const Row*)A.rows + (int64_t)w * A.row_stride + column;
+  float* partial = A.partial + ((int64_t)w * A.pieces + piece) * 2 * A.partial_ld + column;
+  const uint32_t right = (uint32_t)__builtin_amdgcn_readlane((int)key, count + 1);
   float sum[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) sum[i] = 0.0f;
-  uint32_t begun = (uint32_t)__builtin_amdgcn_readlane((int)key, 0);   // the token that `sum` is of
-  bool inside = begun != left;                                         // ... and whether it began in this piece
-  constexpr int kAhead = 8;
-  for (int s = 0; s < count; s += kAhead) {
+  bool inside = starts >> 1 & 1;     // the token that `sum` is of began in this piece
+  for (int s = 0; s < here; s += kAhead) {
     Pack<Row, V> x[kAhead];
+    float old[kAhead][V];
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
-      const int at = s + j < count ? s + j : count - 1;
-      const int64_t r = (uint32_t)__builtin_amdgcn_readlane((int)place, at);
-      x[j] = *reinterpret_cast<const Pack<Row, V>*>(rows + r * A.row_ld);
+      const int at = (s + j < here ? s + j : here - 1) + 1;
+      const int64_t p = (uint32_t)__builtin_amdgcn_readlane((int)place, at);
+      x[j] = *reinterpret_cast<const Pack<Row, V>*>(rows + p * A.row_ld);
+      if (ADD && (ends >> at & 1)) load_sums<V>(sums_of(A, w, (uint32_t)__builtin_amdgcn_readlane((int)key, at), column), old[j]);
     }
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
-      if (s + j >= count) break;
-      const uint32_t k = (uint32_t)__builtin_amdgcn_readlane((int)key, s + j);
-      if (k != begun) {
-        if (in && begun != vocab) {
-          if (inside) put_sums<V>(A, w, begun, c, sum);
-          else store_sums<V>(partial, sum);
-        }
-        begun = k;
-        inside = true;
-#pragma unroll
-        for (int i = 0; i < V; ++i) sum[i] = 0.0f;
-      }
+      if (s + j >= here) break;
+      const int at = s + j + 1;
 #pragma unroll
       for (int i = 0; i < V; ++i) sum[i] += to_float(x[j].e[i]);
+      if (!(ends >> at & 1)) continue;
+      const uint32_t token = (uint32_t)__builtin_amdgcn_readlane((int)key, at);
+      const bool goes_on = at == count && token == right;
+      if (in) {
+        if (inside && !goes_on) put_sums<ADD, V>(A, sums_of(A, w, token, column), sum, old[j]);
+        else store_sums<V>(inside ? partial + A.partial_ld : partial, sum);
+      }
+      inside = true;
+#pragma unroll
+      for (int i = 0; i < V; ++i) sum[i] = 0.0f;
     }
-    if (begun == vocab) return;   // outside the table, and so are all that follow
   }
-  if (!in) return;
-  if (inside && begun != right) put_sums<V>(A, w, begun, c, sum);
-  else store_sums<V>(inside ? partial + A.partial_ld : partial, sum);
 }
 
-// Adds up the partial sums of a token that begins in `piece` and goes on in the next one: a workgroup for 64 * V columns, each wave
-// a share of the pieces.
+// The sum of V columns of partial sums (slot 0) from piece `from` to before `to`, onto `sum`.
 template <int V>
-__global__ __launch_bounds__(64 * kJoinWaves) void k_embed_join(EmbedArgs A) {
-  __shared__ float sums[kJoinWaves][64][V];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, w = blockIdx.y;
-  const int64_t piece = blockIdx.x / A.column_chunks, c = (blockIdx.x % A.column_chunks * 64 + lane) * V;
-  const uint32_t* keys = A.keys + (int64_t)w * A.ntokens;
-  const int64_t next = (piece + 1) * kPiece;
-  if (next >= A.ntokens) return;
-  const uint32_t token = keys[next - 1];
-  if (token != keys[next] || token == (uint32_t)A.vocab) return;
-  const int64_t before = piece * kPiece - 1;
-  if (before >= 0 && keys[before] == token) return;     // began earlier
-  // pieces that begin with the token
-  int64_t reach = 0;
-  for (int64_t p = piece + 1;; p += 64) {
-    const bool on = (p + lane) * kPiece < A.ntokens && keys[(p + lane) * kPiece] == token;
-    const uint64_t all = __ballot(on);
-    if (~all) {
-      reach += __builtin_ctzll(~all);
-      break;
-    }
-    reach += 64;
-  }
-  const bool in = c < A.dim;
-  const float* partial = A.partial + ((int64_t)w * A.pieces + piece) * 2 * A.partial_ld + (in ? c : 0);
-  const int64_t share = reach < 16 ? reach : (reach + kJoinWaves - 1) / kJoinWaves;
-  const int64_t from = share * wave < reach ? share * wave : reach, to = from + share < reach ? from + share : reach;
-  float sum[V];
-#pragma unroll
-  for (int i = 0; i < V; ++i) sum[i] = 0.0f;
-  if (wave == 0) load_sums<V>(partial + A.partial_ld, sum);
-#pragma unroll 4
+__device__ __forceinline__ void add_pieces(const float* partial, int64_t partial_ld, int64_t from, int64_t to, float (&sum)[V]) {
+#pragma unroll 8
   for (int64_t p = from; p < to; ++p) {
     float x[V];
-    load_sums<V>(partial + (p + 1) * 2 * A.partial_ld, x);
+    load_sums<V>(partial + p * 2 * partial_ld, x);
 #pragma unroll
     for (int i = 0; i < V; ++i) sum[i] += x[i];
   }
-  if (share < reach) {
+}
+
+// Adds up the partial sums of the tokens that span pieces.  A wave looks at a piece (for 64 * V columns): if a token begins there and
+// goes on in the next one, it adds up its partial sums, unless there are many; those the workgroup's waves share.  (Its waves look at
+// neighbouring pieces, of which few begin a token with many.)
+template <int V, bool ADD>
+__global__ __launch_bounds__(64 * kJoinWaves) void k_embed_join(EmbedArgs A) {
+  __shared__ float sums[kJoinWaves][64][V];
+  __shared__ int64_t many[kJoinWaves];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, w = blockIdx.y;
+  const uint32_t* keys = A.keys + (int64_t)w * A.ntokens;
+  const float* partial = A.partial + (int64_t)w * A.pieces * 2 * A.partial_ld;
+  const int64_t units = A.pieces * A.column_chunks, first = (int64_t)blockIdx.x * kJoinWaves;
+  {
+    const int64_t piece = (first + wave) % A.pieces, next = (piece + 1) * kPiece, before = piece * kPiece - 1;
+    const int64_t c = ((first + wave) / A.pieces * 64 + lane) * V;
+    int64_t reach = 0;     // pieces after this one that begin with the token
+    uint32_t token = 0;
+    if (first + wave < units && next < A.ntokens) {
+      const uint32_t after = keys[next], left = before >= 0 ? keys[before] : 0xFFFFFFFFu;
+      token = keys[next - 1];
+      if (token == after && token != left && token != (uint32_t)A.vocab)
+        for (int64_t p = piece + 1;; p += 64) {
+          const bool on = (p + lane) * kPiece < A.ntokens && keys[(p + lane) * kPiece] == token;
+          const uint64_t all = __ballot(on);
+          if (~all) {
+            reach += __builtin_ctzll(~all);
+            break;
+          }
+          reach += 64;
+        }
+    }
+    if (lane == 0) many[wave] = reach >= kJoinAlone ? reach : 0;
+    if (reach > 0 && reach < kJoinAlone && c < A.dim) {
+      float sum[V], old[V];
+      if (ADD) load_sums<V>(sums_of(A, w, token, c), old);
+      load_sums<V>(partial + (piece * 2 + 1) * A.partial_ld + c, sum);
+      add_pieces<V>(partial + c, A.partial_ld, piece + 1, piece + 1 + reach, sum);
+      put_sums<ADD, V>(A, sums_of(A, w, token, c), sum, old);
+    }
+  }
+  __syncthreads();
+  for (int v = 0; v < kJoinWaves; ++v) {
+    const int64_t reach = many[v];
+    if (reach == 0) continue;
+    const int64_t piece = (first + v) % A.pieces, share = (reach + kJoinWaves - 1) / kJoinWaves;
+    const int64_t c = ((first + v) / A.pieces * 64 + lane) * V, column = c < A.dim ? c : 0;
+    const int64_t from = share * wave < reach ? share * wave : reach, to = from + share < reach ? from + share : reach;
+    float sum[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) sum[i] = 0.0f;
+    if (wave == 0) load_sums<V>(partial + (piece * 2 + 1) * A.partial_ld + column, sum);
+    add_pieces<V>(partial + column, A.partial_ld, piece + 1 + from, piece + 1 + to, sum);
 #pragma unroll
     for (int i = 0; i < V; ++i) sums[wave][lane][i] = sum[i];
     __syncthreads();
-    if (wave != 0) return;
-    for (int v = 1; v < kJoinWaves; ++v)
+    if (wave == 0 && c < A.dim) {
+      float old[V];
+      float* to_row = sums_of(A, w, keys[(piece + 1) * kPiece], c);
+      if (ADD) load_sums<V>(to_row, old);
 #pragma unroll
-      for (int i = 0; i < V; ++i) sum[i] += sums[v][lane][i];
+      for (int u = 1; u < kJoinWaves; ++u)
+#pragma unroll
+        for (int i = 0; i < V; ++i) sum[i] += sums[u][lane][i];
+      put_sums<ADD, V>(A, to_row, sum, old);
+    }
+    __syncthreads();
   }
-  if (wave == 0 && in) put_sums<V>(A, w, token, c, sum);
 }
 
 }  // namespace choco

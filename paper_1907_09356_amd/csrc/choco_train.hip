@@ -90,7 +90,7 @@ struct EmbedLayout {
   size_t keys, places, keys_next, places_next, counts, partial, total;
   int64_t pieces, partial_ld;
   uint32_t chunks;
-  int digit_bits, passes;
+  int digit_bits, passes, rounds;
   bool one;    // a workgroup orders all of a worker's tokens
 };
 
@@ -102,8 +102,9 @@ EmbedLayout embed_layout(const choco_embed_config& c) {
   while (c.vocab >> bits) ++bits;    // keys go up to vocab itself
   const int most = L.one ? kSortDigit : kChunkDigit;
   L.passes = (bits + most - 1) / most;
-  L.digit_bits = (bits + L.passes - 1) / L.passes;
-  L.chunks = blocks_of(c.tokens, kChunkTokens);
+  L.digit_bits = std::max(2, (bits + L.passes - 1) / L.passes);
+  L.rounds = c.tokens < kLongLists ? kShortRounds : kLongRounds;
+  L.chunks = blocks_of(c.tokens, kChunkThreads * L.rounds);
   L.pieces = (c.tokens + kPiece - 1) / kPiece;
   L.partial_ld = (c.dim + 7) / 8 * 8;
   size_t at = 0;
@@ -410,13 +411,12 @@ int choco_embed_backward(const choco_embed_config* cfg, const void* tokens_dev, 
   EmbedArgs A = embed_args(c, tokens_dev);
   A.rows = dy_dev;
   A.dtable = dtable_dev;
-  A.accumulate = accumulate ? 1 : 0;
   const hipStream_t stream = (hipStream_t)c.stream;
   const int64_t zero_blocks = accumulate ? 0 : (c.vocab * c.dim + kZeroFloats - 1) / kZeroFloats;
   if (!launch_fits((double)zero_blocks * c.n + c.n, kSortThreads)) return CHOCO_E_UNSUPPORTED;
   A.zero_blocks = (uint32_t)zero_blocks;
   if (c.tokens == 0) {   // nothing but zeros
-    k_embed_count<int32_t, true><<<dim3(A.zero_blocks, (uint32_t)c.n), kChunkThreads, 0, stream>>>(A, 0);
+    k_embed_count<int32_t, true, kShortRounds><<<dim3(A.zero_blocks, (uint32_t)c.n), kChunkThreads, 0, stream>>>(A, 0);
     TRY_HIP(hipGetLastError());
     return CHOCO_OK;
   }
@@ -429,34 +429,40 @@ int choco_embed_backward(const choco_embed_config* cfg, const void* tokens_dev, 
   A.digit_bits = L.digit_bits;
   A.passes = L.passes;
   const size_t size = type_bytes(c.row_type);
-  const int v = embed_width(size == 2 ? 8 : 4, c.dim, {{dy_dev, size}, {dtable_dev, 4}},
-                            {{c.row_ld, size}, {c.row_stride, size}, {c.table_stride, 4}});
+  int v = embed_width(size == 2 ? 8 : 4, c.dim, {{dy_dev, size}, {dtable_dev, 4}},
+                      {{c.row_ld, size}, {c.row_stride, size}, {c.table_stride, 4}});
+  while (v > 1 && 32 * v >= c.dim) v /= 2;     // (no more than a lane needs to leave no lane without columns)
   A.column_chunks = (c.dim + 64 * v - 1) / (64 * v);
-  if (!launch_fits((double)A.pieces * (double)A.column_chunks, 64 * kJoinWaves) || !launch_fits((double)L.chunks + zero_blocks, kChunkThreads))
+  if (!launch_fits((double)A.pieces * (double)A.column_chunks, 64) || !launch_fits((double)L.chunks + zero_blocks, kChunkThreads))
     return CHOCO_E_UNSUPPORTED;
   const auto order = [&](auto token) {
     using Tok = decltype(token);
     if (L.one) {
-      k_embed_sort<Tok><<<dim3((uint32_t)(c.n + zero_blocks * c.n)), kSortThreads, 0, stream>>>(A, c.n);
+      k_embed_sort<Tok><<<dim3((uint32_t)(c.n + zero_blocks * c.n)), kSortThreads, sort_lds(c.tokens, L.digit_bits), stream>>>(A, c.n);
       return;
     }
     A.counts = (uint32_t*)(ws + L.counts);
     A.keys_next = (uint32_t*)(ws + L.keys_next);
     A.places_next = (uint32_t*)(ws + L.places_next);
     A.chunks = L.chunks;
-    const dim3 grid(L.chunks, (uint32_t)c.n), grid_and_zeros(L.chunks + A.zero_blocks, (uint32_t)c.n);
-    for (int pass = 0; pass < L.passes; ++pass) {
-      const int shift = pass * L.digit_bits;
-      if (pass == 0) {
-        k_embed_count<Tok, true><<<grid_and_zeros, kChunkThreads, 0, stream>>>(A, shift);
-        k_embed_scatter<Tok, true><<<grid, kChunkThreads, 0, stream>>>(A, shift);
-      } else {
-        k_embed_count<Tok, false><<<grid, kChunkThreads, 0, stream>>>(A, shift);
-        k_embed_scatter<Tok, false><<<grid, kChunkThreads, 0, stream>>>(A, shift);
+    const auto passes = [&](auto length) {
+      constexpr int ROUNDS = decltype(length)::value;
+      const dim3 grid(L.chunks, (uint32_t)c.n), grid_and_zeros(L.chunks + A.zero_blocks, (uint32_t)c.n);
+      for (int pass = 0; pass < L.passes; ++pass) {
+        const int shift = pass * L.digit_bits;
+        if (pass == 0) {
+          k_embed_count<Tok, true, ROUNDS><<<grid_and_zeros, kChunkThreads, 0, stream>>>(A, shift);
+          k_embed_scatter<Tok, true, ROUNDS><<<grid, kChunkThreads, 0, stream>>>(A, shift);
+        } else {
+          k_embed_count<Tok, false, ROUNDS><<<grid, kChunkThreads, 0, stream>>>(A, shift);
+          k_embed_scatter<Tok, false, ROUNDS><<<grid, kChunkThreads, 0, stream>>>(A, shift);
+        }
+        std::swap(A.keys, A.keys_next);
+        std::swap(A.places, A.places_next);
       }
-      std::swap(A.keys, A.keys_next);
-      std::swap(A.places, A.places_next);
-    }
+    };
+    if (L.rounds == kShortRounds) passes(std::integral_constant<int, kShortRounds>{});
+    else passes(std::integral_constant<int, kLongRounds>{});
   };
   if (c.token_type == CHOCO_I32) order(int32_t{});
   else order(int64_t{});
@@ -467,8 +473,13 @@ int choco_embed_backward(const choco_embed_config* cfg, const void* tokens_dev, 
       using Row = decltype(row);
       constexpr int V = decltype(width)::value;
       if constexpr (V * sizeof(Row) <= 16) {
-        k_embed_sum<Row, V><<<dim3(blocks_of(units, 4), (uint32_t)c.n), 256, 0, stream>>>(A);
-        if (A.pieces > 1) k_embed_join<V><<<dim3((uint32_t)units, (uint32_t)c.n), 64 * kJoinWaves, 0, stream>>>(A);
+        const auto sums = [&](auto add) {
+          constexpr bool ADD = decltype(add)::value;
+          k_embed_sum<Row, V, ADD><<<dim3(blocks_of(units, 4), (uint32_t)c.n), 256, 0, stream>>>(A);
+          if (A.pieces > 1) k_embed_join<V, ADD><<<dim3(blocks_of(units, kJoinWaves), (uint32_t)c.n), 64 * kJoinWaves, 0, stream>>>(A);
+        };
+        if (accumulate) sums(std::true_type{});
+        else sums(std::false_type{});
       }
     });
   });

@@ -84,7 +84,7 @@ def _ptr(t):
 
 
 def _stream(t, stream):
-    return torch.cuda.current_stream(t.device).cuda_stream if stream is None else stream
+    return torch._C._cuda_getCurrentRawStream(t.get_device()) if stream is None else stream
 
 
 def _scratch(nbytes, like):
@@ -103,6 +103,8 @@ def _planned(cfg, query):
 def _embed_plan(token_shape, token_stride, token_type, table_shape, table_stride, table_type, row_shape, row_stride, row_type,
                 scale, stream):
     """The configuration of a call, by what of its tensors goes into it."""
+    assert len(token_shape) == 2 and len(table_shape) == 3 and len(row_shape) == 3
+    assert token_type in TOKEN_TYPES and table_type in TYPES and row_type in TYPES
     (n, count), (tables, vocab, dim) = token_shape, table_shape
     assert tables == n and row_shape == (n, count, dim)
     assert count <= 1 or token_stride[1] == 1
@@ -118,9 +120,7 @@ def _embed_plan(token_shape, token_stride, token_type, table_shape, table_stride
 
 
 def _embed_config(tokens, table, rows, scale, stream):
-    assert tokens.is_cuda and table.device == tokens.device and rows.device == tokens.device
-    assert tokens.dim() == 2 and table.dim() == 3 and rows.dim() == 3
-    assert tokens.dtype in TOKEN_TYPES and table.dtype in TYPES and rows.dtype in TYPES
+    assert tokens.is_cuda and table.get_device() == rows.get_device() == tokens.get_device()
     return _embed_plan(tokens.shape, tokens.stride(), tokens.dtype, table.shape, table.stride(), table.dtype, rows.shape,
                        rows.stride(), rows.dtype, scale, _stream(tokens, stream))
 
@@ -152,6 +152,7 @@ def embed_grad(tokens, dout, dtable, scale=1.0, accumulate=False, stream=None):
 @functools.lru_cache(maxsize=512)
 def _recur_plan(shape, dtype, strides, stream):
     """The configuration of a call: strides of f, u, o, y (backward: dy), df, du, do, None for one that is not there."""
+    assert len(shape) == 3 and dtype in TYPES
     assert shape[2] <= 1 or all(s is None or s[2] == 1 for s in strides)
     cfg = RecurConfig(batch=shape[0], steps=shape[1], dim=shape[2], type=TYPES[dtype], stream=stream)
     for name, s in zip(("f", "u", "o", "y", "df", "du", "do"), strides):
@@ -161,23 +162,29 @@ def _recur_plan(shape, dtype, strides, stream):
 
 
 def _recur_config(f, stream, *tensors):
-    device, dtype, shape = f.device, f.dtype, f.shape
+    device, dtype, shape = f.get_device(), f.dtype, f.shape
     strides = [f.stride()]
     for t in tensors:
-        assert t is None or (t.device == device and t.dtype == dtype and t.shape == shape)
-        strides.append(None if t is None else t.stride())
+        if t is not None:
+            assert t.dtype == dtype and t.shape == shape and t.get_device() == device
+            t = t.stride()
+        strides.append(t)
     return _recur_plan(shape, dtype, tuple(strides), _stream(f, stream))
 
 
 def _state(t, f):
-    assert t is None or (t.device == f.device and t.dtype == torch.float32 and t.is_contiguous()
-                         and t.shape == (f.shape[0], f.shape[2]))
-    return t
+    """The address of a state of every sequence, or None."""
+    if t is None:
+        return None
+    assert t.get_device() == f.get_device() and t.dtype == torch.float32 and t.is_contiguous() and t.shape == f.shape[::2]
+    return t.data_ptr()
 
 
 def _lengths(t, f):
-    assert t is None or (t.device == f.device and t.dtype == torch.int32 and t.is_contiguous() and t.shape == f.shape[:1])
-    return t
+    if t is None:
+        return None
+    assert t.get_device() == f.get_device() and t.dtype == torch.int32 and t.is_contiguous() and t.shape == f.shape[:1]
+    return t.data_ptr()
 
 
 def recurrence(f, u, o=None, h0=None, lengths=None, save=False, out=None, h_last=None, stream=None):
@@ -186,19 +193,19 @@ def recurrence(f, u, o=None, h0=None, lengths=None, save=False, out=None, h_last
     f, u, o (batch, steps, dim) of one type, strided as they come (columns of one projection); h0 (batch, dim) of
     float32, zero without; lengths (batch,) of int32.  save: keep what `recurrence_grad` needs (else None is returned).
     h_last may be h0 itself, as in token by token generation."""
-    assert f.is_cuda and f.dim() == 3 and f.dtype in TYPES
+    assert f.is_cuda
     B, T, C = f.shape
-    y = torch.empty((B, T, C), dtype=f.dtype, device=f.device) if out is None else out
+    device = f.device
+    y = torch.empty((B, T, C), dtype=f.dtype, device=device) if out is None else out
     if h_last is None:
-        h_last = torch.empty((B, C), dtype=torch.float32, device=f.device)
+        h_last = torch.empty((B, C), dtype=torch.float32, device=device)
     saved = None
     if save:
-        saved = torch.empty(((T + SAVE_STEPS - 1) // SAVE_STEPS, B, C), dtype=torch.float32, device=f.device)
+        saved = torch.empty(((T + SAVE_STEPS - 1) // SAVE_STEPS, B, C), dtype=torch.float32, device=device)
     cfg, nbytes = _recur_config(f, stream, u, o, y)
     ws = _scratch(nbytes, f)
-    _check(lib().choco_recur_forward(cfg, _ptr(f), _ptr(u), _ptr(o), _ptr(_state(h0, f)),
-                                     _ptr(_lengths(lengths, f)), _ptr(y), _ptr(_state(h_last, f)), _ptr(saved), _ptr(ws),
-                                     nbytes), "choco_recur_forward")
+    _check(lib().choco_recur_forward(cfg, f.data_ptr(), u.data_ptr(), _ptr(o), _state(h0, f), _lengths(lengths, f), y.data_ptr(),
+                                     _state(h_last, f), _ptr(saved), _ptr(ws), nbytes), "choco_recur_forward")
     return y, h_last, saved
 
 
@@ -206,19 +213,19 @@ def recurrence_grad(f, u, saved, dy, o=None, lengths=None, dlast=None, stream=No
     """Backward pass of `recurrence`: (df, du, do or None, dh0), the first three columns of one matrix.
 
     saved as `recurrence(..., save=True)` returned it; dlast the gradient of the last states, zero without."""
-    assert f.is_cuda and f.dim() == 3 and f.dtype in TYPES
+    assert f.is_cuda
     B, T, C = f.shape
-    assert saved.device == f.device and saved.dtype == torch.float32 and saved.is_contiguous()
+    assert saved.get_device() == f.get_device() and saved.dtype == torch.float32 and saved.is_contiguous()
     assert saved.shape == ((T + SAVE_STEPS - 1) // SAVE_STEPS, B, C)
     parts = 2 if o is None else 3
-    grads = torch.empty((B, T, parts * C), dtype=f.dtype, device=f.device).split(C, 2) if C else [torch.empty_like(f)] * parts
+    grads = torch.empty((B, T, parts, C), dtype=f.dtype, device=f.device).unbind(2)
     df, du, do = grads[0], grads[1], None if o is None else grads[2]
     dh0 = torch.empty((B, C), dtype=torch.float32, device=f.device)
     cfg, nbytes = _recur_config(f, stream, u, o, dy, df, du, do)
     ws = _scratch(nbytes, f)
-    _check(lib().choco_recur_backward(cfg, _ptr(f), _ptr(u), _ptr(o), _ptr(_lengths(lengths, f)), _ptr(saved),
-                                      _ptr(dy), _ptr(_state(dlast, f)), _ptr(df), _ptr(du), _ptr(do), _ptr(dh0), _ptr(ws),
-                                      nbytes), "choco_recur_backward")
+    _check(lib().choco_recur_backward(cfg, f.data_ptr(), u.data_ptr(), _ptr(o), _lengths(lengths, f), saved.data_ptr(),
+                                      dy.data_ptr(), _state(dlast, f), df.data_ptr(), du.data_ptr(), _ptr(do), dh0.data_ptr(),
+                                      _ptr(ws), nbytes), "choco_recur_backward")
     return df, du, do, dh0
 
 
