@@ -60,7 +60,7 @@ int choco_embed_backward(const choco_embed_config* cfg, const void* tokens_dev, 
  * States are fp32; y is rounded once.  A sequence of lengths[b] < steps steps keeps its state from there on
  * and its further y (and gradients) are zero, whatever its further inputs hold; lengths are clamped to [0, steps].
  * Generation is steps = 1 with h0 = the last state; h_last may be h0's own buffer. */
-#define CHOCO_RECUR_SAVE_STEPS 16
+#define CHOCO_RECUR_SAVE_STEPS 8
 typedef struct {
   int64_t batch, steps, dim; /* >= 0 each, below 2^31; batch * dim and batch * steps below 2^40                 */
   int32_t type;              /* of f, u, o, y and their gradients: CHOCO_F32 / BF16 / F16                */

@@ -1,5 +1,21 @@
 // Gated linear recurrence h_t = a_t h_{t-1} + (1 - a_t) u_t, a = sigmoid(f), y = sigmoid(o) h, and its backward
 // pass (device code).
+//
+// How the work is split.  A strip is 64 * V channels of one sequence, V channels a lane.  A workgroup takes a tile: the
+// steps of a strip that its waves hold in registers, kSaveSteps each.  A wave loads its steps at once and reduces them to the map
+// h -> A h + H; the waves exchange these maps through LDS, and each applies those before its own to the state before the
+// tile and goes through its steps, which are still in registers, once more.  So everything is read once, and the chain from
+// step to step is as long as a tile has waves.
+//
+// Sequences longer than a tile are chains of tiles.  A tile publishes its map as soon as it has it; kChainTiles of them in a row
+// form a link: each applies to the state before the link the maps of the tiles before it in the link, and the last one
+// publishes the state after it.  Which values are combined, and in which order, is fixed, so the bits of a result do not depend on
+// timing.  A published value is one 64-bit word with the map's A in its lower half, all ones until it is there, stored and
+// loaded by relaxed atomics of the device's scope: a word carries its own readiness and nothing else has to be ordered
+// with it.  A workgroup takes its place in a chain from the chain's counter when it starts.  What it waits for are tiles that have
+// taken theirs before, so they are running or done; their maps do not wait for anything, and the state before a link waits for
+// earlier links only: whatever the order in which workgroups are started, every wait ends.  (A wait gives up after kMostPolls
+// all the same; what it waited for is then NaN.)
 #pragma once
 
 #include <type_traits>
@@ -8,13 +24,17 @@
 
 namespace choco {
 
-constexpr int kSaveSteps = 16;   // the forward pass keeps the state before every so many steps
-
-#ifndef RW
-#define RW 8
+#ifndef SAVE
+#define SAVE 8
+#define RW 16
+#define CT 8
 #endif
-constexpr int kRecurWaves = RW;   // most waves of a workgroup
-constexpr int kMaxSegments = 64; // most pieces that a sequence is split into
+constexpr int kSaveSteps = SAVE;    // steps of a wave; the forward pass keeps the state before every so many
+constexpr int kRecurWaves = RW;     // most waves of a workgroup
+constexpr int kTileSteps = kSaveSteps * kRecurWaves;
+constexpr int kChainTiles = CT;
+constexpr int kMostPolls = 1 << 20;
+constexpr int kTakenWords = 64;     // from one chain's counter to the next: additions to one line wait for each other, 11 ns each
 
 struct RecurArgs {
   const void *f, *u, *o, *dy;
@@ -26,9 +46,11 @@ struct RecurArgs {
   int64_t batch, steps, dim;
   int64_t f_seq, f_step, u_seq, u_step, o_seq, o_step, y_seq, y_step;
   int64_t df_seq, df_step, du_seq, du_step, do_seq, do_step;
-  float2* parts;            // [segments][batch][dim], see k_recur_part; null: one segment
-  int64_t segment_steps;    // a multiple of kSaveSteps * (waves of a workgroup)
-  uint32_t strips, segments;
+  // chains (strips of all sequences): words of their tiles' maps [chains][tiles][64 * V], of the states before their links
+  // [chains][links][64 * V], and how many tiles have been taken [chains][kTakenWords]
+  uint64_t *maps, *states;
+  uint32_t* taken;
+  uint32_t strips, chains, tiles, links;
 };
 
 // sigmoid(x) and 1 - sigmoid(x), the smaller of the two not by a difference: the exponential's argument is rounded to
@@ -48,33 +70,82 @@ __device__ __forceinline__ int64_t steps_of(const RecurArgs& A, int64_t b) {
   return n < 0 ? 0 : n > A.steps ? A.steps : n;
 }
 
-// How the work is split.  A strip is 64 * V channels of one sequence, V channels a lane.  A workgroup takes a strip (of
-// one segment of the sequence) and goes through its steps in rounds, kSaveSteps of a round for each wave: a wave loads
-// its steps at once, reduces them to the map h -> A h + H, the waves exchange these maps through LDS, and each applies
-// the maps before its own to the state and goes through its steps, which are still in registers, once more.  Everything
-// is read once, and the chain from step to step is as long as a round has waves, not steps.
-// Sequences with too few strips to fill the chip are split into segments, whose maps a first kernel (k_recur_part)
-// computes: f and u (backward: f, o and dy) are then read twice.
+// ---- words of a chain ----
+constexpr uint64_t kNotThere = ~(uint64_t)0;
+__device__ __forceinline__ void publish(uint64_t* word, float a, float h) {
+  uint32_t low = __float_as_uint(a);
+  if (low == 0xFFFFFFFFu) low = 0x7FC00000u;     // any other NaN
+  __hip_atomic_store(word, (uint64_t)__float_as_uint(h) << 32 | low, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <int V>
+__device__ __forceinline__ void await(uint64_t* words, float (&a)[V], float (&h)[V]) {
+  uint64_t x[V];
+  for (int polls = 0; polls < kMostPolls; ++polls) {
+    bool there = true;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      x[i] = __hip_atomic_load(words + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      there = there && (uint32_t)x[i] != 0xFFFFFFFFu;
+    }
+    if (__all(there)) break;
+    __builtin_amdgcn_s_sleep(1);
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    a[i] = __uint_as_float((uint32_t)x[i]);
+    h[i] = __uint_as_float((uint32_t)(x[i] >> 32));
+  }
+}
+
+// Before the chains start: no word is there but the states before the first links (`first`, batch x dim, or zero), nothing is
+// taken.
+__global__ __launch_bounds__(256) void k_recur_chains(RecurArgs A, const float* first, int width) {
+  const int64_t maps = (int64_t)A.chains * A.tiles * width, states = (int64_t)A.chains * A.links * width;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < maps + states + A.chains; i += (int64_t)gridDim.x * 256) {
+    if (i < maps) {
+      A.maps[i] = kNotThere;
+    } else if (i < maps + states) {
+      const int64_t j = i - maps, chain = j / ((int64_t)A.links * width);
+      uint64_t word = kNotThere;
+      if (j % ((int64_t)A.links * width) < width) {
+        const int64_t b = chain / A.strips;
+        int64_t c = chain % A.strips * width + j % width;
+        if (c >= A.dim) c = chain % A.strips * width;
+        word = first ? (uint64_t)__float_as_uint(first[b * A.dim + c]) << 32 : 0;
+      }
+      A.states[j] = word;
+    } else {
+      A.taken[(i - maps - states) * kTakenWords] = 0;
+    }
+  }
+}
+
+// ---- a workgroup's tile ----
 struct RecurPlace {
-  int64_t b, strip, len, begin, end;   // sequence, first channel of the strip, its length, the segment's steps
-  uint32_t segment;
+  int64_t b, strip, len, begin;    // sequence, first channel of the strip, its length, the tile's first step
+  uint32_t chain, tile, turn;      // turn: the tile's place in its chain (backward: counted from the last)
   int lane;                        // first channel of the lane in the strip (of one that has none: 0, and it writes nothing)
   bool in;                         // the lane has channels
 };
 
-template <int V>
-__device__ __forceinline__ RecurPlace recur_place(const RecurArgs& A) {
+template <int V, bool CHAIN, bool BACK>
+__device__ __forceinline__ RecurPlace recur_place(const RecurArgs& A, uint32_t* taken) {
   RecurPlace P;
-  const uint32_t rest = blockIdx.x / A.strips, strip = blockIdx.x % A.strips;
-  P.segment = rest / (uint32_t)A.batch;
-  P.b = rest % (uint32_t)A.batch;
-  P.strip = (int64_t)strip * (64 * V);
+  P.chain = CHAIN ? blockIdx.x % A.chains : blockIdx.x;
+  P.turn = 0;
+  if (CHAIN) {
+    if (threadIdx.x == 0) *taken = atomicAdd(A.taken + (int64_t)P.chain * kTakenWords, 1u);
+    __syncthreads();
+    P.turn = __builtin_amdgcn_readfirstlane(*taken);
+  }
+  P.tile = BACK ? A.tiles - 1 - P.turn : P.turn;
+  P.b = P.chain / A.strips;
+  P.strip = (int64_t)(P.chain % A.strips) * (64 * V);
   P.lane = (threadIdx.x & 63) * V;
   P.in = P.strip + P.lane < A.dim;
   if (!P.in) P.lane = 0;
   P.len = steps_of(A, P.b);
-  P.begin = P.segment * A.segment_steps;
-  P.end = P.begin + A.segment_steps < A.steps ? P.begin + A.segment_steps : A.steps;
+  P.begin = (int64_t)P.tile * kTileSteps;
   return P;
 }
 
@@ -113,306 +184,214 @@ __device__ __forceinline__ int steps_left(int64_t end, int64_t t) {
   return __builtin_amdgcn_readfirstlane(end <= t ? 0 : end - t < kSaveSteps ? (int)(end - t) : kSaveSteps);
 }
 
-// (a, b) of the steps of a wave, and all of them in one map after (ma, mh); steps that are not in the sequence pass the state on.
-template <class T, int V>
-__device__ __forceinline__ void step_maps(const uint32_t (&f)[kSaveSteps], const uint32_t (&u)[kSaveSteps], int n,
-                                          float (&a)[kSaveSteps][V], float (&b)[kSaveSteps][V], float (&ma)[V], float (&mh)[V]) {
-#pragma unroll
-  for (int j = 0; j < kSaveSteps; ++j)
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      float down;
-      gate(entry<T>(f[j], i), a[j][i], down);
-      b[j][i] = down * entry<T>(u[j], i);
-      if (j >= n) {
-        a[j][i] = 1.0f;
-        b[j][i] = 0.0f;
-      }
-      mh[i] = fmaf(a[j][i], mh[i], b[j][i]);
-      ma[i] *= a[j][i];
-    }
-}
-
-// The waves' maps in LDS, two rounds in turn (so that one barrier a round is enough).
 template <int V>
-struct RecurMaps {
-  float a[2][kRecurWaves][64][V], h[2][kRecurWaves][64][V];
+struct RecurShared {
+  float a[kRecurWaves][64][V], h[kRecurWaves][64][V];               // the waves' maps, in the order of the recurrence
+  float link_a[kChainTiles][64][V], link_h[kChainTiles][64][V];     // those of the tiles before in the link; last: the state before it
+  uint32_t taken;
 };
 
-template <class T, int V, bool GATED>
-__global__ __launch_bounds__(64 * kRecurWaves) void k_recur(RecurArgs A) {
-  __shared__ RecurMaps<V> S;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  const RecurPlace P = recur_place<V>(A);
-  float h[V];
-#pragma unroll
-  for (int i = 0; i < V; ++i) h[i] = A.parts || !A.h0 ? 0.0f : A.h0[P.b * A.dim + P.strip + P.lane + i];
-  if (A.parts)
-    for (uint32_t s = 0; s <= P.segment; ++s)
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const float2 m = A.parts[((int64_t)s * A.batch + P.b) * A.dim + P.strip + P.lane + i];
-        h[i] = fmaf(m.x, h[i], m.y);
-      }
-  int turn = 0;
-  for (int64_t t = P.begin; t < P.end; t += kSaveSteps * waves, turn ^= 1) {
-    const int64_t t0 = t + kSaveSteps * wave;
-    const int n = steps_left(P.len, t0), all = steps_left(P.end, t0);
-    float a[kSaveSteps][V], b[kSaveSteps][V];
-    uint32_t o[kSaveSteps];
-    float ma[V], mh[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      ma[i] = 1.0f;
-      mh[i] = 0.0f;
-    }
-    if (n > 0) {
-      uint32_t f[kSaveSteps], u[kSaveSteps];
-      load_steps<T, V>(A.f, A.f_seq, A.f_step, P, t0, n, f);
-      load_steps<T, V>(A.u, A.u_seq, A.u_step, P, t0, n, u);
-      if (GATED) load_steps<T, V>(A.o, A.o_seq, A.o_step, P, t0, n, o);
-      step_maps<T, V>(f, u, n, a, b, ma, mh);
-    }
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      S.a[turn][wave][lane][i] = ma[i];
-      S.h[turn][wave][lane][i] = mh[i];
-    }
-    __syncthreads();
-    float g[V];
-    for (int w = 0; w < waves; ++w)
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        if (w == wave) g[i] = h[i];
-        h[i] = fmaf(S.a[turn][w][lane][i], h[i], S.h[turn][w][lane][i]);
-      }
-    if (!P.in || all == 0) continue;
-    if (A.saved) {
-#pragma unroll
-      for (int i = 0; i < V; ++i) A.saved[((t0 / kSaveSteps) * A.batch + P.b) * A.dim + P.strip + P.lane + i] = g[i];
-    }
-#pragma unroll
-    for (int j = 0; j < kSaveSteps; ++j) {
-      float out[V];
-      if (j >= all) break;
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        out[i] = 0.0f;
-        if (j < n) {
-          g[i] = fmaf(a[j][i], g[i], b[j][i]);
-          out[i] = GATED ? gate(entry<T>(o[j], i)) * g[i] : g[i];
-        }
-      }
-      store_step<T, V>(A.y, A.y_seq, A.y_step, P, t0 + j, out);
-    }
-  }
-  if (A.h_last && P.in && wave == 0 && P.segment + 1 == A.segments)
-#pragma unroll
-    for (int i = 0; i < V; ++i) A.h_last[P.b * A.dim + P.strip + P.lane + i] = h[i];
-}
-
-// The maps of the segments: parts[0] = (0, h0), parts[s + 1] = that of segment s; the last one's is not needed.  A wave
-// takes a piece of the segment in one go.
-template <class T, int V>
-__global__ __launch_bounds__(64 * kRecurWaves) void k_recur_part(RecurArgs A) {
-  __shared__ RecurMaps<V> S;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  const RecurPlace P = recur_place<V>(A);
-  const int64_t piece = A.segment_steps / waves;
-  float ma[V], mh[V];
+// From the waves' maps (m_a, m_h; `turn`: a wave's place in the order of the recurrence) and the state `h` before the tile
+// (outside chains: given) to the state before the wave's own steps; the last wave's ends as the one after the tile.
+template <int V, bool CHAIN>
+__device__ __forceinline__ void recur_carry(const RecurArgs& A, const RecurPlace& P, RecurShared<V>& S, int turn, int waves,
+                                            const float (&ma)[V], const float (&mh)[V], float (&h)[V], float (&after)[V]) {
+  const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int i = 0; i < V; ++i) {
+    S.a[turn][lane][i] = ma[i];
+    S.h[turn][lane][i] = mh[i];
+  }
+  __syncthreads();
+  if (CHAIN) {
+    const uint32_t link = P.turn / kChainTiles, before = P.turn % kChainTiles;
+    if (turn == waves - 1 && before + 1 < kChainTiles && P.turn + 1 < A.tiles) {
+      float ta[V], th[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        ta[i] = 1.0f;
+        th[i] = 0.0f;
+      }
+      for (int w = 0; w < waves; ++w)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          th[i] = fmaf(S.a[w][lane][i], th[i], S.h[w][lane][i]);
+          ta[i] *= S.a[w][lane][i];
+        }
+#pragma unroll
+      for (int i = 0; i < V; ++i) publish(A.maps + ((int64_t)P.chain * A.tiles + P.turn) * (64 * V) + lane * V + i, ta[i], th[i]);
+    }
+    for (uint32_t k = turn; k <= before; k += waves) {     // the maps before, and the state before them
+      float la[V], lh[V];
+      await<V>((k < before ? A.maps + ((int64_t)P.chain * A.tiles + P.turn - before + k) * (64 * V)
+                           : A.states + ((int64_t)P.chain * A.links + link) * (64 * V)) + lane * V, la, lh);
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        S.link_a[k][lane][i] = la[i];
+        S.link_h[k][lane][i] = lh[i];
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < V; ++i) h[i] = S.link_h[before][lane][i];
+    for (uint32_t w = 0; w < before; ++w)
+#pragma unroll
+      for (int i = 0; i < V; ++i) h[i] = fmaf(S.link_a[w][lane][i], h[i], S.link_h[w][lane][i]);
+  }
+  for (int w = 0; w < turn; ++w)
+#pragma unroll
+    for (int i = 0; i < V; ++i) h[i] = fmaf(S.a[w][lane][i], h[i], S.h[w][lane][i]);
+  if (turn != waves - 1) return;
+#pragma unroll
+  for (int i = 0; i < V; ++i) after[i] = fmaf(ma[i], h[i], mh[i]);
+  if (CHAIN && P.turn % kChainTiles + 1 == kChainTiles && P.turn + 1 < A.tiles)
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      publish(A.states + ((int64_t)P.chain * A.links + P.turn / kChainTiles + 1) * (64 * V) + lane * V + i, 0.0f, after[i]);
+}
+
+template <class T, int V, bool GATED, bool CHAIN>
+__global__ __launch_bounds__(64 * kRecurWaves) void k_recur(RecurArgs A) {
+  __shared__ RecurShared<V> S;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+  const RecurPlace P = recur_place<V, CHAIN, false>(A, &S.taken);
+  const int64_t state = P.b * A.dim + P.strip + P.lane, t0 = P.begin + kSaveSteps * wave;
+  const int n = steps_left(P.len, t0), all = steps_left(A.steps, t0);
+  float h[V], a[kSaveSteps][V], b[kSaveSteps][V], ma[V], mh[V], after[V];
+  uint32_t o[kSaveSteps];
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    h[i] = CHAIN || !A.h0 ? 0.0f : A.h0[state + i];
     ma[i] = 1.0f;
     mh[i] = 0.0f;
   }
-  for (int64_t t0 = P.begin + wave * piece; t0 < P.begin + (wave + 1) * piece; t0 += kSaveSteps) {
-    const int n = steps_left(P.len, t0);
-    if (n == 0) break;
+  if (n > 0) {
     uint32_t f[kSaveSteps], u[kSaveSteps];
     load_steps<T, V>(A.f, A.f_seq, A.f_step, P, t0, n, f);
     load_steps<T, V>(A.u, A.u_seq, A.u_step, P, t0, n, u);
-    float a[kSaveSteps][V], b[kSaveSteps][V];
-    step_maps<T, V>(f, u, n, a, b, ma, mh);
-  }
+    if (GATED) load_steps<T, V>(A.o, A.o_seq, A.o_step, P, t0, n, o);
 #pragma unroll
-  for (int i = 0; i < V; ++i) {
-    S.a[0][wave][lane][i] = ma[i];
-    S.h[0][wave][lane][i] = mh[i];
-  }
-  __syncthreads();
-  if (wave != 0 || !P.in) return;
+    for (int j = 0; j < kSaveSteps; ++j)
 #pragma unroll
-  for (int i = 0; i < V; ++i) {
-    for (int w = 1; w < waves; ++w) {
-      mh[i] = fmaf(S.a[0][w][lane][i], mh[i], S.h[0][w][lane][i]);
-      ma[i] *= S.a[0][w][lane][i];
+      for (int i = 0; i < V; ++i) {
+        float down;
+        gate(entry<T>(f[j], i), a[j][i], down);
+        b[j][i] = down * entry<T>(u[j], i);
+        if (j >= n) {     // not in the sequence: the state is passed on
+          a[j][i] = 1.0f;
+          b[j][i] = 0.0f;
+        }
+        mh[i] = fmaf(a[j][i], mh[i], b[j][i]);
+        ma[i] *= a[j][i];
+      }
+  }
+  recur_carry<V, CHAIN>(A, P, S, wave, waves, ma, mh, h, after);
+  if (!P.in) return;
+  if (A.h_last && P.tile + 1 == A.tiles && wave == waves - 1)
+#pragma unroll
+    for (int i = 0; i < V; ++i) A.h_last[state + i] = after[i];
+  if (all == 0) return;
+  if (A.saved)
+#pragma unroll
+    for (int i = 0; i < V; ++i) A.saved[(t0 / kSaveSteps) * A.batch * A.dim + state + i] = h[i];
+#pragma unroll
+  for (int j = 0; j < kSaveSteps; ++j) {
+    if (j >= all) break;
+    float out[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      out[i] = 0.0f;
+      if (j < n) {
+        h[i] = fmaf(a[j][i], h[i], b[j][i]);
+        out[i] = GATED ? gate(entry<T>(o[j], i)) * h[i] : h[i];
+      }
     }
-    const int64_t at = P.b * A.dim + P.strip + P.lane + i;
-    A.parts[(int64_t)(P.segment + 1) * A.batch * A.dim + at] = make_float2(ma[i], mh[i]);
-    if (P.segment == 0) A.parts[at] = make_float2(0.0f, A.h0 ? A.h0[at] : 0.0f);
+    store_step<T, V>(A.y, A.y_seq, A.y_step, P, t0 + j, out);
   }
 }
 
 // Backward: the same from the last steps back, with the map of a step on a_{t+1} e_{t+1}: e -> a (e + dy s).  The states
 // before each wave's steps are those that the forward pass kept.
-template <class T, int V, bool GATED>
+template <class T, int V, bool GATED, bool CHAIN>
 __global__ __launch_bounds__(64 * kRecurWaves) void k_recur_back(RecurArgs A) {
-  __shared__ RecurMaps<V> S;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  const RecurPlace P = recur_place<V>(A);
-  float e[V];
-#pragma unroll
-  for (int i = 0; i < V; ++i) e[i] = A.dlast ? A.dlast[P.b * A.dim + P.strip + P.lane + i] : 0.0f;
-  if (A.parts)
-    for (uint32_t s = A.segments - 1; s > P.segment; --s)
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const float2 m = A.parts[((int64_t)s * A.batch + P.b) * A.dim + P.strip + P.lane + i];
-        e[i] = fmaf(m.x, e[i], m.y);
-      }
-  const int64_t round = kSaveSteps * waves;
-  int turn = 0;
-  for (int64_t t = P.begin + (P.end - P.begin + round - 1) / round * round - round; t >= P.begin; t -= round, turn ^= 1) {
-    const int64_t t0 = t + kSaveSteps * wave;
-    const int n = steps_left(P.len, t0), all = steps_left(P.end, t0);
-    // of each step: a, dy s, 1 - a, (h_{t-1} - u) a
-    float a[kSaveSteps][V], into[kSaveSteps][V], down[kSaveSteps][V], off[kSaveSteps][V];
-    float ma[V], me[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      ma[i] = 1.0f;
-      me[i] = 0.0f;
-    }
-    if (n > 0) {
-      uint32_t f[kSaveSteps], u[kSaveSteps], o[kSaveSteps], d[kSaveSteps];
-      load_steps<T, V>(A.f, A.f_seq, A.f_step, P, t0, n, f);
-      load_steps<T, V>(A.u, A.u_seq, A.u_step, P, t0, n, u);
-      load_steps<T, V>(A.dy, A.y_seq, A.y_step, P, t0, n, d);
-      if (GATED) load_steps<T, V>(A.o, A.o_seq, A.o_step, P, t0, n, o);
-      float h[V];
-#pragma unroll
-      for (int i = 0; i < V; ++i) h[i] = A.saved[((t0 / kSaveSteps) * A.batch + P.b) * A.dim + P.strip + P.lane + i];
-#pragma unroll
-      for (int j = 0; j < kSaveSteps; ++j) {
-        float go[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          const float x = entry<T>(u[j], i), dy = entry<T>(d[j], i);
-          gate(entry<T>(f[j], i), a[j][i], down[j][i]);
-          off[j][i] = (h[i] - x) * a[j][i];
-          h[i] = fmaf(a[j][i], h[i], down[j][i] * x);
-          into[j][i] = dy;
-          if (GATED) {
-            float s, r;
-            gate(entry<T>(o[j], i), s, r);
-            into[j][i] = dy * s;
-            go[i] = dy * h[i] * s * r;
-          }
-          if (j >= n) {
-            a[j][i] = 1.0f;
-            into[j][i] = 0.0f;
-          }
-        }
-        if (GATED && P.in && j < n) store_step<T, V>(A.dout, A.do_seq, A.do_step, P, t0 + j, go);
-      }
-#pragma unroll
-      for (int j = kSaveSteps - 1; j >= 0; --j) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          me[i] = (me[i] + into[j][i]) * a[j][i];
-          ma[i] *= a[j][i];
-        }
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      S.a[turn][wave][lane][i] = ma[i];
-      S.h[turn][wave][lane][i] = me[i];
-    }
-    __syncthreads();
-    float g[V];
-    for (int w = waves - 1; w >= 0; --w)
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        if (w == wave) g[i] = e[i];
-        e[i] = fmaf(S.a[turn][w][lane][i], e[i], S.h[turn][w][lane][i]);
-      }
-    if (!P.in || all == 0) continue;
-#pragma unroll
-    for (int j = kSaveSteps - 1; j >= 0; --j) {
-      if (j >= all) continue;
-      float gf[V], gu[V];
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        gf[i] = gu[i] = 0.0f;
-        if (j < n) {
-          g[i] += into[j][i];
-          gu[i] = g[i] * down[j][i];
-          gf[i] = gu[i] * off[j][i];
-          g[i] *= a[j][i];
-        }
-      }
-      store_step<T, V>(A.df, A.df_seq, A.df_step, P, t0 + j, gf);
-      store_step<T, V>(A.du, A.du_seq, A.du_step, P, t0 + j, gu);
-      if (GATED && j >= n) {
-        const float zero[V] = {};
-        store_step<T, V>(A.dout, A.do_seq, A.do_step, P, t0 + j, zero);
-      }
-    }
-  }
-  if (A.dh0 && P.in && wave == 0 && P.segment == 0)
-#pragma unroll
-    for (int i = 0; i < V; ++i) A.dh0[P.b * A.dim + P.strip + P.lane + i] = e[i];
-}
-
-// parts[s] = the map of segment s; the first one's is not needed.
-template <class T, int V, bool GATED>
-__global__ __launch_bounds__(64 * kRecurWaves) void k_recur_back_part(RecurArgs A) {
-  __shared__ RecurMaps<V> S;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  RecurPlace P = recur_place<V>(A);
-  P.begin += A.segment_steps;     // from the second segment on
-  const int64_t piece = A.segment_steps / waves;
-  float ma[V], me[V];
+  __shared__ RecurShared<V> S;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+  const RecurPlace P = recur_place<V, CHAIN, true>(A, &S.taken);
+  const int64_t state = P.b * A.dim + P.strip + P.lane, t0 = P.begin + kSaveSteps * wave;
+  const int n = steps_left(P.len, t0), all = steps_left(A.steps, t0);
+  // of each step: a, dy s, 1 - a, (h_{t-1} - u) a
+  float e[V], a[kSaveSteps][V], into[kSaveSteps][V], down[kSaveSteps][V], off[kSaveSteps][V], ma[V], me[V], after[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
+    e[i] = CHAIN || !A.dlast ? 0.0f : A.dlast[state + i];
     ma[i] = 1.0f;
     me[i] = 0.0f;
   }
-  for (int64_t t0 = P.begin + (wave + 1) * piece - kSaveSteps; t0 >= P.begin + wave * piece; t0 -= kSaveSteps) {
-    const int n = steps_left(P.len, t0);
-    if (n == 0) continue;
-    uint32_t f[kSaveSteps], o[kSaveSteps], d[kSaveSteps];
+  if (n > 0) {
+    uint32_t f[kSaveSteps], u[kSaveSteps], o[kSaveSteps], d[kSaveSteps];
     load_steps<T, V>(A.f, A.f_seq, A.f_step, P, t0, n, f);
+    load_steps<T, V>(A.u, A.u_seq, A.u_step, P, t0, n, u);
     load_steps<T, V>(A.dy, A.y_seq, A.y_step, P, t0, n, d);
     if (GATED) load_steps<T, V>(A.o, A.o_seq, A.o_step, P, t0, n, o);
+    float h[V];
 #pragma unroll
-    for (int j = kSaveSteps - 1; j >= 0; --j) {
-      if (j >= n) continue;
+    for (int i = 0; i < V; ++i) h[i] = A.saved[(t0 / kSaveSteps) * A.batch * A.dim + state + i];
+#pragma unroll
+    for (int j = 0; j < kSaveSteps; ++j) {
+      float go[V];
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        const float a = gate(entry<T>(f[j], i));
-        float into = entry<T>(d[j], i);
-        if (GATED) into *= gate(entry<T>(o[j], i));
-        me[i] = (me[i] + into) * a;
-        ma[i] *= a;
+        const float x = entry<T>(u[j], i), dy = entry<T>(d[j], i);
+        gate(entry<T>(f[j], i), a[j][i], down[j][i]);
+        off[j][i] = (h[i] - x) * a[j][i];
+        h[i] = fmaf(a[j][i], h[i], down[j][i] * x);
+        into[j][i] = dy;
+        if (GATED) {
+          float s, r;
+          gate(entry<T>(o[j], i), s, r);
+          into[j][i] = dy * s;
+          go[i] = dy * h[i] * s * r;
+        }
+        if (j >= n) {
+          a[j][i] = 1.0f;
+          into[j][i] = 0.0f;
+        }
+      }
+      if (GATED && P.in && j < n) store_step<T, V>(A.dout, A.do_seq, A.do_step, P, t0 + j, go);
+    }
+#pragma unroll
+    for (int j = kSaveSteps - 1; j >= 0; --j)
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        me[i] = (me[i] + into[j][i]) * a[j][i];
+        ma[i] *= a[j][i];
+      }
+  }
+  recur_carry<V, CHAIN>(A, P, S, waves - 1 - wave, waves, ma, me, e, after);
+  if (!P.in) return;
+  if (A.dh0 && P.tile == 0 && wave == 0)
+#pragma unroll
+    for (int i = 0; i < V; ++i) A.dh0[state + i] = after[i];
+#pragma unroll
+  for (int j = kSaveSteps - 1; j >= 0; --j) {
+    if (j >= all) continue;
+    float gf[V], gu[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      gf[i] = gu[i] = 0.0f;
+      if (j < n) {
+        e[i] += into[j][i];
+        gu[i] = e[i] * down[j][i];
+        gf[i] = gu[i] * off[j][i];
+        e[i] *= a[j][i];
       }
     }
-  }
-#pragma unroll
-  for (int i = 0; i < V; ++i) {
-    S.a[0][wave][lane][i] = ma[i];
-    S.h[0][wave][lane][i] = me[i];
-  }
-  __syncthreads();
-  if (wave != waves - 1 || !P.in) return;
-#pragma unroll
-  for (int i = 0; i < V; ++i) {
-    for (int w = waves - 2; w >= 0; --w) {
-      me[i] = fmaf(S.a[0][w][lane][i], me[i], S.h[0][w][lane][i]);
-      ma[i] *= S.a[0][w][lane][i];
+    store_step<T, V>(A.df, A.df_seq, A.df_step, P, t0 + j, gf);
+    store_step<T, V>(A.du, A.du_seq, A.du_step, P, t0 + j, gu);
+    if (GATED && j >= n) {
+      const float zero[V] = {};
+      store_step<T, V>(A.dout, A.do_seq, A.do_step, P, t0 + j, zero);
     }
-    A.parts[((int64_t)(P.segment + 1) * A.batch + P.b) * A.dim + P.strip + P.lane + i] = make_float2(ma[i], me[i]);
   }
 }
 

@@ -33,11 +33,6 @@ thread_local int g_last_hip_error = 0;
   } while (0)
 
 constexpr int64_t kMaxIndex = (int64_t)1 << 31;
-#ifndef FEW
-#define FEW 4096
-#define WANTED 8192
-#endif
-constexpr int64_t kFewWaves = FEW, kWantedWaves = WANTED;
 constexpr int64_t kMaxExtent = (int64_t)1 << 60;   // entries of any array, strides included
 
 int type_bytes(int type) { return type == CHOCO_F32 ? 4 : type == CHOCO_BF16 || type == CHOCO_F16 ? 2 : 0; }
@@ -199,51 +194,55 @@ bool recur_pairs(const choco_recur_config& c, bool gated, bool back, std::initia
   return true;
 }
 
-// Waves of a workgroup, segments of a sequence and their steps, for strips of `width` channels.
+// Chains of tiles (see choco_recur.h) for strips of `width` channels.
 struct RecurPlan {
-  int64_t strips, segments, segment_steps;
+  int64_t strips, chains, tiles, links;
   int waves;
 };
 
 RecurPlan plan_recur(const choco_recur_config& c, int width) {
   RecurPlan P{};
   P.strips = (c.dim + width - 1) / width;
-  P.waves = (int)std::max<int64_t>(1, std::min<int64_t>(kRecurWaves, (c.steps + kSaveSteps - 1) / kSaveSteps));
-  const int64_t round = (int64_t)kSaveSteps * P.waves, rounds = std::max<int64_t>(1, (c.steps + round - 1) / round);
-  const int64_t waves = P.strips * c.batch * P.waves;
-  P.segments = 1;
-  if (waves < kFewWaves && rounds >= 4) {
-    P.segments = std::min<int64_t>(std::min<int64_t>(kMaxSegments, rounds / 2), (kWantedWaves + waves - 1) / waves);
-  }
-  const int64_t each = (rounds + P.segments - 1) / P.segments;
-  P.segments = std::max<int64_t>(1, (rounds + each - 1) / each);
-  P.segment_steps = each * round;
+  P.chains = P.strips * c.batch;
+  P.tiles = std::max<int64_t>(1, (c.steps + kTileSteps - 1) / kTileSteps);
+  P.links = (P.tiles + kChainTiles - 1) / kChainTiles;
+  P.waves = P.tiles > 1 ? kRecurWaves : (int)std::max<int64_t>(1, (c.steps + kSaveSteps - 1) / kSaveSteps);
   return P;
 }
+
+// Words of a chain's maps and states, and of the whole workspace with the counters.
+double chain_words(const RecurPlan& P, int width) { return P.tiles > 1 ? (double)P.chains * (double)(P.tiles + P.links) * width : 0.0; }
 
 size_t recur_workspace(const choco_recur_config& c) {
   // (a call takes the wide strips or the narrow ones, whatever its pointers allow: room for either)
   size_t most = 0;
   for (int width : {64, 128}) {
     const RecurPlan P = plan_recur(c, width);
-    if (P.segments > 1) most = std::max(most, (size_t)P.segments * c.batch * c.dim * sizeof(float2));
+    if (P.tiles > 1) most = std::max(most, (size_t)chain_words(P, width) * sizeof(uint64_t) + (size_t)P.chains * kTakenWords * sizeof(uint32_t));
   }
   return most;
 }
 
 // The launches of a call: false where a grid does not hold them.
-bool place_recur(const choco_recur_config& c, bool pairs, void* workspace, RecurArgs& A, dim3& grid, dim3& part, int& threads) {
-  const RecurPlan P = plan_recur(c, pairs ? 128 : 64);
-  const double groups = (double)P.strips * (double)c.batch;
-  if (!launch_fits(groups * (double)P.segments, 64 * P.waves)) return false;
-  A.strips = (uint32_t)P.strips;
-  A.segments = (uint32_t)P.segments;
-  A.segment_steps = P.segment_steps;
-  A.parts = P.segments > 1 ? (float2*)workspace : nullptr;
+bool place_recur(const choco_recur_config& c, int width, void* workspace, RecurArgs& A, dim3& grid, int& threads) {
+  const RecurPlan P = plan_recur(c, width);
   threads = 64 * P.waves;
-  grid = dim3((uint32_t)(P.strips * c.batch * P.segments));
-  part = dim3((uint32_t)(P.strips * c.batch * (P.segments - 1)));
+  if (!launch_fits((double)P.chains * (double)P.tiles, threads)) return false;
+  A.strips = (uint32_t)P.strips;
+  A.chains = (uint32_t)P.chains;
+  A.tiles = (uint32_t)P.tiles;
+  A.links = (uint32_t)P.links;
+  A.maps = (uint64_t*)workspace;
+  A.states = A.maps + P.chains * P.tiles * width;
+  A.taken = (uint32_t*)(A.states + P.chains * P.links * width);
+  grid = dim3((uint32_t)(P.chains * P.tiles));
   return true;
+}
+
+// Launches what starts the chains (`first`: the states before them) of a call that has any.
+void start_chains(const RecurArgs& A, int width, const float* first, hipStream_t stream) {
+  const double words = (double)A.chains * (A.tiles + A.links) * width + A.chains;
+  k_recur_chains<<<dim3((uint32_t)std::min(2048.0, words / 256 + 1)), 256, 0, stream>>>(A, first, width);
 }
 
 // calls fn with the channels a lane takes (a type's only where it can be two)
@@ -254,6 +253,8 @@ void with_width(bool pairs, Fn&& fn) {
   }
   fn(std::integral_constant<int, 1>{});
 }
+
+static_assert(kSaveSteps == CHOCO_RECUR_SAVE_STEPS, "the header says what is kept");
 
 int64_t saved_floats(const choco_recur_config& c) {
   return (c.steps + CHOCO_RECUR_SAVE_STEPS - 1) / CHOCO_RECUR_SAVE_STEPS * c.batch * c.dim;
@@ -526,17 +527,22 @@ int choco_recur_forward(const choco_recur_config* cfg, const void* f_dev, const 
   A.h_last = h_last_dev;
   A.saved = saved_dev;
   const bool pairs = recur_pairs(c, o_dev, false, {f_dev, u_dev, o_dev, y_dev});
-  dim3 grid, part;
+  const int width = pairs ? 128 : 64;
+  dim3 grid;
   int threads;
-  if (!place_recur(c, pairs, workspace_dev, A, grid, part, threads)) return CHOCO_E_UNSUPPORTED;
+  if (!place_recur(c, width, workspace_dev, A, grid, threads)) return CHOCO_E_UNSUPPORTED;
   const hipStream_t stream = (hipStream_t)c.stream;
+  if (A.tiles > 1) start_chains(A, width, h0_dev, stream);
   with_type(c.type, [&](auto x) {
     using T = decltype(x);
-    with_width<T>(pairs, [&](auto width) {
-      constexpr int V = decltype(width)::value;
-      if (A.parts) k_recur_part<T, V><<<part, threads, 0, stream>>>(A);
-      if (o_dev) k_recur<T, V, true><<<grid, threads, 0, stream>>>(A);
-      else k_recur<T, V, false><<<grid, threads, 0, stream>>>(A);
+    with_width<T>(pairs, [&](auto each) {
+      constexpr int V = decltype(each)::value;
+      const auto launch = [&](auto gated) {
+        if (A.tiles > 1) k_recur<T, V, decltype(gated)::value, true><<<grid, threads, 0, stream>>>(A);
+        else k_recur<T, V, decltype(gated)::value, false><<<grid, threads, 0, stream>>>(A);
+      };
+      if (o_dev) launch(std::true_type{});
+      else launch(std::false_type{});
     });
   });
   TRY_HIP(hipGetLastError());
@@ -573,21 +579,22 @@ int choco_recur_backward(const choco_recur_config* cfg, const void* f_dev, const
   A.dout = do_dev;
   A.dh0 = dh0_dev;
   const bool pairs = recur_pairs(c, o_dev, true, {f_dev, u_dev, o_dev, dy_dev, df_dev, du_dev, do_dev});
-  dim3 grid, part;
+  const int width = pairs ? 128 : 64;
+  dim3 grid;
   int threads;
-  if (!place_recur(c, pairs, workspace_dev, A, grid, part, threads)) return CHOCO_E_UNSUPPORTED;
+  if (!place_recur(c, width, workspace_dev, A, grid, threads)) return CHOCO_E_UNSUPPORTED;
   const hipStream_t stream = (hipStream_t)c.stream;
+  if (A.tiles > 1) start_chains(A, width, dlast_dev, stream);
   with_type(c.type, [&](auto x) {
     using T = decltype(x);
-    with_width<T>(pairs, [&](auto width) {
-      constexpr int V = decltype(width)::value;
-      if (o_dev) {
-        if (A.parts) k_recur_back_part<T, V, true><<<part, threads, 0, stream>>>(A);
-        k_recur_back<T, V, true><<<grid, threads, 0, stream>>>(A);
-      } else {
-        if (A.parts) k_recur_back_part<T, V, false><<<part, threads, 0, stream>>>(A);
-        k_recur_back<T, V, false><<<grid, threads, 0, stream>>>(A);
-      }
+    with_width<T>(pairs, [&](auto each) {
+      constexpr int V = decltype(each)::value;
+      const auto launch = [&](auto gated) {
+        if (A.tiles > 1) k_recur_back<T, V, decltype(gated)::value, true><<<grid, threads, 0, stream>>>(A);
+        else k_recur_back<T, V, decltype(gated)::value, false><<<grid, threads, 0, stream>>>(A);
+      };
+      if (o_dev) launch(std::true_type{});
+      else launch(std::false_type{});
     });
   });
   TRY_HIP(hipGetLastError());

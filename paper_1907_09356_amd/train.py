@@ -15,7 +15,7 @@ from .binding import _check
 
 F32, BF16, F16 = 0, 1, 2
 I32, I64 = 0, 1
-SAVE_STEPS, BLOCK = 16, 256
+SAVE_STEPS, BLOCK = 8, 256
 TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 TOKEN_TYPES = {torch.int32: I32, torch.int64: I64}
 

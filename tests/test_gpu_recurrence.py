@@ -110,7 +110,7 @@ def both(batch, steps, dim, dtype, gated, lengths, seed, state=True, **kw):
     check("y", y, wy, by, dtype)
     check("h", last, wl, bl, torch.float32)
     for k in range(saved.shape[0]):
-        check("saved", saved[k], H[16 * k], BH[16 * k], torch.float32)
+        check("saved", saved[k], H[T.SAVE_STEPS * k], BH[T.SAVE_STEPS * k], torch.float32)
     # without `saved` the same bits
     y2, last2, none = T.recurrence(cf, cu, co, h0=h0.cuda() if state else None, lengths=ln)
     assert none is None and torch.equal(y2, y) and torch.equal(last2, last)
@@ -341,7 +341,7 @@ def test_other_streams_and_graphs(steps, dim):
 
 def test_arguments_are_checked():
     f = torch.zeros((2, 20, 8), device="cuda")
-    saved = torch.zeros((2, 2, 8), device="cuda")
+    saved = torch.zeros((3, 2, 8), device="cuda")
     for bad in (lambda: T.recurrence(f, f.bfloat16()), lambda: T.recurrence(f, f[:, :3]), lambda: T.recurrence(f.double(), f.double()),
                 lambda: T.recurrence(f, f, h0=saved[0, :1]), lambda: T.recurrence(f, f, lengths=torch.zeros(2, device="cuda")),
                 lambda: T.recurrence(f.transpose(1, 2), f.transpose(1, 2)), lambda: T.recurrence_grad(f, f, saved[:1], f),
