@@ -24,15 +24,13 @@
 
 namespace choco {
 
-#ifndef SAVE
-#define SAVE 8
-#define RW 16
-#define CT 8
-#endif
-constexpr int kSaveSteps = SAVE;    // steps of a wave; the forward pass keeps the state before every so many
-constexpr int kRecurWaves = RW;     // most waves of a workgroup
-constexpr int kTileSteps = kSaveSteps * kRecurWaves;
-constexpr int kChainTiles = CT;
+constexpr int kSaveSteps = 8;       // the forward pass keeps the state before every so many
+constexpr int kRecurWaves = 16;     // most waves of a workgroup
+constexpr int kAloneSteps = 8;      // a sequence of one tile: steps of a wave, up to kRecurWaves of them
+constexpr int kChainWaves = 8;      // chains: waves of a tile, and steps of a wave
+constexpr int kForwardSteps = 16;
+constexpr int back_steps(int v) { return v == 1 ? 16 : 8; }
+constexpr int kChainTiles = 16;
 constexpr int kMostPolls = 1 << 20;
 constexpr int kTakenWords = 64;     // from one chain's counter to the next: additions to one line wait for each other, 11 ns each
 
@@ -129,7 +127,7 @@ struct RecurPlace {
 };
 
 template <int V, bool CHAIN, bool BACK>
-__device__ __forceinline__ RecurPlace recur_place(const RecurArgs& A, uint32_t* taken) {
+__device__ __forceinline__ RecurPlace recur_place(const RecurArgs& A, int tile_steps, uint32_t* taken) {
   RecurPlace P;
   P.chain = CHAIN ? blockIdx.x % A.chains : blockIdx.x;
   P.turn = 0;
@@ -145,16 +143,20 @@ __device__ __forceinline__ RecurPlace recur_place(const RecurArgs& A, uint32_t* 
   P.in = P.strip + P.lane < A.dim;
   if (!P.in) P.lane = 0;
   P.len = steps_of(A, P.b);
-  P.begin = (int64_t)P.tile * kTileSteps;
+  P.begin = (int64_t)P.tile * tile_steps;
   return P;
 }
 
+// A sequence of one tile; chains through the caches, with their results written past them, or read past them as well.
+enum { kAlone = 0, kThrough = 1, kPastOut = 2, kPast = 3 };
+
 // What a lane holds of a step, in one register: an entry of 32 bits, or two or one of 16.
-template <class T, int V>
+template <class T, int V, bool PAST>
 __device__ __forceinline__ uint32_t load_word(const T* p) {
   static_assert(V * sizeof(T) <= 4, "one register");
-  if constexpr (V * sizeof(T) == 4) return *reinterpret_cast<const uint32_t*>(p);
-  else return *reinterpret_cast<const uint16_t*>(p);
+  using Word = std::conditional_t<V * sizeof(T) == 4, uint32_t, uint16_t>;
+  if constexpr (PAST) return __builtin_nontemporal_load(reinterpret_cast<const Word*>(p));
+  else return *reinterpret_cast<const Word*>(p);
 }
 template <class T>
 __device__ __forceinline__ float entry(uint32_t word, int i) {
@@ -164,37 +166,47 @@ __device__ __forceinline__ float entry(uint32_t word, int i) {
 }
 
 // Rows t .. t + n - 1 of a lane's channels, n >= 1; the rest of the wave's steps repeat the last row.
-template <class T, int V>
+template <class T, int V, bool PAST, int K>
 __device__ __forceinline__ void load_steps(const void* base, int64_t seq, int64_t step, const RecurPlace& P, int64_t t, int n,
-                                           uint32_t (&x)[kSaveSteps]) {
+                                           uint32_t (&x)[K]) {
   const T* p = (const T*)base + P.b * seq + t * step + P.strip;
 #pragma unroll
-  for (int j = 0; j < kSaveSteps; ++j) {
-    x[j] = load_word<T, V>(p + P.lane);
+  for (int j = 0; j < K; ++j) {
+    x[j] = load_word<T, V, PAST>(p + P.lane);
     p += j + 1 < n ? step : 0;
   }
 }
 
-template <class T, int V>
+template <class T, int V, bool PAST>
 __device__ __forceinline__ void store_step(void* base, int64_t seq, int64_t step, const RecurPlace& P, int64_t t, const float (&x)[V]) {
-  store_floats<T, V>((T*)base + P.b * seq + t * step + P.strip + P.lane, x);
+  T* p = (T*)base + P.b * seq + t * step + P.strip + P.lane;
+  if constexpr (PAST) {
+    typedef T Entries __attribute__((ext_vector_type(V)));
+    Entries v;
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = from_float<T>(x[i]);
+    __builtin_nontemporal_store(v, reinterpret_cast<Entries*>(p));
+  } else {
+    store_floats<T, V>(p, x);
+  }
 }
 
+template <int K>
 __device__ __forceinline__ int steps_left(int64_t end, int64_t t) {
-  return __builtin_amdgcn_readfirstlane(end <= t ? 0 : end - t < kSaveSteps ? (int)(end - t) : kSaveSteps);
+  return __builtin_amdgcn_readfirstlane(end <= t ? 0 : end - t < K ? (int)(end - t) : K);
 }
 
-template <int V>
+template <int V, int W>
 struct RecurShared {
-  float a[kRecurWaves][64][V], h[kRecurWaves][64][V];               // the waves' maps, in the order of the recurrence
+  float a[W][64][V], h[W][64][V];               // the waves' maps, in the order of the recurrence
   float link_a[kChainTiles][64][V], link_h[kChainTiles][64][V];     // those of the tiles before in the link; last: the state before it
   uint32_t taken;
 };
 
 // From the waves' maps (m_a, m_h; `turn`: a wave's place in the order of the recurrence) and the state `h` before the tile
 // (outside chains: given) to the state before the wave's own steps; the last wave's ends as the one after the tile.
-template <int V, bool CHAIN>
-__device__ __forceinline__ void recur_carry(const RecurArgs& A, const RecurPlace& P, RecurShared<V>& S, int turn, int waves,
+template <int V, bool CHAIN, int W>
+__device__ __forceinline__ void recur_carry(const RecurArgs& A, const RecurPlace& P, RecurShared<V, W>& S, int turn, int waves,
                                             const float (&ma)[V], const float (&mh)[V], float (&h)[V], float (&after)[V]) {
   const int lane = threadIdx.x & 63;
 #pragma unroll
@@ -250,15 +262,17 @@ __device__ __forceinline__ void recur_carry(const RecurArgs& A, const RecurPlace
       publish(A.states + ((int64_t)P.chain * A.links + P.turn / kChainTiles + 1) * (64 * V) + lane * V + i, 0.0f, after[i]);
 }
 
-template <class T, int V, bool GATED, bool CHAIN>
-__global__ __launch_bounds__(64 * kRecurWaves) void k_recur(RecurArgs A) {
-  __shared__ RecurShared<V> S;
+template <class T, int V, bool GATED, int MODE>
+__global__ __launch_bounds__(64 * (MODE != kAlone ? kChainWaves : kRecurWaves)) void k_recur(RecurArgs A) {
+  constexpr bool CHAIN = MODE != kAlone;
+  constexpr int K = CHAIN ? kForwardSteps : kAloneSteps, W = CHAIN ? kChainWaves : kRecurWaves;
+  __shared__ RecurShared<V, W> S;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
-  const RecurPlace P = recur_place<V, CHAIN, false>(A, &S.taken);
-  const int64_t state = P.b * A.dim + P.strip + P.lane, t0 = P.begin + kSaveSteps * wave;
-  const int n = steps_left(P.len, t0), all = steps_left(A.steps, t0);
-  float h[V], a[kSaveSteps][V], b[kSaveSteps][V], ma[V], mh[V], after[V];
-  uint32_t o[kSaveSteps];
+  const RecurPlace P = recur_place<V, CHAIN, false>(A, K * W, &S.taken);
+  const int64_t state = P.b * A.dim + P.strip + P.lane, t0 = P.begin + K * wave;
+  const int n = steps_left<K>(P.len, t0), all = steps_left<K>(A.steps, t0);
+  float h[V], a[K][V], b[K][V], ma[V], mh[V], after[V];
+  uint32_t o[K];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     h[i] = CHAIN || !A.h0 ? 0.0f : A.h0[state + i];
@@ -266,12 +280,12 @@ __global__ __launch_bounds__(64 * kRecurWaves) void k_recur(RecurArgs A) {
     mh[i] = 0.0f;
   }
   if (n > 0) {
-    uint32_t f[kSaveSteps], u[kSaveSteps];
-    load_steps<T, V>(A.f, A.f_seq, A.f_step, P, t0, n, f);
-    load_steps<T, V>(A.u, A.u_seq, A.u_step, P, t0, n, u);
-    if (GATED) load_steps<T, V>(A.o, A.o_seq, A.o_step, P, t0, n, o);
+    uint32_t f[K], u[K];
+    load_steps<T, V, MODE == kPast, K>(A.f, A.f_seq, A.f_step, P, t0, n, f);
+    load_steps<T, V, MODE == kPast, K>(A.u, A.u_seq, A.u_step, P, t0, n, u);
+    if (GATED) load_steps<T, V, MODE == kPast, K>(A.o, A.o_seq, A.o_step, P, t0, n, o);
 #pragma unroll
-    for (int j = 0; j < kSaveSteps; ++j)
+    for (int j = 0; j < K; ++j)
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         float down;
@@ -285,42 +299,45 @@ __global__ __launch_bounds__(64 * kRecurWaves) void k_recur(RecurArgs A) {
         ma[i] *= a[j][i];
       }
   }
-  recur_carry<V, CHAIN>(A, P, S, wave, waves, ma, mh, h, after);
+  recur_carry<V, CHAIN, W>(A, P, S, wave, waves, ma, mh, h, after);
   if (!P.in) return;
   if (A.h_last && P.tile + 1 == A.tiles && wave == waves - 1)
 #pragma unroll
     for (int i = 0; i < V; ++i) A.h_last[state + i] = after[i];
   if (all == 0) return;
-  if (A.saved)
 #pragma unroll
-    for (int i = 0; i < V; ++i) A.saved[(t0 / kSaveSteps) * A.batch * A.dim + state + i] = h[i];
+  for (int j = 0; j < K; ++j) {
+    if (j < all) {
+      if (j % kSaveSteps == 0 && A.saved)
 #pragma unroll
-  for (int j = 0; j < kSaveSteps; ++j) {
-    if (j >= all) break;
-    float out[V];
+        for (int i = 0; i < V; ++i) A.saved[((t0 + j) / kSaveSteps) * A.batch * A.dim + state + i] = h[i];
+      float out[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      out[i] = 0.0f;
-      if (j < n) {
-        h[i] = fmaf(a[j][i], h[i], b[j][i]);
-        out[i] = GATED ? gate(entry<T>(o[j], i)) * h[i] : h[i];
+      for (int i = 0; i < V; ++i) {
+        out[i] = 0.0f;
+        if (j < n) {
+          h[i] = fmaf(a[j][i], h[i], b[j][i]);
+          out[i] = GATED ? gate(entry<T>(o[j], i)) * h[i] : h[i];
+        }
       }
+      store_step<T, V, MODE != kAlone && MODE != kThrough>(A.y, A.y_seq, A.y_step, P, t0 + j, out);
     }
-    store_step<T, V>(A.y, A.y_seq, A.y_step, P, t0 + j, out);
   }
 }
 
 // Backward: the same from the last steps back, with the map of a step on a_{t+1} e_{t+1}: e -> a (e + dy s).  The states
 // before each wave's steps are those that the forward pass kept.
-template <class T, int V, bool GATED, bool CHAIN>
-__global__ __launch_bounds__(64 * kRecurWaves) void k_recur_back(RecurArgs A) {
-  __shared__ RecurShared<V> S;
+template <class T, int V, bool GATED, int MODE>
+__global__ __launch_bounds__(64 * (MODE != kAlone ? kChainWaves : kRecurWaves)) void k_recur_back(RecurArgs A) {
+  constexpr bool CHAIN = MODE != kAlone;
+  constexpr int K = CHAIN ? back_steps(V) : kAloneSteps, W = CHAIN ? kChainWaves : kRecurWaves;
+  __shared__ RecurShared<V, W> S;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
-  const RecurPlace P = recur_place<V, CHAIN, true>(A, &S.taken);
-  const int64_t state = P.b * A.dim + P.strip + P.lane, t0 = P.begin + kSaveSteps * wave;
-  const int n = steps_left(P.len, t0), all = steps_left(A.steps, t0);
+  const RecurPlace P = recur_place<V, CHAIN, true>(A, K * W, &S.taken);
+  const int64_t state = P.b * A.dim + P.strip + P.lane, t0 = P.begin + K * wave;
+  const int n = steps_left<K>(P.len, t0), all = steps_left<K>(A.steps, t0);
   // of each step: a, dy s, 1 - a, (h_{t-1} - u) a
-  float e[V], a[kSaveSteps][V], into[kSaveSteps][V], down[kSaveSteps][V], off[kSaveSteps][V], ma[V], me[V], after[V];
+  float e[V], a[K][V], into[K][V], down[K][V], off[K][V], ma[V], me[V], after[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     e[i] = CHAIN || !A.dlast ? 0.0f : A.dlast[state + i];
@@ -328,16 +345,16 @@ __global__ __launch_bounds__(64 * kRecurWaves) void k_recur_back(RecurArgs A) {
     me[i] = 0.0f;
   }
   if (n > 0) {
-    uint32_t f[kSaveSteps], u[kSaveSteps], o[kSaveSteps], d[kSaveSteps];
-    load_steps<T, V>(A.f, A.f_seq, A.f_step, P, t0, n, f);
-    load_steps<T, V>(A.u, A.u_seq, A.u_step, P, t0, n, u);
-    load_steps<T, V>(A.dy, A.y_seq, A.y_step, P, t0, n, d);
-    if (GATED) load_steps<T, V>(A.o, A.o_seq, A.o_step, P, t0, n, o);
+    uint32_t f[K], u[K], o[K], d[K];
+    load_steps<T, V, MODE == kPast, K>(A.f, A.f_seq, A.f_step, P, t0, n, f);
+    load_steps<T, V, MODE == kPast, K>(A.u, A.u_seq, A.u_step, P, t0, n, u);
+    load_steps<T, V, MODE == kPast, K>(A.dy, A.y_seq, A.y_step, P, t0, n, d);
+    if (GATED) load_steps<T, V, MODE == kPast, K>(A.o, A.o_seq, A.o_step, P, t0, n, o);
     float h[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) h[i] = A.saved[(t0 / kSaveSteps) * A.batch * A.dim + state + i];
 #pragma unroll
-    for (int j = 0; j < kSaveSteps; ++j) {
+    for (int j = 0; j < K; ++j) {
       float go[V];
 #pragma unroll
       for (int i = 0; i < V; ++i) {
@@ -357,40 +374,41 @@ __global__ __launch_bounds__(64 * kRecurWaves) void k_recur_back(RecurArgs A) {
           into[j][i] = 0.0f;
         }
       }
-      if (GATED && P.in && j < n) store_step<T, V>(A.dout, A.do_seq, A.do_step, P, t0 + j, go);
+      if (GATED && P.in && j < n) store_step<T, V, MODE != kAlone && MODE != kThrough>(A.dout, A.do_seq, A.do_step, P, t0 + j, go);
     }
 #pragma unroll
-    for (int j = kSaveSteps - 1; j >= 0; --j)
+    for (int j = K - 1; j >= 0; --j)
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         me[i] = (me[i] + into[j][i]) * a[j][i];
         ma[i] *= a[j][i];
       }
   }
-  recur_carry<V, CHAIN>(A, P, S, waves - 1 - wave, waves, ma, me, e, after);
+  recur_carry<V, CHAIN, W>(A, P, S, waves - 1 - wave, waves, ma, me, e, after);
   if (!P.in) return;
   if (A.dh0 && P.tile == 0 && wave == 0)
 #pragma unroll
     for (int i = 0; i < V; ++i) A.dh0[state + i] = after[i];
 #pragma unroll
-  for (int j = kSaveSteps - 1; j >= 0; --j) {
-    if (j >= all) continue;
-    float gf[V], gu[V];
+  for (int j = K - 1; j >= 0; --j) {
+    if (j < all) {
+      float gf[V], gu[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      gf[i] = gu[i] = 0.0f;
-      if (j < n) {
-        e[i] += into[j][i];
-        gu[i] = e[i] * down[j][i];
-        gf[i] = gu[i] * off[j][i];
-        e[i] *= a[j][i];
+      for (int i = 0; i < V; ++i) {
+        gf[i] = gu[i] = 0.0f;
+        if (j < n) {
+          e[i] += into[j][i];
+          gu[i] = e[i] * down[j][i];
+          gf[i] = gu[i] * off[j][i];
+          e[i] *= a[j][i];
+        }
       }
-    }
-    store_step<T, V>(A.df, A.df_seq, A.df_step, P, t0 + j, gf);
-    store_step<T, V>(A.du, A.du_seq, A.du_step, P, t0 + j, gu);
-    if (GATED && j >= n) {
-      const float zero[V] = {};
-      store_step<T, V>(A.dout, A.do_seq, A.do_step, P, t0 + j, zero);
+      store_step<T, V, MODE != kAlone && MODE != kThrough>(A.df, A.df_seq, A.df_step, P, t0 + j, gf);
+      store_step<T, V, MODE != kAlone && MODE != kThrough>(A.du, A.du_seq, A.du_step, P, t0 + j, gu);
+      if (GATED && j >= n) {
+        const float zero[V] = {};
+        store_step<T, V, MODE != kAlone && MODE != kThrough>(A.dout, A.do_seq, A.do_step, P, t0 + j, zero);
+      }
     }
   }
 }

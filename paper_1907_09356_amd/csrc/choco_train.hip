@@ -194,19 +194,24 @@ bool recur_pairs(const choco_recur_config& c, bool gated, bool back, std::initia
   return true;
 }
 
-// Chains of tiles (see choco_recur.h) for strips of `width` channels.
+// Chains of tiles (see choco_recur.h) for strips of `width` channels, a wave of a chain taking so many steps.
 struct RecurPlan {
   int64_t strips, chains, tiles, links;
   int waves;
 };
 
-RecurPlan plan_recur(const choco_recur_config& c, int width) {
+RecurPlan plan_recur(const choco_recur_config& c, int width, int steps) {
   RecurPlan P{};
   P.strips = (c.dim + width - 1) / width;
   P.chains = P.strips * c.batch;
-  P.tiles = std::max<int64_t>(1, (c.steps + kTileSteps - 1) / kTileSteps);
+  P.waves = (int)std::max<int64_t>(1, (c.steps + kAloneSteps - 1) / kAloneSteps);
+  P.tiles = 1;
+  if (c.steps > kAloneSteps * kRecurWaves) {
+    P.waves = kChainWaves;
+    const int64_t tile = (int64_t)P.waves * steps;
+    P.tiles = (c.steps + tile - 1) / tile;
+  }
   P.links = (P.tiles + kChainTiles - 1) / kChainTiles;
-  P.waves = P.tiles > 1 ? kRecurWaves : (int)std::max<int64_t>(1, (c.steps + kSaveSteps - 1) / kSaveSteps);
   return P;
 }
 
@@ -214,18 +219,19 @@ RecurPlan plan_recur(const choco_recur_config& c, int width) {
 double chain_words(const RecurPlan& P, int width) { return P.tiles > 1 ? (double)P.chains * (double)(P.tiles + P.links) * width : 0.0; }
 
 size_t recur_workspace(const choco_recur_config& c) {
-  // (a call takes the wide strips or the narrow ones, whatever its pointers allow: room for either)
+  // (a call takes the wide strips or the narrow ones, whatever its pointers allow: room for either, and for both passes)
   size_t most = 0;
-  for (int width : {64, 128}) {
-    const RecurPlan P = plan_recur(c, width);
-    if (P.tiles > 1) most = std::max(most, (size_t)chain_words(P, width) * sizeof(uint64_t) + (size_t)P.chains * kTakenWords * sizeof(uint32_t));
-  }
+  for (int v : {1, 2})
+    for (int steps : {kForwardSteps, back_steps(v)}) {
+      const RecurPlan P = plan_recur(c, 64 * v, steps);
+      if (P.tiles > 1) most = std::max(most, (size_t)chain_words(P, 64 * v) * sizeof(uint64_t) + (size_t)P.chains * kTakenWords * sizeof(uint32_t));
+    }
   return most;
 }
 
 // The launches of a call: false where a grid does not hold them.
-bool place_recur(const choco_recur_config& c, int width, void* workspace, RecurArgs& A, dim3& grid, int& threads) {
-  const RecurPlan P = plan_recur(c, width);
+bool place_recur(const choco_recur_config& c, int width, int steps, void* workspace, RecurArgs& A, dim3& grid, int& threads) {
+  const RecurPlan P = plan_recur(c, width, steps);
   threads = 64 * P.waves;
   if (!launch_fits((double)P.chains * (double)P.tiles, threads)) return false;
   A.strips = (uint32_t)P.strips;
@@ -243,6 +249,22 @@ bool place_recur(const choco_recur_config& c, int width, void* workspace, RecurA
 void start_chains(const RecurArgs& A, int width, const float* first, hipStream_t stream) {
   const double words = (double)A.chains * (A.tiles + A.links) * width + A.chains;
   k_recur_chains<<<dim3((uint32_t)std::min(2048.0, words / 256 + 1)), 256, 0, stream>>>(A, first, width);
+}
+
+// Past the caches?  A call moves `arrays` arrays of batch x steps x dim.  Small results are left in the caches for what reads them
+// next.  us, through the caches | results past them | all past them: forward, MB moved 134 33.5 | 32.6 | 34.5, 335 77 | 61 | 69,
+// 872 232 | 224 | 210; backward 235 52.0 | 51.1 | 58.6, 587 137 | 129 | 124, 839 228 | 214 | 202.  Tiles alone: 100 22 | 27 | 33.
+int recur_mode(const choco_recur_config& c, const RecurArgs& A, int arrays) {
+  if (A.tiles <= 1) return kAlone;
+  const double mib = (double)c.batch * (double)c.steps * (double)c.dim * type_bytes(c.type) * arrays / 1048576.0;
+  return mib > 384.0 ? kPast : mib > 128.0 ? kPastOut : kThrough;
+}
+template <class Fn>
+void with_mode(int mode, Fn&& fn) {
+  if (mode == kAlone) fn(std::integral_constant<int, kAlone>{});
+  else if (mode == kThrough) fn(std::integral_constant<int, kThrough>{});
+  else if (mode == kPastOut) fn(std::integral_constant<int, kPastOut>{});
+  else fn(std::integral_constant<int, kPast>{});
 }
 
 // calls fn with the channels a lane takes (a type's only where it can be two)
@@ -530,7 +552,7 @@ int choco_recur_forward(const choco_recur_config* cfg, const void* f_dev, const 
   const int width = pairs ? 128 : 64;
   dim3 grid;
   int threads;
-  if (!place_recur(c, width, workspace_dev, A, grid, threads)) return CHOCO_E_UNSUPPORTED;
+  if (!place_recur(c, width, kForwardSteps, workspace_dev, A, grid, threads)) return CHOCO_E_UNSUPPORTED;
   const hipStream_t stream = (hipStream_t)c.stream;
   if (A.tiles > 1) start_chains(A, width, h0_dev, stream);
   with_type(c.type, [&](auto x) {
@@ -538,8 +560,9 @@ int choco_recur_forward(const choco_recur_config* cfg, const void* f_dev, const 
     with_width<T>(pairs, [&](auto each) {
       constexpr int V = decltype(each)::value;
       const auto launch = [&](auto gated) {
-        if (A.tiles > 1) k_recur<T, V, decltype(gated)::value, true><<<grid, threads, 0, stream>>>(A);
-        else k_recur<T, V, decltype(gated)::value, false><<<grid, threads, 0, stream>>>(A);
+        with_mode(recur_mode(c, A, o_dev ? 4 : 3), [&](auto mode) {
+          k_recur<T, V, decltype(gated)::value, decltype(mode)::value><<<grid, threads, 0, stream>>>(A);
+        });
       };
       if (o_dev) launch(std::true_type{});
       else launch(std::false_type{});
@@ -582,7 +605,7 @@ int choco_recur_backward(const choco_recur_config* cfg, const void* f_dev, const
   const int width = pairs ? 128 : 64;
   dim3 grid;
   int threads;
-  if (!place_recur(c, width, workspace_dev, A, grid, threads)) return CHOCO_E_UNSUPPORTED;
+  if (!place_recur(c, width, back_steps(width / 64), workspace_dev, A, grid, threads)) return CHOCO_E_UNSUPPORTED;
   const hipStream_t stream = (hipStream_t)c.stream;
   if (A.tiles > 1) start_chains(A, width, dlast_dev, stream);
   with_type(c.type, [&](auto x) {
@@ -590,8 +613,9 @@ int choco_recur_backward(const choco_recur_config* cfg, const void* f_dev, const
     with_width<T>(pairs, [&](auto each) {
       constexpr int V = decltype(each)::value;
       const auto launch = [&](auto gated) {
-        if (A.tiles > 1) k_recur_back<T, V, decltype(gated)::value, true><<<grid, threads, 0, stream>>>(A);
-        else k_recur_back<T, V, decltype(gated)::value, false><<<grid, threads, 0, stream>>>(A);
+        with_mode(recur_mode(c, A, o_dev ? 7 : 5), [&](auto mode) {
+          k_recur_back<T, V, decltype(gated)::value, decltype(mode)::value><<<grid, threads, 0, stream>>>(A);
+        });
       };
       if (o_dev) launch(std::true_type{});
       else launch(std::false_type{});
