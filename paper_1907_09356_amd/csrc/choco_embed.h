@@ -1,6 +1,8 @@
 // Embedding lookup with scaling, and its gradient summed by token (device code).
 #pragma once
 
+#include <type_traits>
+
 #include "choco_types.h"
 
 namespace choco {
@@ -322,28 +324,21 @@ __global__ __launch_bounds__(kChunkThreads) void k_embed_scatter(EmbedArgs A, in
     }
 }
 
-// V floats in vectors of at most 16 bytes.
-template <int V>
-__device__ __forceinline__ void load_sums(const float* p, float (&x)[V]) {
-  constexpr int S = V < 4 ? V : 4;
-#pragma unroll
-  for (int i = 0; i < V; i += S) {
-    const Pack<float, S> v = *reinterpret_cast<const Pack<float, S>*>(p + i);
-#pragma unroll
-    for (int k = 0; k < S; ++k) x[i + k] = v.e[k];
+// A lane's columns of a row: registers of one entry of 32 bits, or two or one of 16.  (The words are taken apart where they are used:
+// a load of 16-bit floats would lose its way past the caches in the compiler.)
+template <class Row, int V>
+struct RowWords {
+  static constexpr int kWords = sizeof(Row) == 4 ? V : 1;
+  using Word = std::conditional_t<V * sizeof(Row) == 2, uint16_t, uint32_t>;
+  typedef Word Words __attribute__((ext_vector_type(kWords)));
+  Words words;
+  template <bool PAST>
+  __device__ __forceinline__ void load(const Row* p) {
+    if constexpr (PAST) words = __builtin_nontemporal_load(reinterpret_cast<const Words*>(p));
+    else words = *reinterpret_cast<const Words*>(p);
   }
-}
-template <int V>
-__device__ __forceinline__ void store_sums(float* p, const float (&x)[V]) {
-  constexpr int S = V < 4 ? V : 4;
-#pragma unroll
-  for (int i = 0; i < V; i += S) {
-    Pack<float, S> v;
-#pragma unroll
-    for (int k = 0; k < S; ++k) v.e[k] = x[i + k];
-    *reinterpret_cast<Pack<float, S>*>(p + i) = v;
-  }
-}
+  __device__ __forceinline__ float at(int i) const { return sizeof(Row) == 4 ? entry<Row>(words[i], 0) : entry<Row>(words[0], i); }
+};
 __device__ __forceinline__ float* sums_of(const EmbedArgs& A, int w, uint32_t token, int64_t c) {
   return A.dtable + (int64_t)w * A.table_stride + (int64_t)token * A.dim + c;
 }
@@ -353,12 +348,12 @@ __device__ __forceinline__ void put_sums(const EmbedArgs& A, float* p, const flo
   float x[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) x[i] = ADD ? sum[i] * A.scale + old[i] : sum[i] * A.scale;
-  store_sums<V>(p, x);
+  store_floats<float, V>(p, x);
 }
 
 // A wave adds up the rows of a piece, for 64 * V columns.  Partial sums: slot 0 of a piece, its first token, where that is also the
 // last of the piece before; slot 1, its last token, where that goes on in the next piece (and is not in slot 0).
-template <class Row, int V, bool ADD>
+template <class Row, int V, bool ADD, bool PAST>
 __global__ __launch_bounds__(256) void k_embed_sum(EmbedArgs A) {
   const int lane = threadIdx.x & 63, w = blockIdx.y;
   const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -388,27 +383,27 @@ __global__ __launch_bounds__(256) void k_embed_sum(EmbedArgs A) {
   for (int i = 0; i < V; ++i) sum[i] = 0.0f;
   bool inside = starts >> 1 & 1;     // the token that `sum` is of began in this piece
   for (int s = 0; s < here; s += kAhead) {
-    Pack<Row, V> x[kAhead];
+    RowWords<Row, V> x[kAhead];
     float old[kAhead][V];
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       const int at = (s + j < here ? s + j : here - 1) + 1;
       const int64_t p = (uint32_t)__builtin_amdgcn_readlane((int)place, at);
-      x[j] = *reinterpret_cast<const Pack<Row, V>*>(rows + p * A.row_ld);
-      if (ADD && (ends >> at & 1)) load_sums<V>(sums_of(A, w, (uint32_t)__builtin_amdgcn_readlane((int)key, at), column), old[j]);
+      x[j].template load<PAST>(rows + p * A.row_ld);
+      if (ADD && (ends >> at & 1)) load_floats<float, V>(sums_of(A, w, (uint32_t)__builtin_amdgcn_readlane((int)key, at), column), old[j]);
     }
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       if (s + j >= here) break;
       const int at = s + j + 1;
 #pragma unroll
-      for (int i = 0; i < V; ++i) sum[i] += to_float(x[j].e[i]);
+      for (int i = 0; i < V; ++i) sum[i] += x[j].at(i);
       if (!(ends >> at & 1)) continue;
       const uint32_t token = (uint32_t)__builtin_amdgcn_readlane((int)key, at);
       const bool goes_on = at == count && token == right;
       if (in) {
         if (inside && !goes_on) put_sums<ADD, V>(A, sums_of(A, w, token, column), sum, old[j]);
-        else store_sums<V>(inside ? partial + A.partial_ld : partial, sum);
+        else store_floats<float, V>(inside ? partial + A.partial_ld : partial, sum);
       }
       inside = true;
 #pragma unroll
@@ -423,7 +418,7 @@ __device__ __forceinline__ void add_pieces(const float* partial, int64_t partial
 #pragma unroll 8
   for (int64_t p = from; p < to; ++p) {
     float x[V];
-    load_sums<V>(partial + p * 2 * partial_ld, x);
+    load_floats<float, V>(partial + p * 2 * partial_ld, x);
 #pragma unroll
     for (int i = 0; i < V; ++i) sum[i] += x[i];
   }
@@ -462,8 +457,8 @@ __global__ __launch_bounds__(64 * kJoinWaves) void k_embed_join(EmbedArgs A) {
     if (lane == 0) many[wave] = reach >= kJoinAlone ? reach : 0;
     if (reach > 0 && reach < kJoinAlone && c < A.dim) {
       float sum[V], old[V];
-      if (ADD) load_sums<V>(sums_of(A, w, token, c), old);
-      load_sums<V>(partial + (piece * 2 + 1) * A.partial_ld + c, sum);
+      if (ADD) load_floats<float, V>(sums_of(A, w, token, c), old);
+      load_floats<float, V>(partial + (piece * 2 + 1) * A.partial_ld + c, sum);
       add_pieces<V>(partial + c, A.partial_ld, piece + 1, piece + 1 + reach, sum);
       put_sums<ADD, V>(A, sums_of(A, w, token, c), sum, old);
     }
@@ -478,7 +473,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void k_embed_join(EmbedArgs A) {
     float sum[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) sum[i] = 0.0f;
-    if (wave == 0) load_sums<V>(partial + (piece * 2 + 1) * A.partial_ld + column, sum);
+    if (wave == 0) load_floats<float, V>(partial + (piece * 2 + 1) * A.partial_ld + column, sum);
     add_pieces<V>(partial + column, A.partial_ld, piece + 1 + from, piece + 1 + to, sum);
 #pragma unroll
     for (int i = 0; i < V; ++i) sums[wave][lane][i] = sum[i];
@@ -486,7 +481,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void k_embed_join(EmbedArgs A) {
     if (wave == 0 && c < A.dim) {
       float old[V];
       float* to_row = sums_of(A, w, keys[(piece + 1) * kPiece], c);
-      if (ADD) load_sums<V>(to_row, old);
+      if (ADD) load_floats<float, V>(to_row, old);
 #pragma unroll
       for (int u = 1; u < kJoinWaves; ++u)
 #pragma unroll

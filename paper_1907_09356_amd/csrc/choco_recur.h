@@ -158,13 +158,6 @@ __device__ __forceinline__ uint32_t load_word(const T* p) {
   if constexpr (PAST) return __builtin_nontemporal_load(reinterpret_cast<const Word*>(p));
   else return *reinterpret_cast<const Word*>(p);
 }
-template <class T>
-__device__ __forceinline__ float entry(uint32_t word, int i) {
-  if constexpr (sizeof(T) == 4) return __uint_as_float(word);
-  else if constexpr (std::is_same_v<T, bf16_t>) return __uint_as_float(i ? word & 0xFFFF0000u : word << 16);
-  else return (float)__builtin_bit_cast(f16_t, (uint16_t)(i ? word >> 16 : word));
-}
-
 // Rows t .. t + n - 1 of a lane's channels, n >= 1; the rest of the wave's steps repeat the last row.
 template <class T, int V, bool PAST, int K>
 __device__ __forceinline__ void load_steps(const void* base, int64_t seq, int64_t step, const RecurPlace& P, int64_t t, int n,

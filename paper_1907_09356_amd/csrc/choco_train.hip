@@ -452,9 +452,13 @@ int choco_embed_backward(const choco_embed_config* cfg, const void* tokens_dev, 
   A.digit_bits = L.digit_bits;
   A.passes = L.passes;
   const size_t size = type_bytes(c.row_type);
-  int v = embed_width(size == 2 ? 8 : 4, c.dim, {{dy_dev, size}, {dtable_dev, 4}},
-                      {{c.row_ld, size}, {c.row_stride, size}, {c.table_stride, 4}});
-  while (v > 1 && 32 * v >= c.dim) v /= 2;     // (no more than a lane needs to leave no lane without columns)
+  // Two columns a lane: with eight (or four) a wave holds so many rows of sums and old values that too few waves fit to keep the
+  // memory busy (65,536 rows of 1024 in bf16: eight 111 us, four 101, two 99).
+  int v = embed_width(2, c.dim, {{dy_dev, size}, {dtable_dev, 4}}, {{c.row_ld, size}, {c.row_stride, size}, {c.table_stride, 4}});
+  if (c.dim <= 64) v = 1;     // (no lane without columns)
+  // Gradients of the rows past the caches where they do not fit there (134 MB: 112-125 us through, 102-112 past them; 23 MB,
+  // just written: 26 and 30).
+  const bool past = (double)c.n * (double)c.tokens * (double)c.dim * size > 96.0 * 1048576.0;
   A.column_chunks = (c.dim + 64 * v - 1) / (64 * v);
   if (!launch_fits((double)A.pieces * (double)A.column_chunks, 64) || !launch_fits((double)L.chunks + zero_blocks, kChunkThreads))
     return CHOCO_E_UNSUPPORTED;
@@ -492,19 +496,21 @@ int choco_embed_backward(const choco_embed_config* cfg, const void* tokens_dev, 
   TRY_HIP(hipGetLastError());
   const int64_t units = A.pieces * A.column_chunks;
   with_type(c.row_type, [&](auto row) {
-    with_vector(v, [&](auto width) {
+    const auto sums = [&](auto width, auto add) {
       using Row = decltype(row);
       constexpr int V = decltype(width)::value;
-      if constexpr (V * sizeof(Row) <= 16) {
-        const auto sums = [&](auto add) {
-          constexpr bool ADD = decltype(add)::value;
-          k_embed_sum<Row, V, ADD><<<dim3(blocks_of(units, 4), (uint32_t)c.n), 256, 0, stream>>>(A);
-          if (A.pieces > 1) k_embed_join<V, ADD><<<dim3(blocks_of(units, kJoinWaves), (uint32_t)c.n), 64 * kJoinWaves, 0, stream>>>(A);
-        };
-        if (accumulate) sums(std::true_type{});
-        else sums(std::false_type{});
-      }
-    });
+      constexpr bool ADD = decltype(add)::value;
+      const dim3 grid(blocks_of(units, 4), (uint32_t)c.n);
+      if (past) k_embed_sum<Row, V, ADD, true><<<grid, 256, 0, stream>>>(A);
+      else k_embed_sum<Row, V, ADD, false><<<grid, 256, 0, stream>>>(A);
+      if (A.pieces > 1) k_embed_join<V, ADD><<<dim3(blocks_of(units, kJoinWaves), (uint32_t)c.n), 64 * kJoinWaves, 0, stream>>>(A);
+    };
+    const auto with_add = [&](auto width) {
+      if (accumulate) sums(width, std::true_type{});
+      else sums(width, std::false_type{});
+    };
+    if (v == 2) with_add(std::integral_constant<int, 2>{});
+    else with_add(std::integral_constant<int, 1>{});
   });
   TRY_HIP(hipGetLastError());
   return CHOCO_OK;

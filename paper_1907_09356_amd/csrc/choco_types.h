@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 namespace choco {
 
 typedef __bf16 bf16_t;
@@ -32,6 +34,14 @@ __device__ __forceinline__ void store_floats(T* p, const float (&x)[V]) {
 #pragma unroll
   for (int i = 0; i < V; ++i) v.e[i] = from_float<T>(x[i]);
   *reinterpret_cast<Pack<T, V>*>(p) = v;
+}
+
+// Entry i of a register's worth of them.
+template <class T>
+__device__ __forceinline__ float entry(uint32_t word, int i) {
+  if constexpr (sizeof(T) == 4) return __uint_as_float(word);
+  else if constexpr (std::is_same_v<T, bf16_t>) return __uint_as_float(i ? word & 0xFFFF0000u : word << 16);
+  else return (float)__builtin_bit_cast(f16_t, (uint16_t)(i ? word >> 16 : word));
 }
 
 }  // namespace choco
