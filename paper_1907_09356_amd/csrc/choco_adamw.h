@@ -103,7 +103,8 @@ __device__ __forceinline__ void load_four(const T* p, int lane, int left, T (&x)
   if (ALIGNED && (left >= kMomentBlock || lane * 4 + 4 <= left)) {
     typedef T Four __attribute__((ext_vector_type(4)));
     Four v;
-    if constexpr (STREAM) v = __builtin_nontemporal_load(reinterpret_cast<const Four*>(p + lane * 4));
+    // (codes through the caches: asked for past them, 127 M entries take 570 us instead of 518)
+    if constexpr (STREAM && sizeof(T) > 1) v = __builtin_nontemporal_load(reinterpret_cast<const Four*>(p + lane * 4));
     else v = *reinterpret_cast<const Four*>(p + lane * 4);
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = v[i];
