@@ -23,6 +23,7 @@ struct EmbedArgs {
   int64_t partial_ld, pieces, column_chunks;
   uint32_t chunks, zero_blocks;      // zero_blocks: per worker, of kZeroFloats each
   int digit_bits, passes;
+  bool zero_past;                    // cleared past the caches
 };
 
 constexpr int kSortThreads = 1024;                     // a workgroup that orders all of a worker's tokens in LDS ...
@@ -49,7 +50,7 @@ __device__ __forceinline__ int32_t token_at(const EmbedArgs& A, int worker, int6
 // y[w, r, :] = scale * table[w, token, :].  A group of 2^LANES_LOG2 lanes takes a row, V entries a lane at a time, and
 // asks for kRowAhead such pieces before it writes the first.
 constexpr int kRowAhead = 4;
-template <class Tok, class Tab, class Row, int V>
+template <class Tok, class Tab, class Row, int V, bool PAST>
 __global__ __launch_bounds__(256) void k_embed(EmbedArgs A, int lanes_log2) {
   const int lane = threadIdx.x & ((1 << lanes_log2) - 1);
   const int64_t r = (int64_t)blockIdx.x * (256 >> lanes_log2) + (threadIdx.x >> lanes_log2);
@@ -70,7 +71,8 @@ __global__ __launch_bounds__(256) void k_embed(EmbedArgs A, int lanes_log2) {
       float y[V];
 #pragma unroll
       for (int i = 0; i < V; ++i) y[i] = t >= 0 ? to_float(x[j].e[i]) * A.scale : 0.0f;
-      store_floats<Row, V>(to + c + j * step, y);
+      if constexpr (PAST) store_floats_past<Row, V>(to + c + j * step, y);
+      else store_floats<Row, V>(to + c + j * step, y);
     }
   }
 }
@@ -87,14 +89,18 @@ __global__ __launch_bounds__(256) void k_embed(EmbedArgs A, int lanes_log2) {
 // Part `block` of the gradient's clearing, by a whole workgroup.
 __device__ __forceinline__ void zero_part(const EmbedArgs& A, int64_t worker, int64_t block) {
   float* base = A.dtable + worker * A.table_stride;
+  const float zeros[4] = {};
   const int64_t size = A.vocab * A.dim;
   int64_t from = block * kZeroFloats, to = from + kZeroFloats < size ? from + kZeroFloats : size;
   // whole 16-byte vectors of memory between a few single floats at the ends
   const int64_t lead = (4 - (int64_t)(((uintptr_t)(base + from) >> 2) & 3)) & 3;
   const int64_t first = from + lead < to ? from + lead : to, last = first + (to - first) / 4 * 4;
   for (int64_t i = from + threadIdx.x; i < first; i += blockDim.x) base[i] = 0.0f;
-  for (int64_t i = first + 4 * (int64_t)threadIdx.x; i < last; i += 4 * (int64_t)blockDim.x)
-    *reinterpret_cast<Pack<float, 4>*>(base + i) = Pack<float, 4>{};
+  if (A.zero_past) {
+    for (int64_t i = first + 4 * (int64_t)threadIdx.x; i < last; i += 4 * (int64_t)blockDim.x) store_floats_past<float, 4>(base + i, zeros);
+  } else {
+    for (int64_t i = first + 4 * (int64_t)threadIdx.x; i < last; i += 4 * (int64_t)blockDim.x) store_floats<float, 4>(base + i, zeros);
+  }
   for (int64_t i = last + threadIdx.x; i < to; i += blockDim.x) base[i] = 0.0f;
 }
 
@@ -343,12 +349,13 @@ __device__ __forceinline__ float* sums_of(const EmbedArgs& A, int w, uint32_t to
   return A.dtable + (int64_t)w * A.table_stride + (int64_t)token * A.dim + c;
 }
 // scale * sum to (ADD: onto `old`, what is there) the gradient.
-template <bool ADD, int V>
+template <bool ADD, bool PAST, int V>
 __device__ __forceinline__ void put_sums(const EmbedArgs& A, float* p, const float (&sum)[V], const float (&old)[V]) {
   float x[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) x[i] = ADD ? sum[i] * A.scale + old[i] : sum[i] * A.scale;
-  store_floats<float, V>(p, x);
+  if constexpr (PAST) store_floats_past<float, V>(p, x);
+  else store_floats<float, V>(p, x);
 }
 
 // A wave adds up the rows of a piece, for 64 * V columns.  Partial sums: slot 0 of a piece, its first token, where that is also the
@@ -402,7 +409,7 @@ __global__ __launch_bounds__(256) void k_embed_sum(EmbedArgs A) {
       const uint32_t token = (uint32_t)__builtin_amdgcn_readlane((int)key, at);
       const bool goes_on = at == count && token == right;
       if (in) {
-        if (inside && !goes_on) put_sums<ADD, V>(A, sums_of(A, w, token, column), sum, old[j]);
+        if (inside && !goes_on) put_sums<ADD, PAST, V>(A, sums_of(A, w, token, column), sum, old[j]);
         else store_floats<float, V>(inside ? partial + A.partial_ld : partial, sum);
       }
       inside = true;
@@ -460,7 +467,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void k_embed_join(EmbedArgs A) {
       if (ADD) load_floats<float, V>(sums_of(A, w, token, c), old);
       load_floats<float, V>(partial + (piece * 2 + 1) * A.partial_ld + c, sum);
       add_pieces<V>(partial + c, A.partial_ld, piece + 1, piece + 1 + reach, sum);
-      put_sums<ADD, V>(A, sums_of(A, w, token, c), sum, old);
+      put_sums<ADD, false, V>(A, sums_of(A, w, token, c), sum, old);
     }
   }
   __syncthreads();
@@ -486,7 +493,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void k_embed_join(EmbedArgs A) {
       for (int u = 1; u < kJoinWaves; ++u)
 #pragma unroll
         for (int i = 0; i < V; ++i) sum[i] += sums[u][lane][i];
-      put_sums<ADD, V>(A, to_row, sum, old);
+      put_sums<ADD, false, V>(A, to_row, sum, old);
     }
     __syncthreads();
   }

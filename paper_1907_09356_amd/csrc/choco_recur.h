@@ -173,15 +173,8 @@ __device__ __forceinline__ void load_steps(const void* base, int64_t seq, int64_
 template <class T, int V, bool PAST>
 __device__ __forceinline__ void store_step(void* base, int64_t seq, int64_t step, const RecurPlace& P, int64_t t, const float (&x)[V]) {
   T* p = (T*)base + P.b * seq + t * step + P.strip + P.lane;
-  if constexpr (PAST) {
-    typedef T Entries __attribute__((ext_vector_type(V)));
-    Entries v;
-#pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = from_float<T>(x[i]);
-    __builtin_nontemporal_store(v, reinterpret_cast<Entries*>(p));
-  } else {
-    store_floats<T, V>(p, x);
-  }
+  if constexpr (PAST) store_floats_past<T, V>(p, x);
+  else store_floats<T, V>(p, x);
 }
 
 template <int K>

@@ -403,6 +403,9 @@ int choco_embed_forward(const choco_embed_config* cfg, const void* tokens_dev, c
   const int64_t blocks = (c.tokens + (256 >> lanes_log2) - 1) / (256 >> lanes_log2);
   if (!launch_fits(blocks, 256)) return CHOCO_E_UNSUPPORTED;
   const dim3 grid((uint32_t)blocks, (uint32_t)c.n);
+  // Rows past the caches where they do not stay there until they are read.  us, through | past: 16 MB written 7.7 | 7.8, 64 MB
+  // 18.0 | 17.0, 134 MB 36.6 | 31.4, 201 MB 57.0 | 44.6, 268 MB 86 | 60.
+  const bool past = (double)c.n * (double)c.tokens * (double)c.dim * row_size > 96.0 * 1048576.0;
   with_type(c.table_type, [&](auto tab) {
     with_type(c.row_type, [&](auto row) {
       with_vector(v, [&](auto width) {
@@ -410,8 +413,12 @@ int choco_embed_forward(const choco_embed_config* cfg, const void* tokens_dev, c
         using Row = decltype(row);
         constexpr int V = decltype(width)::value;
         if constexpr (V * std::max(sizeof(Tab), sizeof(Row)) <= 16) {
-          if (c.token_type == CHOCO_I32) k_embed<int32_t, Tab, Row, V><<<grid, 256, 0, (hipStream_t)c.stream>>>(A, lanes_log2);
-          else k_embed<int64_t, Tab, Row, V><<<grid, 256, 0, (hipStream_t)c.stream>>>(A, lanes_log2);
+          const auto launch = [&](auto token) {
+            if (past) k_embed<decltype(token), Tab, Row, V, true><<<grid, 256, 0, (hipStream_t)c.stream>>>(A, lanes_log2);
+            else k_embed<decltype(token), Tab, Row, V, false><<<grid, 256, 0, (hipStream_t)c.stream>>>(A, lanes_log2);
+          };
+          if (c.token_type == CHOCO_I32) launch(int32_t{});
+          else launch(int64_t{});
         }
       });
     });
@@ -438,6 +445,7 @@ int choco_embed_backward(const choco_embed_config* cfg, const void* tokens_dev, 
   const int64_t zero_blocks = accumulate ? 0 : (c.vocab * c.dim + kZeroFloats - 1) / kZeroFloats;
   if (!launch_fits((double)zero_blocks * c.n + c.n, kSortThreads)) return CHOCO_E_UNSUPPORTED;
   A.zero_blocks = (uint32_t)zero_blocks;
+  A.zero_past = (double)c.n * (double)c.vocab * (double)c.dim * 4 > 96.0 * 1048576.0;   // (692 MB cleared and 9 K rows added: 142 | 139 us)
   if (c.tokens == 0) {   // nothing but zeros
     k_embed_count<int32_t, true, kShortRounds><<<dim3(A.zero_blocks, (uint32_t)c.n), kChunkThreads, 0, stream>>>(A, 0);
     TRY_HIP(hipGetLastError());
@@ -456,8 +464,8 @@ int choco_embed_backward(const choco_embed_config* cfg, const void* tokens_dev, 
   // memory busy (65,536 rows of 1024 in bf16: eight 111 us, four 101, two 99).
   int v = embed_width(2, c.dim, {{dy_dev, size}, {dtable_dev, 4}}, {{c.row_ld, size}, {c.row_stride, size}, {c.table_stride, 4}});
   if (c.dim <= 64) v = 1;     // (no lane without columns)
-  // Gradients of the rows past the caches where they do not fit there (134 MB: 112-125 us through, 102-112 past them; 23 MB,
-  // just written: 26 and 30).
+  // Rows and sums past the caches where the rows do not fit there (65,536 of 1024 in bf16, 134 MB: 99 us through, 88 with the rows
+  // past them, 83 with the sums as well; 23 MB, just written: 26 and 30).
   const bool past = (double)c.n * (double)c.tokens * (double)c.dim * size > 96.0 * 1048576.0;
   A.column_chunks = (c.dim + 64 * v - 1) / (64 * v);
   if (!launch_fits((double)A.pieces * (double)A.column_chunks, 64) || !launch_fits((double)L.chunks + zero_blocks, kChunkThreads))

@@ -36,6 +36,16 @@ __device__ __forceinline__ void store_floats(T* p, const float (&x)[V]) {
   *reinterpret_cast<Pack<T, V>*>(p) = v;
 }
 
+// ... past the caches.
+template <class T, int V>
+__device__ __forceinline__ void store_floats_past(T* p, const float (&x)[V]) {
+  typedef T Entries __attribute__((ext_vector_type(V)));
+  Entries v;
+#pragma unroll
+  for (int i = 0; i < V; ++i) v[i] = from_float<T>(x[i]);
+  __builtin_nontemporal_store(v, reinterpret_cast<Entries*>(p));
+}
+
 // Entry i of a register's worth of them.
 template <class T>
 __device__ __forceinline__ float entry(uint32_t word, int i) {

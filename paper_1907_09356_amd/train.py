@@ -195,13 +195,12 @@ def recurrence(f, u, o=None, h0=None, lengths=None, save=False, out=None, h_last
     h_last may be h0 itself, as in token by token generation."""
     assert f.is_cuda
     B, T, C = f.shape
-    device = f.device
-    y = torch.empty((B, T, C), dtype=f.dtype, device=device) if out is None else out
+    y = f.new_empty((B, T, C)) if out is None else out
     if h_last is None:
-        h_last = torch.empty((B, C), dtype=torch.float32, device=device)
+        h_last = torch.empty((B, C), dtype=torch.float32, device=f.device) if h0 is None else torch.empty_like(h0)
     saved = None
     if save:
-        saved = torch.empty(((T + SAVE_STEPS - 1) // SAVE_STEPS, B, C), dtype=torch.float32, device=device)
+        saved = torch.empty(((T + SAVE_STEPS - 1) // SAVE_STEPS, B, C), dtype=torch.float32, device=f.device)
     cfg, nbytes = _recur_config(f, stream, u, o, y)
     ws = _scratch(nbytes, f)
     _check(lib().choco_recur_forward(cfg, f.data_ptr(), u.data_ptr(), _ptr(o), _state(h0, f), _lengths(lengths, f), y.data_ptr(),
