@@ -46,7 +46,7 @@ typedef struct {
 /* Bytes of device workspace that choco_embed_backward needs (16-byte aligned); may be 0. */
 int choco_embed_workspace_bytes(const choco_embed_config* cfg, size_t* bytes_host);
 /* CHOCO_E_INVAL: a size, type or stride outside its range, a null pointer, a pointer that is not aligned to its
-   entries. */
+   entries.  CHOCO_E_UNSUPPORTED: more work than one launch holds. */
 int choco_embed_forward(const choco_embed_config* cfg, const void* tokens_dev, const void* table_dev, void* y_dev);
 /* accumulate = 0: every entry of the vocab x dim gradient is written (zero for tokens that do not occur);
    1: the sums are added to what is there, other rows are left alone (a table that is also the output layer).
@@ -76,7 +76,7 @@ typedef struct {
 int choco_recur_saved_bytes(const choco_recur_config* cfg, size_t* bytes_host);
 /* Bytes of device workspace that either pass needs (16-byte aligned); may be 0. */
 int choco_recur_workspace_bytes(const choco_recur_config* cfg, size_t* bytes_host);
-/* o_dev, h0_dev (batch x dim fp32; zero without), lengths_dev (batch int32), h_last_dev (batch x dim fp32) and
+/* Errors as above.  o_dev, h0_dev (batch x dim fp32; zero without), lengths_dev (batch int32), h_last_dev (batch x dim fp32) and
    saved_dev may be NULL. */
 int choco_recur_forward(const choco_recur_config* cfg, const void* f_dev, const void* u_dev, const void* o_dev,
                         const float* h0_dev, const int32_t* lengths_dev, void* y_dev, float* h_last_dev, float* saved_dev,

@@ -66,6 +66,11 @@ int check_embed(const choco_embed_config* c) {
   return CHOCO_OK;
 }
 
+// The gradient's partial sums take a sixteenth of the rows' entries in fp32: below 2^50 bytes with any number of workers.
+bool embed_fits(const choco_embed_config& c) {
+  return (double)c.n * ((double)c.tokens + kPiece) * ((double)c.dim + 8.0) < 1125899906842624.0;
+}
+
 EmbedArgs embed_args(const choco_embed_config& c, const void* tokens) {
   EmbedArgs A{};
   A.tokens = tokens;
@@ -218,6 +223,16 @@ RecurPlan plan_recur(const choco_recur_config& c, int width, int steps) {
 // Words of a chain's maps and states, and of the whole workspace with the counters.
 double chain_words(const RecurPlan& P, int width) { return P.tiles > 1 ? (double)P.chains * (double)(P.tiles + P.links) * width : 0.0; }
 
+// A call's launches hold it, whichever way it is split.
+bool recur_fits(const choco_recur_config& c) {
+  for (int v : {1, 2})
+    for (int steps : {kForwardSteps, back_steps(v)}) {
+      const RecurPlan P = plan_recur(c, 64 * v, steps);
+      if (!launch_fits((double)P.chains * (double)P.tiles, 64 * P.waves)) return false;
+    }
+  return true;
+}
+
 size_t recur_workspace(const choco_recur_config& c) {
   // (a call takes the wide strips or the narrow ones, whatever its pointers allow: room for either, and for both passes)
   size_t most = 0;
@@ -229,11 +244,10 @@ size_t recur_workspace(const choco_recur_config& c) {
   return most;
 }
 
-// The launches of a call: false where a grid does not hold them.
-bool place_recur(const choco_recur_config& c, int width, int steps, void* workspace, RecurArgs& A, dim3& grid, int& threads) {
+// The launch of a call.
+void place_recur(const choco_recur_config& c, int width, int steps, void* workspace, RecurArgs& A, dim3& grid, int& threads) {
   const RecurPlan P = plan_recur(c, width, steps);
   threads = 64 * P.waves;
-  if (!launch_fits((double)P.chains * (double)P.tiles, threads)) return false;
   A.strips = (uint32_t)P.strips;
   A.chains = (uint32_t)P.chains;
   A.tiles = (uint32_t)P.tiles;
@@ -242,7 +256,6 @@ bool place_recur(const choco_recur_config& c, int width, int steps, void* worksp
   A.states = A.maps + P.chains * P.tiles * width;
   A.taken = (uint32_t*)(A.states + P.chains * P.links * width);
   grid = dim3((uint32_t)(P.chains * P.tiles));
-  return true;
 }
 
 // Launches what starts the chains (`first`: the states before them) of a call that has any.
@@ -380,6 +393,7 @@ int choco_train_last_hip_error(void) { return g_last_hip_error; }
 int choco_embed_workspace_bytes(const choco_embed_config* cfg, size_t* bytes_host) {
   if (!bytes_host) return CHOCO_E_INVAL;
   if (const int rc = check_embed(cfg)) return rc;
+  if (!embed_fits(*cfg)) return CHOCO_E_UNSUPPORTED;
   *bytes_host = embed_layout(*cfg).total;
   return CHOCO_OK;
 }
@@ -435,6 +449,7 @@ int choco_embed_backward(const choco_embed_config* cfg, const void* tokens_dev, 
   if (!dtable_dev || (c.tokens > 0 && (!tokens_dev || !dy_dev))) return CHOCO_E_INVAL;
   if (!aligned_to(tokens_dev, c.token_type == CHOCO_I32 ? 4 : 8) || !aligned_to(dtable_dev, 4) || !aligned_to(dy_dev, type_bytes(c.row_type)))
     return CHOCO_E_INVAL;
+  if (!embed_fits(c)) return CHOCO_E_UNSUPPORTED;
   const EmbedLayout L = embed_layout(c);
   if (L.total > 0 && (!workspace_dev || !aligned_to(workspace_dev, 16))) return CHOCO_E_INVAL;
   if (L.total > workspace_bytes) return CHOCO_E_NOMEM;
@@ -534,6 +549,7 @@ int choco_recur_saved_bytes(const choco_recur_config* cfg, size_t* bytes_host) {
 int choco_recur_workspace_bytes(const choco_recur_config* cfg, size_t* bytes_host) {
   if (!bytes_host) return CHOCO_E_INVAL;
   if (const int rc = check_recur(cfg)) return rc;
+  if (!recur_fits(*cfg)) return CHOCO_E_UNSUPPORTED;
   *bytes_host = recur_workspace(*cfg);
   return CHOCO_OK;
 }
@@ -554,6 +570,7 @@ int choco_recur_forward(const choco_recur_config* cfg, const void* f_dev, const 
   if (!aligned_to(f_dev, size) || !aligned_to(u_dev, size) || !aligned_to(o_dev, size) || !aligned_to(y_dev, size) ||
       !aligned_to(h0_dev, 4) || !aligned_to(lengths_dev, 4) || !aligned_to(h_last_dev, 4) || !aligned_to(saved_dev, 4))
     return CHOCO_E_INVAL;
+  if (!recur_fits(c)) return CHOCO_E_UNSUPPORTED;
   const size_t need = recur_workspace(c);
   if (need > 0 && (!workspace_dev || !aligned_to(workspace_dev, 16))) return CHOCO_E_INVAL;
   if (need > workspace_bytes) return CHOCO_E_NOMEM;
@@ -566,7 +583,7 @@ int choco_recur_forward(const choco_recur_config* cfg, const void* f_dev, const 
   const int width = pairs ? 128 : 64;
   dim3 grid;
   int threads;
-  if (!place_recur(c, width, kForwardSteps, workspace_dev, A, grid, threads)) return CHOCO_E_UNSUPPORTED;
+  place_recur(c, width, kForwardSteps, workspace_dev, A, grid, threads);
   const hipStream_t stream = (hipStream_t)c.stream;
   if (A.tiles > 1) start_chains(A, width, h0_dev, stream);
   with_type(c.type, [&](auto x) {
@@ -604,6 +621,7 @@ int choco_recur_backward(const choco_recur_config* cfg, const void* f_dev, const
       !aligned_to(df_dev, size) || !aligned_to(du_dev, size) || !aligned_to(do_dev, size) || !aligned_to(lengths_dev, 4) ||
       !aligned_to(saved_dev, 4) || !aligned_to(dlast_dev, 4) || !aligned_to(dh0_dev, 4))
     return CHOCO_E_INVAL;
+  if (!recur_fits(c)) return CHOCO_E_UNSUPPORTED;
   const size_t need = recur_workspace(c);
   if (need > 0 && (!workspace_dev || !aligned_to(workspace_dev, 16))) return CHOCO_E_INVAL;
   if (need > workspace_bytes) return CHOCO_E_NOMEM;
@@ -619,7 +637,7 @@ int choco_recur_backward(const choco_recur_config* cfg, const void* f_dev, const
   const int width = pairs ? 128 : 64;
   dim3 grid;
   int threads;
-  if (!place_recur(c, width, back_steps(width / 64), workspace_dev, A, grid, threads)) return CHOCO_E_UNSUPPORTED;
+  place_recur(c, width, back_steps(width / 64), workspace_dev, A, grid, threads);
   const hipStream_t stream = (hipStream_t)c.stream;
   if (A.tiles > 1) start_chains(A, width, dlast_dev, stream);
   with_type(c.type, [&](auto x) {

@@ -1,8 +1,9 @@
 """ctypes binding of include/choco_train.h: embedding lookup and gradient, gated linear recurrence, AdamW.
 
-Argument marshalling only, like `binding`: torch provides device memory and the stream (the current one of the
-tensors' device unless `stream` is given), every computation runs in the HIP library.  A tensor that is used on
-another stream than the one it was made on has to be kept by the caller until that stream is done with it.
+Argument marshalling only, like `binding`: torch provides device memory and the stream, every computation runs in the
+HIP library.  The functions enqueue on torch's current stream of the tensors' device, an `AdamW` on the one that was
+current when it was made.  As with torch's own operations, a tensor that is used on another stream than the one it was made on
+has to be kept until that stream is done with it.
 """
 import ctypes
 import functools
@@ -83,8 +84,8 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _stream(t, stream):
-    return torch._C._cuda_getCurrentRawStream(t.get_device()) if stream is None else stream
+def _stream(t):
+    return torch._C._cuda_getCurrentRawStream(t.get_device())
 
 
 def _scratch(nbytes, like):
@@ -119,29 +120,29 @@ def _embed_plan(token_shape, token_stride, token_type, table_shape, table_stride
                                 stream=stream), lib().choco_embed_workspace_bytes)
 
 
-def _embed_config(tokens, table, rows, scale, stream):
+def _embed_config(tokens, table, rows, scale):
     assert tokens.is_cuda and table.get_device() == rows.get_device() == tokens.get_device()
     return _embed_plan(tokens.shape, tokens.stride(), tokens.dtype, table.shape, table.stride(), table.dtype, rows.shape,
-                       rows.stride(), rows.dtype, scale, _stream(tokens, stream))
+                       rows.stride(), rows.dtype, scale, _stream(tokens))
 
 
-def embed(tokens, table, scale=1.0, out_dtype=None, out=None, stream=None):
+def embed(tokens, table, scale=1.0, out_dtype=None, out=None):
     """scale * table[w, tokens[w, r]] for every worker w: (n, R, dim).
 
     tokens (n, R) of int32 or int64, zero rows for those outside [0, vocab); table (n, vocab, dim), e.g. a tensor's slice of the
     workers' rows, `X[:, a:a + vocab * dim].view(n, vocab, dim)`."""
     if out is None:
         out = torch.empty(tokens.shape + table.shape[2:], dtype=out_dtype or table.dtype, device=table.device)
-    cfg, _ = _embed_config(tokens, table, out, float(scale), stream)
+    cfg, _ = _embed_config(tokens, table, out, float(scale))
     _check(lib().choco_embed_forward(cfg, tokens.data_ptr(), table.data_ptr(), out.data_ptr()), "choco_embed_forward")
     return out
 
 
-def embed_grad(tokens, dout, dtable, scale=1.0, accumulate=False, stream=None):
+def embed_grad(tokens, dout, dtable, scale=1.0, accumulate=False):
     """The gradient of `embed` with respect to its table, written (or added) to dtable (n, vocab, dim) of float32,
     e.g. a tensor's slice of the workers' gradient rows."""
     assert dtable.dtype == torch.float32
-    cfg, nbytes = _embed_config(tokens, dtable, dout, float(scale), stream)
+    cfg, nbytes = _embed_config(tokens, dtable, dout, float(scale))
     ws = _scratch(nbytes, dtable)
     _check(lib().choco_embed_backward(cfg, tokens.data_ptr(), dout.data_ptr(), dtable.data_ptr(), 1 if accumulate else 0,
                                       _ptr(ws), nbytes), "choco_embed_backward")
@@ -161,7 +162,7 @@ def _recur_plan(shape, dtype, strides, stream):
     return _planned(cfg, lib().choco_recur_workspace_bytes)
 
 
-def _recur_config(f, stream, *tensors):
+def _recur_config(f, *tensors):
     device, dtype, shape = f.get_device(), f.dtype, f.shape
     strides = [f.stride()]
     for t in tensors:
@@ -169,7 +170,7 @@ def _recur_config(f, stream, *tensors):
             assert t.dtype == dtype and t.shape == shape and t.get_device() == device
             t = t.stride()
         strides.append(t)
-    return _recur_plan(shape, dtype, tuple(strides), _stream(f, stream))
+    return _recur_plan(shape, dtype, tuple(strides), _stream(f))
 
 
 def _state(t, f):
@@ -187,7 +188,7 @@ def _lengths(t, f):
     return t.data_ptr()
 
 
-def recurrence(f, u, o=None, h0=None, lengths=None, save=False, out=None, h_last=None, stream=None):
+def recurrence(f, u, o=None, h0=None, lengths=None, save=False, out=None, h_last=None):
     """h_t = a_t h_{t-1} + (1 - a_t) u_t with a = sigmoid(f), y = sigmoid(o) h (or h): (y, last states, saved).
 
     f, u, o (batch, steps, dim) of one type, strided as they come (columns of one projection); h0 (batch, dim) of
@@ -201,14 +202,14 @@ def recurrence(f, u, o=None, h0=None, lengths=None, save=False, out=None, h_last
     saved = None
     if save:
         saved = torch.empty(((T + SAVE_STEPS - 1) // SAVE_STEPS, B, C), dtype=torch.float32, device=f.device)
-    cfg, nbytes = _recur_config(f, stream, u, o, y)
+    cfg, nbytes = _recur_config(f, u, o, y)
     ws = _scratch(nbytes, f)
     _check(lib().choco_recur_forward(cfg, f.data_ptr(), u.data_ptr(), _ptr(o), _state(h0, f), _lengths(lengths, f), y.data_ptr(),
                                      _state(h_last, f), _ptr(saved), _ptr(ws), nbytes), "choco_recur_forward")
     return y, h_last, saved
 
 
-def recurrence_grad(f, u, saved, dy, o=None, lengths=None, dlast=None, stream=None):
+def recurrence_grad(f, u, saved, dy, o=None, lengths=None, dlast=None):
     """Backward pass of `recurrence`: (df, du, do or None, dh0), the first three columns of one matrix.
 
     saved as `recurrence(..., save=True)` returned it; dlast the gradient of the last states, zero without."""
@@ -220,7 +221,7 @@ def recurrence_grad(f, u, saved, dy, o=None, lengths=None, dlast=None, stream=No
     grads = torch.empty((B, T, parts, C), dtype=f.dtype, device=f.device).unbind(2)
     df, du, do = grads[0], grads[1], None if o is None else grads[2]
     dh0 = torch.empty((B, C), dtype=torch.float32, device=f.device)
-    cfg, nbytes = _recur_config(f, stream, u, o, dy, df, du, do)
+    cfg, nbytes = _recur_config(f, u, o, dy, df, du, do)
     ws = _scratch(nbytes, f)
     _check(lib().choco_recur_backward(cfg, f.data_ptr(), u.data_ptr(), _ptr(o), _lengths(lengths, f), saved.data_ptr(),
                                       dy.data_ptr(), _state(dlast, f), df.data_ptr(), du.data_ptr(), _ptr(do), dh0.data_ptr(),
@@ -260,10 +261,10 @@ class AdamW:
     step of `binding.Choco` on the same X may follow.  tensors: (start, length) arrays, e.g. the first two of a layer table;
     the whole row is one without."""
 
-    def __init__(self, X, d, tensors=None, stream=None, **kw):
+    def __init__(self, X, d, tensors=None, **kw):
         assert X.is_cuda and X.dtype == torch.float32 and X.is_contiguous() and X.dim() == 2
         self.X, self.d = X, int(d)
-        self.cfg, keep = make_adamw_config(X.shape[0], d, X.shape[1], tensors, stream=_stream(X, stream), **kw)
+        self.cfg, keep = make_adamw_config(X.shape[0], d, X.shape[1], tensors, stream=_stream(X), **kw)
         need, a = _size(), _vp()
         _check(lib().choco_adamw_workspace_bytes(ctypes.byref(self.cfg), ctypes.byref(need)), "choco_adamw_workspace_bytes")
         self.workspace = torch.empty(need.value + 256, dtype=torch.uint8, device=X.device)

@@ -159,6 +159,22 @@ def test_recurrence_refuses_a_small_workspace():
             assert L.choco_recur_backward(ctypes.byref(c), P, P, P, None, P, P, P, P, P, P, P, ws, nbytes) == code
 
 
+def test_more_than_a_launch_holds_is_unsupported():
+    big = 2 ** 31 - 1
+    out = ctypes.c_size_t()
+    c = recur_cfg(batch=500, steps=big, dim=4096, **{k: (big * 4096, 4096) for k in ("f", "u", "o", "y", "df", "du", "do")})
+    assert recur_codes(c) == (B.E_UNSUPPORTED, B.E_UNSUPPORTED)
+    assert T.lib().choco_recur_workspace_bytes(ctypes.byref(c), ctypes.byref(out)) == B.E_UNSUPPORTED
+    c = embed_cfg(n=1, tokens=big, vocab=10, dim=big, token_stride=big, table_stride=10 * big, row_stride=big * big, row_ld=big)
+    assert embed_codes(c) == (B.E_INVAL, B.E_INVAL)                    # an array of more than 2^60 entries
+    c = embed_cfg(n=1, tokens=2 ** 30, vocab=10, dim=2 ** 28, token_stride=2 ** 30, table_stride=10 * 2 ** 28, row_stride=2 ** 58,
+                  row_ld=2 ** 28)
+    assert embed_codes(c)[1] == B.E_UNSUPPORTED
+    assert T.lib().choco_embed_workspace_bytes(ctypes.byref(c), ctypes.byref(out)) == B.E_UNSUPPORTED
+    c = embed_cfg(n=1, tokens=2 ** 30, vocab=10, dim=64, token_stride=2 ** 30, row_stride=2 ** 36, row_ld=64)
+    assert embed_codes(c)[0] == B.E_UNSUPPORTED
+
+
 def test_recurrence_with_nothing_to_do():
     assert recur_codes(recur_cfg(batch=0)) == (B.OK, B.OK)
     assert recur_codes(recur_cfg(dim=0)) == (B.OK, B.OK)
