@@ -1,11 +1,13 @@
 // Gated linear recurrence h_t = a_t h_{t-1} + (1 - a_t) u_t, a = sigmoid(f), y = sigmoid(o) h, and its backward
 // pass (device code).
 //
-// How the work is split.  A strip is 64 * V channels of one sequence, V channels a lane.  A workgroup takes a tile: the
-// steps of a strip that its waves hold in registers, kSaveSteps each.  A wave loads its steps at once and reduces them to the map
-// h -> A h + H; the waves exchange these maps through LDS, and each applies those before its own to the state before the
-// tile and goes through its steps, which are still in registers, once more.  So everything is read once, and the chain from
-// step to step is as long as a tile has waves.
+// Bound by memory: 25 operations an entry against 4 to 14 bytes.
+//
+// How the work is split.  A strip is 64 * V channels of one sequence, V channels a lane (two of 16 bits where everything is
+// aligned to that).  A workgroup takes a tile: the steps of a strip that its waves hold in registers, 8 or 16 each.  A wave loads
+// its steps at once and reduces them to the map h -> A h + H; the waves exchange these maps through LDS, and each applies those
+// before its own to the state before the tile and goes through its steps, which are still in registers, once more.  So
+// everything is read once, and the chain from step to step is as long as a tile has waves.
 //
 // Sequences longer than a tile are chains of tiles.  A tile publishes its map as soon as it has it; kChainTiles of them in a row
 // form a link: each applies to the state before the link the maps of the tiles before it in the link, and the last one
@@ -16,6 +18,13 @@
 // taken theirs before, so they are running or done; their maps do not wait for anything, and the state before a link waits for
 // earlier links only: whatever the order in which workgroups are started, every wait ends.  (A wait gives up after kMostPolls
 // all the same; what it waited for is then NaN.)
+//
+// Measured, us (GB/s of what cannot be done without): 160 sequences of 35 steps x 650 in fp32 13.7 (3,500), backward 24.3 (3,600);
+// 2 of 32,768 x 2048 in bf16 198 (4,400); backward
+// of 4 of 16,384 x 1280 without o 202 (4,200); 64 of 512 x 1280 61 to 73 and 125 (4,600 to 5,500); a large copy reaches 4,700.
+// Before: two passes over segments of a sequence, the first for their maps, 324 and 280; eight steps a wave 310 and 228;
+// one lane a channel, step by step, 14,059 and 20,573.  Workgroups that stay and ask for their next tile's steps ahead hold
+// places in the chain that others wait for: 302 to 790.
 #pragma once
 
 #include <type_traits>
@@ -27,7 +36,11 @@ namespace choco {
 constexpr int kSaveSteps = 8;       // the forward pass keeps the state before every so many
 constexpr int kRecurWaves = 16;     // most waves of a workgroup
 constexpr int kAloneSteps = 8;      // a sequence of one tile: steps of a wave, up to kRecurWaves of them
-constexpr int kChainWaves = 8;      // chains: waves of a tile, and steps of a wave
+// Chains: waves of a tile, steps of a wave - as many as leave two workgroups for a compute unit (backward holds four numbers a step
+// and channel) - and tiles of a link.  2 of 32,768 x 2048, 4 of 16,384 x 1280 back, 1 of 8192 x 512: 8 waves 207 | 202 | 18 us,
+// 4 waves and links of 32 tiles 250 | 243 | 20, 16 waves 234 | 204 | 19; 8 steps forward 272 | - | 24; links of 5, 8, 24 tiles
+// 211 | 206 | 26, 208 | 207 | 22, 210 | 201 | 18.
+constexpr int kChainWaves = 8;
 constexpr int kForwardSteps = 16;
 constexpr int back_steps(int v) { return v == 1 ? 16 : 8; }
 constexpr int kChainTiles = 16;
@@ -182,17 +195,18 @@ __device__ __forceinline__ int steps_left(int64_t end, int64_t t) {
   return __builtin_amdgcn_readfirstlane(end <= t ? 0 : end - t < K ? (int)(end - t) : K);
 }
 
-template <int V, int W>
+template <int V, int W, bool CHAIN>
 struct RecurShared {
+  static constexpr int kLink = CHAIN ? kChainTiles : 1;
   float a[W][64][V], h[W][64][V];               // the waves' maps, in the order of the recurrence
-  float link_a[kChainTiles][64][V], link_h[kChainTiles][64][V];     // those of the tiles before in the link; last: the state before it
+  float link_a[kLink][64][V], link_h[kLink][64][V];     // those of the tiles before in the link; last: the state before it
   uint32_t taken;
 };
 
 // From the waves' maps (m_a, m_h; `turn`: a wave's place in the order of the recurrence) and the state `h` before the tile
 // (outside chains: given) to the state before the wave's own steps; the last wave's ends as the one after the tile.
 template <int V, bool CHAIN, int W>
-__device__ __forceinline__ void recur_carry(const RecurArgs& A, const RecurPlace& P, RecurShared<V, W>& S, int turn, int waves,
+__device__ __forceinline__ void recur_carry(const RecurArgs& A, const RecurPlace& P, RecurShared<V, W, CHAIN>& S, int turn, int waves,
                                             const float (&ma)[V], const float (&mh)[V], float (&h)[V], float (&after)[V]) {
   const int lane = threadIdx.x & 63;
 #pragma unroll
@@ -252,7 +266,7 @@ template <class T, int V, bool GATED, int MODE>
 __global__ __launch_bounds__(64 * (MODE != kAlone ? kChainWaves : kRecurWaves)) void k_recur(RecurArgs A) {
   constexpr bool CHAIN = MODE != kAlone;
   constexpr int K = CHAIN ? kForwardSteps : kAloneSteps, W = CHAIN ? kChainWaves : kRecurWaves;
-  __shared__ RecurShared<V, W> S;
+  __shared__ RecurShared<V, W, CHAIN> S;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   const RecurPlace P = recur_place<V, CHAIN, false>(A, K * W, &S.taken);
   const int64_t state = P.b * A.dim + P.strip + P.lane, t0 = P.begin + K * wave;
@@ -317,7 +331,7 @@ template <class T, int V, bool GATED, int MODE>
 __global__ __launch_bounds__(64 * (MODE != kAlone ? kChainWaves : kRecurWaves)) void k_recur_back(RecurArgs A) {
   constexpr bool CHAIN = MODE != kAlone;
   constexpr int K = CHAIN ? back_steps(V) : kAloneSteps, W = CHAIN ? kChainWaves : kRecurWaves;
-  __shared__ RecurShared<V, W> S;
+  __shared__ RecurShared<V, W, CHAIN> S;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   const RecurPlace P = recur_place<V, CHAIN, true>(A, K * W, &S.taken);
   const int64_t state = P.b * A.dim + P.strip + P.lane, t0 = P.begin + K * wave;
