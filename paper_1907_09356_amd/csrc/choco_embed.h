@@ -26,6 +26,7 @@ struct EmbedArgs {
   bool zero_past;                    // cleared past the caches
 };
 
+constexpr int kFew = 128;                              // so many tokens are compared with each other instead of ordered
 constexpr int kSortThreads = 1024;                     // a workgroup that orders all of a worker's tokens in LDS ...
 constexpr int kSortRounds = 8;
 constexpr int kSortOne = kSortThreads * kSortRounds;   // ... of which there are no more than this
@@ -421,6 +422,50 @@ __global__ __launch_bounds__(256) void k_embed_sum(EmbedArgs A) {
       for (int i = 0; i < V; ++i) sum[i] = 0.0f;
     }
   }
+}
+
+// A few tokens (no more than kFew): a wave for each of them and 64 * V columns.  The first of its kind adds up the rows of all of
+// its kind, in their order.  One launch instead of three: 64 tokens of 512 added 17.3 -> 6.0 us, 8 x 128 19.2 -> 5.9; of 128 tokens that are all the
+// same one wave adds up 128 rows, eight at a time (13.5 -> 10.4).
+template <class Tok, class Row, int V, bool ADD>
+__global__ __launch_bounds__(256) void k_embed_few(EmbedArgs A) {
+  const int lane = threadIdx.x & 63, w = blockIdx.y;
+  const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (unit >= A.ntokens * A.column_chunks) return;
+  const int r = (int)(unit / A.column_chunks);
+  const int64_t c = (unit % A.column_chunks * 64 + lane) * V;
+  const int32_t low = lane < A.ntokens ? token_at<Tok>(A, w, lane) : -1, high = lane + 64 < A.ntokens ? token_at<Tok>(A, w, lane + 64) : -1;
+  const int32_t token = r < 64 ? __builtin_amdgcn_readlane(low, r) : __builtin_amdgcn_readlane(high, r - 64);
+  if (token < 0) return;
+  uint64_t same_low = __ballot(low == token), same_high = __ballot(high == token);
+  if (r < 64 ? (same_low & (((uint64_t)1 << r) - 1)) != 0 : (same_low | (same_high & (((uint64_t)1 << (r - 64)) - 1))) != 0) return;
+  const bool in = c < A.dim;
+  const int64_t column = in ? c : 0;
+  const Row* rows = (const Row*)A.rows + (int64_t)w * A.row_stride + column;
+  float sum[V], old[V];
+  if (ADD) load_floats<float, V>(sums_of(A, w, (uint32_t)token, column), old);
+#pragma unroll
+  for (int i = 0; i < V; ++i) sum[i] = 0.0f;
+  int left = __popcll(same_low) + __popcll(same_high), at = r;
+  for (; left > 0; left -= kAhead) {
+    RowWords<Row, V> x[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {     // (where none is left: the last one again)
+      if (same_low) {
+        at = __builtin_ctzll(same_low);
+        same_low &= same_low - 1;
+      } else if (same_high) {
+        at = 64 + __builtin_ctzll(same_high);
+        same_high &= same_high - 1;
+      }
+      x[j].template load<false>(rows + at * A.row_ld);
+    }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+#pragma unroll
+      for (int i = 0; i < V; ++i) sum[i] += j < left ? x[j].at(i) : 0.0f;
+  }
+  if (in) put_sums<ADD, false, V>(A, sums_of(A, w, (uint32_t)token, column), sum, old);
 }
 
 // The sum of V columns of partial sums (slot 0) from piece `from` to before `to`, onto `sum`.

@@ -96,7 +96,7 @@ struct EmbedLayout {
 
 EmbedLayout embed_layout(const choco_embed_config& c) {
   EmbedLayout L{};
-  if (c.n == 0 || c.tokens == 0 || c.dim == 0) return L;
+  if (c.n == 0 || c.tokens <= kFew || c.dim == 0) return L;
   L.one = c.tokens <= kSortOne;
   int bits = 1;
   while (c.vocab >> bits) ++bits;    // keys go up to vocab itself
@@ -461,8 +461,38 @@ int choco_embed_backward(const choco_embed_config* cfg, const void* tokens_dev, 
   if (!launch_fits((double)zero_blocks * c.n + c.n, kSortThreads)) return CHOCO_E_UNSUPPORTED;
   A.zero_blocks = (uint32_t)zero_blocks;
   A.zero_past = (double)c.n * (double)c.vocab * (double)c.dim * 4 > 96.0 * 1048576.0;   // (692 MB cleared and 9 K rows added: 142 | 139 us)
-  if (c.tokens == 0) {   // nothing but zeros
-    k_embed_count<int32_t, true, kShortRounds><<<dim3(A.zero_blocks, (uint32_t)c.n), kChunkThreads, 0, stream>>>(A, 0);
+  const size_t size = type_bytes(c.row_type);
+  // Two columns a lane: with eight (or four) a wave holds so many rows of sums and old values that too few waves fit to keep the
+  // memory busy (65,536 rows of 1024 in bf16: eight 111 us, four 101, two 99).
+  int v = embed_width(2, c.dim, {{dy_dev, size}, {dtable_dev, 4}}, {{c.row_ld, size}, {c.row_stride, size}, {c.table_stride, 4}});
+  if (c.dim <= 64) v = 1;     // (no lane without columns)
+  // Rows and sums past the caches where the rows do not fit there (65,536 of 1024 in bf16, 134 MB: 99 us through, 88 with the rows
+  // past them, 83 with the sums as well; 23 MB, just written: 26 and 30).
+  const bool past = (double)c.n * (double)c.tokens * (double)c.dim * size > 96.0 * 1048576.0;
+  A.column_chunks = (c.dim + 64 * v - 1) / (64 * v);
+  if (c.tokens <= kFew) {
+    if (!launch_fits((double)c.tokens * (double)A.column_chunks, 64)) return CHOCO_E_UNSUPPORTED;
+    if (!accumulate) {   // zeros first
+      k_embed_count<int32_t, true, kShortRounds><<<dim3(A.zero_blocks, (uint32_t)c.n), kChunkThreads, 0, stream>>>(A, 0);
+      TRY_HIP(hipGetLastError());
+    }
+    if (c.tokens == 0) return CHOCO_OK;
+    with_type(c.row_type, [&](auto row) {
+      const auto launch = [&](auto token, auto width, auto add) {
+        k_embed_few<decltype(token), decltype(row), decltype(width)::value, decltype(add)::value>
+            <<<dim3(blocks_of(c.tokens * A.column_chunks, 4), (uint32_t)c.n), 256, 0, stream>>>(A);
+      };
+      const auto with_add = [&](auto token, auto width) {
+        if (accumulate) launch(token, width, std::true_type{});
+        else launch(token, width, std::false_type{});
+      };
+      const auto with_lanes = [&](auto token) {
+        if (v == 2) with_add(token, std::integral_constant<int, 2>{});
+        else with_add(token, std::integral_constant<int, 1>{});
+      };
+      if (c.token_type == CHOCO_I32) with_lanes(int32_t{});
+      else with_lanes(int64_t{});
+    });
     TRY_HIP(hipGetLastError());
     return CHOCO_OK;
   }
@@ -474,15 +504,6 @@ int choco_embed_backward(const choco_embed_config* cfg, const void* tokens_dev, 
   A.pieces = L.pieces;
   A.digit_bits = L.digit_bits;
   A.passes = L.passes;
-  const size_t size = type_bytes(c.row_type);
-  // Two columns a lane: with eight (or four) a wave holds so many rows of sums and old values that too few waves fit to keep the
-  // memory busy (65,536 rows of 1024 in bf16: eight 111 us, four 101, two 99).
-  int v = embed_width(2, c.dim, {{dy_dev, size}, {dtable_dev, 4}}, {{c.row_ld, size}, {c.row_stride, size}, {c.table_stride, 4}});
-  if (c.dim <= 64) v = 1;     // (no lane without columns)
-  // Rows and sums past the caches where the rows do not fit there (65,536 of 1024 in bf16, 134 MB: 99 us through, 88 with the rows
-  // past them, 83 with the sums as well; 23 MB, just written: 26 and 30).
-  const bool past = (double)c.n * (double)c.tokens * (double)c.dim * size > 96.0 * 1048576.0;
-  A.column_chunks = (c.dim + 64 * v - 1) / (64 * v);
   if (!launch_fits((double)A.pieces * (double)A.column_chunks, 64) || !launch_fits((double)L.chunks + zero_blocks, kChunkThreads))
     return CHOCO_E_UNSUPPORTED;
   const auto order = [&](auto token) {

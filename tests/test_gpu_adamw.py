@@ -272,6 +272,32 @@ def test_rows_of_more_than_32_bits_of_entries(bits):
     assert int((X != 0).sum()) == 2 * (3 + 1025)
 
 
+def test_state_that_does_not_fit_the_caches():
+    # more than 320 MB go past the caches: the same bits as a worker at a time; in 8 bits, whose words depend on the worker, the
+    # first worker's
+    n, d = 9, 4_000_003
+    ld = d + 1
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    X0 = torch.empty((n, ld), device="cuda").normal_(generator=gen)
+    G = torch.empty((n, ld), device="cuda").normal_(generator=gen)
+    for bits in (32, 8):
+        X = X0.clone()
+        opt = T.AdamW(X, d, ([0, 1_000_004], [1_000_001, 2_999_999]), state_bits=bits, weight_decay=0.1)
+        for w in range(n if bits == 32 else 1):
+            x = X0[w:w + 1].clone()
+            alone = T.AdamW(x, d, ([0, 1_000_004], [1_000_001, 2_999_999]), state_bits=bits, weight_decay=0.1)
+            for _ in range(2):
+                alone.step(G[w:w + 1], 0.01)
+            if w == 0:
+                for _ in range(2):
+                    opt.step(G, 0.01)
+            assert torch.equal(x[0], X[w])
+            for a, b in zip(alone.moments(), opt.moments()):
+                assert torch.equal(a[0], b[w])
+            alone.close()
+        opt.close()
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 def test_other_streams_and_graphs(bits):
     n, d = 3, 5000

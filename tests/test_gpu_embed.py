@@ -41,6 +41,8 @@ SIZES = [   # n, tokens, vocab, dim, how
     (1, 1, 1, 1, "uniform"), (1, 1, 5, 650, "uniform"), (3, 7, 11, 33, "uniform"), (2, 64, 50, 4, "frequent"),
     (2, 65, 200, 130, "one"), (8, 20, 333, 650, "uniform"), (1, 300, 40, 257, "frequent"), (2, 50, 9, 12, "outside"),
     (1, 2049, 700, 96, "frequent"), (1, 9001, 1500, 20, "frequent"), (2, 4100, 33, 66, "uniform"), (1, 5000, 7, 5, "one"),
+    (2, 128, 60, 70, "frequent"), (2, 129, 60, 70, "frequent"), (1, 128, 3, 10, "one"), (1, 8192, 5000, 4, "frequent"),
+    (1, 8193, 5000, 4, "frequent"), (1, 131_072, 9000, 2, "frequent"),
     (1, 40_000, 70_000, 3, "frequent"), (1, 20_011, 300, 40, "one"), (3, 17_000, 1000, 8, "uniform"), (1, 6000, 1_100_000, 2, "frequent"),
 ]
 
@@ -185,6 +187,31 @@ def test_tables_of_more_than_32_bits_of_entries():
     T.embed_grad(tokens, dy, dtable)
     assert dtable[0, :, 0].nonzero()[:, 0].tolist() == [0, vocab - 2, vocab - 1]
     assert float(dtable[0].sum(dtype=torch.float64)) == 3 * 5.0 * dim
+
+
+@pytest.mark.parametrize("kind", [torch.float32, torch.bfloat16])
+def test_results_that_do_not_fit_the_caches(kind):
+    # rows of more than 96 MB are written and read past the caches: the same bits as in shares of them (lookups), and as sums
+    # in 64 bits within the bound (gradients)
+    count, vocab, dim = 60_000, 9000, 1024 if kind == torch.bfloat16 else 512
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    tokens = torch.from_numpy(draw_tokens(1, count, vocab, 13, "frequent")).cuda()
+    table = torch.empty((1, vocab, dim), dtype=kind, device="cuda").normal_(generator=gen)
+    y = T.embed(tokens, table, scale=3.0)
+    for at in range(0, count, 15_000):
+        assert torch.equal(y[:, at:at + 15_000], T.embed(tokens[:, at:at + 15_000].contiguous(), table, scale=3.0))
+    there = tokens[0] >= 0
+    rows = y[0, there].double()
+    for accumulate in (False, True):
+        old = torch.empty((1, vocab, dim), device="cuda").normal_(generator=gen)
+        got = old.clone()
+        T.embed_grad(tokens, y, got, scale=0.5, accumulate=accumulate)
+        base = old[0].double() if accumulate else torch.zeros((vocab, dim), dtype=torch.float64, device="cuda")
+        want = base.index_add(0, tokens[0, there], rows * 0.5)
+        size = torch.zeros_like(base).index_add_(0, tokens[0, there], rows.abs() * 0.5)
+        number = torch.bincount(tokens[0, there], minlength=vocab)[:, None]
+        bound = U * (number + 3) * size + U * (base.abs() + size)
+        assert bool(((got[0].double() - want).abs() <= bound).all())
 
 
 def test_other_streams_and_graphs():

@@ -298,6 +298,26 @@ def test_many_sequences():
     check("dh0", dh0, want["dh0"], want["bdh0"], torch.float32)
 
 
+@pytest.mark.parametrize("dtype,batch", [(torch.float32, 40), (torch.bfloat16, 44), (torch.bfloat16, 120)])
+@pytest.mark.parametrize("gated", [True, False])
+def test_results_that_do_not_fit_the_caches(dtype, batch, gated):
+    # more than 128 and more than 384 MB are written, and read, past the caches: the same bits as a few sequences at a time
+    steps, dim, few = 700, 770, 4
+    gen = torch.Generator(device="cuda").manual_seed(batch)
+    proj = torch.empty((batch, steps, 3 * dim), device="cuda", dtype=dtype).normal_(generator=gen)
+    f, u, o = proj.split(dim, 2)
+    o = o if gated else None
+    dy = torch.empty((batch, steps, dim), device="cuda", dtype=dtype).normal_(generator=gen)
+    y, last, saved = T.recurrence(f, u, o, save=True)
+    grads = T.recurrence_grad(f, u, saved, dy, o)
+    for b in range(0, batch, few):
+        p = slice(b, b + few)
+        part = T.recurrence(f[p], u[p], None if o is None else o[p], save=True)
+        assert torch.equal(part[0], y[p]) and torch.equal(part[1], last[p]) and torch.equal(part[2], saved[:, p])
+        for a, c in zip(T.recurrence_grad(f[p], u[p], part[2], dy[p], None if o is None else o[p]), grads):
+            assert a is None and c is None or torch.equal(a, c[p])
+
+
 def test_empty_shapes():
     h0 = torch.ones((3, 8), device="cuda")
     f = torch.zeros((3, 0, 8), device="cuda")
