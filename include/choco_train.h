@@ -99,7 +99,7 @@ int choco_recur_backward(const choco_recur_config* cfg, const void* f_dev, const
  * state_bits 32: m and v in fp32.  8: in a byte each, relative to a power of two that CHOCO_ADAMW_BLOCK consecutive
  * entries of a tensor share (blocks start at its first entry) and that brings the largest of them into (0.9375, 1.875].
  * m is a sign, 4 bits of exponent and 3 of mantissa, v 5 and 3, both with gradual underflow: m reaches down to 2^-17,
- * v to 2^-33 of its block's largest.  A block whose largest lies below the normal numbers is held as zero.  Rounding is
+ * v to 2^-33 of its block's largest.  (A block whose largest lies below the normal numbers is held relative to 2^-126.)  Rounding is
  * stochastic: with nearest rounding a v that moves by 0.1 % a step would never leave its code.  The random bits
  * are those of the Philox word of (seed, step, worker, entry), stream 3, the lower 16 for m and the upper 16 for
  * v, so a run is reproducible.  A positive v is never held as zero (x would move by m / eps).  The update of x takes m and
@@ -118,7 +118,7 @@ typedef struct {
   const float* weight_decay_host; /* per tensor (or one entry where ntensors = 0), >= 0; NULL: none  */
   const float* lr_scale_host;     /* likewise; NULL: 1                                                */
   double beta1, beta2;   /* in [0, 1)                                                                 */
-  double eps;            /* > 0, and not 0 as a float                                                 */
+  double eps;            /* >= 2^-60 / sqrt(1 - beta2) (2.8e-17 for 0.999): below that v's own range in fp32 shows in x */
   int32_t state_bits;    /* 32 or 8                                                                   */
   uint64_t seed;
   void* stream;

@@ -16,6 +16,9 @@ enum { STREAM_ADAMW = 3 };
 constexpr int kMomentBlock = 256;   // entries of a tensor that share a scale
 constexpr int kTileBlocks = 4;      // ... and how many such blocks of one tensor a wave takes
 constexpr int kTile = kMomentBlock * kTileBlocks;
+// eps is at least this / sqrt(1 - beta2).  A step rounds v by up to 2^-149 (two products below the normal numbers), and
+// t steps' worth of that over 1 - beta2^t, the root taken, is 2^-74.5 / sqrt(1 - beta2): 2^-14 of eps at the most.
+constexpr double kLeastEps = 0x1p-60;
 
 // A piece of a tensor: what a wave takes.
 struct AdamwTile {
@@ -41,9 +44,12 @@ struct AdamwArgs {
 };
 
 // The new x.  Square root and reciprocal to one unit in the last place each: they only scale the step, which is
-// small against x.  (A v below the normal numbers counts as zero here: its root is nothing against eps.)
+// small against x.  The square root's instruction takes a v below the normal numbers for zero, so a small one is scaled up
+// first; what then is lost of v are fp32's own roundings, which the least eps that a plan may have (kLeastEps) outweighs.  It
+// is a normal number, as the reciprocal's instruction wants it.
 __device__ __forceinline__ float adamw_x(const AdamwArgs& A, float x, float m, float v, float rate, float keep) {
-  const float root = __builtin_amdgcn_sqrtf(v) * A.root_scale + A.eps;
+  const bool low = v < 0x1p-100f;
+  const float root = __builtin_amdgcn_sqrtf(low ? v * 0x1p32f : v) * (low ? A.root_scale * 0x1p-16f : A.root_scale) + A.eps;
   return x * keep - rate * m * __builtin_amdgcn_rcpf(root);
 }
 
@@ -52,13 +58,15 @@ __device__ __forceinline__ float adamw_x(const AdamwArgs& A, float x, float m, f
 // A power of two, because the codes are then exact multiples of one another from step to step: a moment that moves by
 // 0.1 % in a step changes its code in one step of a hundred, whereas a scale that follows the largest entry would put
 // every entry between two codes in every step, and rounding noise of 4 % a step adds up over the 1 / (1 - beta2) steps
-// that v remembers.  (Simulated over 4000 steps: v stays within 0.3 % of itself on average, with a spread of 20 %; m 9 %.)  0: the block is held as zero; 255 and more: something in it is infinite or NaN.
+// that v remembers.  (Simulated over 4000 steps: v stays within 0.3 % of itself on average, with a spread of 20 %; m 9 %.)  A
+// block whose largest lies below the normal numbers has the least normal scale, that of field 1; code 1 of v then stands for less than any
+// number, so a positive v stays positive.  Fields of 255 and more: something in the block is infinite or NaN.
 typedef uint16_t Fields __attribute__((ext_vector_type(2)));   // of m and of v
 __device__ __forceinline__ uint32_t scale_field(float x) { return ((__float_as_uint(x) & 0x7FFFFFFFu) + 0xFFFFFu) >> 23; }
 __device__ __forceinline__ float scale_of(uint32_t field) { return __uint_as_float(field >= 255u ? 0x7FC00000u : field << 23); }
-// 2^-k of a scale 2^k; 0 for the fields of no power of two.
+// 2^-k of a scale 2^k, fields from 1; 0 for those of no power of two.
 __device__ __forceinline__ float inverse_scale(uint32_t field) {
-  return field == 0u || field >= 255u ? 0.0f : field == 254u ? 5.87747175e-39f : __uint_as_float((254u - field) << 23);
+  return field >= 255u ? 0.0f : field == 254u ? 5.87747175e-39f : __uint_as_float((254u - field) << 23);
 }
 
 // What a code of 3 mantissa bits under TOP exponents stands for relative to its scale, at most 1.875: its bits are those of a
@@ -194,7 +202,7 @@ __device__ __forceinline__ void adamw_tile(const AdamwArgs& A, const AdamwTile& 
   for (int b = 0; b < BLOCKS; ++b) {
     const int64_t e = at + b * kMomentBlock;
     const int left = FULL ? kMomentBlock : tile.len - first - b * kMomentBlock;
-    Fields top = {0, 0};
+    Fields top = {1, 1};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if (BITS == 8) {

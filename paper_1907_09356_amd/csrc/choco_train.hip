@@ -311,7 +311,7 @@ int check_adamw(const choco_adamw_config* c) {
   if (ld < c->d || (ld & 3) != 0 || ld > kMaxIndex) return CHOCO_E_INVAL;
   if (!(c->beta1 >= 0.0 && c->beta1 < 1.0) || !(c->beta2 >= 0.0 && c->beta2 < 1.0)) return CHOCO_E_INVAL;
   if ((float)c->beta1 >= 1.0f || (float)c->beta2 >= 1.0f) return CHOCO_E_INVAL;
-  if (!((float)c->eps > 0.0f) || !std::isfinite((float)c->eps)) return CHOCO_E_INVAL;
+  if (!(c->eps >= kLeastEps / std::sqrt(1.0 - c->beta2)) || !std::isfinite((float)c->eps)) return CHOCO_E_INVAL;
   if (c->state_bits != 32 && c->state_bits != 8) return CHOCO_E_INVAL;
   if (c->ntensors < 0 || (c->ntensors > 0 && (!c->start_host || !c->len_host))) return CHOCO_E_INVAL;
   const int32_t rows = c->ntensors > 0 ? c->ntensors : 1;

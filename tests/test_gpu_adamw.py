@@ -198,6 +198,32 @@ def test_no_gradient_at_all(bits):
 
 
 @pytest.mark.parametrize("bits", [32, 8])
+def test_the_least_eps_and_gradients_whose_squares_underflow(bits):
+    # x starts at 0, so x' is the step alone.  v is off by what fp32 loses below its normal numbers, 2^-149, which is 2^-14 of
+    # the least eps once it is under the root; the step's other roundings as above, m's own below the normal numbers 2^-149 too
+    sizes = [0.0, 1e-38, 1e-35, 1e-30, 1e-24, 1e-22, 1e-21, 3e-21, 1e-20, 1e-19, 3e-19, 1e-18, 1e-17, 1e-15, 1e-10, 1.0]
+    g = np.repeat(np.array(sizes), BLOCK) * (0.5 + np.random.default_rng(1).random(BLOCK * len(sizes)))
+    G = torch.from_numpy(g.astype(np.float32)[None]).cuda()
+    gr = G.double().cpu().numpy()
+    X = torch.zeros_like(G)
+    betas = (0.9, 0.999)
+    eps = 2.0 ** -60 / (1 - betas[1]) ** 0.5
+    opt = T.AdamW(X, g.size, betas=betas, eps=eps, state_bits=bits, seed=3)
+    for t in range(1, 4):
+        m0, v0 = (s.double().cpu().numpy() for s in opt.moments())
+        X.zero_()
+        opt.step(G, 1.0)
+        m, v = betas[0] * m0 + (1 - betas[0]) * gr, betas[1] * v0 + (1 - betas[1]) * gr * gr
+        step = m / (1 - betas[0] ** t) / (np.sqrt(v / (1 - betas[1] ** t)) + eps)
+        bound = np.abs(step) * (2.0 ** -14 + 64 * U + 4 * 2.0 ** -149 / np.maximum(m, 1e-300))
+        assert np.all(np.abs(X.double().cpu().numpy() + step) <= bound), t
+        gm, gv = (s.double().cpu().numpy() for s in opt.moments())
+        assert np.all(gv[v >= 2.0 ** -148] > 0) and np.all(gm[m > 0] > 0)
+        assert not gm[gr == 0].any() and not gv[gr == 0].any()
+    opt.close()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
 def test_a_worker_whose_factor_is_not_finite_is_left_alone(bits):
     n, d = 5, 1500
     X = torch.from_numpy(rows(n, d, d, 1, 0.1)).cuda()

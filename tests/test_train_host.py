@@ -207,6 +207,15 @@ def test_adamw_refuses_bad_configurations(over):
     assert adamw_code(**over) == B.E_INVAL
 
 
+@pytest.mark.parametrize("beta2", [0.0, 0.9, 0.999, 0.99999])
+def test_adamw_refuses_an_eps_that_the_second_moments_range_outweighs(beta2):
+    least = 2.0 ** -60 / (1 - beta2) ** 0.5
+    for eps in (1e-39, 1e-30, least / 2, float("nan")):
+        assert adamw_code(betas=(0.9, beta2), eps=eps) == B.E_INVAL
+    for eps in (least, 1e-15, 1e-8):
+        assert adamw_code(betas=(0.9, beta2), eps=eps) == B.OK
+
+
 def test_adamw_accepts_any_disjoint_tensors():
     for bits in (32, 8):
         assert adamw_code(state_bits=bits) == B.OK
