@@ -121,7 +121,7 @@ typedef struct {
   double eps;            /* >= 2^-60 / sqrt(1 - beta2) (2.8e-17 for 0.999): below that v's own range in fp32 shows in x */
   int32_t state_bits;    /* 32 or 8                                                                   */
   uint64_t seed;
-  void* stream;
+  void* stream;          /* of choco_adamw_init and, until choco_adamw_set_stream, of the calls after it */
 } choco_adamw_config;
 
 int choco_adamw_workspace_bytes(const choco_adamw_config* cfg, size_t* bytes_host);
@@ -138,6 +138,9 @@ int choco_adamw_moments(choco_adamw* a, float* m_dev, float* v_dev);
 /* The part of the workspace that holds the moments: what to save, and with t to put back, to resume a run.  In 32 bits it is m
    and then v, n x ld floats each, v on the next multiple of 256 bytes. */
 int choco_adamw_state(choco_adamw* a, void** state_dev, size_t* bytes_host);
+/* The stream of the calls that follow, at first the configuration's.  Waits for nothing: what is under way on the former stream is
+   the caller's to order. */
+int choco_adamw_set_stream(choco_adamw* a, void* stream);
 int choco_adamw_get_step(choco_adamw* a, uint64_t* t_host);
 int choco_adamw_set_step(choco_adamw* a, uint64_t t);
 /* Does not wait for the stream.  NULL is allowed. */

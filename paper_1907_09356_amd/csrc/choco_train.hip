@@ -818,6 +818,12 @@ int choco_adamw_state(choco_adamw* a, void** state_dev, size_t* bytes_host) {
   return CHOCO_OK;
 }
 
+int choco_adamw_set_stream(choco_adamw* a, void* stream) {
+  if (!a) return CHOCO_E_INVAL;
+  a->stream = (hipStream_t)stream;
+  return CHOCO_OK;
+}
+
 int choco_adamw_get_step(choco_adamw* a, uint64_t* t_host) {
   if (!a || !t_host) return CHOCO_E_INVAL;
   *t_host = a->t;

@@ -1,9 +1,9 @@
 """ctypes binding of include/choco_train.h: embedding lookup and gradient, gated linear recurrence, AdamW.
 
 Argument marshalling only, like `binding`: torch provides device memory and the stream, every computation runs in the
-HIP library.  The functions enqueue on torch's current stream of the tensors' device, an `AdamW` on the one that was
-current when it was made.  As with torch's own operations, a tensor that is used on another stream than the one it was made on
-has to be kept until that stream is done with it.
+HIP library.  Functions and methods enqueue on torch's current stream of the tensors' device.  As with torch's own operations, work of
+one stream that needs that of another has to wait for it, and a tensor that is used on another stream than the one it was
+made on has to be kept until that stream is done with it (an `AdamW` sees to its own workspace).
 """
 import ctypes
 import functools
@@ -23,8 +23,8 @@ TOKEN_TYPES = {torch.int32: I32, torch.int64: I64}
 EXPORTS = [
     "choco_embed_workspace_bytes", "choco_embed_forward", "choco_embed_backward", "choco_recur_saved_bytes",
     "choco_recur_workspace_bytes", "choco_recur_forward", "choco_recur_backward", "choco_adamw_workspace_bytes",
-    "choco_adamw_init", "choco_adamw_step", "choco_adamw_moments", "choco_adamw_state", "choco_adamw_get_step",
-    "choco_adamw_set_step", "choco_adamw_destroy", "choco_train_last_hip_error",
+    "choco_adamw_init", "choco_adamw_step", "choco_adamw_moments", "choco_adamw_state", "choco_adamw_set_stream",
+    "choco_adamw_get_step", "choco_adamw_set_step", "choco_adamw_destroy", "choco_train_last_hip_error",
 ]
 
 _i32, _i64, _u64, _f32, _f64 = ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64, ctypes.c_float, ctypes.c_double
@@ -70,6 +70,7 @@ def lib():
         L.choco_adamw_step.argtypes = [_vp, _vp, _i32, _f32, _vp]
         L.choco_adamw_moments.argtypes = [_vp, _vp, _vp]
         L.choco_adamw_state.argtypes = [_vp, ctypes.POINTER(_vp), size]
+        L.choco_adamw_set_stream.argtypes = [_vp, _vp]
         L.choco_adamw_get_step.argtypes = [_vp, ctypes.POINTER(_u64)]
         L.choco_adamw_set_step.argtypes = [_vp, _u64]
         L.choco_adamw_destroy.argtypes = [_vp]
@@ -263,8 +264,8 @@ class AdamW:
 
     def __init__(self, X, d, tensors=None, **kw):
         assert X.is_cuda and X.dtype == torch.float32 and X.is_contiguous() and X.dim() == 2
-        self.X, self.d = X, int(d)
-        self.cfg, keep = make_adamw_config(X.shape[0], d, X.shape[1], tensors, stream=_stream(X), **kw)
+        self.X, self.d, self.stream = X, int(d), _stream(X)
+        self.cfg, keep = make_adamw_config(X.shape[0], d, X.shape[1], tensors, stream=self.stream, **kw)
         need, a = _size(), _vp()
         _check(lib().choco_adamw_workspace_bytes(ctypes.byref(self.cfg), ctypes.byref(need)), "choco_adamw_workspace_bytes")
         self.workspace = torch.empty(need.value + 256, dtype=torch.uint8, device=X.device)
@@ -284,6 +285,14 @@ class AdamW:
         except Exception:
             pass
 
+    def _follow(self):
+        """Takes the current stream for the next call; the workspace is then kept from reuse until that stream is done, too."""
+        stream = _stream(self.X)
+        if stream != self.stream:
+            self.workspace.record_stream(torch.cuda.current_stream(self.X.device))
+            _check(lib().choco_adamw_set_stream(self.handle, stream), "choco_adamw_set_stream")
+            self.stream = stream
+
     def step(self, G, lr, grad_scale=None):
         """G: gradients (n, ld) of float32 or bfloat16; grad_scale: (n,) of float32 on the device, a factor for each
         worker's gradient (one that is not finite leaves the worker as it is)."""
@@ -291,6 +300,7 @@ class AdamW:
         if grad_scale is not None:
             assert grad_scale.device == G.device and grad_scale.dtype == torch.float32
             assert grad_scale.is_contiguous() and grad_scale.shape == G.shape[:1]
+        self._follow()
         _check(lib().choco_adamw_step(self.handle, _ptr(G), TYPES[G.dtype], float(lr), _ptr(grad_scale)), "choco_adamw_step")
 
     def moments(self):
@@ -301,6 +311,7 @@ class AdamW:
             m, v = (state[at:at + size].view(torch.float32).view(n, ld) for at in (0, (size + 255) // 256 * 256))
         else:
             m, v = torch.empty_like(self.X), torch.empty_like(self.X)
+            self._follow()
             _check(lib().choco_adamw_moments(self.handle, m.data_ptr(), v.data_ptr()), "choco_adamw_moments")
         return m[:, :self.d], v[:, :self.d]
 

@@ -355,6 +355,50 @@ def test_other_streams_and_graphs(bits):
 
 
 @pytest.mark.parametrize("bits", [32, 8])
+def test_the_current_stream_is_followed(bits):
+    # made on one stream, used on another one whose earlier work is still under way, then captured on a third
+    n, d = 3, 5000
+    X0 = torch.from_numpy(rows(n, d, d, 1, 0.1)).cuda()
+    grads = [torch.from_numpy(rows(n, d, d, 2 + t, 0.1)).cuda() for t in range(3)]
+    plain = X0.clone()
+    opt = T.AdamW(plain, d, state_bits=bits, seed=9)
+    want = []
+    for G in grads:
+        opt.step(G, 0.01)
+        want.append((plain.clone(),) + tuple(t.clone() for t in opt.moments()))
+    opt.close()
+    X, G = X0.clone(), torch.zeros_like(X0)
+    opt = T.AdamW(X, d, state_bits=bits, seed=9)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for t in range(2):
+            torch.cuda._sleep(5_000_000)
+            G.copy_(grads[t])
+            opt.step(G, 0.01)
+            got = (X.clone(),) + tuple(s.clone() for s in opt.moments())
+            G.zero_()
+            for a, b in zip(got, want[t]):
+                assert torch.equal(a, b), t
+    torch.cuda.synchronize()
+    x1, s1 = X.clone(), opt.state().clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        G.copy_(grads[2])
+        opt.step(G, 0.01)
+    assert torch.equal(X, x1)           # captured, not run
+    for replay in range(3):
+        graph.replay()
+        for a, b in zip((X,) + opt.moments(), want[2]):
+            assert torch.equal(a, b), replay
+        X.copy_(x1)
+        opt.state().copy_(s1)
+        G.zero_()
+        torch.cuda.synchronize()
+    opt.close()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
 def test_moments_as_copies(bits):
     # the C call writes both moments whatever they are held in, zero outside the tensors
     n, d, tensors = 2, 700, ([5, 300], [200, 333])

@@ -7,6 +7,7 @@ import re
 
 import numpy as np
 import pytest
+import torch
 
 from paper_1907_09356_amd import binding as B
 from paper_1907_09356_amd import train as T
@@ -253,3 +254,61 @@ def test_adamw_refuses_bad_pointers():
     assert L.choco_adamw_set_step(None, 3) == B.E_INVAL
     assert L.choco_adamw_state(None, ctypes.byref(a), ctypes.byref(need)) == B.E_INVAL
     assert L.choco_adamw_destroy(None) == B.OK
+
+
+def test_adamw_refuses_to_set_the_stream_of_nothing():
+    assert T.lib().choco_adamw_set_stream(None, None) == B.E_INVAL
+
+
+# ---- the binding's calls, written down instead of made ----
+class OnDevice(torch.Tensor):
+    """A tensor in host memory that says it is on a device."""
+    is_cuda = True
+    number = 0
+
+    def get_device(self):
+        return self.number
+
+
+def on_device(t):
+    return torch.Tensor._make_subclass(OnDevice, t)
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """[(name, arguments)] of the library's calls; calls.current: the current stream."""
+    class Calls(list):
+        current = 0
+
+    made = Calls()
+
+    class Library:
+        def __getattr__(self, name):
+            def call(*args):
+                made.append((name, args))
+                return B.OK
+            call.__name__ = name
+            return call
+
+    monkeypatch.setattr(T, "lib", Library)
+    monkeypatch.setattr(T, "_stream", lambda t: made.current)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: made.current)
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, stream: made.append(("record_stream", (t.data_ptr(), stream))),
+                        raising=False)
+    return made
+
+
+def test_an_optimiser_launches_on_the_stream_that_is_current(calls):
+    X = on_device(torch.zeros((2, 64)))
+    opt = T.AdamW(X, 60, state_bits=8)
+    for current in (0, 7, 7, 9):
+        calls.current = current
+        for use in (lambda: opt.step(X, 0.1), opt.moments):
+            before = len(calls)
+            use()
+            launch = [i for i, c in enumerate(calls) if c[0] in ("choco_adamw_step", "choco_adamw_moments")][-1]
+            assert launch >= before
+            streams = [c[1][1] for c in calls[:launch] if c[0] == "choco_adamw_set_stream"]
+            assert (streams[-1] if streams else opt.cfg.stream or 0) == current
+            if current != 0:        # the workspace's memory is not handed out again before that stream is done
+                assert ("record_stream", (opt.workspace.data_ptr(), current)) in calls
