@@ -304,19 +304,15 @@ class AdamW:
         _check(lib().choco_adamw_step(self.handle, _ptr(G), TYPES[G.dtype], float(lr), _ptr(grad_scale)), "choco_adamw_step")
 
     def moments(self):
-        """(m, v), float32 of (n, d): in 32 bits the state itself (it moves with the next step), in 8 bits what it stands for now."""
-        n, ld = self.X.shape
-        if self.cfg.state_bits == 32:
-            state, size = self.state(), n * ld * 4
-            m, v = (state[at:at + size].view(torch.float32).view(n, ld) for at in (0, (size + 255) // 256 * 256))
-        else:
-            m, v = torch.empty_like(self.X), torch.empty_like(self.X)
-            self._follow()
-            _check(lib().choco_adamw_moments(self.handle, m.data_ptr(), v.data_ptr()), "choco_adamw_moments")
+        """(m, v) as they are now, float32 of (n, d), in 8 bits what the codes stand for."""
+        m, v = torch.empty_like(self.X), torch.empty_like(self.X)
+        self._follow()
+        _check(lib().choco_adamw_moments(self.handle, m.data_ptr(), v.data_ptr()), "choco_adamw_moments")
         return m[:, :self.d], v[:, :self.d]
 
     def state(self):
-        """The moments as they are held, a view of bytes: copy it (and `get_step`) to save a run, copy back to resume it."""
+        """The moments as they are held, a view of bytes that moves with the next step: copy it (and `get_step`) to save a run,
+        copy back to resume it.  In 32 bits it is m and then v, as choco_train.h says: to look at them without a copy."""
         p, count = _vp(), _size()
         _check(lib().choco_adamw_state(self.handle, ctypes.byref(p), ctypes.byref(count)), "choco_adamw_state")
         at = p.value - self.workspace.data_ptr()

@@ -355,6 +355,28 @@ def test_other_streams_and_graphs(bits):
 
 
 @pytest.mark.parametrize("bits", [32, 8])
+def test_moments_keep_what_they_were(bits):
+    # neither a later step changes them nor does writing to them change the optimiser
+    n, d = 2, 1300
+    X = torch.from_numpy(rows(n, d, d, 1, 0.1)).cuda()
+    G = torch.from_numpy(rows(n, d, d, 2, 0.1)).cuda()
+    opt = T.AdamW(X, d, state_bits=bits)
+    opt.step(G, 0.01)
+    before = opt.moments()
+    kept = [t.clone() for t in before]
+    opt.step(2 * G, 0.01)
+    for a, b in zip(before, kept):
+        assert torch.equal(a, b)
+    now = opt.moments()
+    kept = [t.clone() for t in now]
+    for t in now:
+        t.fill_(7.0)
+    for a, b in zip(opt.moments(), kept):
+        assert torch.equal(a, b)
+    opt.close()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
 def test_the_current_stream_is_followed(bits):
     # made on one stream, used on another one whose earlier work is still under way, then captured on a third
     n, d = 3, 5000

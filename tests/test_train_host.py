@@ -312,3 +312,15 @@ def test_an_optimiser_launches_on_the_stream_that_is_current(calls):
             assert (streams[-1] if streams else opt.cfg.stream or 0) == current
             if current != 0:        # the workspace's memory is not handed out again before that stream is done
                 assert ("record_stream", (opt.workspace.data_ptr(), current)) in calls
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_moments_are_not_the_state_itself(calls, bits):
+    X = on_device(torch.zeros((2, 64)))
+    opt = T.AdamW(X, 60, state_bits=bits)
+    opt.moments()
+    m, v = opt.moments()
+    name, (handle, m_at, v_at) = calls[-1]
+    assert name == "choco_adamw_moments" and (m_at, v_at) == (m.data_ptr(), v.data_ptr())
+    own = opt.workspace.untyped_storage().data_ptr()
+    assert own not in (m.untyped_storage().data_ptr(), v.untyped_storage().data_ptr())
