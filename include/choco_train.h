@@ -6,8 +6,8 @@
  *
  * The conventions of choco.h hold: CHOCO_OK or a negative code, nothing printed, nothing aborts; *_dev are
  * device pointers, *_host host pointers; buffers belong to the caller, the library allocates no device memory;
- * work is enqueued on the caller's stream and no call waits for it, except choco_adamw_init (it copies a table
- * of the tensors to the device).  Calls with nothing to do (no tokens, no sequences, no channels) return CHOCO_OK
+ * work is enqueued on the caller's stream, with the device current that the stream and the pointers are of, and no call
+ * waits for it, except choco_adamw_init (it copies a table of the tensors to the device).  Calls with nothing to do (no tokens, no sequences, no channels) return CHOCO_OK
  * and enqueue nothing.
  */
 #ifndef CHOCO_TRAIN_H

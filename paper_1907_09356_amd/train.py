@@ -89,6 +89,21 @@ def _stream(t):
     return torch._C._cuda_getCurrentRawStream(t.get_device())
 
 
+_current_device = torch._C._cuda_getDevice
+
+
+def _enqueue(t, name, *args):
+    """A call of the library that works on t's device: made with that device current, as kernels go to the current one."""
+    call, device = getattr(lib(), name), t.get_device()
+    if device == _current_device():
+        code = call(*args)
+    else:
+        with torch.cuda.device(device):
+            code = call(*args)
+    if code:
+        _check(code, name)
+
+
 def _scratch(nbytes, like):
     return torch.empty(nbytes, dtype=torch.uint8, device=like.device) if nbytes else None
 
@@ -135,7 +150,7 @@ def embed(tokens, table, scale=1.0, out_dtype=None, out=None):
     if out is None:
         out = torch.empty(tokens.shape + table.shape[2:], dtype=out_dtype or table.dtype, device=table.device)
     cfg, _ = _embed_config(tokens, table, out, float(scale))
-    _check(lib().choco_embed_forward(cfg, tokens.data_ptr(), table.data_ptr(), out.data_ptr()), "choco_embed_forward")
+    _enqueue(out, "choco_embed_forward", cfg, tokens.data_ptr(), table.data_ptr(), out.data_ptr())
     return out
 
 
@@ -145,8 +160,8 @@ def embed_grad(tokens, dout, dtable, scale=1.0, accumulate=False):
     assert dtable.dtype == torch.float32
     cfg, nbytes = _embed_config(tokens, dtable, dout, float(scale))
     ws = _scratch(nbytes, dtable)
-    _check(lib().choco_embed_backward(cfg, tokens.data_ptr(), dout.data_ptr(), dtable.data_ptr(), 1 if accumulate else 0,
-                                      _ptr(ws), nbytes), "choco_embed_backward")
+    _enqueue(dtable, "choco_embed_backward", cfg, tokens.data_ptr(), dout.data_ptr(), dtable.data_ptr(), 1 if accumulate else 0,
+             _ptr(ws), nbytes)
     return dtable
 
 
@@ -205,8 +220,8 @@ def recurrence(f, u, o=None, h0=None, lengths=None, save=False, out=None, h_last
         saved = torch.empty(((T + SAVE_STEPS - 1) // SAVE_STEPS, B, C), dtype=torch.float32, device=f.device)
     cfg, nbytes = _recur_config(f, u, o, y)
     ws = _scratch(nbytes, f)
-    _check(lib().choco_recur_forward(cfg, f.data_ptr(), u.data_ptr(), _ptr(o), _state(h0, f), _lengths(lengths, f), y.data_ptr(),
-                                     _state(h_last, f), _ptr(saved), _ptr(ws), nbytes), "choco_recur_forward")
+    _enqueue(f, "choco_recur_forward", cfg, f.data_ptr(), u.data_ptr(), _ptr(o), _state(h0, f), _lengths(lengths, f), y.data_ptr(),
+             _state(h_last, f), _ptr(saved), _ptr(ws), nbytes)
     return y, h_last, saved
 
 
@@ -224,9 +239,8 @@ def recurrence_grad(f, u, saved, dy, o=None, lengths=None, dlast=None):
     dh0 = torch.empty((B, C), dtype=torch.float32, device=f.device)
     cfg, nbytes = _recur_config(f, u, o, dy, df, du, do)
     ws = _scratch(nbytes, f)
-    _check(lib().choco_recur_backward(cfg, f.data_ptr(), u.data_ptr(), _ptr(o), _lengths(lengths, f), saved.data_ptr(),
-                                      dy.data_ptr(), _state(dlast, f), df.data_ptr(), du.data_ptr(), _ptr(do), dh0.data_ptr(),
-                                      _ptr(ws), nbytes), "choco_recur_backward")
+    _enqueue(f, "choco_recur_backward", cfg, f.data_ptr(), u.data_ptr(), _ptr(o), _lengths(lengths, f), saved.data_ptr(),
+             dy.data_ptr(), _state(dlast, f), df.data_ptr(), du.data_ptr(), _ptr(do), dh0.data_ptr(), _ptr(ws), nbytes)
     return df, du, do, dh0
 
 
@@ -270,7 +284,7 @@ class AdamW:
         _check(lib().choco_adamw_workspace_bytes(ctypes.byref(self.cfg), ctypes.byref(need)), "choco_adamw_workspace_bytes")
         self.workspace = torch.empty(need.value + 256, dtype=torch.uint8, device=X.device)
         base = (self.workspace.data_ptr() + 255) // 256 * 256
-        _check(lib().choco_adamw_init(ctypes.byref(self.cfg), _ptr(X), base, need.value, ctypes.byref(a)), "choco_adamw_init")
+        _enqueue(X, "choco_adamw_init", ctypes.byref(self.cfg), _ptr(X), base, need.value, ctypes.byref(a))
         del keep
         self.handle = a
 
@@ -301,13 +315,13 @@ class AdamW:
             assert grad_scale.device == G.device and grad_scale.dtype == torch.float32
             assert grad_scale.is_contiguous() and grad_scale.shape == G.shape[:1]
         self._follow()
-        _check(lib().choco_adamw_step(self.handle, _ptr(G), TYPES[G.dtype], float(lr), _ptr(grad_scale)), "choco_adamw_step")
+        _enqueue(self.X, "choco_adamw_step", self.handle, _ptr(G), TYPES[G.dtype], float(lr), _ptr(grad_scale))
 
     def moments(self):
         """(m, v) as they are now, float32 of (n, d), in 8 bits what the codes stand for."""
         m, v = torch.empty_like(self.X), torch.empty_like(self.X)
         self._follow()
-        _check(lib().choco_adamw_moments(self.handle, m.data_ptr(), v.data_ptr()), "choco_adamw_moments")
+        _enqueue(self.X, "choco_adamw_moments", self.handle, m.data_ptr(), v.data_ptr())
         return m[:, :self.d], v[:, :self.d]
 
     def state(self):

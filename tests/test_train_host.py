@@ -276,26 +276,47 @@ def on_device(t):
 
 @pytest.fixture
 def calls(monkeypatch):
-    """[(name, arguments)] of the library's calls; calls.current: the current stream."""
+    """[(name, arguments)] of the library's calls; calls.current: the current stream; calls.devices: the device that was
+    current at each."""
     class Calls(list):
-        current = 0
+        current, device = 0, 0
 
     made = Calls()
+    made.devices = []
+
+    class Device:
+        def __init__(self, number):
+            self.number = number
+
+        def __enter__(self):
+            self.before, made.device = made.device, self.number
+
+        def __exit__(self, *error):
+            made.device = self.before
 
     class Library:
         def __getattr__(self, name):
             def call(*args):
                 made.append((name, args))
+                made.devices.append((name, made.device))
                 return B.OK
             call.__name__ = name
             return call
 
     monkeypatch.setattr(T, "lib", Library)
     monkeypatch.setattr(T, "_stream", lambda t: made.current)
+    monkeypatch.setattr(T, "_current_device", lambda: made.device, raising=False)
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    empty = torch.empty
+    monkeypatch.setattr(torch, "empty", lambda *a, **kw: on_device(empty(*a, **kw)))
     monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: made.current)
     monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, stream: made.append(("record_stream", (t.data_ptr(), stream))),
                         raising=False)
-    return made
+    for plan in (T._embed_plan, T._recur_plan):
+        plan.cache_clear()
+    yield made
+    for plan in (T._embed_plan, T._recur_plan):      # (made with a library that asks for no workspace)
+        plan.cache_clear()
 
 
 def test_an_optimiser_launches_on_the_stream_that_is_current(calls):
@@ -324,3 +345,25 @@ def test_moments_are_not_the_state_itself(calls, bits):
     assert name == "choco_adamw_moments" and (m_at, v_at) == (m.data_ptr(), v.data_ptr())
     own = opt.workspace.untyped_storage().data_ptr()
     assert own not in (m.untyped_storage().data_ptr(), v.untyped_storage().data_ptr())
+
+
+@pytest.mark.parametrize("number,current", [(0, 0), (1, 0), (0, 1), (2, 2)])
+def test_calls_are_made_with_the_tensors_device_current(calls, monkeypatch, number, current):
+    monkeypatch.setattr(OnDevice, "number", number)
+    calls.device = current
+    tokens = on_device(torch.zeros((2, 3), dtype=torch.int64))
+    table, rows = on_device(torch.zeros((2, 5, 4))), on_device(torch.zeros((2, 3, 4)))
+    T.embed(tokens, table, out=rows)
+    T.embed_grad(tokens, rows, table)
+    state = on_device(torch.zeros((2, 4)))
+    T.recurrence(rows, rows, h_last=state, out=rows)
+    T.recurrence_grad(rows, rows, on_device(torch.zeros((1, 2, 4))), rows)
+    X = on_device(torch.zeros((2, 64)))
+    opt = T.AdamW(X, 60, state_bits=8)
+    opt.step(X, 0.1)
+    opt.moments()
+    names = ["choco_embed_forward", "choco_embed_backward", "choco_recur_forward", "choco_recur_backward", "choco_adamw_init",
+             "choco_adamw_step", "choco_adamw_moments"]
+    at = [(name, device) for name, device in calls.devices if name in names]
+    assert at == [(name, number) for name in names]
+    assert calls.device == current
