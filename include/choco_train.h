@@ -72,7 +72,7 @@ typedef struct {
 } choco_recur_config;
 
 /* Bytes of what the forward pass keeps for the backward one: the fp32 state before every
-   CHOCO_RECUR_SAVE_STEPS-th step, ceil(steps / CHOCO_RECUR_SAVE_STEPS) x batch x dim. */
+   CHOCO_RECUR_SAVE_STEPS-th step, ceil(steps / CHOCO_RECUR_SAVE_STEPS) x batch x dim.  Errors as of the passes. */
 int choco_recur_saved_bytes(const choco_recur_config* cfg, size_t* bytes_host);
 /* Bytes of device workspace that either pass needs (16-byte aligned); may be 0. */
 int choco_recur_workspace_bytes(const choco_recur_config* cfg, size_t* bytes_host);

@@ -291,6 +291,7 @@ void with_width(bool pairs, Fn&& fn) {
 
 static_assert(kSaveSteps == CHOCO_RECUR_SAVE_STEPS, "the header says what is kept");
 
+// (of a call that its launches hold: far from 64 bits)
 int64_t saved_floats(const choco_recur_config& c) {
   return (c.steps + CHOCO_RECUR_SAVE_STEPS - 1) / CHOCO_RECUR_SAVE_STEPS * c.batch * c.dim;
 }
@@ -563,6 +564,7 @@ int choco_embed_backward(const choco_embed_config* cfg, const void* tokens_dev, 
 int choco_recur_saved_bytes(const choco_recur_config* cfg, size_t* bytes_host) {
   if (!bytes_host) return CHOCO_E_INVAL;
   if (const int rc = check_recur(cfg)) return rc;
+  if (!recur_fits(*cfg)) return CHOCO_E_UNSUPPORTED;
   *bytes_host = (size_t)saved_floats(*cfg) * sizeof(float);
   return CHOCO_OK;
 }

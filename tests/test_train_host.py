@@ -176,6 +176,16 @@ def test_more_than_a_launch_holds_is_unsupported():
     assert embed_codes(c)[0] == B.E_UNSUPPORTED
 
 
+def test_kept_states_are_only_counted_for_what_a_launch_holds():
+    big = 2 ** 31 - 1
+    out = ctypes.c_size_t(7)
+    for batch, steps, dim in ((511, big, big), (500, big, 4096), (1, big, 2 ** 20)):
+        c = recur_cfg(batch=batch, steps=steps, dim=dim)
+        assert T.lib().choco_recur_workspace_bytes(ctypes.byref(c), ctypes.byref(out)) == B.E_UNSUPPORTED
+        assert T.lib().choco_recur_saved_bytes(ctypes.byref(c), ctypes.byref(out)) == B.E_UNSUPPORTED
+    assert out.value == 7
+
+
 def test_recurrence_with_nothing_to_do():
     assert recur_codes(recur_cfg(batch=0)) == (B.OK, B.OK)
     assert recur_codes(recur_cfg(dim=0)) == (B.OK, B.OK)
