@@ -124,6 +124,7 @@ typedef struct {
   void* stream;          /* of choco_adamw_init and, until choco_adamw_set_stream, of the calls after it */
 } choco_adamw_config;
 
+/* CHOCO_E_UNSUPPORTED: more tensors, and gaps between them, than one launch holds (some 2^26 pieces of up to 1024 entries). */
 int choco_adamw_workspace_bytes(const choco_adamw_config* cfg, size_t* bytes_host);
 /* x_dev 16-byte, workspace_dev 256-byte aligned; moments start at zero, t at 0.  On error *out is NULL. */
 int choco_adamw_init(const choco_adamw_config* cfg, float* x_dev, void* workspace_dev, size_t workspace_bytes,

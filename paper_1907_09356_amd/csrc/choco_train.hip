@@ -300,7 +300,7 @@ int64_t saved_floats(const choco_recur_config& c) {
 
 struct AdamwLayout {
   size_t state, m, v, m_scale, v_scale, state_end, tiles, total;
-  int32_t ntiles, nblocks, ngaps;
+  int64_t ntiles, nblocks, ngaps;
 };
 
 int64_t resolve_adamw_ld(const choco_adamw_config& c) { return c.ld == 0 ? (c.d + 3) / 4 * 4 : c.ld; }
@@ -345,16 +345,14 @@ void for_tensors(const choco_adamw_config& c, Fn&& fn) {
 
 AdamwLayout adamw_layout(const choco_adamw_config& c) {
   AdamwLayout L{};
-  int64_t tiles = 0, blocks = 0, gaps = 0, end = 0;   // (at most ld of each: 32 bits hold them)
+  int64_t end = 0;
   for_tensors(c, [&](int32_t, int64_t start, int64_t len) {
-    tiles += (len + kTile - 1) / kTile;
-    blocks += (len + kMomentBlock - 1) / kMomentBlock;
-    gaps += (start - end + kTile - 1) / kTile;
+    L.ntiles += (len + kTile - 1) / kTile;
+    L.nblocks += (len + kMomentBlock - 1) / kMomentBlock;
+    L.ngaps += (start - end + kTile - 1) / kTile;
     end = start + len;
   });
-  L.ngaps = (int32_t)(gaps + (resolve_adamw_ld(c) - end + kTile - 1) / kTile);
-  L.ntiles = (int32_t)tiles;
-  L.nblocks = (int32_t)blocks;
+  L.ngaps += (resolve_adamw_ld(c) - end + kTile - 1) / kTile;
   const size_t entries = (size_t)c.n * (size_t)resolve_adamw_ld(c);
   size_t at = 0;
   const auto take = [&](size_t bytes) {
@@ -369,10 +367,13 @@ AdamwLayout adamw_layout(const choco_adamw_config& c) {
     L.v_scale = take((size_t)c.n * L.nblocks * sizeof(float));
   }
   L.state_end = at;
-  L.tiles = take(((size_t)L.ntiles + L.ngaps) * sizeof(AdamwTile));
+  L.tiles = take((size_t)(L.ntiles + L.ngaps) * sizeof(AdamwTile));
   L.total = at;
   return L;
 }
+
+// A launch holds a step, and a read-back with its tiles of no tensor.
+bool adamw_fits(const AdamwLayout& L) { return launch_fits((double)((L.ntiles + L.ngaps + 3) / 4), 256); }
 
 }  // namespace
 
@@ -683,7 +684,9 @@ int choco_recur_backward(const choco_recur_config* cfg, const void* f_dev, const
 int choco_adamw_workspace_bytes(const choco_adamw_config* cfg, size_t* bytes_host) {
   if (!bytes_host) return CHOCO_E_INVAL;
   if (const int rc = check_adamw(cfg)) return rc;
-  *bytes_host = adamw_layout(*cfg).total;
+  const AdamwLayout L = adamw_layout(*cfg);
+  if (!adamw_fits(L)) return CHOCO_E_UNSUPPORTED;
+  *bytes_host = L.total;
   return CHOCO_OK;
 }
 
@@ -695,10 +698,11 @@ int choco_adamw_init(const choco_adamw_config* cfg, float* x_dev, void* workspac
   if (!x_dev || !workspace_dev || !aligned_to(x_dev, 16) || !aligned_to(workspace_dev, 256)) return CHOCO_E_INVAL;
   const choco_adamw_config& c = *cfg;
   const AdamwLayout L = adamw_layout(c);
+  if (!adamw_fits(L)) return CHOCO_E_UNSUPPORTED;
   if (workspace_bytes < L.total) return CHOCO_E_NOMEM;
   try {
     std::vector<AdamwTile> tiles;
-    tiles.reserve((size_t)L.ntiles + L.ngaps);
+    tiles.reserve((size_t)(L.ntiles + L.ngaps));
     const auto gap = [&](int64_t at, int64_t end) {   // entries of no tensor, behind the tensors' tiles
       for (; at < end; at += kTile) {
         AdamwTile tile{};
@@ -749,8 +753,8 @@ int choco_adamw_init(const choco_adamw_config* cfg, float* x_dev, void* workspac
     A.m_scale = (float*)(ws + L.m_scale);
     A.v_scale = (float*)(ws + L.v_scale);
     A.tiles = (const AdamwTile*)(ws + L.tiles);
-    A.ntiles = L.ntiles;
-    A.nblocks = L.nblocks;
+    A.ntiles = (int32_t)L.ntiles;      // (a launch holds them)
+    A.nblocks = (int32_t)L.nblocks;
     A.ld = resolve_adamw_ld(c);
     A.beta1 = (float)c.beta1;
     A.one_minus_beta1 = (float)(1.0 - c.beta1);
@@ -805,7 +809,7 @@ int choco_adamw_moments(choco_adamw* a, float* m_dev, float* v_dev) {
   AdamwArgs A = a->args;
   A.m_out = m_dev;
   A.v_out = v_dev;
-  A.ntiles += a->layout.ngaps;
+  A.ntiles += (int32_t)a->layout.ngaps;
   const dim3 grid(blocks_of(A.ntiles, 4), (uint32_t)a->n);
   if (a->state_bits == 32) k_adamw_moments<32><<<grid, 256, 0, a->stream>>>(A);
   else k_adamw_moments<8><<<grid, 256, 0, a->stream>>>(A);

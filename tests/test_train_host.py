@@ -235,6 +235,12 @@ def test_adamw_accepts_any_disjoint_tensors():
         assert adamw_code(state_bits=bits, tensors=([1000], [0])) == B.OK
 
 
+def test_adamw_with_more_tensors_than_a_launch_holds_is_unsupported():
+    # a tensor of one entry, a gap of one, ...: a tile each, of which a workgroup takes four
+    for count, code in ((2 ** 25 + 1, B.E_UNSUPPORTED), (2 ** 25 - 8, B.OK)):
+        assert adamw_code(d=2 * count, tensors=(np.arange(0, 2 * count, 2), np.ones(count, dtype=np.int64))) == code
+
+
 def test_adamw_workspace_in_bytes_per_entry():
     def need(bits):
         c, keep = T.make_adamw_config(4, 1 << 20, state_bits=bits)
