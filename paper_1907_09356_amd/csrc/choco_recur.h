@@ -69,16 +69,28 @@ struct RecurArgs {
   uint32_t strips, chains, tiles, links;
 };
 
-// sigmoid(x) and 1 - sigmoid(x), the smaller of the two not by a difference: the exponential's argument is rounded to
-// |x| 2^-24, the rest is good to a few 2^-24.  exp(-x) may overflow: up is then 0 and down 1.
+// exp(-x) for an x of type T.  The instruction takes a power of two: its argument is a product rounded to |x| 2^-24, and what that
+// leaves is put back as a factor (without it 1 - sigmoid(60) is off by 29 2^-24 on average, with it by less than one).  Infinite
+// arguments leave nothing.  An x of 16 bits is itself rounded to |x| 2^-9 or 2^-12, against which the product's rounding is
+// nothing, and goes without: 2 of 32,768 x 2048 in bf16 208 us, with it 220.
+template <class T>
+__device__ __forceinline__ float exp_minus(float x) {
+  constexpr float kHigh = -1.44269502f, kLow = -1.92596299e-8f;     // together -log2(e)
+  const float p = x * kHigh;
+  if constexpr (sizeof(T) == 2) return __builtin_amdgcn_exp2f(p);
+  const float left = fmaf(x, kLow, fmaf(x, kHigh, -p));
+  return __builtin_amdgcn_exp2f(p) * (fabsf(p) < 256.0f ? fmaf(left, 0.693147182f, 1.0f) : 1.0f);
+}
+// sigmoid(x) and 1 - sigmoid(x), the smaller of the two not by a difference: in fp32 good to 10 2^-24 each.  exp(-x) may overflow: up
+// is then 0 and down 1.
+template <class T>
 __device__ __forceinline__ void gate(float x, float& up, float& down) {
-  const float e = __builtin_amdgcn_exp2f(x * -1.44269504f);
+  const float e = exp_minus<T>(x);
   up = __builtin_amdgcn_rcpf(1.0f + e);
   down = x >= 0.0f ? e * up : 1.0f - up;
 }
-__device__ __forceinline__ float gate(float x) {
-  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * -1.44269504f));
-}
+template <class T>
+__device__ __forceinline__ float gate(float x) { return __builtin_amdgcn_rcpf(1.0f + exp_minus<T>(x)); }
 
 __device__ __forceinline__ int64_t steps_of(const RecurArgs& A, int64_t b) {
   if (!A.lengths) return A.steps;
@@ -294,7 +306,7 @@ __global__ __launch_bounds__(64 * (MODE != kAlone ? kChainWaves : kRecurWaves)) 
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         float down;
-        gate(entry<T>(f[j], i), a[j][i], down);
+        gate<T>(entry<T>(f[j], i), a[j][i], down);
         b[j][i] = down * entry<T>(u[j], i);
         if (j >= n) {     // not in the sequence: the state is passed on
           a[j][i] = 1.0f;
@@ -322,7 +334,7 @@ __global__ __launch_bounds__(64 * (MODE != kAlone ? kChainWaves : kRecurWaves)) 
         out[i] = 0.0f;
         if (j < n) {
           h[i] = fmaf(a[j][i], h[i], b[j][i]);
-          out[i] = GATED ? gate(entry<T>(o[j], i)) * h[i] : h[i];
+          out[i] = GATED ? gate<T>(entry<T>(o[j], i)) * h[i] : h[i];
         }
       }
       store_step<T, V, MODE != kAlone && MODE != kThrough>(A.y, A.y_seq, A.y_step, P, t0 + j, out);
@@ -364,13 +376,13 @@ __global__ __launch_bounds__(64 * (MODE != kAlone ? kChainWaves : kRecurWaves)) 
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         const float x = entry<T>(u[j], i), dy = entry<T>(d[j], i);
-        gate(entry<T>(f[j], i), a[j][i], down[j][i]);
+        gate<T>(entry<T>(f[j], i), a[j][i], down[j][i]);
         off[j][i] = (h[i] - x) * a[j][i];
         h[i] = fmaf(a[j][i], h[i], down[j][i] * x);
         into[j][i] = dy;
         if (GATED) {
           float s, r;
-          gate(entry<T>(o[j], i), s, r);
+          gate<T>(entry<T>(o[j], i), s, r);
           into[j][i] = dy * s;
           go[i] = dy * h[i] * s * r;
         }

@@ -155,6 +155,21 @@ def test_gates_at_their_ends(shift):
     both(2, 200, 72, torch.float16, False, [200, 77], seed=26, shift=shift, spread=1.0)
 
 
+def test_gates_to_the_last_places():
+    # one step with dy = 1: du is 1 - sigmoid(f), dh0 sigmoid(f), and y = sigmoid(o) h0 where the state is kept.  An exponential good
+    # to 4 2^-24 (its instruction 2, two roundings), a sum, a reciprocal (2), a product or difference: 10, one more for the second order
+    size = np.concatenate((np.linspace(-86, 86, 20_000), np.random.default_rng(1).standard_normal(20_000) * 4)).astype(np.float32)
+    x = torch.from_numpy(size).cuda().view(4, 1, -1)
+    zero, one = torch.zeros_like(x), torch.ones_like(x)
+    h0 = one[:, 0].contiguous()
+    y = T.recurrence(torch.full_like(x, 120.0), zero, x, h0=h0)[0]
+    saved = T.recurrence(x, zero, h0=h0, save=True)[2]
+    _, du, _, dh0 = T.recurrence_grad(x, zero, saved, one)
+    at = size.astype(np.float64)
+    for got, want in ((y, sigmoid(at)), (dh0, sigmoid(at)), (du, sigmoid(-at))):
+        assert np.max(np.abs(got.double().cpu().numpy().ravel() / want - 1)) <= 11 * 2.0 ** -24
+
+
 @pytest.mark.parametrize("steps", [37, 700])
 def test_infinite_gates_and_masked_steps(steps):
     # f = +-inf: keep, or take the input; NaN and infinities beyond a sequence's end are not looked at
