@@ -59,6 +59,9 @@ int choco_embed_backward(const choco_embed_config* cfg, const void* tokens_dev, 
  *   h_t = a h_{t-1} + (1 - a) u_t,   y_t = sigmoid(o_t) h_t  (y_t = h_t without o)
  * States are fp32; y is rounded once.  A sequence of lengths[b] < steps steps keeps its state from there on
  * and its further y (and gradients) are zero, whatever its further inputs hold; lengths are clamped to [0, steps].
+ * A state that is infinite stays so or becomes NaN (where the product of the gates since is below fp32's range), in its channel of
+ * its sequence only.  In long sequences workgroups wait for the states of earlier ones; a wait that does not end within some
+ * seconds is given up and the states after it are NaN, without an error code.
  * Generation is steps = 1 with h0 = the last state; h_last may be h0's own buffer. */
 #define CHOCO_RECUR_SAVE_STEPS 8
 typedef struct {

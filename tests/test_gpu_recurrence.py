@@ -275,6 +275,62 @@ def test_layouts(dtype, offset):
         assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("offset", [0, 1, 2])
+def test_layouts_of_long_sequences(dtype, offset):
+    # the same for sequences of several tiles: steps before sequences, columns that start anywhere, ragged
+    batch, steps, dim = 3, 2100, 66
+    gen = torch.Generator(device="cuda").manual_seed(54)
+    base = torch.empty((steps, batch, 3 * dim + 5), device="cuda", dtype=dtype).normal_(generator=gen)
+    f, u, o = (base[..., offset + k * dim:offset + (k + 1) * dim].transpose(0, 1) for k in range(3))
+    lengths = torch.tensor([2100, 129, 1937], dtype=torch.int32).cuda()
+    h0 = torch.empty((batch, dim), device="cuda").normal_(generator=gen)
+    out = torch.full((steps, batch, dim + 3), 9.0, dtype=dtype, device="cuda")
+    y, last, saved = T.recurrence(f, u, o, h0=h0, lengths=lengths, save=True, out=out[..., offset:offset + dim].transpose(0, 1))
+    plain = [t.float().contiguous().double().cpu().numpy() for t in (f, u, o, h0)]
+    wy, by, wl, bl, H, BH = forward(*plain, lengths.cpu().numpy())
+    check("y", y, wy, by, dtype)
+    check("h", last, wl, bl, torch.float32)
+    assert bool((out[..., :offset] == 9).all()) and bool((out[..., offset + dim:] == 9).all())
+    dy = torch.empty((steps, batch, dim + 3), device="cuda", dtype=dtype).normal_(generator=gen)
+    view = dy[..., offset:offset + dim].transpose(0, 1)
+    df, du, do, dh0 = T.recurrence_grad(f, u, saved, view, o, lengths=lengths)
+    want = backward(plain[0], plain[1], plain[2], lengths.cpu().numpy(), H, BH, view.double().cpu().numpy(), np.zeros((batch, dim)))
+    for name, got in (("df", df), ("du", du), ("do", do)):
+        check(name, got, want[name], want["b" + name], dtype)
+    check("dh0", dh0, want["dh0"], want["bdh0"], torch.float32)
+
+
+@pytest.mark.parametrize("steps,dim", [(100, 130), (129, 130), (2500, 66)])
+def test_the_last_state_in_place_of_the_first(steps, dim):
+    proj, f, u, o, h0, _, _ = inputs(3, steps, dim, torch.float32, True, 42)
+    f, u, o, state = f.cuda(), u.cuda(), o.cuda(), h0.cuda()
+    y, last, _ = T.recurrence(f, u, o, h0=state)
+    y2, last2, _ = T.recurrence(f, u, o, h0=state, h_last=state)
+    assert last2 is state and torch.equal(y, y2) and torch.equal(last, state)
+
+
+@pytest.mark.parametrize("steps", [90, 1500])
+def test_infinite_states_stay_in_their_channel_from_their_step_on(steps):
+    # from h0, or from an input on: not finite to the end (infinite, or NaN where what is left of the state is below fp32's range)
+    for start in (0, 3, steps // 2):
+        f = torch.randn((2, steps, 70), device="cuda")
+        u = torch.randn((2, steps, 70), device="cuda")
+        h0 = torch.zeros((2, 70), device="cuda")
+        if start == 0:
+            h0[1, 4] = float("inf")
+        else:
+            u[1, start, 4] = float("-inf")
+        y, last, saved = T.recurrence(f, u, h0=h0, save=True)
+        hit = torch.zeros((2, steps, 70), dtype=torch.bool, device="cuda")
+        hit[1, start:, 4] = True
+        assert torch.equal(~torch.isfinite(y), hit)
+        assert torch.equal(~torch.isfinite(last), hit[:, -1])
+        df, du, _, dh0 = T.recurrence_grad(f, u, saved, torch.ones_like(f))
+        hit[1, :, 4] = True
+        assert bool(torch.isfinite(df[~hit]).all()) and bool(torch.isfinite(du).all()) and bool(torch.isfinite(dh0).all())
+
+
 def test_one_gate_for_all_steps():
     # inputs may repeat: a stride of zero
     batch, steps, dim = 2, 45, 96
