@@ -32,8 +32,12 @@ constexpr int kSortRounds = 8;
 constexpr int kSortOne = kSortThreads * kSortRounds;   // ... of which there are no more than this
 constexpr int kSortDigit = 9;                          // bits of the key in one pass, at most
 constexpr int kChunkThreads = 256;                     // otherwise: a workgroup for each so many tokens ...
-constexpr int kShortRounds = 4, kLongRounds = 16;      // ... times this: more workgroups, but each reads the counts of all chunks,
-constexpr int64_t kLongLists = 1 << 17;                // so kLongRounds from so many tokens on
+// ... times this: more workgroups, but each reads the counts of all chunks, so kLongRounds from kLongLists tokens on.  us, 4 | 16, rows
+// of 64 in bf16 added, vocabulary 50,257, one worker: 64 K tokens 36 | 58, 128 K 44 | 63, 256 K 59 | 74, 512 K 94 | 100, 1 M 189 | 144;
+// 4 workers: 128 K 75 | 93, 256 K 122 | 122, 512 K 238 | 192; 16: 64 K 114 | 126, 128 K 198 | 197, 256 K 375 | 333; vocabulary 1000, one
+// worker: 128 K 38 | 45, 256 K 60 | 60, 512 K 105 | 86; of 1 M words: 60 | 72, 92 | 89, 167 | 126.
+constexpr int kShortRounds = 4, kLongRounds = 16;
+constexpr int64_t kLongLists = 1 << 18;
 constexpr int kChunkDigit = 10;
 constexpr int kPiece = 32;                             // ordered tokens that a wave adds up ... (16, 48: within 2 %)
 constexpr int kAhead = 8;                              // ... asking for so many rows at once (16: the same)

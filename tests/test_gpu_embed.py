@@ -104,6 +104,13 @@ def test_gradient(n, count, vocab, dim, how, kind, accumulate):
     assert torch.equal(again, dtable)
 
 
+@pytest.mark.parametrize("n,count,vocab,dim,how", [(1, 262_143, 9000, 2, "frequent"), (1, 262_144, 9000, 2, "frequent"),
+                                                   (2, 300_001, 70_000, 3, "frequent"), (1, 270_000, 900, 4, "one")])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_gradient_of_long_lists(n, count, vocab, dim, how, accumulate):
+    test_gradient(n, count, vocab, dim, how, torch.bfloat16, accumulate)
+
+
 def test_gradient_by_differences():
     # the loss sum(w * y) is linear in the table: a difference quotient is exact but for its own roundings
     n, count, vocab, dim = 1, 9, 6, 5
