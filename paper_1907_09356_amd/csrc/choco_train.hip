@@ -468,9 +468,10 @@ int choco_embed_backward(const choco_embed_config* cfg, const void* tokens_dev, 
   // memory busy (65,536 rows of 1024 in bf16: eight 111 us, four 101, two 99).
   int v = embed_width(2, c.dim, {{dy_dev, size}, {dtable_dev, 4}}, {{c.row_ld, size}, {c.row_stride, size}, {c.table_stride, 4}});
   if (c.dim <= 64) v = 1;     // (no lane without columns)
-  // Rows and sums past the caches where the rows do not fit there (65,536 of 1024 in bf16, 134 MB: 99 us through, 88 with the rows
-  // past them, 83 with the sums as well; 23 MB, just written: 26 and 30).
-  const bool past = (double)c.n * (double)c.tokens * (double)c.dim * size > 96.0 * 1048576.0;
+  // Rows and sums past the caches where the rows, other ones with every step, would push too much else out of them.  us, through | past,
+  // rows of 1024 added: fp32 16 MB 28 | 28, 32 MB 40 | 42, 64 MB 51 | 50, 96 MB 69 | 60, 256 MB 125 | 106, 512 MB 228 | 209; bf16
+  // 16 MB 39 | 40, 32 MB 42 | 44, 64 MB 65 | 58, 96 MB 83 | 71, 256 MB 170 | 156, 512 MB 261 | 235.
+  const bool past = (double)c.n * (double)c.tokens * (double)c.dim * size > 48.0 * 1048576.0;
   A.column_chunks = (c.dim + 64 * v - 1) / (64 * v);
   if (c.tokens <= kFew) {
     if (!launch_fits((double)c.tokens * (double)A.column_chunks, 64)) return CHOCO_E_UNSUPPORTED;

@@ -221,6 +221,26 @@ def test_results_that_do_not_fit_the_caches(kind):
         assert bool(((got[0].double() - want).abs() <= bound).all())
 
 
+@pytest.mark.parametrize("count", [100, 500, 9000, 40_000])
+def test_gradients_that_do_not_fit_the_caches(count):
+    # more than 64 MB to be cleared, by either way of putting tokens in order and without; rows of 0.3 to 104 MB to add up
+    n, vocab, dim = 2, 20_001, 650
+    gen = torch.Generator(device="cuda").manual_seed(count)
+    tokens = torch.from_numpy(draw_tokens(n, count, vocab, 14, "frequent")).cuda()
+    dy = torch.empty((n, count, dim), device="cuda").normal_(generator=gen)
+    buffer = torch.full((n, vocab * dim + 6), 5.0, device="cuda")
+    got = buffer[:, 1:vocab * dim + 1].view(n, vocab, dim)
+    T.embed_grad(tokens, dy, got, scale=2.0)
+    for w in range(n):
+        there = tokens[w] >= 0
+        at, rows = tokens[w, there], 2.0 * dy[w, there].double()
+        zero = torch.zeros((vocab, dim), dtype=torch.float64, device="cuda")
+        want, size = zero.index_add(0, at, rows), zero.index_add(0, at, rows.abs())
+        number = torch.bincount(at, minlength=vocab)[:, None]
+        assert bool(((got[w].double() - want).abs() <= U * (number + 3) * size).all())
+    assert bool((buffer[:, :1] == 5).all()) and bool((buffer[:, vocab * dim + 1:] == 5).all())
+
+
 def test_other_streams_and_graphs():
     n, count, vocab, dim = 2, 1500, 5000, 50
     tokens = torch.from_numpy(draw_tokens(n, count, vocab, 11, "frequent")).cuda()
