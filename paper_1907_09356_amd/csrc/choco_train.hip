@@ -462,7 +462,11 @@ int choco_embed_backward(const choco_embed_config* cfg, const void* tokens_dev, 
   const int64_t zero_blocks = accumulate ? 0 : (c.vocab * c.dim + kZeroFloats - 1) / kZeroFloats;
   if (!launch_fits((double)zero_blocks * c.n + c.n, kSortThreads)) return CHOCO_E_UNSUPPORTED;
   A.zero_blocks = (uint32_t)zero_blocks;
-  A.zero_past = (double)c.n * (double)c.vocab * (double)c.dim * 4 > 96.0 * 1048576.0;   // (692 MB cleared and 9 K rows added: 142 | 139 us)
+  // Cleared past the caches where what is cleared would push the rows out that are added up afterwards, but up to 64 MB left there for
+  // what reads the gradient next.  us, through | past, rows of 640 in fp32, of 1120 tokens cleared 64 MB 23 | 23, 128 MB 36 | 34, 692 MB
+  // 134 | 135; 8192 tokens 64 MB 39 | 39, 86 MB 53 | 39, 128 MB 53 | 39, 256 MB 64 | 61; 32,768 tokens 16 MB 51 | 50, 64 MB 67 | 60,
+  // 96 MB 74 | 67, 256 MB 108 | 101; but 100 tokens, with a launch that only clears, 128 MB 28 | 27, 256 MB 49 | 51, 692 MB 123 | 132.
+  A.zero_past = c.tokens > kFew && (double)c.n * (double)c.vocab * (double)c.dim * 4 > 64.0 * 1048576.0;
   const size_t size = type_bytes(c.row_type);
   // Two columns a lane: with eight (or four) a wave holds so many rows of sums and old values that too few waves fit to keep the
   // memory busy (65,536 rows of 1024 in bf16: eight 111 us, four 101, two 99).
