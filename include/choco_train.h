@@ -36,7 +36,8 @@ typedef struct {
   int32_t table_type;    /* forward: CHOCO_F32 / BF16 / F16; the gradient is always CHOCO_F32        */
   int32_t row_type;      /* of y and dy: CHOCO_F32 / BF16 / F16                                      */
   int64_t token_stride;  /* entries from worker to worker, >= tokens                                 */
-  int64_t table_stride;  /* ... of the table or its gradient, >= vocab * dim; a table's rows lie dim apart */
+  int64_t table_stride;  /* ... of the table or its gradient, >= vocab * dim; a table's rows lie dim apart.  (Workers that
+                            share one table are one worker with all their tokens.)                   */
   int64_t row_stride;    /* ... of y / dy, >= tokens * row_ld                                        */
   int64_t row_ld;        /* entries from one row of y / dy to the next, >= dim                       */
   float scale;
@@ -107,7 +108,8 @@ int choco_recur_backward(const choco_recur_config* cfg, const void* f_dev, const
  * are those of the Philox word of (seed, step, worker, entry), stream 3, the lower 16 for m and the upper 16 for
  * v, so a run is reproducible.  A positive v is never held as zero (x would move by m / eps).  The update of x takes m and
  * v before they are rounded.
- * An infinite or NaN gradient makes its entry of x and its m and v NaN or infinite; in 8 bits m and v of its whole block. */
+ * An infinite or NaN gradient makes its entry of x and its m and v NaN or infinite; in 8 bits m and v of its whole block.
+ * One whose square is infinite in fp32 (above 1.8e19) does that to v. */
 #define CHOCO_ADAMW_BLOCK 256
 typedef struct choco_adamw choco_adamw; /* opaque, host memory, freed by choco_adamw_destroy */
 typedef struct {

@@ -89,11 +89,15 @@ __global__ __launch_bounds__(256) void k_embed(EmbedArgs A, int lanes_log2) {
 // 2. A wave adds up the rows of kPiece consecutive ordered tokens, for 64 * V columns: sums of tokens that lie in the piece
 //    as a whole go to the gradient, those that reach over its ends to `partial`.
 // 3. The partial sums of a token that spans pieces are added in their order.
-// So work is split evenly whatever the tokens are (one word in a sixteenth of the places is ordinary), no float is added by
+// So the rows are split evenly whatever the tokens are (one word in a sixteenth of the places is ordinary), no float is added by
 // atomics, and every row of the gradient is written by one wave.
 // Bound by memory where the gradient is cleared: 8 x 1120 tokens into 8 x 33,278 x 650 138 us, of which 117 clear 692 MB (5.9 TB/s)
 // and hide the order, 12 to 18 add up and 5 join.  Added to what is there: 65,536 tokens of 1024 in bf16 83 us, 26 for
 // the order, 49 to add up (5.6 TB/s), 9 to join; 8 x 1120 tokens 26.  A wave per token that looks for its like: 565 and 25,657.
+// What does not scale: the partial sums of one token are joined by one workgroup for 64 * V columns, so a token that fills the list
+// takes time in proportion (rows of 128 in bf16, all of one token: 64 K 63 us, 1 M 625, 4 M 2,508; 1 M of 1024 1,149 against 708 for
+// frequent words); and every chunk of a long list reads the counts of all of them (rows of 64 in bf16, vocabulary 50,257: 1 M
+// tokens 144 us, 4 M 467, 16 M 2,770, where reading the rows takes some 450).
 
 // Part `block` of the gradient's clearing, by a whole workgroup.
 __device__ __forceinline__ void zero_part(const EmbedArgs& A, int64_t worker, int64_t block) {

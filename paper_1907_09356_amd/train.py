@@ -3,7 +3,8 @@
 Argument marshalling only, like `binding`: torch provides device memory and the stream, every computation runs in the
 HIP library.  Functions and methods enqueue on torch's current stream of the tensors' device.  As with torch's own operations, work of
 one stream that needs that of another has to wait for it, and a tensor that is used on another stream than the one it was
-made on has to be kept until that stream is done with it (an `AdamW` sees to its own workspace).
+made on has to be kept until that stream is done with it (an `AdamW` sees to its own workspace).  Nothing here is recorded by
+torch's automatic differentiation: results do not require a gradient, and the gradients are calls of their own.
 """
 import ctypes
 import functools
