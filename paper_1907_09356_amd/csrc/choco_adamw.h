@@ -2,9 +2,9 @@
 //
 // Bound by memory: 28 bytes an entry in 32 bits (x, m and v in and out, g in), 16 in 8 bits (14 with g in bf16).  The tensors of a row are
 // cut into tiles of 1024 entries, a wave each, listed in a table, so one launch takes all tensors of all workers and no
-// wave looks for its tensor; a tile's loads are all asked for before the first is used.  254 M entries in 32 bits 1,305 us (5.5 TB/s),
-// 127 M in 8 bits 310 (5.7 TB/s) and their read-back 206; 2.2 M, out of the
-// caches, 10.4 (6.0 TB/s).  Entry by entry before: 2,273, and 790 with the read-back.  Tiles of 512 or 2048 entries: 0 to 4 % slower.
+// wave looks for its tensor; a tile's loads are all asked for before the first is used.  254 M entries in 32 bits 1,305 us (5.5 TB/s)
+// and their read-back 732, 127 M in 8 bits 310 to 333 (5.5 to 5.9 TB/s) and their read-back 206; 2.2 M, out of the caches, 10.4 (6.0 TB/s).
+// Entry by entry before: 2,273, and 790 with the read-back of 8 bits.  Tiles of 512 or 2048 entries: 0 to 4 % slower.
 #pragma once
 
 #include "choco_philox.h"

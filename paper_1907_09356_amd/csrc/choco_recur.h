@@ -19,9 +19,11 @@
 // earlier links only: whatever the order in which workgroups are started, every wait ends.  (A wait gives up after kMostPolls
 // all the same; what it waited for is then NaN.)
 //
-// Measured, us (GB/s of what cannot be done without): 160 sequences of 35 steps x 650 in fp32 13.7 (3,500), backward 24.3 (3,600);
-// 2 of 32,768 x 2048 in bf16 198 (4,400); backward
-// of 4 of 16,384 x 1280 without o 202 (4,200); 64 of 512 x 1280 61 to 73 and 125 (4,600 to 5,500); a large copy reaches 4,700.
+// Measured, us (GB/s of what cannot be done without): 160 sequences of 35 steps x 650 in fp32 14 (3,450), backward 22 to 23.5 (3,750 to
+// 4,000); 2 of 32,768 x 2048 in bf16 197 to 208 (4,200 to 4,400), with the states kept 213; backward of 4 of 16,384 x 1280 without o 200 to
+// 202 (4,200); 64 of 512 x 1280 73 and 125 (4,600 to 4,700); a large copy reaches 4,700.  1 of 8192 x 512 in fp32 without o 18 and 22,
+// of which 3 start the chains (50 MB and 84 MB, 8.5 and 14 us at the rate of two reads and a write): every tile is under way at once,
+// and the last of 64 waits for three links.
 // Before: two passes over segments of a sequence, the first for their maps, 324 and 280; eight steps a wave 310 and 228;
 // one lane a channel, step by step, 14,059 and 20,573.  Workgroups that stay and ask for their next tile's steps ahead hold
 // places in the chain that others wait for: 302 to 790.
@@ -35,8 +37,8 @@ namespace choco {
 
 constexpr int kSaveSteps = 8;       // the forward pass keeps the state before every so many
 constexpr int kRecurWaves = 16;     // most waves of a workgroup
-// A sequence of one tile: steps of a wave, up to kRecurWaves of them.  160 x 35 x 650 in fp32, 8 | 16 steps: 13.7 | 14.6 us, back
-// 21.8 | 24.3.
+// A sequence of one tile: steps of a wave, up to kRecurWaves of them.  160 x 35 x 650 in fp32, 8 | 16 steps: 14.0 | 14.9 us, back
+// 22.0 | 25.3.
 constexpr int kAloneSteps = 8;
 // Chains: waves of a tile, steps of a wave - as many as leave two workgroups for a compute unit (backward holds four numbers a step
 // and channel) - and tiles of a link.  2 of 32,768 x 2048, 4 of 16,384 x 1280 back, 1 of 8192 x 512: 8 waves 207 | 202 | 18 us,
