@@ -1,0 +1,319 @@
+// Newton-Schulz iterations X <- a X + (b P + c P^2) X, P = X X^T, on stacks of matrices, and an optimiser step along their
+// result (device code).
+//
+// A matrix is taken with its shorter side first: a x b entries, a <= b.  Every product is of rows with rows, D[m][n] = sum over k of
+// L[m][k] R[n][k]:  P from X and X,  Q = b P + c P^2 from P and P (symmetric),  X' = a X + Q X from Q and X^T.  So X is held both
+// ways, X^T twice (a launch reads one and writes the other).
+//
+// Operands are two fp16 numbers for one fp32, 2^13 x = high + low.  No entry of X, P or Q is beyond 3 (their singular
+// values are not), so high is below 2^15, and low keeps 11 bits more down to 2^-24: 22 bits of an entry above 2^-15, 2^-38 of a smaller
+// one.  A product takes high high + high low + low high on the matrix cores, where sums are fp32; the last, low low, is 2^-22 of the
+// first.
+#pragma once
+
+#include "choco_types.h"
+
+namespace choco {
+
+constexpr float kMuonA = 3.4445f, kMuonB = -4.7750f, kMuonC = 2.0315f;
+constexpr float kMuonUp = 8192.0f, kMuonDown = 1.0f / 8192.0f;
+constexpr int kMuonPad = 64;      // rows of operands end on a multiple of so many entries, with zeros
+constexpr int kMuonTile = 64;     // of what a workgroup makes
+constexpr int kMuonMost = 1 << 16;
+
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef float float4_t __attribute__((ext_vector_type(4)));
+
+// Matrices of one shape: one of each of `count` workers from `first` on.
+struct MuonShape {
+  int64_t source, source_of;      // entries from the source's begin to the first worker's matrix, and from there to the next's
+  int64_t target, target_of;      // of x or of the result
+  int64_t moment;                 // of worker 0's momentum; the next is rows * cols behind
+  int64_t source_ld, target_ld;
+  int64_t scratch, scratch_of;    // bytes
+  int64_t partials;               // sums of squares of the tiles, one matrix behind the other
+  int32_t rows, cols, a, b, a_ld, b_ld, first, count;
+  float decay, rate;
+  uint32_t start_begin, gram_begin, apply_begin;    // tiles before these matrices'
+  uint32_t start_tiles, gram_tiles, apply_tiles;    // of one of them
+};
+
+struct MuonArgs {
+  MuonShape one;                  // without a table
+  const MuonShape* table;
+  int32_t count;
+  const void* source;             // gradients or matrices
+  float* target;                  // parameters or result
+  float* moments;                 // null: matrices as they are
+  const float* grad_scale;
+  double* partials;
+  char* scratch;
+  float momentum, lr;
+  int32_t nesterov;
+  int32_t now;                    // which of the X^T is read
+  bool last;
+};
+
+__device__ __forceinline__ int64_t plane(int64_t rows, int64_t ld) { return rows * ld; }
+// The operands of a matrix, high planes with the low ones behind them.
+struct MuonPlanes {
+  f16_t *x, *xt[2], *p, *q;
+  int64_t x_low, xt_low, p_low;
+};
+inline __host__ __device__ int64_t muon_scratch(int64_t a, int64_t b, int64_t a_ld, int64_t b_ld) {
+  return 4 * (a * b_ld + 2 * b * a_ld + 2 * a * a_ld);
+}
+__device__ __forceinline__ MuonPlanes planes_of(const MuonArgs& A, const MuonShape& S, int i) {
+  MuonPlanes P;
+  P.x_low = (int64_t)S.a * S.b_ld;
+  P.xt_low = (int64_t)S.b * S.a_ld;
+  P.p_low = (int64_t)S.a * S.a_ld;
+  P.x = (f16_t*)(A.scratch + S.scratch + i * S.scratch_of);
+  P.xt[0] = P.x + 2 * P.x_low;
+  P.xt[1] = P.xt[0] + 2 * P.xt_low;
+  P.p = P.xt[1] + 2 * P.xt_low;
+  P.q = P.p + 2 * P.p_low;
+  return P;
+}
+
+// Which matrices a tile belongs to: the last whose tiles begin at or before it.
+__device__ __forceinline__ MuonShape shape_of(const MuonArgs& A, uint32_t tile, uint32_t MuonShape::*begin) {
+  if (!A.table) return A.one;
+  int lo = 0, hi = A.count - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) / 2;
+    if (A.table[mid].*begin <= tile) lo = mid;
+    else hi = mid - 1;
+  }
+  return A.table[lo];
+}
+
+__device__ __forceinline__ void split(float x, f16_t& high, f16_t& low) {
+  high = (f16_t)x;
+  low = (f16_t)(x - (float)high);
+}
+
+// ---- from gradients to the first X ----
+// A tile of 64 x 64 entries of the matrix as it lies in memory; a thread takes 16 of a column.
+struct MuonTile {
+  int i;              // which of the shape's matrices
+  int64_t row, col;
+};
+__device__ __forceinline__ MuonTile start_tile(const MuonShape& S) {
+  const uint32_t at = blockIdx.x - S.start_begin, in = at % S.start_tiles, wide = (S.cols + 63) / 64;
+  return {(int)(at / S.start_tiles), (int64_t)(in / wide) * 64, (int64_t)(in % wide) * 64};
+}
+template <class T>
+__device__ __forceinline__ float source_entry(const MuonArgs& A, const MuonShape& S, int i, int64_t r, int64_t c) {
+  return to_float(((const T*)A.source)[S.source + i * S.source_of + r * S.source_ld + c]);
+}
+// The momentum's update; the sum of squares of what is to be orthogonalised.
+template <class T, bool STEP>
+__global__ __launch_bounds__(256) void k_muon_squares(MuonArgs A) {
+  __shared__ double part[4];
+  const MuonShape S = shape_of(A, blockIdx.x, &MuonShape::start_begin);
+  const MuonTile M = start_tile(S);
+  const int worker = S.first + M.i;
+  const float scale = STEP && A.grad_scale ? A.grad_scale[worker] : 1.0f;
+  const int64_t c = M.col + (threadIdx.x & 63);
+  double sum = 0.0;
+  if (c < S.cols)
+    for (int j = threadIdx.x >> 6; j < 64; j += 4) {
+      const int64_t r = M.row + j;
+      if (r >= S.rows) break;
+      float u = source_entry<T>(A, S, M.i, r, c);
+      if (STEP) {
+        float* m = A.moments + S.moment + ((int64_t)worker * S.rows + r) * S.cols + c;
+        if (__builtin_isfinite(scale)) {
+          const float g = u * scale, now = fmaf(A.momentum, *m, g);
+          *m = now;
+          u = A.nesterov ? fmaf(A.momentum, now, g) : now;
+        } else {
+          u = 0.0f;
+        }
+      }
+      sum += (double)u * (double)u;
+    }
+  for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) A.partials[S.partials + blockIdx.x - S.start_begin] = (part[0] + part[1]) + (part[2] + part[3]);
+}
+// X = u / |u|, both ways.
+template <class T, bool STEP>
+__global__ __launch_bounds__(256) void k_muon_start(MuonArgs A) {
+  __shared__ float tile[64][65];
+  __shared__ double part[4];
+  const MuonShape S = shape_of(A, blockIdx.x, &MuonShape::start_begin);
+  const MuonTile M = start_tile(S);
+  const int worker = S.first + M.i;
+  const float scale = STEP && A.grad_scale ? A.grad_scale[worker] : 1.0f;
+  double sum = 0.0;
+  for (uint32_t t = threadIdx.x; t < S.start_tiles; t += 256) sum += A.partials[S.partials + (int64_t)M.i * S.start_tiles + t];
+  for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
+  __syncthreads();
+  sum = (part[0] + part[1]) + (part[2] + part[3]);
+  const double up = sum == 0.0 ? 0.0 : (double)kMuonUp / sqrt(sum);
+  const int64_t c = M.col + (threadIdx.x & 63);
+  for (int j = threadIdx.x >> 6; j < 64; j += 4) {
+    const int64_t r = M.row + j;
+    float u = 0.0f;
+    if (c < S.cols && r < S.rows) {
+      u = source_entry<T>(A, S, M.i, r, c);
+      if (STEP) {
+        const float g = u * scale, now = A.moments[S.moment + ((int64_t)worker * S.rows + r) * S.cols + c];
+        u = A.nesterov ? fmaf(A.momentum, now, g) : now;
+      }
+      u = (float)((double)u * up);
+    }
+    tile[j][threadIdx.x & 63] = u;
+  }
+  __syncthreads();
+  const MuonPlanes P = planes_of(A, S, M.i);
+  const bool tall = S.rows > S.cols;
+  // rows of X are rows of memory, or its columns
+  f16_t *const along = tall ? P.xt[0] : P.x, *const across = tall ? P.x : P.xt[0];
+  const int64_t along_low = tall ? P.xt_low : P.x_low, across_low = tall ? P.x_low : P.xt_low;
+  const int64_t along_ld = tall ? S.a_ld : S.b_ld, across_ld = tall ? S.b_ld : S.a_ld;
+  for (int j = threadIdx.x >> 6; j < 64; j += 4) {
+    const int e = threadIdx.x & 63;
+    f16_t high, low;
+    if (M.row + j < S.rows) {
+      split(tile[j][e], high, low);
+      f16_t* to = along + (M.row + j) * along_ld + M.col + e;
+      to[0] = high;
+      to[along_low] = low;
+    }
+    if (M.col + j < S.cols) {
+      split(tile[e][j], high, low);
+      f16_t* to = across + (M.col + j) * across_ld + M.row + e;
+      to[0] = high;
+      to[across_low] = low;
+    }
+  }
+}
+
+// ---- products ----
+enum { kGram = 0, kSquare = 1, kApply = 2 };
+
+// Tile `at` of the lower triangle, row after row: its row and column.
+__device__ __forceinline__ void triangle(uint32_t at, uint32_t& i, uint32_t& j) {
+  i = (uint32_t)((sqrtf(8.0f * (float)at + 1.0f) - 1.0f) * 0.5f);
+  while (i * (i + 1) / 2 > at) --i;
+  while ((i + 1) * (i + 2) / 2 <= at) ++i;
+  j = at - i * (i + 1) / 2;
+}
+
+template <int KIND>
+__global__ __launch_bounds__(256) void k_muon_product(MuonArgs A) {
+  constexpr uint32_t MuonShape::*kBegin = KIND == kApply ? &MuonShape::apply_begin : &MuonShape::gram_begin;
+  const MuonShape S = shape_of(A, blockIdx.x, kBegin);
+  const uint32_t at = blockIdx.x - S.*kBegin, tiles = KIND == kApply ? S.apply_tiles : S.gram_tiles, in = at % tiles;
+  const int which = (int)(at / tiles);
+  const MuonPlanes P = planes_of(A, S, which);
+  uint32_t ti, tj;
+  if (KIND == kApply) {
+    const uint32_t high = (S.a + kMuonTile - 1) / kMuonTile;
+    ti = in % high;
+    tj = in / high;
+  } else {
+    triangle(in, ti, tj);
+  }
+  // (rows of n: the other operand's)
+  const f16_t *left = KIND == kGram ? P.x : KIND == kSquare ? P.p : P.q, *right = KIND == kApply ? P.xt[A.now] : left;
+  const int64_t left_low = KIND == kGram ? P.x_low : P.p_low, right_low = KIND == kApply ? P.xt_low : left_low;
+  const int64_t ld = KIND == kGram ? S.b_ld : S.a_ld;
+  const int ms = S.a, ns = KIND == kApply ? S.b : S.a;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4;
+  const int m0 = ti * kMuonTile + (wave & 1) * 32, n0 = tj * kMuonTile + (wave >> 1) * 32;
+  float4_t acc[2][2] = {};
+  const f16_t *pl[2], *pr[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    pl[i] = left + (int64_t)min(m0 + 16 * i + l, ms - 1) * ld + 8 * g;
+    pr[i] = right + (int64_t)min(n0 + 16 * i + l, ns - 1) * ld + 8 * g;
+  }
+  for (int64_t k = 0; k < ld; k += 32) {
+    half8 lh[2], ll[2], rh[2], rl[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      lh[i] = *(const half8*)(pl[i] + k);
+      ll[i] = *(const half8*)(pl[i] + left_low + k);
+      rh[i] = *(const half8*)(pr[i] + k);
+      rl[i] = *(const half8*)(pr[i] + right_low + k);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ll[i], rh[j], acc[i][j], 0, 0, 0);
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lh[i], rl[j], acc[i][j], 0, 0, 0);
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lh[i], rh[j], acc[i][j], 0, 0, 0);
+      }
+  }
+  const int worker = S.first + which;
+  const bool skip = A.moments && A.grad_scale && !__builtin_isfinite(A.grad_scale[worker]);
+  const bool tall = S.rows > S.cols;
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int m = m0 + 16 * i + 4 * g + r, n = n0 + 16 * j + l;
+        if (KIND != kApply) {
+          float x = 0.0f;       // behind a row, for sums over whole rows
+          if (m < ms && n < ns) {
+            x = acc[i][j][r] * kMuonDown;
+            if (KIND == kSquare) {
+              const f16_t* p = P.p + (int64_t)m * ld + n;
+              x = kMuonC * x + kMuonB * ((float)p[0] + (float)p[P.p_low]);
+            }
+          }
+          f16_t high, low;
+          split(x, high, low);
+          f16_t* const made = KIND == kGram ? P.p : P.q;
+          if (m < ms && n < S.a_ld) {
+            f16_t* to = made + (int64_t)m * S.a_ld + n;
+            to[0] = high;
+            to[P.p_low] = low;
+          }
+          if (ti != tj && n < ns && m < S.a_ld) {     // and its mirror image
+            f16_t* to = made + (int64_t)n * S.a_ld + m;
+            to[0] = high;
+            to[P.p_low] = low;
+          }
+          continue;
+        }
+        if (A.last) {
+          if (m >= ms || n >= ns || skip) continue;
+          const f16_t* p = P.xt[A.now] + (int64_t)n * S.a_ld + m;
+          const float x = kMuonDown * (acc[i][j][r] * kMuonDown + kMuonA * ((float)p[0] + (float)p[P.xt_low]));
+          float* to = A.target + S.target + which * S.target_of + (int64_t)(tall ? n : m) * S.target_ld + (tall ? m : n);
+          if (A.moments) *to = *to * (1.0f - A.lr * S.decay) - A.lr * S.rate * x;
+          else *to = x;
+          continue;
+        }
+        // X and X^T, zeros behind their rows
+        float x = 0.0f;
+        if (m < ms && n < ns) {
+          const f16_t* p = P.xt[A.now] + (int64_t)n * S.a_ld + m;
+          x = acc[i][j][r] * kMuonDown + kMuonA * ((float)p[0] + (float)p[P.xt_low]);
+        }
+        f16_t high, low;
+        split(x, high, low);
+        if (m < ms && n < S.b_ld) {
+          f16_t* to = P.x + (int64_t)m * S.b_ld + n;
+          to[0] = high;
+          to[P.x_low] = low;
+        }
+        if (n < ns && m < S.a_ld) {
+          f16_t* to = P.xt[A.now ^ 1] + (int64_t)n * S.a_ld + m;
+          to[0] = high;
+          to[P.xt_low] = low;
+        }
+      }
+}
+
+}  // namespace choco

@@ -13,6 +13,7 @@
 #include <vector>
 
 #include "choco_train.h"
+#include "choco_host.h"
 #include "choco_adamw.h"
 #include "choco_embed.h"
 #include "choco_recur.h"
@@ -20,34 +21,6 @@
 using namespace choco;
 
 namespace {
-
-thread_local int g_last_hip_error = 0;
-
-#define TRY_HIP(expr)                        \
-  do {                                       \
-    const hipError_t e_ = (expr);            \
-    if (e_ != hipSuccess) {                  \
-      g_last_hip_error = (int)e_;            \
-      return CHOCO_E_HIP;                    \
-    }                                        \
-  } while (0)
-
-constexpr int64_t kMaxIndex = (int64_t)1 << 31;
-constexpr int64_t kMaxExtent = (int64_t)1 << 60;   // entries of any array, strides included
-
-int type_bytes(int type) { return type == CHOCO_F32 ? 4 : type == CHOCO_BF16 || type == CHOCO_F16 ? 2 : 0; }
-bool aligned_to(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
-// A grid's first dimension holds less than 2^32 threads.
-bool launch_fits(double blocks, int threads) { return blocks * threads < 4294967296.0; }
-uint32_t blocks_of(int64_t items, int64_t per_block) { return (uint32_t)((items + per_block - 1) / per_block); }
-
-// calls FN.operator()<T>() for the C++ type of a CHOCO_F32 / BF16 / F16
-template <class Fn>
-void with_type(int type, Fn&& fn) {
-  if (type == CHOCO_F32) fn(float{});
-  else if (type == CHOCO_BF16) fn(bf16_t{});
-  else fn(f16_t{});
-}
 
 // ---- embedding ----
 

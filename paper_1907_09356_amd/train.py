@@ -1,9 +1,10 @@
-"""ctypes binding of include/choco_train.h: embedding lookup and gradient, gated linear recurrence, AdamW.
+"""ctypes binding of include/choco_train.h: embedding lookup and gradient, gated linear recurrence, linear attention with decays,
+AdamW, orthogonalised matrices and an optimiser that steps along them.
 
 Argument marshalling only, like `binding`: torch provides device memory and the stream, every computation runs in the
 HIP library.  Functions and methods enqueue on torch's current stream of the tensors' device.  As with torch's own operations, work of
 one stream that needs that of another has to wait for it, and a tensor that is used on another stream than the one it was
-made on has to be kept until that stream is done with it (an `AdamW` sees to its own workspace).  Nothing here is recorded by
+made on has to be kept until that stream is done with it (an `AdamW` or `Muon` sees to its own workspace).  Nothing here is recorded by
 torch's automatic differentiation: results do not require a gradient, and the gradients are calls of their own.
 """
 import ctypes
@@ -23,9 +24,12 @@ TOKEN_TYPES = {torch.int32: I32, torch.int64: I64}
 
 EXPORTS = [
     "choco_embed_workspace_bytes", "choco_embed_forward", "choco_embed_backward", "choco_recur_saved_bytes",
-    "choco_recur_workspace_bytes", "choco_recur_forward", "choco_recur_backward", "choco_adamw_workspace_bytes",
+    "choco_recur_workspace_bytes", "choco_recur_forward", "choco_recur_backward", "choco_linear_saved_bytes",
+    "choco_linear_workspace_bytes", "choco_linear_forward", "choco_linear_backward", "choco_adamw_workspace_bytes",
     "choco_adamw_init", "choco_adamw_step", "choco_adamw_moments", "choco_adamw_state", "choco_adamw_set_stream",
-    "choco_adamw_get_step", "choco_adamw_set_step", "choco_adamw_destroy", "choco_train_last_hip_error",
+    "choco_adamw_get_step", "choco_adamw_set_step", "choco_adamw_destroy", "choco_orthogonalize_workspace_bytes",
+    "choco_orthogonalize", "choco_muon_workspace_bytes", "choco_muon_init", "choco_muon_step", "choco_muon_state",
+    "choco_muon_set_stream", "choco_muon_destroy", "choco_train_last_hip_error",
 ]
 
 _i32, _i64, _u64, _f32, _f64 = ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64, ctypes.c_float, ctypes.c_double
@@ -50,6 +54,24 @@ class AdamwConfig(ctypes.Structure):
                 ("state_bits", _i32), ("seed", _u64), ("stream", _vp)]
 
 
+class LinearConfig(ctypes.Structure):
+    _fields_ = [("batch", _i64), ("steps", _i64)] + [
+        (name, _i32) for name in ("heads", "q_heads", "k_heads", "v_heads", "dim_k", "dim_v", "type", "gate_steps")] + [
+        (name + "_stride", _i64 * 3) for name in ("q", "k", "v", "y", "g", "dq", "dk", "dv")] + [("stream", _vp)]
+
+
+class OrthogonalizeConfig(ctypes.Structure):
+    _fields_ = [("batch", _i64), ("rows", _i64), ("cols", _i64), ("type", _i32), ("x_stride", _i64 * 2), ("y_stride", _i64 * 2),
+                ("iterations", _i32), ("stream", _vp)]
+
+
+class MuonConfig(ctypes.Structure):
+    _fields_ = [("n", _i32), ("d", _i64), ("ld", _i64), ("ntensors", _i32), ("start_host", ctypes.POINTER(_i64)),
+                ("rows_host", ctypes.POINTER(_i64)), ("cols_host", ctypes.POINTER(_i64)),
+                ("weight_decay_host", ctypes.POINTER(_f32)), ("lr_scale_host", ctypes.POINTER(_f32)), ("momentum", _f64),
+                ("nesterov", _i32), ("iterations", _i32), ("stream", _vp)]
+
+
 _lib = None
 
 
@@ -59,6 +81,7 @@ def lib():
     if _lib is None:
         L = binding.lib()
         embed, recur, adamw, size = (ctypes.POINTER(t) for t in (EmbedConfig, RecurConfig, AdamwConfig, _size))
+        linear, stack, muon = (ctypes.POINTER(t) for t in (LinearConfig, OrthogonalizeConfig, MuonConfig))
         L.choco_embed_workspace_bytes.argtypes = [embed, size]
         L.choco_embed_forward.argtypes = [embed, _vp, _vp, _vp]
         L.choco_embed_backward.argtypes = [embed, _vp, _vp, _vp, ctypes.c_int, _vp, _size]
@@ -75,6 +98,18 @@ def lib():
         L.choco_adamw_get_step.argtypes = [_vp, ctypes.POINTER(_u64)]
         L.choco_adamw_set_step.argtypes = [_vp, _u64]
         L.choco_adamw_destroy.argtypes = [_vp]
+        L.choco_linear_saved_bytes.argtypes = [linear, size]
+        L.choco_linear_workspace_bytes.argtypes = [linear, ctypes.c_int, size]
+        L.choco_linear_forward.argtypes = [linear] + [_vp] * 10 + [_size]
+        L.choco_linear_backward.argtypes = [linear] + [_vp] * 14 + [_size]
+        L.choco_orthogonalize_workspace_bytes.argtypes = [stack, size]
+        L.choco_orthogonalize.argtypes = [stack, _vp, _vp, _vp, _size]
+        L.choco_muon_workspace_bytes.argtypes = [muon, size]
+        L.choco_muon_init.argtypes = [muon, _vp, _vp, _size, ctypes.POINTER(_vp)]
+        L.choco_muon_step.argtypes = [_vp, _vp, _i32, _f32, _vp]
+        L.choco_muon_state.argtypes = [_vp, ctypes.POINTER(_vp), size]
+        L.choco_muon_set_stream.argtypes = [_vp, _vp]
+        L.choco_muon_destroy.argtypes = [_vp]
         L.choco_train_last_hip_error.argtypes = []
         for name in EXPORTS:
             getattr(L, name).restype = ctypes.c_int
@@ -245,6 +280,84 @@ def recurrence_grad(f, u, saved, dy, o=None, lengths=None, dlast=None):
     return df, du, do, dh0
 
 
+# ---- linear attention -----------------------------------------------------------------------------
+@functools.lru_cache(maxsize=512)
+def _linear_plan(back, shapes, dtype, strides, gate_shape, gate_stride, stream):
+    """The configuration of a call and its workspace: shapes of q, k, v, y (backward: dy); strides of these and of dq, dk, dv."""
+    assert dtype in TYPES and all(len(s) == 4 for s in shapes)
+    (B, T, hq, dk), (_, _, hk, _), (_, _, hv, dv), (_, _, H, _) = shapes
+    assert shapes == ((B, T, hq, dk), (B, T, hk, dk), (B, T, hv, dv), (B, T, H, dv))
+    assert gate_shape in ((H,), (B, T, H))
+    dims = (dk, dk, dv, dv, dk, dk, dv)
+    assert all(d <= 1 or s[3] == 1 for d, s in zip(dims, strides))
+    gate_stride = (0, 0) + gate_stride if len(gate_shape) == 1 else gate_stride
+    cfg = LinearConfig(batch=B, steps=T, heads=H, q_heads=hq, k_heads=hk, v_heads=hv, dim_k=dk, dim_v=dv, type=TYPES[dtype],
+                       gate_steps=len(gate_shape) == 3, g_stride=(_i64 * 3)(*gate_stride), stream=stream)
+    for name, s in zip(("q", "k", "v", "y", "dq", "dk", "dv"), strides):
+        getattr(cfg, name + "_stride")[:] = s[:3]
+    need, kept = _size(), _size()
+    _check(lib().choco_linear_workspace_bytes(ctypes.byref(cfg), back, ctypes.byref(need)), "choco_linear_workspace_bytes")
+    _check(lib().choco_linear_saved_bytes(ctypes.byref(cfg), ctypes.byref(kept)), "choco_linear_saved_bytes")
+    return ctypes.byref(cfg), need.value, kept.value
+
+
+def _linear_config(back, g, tensors):
+    q = tensors[0]
+    device, dtype = q.get_device(), q.dtype
+    assert q.is_cuda and g.get_device() == device and g.dtype == torch.float32
+    for t in tensors:
+        assert t.dtype == dtype and t.get_device() == device
+    return _linear_plan(back, tuple(t.shape for t in tensors[:4]), dtype, tuple(t.stride() for t in tensors), g.shape, g.stride(),
+                        _stream(q))
+
+
+def _head_state(t, q, shape):
+    """The address of a state of every sequence and head, or None."""
+    if t is None:
+        return None
+    assert t.get_device() == q.get_device() and t.dtype == torch.float32 and t.is_contiguous() and t.shape == shape
+    return t.data_ptr()
+
+
+def linear_attention(q, k, v, g, h0=None, lengths=None, save=False, out=None, h_last=None):
+    """S_t = exp(g_t) S_{t-1} + k_t v_t^T, y_t = S_t^T q_t for every sequence and head: (y, last states, saved).
+
+    q, k (batch, steps, heads of each, dk), v (batch, steps, heads of v, dv) of one type, strided as they come (columns of one
+    projection); the logarithms g <= 0 of the decays, float32 of (heads,) or (batch, steps, heads), say how many heads there are,
+    and each of the others' divides it: neighbouring heads share.  y (batch, steps, heads, dv); states (batch, heads, dk, dv) of
+    float32, h0 zero without; lengths (batch,) of int32; dk and dv up to 256.  save: keep what `linear_attention_grad` needs (else
+    None is returned).  h_last may be h0 itself, as in token by token generation."""
+    B, T, _, dk = q.shape
+    dv, H = v.shape[3], g.shape[-1]
+    y = v.new_empty((B, T, H, dv)) if out is None else out
+    state = (B, H, dk, dv)
+    if h_last is None:
+        h_last = torch.empty(state, dtype=torch.float32, device=q.device)
+    cfg, nbytes, kept = _linear_config(0, g, (q, k, v, y))
+    saved = torch.empty(kept // 4, dtype=torch.float32, device=q.device) if save else None
+    ws = _scratch(nbytes, q)
+    _enqueue(q, "choco_linear_forward", cfg, q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), _head_state(h0, q, state),
+             _lengths(lengths, q), y.data_ptr(), _head_state(h_last, q, state), _ptr(saved), _ptr(ws), nbytes)
+    return y, h_last, saved
+
+
+def linear_attention_grad(q, k, v, g, saved, dy, lengths=None, dlast=None):
+    """Backward pass of `linear_attention`: (dq, dk, dv, dg, dh0), each of its input's shape.
+
+    saved as `linear_attention(..., save=True)` returned it; dlast the gradient of the last states, zero without."""
+    state = (q.shape[0], g.shape[-1], q.shape[3], v.shape[3])
+    dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+    dg = torch.empty(g.shape, dtype=torch.float32, device=q.device)
+    dh0 = torch.empty(state, dtype=torch.float32, device=q.device)
+    cfg, nbytes, kept = _linear_config(1, g, (q, k, v, dy, dq, dk, dv))
+    assert saved.get_device() == q.get_device() and saved.dtype == torch.float32 and saved.is_contiguous() and saved.numel() * 4 == kept
+    ws = _scratch(nbytes, q)
+    _enqueue(q, "choco_linear_backward", cfg, q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), _lengths(lengths, q),
+             saved.data_ptr(), dy.data_ptr(), _head_state(dlast, q, state), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
+             dg.data_ptr(), dh0.data_ptr(), _ptr(ws), nbytes)
+    return dq, dk, dv, dg, dh0
+
+
 # ---- AdamW ----------------------------------------------------------------------------------------
 def make_adamw_config(n, d, ld=0, tensors=None, weight_decay=None, lr_scale=None, betas=(0.9, 0.999), eps=1e-8, state_bits=32,
                       seed=0, stream=None):
@@ -340,3 +453,108 @@ class AdamW:
 
     def set_step(self, t):
         _check(lib().choco_adamw_set_step(self.handle, int(t)), "choco_adamw_set_step")
+
+
+# ---- orthogonalised matrices ----------------------------------------------------------------------
+@functools.lru_cache(maxsize=512)
+def _orthogonalize_plan(shape, dtype, stride, out_stride, iterations, stream):
+    assert len(shape) == 3 and dtype in TYPES
+    assert shape[2] <= 1 or stride[2] == out_stride[2] == 1
+    return _planned(OrthogonalizeConfig(batch=shape[0], rows=shape[1], cols=shape[2], type=TYPES[dtype],
+                                        x_stride=(_i64 * 2)(*stride[:2]), y_stride=(_i64 * 2)(*out_stride[:2]),
+                                        iterations=iterations, stream=stream), lib().choco_orthogonalize_workspace_bytes)
+
+
+def orthogonalize(x, iterations=5, out=None):
+    """The matrices x (batch, rows, cols) after Newton-Schulz iterations from x over its Frobenius norm, float32: with five, singular
+    values that were not far below the largest lie within 0.7 and 1.2, in the same directions."""
+    assert x.is_cuda and x.dim() == 3
+    if out is None:
+        out = torch.empty(x.shape, dtype=torch.float32, device=x.device)
+    assert out.dtype == torch.float32 and out.shape == x.shape and out.get_device() == x.get_device()
+    cfg, nbytes = _orthogonalize_plan(x.shape, x.dtype, x.stride(), out.stride(), int(iterations), _stream(x))
+    ws = _scratch(nbytes, x)
+    _enqueue(x, "choco_orthogonalize", cfg, x.data_ptr(), out.data_ptr(), _ptr(ws), nbytes)
+    return out
+
+
+def make_muon_config(n, d, ld, matrices, weight_decay=None, lr_scale=None, momentum=0.95, nesterov=True, iterations=5, stream=None):
+    """Fill a choco_muon_config.  Returns (config, keepalive).  matrices = (start, rows, cols) arrays; weight_decay and
+    lr_scale a number or one per matrix."""
+    cfg = MuonConfig(n=int(n), d=int(d), ld=int(ld), momentum=float(momentum), nesterov=int(bool(nesterov)),
+                     iterations=int(iterations), stream=stream)
+    keep = []
+
+    def array(values, dtype, kind):
+        a = np.ascontiguousarray(values, dtype=dtype)
+        keep.append(a)
+        return a.ctypes.data_as(ctypes.POINTER(kind))
+
+    start, rows, cols = matrices
+    assert len(start) == len(rows) == len(cols)
+    cfg.ntensors = count = len(start)
+    cfg.start_host, cfg.rows_host, cfg.cols_host = (array(v, np.int64, _i64) for v in (start, rows, cols))
+    if weight_decay is not None:
+        cfg.weight_decay_host = array(np.broadcast_to(weight_decay, (count,)), np.float32, _f32)
+    if lr_scale is not None:
+        cfg.lr_scale_host = array(np.broadcast_to(lr_scale, (count,)), np.float32, _f32)
+    return cfg, tuple(keep)
+
+
+class Muon:
+    """Steps along orthogonalised momentum of matrices in the parameter rows X (n, ld) of all workers, in place: `step` takes the
+    place of their local update, an `AdamW` on the same X may take the other tensors.  matrices: (start, rows, cols) arrays;
+    lr_scale: sqrt(max(1, rows / cols)) where it is not given."""
+
+    def __init__(self, X, d, matrices, **kw):
+        assert X.is_cuda and X.dtype == torch.float32 and X.is_contiguous() and X.dim() == 2
+        self.X, self.stream = X, _stream(X)
+        self.shapes = [(X.shape[0], int(r), int(c)) for r, c in zip(matrices[1], matrices[2])]
+        cfg, keep = make_muon_config(X.shape[0], d, X.shape[1], matrices, stream=self.stream, **kw)
+        need, a = _size(), _vp()
+        _check(lib().choco_muon_workspace_bytes(ctypes.byref(cfg), ctypes.byref(need)), "choco_muon_workspace_bytes")
+        self.workspace = torch.empty(need.value + 256, dtype=torch.uint8, device=X.device)
+        base = (self.workspace.data_ptr() + 255) // 256 * 256
+        _enqueue(X, "choco_muon_init", ctypes.byref(cfg), _ptr(X), base, need.value, ctypes.byref(a))
+        del keep
+        self.handle = a
+
+    def close(self):
+        if getattr(self, "handle", None):
+            lib().choco_muon_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def step(self, G, lr, grad_scale=None):
+        """G: gradients (n, ld) of float32 or bfloat16; grad_scale: (n,) of float32 on the device, a factor for each
+        worker's gradient (one that is not finite leaves the worker as it is)."""
+        assert G.device == self.X.device and G.is_contiguous() and G.shape == self.X.shape and G.dtype in (torch.float32, torch.bfloat16)
+        if grad_scale is not None:
+            assert grad_scale.device == G.device and grad_scale.dtype == torch.float32
+            assert grad_scale.is_contiguous() and grad_scale.shape == G.shape[:1]
+        stream = _stream(self.X)
+        if stream != self.stream:       # the workspace is then kept from reuse until that stream is done, too
+            self.workspace.record_stream(torch.cuda.current_stream(self.X.device))
+            _check(lib().choco_muon_set_stream(self.handle, stream), "choco_muon_set_stream")
+            self.stream = stream
+        _enqueue(self.X, "choco_muon_step", self.handle, _ptr(G), TYPES[G.dtype], float(lr), _ptr(grad_scale))
+
+    def state(self):
+        """The momenta as they are held, a view of bytes that moves with the next step: copy it to save a run, copy back to resume it."""
+        p, count = _vp(), _size()
+        _check(lib().choco_muon_state(self.handle, ctypes.byref(p), ctypes.byref(count)), "choco_muon_state")
+        at = p.value - self.workspace.data_ptr()
+        return self.workspace[at:at + count.value]
+
+    def momentum(self):
+        """The momenta, float32 of (n, rows, cols) for each matrix: views that move with the next step."""
+        flat, at, out = self.state().view(torch.float32), 0, []
+        for n, rows, cols in self.shapes:
+            out.append(flat[at:at + n * rows * cols].view(n, rows, cols))
+            at += n * rows * cols
+        return out

@@ -1,0 +1,298 @@
+"""Orthogonalised matrices and the optimiser that steps along them, against the iteration in 64 bits.
+
+Tolerances, in Frobenius norms.  One iteration's results are sums of products of operands that are off by 2^-22 of the largest in
+their row or column, with 2^-22 left out of each product, and of at most K = the longer side terms, each addition off by 2^-24: with
+|X| = 1 at the start and spectral norms at most 1.5 (of X and P) and 3 (of Q), an iteration adds at most
+e = (3 + 2 |b| + 4 |c|) (4 2^-22 + K 2^-24) times the norm of what it multiplies.  The next iteration takes an error times at
+most a = 3.45 + ... < 5 (the polynomial's slope for singular values up to 1.25).  |X_i|_F is at most a^i and at most
+1.25 sqrt(shorter side)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_1907_09356_amd import train as T
+
+pytestmark = pytest.mark.gpu
+A, B, C = 3.4445, -4.7750, 2.0315
+SLOPE = 5.0
+
+
+def iterate(u, iterations):
+    u = u.double()
+    tall = u.shape[1] > u.shape[2]
+    x = u.transpose(1, 2) if tall else u
+    norm = x.square().sum((1, 2), keepdim=True).sqrt()
+    x = torch.where(norm > 0, x / norm, torch.zeros_like(x))
+    for _ in range(iterations):
+        p = x @ x.transpose(1, 2).contiguous()
+        x = A * x + (B * p + C * (p @ p)) @ x
+    return x.transpose(1, 2) if tall else x
+
+
+def allowed(rows, cols, iterations):
+    """Of the result's error in the Frobenius norm."""
+    K, side = max(rows, cols), min(rows, cols)
+    e = (3 + 2 * abs(B) + 4 * C) * (4 * 2.0 ** -22 + K * 2.0 ** -24)
+    total = 0.0
+    for i in range(iterations):
+        norm = min(3.4445 ** i, 1.25 * math.sqrt(side))
+        total += e * norm * SLOPE ** (iterations - 1 - i)
+    return total
+
+
+def matrices(shape, seed=1, dtype=torch.float32, scale=0.01):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    n, rows, cols = shape
+    rank = max(1, min(rows, cols) // 8)
+    x = torch.empty(shape, device="cuda").normal_(0.0, 1.0, generator=gen)
+    x += torch.bmm(torch.empty((n, rows, rank), device="cuda").normal_(0.0, 2.0, generator=gen),
+                   torch.empty((n, rank, cols), device="cuda").normal_(0.0, 1.0, generator=gen))
+    return (x * scale).to(dtype)
+
+
+def check(got, exact, iterations):
+    off = (got.double() - exact).flatten(1).norm(dim=1)
+    assert bool((off <= allowed(exact.shape[1], exact.shape[2], iterations)).all()), (exact.shape, off.max().item())
+
+
+SHAPES = [(1, 1), (1, 7), (5, 1), (2, 3), (16, 16), (17, 33), (63, 64), (64, 63), (65, 129), (128, 128), (130, 70), (200, 333), (333, 200), (50, 2000), (2000, 50),
+          (513, 640)]
+
+
+@pytest.mark.parametrize("rows, cols", SHAPES)
+@pytest.mark.parametrize("iterations", [1, 2, 5])
+def test_against_64_bits(rows, cols, iterations):
+    x = matrices((3, rows, cols), seed=rows + cols)
+    check(T.orthogonalize(x, iterations=iterations), iterate(x, iterations), iterations)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("scale", [1e-4, 1.0, 100.0])
+def test_types_and_magnitudes(dtype, scale):
+    x = matrices((2, 96, 200), dtype=dtype, scale=scale)
+    check(T.orthogonalize(x), iterate(x, 5), 5)
+
+
+@pytest.mark.parametrize("scale", [1e-37, 1e-25, 1e25, 1e37])
+def test_squares_beyond_fp32(scale):
+    x = matrices((2, 40, 72), scale=1.0)
+    want = T.orthogonalize(x / x.abs().max())
+    got = T.orthogonalize(x / x.abs().max() * scale)
+    assert float((got - want).norm()) <= allowed(40, 72, 5) * 4
+
+
+def test_singular_values_end_near_one():
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    q1 = torch.linalg.qr(torch.randn(150, 150, device="cuda", dtype=torch.float64, generator=gen))[0]
+    q2 = torch.linalg.qr(torch.randn(260, 260, device="cuda", dtype=torch.float64, generator=gen))[0][:150]
+    s = torch.logspace(-1, 0, 150, device="cuda", dtype=torch.float64)
+    x = (q1 * s) @ q2
+    o = T.orthogonalize(x.float()[None])[0].double()
+    got = torch.diagonal(q1.T @ o @ q2.T)
+    value = s / s.norm()
+    for _ in range(5):
+        value = A * value + B * value ** 3 + C * value ** 5
+    assert float((got - value).abs().max()) <= allowed(150, 260, 5)
+    assert float(got.min()) > 0.6 and float(got.max()) < 1.25
+
+
+def test_zeros_and_values_that_are_not_finite_stay_in_their_matrix():
+    x = matrices((5, 70, 90))
+    want = T.orthogonalize(x)
+    y = x.clone()
+    y[1] = 0
+    y[2, 3, 4] = torch.nan
+    y[3, 69, 89] = torch.inf
+    got = T.orthogonalize(y)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[4], want[4])
+    assert not got[1].any() and bool(got[2].isnan().all()) and bool(got[3].isnan().all())
+
+
+def test_empty_stacks():
+    for shape in ((0, 4, 4), (3, 0, 4), (3, 4, 0)):
+        assert T.orthogonalize(torch.zeros(shape, device="cuda")).shape == shape
+
+
+def test_strides():
+    x = matrices((3, 40, 100))
+    want = T.orthogonalize(x)
+    wide = torch.full((3, 41, 108), torch.nan, device="cuda")
+    wide[:, 1:, 5:105] = x
+    out = torch.zeros((40, 3, 101), device="cuda").transpose(0, 1)[..., :100]
+    got = T.orthogonalize(wide[:, 1:, 5:105], out=out)
+    assert got is out and torch.equal(got, want)
+    rows = x.transpose(0, 1).contiguous().transpose(0, 1)
+    assert torch.equal(T.orthogonalize(rows), want)
+    assert torch.equal(T.orthogonalize(x[:1].expand(3, -1, -1)), want[:1].expand(3, -1, -1))
+
+
+def test_tall_is_the_transposed_of_wide():
+    x = matrices((2, 300, 120))
+    a, b = T.orthogonalize(x), T.orthogonalize(x.transpose(1, 2).contiguous())
+    assert float((a - b.transpose(1, 2)).norm()) <= 2 * allowed(300, 120, 5)
+
+
+def test_same_inputs_same_bits_and_graphs():
+    x = matrices((6, 200, 130))
+    want = T.orthogonalize(x)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        again = T.orthogonalize(x)
+    torch.cuda.current_stream().wait_stream(stream)
+    assert torch.equal(again, want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = T.orthogonalize(x)
+    for _ in range(3):
+        got.zero_()
+        T.orthogonalize(x + 1)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
+
+
+# ---- the optimiser ----
+def rows_of(shapes, n, gap=5):
+    start, at = [], 3
+    for r, c in shapes:
+        start.append(at)
+        at += r * c + gap
+    return np.array(start), at, (at + 63) // 64 * 64
+
+
+class Plain:
+    def __init__(self, X, start, shapes, momentum, nesterov, decay, scale, iterations):
+        self.X = X.double().clone()
+        self.m = [torch.zeros((X.shape[0],) + s, dtype=torch.float64, device="cuda") for s in shapes]
+        self.how = (start, shapes, momentum, nesterov, decay, scale, iterations)
+
+    def step(self, G, lr, clip):
+        start, shapes, momentum, nesterov, decay, scale, iterations = self.how
+        for i, (a, (r, c)) in enumerate(zip(start, shapes)):
+            x = self.X[:, a:a + r * c].view(-1, r, c)
+            g = G[:, a:a + r * c].double().reshape(-1, r, c) * clip.double()[:, None, None]
+            on = torch.isfinite(clip)[:, None, None]
+            self.m[i] = torch.where(on, momentum * self.m[i] + g, self.m[i])
+            u = torch.where(on, g + momentum * self.m[i] if nesterov else self.m[i], 0.0)
+            new = x * (1 - lr * decay[i]) - lr * scale[i] * iterate(u, iterations)
+            x.copy_(torch.where(on, new, x))
+
+
+@pytest.mark.parametrize("n, shapes, grad, nesterov, iterations", [
+    (1, [(8, 8)], torch.float32, True, 5), (3, [(64, 192), (192, 64), (1, 40), (130, 7)], torch.float32, True, 5),
+    (2, [(200, 100), (33, 65)], torch.bfloat16, False, 5), (5, [(40, 40)] * 7, torch.bfloat16, True, 3), (1, [(700, 150)], torch.float32, False, 1),
+])
+def test_steps_against_64_bits(n, shapes, grad, nesterov, iterations):
+    start, d, ld = rows_of(shapes, n)
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    X = torch.empty((n, ld), device="cuda").normal_(0.0, 0.05, generator=gen)
+    before = X.clone()
+    decay = np.linspace(0.0, 0.1, len(shapes))
+    scale = np.array([math.sqrt(max(1.0, r / c)) for r, c in shapes])
+    plain = Plain(X, start, shapes, 0.9, nesterov, decay, scale, iterations)
+    opt = T.Muon(X, d, (start, [s[0] for s in shapes], [s[1] for s in shapes]), momentum=0.9, nesterov=nesterov, weight_decay=decay, iterations=iterations)
+    steps, lr = 3, 0.02
+    for t in range(steps):
+        G = torch.empty((n, ld), device="cuda").normal_(0.0, 0.1, generator=gen).to(grad)
+        clip = torch.rand(n, device="cuda", generator=gen) + 0.5
+        if t == 1 and n > 1:
+            clip[1] = torch.inf
+        opt.step(G, lr, grad_scale=clip)
+        plain.step(G, lr, clip)
+        for i, (r, c) in enumerate(shapes):
+            m = opt.momentum()[i]
+            # a product and two additions a step, of terms below 0.1 x 6 x 1.5 x 3
+            assert float((m.double() - plain.m[i]).abs().max()) <= 4 * (t + 1) * 2.0 ** -24 * 2.7
+            a = start[i]
+            off = (X[:, a:a + r * c].double() - plain.X[:, a:a + r * c]).norm(dim=1).max().item()
+            # each step's result, and three roundings of x; u is good to 2^-21 of its norm, which the first iteration takes
+            each = lr * scale[i] * (allowed(r, c, iterations) + SLOPE ** iterations * 2.0 ** -20)
+            assert off <= (t + 1) * (each + 3 * 2.0 ** -24 * float(plain.X[:, a:a + r * c].norm(dim=1).max())), (t, r, c, off)
+    inside = torch.zeros(ld, dtype=torch.bool, device="cuda")
+    for a, (r, c) in zip(start, shapes):
+        inside[a:a + r * c] = True
+    assert torch.equal(X[:, ~inside], before[:, ~inside])
+    opt.close()
+
+
+def test_scales_of_the_learning_rate_and_no_clipping():
+    shapes = [(30, 20), (20, 30)]
+    start, d, ld = rows_of(shapes, 2)
+    G = torch.randn((2, ld), device="cuda")
+    moved = []
+    for kw, scale in ((dict(), None), (dict(lr_scale=[2.0, 0.5]), torch.ones(2, device="cuda")), (dict(lr_scale=0.0), None)):
+        X = torch.zeros((2, ld), device="cuda")
+        opt = T.Muon(X, d, (start, [30, 20], [20, 30]), **kw)
+        opt.step(G, 0.5, grad_scale=scale)
+        moved.append([X[:, a:a + 600].clone() for a in start])
+    factor = math.sqrt(1.5)
+    assert torch.allclose(moved[1][0] * (factor / 2), moved[0][0], rtol=1e-6, atol=1e-9)
+    assert torch.allclose(moved[1][1] * 2, moved[0][1], rtol=1e-6, atol=1e-9)
+    assert not moved[2][0].any() and not moved[2][1].any()
+
+
+def test_state_saves_and_resumes_a_run():
+    shapes = [(33, 50), (70, 20)]
+    start, d, ld = rows_of(shapes, 2)
+    what = (start, [33, 70], [50, 20])
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    X = torch.empty((2, ld), device="cuda").normal_(generator=gen)
+    Gs = [torch.empty((2, ld), device="cuda").normal_(generator=gen) for _ in range(4)]
+    opt = T.Muon(X, d, what)
+    for G in Gs[:2]:
+        opt.step(G, 0.1)
+    kept, state = X.clone(), opt.state().clone()
+    assert state.numel() == 4 * 2 * (33 * 50 + 70 * 20)
+    for G in Gs[2:]:
+        opt.step(G, 0.1)
+    again = T.Muon(kept, d, what)
+    again.state().copy_(state)
+    for G in Gs[2:]:
+        again.step(G, 0.1)
+    assert torch.equal(kept, X)
+
+
+def test_streams_and_graphs():
+    shapes = [(40, 90), (90, 40)]
+    start, d, ld = rows_of(shapes, 3)
+    what = (start, [40, 90], [90, 40])
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    first = torch.empty((3, ld), device="cuda").normal_(generator=gen)
+    G = torch.empty((3, ld), device="cuda").normal_(generator=gen)
+    X = first.clone()
+    opt, want = T.Muon(X, d, what), []
+    for _ in range(4):
+        opt.step(G, 0.1)
+        want.append(X.clone())
+    Y = first.clone()
+    opt = T.Muon(Y, d, what)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        opt.step(G, 0.1)
+    torch.cuda.current_stream().wait_stream(stream)
+    assert torch.equal(Y, want[0])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        opt.step(G, 0.1)
+    for t in range(1, 4):
+        other = T.orthogonalize(torch.randn(2, 30, 30, device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(Y, want[t]) and bool(other.isfinite().all())
+
+
+def test_many_workers_of_a_large_matrix_in_rounds():
+    # operands of 130 workers are more than a round's: each worker's result is that of the worker alone
+    n, r, c = 130, 700, 800
+    X = torch.zeros((n, r * c), device="cuda")
+    G = torch.empty((n, r * c), device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(4))
+    opt = T.Muon(X, r * c, ([0], [r], [c]))
+    opt.step(G, 1.0)
+    for w in (0, 64, n - 1):
+        one = torch.zeros((1, r * c), device="cuda")
+        T.Muon(one, r * c, ([0], [r], [c])).step(G[w:w + 1].contiguous(), 1.0)
+        assert torch.equal(one[0], X[w])
