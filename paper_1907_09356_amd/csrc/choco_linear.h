@@ -7,6 +7,8 @@
 // where w = e^g_t forwards, and backwards the next step's, 1 at a sequence's last.
 #pragma once
 
+#include <type_traits>
+
 #include "choco_types.h"
 
 namespace choco {
@@ -25,7 +27,7 @@ struct LinearPass {
   int32_t state_a, state_c; // strides of a state's entries in memory; a state has da * dc
   const float* first;       // state before a sequence's first step of the pass, or null: zero; `first_of` states from one head to the next
   float* last;              // state after its last step, backwards decayed by the first step's w: of S_0
-  float* kept;              // states before the pass' pieces of kLinearSave steps, of each sequence and head `kept_of`; forwards and the last
+  float* kept;              // forwards: states before every kLinearSave-th step and the last one, `kept_of` of each sequence and head
   int64_t kept_of, first_of;
   float* dots;              // [slices][batch * heads][steps]
   bool back, wide;          // wide: out is fp32 whatever the inputs' type
@@ -93,8 +95,7 @@ __global__ __launch_bounds__(256) void k_linear_steps(LinearArgs A, LinearPass P
     __syncthreads();
     for (int i = 0; i < n; ++i) {
       const int64_t t = P.back ? len - 1 - (i0 + i) : i0 + i;
-      if (P.kept && (P.back ? t == len - 1 || t % kLinearSave == kLinearSave - 1 : t % kLinearSave == 0))
-        keep(P.kept + (bh * P.kept_of + t / kLinearSave) * state, 1.0f);
+      if (P.kept && t % kLinearSave == 0) keep(P.kept + (bh * P.kept_of + t / kLinearSave) * state, 1.0f);
       float w = 1.0f;
       if (!P.back) w = linear_decay(log_gate(A, b, t, h));
       else if (t + 1 < len) w = linear_decay(log_gate(A, b, t + 1, h));
@@ -121,8 +122,389 @@ __global__ __launch_bounds__(256) void k_linear_steps(LinearArgs A, LinearPass P
   }
   if (in)
     for (int64_t t = len + wave; t < A.steps; t += 4) store_result<T>(P, out + t * P.out_step, 0.0f);
-  if (P.kept && !P.back) keep(P.kept + (bh * P.kept_of + (len + kLinearSave - 1) / kLinearSave) * state, 1.0f);
+  if (P.kept) keep(P.kept + (bh * P.kept_of + (len + kLinearSave - 1) / kLinearSave) * state, 1.0f);
   if (P.last) keep(P.last + bh * state, P.back && len > 0 ? linear_decay(log_gate(A, b, 0, h)) : 1.0f);
+}
+
+// ---- in chunks ----
+// With c_t the sum of the logarithms of w since the chunk began and S the state before it,
+//   out_t = e^c_t S^T a_t + sum over s <= t of e^(c_t - c_s) (a_t b_s) c_s,   S <- e^c_end S + sum of e^(c_end - c_s) b_s c_s^T:
+// four products of matrices, on the matrix cores, out^T = S^T a^T + c^T P^T with P^T = (b a^T) weighted.  A wave takes 16 columns of the result
+// and holds the state's in registers as the matrix cores leave a product: a lane has a column's rows 4 g to 4 g + 3 of every 16.
+// That is how the cores take a left operand whose inner index is the row, so neither S nor P^T goes through LDS; every wave makes
+// P^T of its own.  Differences of c are taken of c in two floats: a start-over leaves the steps behind it exact.
+//
+// Entries of 32 bits (and of fp16, taken as 32 bits) go to the fp32 matrix instruction.  Those of bf16 are operands as they are; what is fp32
+// by nature (P, S, weighted c) enters as a sum of bf16 numbers, two of them (2^-17) for a result of 16 bits, three (2^-25) for states
+// and wherever the result also goes into fp32 sums.
+constexpr int kChunk = 64;
+constexpr float kLog2Least = -300.0f;     // stands for -infinity: less than any difference that counts
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+template <class Core>
+struct Operand;
+template <>
+struct Operand<float> {
+  typedef f32x4 Frag;
+  static constexpr int kInner = 16, kTiles = 1;     // entries of the inner index; tiles of a product that make an operand
+  static __device__ __forceinline__ Frag load(const float* row, int j, int g) { return *(const f32x4*)(row + 16 * j + 4 * g); }
+  static __device__ __forceinline__ f32x4 mma(Frag a, Frag b, f32x4 c) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
+    return c;
+  }
+};
+template <>
+struct Operand<bf16_t> {
+  typedef bf16x8 Frag;
+  static constexpr int kInner = 32, kTiles = 2;
+  static __device__ __forceinline__ Frag load(const bf16_t* row, int j, int g) {
+    const bf16x4 lo = *(const bf16x4*)(row + 32 * j + 4 * g), hi = *(const bf16x4*)(row + 32 * j + 16 + 4 * g);
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+  static __device__ __forceinline__ f32x4 mma(Frag a, Frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+};
+// fp32 numbers of an operand as so many operands that add up to it.
+template <class Core, int N>
+__device__ __forceinline__ void pieces_of(const f32x4 (&x)[Operand<Core>::kTiles], typename Operand<Core>::Frag (&p)[N]) {
+  if constexpr (std::is_same_v<Core, float>) {
+    static_assert(N == 1);
+    p[0] = x[0];
+  } else {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        float left = x[t][r];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          p[i][4 * t + r] = (bf16_t)left;
+          if (i + 1 < N) left -= (float)p[i][4 * t + r];
+        }
+      }
+  }
+}
+
+// How a launch goes through the chunks.
+struct LinearChunks {
+  float* states;        // before each segment, `states_of` of da * dc for each sequence and head; null: one segment, from P.first
+  int64_t states_of;
+  double* totals;       // STATE: sums of the segments' logarithms (base 2), [batch * heads][segments]
+  int32_t segments, chunks;      // a segment has so many chunks
+  int32_t slices;
+  uint32_t blocks;
+  int32_t vec_a, vec_b, vec_c, vec_out;   // entries that a load or store takes
+};
+
+// One XCD's workgroups take neighbouring parts of the work: slices of the same head share their a and b in its L2.
+__device__ __forceinline__ uint32_t by_xcd(uint32_t block, uint32_t blocks) {
+  const uint32_t x = block & 7, each = blocks >> 3, more = blocks & 7;
+  return x * each + min(x, more) + (block >> 3);
+}
+
+template <class In, int V>
+__device__ __forceinline__ void load_entries(const In* p, int have, float (&x)[V], int vec) {
+  // (have: entries that are there; vec divides them or is 1)
+  if (vec * sizeof(In) == 16 && V * sizeof(In) == 16) {
+    if (have >= V) load_floats<In, V>(p, x);
+    else
+#pragma unroll
+      for (int i = 0; i < V; ++i) x[i] = 0.0f;
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < V; i += 2) {
+    if (vec >= 2) {
+      float two[2] = {0.0f, 0.0f};
+      if (i < have) load_floats<In, 2>(p + i, two);
+      x[i] = two[0];
+      x[i + 1] = two[1];
+    } else {
+      x[i] = i < have ? to_float(p[i]) : 0.0f;
+      x[i + 1] = i + 1 < have ? to_float(p[i + 1]) : 0.0f;
+    }
+  }
+}
+
+template <class Core, int DA>
+struct ChunkShared {
+  static constexpr int kPad = 16 / sizeof(Core);
+  static constexpr bool kTurned = sizeof(Core) == 2;      // b by columns as well
+  Core a[kChunk][DA + kPad], b[kChunk][DA + kPad];
+  Core c[kChunk][kLinearSlice + kPad];
+  Core turned[kTurned ? DA : 1][kTurned ? kChunk + kPad : 1];
+  float c_high[kChunk], c_low[kChunk], to_end[kChunk], dots[4][kChunk];
+};
+
+// 64 steps' rows of `dim` entries, zero where `time` says -1, W columns.
+template <class In, class Core, int W, int STRIDE, bool TURNED, class Time>
+__device__ __forceinline__ void stage(Core (&to)[kChunk][STRIDE], Core* turned, const In* from, int64_t step, int dim, int vec, Time time) {
+  constexpr int V = 8, R = TURNED ? 4 : 1, kUnits = kChunk / R * (W / V);
+  for (int u = threadIdx.x; u < kUnits; u += blockDim.x) {
+    const int col = u % (W / V) * V, row = u / (W / V) * R;
+    float x[R][V];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int64_t t = time(row + r);
+      if (t < 0) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[r][i] = 0.0f;
+      } else {
+        const In* p = from + t * step + col;
+        if constexpr (sizeof(In) == 2) {
+          load_entries<In, 8>(p, dim - col, x[r], vec);
+        } else {
+          float lo[4], hi[4];
+          load_entries<In, 4>(p, dim - col, lo, vec);
+          load_entries<In, 4>(p + 4, dim - col - 4, hi, vec);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            x[r][i] = lo[i];
+            x[r][4 + i] = hi[i];
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) store_floats<Core, 16 / sizeof(Core)>(&to[row + r][col], *(const float(*)[16 / sizeof(Core)])&x[r][0]);
+    if constexpr (sizeof(Core) == 4)
+#pragma unroll
+      for (int r = 0; r < R; ++r) store_floats<Core, 4>(&to[row + r][col + 4], *(const float(*)[4])&x[r][4]);
+    if constexpr (TURNED)
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const float four[4] = {x[0][i], x[1][i], x[2][i], x[3][i]};
+        store_floats<Core, 4>(turned + (int64_t)(col + i) * (kChunk + 8) + row, four);
+      }
+  }
+}
+
+// STATE: only the segments' own contributions to the state, and their logarithms' sums.
+template <class In, class Core, int DA, int N_OUT, int N_STATE, bool STATE>
+__global__ __launch_bounds__(256) void k_linear_chunks(LinearArgs A, LinearPass P, LinearChunks C) {
+  typedef Operand<Core> Op;
+  typedef typename Op::Frag Frag;
+  constexpr int kJ = DA / Op::kInner, kT = Op::kTiles, kS = kChunk / Op::kInner;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  ChunkShared<Core, DA>& S = *reinterpret_cast<ChunkShared<Core, DA>*>(lds);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4;
+  const uint32_t at = by_xcd(blockIdx.x, C.blocks);
+  const int slice = at % C.slices, segment = at / C.slices % C.segments;
+  const int64_t bh = at / C.slices / C.segments, b = bh / A.heads, len = steps_of(A, b), entries = (int64_t)P.da * P.dc;
+  const int h = (int)(bh % A.heads), col = slice * kLinearSlice + 16 * wave;     // the wave's first column
+  const In* pa = (const In*)P.a + b * P.a_seq + (h / P.a_share) * P.a_head;
+  const In* pb = (const In*)P.b + b * P.b_seq + (h / P.b_share) * P.b_head;
+  const In* pc = (const In*)P.c + b * P.c_seq + (h / P.c_share) * P.c_head + slice * kLinearSlice;
+  const In* px = (const In*)P.x + b * P.x_seq + (h / P.x_share) * P.x_head;
+  const int64_t out = b * P.out_seq + h * P.out_head;
+  const int64_t begin = (int64_t)segment * C.chunks * kChunk;
+  const int64_t end = segment + 1 == C.segments ? A.steps : begin + (int64_t)C.chunks * kChunk;
+  const int in_slice = min(P.dc - slice * kLinearSlice, kLinearSlice);
+
+  f32x4 state[kJ * kT];       // rows 16 j + 4 g + r of column `col + l`
+  const float* from = STATE ? nullptr : C.states ? C.states + (bh * C.states_of + segment) * entries : P.first ? P.first + bh * P.first_of * entries : nullptr;
+  const bool column = col + l < P.dc;
+#pragma unroll
+  for (int j = 0; j < kJ * kT; ++j)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int row = 16 * j + 4 * g + r;
+      state[j][r] = from && column && row < P.da ? from[(int64_t)row * P.state_a + (int64_t)(col + l) * P.state_c] : 0.0f;
+    }
+  const auto keep = [&](float* to, float w) {
+#pragma unroll
+    for (int j = 0; j < kJ * kT; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int row = 16 * j + 4 * g + r;
+        if (column && row < P.da) to[(int64_t)row * P.state_a + (int64_t)(col + l) * P.state_c] = state[j][r] * w;
+      }
+  };
+  double total = 0.0;
+
+  const int64_t inside = min(end, len);       // steps of the segment that are in the sequence end here
+  const int64_t chunks = inside > begin ? (inside - begin + kChunk - 1) / kChunk : 0;
+  for (int64_t i = 0; i < chunks; ++i) {
+    const int64_t t0 = begin + (P.back ? chunks - 1 - i : i) * kChunk;
+    const int there = (int)min((int64_t)kChunk, inside - t0);
+    const auto time = [&](int row) -> int64_t {       // of a row of the chunk, -1 behind the sequence
+      const int t = P.back ? kChunk - 1 - row : row;
+      return t < there ? t0 + t : -1;
+    };
+    if (!STATE && P.kept && t0 % kLinearSave == 0) keep(P.kept + (bh * P.kept_of + t0 / kLinearSave) * entries, 1.0f);
+    __syncthreads();
+    if (!STATE) stage<In, Core, DA, DA + ChunkShared<Core, DA>::kPad, false>(S.a, (Core*)nullptr, pa, P.a_step, P.da, C.vec_a, time);
+    stage<In, Core, DA, DA + ChunkShared<Core, DA>::kPad, ChunkShared<Core, DA>::kTurned>(S.b, &S.turned[0][0], pb, P.b_step, P.da, C.vec_b, time);
+    stage<In, Core, kLinearSlice, kLinearSlice + ChunkShared<Core, DA>::kPad, false>(S.c, (Core*)nullptr, pc, P.c_step, in_slice, C.vec_c, time);
+    if (wave == 0) {      // the logarithms' sums
+      const int64_t t = time(lane) + (P.back ? 1 : 0);
+      double x = 0.0;
+      if (time(lane) >= 0 && t < len) {
+        const float log = log_gate(A, b, t, h);
+        x = log < kLinearLeast ? (double)kLog2Least : (double)log * 1.4426950408889634;
+      }
+      for (int o = 1; o < 64; o <<= 1) {
+        const double y = __shfl_up(x, o);
+        if (lane >= o) x += y;
+      }
+      const double all = __shfl(x, 63);
+      S.c_high[lane] = (float)x;
+      S.c_low[lane] = (float)(x - (double)(float)x);
+      S.to_end[lane] = __builtin_amdgcn_exp2f((float)(all - x));
+      total += all;
+    }
+    __syncthreads();
+    Frag cf[kS];       // column l's entries, a lane's steps
+#pragma unroll
+    for (int s = 0; s < kS; ++s)
+#pragma unroll
+      for (int t = 0; t < kT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) cf[s][4 * t + r] = S.c[16 * (s * kT + t) + 4 * g + r][16 * wave + l];
+    if constexpr (!STATE) {
+      f32x4 y[4] = {};
+#pragma unroll
+      for (int j = 0; j < kJ; ++j) {
+        Frag p[N_OUT];
+        pieces_of<Core, N_OUT>(*(const f32x4(*)[kT])&state[j * kT], p);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const Frag q = Op::load(&S.a[16 * t + l][0], j, g);
+#pragma unroll
+          for (int n = N_OUT - 1; n >= 0; --n) y[t] = Op::mma(p[n], q, y[t]);
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const float high = S.c_high[16 * t + l], low = S.c_low[16 * t + l];
+        const float here = __builtin_amdgcn_exp2f(high + low);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) y[t][r] *= here;
+        Frag q[kJ];
+#pragma unroll
+        for (int j = 0; j < kJ; ++j) q[j] = Op::load(&S.a[16 * t + l][0], j, g);
+#pragma unroll
+        for (int s = 0; s < (t + kT) / kT; ++s) {
+          f32x4 w[kT];
+#pragma unroll
+          for (int u = 0; u < kT; ++u) {
+            const int from = s * kT + u;      // steps 16 from + 4 g + r
+            w[u] = f32x4{};
+            if (from > t) continue;
+#pragma unroll
+            for (int j = 0; j < kJ; ++j) w[u] = Op::mma(Op::load(&S.b[16 * from + l][0], j, g), q[j], w[u]);
+            const f32x4 high_s = *(const f32x4*)&S.c_high[16 * from + 4 * g], low_s = *(const f32x4*)&S.c_low[16 * from + 4 * g];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const float weighted = w[u][r] * __builtin_amdgcn_exp2f((high - high_s[r]) + (low - low_s[r]));
+              w[u][r] = from < t || 4 * g + r <= l ? weighted : 0.0f;
+            }
+          }
+          Frag p[N_OUT];
+          pieces_of<Core, N_OUT>(w, p);
+#pragma unroll
+          for (int n = N_OUT - 1; n >= 0; --n) y[t] = Op::mma(cf[s], p[n], y[t]);
+        }
+        // rows of the result: step 16 t + l, columns 4 g to 4 g + 3 of the wave's
+        const int64_t when = time(16 * t + l);
+        const int first = col + 4 * g;
+        if (when >= 0) {
+          const int64_t to = out + when * P.out_step + first;
+          if (C.vec_out == 4 && first < P.dc) {
+            const float x[4] = {y[t][0], y[t][1], y[t][2], y[t][3]};
+            if (P.wide) store_floats<float, 4>((float*)P.out + to, x);
+            else store_floats<In, 4>((In*)P.out + to, x);
+          } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (first + r < P.dc) store_result<In>(P, to + r, y[t][r]);
+          }
+        }
+        if (P.dots) {
+          float d = 0.0f;
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (when >= 0 && first + r < P.dc) d = fmaf(y[t][r], to_float(px[when * P.x_step + first + r]), d);
+          d += __shfl_xor(d, 16);
+          d += __shfl_xor(d, 32);
+          if (g == 0) S.dots[wave][16 * t + l] = d;
+        }
+      }
+      if (P.dots) {
+        __syncthreads();
+        if (wave == 0 && time(lane) >= 0) {
+          float d = S.dots[0][lane];
+          for (int w = 1; w < (int)(blockDim.x >> 6); ++w) d += S.dots[w][lane];
+          P.dots[((int64_t)slice * A.batch * A.heads + bh) * A.steps + time(lane)] = d;
+        }
+      }
+      if (i + 1 == chunks && (C.states || !P.last) && !P.kept) break;      // nobody reads the state
+    }
+    const float all = __builtin_amdgcn_exp2f(S.c_high[kChunk - 1] + S.c_low[kChunk - 1]);
+#pragma unroll
+    for (int j = 0; j < kJ * kT; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) state[j][r] *= all;
+#pragma unroll
+    for (int s = 0; s < kS; ++s) {
+      f32x4 w[kT];
+#pragma unroll
+      for (int t = 0; t < kT; ++t) {
+        const f32x4 left = *(const f32x4*)&S.to_end[16 * (s * kT + t) + 4 * g];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) w[t][r] = (float)cf[s][4 * t + r] * left[r];
+      }
+      Frag p[N_STATE];
+      pieces_of<Core, N_STATE>(w, p);
+#pragma unroll
+      for (int j = 0; j < kJ * kT; ++j) {
+        Frag rows;
+        if constexpr (ChunkShared<Core, DA>::kTurned) {
+          rows = Op::load(&S.turned[16 * j + l][0], s, g);
+        } else {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) rows[r] = S.b[16 * s + 4 * g + r][16 * j + l];
+        }
+#pragma unroll
+        for (int n = N_STATE - 1; n >= 0; --n) state[j] = Op::mma(rows, p[n], state[j]);
+      }
+    }
+  }
+  if constexpr (STATE) {
+    keep(C.states + (bh * C.states_of + segment) * entries, 1.0f);
+    if (slice == 0 && threadIdx.x == 0) C.totals[bh * C.segments + segment] = total;
+    return;
+  }
+  // zeros behind the sequence
+  const int64_t zero = max(begin, len);
+  const int width = in_slice;
+  for (int64_t e = threadIdx.x; e < (end - zero) * width; e += blockDim.x)
+    store_result<In>(P, out + (zero + e / width) * P.out_step + slice * kLinearSlice + e % width, 0.0f);
+  if (P.kept && (len == 0 ? segment == 0 : begin < len && len <= end))
+    keep(P.kept + (bh * P.kept_of + (len + kLinearSave - 1) / kLinearSave) * entries, 1.0f);
+  if (P.last && !C.states) keep(P.last + bh * entries, P.back && len > 0 ? linear_decay(log_gate(A, b, 0, h)) : 1.0f);
+}
+
+// From the segments' own contributions to the states before them, in place, and the last one.
+__global__ __launch_bounds__(256) void k_linear_scan(LinearArgs A, float* states, const double* totals, int segments, int64_t entries, const float* first,
+                                                     float* last, bool back) {
+  const int64_t each = (entries + 255) / 256, count = A.batch * A.heads * each;
+  for (int64_t block = blockIdx.x; block < count; block += gridDim.x) {
+    const int64_t bh = block / each, b = bh / A.heads, e = block % each * 256 + threadIdx.x;
+    if (e >= entries) continue;
+    float s = first ? first[bh * entries + e] : 0.0f;
+    float* p = states + bh * segments * entries + e;
+    for (int i = 0; i < segments; ++i) {
+      const int at = back ? segments - 1 - i : i;
+      const float own = p[at * entries];
+      p[at * entries] = s;
+      s = fmaf(s, __builtin_amdgcn_exp2f((float)totals[bh * segments + at]), own);
+    }
+    if (last) last[bh * entries + e] = back && steps_of(A, b) > 0 ? s * linear_decay(log_gate(A, b, 0, (int)(bh % A.heads))) : s;
+  }
 }
 
 // ---- the gates' gradient ----

@@ -62,20 +62,32 @@ bool linear_fits(const choco_linear_config& c) {
 }
 
 struct LinearLayout {
-  size_t later, dots, sums, wide, total;
+  size_t later, totals, dots, sums, wide, total;
 };
+void segments_of(const choco_linear_config& c, int32_t& segments, int32_t& chunks);
 LinearLayout linear_layout(const choco_linear_config& c, bool back) {
   LinearLayout L{};
   Parts parts;
-  if (c.batch == 0 || c.heads == 0 || !back) return L;
+  if (c.batch == 0 || c.heads == 0) return L;
   const size_t rows = (size_t)rows_of(c), state = (size_t)c.dim_k * c.dim_v, steps = (size_t)c.steps;
-  L.later = parts.take(rows * (size_t)pieces_of(c) * state * sizeof(float));
-  L.dots = parts.take(rows * steps * 2 * slices_of(c.dim_k) * sizeof(float));
-  L.sums = parts.take(rows * (size_t)pieces_of(c) * sizeof(float));
-  size_t most = 0;
-  if (c.q_heads != c.heads || c.k_heads != c.heads) most = c.dim_k;
-  if (c.v_heads != c.heads) most = std::max(most, (size_t)c.dim_v);
-  L.wide = parts.take(rows * steps * most * sizeof(float));
+  size_t segments = (size_t)pieces_of(c);
+  if (!back) {
+    int32_t count, each;
+    segments_of(c, count, each);
+    segments = (size_t)count;
+  }
+  if (segments > 1) {
+    L.later = parts.take(rows * segments * state * sizeof(float));
+    L.totals = parts.take(rows * segments * sizeof(double));
+  }
+  if (back) {
+    L.dots = parts.take(rows * steps * 2 * slices_of(c.dim_k) * sizeof(float));
+    L.sums = parts.take(rows * (size_t)pieces_of(c) * sizeof(float));
+    size_t most = 0;
+    if (c.q_heads != c.heads || c.k_heads != c.heads) most = c.dim_k;
+    if (c.v_heads != c.heads) most = std::max(most, (size_t)c.dim_v);
+    L.wide = parts.take(rows * steps * most * sizeof(float));
+  }
   L.total = parts.at;
   return L;
 }
@@ -116,8 +128,51 @@ LinearArgs linear_args(const choco_linear_config& c, const float* g, const int32
   return A;
 }
 
+// Entries of rows that a load or store takes: as many as `most`, two or one, as the rows are aligned.
+int width_of(const Rows& r, size_t size, int most, const choco_linear_config& c) {
+  for (int v = most; v > 1; v = v > 2 ? 2 : 1) {
+    const size_t bytes = v * size;
+    bool ok = r.dim % v == 0 && aligned_to(r.p, bytes);
+    const int64_t count[3] = {c.batch, c.steps, r.heads};
+    for (int i = 0; i < 3; ++i) ok = ok && (count[i] <= 1 || (size_t)r.stride[i] * size % bytes == 0);
+    if (ok) return v;
+  }
+  return 1;
+}
+
+// Up to so many steps are taken one by one.
+constexpr int64_t kStepByStep = 8;
+
+template <class In, class Core, int DA, int N_OUT, int N_STATE, bool STATE>
+int launch_chunks(const choco_linear_config& c, const LinearArgs& A, const LinearPass& P, LinearChunks C) {
+  const size_t lds = sizeof(ChunkShared<Core, DA>);
+  const auto kernel = k_linear_chunks<In, Core, DA, N_OUT, N_STATE, STATE>;
+  if (lds > 65536) {
+    static const hipError_t allowed = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    TRY_HIP(allowed);
+  }
+  C.slices = slices_of(P.dc);
+  C.blocks = (uint32_t)(rows_of(c) * C.segments * C.slices);
+  const int waves = std::min(4, (P.dc + 15) / 16);
+  kernel<<<dim3(C.blocks), 64 * waves, lds, (hipStream_t)c.stream>>>(A, P, C);
+  TRY_HIP(hipGetLastError());
+  return CHOCO_OK;
+}
+// N_OUT: bf16 numbers for one of fp32 where the result goes
+template <class In, int N_OUT, bool STATE>
+int run_chunks(const choco_linear_config& c, const LinearArgs& A, const LinearPass& P, const LinearChunks& C) {
+  const auto with_core = [&](auto dim) -> int {
+    constexpr int DA = decltype(dim)::value;
+    if constexpr (std::is_same_v<In, bf16_t>) return launch_chunks<In, bf16_t, DA, N_OUT, 3, STATE>(c, A, P, C);
+    else return launch_chunks<In, float, DA, 1, 1, STATE>(c, A, P, C);
+  };
+  if (P.da <= 64) return with_core(std::integral_constant<int, 64>{});
+  if (P.da <= 128) return with_core(std::integral_constant<int, 128>{});
+  return with_core(std::integral_constant<int, 256>{});
+}
+
 template <class T>
-int run_pass(const choco_linear_config& c, const LinearArgs& A, const LinearPass& P) {
+int run_steps(const choco_linear_config& c, const LinearArgs& A, const LinearPass& P) {
   const dim3 grid((uint32_t)(rows_of(c) * slices_of(P.dc)));
   const hipStream_t stream = (hipStream_t)c.stream;
   if (P.da <= 64) k_linear_steps<T, 16><<<grid, 256, 0, stream>>>(A, P);
@@ -125,6 +180,55 @@ int run_pass(const choco_linear_config& c, const LinearArgs& A, const LinearPass
   else k_linear_steps<T, 64><<<grid, 256, 0, stream>>>(A, P);
   TRY_HIP(hipGetLastError());
   return CHOCO_OK;
+}
+
+LinearChunks chunks_of(const choco_linear_config& c, const LinearPass& P, const Rows& a, const Rows& b, const Rows& v, const Rows& out) {
+  LinearChunks C{};
+  const size_t size = type_bytes(c.type);
+  C.segments = 1;
+  C.chunks = (int32_t)((c.steps + kChunk - 1) / kChunk);
+  C.vec_a = width_of(a, size, (int)(16 / size), c);
+  C.vec_b = width_of(b, size, (int)(16 / size), c);
+  C.vec_c = width_of(v, size, (int)(16 / size), c);
+  C.vec_out = width_of(out, P.wide ? 4 : size, 4, c);
+  return C;
+}
+
+// The states before all segments.
+template <class T>
+int run_states(const choco_linear_config& c, const LinearArgs& A, const LinearPass& P, const LinearChunks& C, const float* first, float* last) {
+  if (const int rc = run_chunks<T, 1, true>(c, A, P, C)) return rc;
+  const int64_t entries = (int64_t)P.da * P.dc;
+  const dim3 grid((uint32_t)std::min<int64_t>(65536, rows_of(c) * ((entries + 255) / 256)));
+  k_linear_scan<<<grid, 256, 0, (hipStream_t)c.stream>>>(A, C.states, C.totals, C.segments, entries, first, last, P.back);
+  TRY_HIP(hipGetLastError());
+  return CHOCO_OK;
+}
+
+// Segments of a forward pass in chunks: as many as give so many workgroups, none shorter than kLinearSave steps.
+constexpr int64_t kWorkgroups = 1024;
+void segments_of(const choco_linear_config& c, int32_t& segments, int32_t& chunks) {
+  const int64_t all = (c.steps + kChunk - 1) / kChunk, alone = rows_of(c) * slices_of(c.dim_v), least = kLinearSave / kChunk;
+  int64_t each = std::max(all, least);
+  if (alone < kWorkgroups / 2 && all > least) each = std::max(least, (all * alone + kWorkgroups - 1) / kWorkgroups);
+  each = (each + least - 1) / least * least;
+  chunks = (int32_t)each;
+  segments = (int32_t)std::max<int64_t>(1, (all + each - 1) / each);
+}
+
+template <class T>
+int run_forward(const choco_linear_config& c, const LinearArgs& A, LinearPass P, const Rows& q, const Rows& k, const Rows& v, const Rows& y, char* ws) {
+  if (c.steps <= kStepByStep) return run_steps<T>(c, A, P);
+  LinearChunks C = chunks_of(c, P, q, k, v, y);
+  segments_of(c, C.segments, C.chunks);
+  if (C.segments > 1) {
+    const LinearLayout L = linear_layout(c, false);
+    C.states = (float*)(ws + L.later);
+    C.totals = (double*)(ws + L.totals);
+    C.states_of = C.segments;
+    if (const int rc = run_states<T>(c, A, P, C, P.first, P.last)) return rc;
+  }
+  return run_chunks<T, 2, false>(c, A, P, C);
 }
 
 template <class T>
@@ -138,30 +242,63 @@ int run_backward(const choco_linear_config& c, const LinearArgs& A, const void* 
   float* const later = (float*)(ws + L.later);
   float* const q_dots = (float*)(ws + L.dots);
   float* const k_dots = q_dots + rows * c.steps * slices_of(c.dim_k);
-  // a gradient of heads that share one: of every head to the workspace, then added up
-  const auto through = [&](LinearPass P, int32_t heads, int32_t dim) -> int {
-    if (heads == c.heads) return run_pass<T>(c, A, P);
-    LinearPass W = P;
-    W.out = ws + L.wide;
-    W.wide = true;
-    W.out_head = dim;
-    W.out_step = (int64_t)c.heads * dim;
-    W.out_seq = W.out_step * c.steps;
-    if (const int rc = run_pass<T>(c, A, W)) return rc;
+  const bool stepwise = c.steps <= kStepByStep, several = pieces > 1;
+  // a pass on its own arrays; a gradient of heads that share one: of every head to the workspace, then added up
+  const auto through = [&](LinearPass P, const Rows& ra, const Rows& rb, const Rows& rc_, Rows out, const float* states, int64_t states_of) -> int {
+    const LinearPass given = P;
+    const int32_t heads = out.heads, dim = out.dim;
+    const int64_t wide_stride[3] = {(int64_t)c.heads * dim * c.steps, (int64_t)c.heads * dim, dim};
+    if (heads != c.heads) {
+      P.out = ws + L.wide;
+      P.wide = true;
+      P.out_seq = wide_stride[0];
+      P.out_step = wide_stride[1];
+      P.out_head = wide_stride[2];
+      out = Rows{P.out, wide_stride, c.heads, dim};
+    }
+    if (stepwise) {
+      if (const int rc = run_steps<T>(c, A, P)) return rc;
+    } else {
+      LinearChunks C = chunks_of(c, P, ra, rb, rc_, out);
+      C.segments = (int32_t)pieces;
+      C.chunks = kLinearSave / kChunk;
+      if (several) {
+        C.states = const_cast<float*>(states);
+        C.states_of = states_of;
+      }
+      if (const int rc = P.dots ? run_chunks<T, 3, false>(c, A, P, C) : run_chunks<T, 2, false>(c, A, P, C)) return rc;
+    }
+    if (heads == c.heads) return CHOCO_OK;
     const int64_t count = c.batch * c.steps * heads * dim;
     if (count == 0) return CHOCO_OK;
     k_linear_share<T><<<dim3((uint32_t)std::min<int64_t>(4096, (count + 255) / 256)), 256, 0, stream>>>(
-        (const float*)W.out, P.out, c.batch * c.steps, c.steps, heads, c.heads / heads, dim, P.out_seq, P.out_step, P.out_head);
+        (const float*)P.out, given.out, c.batch * c.steps, c.steps, heads, c.heads / heads, dim, given.out_seq, given.out_step, given.out_head);
     TRY_HIP(hipGetLastError());
     return CHOCO_OK;
   };
+  const Rows DQ{dq, c.dq_stride, c.q_heads, c.dim_k}, DK{dk, c.dk_stride, c.k_heads, c.dim_k}, DV{dv, c.dv_stride, c.v_heads, c.dim_v};
   LinearPass P = pass_of(c, Y, V, K, dq, c.dq_stride);
   state_of(c, true, P);
-  P.first = saved;      // (with its own distance from one sequence's to the next)
+  P.first = saved;
+  P.first_of = pieces + 1;
   P.x = q; P.x_seq = c.q_stride[0]; P.x_step = c.q_stride[1]; P.x_head = c.q_stride[2]; P.x_share = c.heads / c.q_heads;
   P.dots = dg ? q_dots : nullptr;
-  P.first_of = pieces + 1;
-  if (const int rc = through(P, c.q_heads, c.dim_k)) return rc;
+  if (const int rc = through(P, Y, V, K, DQ, saved, pieces + 1)) return rc;
+  LinearPass last = pass_of(c, K, Q, Y, dv, c.dv_stride);
+  state_of(c, false, last);
+  last.back = true;
+  last.first = dlast;
+  last.first_of = 1;
+  last.last = dh0;
+  if (!stepwise && several) {
+    LinearChunks C = chunks_of(c, last, K, Q, Y, DV);
+    C.segments = (int32_t)pieces;
+    C.chunks = kLinearSave / kChunk;
+    C.states = later;
+    C.states_of = pieces;
+    C.totals = (double*)(ws + L.totals);
+    if (const int rc = run_states<T>(c, A, last, C, dlast, dh0)) return rc;
+  }
   P = pass_of(c, V, Y, Q, dk, c.dk_stride);
   state_of(c, true, P);
   P.back = true;
@@ -169,16 +306,8 @@ int run_backward(const choco_linear_config& c, const LinearArgs& A, const void* 
   P.first_of = 1;
   P.x = k; P.x_seq = c.k_stride[0]; P.x_step = c.k_stride[1]; P.x_head = c.k_stride[2]; P.x_share = c.heads / c.k_heads;
   P.dots = dg ? k_dots : nullptr;
-  if (const int rc = through(P, c.k_heads, c.dim_k)) return rc;
-  P = pass_of(c, K, Q, Y, dv, c.dv_stride);
-  state_of(c, false, P);
-  P.back = true;
-  P.first = dlast;
-  P.first_of = 1;
-  P.last = dh0;
-  P.kept = dg ? later : nullptr;
-  P.kept_of = pieces;
-  if (const int rc = through(P, c.v_heads, c.dim_v)) return rc;
+  if (const int rc = through(P, V, Y, Q, DK, later, pieces)) return rc;
+  if (const int rc = through(last, K, Q, Y, DV, later, pieces)) return rc;
   if (!dg) return CHOCO_OK;
   LinearGates G{};
   G.q_dots = q_dots; G.k_dots = k_dots;
@@ -242,8 +371,9 @@ int choco_linear_forward(const choco_linear_config* cfg, const void* q_dev, cons
   if (L.total > 0 && (!workspace_dev || !aligned_to(workspace_dev, 16))) return CHOCO_E_INVAL;
   if (L.total > workspace_bytes) return CHOCO_E_NOMEM;
   const LinearArgs A = linear_args(c, g_dev, lengths_dev);
-  LinearPass P = pass_of(c, {q_dev, c.q_stride, c.q_heads, c.dim_k}, {k_dev, c.k_stride, c.k_heads, c.dim_k},
-                         {v_dev, c.v_stride, c.v_heads, c.dim_v}, y_dev, c.y_stride);
+  const Rows q{q_dev, c.q_stride, c.q_heads, c.dim_k}, k{k_dev, c.k_stride, c.k_heads, c.dim_k}, v{v_dev, c.v_stride, c.v_heads, c.dim_v},
+      y{y_dev, c.y_stride, c.heads, c.dim_v};
+  LinearPass P = pass_of(c, q, k, v, y_dev, c.y_stride);
   state_of(c, false, P);
   P.first = h0_dev;
   P.first_of = 1;
@@ -251,7 +381,7 @@ int choco_linear_forward(const choco_linear_config* cfg, const void* q_dev, cons
   P.kept = saved_dev;
   P.kept_of = pieces_of(c) + 1;
   int rc = CHOCO_OK;
-  with_type(c.type, [&](auto x) { rc = run_pass<decltype(x)>(c, A, P); });
+  with_type(c.type, [&](auto x) { rc = run_forward<decltype(x)>(c, A, P, q, k, v, y, (char*)workspace_dev); });
   return rc;
 }
 

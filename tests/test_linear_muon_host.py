@@ -99,6 +99,9 @@ def test_linear_attention_refuses_what_no_launch_holds():
 def test_linear_attention_with_nothing_to_do():
     assert linear_codes(linear_cfg(batch=0)) == (B.OK, B.OK)
     assert linear_codes(linear_cfg(heads=0)) == (B.OK, B.OK)
+    out = ctypes.c_size_t()
+    for back in (0, 1):
+        assert T.lib().choco_linear_workspace_bytes(ctypes.byref(linear_cfg(steps=0)), back, ctypes.byref(out)) == B.OK
 
 
 def test_linear_attention_checks_its_tensors():
