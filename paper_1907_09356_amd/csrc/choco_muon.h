@@ -17,8 +17,7 @@ namespace choco {
 
 constexpr float kMuonA = 3.4445f, kMuonB = -4.7750f, kMuonC = 2.0315f;
 constexpr float kMuonUp = 8192.0f, kMuonDown = 1.0f / 8192.0f;
-constexpr int kMuonPad = 64;      // rows of operands end on a multiple of so many entries, with zeros
-constexpr int kMuonTile = 64;     // of what a workgroup makes
+constexpr int kMuonPad = 32;      // rows of operands end on a multiple of so many entries, with zeros: a step along the inner index
 constexpr int kMuonMost = 1 << 16;
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
@@ -76,16 +75,27 @@ __device__ __forceinline__ MuonPlanes planes_of(const MuonArgs& A, const MuonSha
   return P;
 }
 
-// Which matrices a tile belongs to: the last whose tiles begin at or before it.
-__device__ __forceinline__ MuonShape shape_of(const MuonArgs& A, uint32_t tile, uint32_t MuonShape::*begin) {
+// Which matrices a tile belongs to: the last whose tiles begin at or before it.  (The table is read as constant memory, so that what
+// comes of it stays in scalar registers.)
+typedef const __attribute__((address_space(4))) uint32_t ConstantWord;
+static_assert(sizeof(MuonShape) % 4 == 0);
+__device__ __forceinline__ MuonShape shape_at(const MuonArgs& A, int i) {
+  struct Words { uint32_t w[sizeof(MuonShape) / 4]; } words;
+  ConstantWord* from = (ConstantWord*)(uintptr_t)(A.table + i);
+#pragma unroll
+  for (size_t k = 0; k < sizeof(MuonShape) / 4; ++k) words.w[k] = from[k];
+  return __builtin_bit_cast(MuonShape, words);
+}
+template <uint32_t MuonShape::*BEGIN>
+__device__ __forceinline__ MuonShape shape_of(const MuonArgs& A, uint32_t tile) {
   if (!A.table) return A.one;
   int lo = 0, hi = A.count - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) / 2;
-    if (A.table[mid].*begin <= tile) lo = mid;
+    if (shape_at(A, mid).*BEGIN <= tile) lo = mid;
     else hi = mid - 1;
   }
-  return A.table[lo];
+  return shape_at(A, lo);
 }
 
 __device__ __forceinline__ void split(float x, f16_t& high, f16_t& low) {
@@ -111,7 +121,7 @@ __device__ __forceinline__ float source_entry(const MuonArgs& A, const MuonShape
 template <class T, bool STEP>
 __global__ __launch_bounds__(256) void k_muon_squares(MuonArgs A) {
   __shared__ double part[4];
-  const MuonShape S = shape_of(A, blockIdx.x, &MuonShape::start_begin);
+  const MuonShape S = shape_of<&MuonShape::start_begin>(A, blockIdx.x);
   const MuonTile M = start_tile(S);
   const int worker = S.first + M.i;
   const float scale = STEP && A.grad_scale ? A.grad_scale[worker] : 1.0f;
@@ -144,7 +154,7 @@ template <class T, bool STEP>
 __global__ __launch_bounds__(256) void k_muon_start(MuonArgs A) {
   __shared__ float tile[64][65];
   __shared__ double part[4];
-  const MuonShape S = shape_of(A, blockIdx.x, &MuonShape::start_begin);
+  const MuonShape S = shape_of<&MuonShape::start_begin>(A, blockIdx.x);
   const MuonTile M = start_tile(S);
   const int worker = S.first + M.i;
   const float scale = STEP && A.grad_scale ? A.grad_scale[worker] : 1.0f;
@@ -179,13 +189,13 @@ __global__ __launch_bounds__(256) void k_muon_start(MuonArgs A) {
   for (int j = threadIdx.x >> 6; j < 64; j += 4) {
     const int e = threadIdx.x & 63;
     f16_t high, low;
-    if (M.row + j < S.rows) {
+    if (M.row + j < S.rows && M.col + e < along_ld) {
       split(tile[j][e], high, low);
       f16_t* to = along + (M.row + j) * along_ld + M.col + e;
       to[0] = high;
       to[along_low] = low;
     }
-    if (M.col + j < S.cols) {
+    if (M.col + j < S.cols && M.row + e < across_ld) {
       split(tile[e][j], high, low);
       f16_t* to = across + (M.col + j) * across_ld + M.row + e;
       to[0] = high;
@@ -205,115 +215,169 @@ __device__ __forceinline__ void triangle(uint32_t at, uint32_t& i, uint32_t& j) 
   j = at - i * (i + 1) / 2;
 }
 
-template <int KIND>
-__global__ __launch_bounds__(256) void k_muon_product(MuonArgs A) {
+// 16 bytes for each lane of a wave, straight into LDS, where the lanes' lie one behind the other.
+__device__ __forceinline__ void to_lds(const void* from, void* to) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
+
+// A workgroup makes a tile of TILE x TILE entries, a wave a quarter.  A step along the inner index takes 32 entries of TILE rows of both
+// operands, high and low, into one of two buffers while the other one's are multiplied.  In a buffer a row's four 16-byte
+// parts are exchanged by bits 2 and 3 of its number, so that 16 lanes that read one part of 16 rows meet 16 different banks.
+template <int KIND, int TILE>
+__global__ __launch_bounds__(256, 2) void k_muon_product(MuonArgs A) {
+  constexpr int W = TILE / 32;      // 16-row parts of a wave's side
+  constexpr int kLoads = TILE / 16; // of a wave, a step
+  __shared__ __attribute__((aligned(1024))) f16_t lds[2][4][TILE][32];    // left high, left low, right high, right low
   constexpr uint32_t MuonShape::*kBegin = KIND == kApply ? &MuonShape::apply_begin : &MuonShape::gram_begin;
-  const MuonShape S = shape_of(A, blockIdx.x, kBegin);
+  const MuonShape S = shape_of<kBegin>(A, blockIdx.x);
   const uint32_t at = blockIdx.x - S.*kBegin, tiles = KIND == kApply ? S.apply_tiles : S.gram_tiles, in = at % tiles;
   const int which = (int)(at / tiles);
   const MuonPlanes P = planes_of(A, S, which);
   uint32_t ti, tj;
   if (KIND == kApply) {
-    const uint32_t high = (S.a + kMuonTile - 1) / kMuonTile;
+    const uint32_t high = (S.a + TILE - 1) / TILE;
     ti = in % high;
     tj = in / high;
   } else {
     triangle(in, ti, tj);
   }
-  // (rows of n: the other operand's)
   const f16_t *left = KIND == kGram ? P.x : KIND == kSquare ? P.p : P.q, *right = KIND == kApply ? P.xt[A.now] : left;
   const int64_t left_low = KIND == kGram ? P.x_low : P.p_low, right_low = KIND == kApply ? P.xt_low : left_low;
   const int64_t ld = KIND == kGram ? S.b_ld : S.a_ld;
   const int ms = S.a, ns = KIND == kApply ? S.b : S.a;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4;
-  const int m0 = ti * kMuonTile + (wave & 1) * 32, n0 = tj * kMuonTile + (wave >> 1) * 32;
-  float4_t acc[2][2] = {};
-  const f16_t *pl[2], *pr[2];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4;
+  const int m0 = ti * TILE, n0 = tj * TILE, mw = (wave & 1) * (TILE / 2), nw = (wave >> 1) * (TILE / 2);
+
+  // what a lane loads each step: wave w plane w's rows, 16 a load
+  const f16_t* from = (wave < 2 ? left : right) + (wave & 1) * (wave < 2 ? left_low : right_low);
+  const int first = wave < 2 ? m0 : n0, rows = wave < 2 ? ms : ns;
+  const f16_t* source[kLoads];
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    pl[i] = left + (int64_t)min(m0 + 16 * i + l, ms - 1) * ld + 8 * g;
-    pr[i] = right + (int64_t)min(n0 + 16 * i + l, ns - 1) * ld + 8 * g;
+  for (int i = 0; i < kLoads; ++i) {
+    const int row = 16 * i + (lane >> 2), part = (lane & 3) ^ ((row >> 2) & 3);
+    source[i] = from + (int64_t)min(first + row, rows - 1) * ld + 8 * part;
   }
-  for (int64_t k = 0; k < ld; k += 32) {
-    half8 lh[2], ll[2], rh[2], rl[2];
+  const auto load = [&](int64_t k, int buffer) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      lh[i] = *(const half8*)(pl[i] + k);
-      ll[i] = *(const half8*)(pl[i] + left_low + k);
-      rh[i] = *(const half8*)(pr[i] + k);
-      rl[i] = *(const half8*)(pr[i] + right_low + k);
+    for (int i = 0; i < kLoads; ++i) to_lds(source[i] + k, &lds[buffer][wave][16 * i][0]);
+  };
+  const int swap = 8 * (g ^ ((l >> 2) & 3));
+  float4_t acc[W][W] = {};
+  load(0, 0);
+  for (int64_t k = 0; k < ld; k += 32) {
+    const int buffer = (k >> 5) & 1;
+    // this step's parts are there for everybody, and everybody is done with the other buffer
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    half8 f[4][W];
+#pragma unroll
+    for (int p = 0; p < 4; ++p)
+#pragma unroll
+      for (int i = 0; i < W; ++i) f[p][i] = *(const half8*)&lds[buffer][p][(p < 2 ? mw : nw) + 16 * i + l][swap];
+    if (k + 32 < ld) load(k + 32, buffer ^ 1);
+#pragma unroll
+    for (int i = 0; i < W; ++i)
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[1][i], f[2][j], acc[i][j], 0, 0, 0);
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[0][i], f[3][j], acc[i][j], 0, 0, 0);
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[0][i], f[2][j], acc[i][j], 0, 0, 0);
+      }
+  }
+  // The tile in LDS, fp32, columns exchanged by the rows' number so that reading down a column meets all banks, then out of it by
+  // rows and by columns, 8 entries a lane.
+  __syncthreads();
+  float* const tile = (float*)&lds[0][0][0][0];
+  static_assert(sizeof(lds) >= TILE * TILE * sizeof(float));
+  const auto place = [](int m, int n) { return m * TILE + (n ^ ((m >> 1) & (TILE / 2 - 4))); };
+#pragma unroll
+  for (int i = 0; i < W; ++i)
+#pragma unroll
+    for (int j = 0; j < W; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) tile[place(mw + 16 * i + 4 * g + r, nw + 16 * j + l)] = acc[i][j][r] * (KIND == kSquare ? kMuonDown * kMuonC : kMuonDown);
+  __syncthreads();
+  constexpr int kParts = TILE / 8;
+  constexpr bool kAdds = KIND != kGram;     // a X or b P
+  const bool last = KIND == kApply && A.last;
+  f16_t* const own = KIND == kApply ? P.x : P.p;
+  f16_t* const made = KIND == kApply ? P.x : KIND == kGram ? P.p : P.q;
+  f16_t* const turned = KIND == kApply ? P.xt[A.now ^ 1] : made;
+  const int64_t low = KIND == kApply ? P.x_low : P.p_low, turned_low = KIND == kApply ? P.xt_low : P.p_low;
+  const int n_ld = KIND == kApply ? S.b_ld : S.a_ld;
+  const int worker = S.first + which;
+  const bool tall = S.rows > S.cols;
+  const bool skip = last && A.moments && A.grad_scale && !__builtin_isfinite(A.grad_scale[worker]);
+  const auto finish = [&](int m, int n, const float (&x)[8], int count) {      // `count` entries of a row of memory
+    float* to = A.target + S.target + which * S.target_of + (int64_t)(tall ? n : m) * S.target_ld + (tall ? m : n);
+    if (skip) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < count) {
+        const float o = x[e] * kMuonDown;
+        to[e] = A.moments ? to[e] * (1.0f - A.lr * S.decay) - A.lr * S.rate * o : o;
+      }
+  };
+  for (int u = threadIdx.x; u < TILE * kParts; u += 256) {
+    const int i = u / kParts, j = u % kParts * 8, m = m0 + i, n = n0 + j;
+    if (m >= ms || n >= n_ld) continue;
+    float x[8];
+    *(float4_t*)&x[0] = *(const float4_t*)&tile[place(i, j)];
+    *(float4_t*)&x[4] = *(const float4_t*)&tile[place(i, j + 4)];
+    if (KIND != kApply && ti == tj) {     // the lower triangle's mirror image here too: a matrix's bits do not depend on the tiles' size
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (j + e > i) x[e] = tile[place(j + e, i)];
+    }
+    const int64_t at_row = (int64_t)m * n_ld + n;
+    if (kAdds) {
+      const half8 high = *(const half8*)(own + at_row), less = *(const half8*)(own + at_row + low);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] += (KIND == kApply ? kMuonA : kMuonB) * ((float)high[e] + (float)less[e]);
     }
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int e = 0; e < 8; ++e)
+      if (n + e >= ns) x[e] = 0.0f;
+    if (last && !tall) {
+      finish(m, n, x, ns - n);
+      continue;
+    }
+    if (kAdds && (KIND == kApply || ti != tj)) {
+      *(float4_t*)&tile[place(i, j)] = *(const float4_t*)&x[0];
+      *(float4_t*)&tile[place(i, j + 4)] = *(const float4_t*)&x[4];
+    }
+    if (last) continue;
+    half8 high, less;
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ll[i], rh[j], acc[i][j], 0, 0, 0);
-        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lh[i], rl[j], acc[i][j], 0, 0, 0);
-        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lh[i], rh[j], acc[i][j], 0, 0, 0);
-      }
+    for (int e = 0; e < 8; ++e) {
+      high[e] = (f16_t)x[e];
+      less[e] = (f16_t)(x[e] - (float)high[e]);
+    }
+    *(half8*)(made + at_row) = high;
+    *(half8*)(made + at_row + low) = less;
   }
-  const int worker = S.first + which;
-  const bool skip = A.moments && A.grad_scale && !__builtin_isfinite(A.grad_scale[worker]);
-  const bool tall = S.rows > S.cols;
+  if (KIND == kApply ? last && !tall : ti == tj) return;
+  __syncthreads();
+  for (int u = threadIdx.x; u < TILE * kParts; u += 256) {
+    const int j = u / kParts, i = u % kParts * 8, m = m0 + i, n = n0 + j;
+    if (n >= ns || m >= S.a_ld) continue;
+    float x[8];
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+    for (int e = 0; e < 8; ++e) x[e] = m + e < ms ? tile[place(i + e, j)] : 0.0f;
+    if (last) {
+      finish(m, n, x, ms - m);
+      continue;
+    }
+    half8 high, less;
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int m = m0 + 16 * i + 4 * g + r, n = n0 + 16 * j + l;
-        if (KIND != kApply) {
-          float x = 0.0f;       // behind a row, for sums over whole rows
-          if (m < ms && n < ns) {
-            x = acc[i][j][r] * kMuonDown;
-            if (KIND == kSquare) {
-              const f16_t* p = P.p + (int64_t)m * ld + n;
-              x = kMuonC * x + kMuonB * ((float)p[0] + (float)p[P.p_low]);
-            }
-          }
-          f16_t high, low;
-          split(x, high, low);
-          f16_t* const made = KIND == kGram ? P.p : P.q;
-          if (m < ms && n < S.a_ld) {
-            f16_t* to = made + (int64_t)m * S.a_ld + n;
-            to[0] = high;
-            to[P.p_low] = low;
-          }
-          if (ti != tj && n < ns && m < S.a_ld) {     // and its mirror image
-            f16_t* to = made + (int64_t)n * S.a_ld + m;
-            to[0] = high;
-            to[P.p_low] = low;
-          }
-          continue;
-        }
-        if (A.last) {
-          if (m >= ms || n >= ns || skip) continue;
-          const f16_t* p = P.xt[A.now] + (int64_t)n * S.a_ld + m;
-          const float x = kMuonDown * (acc[i][j][r] * kMuonDown + kMuonA * ((float)p[0] + (float)p[P.xt_low]));
-          float* to = A.target + S.target + which * S.target_of + (int64_t)(tall ? n : m) * S.target_ld + (tall ? m : n);
-          if (A.moments) *to = *to * (1.0f - A.lr * S.decay) - A.lr * S.rate * x;
-          else *to = x;
-          continue;
-        }
-        // X and X^T, zeros behind their rows
-        float x = 0.0f;
-        if (m < ms && n < ns) {
-          const f16_t* p = P.xt[A.now] + (int64_t)n * S.a_ld + m;
-          x = acc[i][j][r] * kMuonDown + kMuonA * ((float)p[0] + (float)p[P.xt_low]);
-        }
-        f16_t high, low;
-        split(x, high, low);
-        if (m < ms && n < S.b_ld) {
-          f16_t* to = P.x + (int64_t)m * S.b_ld + n;
-          to[0] = high;
-          to[P.x_low] = low;
-        }
-        if (n < ns && m < S.a_ld) {
-          f16_t* to = P.xt[A.now ^ 1] + (int64_t)n * S.a_ld + m;
-          to[0] = high;
-          to[P.xt_low] = low;
-        }
-      }
+    for (int e = 0; e < 8; ++e) {
+      high[e] = (f16_t)x[e];
+      less[e] = (f16_t)(x[e] - (float)high[e]);
+    }
+    f16_t* to = turned + (int64_t)n * S.a_ld + m;
+    *(half8*)to = high;
+    *(half8*)(to + turned_low) = less;
+  }
 }
 
 }  // namespace choco

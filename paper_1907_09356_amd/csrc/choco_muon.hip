@@ -18,14 +18,16 @@ using namespace choco;
 namespace {
 
 constexpr int kMostIterations = 32;
+// Tiles of 128 x 128 entries where there are at least so many (of the largest product) to fill the card with, else of 64 x 64.
+constexpr double kFewTiles = 384;
 // Matrices that a step takes at once: operands of so many bytes, or one matrix.
 constexpr int64_t kRoundBytes = (int64_t)1 << 30;
 
 int64_t padded(int64_t n) { return (n + kMuonPad - 1) / kMuonPad * kMuonPad; }
-int64_t tiles_of(int64_t n) { return (n + kMuonTile - 1) / kMuonTile; }
+int64_t tiles_of(int64_t n, int tile) { return (n + tile - 1) / tile; }
 
 // A shape's sides, operands and tiles; `count` and what is behind the begins are the caller's.
-MuonShape shape_from(int64_t rows, int64_t cols) {
+MuonShape shape_from(int64_t rows, int64_t cols, int tile) {
   MuonShape S{};
   S.rows = (int32_t)rows;
   S.cols = (int32_t)cols;
@@ -35,9 +37,9 @@ MuonShape shape_from(int64_t rows, int64_t cols) {
   S.b_ld = (int32_t)padded(S.b);
   S.scratch_of = (muon_scratch(S.a, S.b, S.a_ld, S.b_ld) + 255) / 256 * 256;
   S.start_tiles = (uint32_t)(((rows + 63) / 64) * ((cols + 63) / 64));
-  const int64_t high = tiles_of(S.a);
+  const int64_t high = tiles_of(S.a, tile);
   S.gram_tiles = (uint32_t)(high * (high + 1) / 2);
-  S.apply_tiles = (uint32_t)(high * tiles_of(S.b));
+  S.apply_tiles = (uint32_t)(high * tiles_of(S.b, tile));
   return S;
 }
 
@@ -47,7 +49,7 @@ struct Round {
   uint32_t start_tiles, gram_tiles, apply_tiles;
 };
 
-template <class T, bool STEP>
+template <class T, bool STEP, int TILE>
 int run_round(MuonArgs A, const Round& R, int iterations, hipStream_t stream) {
   k_muon_squares<T, STEP><<<dim3(R.start_tiles), 256, 0, stream>>>(A);
   TRY_HIP(hipGetLastError());
@@ -56,14 +58,18 @@ int run_round(MuonArgs A, const Round& R, int iterations, hipStream_t stream) {
   for (int i = 0; i < iterations; ++i) {
     A.now = i & 1;
     A.last = i + 1 == iterations;
-    k_muon_product<kGram><<<dim3(R.gram_tiles), 256, 0, stream>>>(A);
+    k_muon_product<kGram, TILE><<<dim3(R.gram_tiles), 256, 0, stream>>>(A);
     TRY_HIP(hipGetLastError());
-    k_muon_product<kSquare><<<dim3(R.gram_tiles), 256, 0, stream>>>(A);
+    k_muon_product<kSquare, TILE><<<dim3(R.gram_tiles), 256, 0, stream>>>(A);
     TRY_HIP(hipGetLastError());
-    k_muon_product<kApply><<<dim3(R.apply_tiles), 256, 0, stream>>>(A);
+    k_muon_product<kApply, TILE><<<dim3(R.apply_tiles), 256, 0, stream>>>(A);
     TRY_HIP(hipGetLastError());
   }
   return CHOCO_OK;
+}
+template <class T, bool STEP>
+int run_round(const MuonArgs& A, const Round& R, int iterations, int tile, hipStream_t stream) {
+  return tile == 128 ? run_round<T, STEP, 128>(A, R, iterations, stream) : run_round<T, STEP, 64>(A, R, iterations, stream);
 }
 
 // ---- a stack of matrices ----
@@ -86,13 +92,16 @@ int check_orthogonalize(const choco_orthogonalize_config* c) {
 
 struct StackLayout {
   MuonShape shape;
+  int tile;
   int64_t each;       // matrices taken at once
   size_t partials, scratch, total;
 };
 int stack_layout(const choco_orthogonalize_config& c, StackLayout& L) {
   L = {};
   if (c.batch == 0 || c.rows == 0 || c.cols == 0) return CHOCO_OK;
-  L.shape = shape_from(c.rows, c.cols);
+  L.tile = 128;
+  L.shape = shape_from(c.rows, c.cols, L.tile);
+  if ((double)L.shape.apply_tiles * (double)c.batch < kFewTiles) L.shape = shape_from(c.rows, c.cols, L.tile = 64);
   const double most = std::max<double>(L.shape.start_tiles, std::max(L.shape.gram_tiles, L.shape.apply_tiles));
   if (!launch_fits(most, 256)) return CHOCO_E_UNSUPPORTED;
   L.each = std::min<int64_t>(c.batch, std::max<int64_t>(1, kRoundBytes / L.shape.scratch_of));
@@ -129,6 +138,7 @@ int check_muon(const choco_muon_config* c) {
 }
 
 struct MuonLayout {
+  int tile;
   size_t state_end, table, partials, scratch, total;
 };
 // The matrices in rounds, and the workspace.  CHOCO_E_UNSUPPORTED: one that no launch holds.
@@ -136,6 +146,10 @@ int muon_layout(const choco_muon_config& c, std::vector<MuonShape>& table, std::
   const int64_t ld = resolve_ld(c);
   int64_t moment = 0, most_scratch = 0, most_partials = 0, scratch = 0, partials = 0;
   Round now{};
+  double tiles_in_all = 0.0;
+  for (int32_t t = 0; t < c.ntensors; ++t)
+    if (c.rows_host[t] > 0 && c.cols_host[t] > 0) tiles_in_all += (double)c.n * shape_from(c.rows_host[t], c.cols_host[t], 128).apply_tiles;
+  L.tile = tiles_in_all < kFewTiles ? 64 : 128;
   const auto close = [&] {
     if (now.count > 0) rounds.push_back(now);
     now = {};
@@ -145,7 +159,7 @@ int muon_layout(const choco_muon_config& c, std::vector<MuonShape>& table, std::
   for (int32_t t = 0; t < c.ntensors; ++t) {
     const int64_t rows = c.rows_host[t], cols = c.cols_host[t], start = c.start_host[t];
     if (rows == 0 || cols == 0) continue;
-    MuonShape S = shape_from(rows, cols);
+    MuonShape S = shape_from(rows, cols, L.tile);
     S.source = S.target = start;
     S.source_of = S.target_of = ld;
     S.source_ld = S.target_ld = cols;
@@ -247,7 +261,7 @@ int choco_orthogonalize(const choco_orthogonalize_config* cfg, const void* x_dev
     const uint32_t count = (uint32_t)A.one.count;
     const Round R{0, 1, count * L.shape.start_tiles, count * L.shape.gram_tiles, count * L.shape.apply_tiles};
     int rc = CHOCO_OK;
-    with_type(c.type, [&](auto x) { rc = run_round<decltype(x), false>(A, R, c.iterations, (hipStream_t)c.stream); });
+    with_type(c.type, [&](auto x) { rc = run_round<decltype(x), false>(A, R, c.iterations, L.tile, (hipStream_t)c.stream); });
     if (rc) return rc;
   }
   return CHOCO_OK;
@@ -317,8 +331,8 @@ int choco_muon_step(choco_muon* a, const void* g_dev, int32_t grad_type, float l
     A.source = g_dev;
     A.grad_scale = grad_scale_dev;
     A.lr = lr;
-    const int rc = grad_type == CHOCO_F32 ? run_round<float, true>(A, R, a->iterations, a->stream)
-                                          : run_round<bf16_t, true>(A, R, a->iterations, a->stream);
+    const int rc = grad_type == CHOCO_F32 ? run_round<float, true>(A, R, a->iterations, a->layout.tile, a->stream)
+                                          : run_round<bf16_t, true>(A, R, a->iterations, a->layout.tile, a->stream);
     if (rc) return rc;
   }
   return CHOCO_OK;
