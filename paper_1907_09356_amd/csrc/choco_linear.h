@@ -205,86 +205,138 @@ __device__ __forceinline__ uint32_t by_xcd(uint32_t block, uint32_t blocks) {
   return x * each + min(x, more) + (block >> 3);
 }
 
-template <class In, int V>
-__device__ __forceinline__ void load_entries(const In* p, int have, float (&x)[V], int vec) {
-  // (have: entries that are there; vec divides them or is 1)
-  if (vec * sizeof(In) == 16 && V * sizeof(In) == 16) {
-    if (have >= V) load_floats<In, V>(p, x);
-    else
-#pragma unroll
-      for (int i = 0; i < V; ++i) x[i] = 0.0f;
-    return;
-  }
-#pragma unroll
-  for (int i = 0; i < V; i += 2) {
-    if (vec >= 2) {
-      float two[2] = {0.0f, 0.0f};
-      if (i < have) load_floats<In, 2>(p + i, two);
-      x[i] = two[0];
-      x[i + 1] = two[1];
-    } else {
-      x[i] = i < have ? to_float(p[i]) : 0.0f;
-      x[i + 1] = i + 1 < have ? to_float(p[i + 1]) : 0.0f;
-    }
-  }
-}
-
 template <class Core, int DA>
 struct ChunkShared {
   static constexpr int kPad = 16 / sizeof(Core);
   static constexpr bool kTurned = sizeof(Core) == 2;      // b by columns as well
+  static constexpr int kTurnedRow = kChunk + 4;
   Core a[kChunk][DA + kPad], b[kChunk][DA + kPad];
   Core c[kChunk][kLinearSlice + kPad];
-  Core turned[kTurned ? DA : 1][kTurned ? kChunk + kPad : 1];
+  Core turned[kTurned ? DA : 1][kTurned ? kTurnedRow : 1];
   float c_high[kChunk], c_low[kChunk], to_end[kChunk], dots[4][kChunk];
 };
 
-// 64 steps' rows of `dim` entries, zero where `time` says -1, W columns.
-template <class In, class Core, int W, int STRIDE, bool TURNED, class Time>
-__device__ __forceinline__ void stage(Core (&to)[kChunk][STRIDE], Core* turned, const In* from, int64_t step, int dim, int vec, Time time) {
-  constexpr int V = 8, R = TURNED ? 4 : 1, kUnits = kChunk / R * (W / V);
-  for (int u = threadIdx.x; u < kUnits; u += blockDim.x) {
-    const int col = u % (W / V) * V, row = u / (W / V) * R;
-    float x[R][V];
+// A chunk's rows of one array on their way from memory to LDS, in a thread's registers: they are asked for while the chunk before is
+// worked on.  A thread takes R rows of 8 entries at a time.  R = 4, for rows that are also laid out by columns: 16 neighbouring lanes take
+// 4 x 4 of these, which meets all banks both ways.
+template <class In, class Core, int W, int R>
+struct Staged {
+  static constexpr int kWords = 8 * sizeof(In) / 4;      // of 8 entries
+  static constexpr int kAll = kChunk / R * (W / 8), kUnits = (kAll + 255) / 256;
+  uint32_t x[kUnits][R][kWords];
+
+  static __device__ __forceinline__ void place(int i, int& row, int& col) {
+    const int u = i * 256 + (int)threadIdx.x;
+    if constexpr (R == 1) {
+      row = u / (W / 8);
+      col = u % (W / 8) * 8;
+    } else {
+      static_assert(kChunk / R == 16);
+      row = ((u & 3) | (u >> 2 & 12)) * R;
+      col = ((u >> 2 & 3) | (u >> 6) * 4) * 8;
+    }
+  }
+  // `width` entries of a row are there; of rows that `time` says -1, none.  vec: entries that a load takes, 16 bytes, or 2 or 1.
+  template <class Time>
+  __device__ __forceinline__ void load(const In* from, int64_t step, int width, int vec, Time time) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const int64_t t = time(row + r);
-      if (t < 0) {
+    for (int i = 0; i < kUnits; ++i) {
+      int row, col;
+      place(i, row, col);
 #pragma unroll
-        for (int i = 0; i < V; ++i) x[r][i] = 0.0f;
-      } else {
+      for (int r = 0; r < R; ++r) {
+        const int64_t t = row + r < kChunk && col < W ? time(row + r) : -1;
         const In* p = from + t * step + col;
-        if constexpr (sizeof(In) == 2) {
-          load_entries<In, 8>(p, dim - col, x[r], vec);
-        } else {
-          float lo[4], hi[4];
-          load_entries<In, 4>(p, dim - col, lo, vec);
-          load_entries<In, 4>(p + 4, dim - col - 4, hi, vec);
+        const int have = t < 0 ? 0 : width - col;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            x[r][i] = lo[i];
-            x[r][4 + i] = hi[i];
+        for (int w = 0; w < kWords; ++w) x[i][r][w] = 0;
+        if (vec * sizeof(In) == 16) {
+#pragma unroll
+          for (int w = 0; w < kWords; w += 4)
+            if (have > w * (int)(4 / sizeof(In))) {
+              const uint4 v = *reinterpret_cast<const uint4*>(p + w * (4 / sizeof(In)));
+              x[i][r][w] = v.x; x[i][r][w + 1] = v.y; x[i][r][w + 2] = v.z; x[i][r][w + 3] = v.w;
+            }
+        } else if (sizeof(In) == 4 || vec == 2) {
+#pragma unroll
+          for (int w = 0; w < kWords; ++w)
+            if (have > w * (int)(4 / sizeof(In))) x[i][r][w] = *reinterpret_cast<const uint32_t*>(p + w * (4 / sizeof(In)));
+        } else {
+#pragma unroll
+          for (int w = 0; w < kWords; ++w) {
+            const uint16_t* half = reinterpret_cast<const uint16_t*>(p);
+            if (have > 2 * w) x[i][r][w] = half[2 * w];
+            if (have > 2 * w + 1) x[i][r][w] |= (uint32_t)half[2 * w + 1] << 16;
           }
         }
       }
     }
-#pragma unroll
-    for (int r = 0; r < R; ++r) store_floats<Core, 16 / sizeof(Core)>(&to[row + r][col], *(const float(*)[16 / sizeof(Core)])&x[r][0]);
-    if constexpr (sizeof(Core) == 4)
-#pragma unroll
-      for (int r = 0; r < R; ++r) store_floats<Core, 4>(&to[row + r][col + 4], *(const float(*)[4])&x[r][4]);
-    if constexpr (TURNED)
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const float four[4] = {x[0][i], x[1][i], x[2][i], x[3][i]};
-        store_floats<Core, 4>(turned + (int64_t)(col + i) * (kChunk + 8) + row, four);
-      }
   }
+  __device__ __forceinline__ float at(int i, int r, int e) const {
+    if constexpr (sizeof(In) == 4) return __uint_as_float(x[i][r][e]);
+    else return entry<In>(x[i][r][e / 2], e & 1);
+  }
+  template <int STRIDE>
+  __device__ __forceinline__ void store(Core (&to)[kChunk][STRIDE]) const {
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+      int row, col;
+      place(i, row, col);
+      if (row >= kChunk || col >= W) continue;
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        if constexpr (sizeof(Core) == 2) {
+          *reinterpret_cast<uint4*>(&to[row + r][col]) = uint4{x[i][r][0], x[i][r][1], x[i][r][2], x[i][r][3]};
+        } else {
+          *reinterpret_cast<f32x4*>(&to[row + r][col]) = f32x4{at(i, r, 0), at(i, r, 1), at(i, r, 2), at(i, r, 3)};
+          *reinterpret_cast<f32x4*>(&to[row + r][col + 4]) = f32x4{at(i, r, 4), at(i, r, 5), at(i, r, 6), at(i, r, 7)};
+        }
+      }
+    }
+  }
+  // ... by columns: four steps of an entry are 8 bytes
+  template <int STRIDE>
+  __device__ __forceinline__ void store_turned(Core (*to)[STRIDE]) const {
+    static_assert(R == 4 && sizeof(Core) == 2);
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+      int row, col;
+      place(i, row, col);
+      if (col >= W) continue;
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) {
+        const uint32_t w0 = x[i][0][e / 2], w1 = x[i][1][e / 2], w2 = x[i][2][e / 2], w3 = x[i][3][e / 2];
+        *reinterpret_cast<uint2*>(&to[col + e][row]) = uint2{__builtin_amdgcn_perm(w1, w0, 0x05040100u), __builtin_amdgcn_perm(w3, w2, 0x05040100u)};
+        *reinterpret_cast<uint2*>(&to[col + e + 1][row]) = uint2{__builtin_amdgcn_perm(w1, w0, 0x07060302u), __builtin_amdgcn_perm(w3, w2, 0x07060302u)};
+      }
+    }
+  }
+};
+
+// Sums over the lanes up to each.
+template <int CONTROL, int ROWS>
+__device__ __forceinline__ double moved(double x) {
+  const uint64_t bits = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0u, (uint32_t)bits, CONTROL, ROWS, 15, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0u, (uint32_t)(bits >> 32), CONTROL, ROWS, 15, false);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ double sums_to(double x) {
+  x += moved<0x111, 15>(x);       // of 16 lanes: from 1, 2, 4 and 8 before
+  x += moved<0x112, 15>(x);
+  x += moved<0x114, 15>(x);
+  x += moved<0x118, 15>(x);
+  x += moved<0x142, 10>(x);       // the first 16's to the second's, the third's to the fourth's
+  x += moved<0x143, 12>(x);       // the first half's to the second's
+  return x;
 }
 
 // STATE: only the segments' own contributions to the state, and their logarithms' sums.
+// (workgroups of a compute unit: as its LDS holds, two at least where it holds them)
+template <class Core, int DA>
+constexpr int kChunkGroups = sizeof(ChunkShared<Core, DA>) * 2 > 163840 ? 1 : 2;
 template <class In, class Core, int DA, int N_OUT, int N_STATE, bool STATE>
-__global__ __launch_bounds__(256) void k_linear_chunks(LinearArgs A, LinearPass P, LinearChunks C) {
+__global__ __launch_bounds__(256, (kChunkGroups<Core, DA>)) void k_linear_chunks(LinearArgs A, LinearPass P, LinearChunks C) {
   typedef Operand<Core> Op;
   typedef typename Op::Frag Frag;
   constexpr int kJ = DA / Op::kInner, kT = Op::kTiles, kS = kChunk / Op::kInner;
@@ -326,37 +378,51 @@ __global__ __launch_bounds__(256) void k_linear_chunks(LinearArgs A, LinearPass 
   double total = 0.0;
 
   const int64_t inside = min(end, len);       // steps of the segment that are in the sequence end here
-  const int64_t chunks = inside > begin ? (inside - begin + kChunk - 1) / kChunk : 0;
-  for (int64_t i = 0; i < chunks; ++i) {
-    const int64_t t0 = begin + (P.back ? chunks - 1 - i : i) * kChunk;
-    const int there = (int)min((int64_t)kChunk, inside - t0);
-    const auto time = [&](int row) -> int64_t {       // of a row of the chunk, -1 behind the sequence
-      const int t = P.back ? kChunk - 1 - row : row;
-      return t < there ? t0 + t : -1;
-    };
+  const int chunks = inside > begin ? (int)((inside - begin + kChunk - 1) / kChunk) : 0;
+  typedef ChunkShared<Core, DA> Shared;
+  Staged<In, Core, DA, 1> next_a;
+  Staged<In, Core, DA, Shared::kTurned ? 4 : 1> next_b;
+  Staged<In, Core, kLinearSlice, 1> next_c;
+  float next_g = 0.0f;
+  const auto begin_of = [&](int i) { return begin + (int64_t)(P.back ? chunks - 1 - i : i) * kChunk; };
+  // the step of a row of a chunk, -1 behind the sequence
+  const auto step_of = [&](int64_t t0, int row) -> int64_t {
+    const int64_t t = t0 + (P.back ? kChunk - 1 - row : row);
+    return t < inside ? t : -1;
+  };
+  const auto ask = [&](int i) {
+    const int64_t t0 = begin_of(i);
+    const auto time = [&](int row) { return step_of(t0, row); };
+    if (!STATE) next_a.load(pa, P.a_step, P.da, C.vec_a, time);
+    next_b.load(pb, P.b_step, P.da, C.vec_b, time);
+    next_c.load(pc, P.c_step, in_slice, C.vec_c, time);
+    if (wave == 0) {
+      const int64_t t = step_of(t0, lane) + (P.back ? 1 : 0);
+      next_g = step_of(t0, lane) >= 0 && t < len ? log_gate(A, b, t, h) : 0.0f;
+    }
+  };
+  if (chunks > 0) ask(0);
+  for (int i = 0; i < chunks; ++i) {
+    const int64_t t0 = begin_of(i);
+    const auto time = [&](int row) { return step_of(t0, row); };
     if (!STATE && P.kept && t0 % kLinearSave == 0) keep(P.kept + (bh * P.kept_of + t0 / kLinearSave) * entries, 1.0f);
     __syncthreads();
-    if (!STATE) stage<In, Core, DA, DA + ChunkShared<Core, DA>::kPad, false>(S.a, (Core*)nullptr, pa, P.a_step, P.da, C.vec_a, time);
-    stage<In, Core, DA, DA + ChunkShared<Core, DA>::kPad, ChunkShared<Core, DA>::kTurned>(S.b, &S.turned[0][0], pb, P.b_step, P.da, C.vec_b, time);
-    stage<In, Core, kLinearSlice, kLinearSlice + ChunkShared<Core, DA>::kPad, false>(S.c, (Core*)nullptr, pc, P.c_step, in_slice, C.vec_c, time);
+    if (!STATE) next_a.store(S.a);
+    if constexpr (Shared::kTurned) next_b.store_turned(S.turned);
+    if (!STATE || !Shared::kTurned) next_b.store(S.b);
+    next_c.store(S.c);
     if (wave == 0) {      // the logarithms' sums
-      const int64_t t = time(lane) + (P.back ? 1 : 0);
-      double x = 0.0;
-      if (time(lane) >= 0 && t < len) {
-        const float log = log_gate(A, b, t, h);
-        x = log < kLinearLeast ? (double)kLog2Least : (double)log * 1.4426950408889634;
-      }
-      for (int o = 1; o < 64; o <<= 1) {
-        const double y = __shfl_up(x, o);
-        if (lane >= o) x += y;
-      }
+      const double x = sums_to(next_g < kLinearLeast ? (double)kLog2Least : (double)next_g * 1.4426950408889634);
       const double all = __shfl(x, 63);
       S.c_high[lane] = (float)x;
       S.c_low[lane] = (float)(x - (double)(float)x);
       S.to_end[lane] = __builtin_amdgcn_exp2f((float)(all - x));
       total += all;
     }
+    if (i + 1 < chunks) ask(i + 1);
     __syncthreads();
+    const bool busy = 16 * wave < in_slice;
+    if (busy) [&] {
     Frag cf[kS];       // column l's entries, a lane's steps
 #pragma unroll
     for (int s = 0; s < kS; ++s)
@@ -365,29 +431,28 @@ __global__ __launch_bounds__(256) void k_linear_chunks(LinearArgs A, LinearPass 
 #pragma unroll
         for (int r = 0; r < 4; ++r) cf[s][4 * t + r] = S.c[16 * (s * kT + t) + 4 * g + r][16 * wave + l];
     if constexpr (!STATE) {
-      f32x4 y[4] = {};
+      Frag before[kJ][N_OUT];
 #pragma unroll
-      for (int j = 0; j < kJ; ++j) {
-        Frag p[N_OUT];
-        pieces_of<Core, N_OUT>(*(const f32x4(*)[kT])&state[j * kT], p);
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const Frag q = Op::load(&S.a[16 * t + l][0], j, g);
-#pragma unroll
-          for (int n = N_OUT - 1; n >= 0; --n) y[t] = Op::mma(p[n], q, y[t]);
-        }
-      }
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
+      for (int j = 0; j < kJ; ++j) pieces_of<Core, N_OUT>(*(const f32x4(*)[kT])&state[j * kT], before[j]);
+      // (steps behind the sequence are its first rows backwards, its last ones forwards)
+      const int there = (int)min((int64_t)kChunk, inside - t0), t_first = P.back ? (kChunk - there) / 16 : 0, t_end = P.back ? 4 : (there + 15) / 16;
+#pragma unroll 1
+      for (int t = t_first; t < t_end; ++t) {
         const float high = S.c_high[16 * t + l], low = S.c_low[16 * t + l];
         const float here = __builtin_amdgcn_exp2f(high + low);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) y[t][r] *= here;
         Frag q[kJ];
+        f32x4 y = {};
 #pragma unroll
-        for (int j = 0; j < kJ; ++j) q[j] = Op::load(&S.a[16 * t + l][0], j, g);
+        for (int j = 0; j < kJ; ++j) {
+          q[j] = Op::load(&S.a[16 * t + l][0], j, g);
 #pragma unroll
-        for (int s = 0; s < (t + kT) / kT; ++s) {
+          for (int n = N_OUT - 1; n >= 0; --n) y = Op::mma(before[j][n], q[j], y);
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) y[r] *= here;
+#pragma unroll
+        for (int s = 0; s < kS; ++s) {
+          if (s * kT > t) continue;
           f32x4 w[kT];
 #pragma unroll
           for (int u = 0; u < kT; ++u) {
@@ -406,7 +471,7 @@ __global__ __launch_bounds__(256) void k_linear_chunks(LinearArgs A, LinearPass 
           Frag p[N_OUT];
           pieces_of<Core, N_OUT>(w, p);
 #pragma unroll
-          for (int n = N_OUT - 1; n >= 0; --n) y[t] = Op::mma(cf[s], p[n], y[t]);
+          for (int n = N_OUT - 1; n >= 0; --n) y = Op::mma(cf[s], p[n], y);
         }
         // rows of the result: step 16 t + l, columns 4 g to 4 g + 3 of the wave's
         const int64_t when = time(16 * t + l);
@@ -414,34 +479,26 @@ __global__ __launch_bounds__(256) void k_linear_chunks(LinearArgs A, LinearPass 
         if (when >= 0) {
           const int64_t to = out + when * P.out_step + first;
           if (C.vec_out == 4 && first < P.dc) {
-            const float x[4] = {y[t][0], y[t][1], y[t][2], y[t][3]};
+            const float x[4] = {y[0], y[1], y[2], y[3]};
             if (P.wide) store_floats<float, 4>((float*)P.out + to, x);
             else store_floats<In, 4>((In*)P.out + to, x);
           } else {
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-              if (first + r < P.dc) store_result<In>(P, to + r, y[t][r]);
+              if (first + r < P.dc) store_result<In>(P, to + r, y[r]);
           }
         }
         if (P.dots) {
           float d = 0.0f;
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            if (when >= 0 && first + r < P.dc) d = fmaf(y[t][r], to_float(px[when * P.x_step + first + r]), d);
+            if (when >= 0 && first + r < P.dc) d = fmaf(y[r], to_float(px[when * P.x_step + first + r]), d);
           d += __shfl_xor(d, 16);
           d += __shfl_xor(d, 32);
           if (g == 0) S.dots[wave][16 * t + l] = d;
         }
       }
-      if (P.dots) {
-        __syncthreads();
-        if (wave == 0 && time(lane) >= 0) {
-          float d = S.dots[0][lane];
-          for (int w = 1; w < (int)(blockDim.x >> 6); ++w) d += S.dots[w][lane];
-          P.dots[((int64_t)slice * A.batch * A.heads + bh) * A.steps + time(lane)] = d;
-        }
-      }
-      if (i + 1 == chunks && (C.states || !P.last) && !P.kept) break;      // nobody reads the state
+      if (i + 1 == chunks && (C.states || !P.last) && !P.kept) return;      // nobody reads the state
     }
     const float all = __builtin_amdgcn_exp2f(S.c_high[kChunk - 1] + S.c_low[kChunk - 1]);
 #pragma unroll
@@ -472,6 +529,15 @@ __global__ __launch_bounds__(256) void k_linear_chunks(LinearArgs A, LinearPass 
         for (int n = N_STATE - 1; n >= 0; --n) state[j] = Op::mma(rows, p[n], state[j]);
       }
     }
+    }();
+    if (!STATE && P.dots) {
+      __syncthreads();
+      if (wave == 0 && time(lane) >= 0) {
+        float d = S.dots[0][lane];
+        for (int w = 1; w < (in_slice + 15) / 16; ++w) d += S.dots[w][lane];
+        P.dots[((int64_t)slice * A.batch * A.heads + bh) * A.steps + time(lane)] = d;
+      }
+    }
   }
   if constexpr (STATE) {
     keep(C.states + (bh * C.states_of + segment) * entries, 1.0f);
@@ -481,7 +547,7 @@ __global__ __launch_bounds__(256) void k_linear_chunks(LinearArgs A, LinearPass 
   // zeros behind the sequence
   const int64_t zero = max(begin, len);
   const int width = in_slice;
-  for (int64_t e = threadIdx.x; e < (end - zero) * width; e += blockDim.x)
+  for (int64_t e = threadIdx.x; e < (end - zero) * width; e += 256)
     store_result<In>(P, out + (zero + e / width) * P.out_step + slice * kLinearSlice + e % width, 0.0f);
   if (P.kept && (len == 0 ? segment == 0 : begin < len && len <= end))
     keep(P.kept + (bh * P.kept_of + (len + kLinearSave - 1) / kLinearSave) * entries, 1.0f);

@@ -153,8 +153,7 @@ int launch_chunks(const choco_linear_config& c, const LinearArgs& A, const Linea
   }
   C.slices = slices_of(P.dc);
   C.blocks = (uint32_t)(rows_of(c) * C.segments * C.slices);
-  const int waves = std::min(4, (P.dc + 15) / 16);
-  kernel<<<dim3(C.blocks), 64 * waves, lds, (hipStream_t)c.stream>>>(A, P, C);
+  kernel<<<dim3(C.blocks), 256, lds, (hipStream_t)c.stream>>>(A, P, C);
   TRY_HIP(hipGetLastError());
   return CHOCO_OK;
 }
