@@ -131,8 +131,8 @@ __global__ __launch_bounds__(256) void k_linear_steps(LinearArgs A, LinearPass P
 //   out_t = e^c_t S^T a_t + sum over s <= t of e^(c_t - c_s) (a_t b_s) c_s,   S <- e^c_end S + sum of e^(c_end - c_s) b_s c_s^T:
 // four products of matrices, on the matrix cores, out^T = S^T a^T + c^T P^T with P^T = (b a^T) weighted.  A wave takes 16 columns of the result
 // and holds the state's in registers as the matrix cores leave a product: a lane has a column's rows 4 g to 4 g + 3 of every 16.
-// That is how the cores take a left operand whose inner index is the row, so neither S nor P^T goes through LDS; every wave makes
-// P^T of its own.  Differences of c are taken of c in two floats: a start-over leaves the steps behind it exact.
+// That is how the cores take a left operand whose inner index is the row, so S does not go through LDS; P^T does, a wave makes
+// a quarter of it.  Differences of c are taken of c in two floats: a start-over leaves the steps behind it exact.
 //
 // Entries of 32 bits (and of fp16, taken as 32 bits) go to the fp32 matrix instruction.  Those of bf16 are operands as they are; what is fp32
 // by nature (P, S, weighted c) enters as a sum of bf16 numbers, two of them (2^-17) for a result of 16 bits, three (2^-25) for states
@@ -196,7 +196,8 @@ struct LinearChunks {
   int32_t segments, chunks;      // a segment has so many chunks
   int32_t slices;
   uint32_t blocks;
-  int32_t vec_a, vec_b, vec_c, vec_out;   // entries that a load or store takes
+  int32_t way;          // how rows are read
+  int32_t vec_out, vec_x;   // entries that a store, or a load of x, takes
 };
 
 // One XCD's workgroups take neighbouring parts of the work: slices of the same head share their a and b in its L2.
@@ -209,21 +210,74 @@ template <class Core, int DA>
 struct ChunkShared {
   static constexpr int kPad = 16 / sizeof(Core);
   static constexpr bool kTurned = sizeof(Core) == 2;      // b by columns as well
-  static constexpr int kTurnedRow = kChunk + 4;
+  static constexpr int kTurnedRow = kChunk + 4, kScoreRow = kChunk + 4;
+  // (P, in 16 bits three pieces of it, lies over a, in 16 bits also over b, and what is missing)
+  static constexpr int kScores = 3 * kChunk * kScoreRow, kRows = 2 * kChunk * (DA + kPad);
   Core a[kChunk][DA + kPad], b[kChunk][DA + kPad];
-  Core c[kChunk][kLinearSlice + kPad];
-  Core turned[kTurned ? DA : 1][kTurned ? kTurnedRow : 1];
-  float c_high[kChunk], c_low[kChunk], to_end[kChunk], dots[4][kChunk];
+  Core more[kTurned && kScores > kRows ? kScores - kRows : 1];
+  alignas(16) Core c[kChunk][kLinearSlice + kPad];
+  alignas(16) Core turned[kTurned ? DA : 1][kTurned ? kTurnedRow : 1];
+  alignas(16) float c_high[kChunk], c_low[kChunk], to_end[kChunk], dots[4][kChunk];
 };
+
+// How rows are read: parts of 16 bytes or words of 4 by offsets of 32 bits, where what is not there has one outside the buffer and comes
+// back as zero, without a branch; or entry by entry by 64-bit addresses, for rows that are on no word's border or far apart.
+enum { kEntries = 0, kWords = 4, kParts = 16 };
+constexpr uint32_t kBufferBytes = 0x80000000u;
+
+typedef uint32_t word2 __attribute__((ext_vector_type(2)));
+typedef uint32_t word4 __attribute__((ext_vector_type(4)));
+
+// Four entries of a row, of which those from `width` on are not there: `at` is their byte in the buffer, ~0 for none at all.
+template <class T>
+__device__ __forceinline__ void load_four(__amdgpu_buffer_rsrc_t buffer, uint32_t at, int width, bool whole, float (&x)[4]) {
+  if (whole) {
+    const uint32_t from = width >= 4 ? at : ~0u;
+    if constexpr (sizeof(T) == 4) {
+      const word4 v = __builtin_amdgcn_raw_buffer_load_b128(buffer, from, 0, 0);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(v[i]);
+    } else {
+      const word2 v = __builtin_amdgcn_raw_buffer_load_b64(buffer, from, 0, 0);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = entry<T>(v[i / 2], i & 1);
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t from = i < width && at != ~0u ? at + i * (uint32_t)sizeof(T) : ~0u;
+    if constexpr (sizeof(T) == 4) x[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(buffer, from, 0, 0));
+    else x[i] = entry<T>(__builtin_amdgcn_raw_buffer_load_b16(buffer, from, 0, 0), 0);
+  }
+}
+template <class T>
+__device__ __forceinline__ void store_four(__amdgpu_buffer_rsrc_t buffer, uint32_t at, int width, bool whole, const f32x4& x) {
+  Pack<T, 4> v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v.e[i] = from_float<T>(x[i]);
+  if (whole) {
+    const uint32_t to = width >= 4 ? at : ~0u;
+    if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(word4, v), buffer, to, 0, 0);
+    else __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(word2, v), buffer, to, 0, 0);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t to = i < width && at != ~0u ? at + i * (uint32_t)sizeof(T) : ~0u;
+    if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v.e[i]), buffer, to, 0, 0);
+    else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, v.e[i]), buffer, to, 0, 0);
+  }
+}
 
 // A chunk's rows of one array on their way from memory to LDS, in a thread's registers: they are asked for while the chunk before is
 // worked on.  A thread takes R rows of 8 entries at a time.  R = 4, for rows that are also laid out by columns: 16 neighbouring lanes take
 // 4 x 4 of these, which meets all banks both ways.
-template <class In, class Core, int W, int R>
+template <class In, class Core, int W, int R, int WAY>
 struct Staged {
-  static constexpr int kWords = 8 * sizeof(In) / 4;      // of 8 entries
+  static constexpr int kWordsOf = 8 * sizeof(In) / 4;      // of 8 entries
   static constexpr int kAll = kChunk / R * (W / 8), kUnits = (kAll + 255) / 256;
-  uint32_t x[kUnits][R][kWords];
+  uint32_t x[kUnits][R][kWordsOf];
 
   static __device__ __forceinline__ void place(int i, int& row, int& col) {
     const int u = i * 256 + (int)threadIdx.x;
@@ -236,37 +290,43 @@ struct Staged {
       col = ((u >> 2 & 3) | (u >> 6) * 4) * 8;
     }
   }
-  // `width` entries of a row are there; of rows that `time` says -1, none.  vec: entries that a load takes, 16 bytes, or 2 or 1.
-  template <class Time>
-  __device__ __forceinline__ void load(const In* from, int64_t step, int width, int vec, Time time) {
+  // Rows of the chunk from `lo` to `hi`, `width` entries each; `first` is the row of the chunk's earliest step, which backwards is the
+  // last row.
+  __device__ __forceinline__ void load(const In* first, int64_t step, bool back, int width, int lo, int hi) {
+    const __amdgpu_buffer_rsrc_t buffer = __builtin_amdgcn_make_buffer_rsrc((void*)first, 0, kBufferBytes, 0x00027000);
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
       int row, col;
       place(i, row, col);
 #pragma unroll
       for (int r = 0; r < R; ++r) {
-        const int64_t t = row + r < kChunk && col < W ? time(row + r) : -1;
-        const In* p = from + t * step + col;
-        const int have = t < 0 ? 0 : width - col;
+        const bool there = row + r >= lo && row + r < hi && col < W;
+        const int t = back ? kChunk - 1 - row - r : row + r;
+        const uint32_t at = ((uint32_t)t * (uint32_t)step + (uint32_t)col) * (uint32_t)sizeof(In);
+        constexpr int kEach = 4 / sizeof(In);      // entries of a word
+        if constexpr (WAY == kParts) {
 #pragma unroll
-        for (int w = 0; w < kWords; ++w) x[i][r][w] = 0;
-        if (vec * sizeof(In) == 16) {
+          for (int w = 0; w < kWordsOf; w += 4) {
+            const word4 v = __builtin_amdgcn_raw_buffer_load_b128(buffer, there && col + w * kEach < width ? at + 4 * w : ~0u, 0, 0);
 #pragma unroll
-          for (int w = 0; w < kWords; w += 4)
-            if (have > w * (int)(4 / sizeof(In))) {
-              const uint4 v = *reinterpret_cast<const uint4*>(p + w * (4 / sizeof(In)));
-              x[i][r][w] = v.x; x[i][r][w + 1] = v.y; x[i][r][w + 2] = v.z; x[i][r][w + 3] = v.w;
-            }
-        } else if (sizeof(In) == 4 || vec == 2) {
+            for (int e = 0; e < 4; ++e) x[i][r][w + e] = v[e];
+          }
+        } else if constexpr (WAY == kWords) {
 #pragma unroll
-          for (int w = 0; w < kWords; ++w)
-            if (have > w * (int)(4 / sizeof(In))) x[i][r][w] = *reinterpret_cast<const uint32_t*>(p + w * (4 / sizeof(In)));
+          for (int w = 0; w < kWordsOf; ++w)
+            x[i][r][w] = __builtin_amdgcn_raw_buffer_load_b32(buffer, there && col + w * kEach < width ? at + 4 * w : ~0u, 0, 0);
         } else {
+          const In* p = first + t * step + col;
 #pragma unroll
-          for (int w = 0; w < kWords; ++w) {
-            const uint16_t* half = reinterpret_cast<const uint16_t*>(p);
-            if (have > 2 * w) x[i][r][w] = half[2 * w];
-            if (have > 2 * w + 1) x[i][r][w] |= (uint32_t)half[2 * w + 1] << 16;
+          for (int w = 0; w < kWordsOf; ++w) {
+            x[i][r][w] = 0;
+            if constexpr (sizeof(In) == 4) {
+              if (there && col + w < width) x[i][r][w] = *reinterpret_cast<const uint32_t*>(p + w);
+            } else {
+              const uint16_t* half = reinterpret_cast<const uint16_t*>(p);
+              if (there && col + 2 * w < width) x[i][r][w] = half[2 * w];
+              if (there && col + 2 * w + 1 < width) x[i][r][w] |= (uint32_t)half[2 * w + 1] << 16;
+            }
           }
         }
       }
@@ -335,7 +395,7 @@ __device__ __forceinline__ double sums_to(double x) {
 // (workgroups of a compute unit: as its LDS holds, two at least where it holds them)
 template <class Core, int DA>
 constexpr int kChunkGroups = sizeof(ChunkShared<Core, DA>) * 2 > 163840 ? 1 : 2;
-template <class In, class Core, int DA, int N_OUT, int N_STATE, bool STATE>
+template <class In, class Core, int DA, int N_OUT, int N_STATE, bool STATE, int WAY>
 __global__ __launch_bounds__(256, (kChunkGroups<Core, DA>)) void k_linear_chunks(LinearArgs A, LinearPass P, LinearChunks C) {
   typedef Operand<Core> Op;
   typedef typename Op::Frag Frag;
@@ -345,7 +405,8 @@ __global__ __launch_bounds__(256, (kChunkGroups<Core, DA>)) void k_linear_chunks
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4;
   const uint32_t at = by_xcd(blockIdx.x, C.blocks);
   const int slice = at % C.slices, segment = at / C.slices % C.segments;
-  const int64_t bh = at / C.slices / C.segments, b = bh / A.heads, len = steps_of(A, b), entries = (int64_t)P.da * P.dc;
+  const int64_t bh = at / C.slices / C.segments, b = bh / A.heads, entries = (int64_t)P.da * P.dc;
+  const int64_t len = __builtin_amdgcn_readfirstlane((int)steps_of(A, b));      // (below 2^31)
   const int h = (int)(bh % A.heads), col = slice * kLinearSlice + 16 * wave;     // the wave's first column
   const In* pa = (const In*)P.a + b * P.a_seq + (h / P.a_share) * P.a_head;
   const In* pb = (const In*)P.b + b * P.b_seq + (h / P.b_share) * P.b_head;
@@ -367,44 +428,42 @@ __global__ __launch_bounds__(256, (kChunkGroups<Core, DA>)) void k_linear_chunks
       state[j][r] = from && column && row < P.da ? from[(int64_t)row * P.state_a + (int64_t)(col + l) * P.state_c] : 0.0f;
     }
   const auto keep = [&](float* to, float w) {
+    int mine = 4 * g;
+    asm volatile("" : "+v"(mine));      // (or its addresses would be kept in registers over the chunks)
+    to += (int64_t)(col + l) * P.state_c + (int64_t)mine * P.state_a;
 #pragma unroll
     for (int j = 0; j < kJ * kT; ++j)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int row = 16 * j + 4 * g + r;
-        if (column && row < P.da) to[(int64_t)row * P.state_a + (int64_t)(col + l) * P.state_c] = state[j][r] * w;
-      }
+      for (int r = 0; r < 4; ++r)
+        if (column && 16 * j + r + mine < P.da) to[(16 * j + r) * P.state_a] = state[j][r] * w;
   };
   double total = 0.0;
 
   const int64_t inside = min(end, len);       // steps of the segment that are in the sequence end here
   const int chunks = inside > begin ? (int)((inside - begin + kChunk - 1) / kChunk) : 0;
   typedef ChunkShared<Core, DA> Shared;
-  Staged<In, Core, DA, 1> next_a;
-  Staged<In, Core, DA, Shared::kTurned ? 4 : 1> next_b;
-  Staged<In, Core, kLinearSlice, 1> next_c;
+  Staged<In, Core, DA, 1, WAY> next_a;
+  Staged<In, Core, DA, Shared::kTurned ? 4 : 1, WAY> next_b;
+  Staged<In, Core, kLinearSlice, 1, WAY> next_c;
   float next_g = 0.0f;
+  const int64_t dir = P.back ? -1 : 1;
   const auto begin_of = [&](int i) { return begin + (int64_t)(P.back ? chunks - 1 - i : i) * kChunk; };
-  // the step of a row of a chunk, -1 behind the sequence
-  const auto step_of = [&](int64_t t0, int row) -> int64_t {
-    const int64_t t = t0 + (P.back ? kChunk - 1 - row : row);
-    return t < inside ? t : -1;
-  };
   const auto ask = [&](int i) {
-    const int64_t t0 = begin_of(i);
-    const auto time = [&](int row) { return step_of(t0, row); };
-    if (!STATE) next_a.load(pa, P.a_step, P.da, C.vec_a, time);
-    next_b.load(pb, P.b_step, P.da, C.vec_b, time);
-    next_c.load(pc, P.c_step, in_slice, C.vec_c, time);
+    const int64_t t0 = begin_of(i), first = t0 + (P.back ? kChunk - 1 : 0);      // the time of row 0
+    const int there = (int)min((int64_t)kChunk, inside - t0), lo = P.back ? kChunk - there : 0, hi = P.back ? kChunk : there;
+    if (!STATE) next_a.load(pa + t0 * P.a_step, P.a_step, P.back, P.da, lo, hi);
+    next_b.load(pb + t0 * P.b_step, P.b_step, P.back, P.da, lo, hi);
+    next_c.load(pc + t0 * P.c_step, P.c_step, P.back, in_slice, lo, hi);
     if (wave == 0) {
-      const int64_t t = step_of(t0, lane) + (P.back ? 1 : 0);
-      next_g = step_of(t0, lane) >= 0 && t < len ? log_gate(A, b, t, h) : 0.0f;
+      const int64_t t = first + dir * lane + (P.back ? 1 : 0);
+      next_g = lane >= lo && lane < hi && t < len ? log_gate(A, b, t, h) : 0.0f;
     }
   };
   if (chunks > 0) ask(0);
   for (int i = 0; i < chunks; ++i) {
-    const int64_t t0 = begin_of(i);
-    const auto time = [&](int row) { return step_of(t0, row); };
+    const int64_t t0 = begin_of(i), first_time = t0 + (P.back ? kChunk - 1 : 0);
+    // rows of the chunk that are in the sequence: forwards its first ones, backwards its last
+    const int there = (int)min((int64_t)kChunk, inside - t0), lo = P.back ? kChunk - there : 0, hi = P.back ? kChunk : there;
     if (!STATE && P.kept && t0 % kLinearSave == 0) keep(P.kept + (bh * P.kept_of + t0 / kLinearSave) * entries, 1.0f);
     __syncthreads();
     if (!STATE) next_a.store(S.a);
@@ -419,10 +478,26 @@ __global__ __launch_bounds__(256, (kChunkGroups<Core, DA>)) void k_linear_chunks
       S.to_end[lane] = __builtin_amdgcn_exp2f((float)(all - x));
       total += all;
     }
+    const int first = col + 4 * g;
+    float times[4][4];      // x
+    if (!STATE && P.dots) {
+      const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc((void*)(px + t0 * P.x_step), 0, kBufferBytes, 0x00027000);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const int row = 16 * t + l, when = P.back ? kChunk - 1 - row : row;
+        const bool here = row >= lo && row < hi;
+        if constexpr (WAY != kEntries) {
+          const uint32_t at = here ? ((uint32_t)when * (uint32_t)P.x_step + (uint32_t)first) * (uint32_t)sizeof(In) : ~0u;
+          load_four<In>(from, at, P.dc - first, C.vec_x == 4, times[t]);
+        } else {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) times[t][r] = here && first + r < P.dc ? to_float(px[(t0 + when) * P.x_step + first + r]) : 0.0f;
+        }
+      }
+    }
     if (i + 1 < chunks) ask(i + 1);
     __syncthreads();
-    const bool busy = 16 * wave < in_slice;
-    if (busy) [&] {
+    const bool busy = 16 * wave < in_slice;      // (the others help with P only)
     Frag cf[kS];       // column l's entries, a lane's steps
 #pragma unroll
     for (int s = 0; s < kS; ++s)
@@ -431,75 +506,105 @@ __global__ __launch_bounds__(256, (kChunkGroups<Core, DA>)) void k_linear_chunks
 #pragma unroll
         for (int r = 0; r < 4; ++r) cf[s][4 * t + r] = S.c[16 * (s * kT + t) + 4 * g + r][16 * wave + l];
     if constexpr (!STATE) {
-      Frag before[kJ][N_OUT];
+      // P^T by tiles of 16 x 16, three for a wave: rows s, columns t, s <= t, and two of zeros that complete an operand of two tiles
+      const uint32_t tiles = wave == 0 ? 0x300010u : wave == 1 ? 0x311101u : wave == 2 ? 0x322021u : 0x332223u;
+      f32x4 score[3];
 #pragma unroll
-      for (int j = 0; j < kJ; ++j) pieces_of<Core, N_OUT>(*(const f32x4(*)[kT])&state[j * kT], before[j]);
-      // (steps behind the sequence are its first rows backwards, its last ones forwards)
-      const int there = (int)min((int64_t)kChunk, inside - t0), t_first = P.back ? (kChunk - there) / 16 : 0, t_end = P.back ? 4 : (there + 15) / 16;
-#pragma unroll 1
-      for (int t = t_first; t < t_end; ++t) {
+      for (int n = 0; n < 3; ++n) {
+        const int t = tiles >> (20 - 8 * n) & 15, s = tiles >> (16 - 8 * n) & 15;
+        score[n] = f32x4{};
+        if (s > t || 16 * t >= hi || 16 * t + 15 < lo) continue;
+#pragma unroll
+        for (int j = 0; j < kJ; ++j) score[n] = Op::mma(Op::load(&S.b[16 * s + l][0], j, g), Op::load(&S.a[16 * t + l][0], j, g), score[n]);
         const float high = S.c_high[16 * t + l], low = S.c_low[16 * t + l];
-        const float here = __builtin_amdgcn_exp2f(high + low);
-        Frag q[kJ];
-        f32x4 y = {};
+        const f32x4 high_s = *(const f32x4*)&S.c_high[16 * s + 4 * g], low_s = *(const f32x4*)&S.c_low[16 * s + 4 * g];
 #pragma unroll
-        for (int j = 0; j < kJ; ++j) {
-          q[j] = Op::load(&S.a[16 * t + l][0], j, g);
-#pragma unroll
-          for (int n = N_OUT - 1; n >= 0; --n) y = Op::mma(before[j][n], q[j], y);
-        }
-#pragma unroll
-        for (int r = 0; r < 4; ++r) y[r] *= here;
-#pragma unroll
-        for (int s = 0; s < kS; ++s) {
-          if (s * kT > t) continue;
-          f32x4 w[kT];
-#pragma unroll
-          for (int u = 0; u < kT; ++u) {
-            const int from = s * kT + u;      // steps 16 from + 4 g + r
-            w[u] = f32x4{};
-            if (from > t) continue;
-#pragma unroll
-            for (int j = 0; j < kJ; ++j) w[u] = Op::mma(Op::load(&S.b[16 * from + l][0], j, g), q[j], w[u]);
-            const f32x4 high_s = *(const f32x4*)&S.c_high[16 * from + 4 * g], low_s = *(const f32x4*)&S.c_low[16 * from + 4 * g];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const float weighted = w[u][r] * __builtin_amdgcn_exp2f((high - high_s[r]) + (low - low_s[r]));
-              w[u][r] = from < t || 4 * g + r <= l ? weighted : 0.0f;
-            }
-          }
-          Frag p[N_OUT];
-          pieces_of<Core, N_OUT>(w, p);
-#pragma unroll
-          for (int n = N_OUT - 1; n >= 0; --n) y = Op::mma(cf[s], p[n], y);
-        }
-        // rows of the result: step 16 t + l, columns 4 g to 4 g + 3 of the wave's
-        const int64_t when = time(16 * t + l);
-        const int first = col + 4 * g;
-        if (when >= 0) {
-          const int64_t to = out + when * P.out_step + first;
-          if (C.vec_out == 4 && first < P.dc) {
-            const float x[4] = {y[0], y[1], y[2], y[3]};
-            if (P.wide) store_floats<float, 4>((float*)P.out + to, x);
-            else store_floats<In, 4>((In*)P.out + to, x);
-          } else {
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-              if (first + r < P.dc) store_result<In>(P, to + r, y[r]);
-          }
-        }
-        if (P.dots) {
-          float d = 0.0f;
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (when >= 0 && first + r < P.dc) d = fmaf(y[r], to_float(px[when * P.x_step + first + r]), d);
-          d += __shfl_xor(d, 16);
-          d += __shfl_xor(d, 32);
-          if (g == 0) S.dots[wave][16 * t + l] = d;
+        for (int r = 0; r < 4; ++r) {
+          const float weighted = score[n][r] * __builtin_amdgcn_exp2f((high - high_s[r]) + (low - low_s[r]));
+          score[n][r] = s < t || 4 * g + r <= l ? weighted : 0.0f;
         }
       }
-      if (i + 1 == chunks && (C.states || !P.last) && !P.kept) return;      // nobody reads the state
+      // what comes of the state before the chunk
+      f32x4 y[4] = {};
+      if (busy) {
+#pragma unroll
+        for (int j = 0; j < kJ; ++j) {
+          Frag p[N_OUT];
+          pieces_of<Core, N_OUT>(*(const f32x4(*)[kT])&state[j * kT], p);
+#pragma unroll
+          for (int t = 0; t < 4; ++t) {
+            const Frag q = Op::load(&S.a[16 * t + l][0], j, g);
+#pragma unroll
+            for (int n = N_OUT - 1; n >= 0; --n) y[t] = Op::mma(p[n], q, y[t]);
+          }
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const float here = __builtin_amdgcn_exp2f(S.c_high[16 * t + l] + S.c_low[16 * t + l]);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) y[t][r] *= here;
+        }
+      }
+      __syncthreads();
+      // P by rows, over a (and b, which in 16 bits is needed by columns only from here on)
+      Core (*const scores)[kChunk][Shared::kScoreRow] = reinterpret_cast<Core (*)[kChunk][Shared::kScoreRow]>(&S.a[0][0]);
+      static_assert(Shared::kTurned ? N_OUT <= 3 : kChunk * Shared::kScoreRow * sizeof(Core) <= sizeof(S.a));
+#pragma unroll
+      for (int n = 0; n < 3; ++n) {
+        const int t = tiles >> (20 - 8 * n) & 15, s = tiles >> (16 - 8 * n) & 15;
+        float left[4] = {score[n][0], score[n][1], score[n][2], score[n][3]};
+#pragma unroll
+        for (int k = 0; k < N_OUT; ++k) {
+          store_floats<Core, 4>(&scores[k][16 * t + l][16 * s + 4 * g], left);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) left[r] -= to_float((Core)left[r]);
+        }
+      }
+      __syncthreads();
+      if (busy) {
+        const uint32_t out_size = P.wide ? 4 : sizeof(In);
+        char* const earliest = (char*)P.out + out_size * (out + t0 * P.out_step);
+        const __amdgpu_buffer_rsrc_t to = __builtin_amdgcn_make_buffer_rsrc(earliest, 0, kBufferBytes, 0x00027000);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          if (16 * t >= hi || 16 * t + 15 < lo) continue;
+#pragma unroll
+          for (int s = 0; s <= t / kT; ++s)
+#pragma unroll
+            for (int n = N_OUT - 1; n >= 0; --n) y[t] = Op::mma(cf[s], Op::load(&scores[n][16 * t + l][0], s, g), y[t]);
+          // rows of the result: step 16 t + l, columns 4 g to 4 g + 3 of the wave's
+          const int row = 16 * t + l, when = P.back ? kChunk - 1 - row : row;
+          const bool here = row >= lo && row < hi;
+          if constexpr (WAY != kEntries) {
+            const uint32_t at = here ? ((uint32_t)when * (uint32_t)P.out_step + (uint32_t)first) * out_size : ~0u;
+            if (P.wide) store_four<float>(to, at, P.dc - first, C.vec_out == 4, y[t]);
+            else store_four<In>(to, at, P.dc - first, C.vec_out == 4, y[t]);
+          } else if (here) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (first + r < P.dc) store_result<In>(P, out + (t0 + when) * P.out_step + first + r, y[t][r]);
+          }
+          if (P.dots) {
+            float d = 0.0f;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) d = fmaf(y[t][r], times[t][r], d);      // (what is not there is zero)
+            d += __shfl_xor(d, 16);
+            d += __shfl_xor(d, 32);
+            if (g == 0) S.dots[wave][row] = d;
+          }
+        }
+      }
+      if (P.dots) {
+        __syncthreads();
+        if (wave == 0 && lane >= lo && lane < hi) {
+          float d = S.dots[0][lane];
+          for (int w = 1; w < (in_slice + 15) / 16; ++w) d += S.dots[w][lane];
+          P.dots[((int64_t)slice * A.batch * A.heads + bh) * A.steps + first_time + dir * lane] = d;
+        }
+      }
+      if (i + 1 == chunks && (C.states || !P.last) && !P.kept) break;      // nobody reads the state
     }
+    if (!busy) continue;
     const float all = __builtin_amdgcn_exp2f(S.c_high[kChunk - 1] + S.c_low[kChunk - 1]);
 #pragma unroll
     for (int j = 0; j < kJ * kT; ++j)
@@ -519,7 +624,7 @@ __global__ __launch_bounds__(256, (kChunkGroups<Core, DA>)) void k_linear_chunks
 #pragma unroll
       for (int j = 0; j < kJ * kT; ++j) {
         Frag rows;
-        if constexpr (ChunkShared<Core, DA>::kTurned) {
+        if constexpr (Shared::kTurned) {
           rows = Op::load(&S.turned[16 * j + l][0], s, g);
         } else {
 #pragma unroll
@@ -527,15 +632,6 @@ __global__ __launch_bounds__(256, (kChunkGroups<Core, DA>)) void k_linear_chunks
         }
 #pragma unroll
         for (int n = N_STATE - 1; n >= 0; --n) state[j] = Op::mma(rows, p[n], state[j]);
-      }
-    }
-    }();
-    if (!STATE && P.dots) {
-      __syncthreads();
-      if (wave == 0 && time(lane) >= 0) {
-        float d = S.dots[0][lane];
-        for (int w = 1; w < (in_slice + 15) / 16; ++w) d += S.dots[w][lane];
-        P.dots[((int64_t)slice * A.batch * A.heads + bh) * A.steps + time(lane)] = d;
       }
     }
   }

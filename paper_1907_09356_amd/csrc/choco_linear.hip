@@ -143,10 +143,10 @@ int width_of(const Rows& r, size_t size, int most, const choco_linear_config& c)
 // Up to so many steps are taken one by one.
 constexpr int64_t kStepByStep = 8;
 
-template <class In, class Core, int DA, int N_OUT, int N_STATE, bool STATE>
+template <class In, class Core, int DA, int N_OUT, int N_STATE, bool STATE, int WAY>
 int launch_chunks(const choco_linear_config& c, const LinearArgs& A, const LinearPass& P, LinearChunks C) {
   const size_t lds = sizeof(ChunkShared<Core, DA>);
-  const auto kernel = k_linear_chunks<In, Core, DA, N_OUT, N_STATE, STATE>;
+  const auto kernel = k_linear_chunks<In, Core, DA, N_OUT, N_STATE, STATE, WAY>;
   if (lds > 65536) {
     static const hipError_t allowed = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     TRY_HIP(allowed);
@@ -160,14 +160,19 @@ int launch_chunks(const choco_linear_config& c, const LinearArgs& A, const Linea
 // N_OUT: bf16 numbers for one of fp32 where the result goes
 template <class In, int N_OUT, bool STATE>
 int run_chunks(const choco_linear_config& c, const LinearArgs& A, const LinearPass& P, const LinearChunks& C) {
-  const auto with_core = [&](auto dim) -> int {
-    constexpr int DA = decltype(dim)::value;
-    if constexpr (std::is_same_v<In, bf16_t>) return launch_chunks<In, bf16_t, DA, N_OUT, 3, STATE>(c, A, P, C);
-    else return launch_chunks<In, float, DA, 1, 1, STATE>(c, A, P, C);
+  const auto with_way = [&](auto dim, auto way) -> int {
+    constexpr int DA = decltype(dim)::value, WAY = decltype(way)::value;
+    if constexpr (std::is_same_v<In, bf16_t>) return launch_chunks<In, bf16_t, DA, N_OUT, 3, STATE, WAY>(c, A, P, C);
+    else return launch_chunks<In, float, DA, 1, 1, STATE, WAY>(c, A, P, C);
   };
-  if (P.da <= 64) return with_core(std::integral_constant<int, 64>{});
-  if (P.da <= 128) return with_core(std::integral_constant<int, 128>{});
-  return with_core(std::integral_constant<int, 256>{});
+  const auto with_dim = [&](auto dim) -> int {
+    if (C.way == kParts) return with_way(dim, std::integral_constant<int, kParts>{});
+    if (C.way == kWords) return with_way(dim, std::integral_constant<int, kWords>{});
+    return with_way(dim, std::integral_constant<int, kEntries>{});
+  };
+  if (P.da <= 64) return with_dim(std::integral_constant<int, 64>{});
+  if (P.da <= 128) return with_dim(std::integral_constant<int, 128>{});
+  return with_dim(std::integral_constant<int, 256>{});
 }
 
 template <class T>
@@ -181,15 +186,23 @@ int run_steps(const choco_linear_config& c, const LinearArgs& A, const LinearPas
   return CHOCO_OK;
 }
 
-LinearChunks chunks_of(const choco_linear_config& c, const LinearPass& P, const Rows& a, const Rows& b, const Rows& v, const Rows& out) {
+// (x: what the result is multiplied with, or null)
+LinearChunks chunks_of(const choco_linear_config& c, const LinearPass& P, const Rows& a, const Rows& b, const Rows& v, const Rows& out, const Rows* x) {
   LinearChunks C{};
-  const size_t size = type_bytes(c.type);
+  const size_t size = type_bytes(c.type), out_size = P.wide ? 4 : size;
+  const auto far = [&](const Rows& r, size_t bytes) {
+    return (double)r.stride[1] * bytes * kChunk + 16.0 * CHOCO_LINEAR_MAX_DIM >= (double)kBufferBytes;
+  };
   C.segments = 1;
   C.chunks = (int32_t)((c.steps + kChunk - 1) / kChunk);
-  C.vec_a = width_of(a, size, (int)(16 / size), c);
-  C.vec_b = width_of(b, size, (int)(16 / size), c);
-  C.vec_c = width_of(v, size, (int)(16 / size), c);
-  C.vec_out = width_of(out, P.wide ? 4 : size, 4, c);
+  C.way = far(out, out_size) || (x && far(*x, size)) ? kEntries : kParts;
+  for (const Rows* r : {&a, &b, &v}) {
+    const int v16 = (int)(16 / size), v4 = (int)(4 / size);
+    if (width_of(*r, size, v16, c) != v16) C.way = std::min(C.way, (int)kWords);
+    if (far(*r, size) || (v4 > 1 && width_of(*r, size, v4, c) != v4)) C.way = kEntries;
+  }
+  C.vec_out = width_of(out, out_size, 4, c);
+  C.vec_x = x ? width_of(*x, size, 4, c) : 1;
   return C;
 }
 
@@ -218,7 +231,7 @@ void segments_of(const choco_linear_config& c, int32_t& segments, int32_t& chunk
 template <class T>
 int run_forward(const choco_linear_config& c, const LinearArgs& A, LinearPass P, const Rows& q, const Rows& k, const Rows& v, const Rows& y, char* ws) {
   if (c.steps <= kStepByStep) return run_steps<T>(c, A, P);
-  LinearChunks C = chunks_of(c, P, q, k, v, y);
+  LinearChunks C = chunks_of(c, P, q, k, v, y, nullptr);
   segments_of(c, C.segments, C.chunks);
   if (C.segments > 1) {
     const LinearLayout L = linear_layout(c, false);
@@ -243,7 +256,8 @@ int run_backward(const choco_linear_config& c, const LinearArgs& A, const void* 
   float* const k_dots = q_dots + rows * c.steps * slices_of(c.dim_k);
   const bool stepwise = c.steps <= kStepByStep, several = pieces > 1;
   // a pass on its own arrays; a gradient of heads that share one: of every head to the workspace, then added up
-  const auto through = [&](LinearPass P, const Rows& ra, const Rows& rb, const Rows& rc_, Rows out, const float* states, int64_t states_of) -> int {
+  const auto through = [&](LinearPass P, const Rows& ra, const Rows& rb, const Rows& rc_, Rows out, const Rows* x, const float* states,
+                           int64_t states_of) -> int {
     const LinearPass given = P;
     const int32_t heads = out.heads, dim = out.dim;
     const int64_t wide_stride[3] = {(int64_t)c.heads * dim * c.steps, (int64_t)c.heads * dim, dim};
@@ -258,7 +272,7 @@ int run_backward(const choco_linear_config& c, const LinearArgs& A, const void* 
     if (stepwise) {
       if (const int rc = run_steps<T>(c, A, P)) return rc;
     } else {
-      LinearChunks C = chunks_of(c, P, ra, rb, rc_, out);
+      LinearChunks C = chunks_of(c, P, ra, rb, rc_, out, x);
       C.segments = (int32_t)pieces;
       C.chunks = kLinearSave / kChunk;
       if (several) {
@@ -282,7 +296,7 @@ int run_backward(const choco_linear_config& c, const LinearArgs& A, const void* 
   P.first_of = pieces + 1;
   P.x = q; P.x_seq = c.q_stride[0]; P.x_step = c.q_stride[1]; P.x_head = c.q_stride[2]; P.x_share = c.heads / c.q_heads;
   P.dots = dg ? q_dots : nullptr;
-  if (const int rc = through(P, Y, V, K, DQ, saved, pieces + 1)) return rc;
+  if (const int rc = through(P, Y, V, K, DQ, dg ? &Q : nullptr, saved, pieces + 1)) return rc;
   LinearPass last = pass_of(c, K, Q, Y, dv, c.dv_stride);
   state_of(c, false, last);
   last.back = true;
@@ -290,7 +304,7 @@ int run_backward(const choco_linear_config& c, const LinearArgs& A, const void* 
   last.first_of = 1;
   last.last = dh0;
   if (!stepwise && several) {
-    LinearChunks C = chunks_of(c, last, K, Q, Y, DV);
+    LinearChunks C = chunks_of(c, last, K, Q, Y, DV, nullptr);
     C.segments = (int32_t)pieces;
     C.chunks = kLinearSave / kChunk;
     C.states = later;
@@ -305,8 +319,8 @@ int run_backward(const choco_linear_config& c, const LinearArgs& A, const void* 
   P.first_of = 1;
   P.x = k; P.x_seq = c.k_stride[0]; P.x_step = c.k_stride[1]; P.x_head = c.k_stride[2]; P.x_share = c.heads / c.k_heads;
   P.dots = dg ? k_dots : nullptr;
-  if (const int rc = through(P, V, Y, Q, DK, later, pieces)) return rc;
-  if (const int rc = through(last, K, Q, Y, DV, later, pieces)) return rc;
+  if (const int rc = through(P, V, Y, Q, DK, dg ? &K : nullptr, later, pieces)) return rc;
+  if (const int rc = through(last, K, Q, Y, DV, nullptr, later, pieces)) return rc;
   if (!dg) return CHOCO_OK;
   LinearGates G{};
   G.q_dots = q_dots; G.k_dots = k_dots;
