@@ -174,17 +174,20 @@ __device__ __forceinline__ void pieces_of(const f32x4 (&x)[Operand<Core>::kTiles
     static_assert(N == 1);
     p[0] = x[0];
   } else {
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int e = 0; e < 8; e += 2) {
+      f32x2 left = {x[e / 4][e % 4], x[e / 4][e % 4 + 1]};
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        float left = x[t][r];
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-          p[i][4 * t + r] = (bf16_t)left;
-          if (i + 1 < N) left -= (float)p[i][4 * t + r];
-        }
+      for (int i = 0; i < N; ++i) {
+        const bf16x2 two = __builtin_convertvector(left, bf16x2);
+        p[i][e] = two.x;
+        p[i][e + 1] = two.y;
+        const uint32_t word = __builtin_bit_cast(uint32_t, two);
+        if (i + 1 < N) left = f32x2{left.x - __uint_as_float(word << 16), left.y - __uint_as_float(word & 0xFFFF0000u)};
       }
+    }
   }
 }
 
@@ -206,18 +209,18 @@ __device__ __forceinline__ uint32_t by_xcd(uint32_t block, uint32_t blocks) {
   return x * each + min(x, more) + (block >> 3);
 }
 
-template <class Core, int DA>
+template <class Core, int DA, int WAVES>
 struct ChunkShared {
-  static constexpr int kPad = 16 / sizeof(Core);
+  static constexpr int kPad = 16 / sizeof(Core), kSlice = 16 * WAVES;
   static constexpr bool kTurned = sizeof(Core) == 2;      // b by columns as well
   static constexpr int kTurnedRow = kChunk + 4, kScoreRow = kChunk + 4;
   // (P, in 16 bits three pieces of it, lies over a, in 16 bits also over b, and what is missing)
   static constexpr int kScores = 3 * kChunk * kScoreRow, kRows = 2 * kChunk * (DA + kPad);
   Core a[kChunk][DA + kPad], b[kChunk][DA + kPad];
   Core more[kTurned && kScores > kRows ? kScores - kRows : 1];
-  alignas(16) Core c[kChunk][kLinearSlice + kPad];
+  alignas(16) Core c[kChunk][kSlice + kPad];
   alignas(16) Core turned[kTurned ? DA : 1][kTurned ? kTurnedRow : 1];
-  alignas(16) float c_high[kChunk], c_low[kChunk], to_end[kChunk], dots[4][kChunk];
+  alignas(16) float c_high[kChunk], c_low[kChunk], to_end[kChunk], dots[WAVES][kChunk];
 };
 
 // How rows are read: parts of 16 bytes or words of 4 by offsets of 32 bits, where what is not there has one outside the buffer and comes
@@ -230,27 +233,46 @@ typedef uint32_t word4 __attribute__((ext_vector_type(4)));
 
 // Four entries of a row, of which those from `width` on are not there: `at` is their byte in the buffer, ~0 for none at all.
 template <class T>
-__device__ __forceinline__ void load_four(__amdgpu_buffer_rsrc_t buffer, uint32_t at, int width, bool whole, float (&x)[4]) {
-  if (whole) {
-    const uint32_t from = width >= 4 ? at : ~0u;
-    if constexpr (sizeof(T) == 4) {
-      const word4 v = __builtin_amdgcn_raw_buffer_load_b128(buffer, from, 0, 0);
+struct Four {
+  uint32_t x[sizeof(T)];
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t buffer, uint32_t at, int width, bool whole) {
+    if (whole) {
+      const uint32_t from = width >= 4 ? at : ~0u;
+      if constexpr (sizeof(T) == 4) {
+        const word4 v = __builtin_amdgcn_raw_buffer_load_b128(buffer, from, 0, 0);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(v[i]);
-    } else {
-      const word2 v = __builtin_amdgcn_raw_buffer_load_b64(buffer, from, 0, 0);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = entry<T>(v[i / 2], i & 1);
+        for (int i = 0; i < 4; ++i) x[i] = v[i];
+      } else {
+        const word2 v = __builtin_amdgcn_raw_buffer_load_b64(buffer, from, 0, 0);
+        x[0] = v.x;
+        x[1] = v.y;
+      }
+      return;
     }
-    return;
-  }
+    const auto from = [&](int i) { return i < width && at != ~0u ? at + i * (uint32_t)sizeof(T) : ~0u; };
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t from = i < width && at != ~0u ? at + i * (uint32_t)sizeof(T) : ~0u;
-    if constexpr (sizeof(T) == 4) x[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(buffer, from, 0, 0));
-    else x[i] = entry<T>(__builtin_amdgcn_raw_buffer_load_b16(buffer, from, 0, 0), 0);
+    for (int i = 0; i < (int)sizeof(T); ++i) {
+      if constexpr (sizeof(T) == 4) x[i] = __builtin_amdgcn_raw_buffer_load_b32(buffer, from(i), 0, 0);
+      else
+        x[i] = __builtin_amdgcn_raw_buffer_load_b16(buffer, from(2 * i), 0, 0) |
+               (uint32_t)__builtin_amdgcn_raw_buffer_load_b16(buffer, from(2 * i + 1), 0, 0) << 16;
+    }
   }
-}
+  __device__ __forceinline__ void load(const T* p, int width) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T); ++i) {
+      if constexpr (sizeof(T) == 4) x[i] = i < width ? *reinterpret_cast<const uint32_t*>(p + i) : 0u;
+      else {
+        const uint16_t* half = reinterpret_cast<const uint16_t*>(p);
+        x[i] = (2 * i < width ? half[2 * i] : 0u) | (2 * i + 1 < width ? (uint32_t)half[2 * i + 1] << 16 : 0u);
+      }
+    }
+  }
+  __device__ __forceinline__ float operator[](int i) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(x[i]);
+    else return entry<T>(x[i / 2], i & 1);
+  }
+};
 template <class T>
 __device__ __forceinline__ void store_four(__amdgpu_buffer_rsrc_t buffer, uint32_t at, int width, bool whole, const f32x4& x) {
   Pack<T, 4> v;
@@ -270,46 +292,54 @@ __device__ __forceinline__ void store_four(__amdgpu_buffer_rsrc_t buffer, uint32
   }
 }
 
-// A chunk's rows of one array on their way from memory to LDS, in a thread's registers: they are asked for while the chunk before is
-// worked on.  A thread takes R rows of 8 entries at a time.  R = 4, for rows that are also laid out by columns: 16 neighbouring lanes take
-// 4 x 4 of these, which meets all banks both ways.
-template <class In, class Core, int W, int R, int WAY>
+// A chunk's rows of one array on their way from memory to LDS, in the registers of WAVES waves: they are asked for while the chunk
+// before is worked on.  A thread takes R rows of V entries at a time: one of eight, or, for rows that are also laid out by
+// columns, four of four, 16 neighbouring lanes 4 x 4 of these, which meets all banks both ways.
+template <class In, class Core, int W, int R, int WAVES, int WAY>
 struct Staged {
-  static constexpr int kWordsOf = 8 * sizeof(In) / 4;      // of 8 entries
-  static constexpr int kAll = kChunk / R * (W / 8), kUnits = (kAll + 255) / 256;
+  static constexpr int V = R == 1 ? 8 : 4;
+  static constexpr int kWordsOf = V * sizeof(In) / 4;      // of V entries
+  static constexpr int kThreads = 64 * WAVES, kAll = kChunk / R * (W / V), kUnits = (kAll + kThreads - 1) / kThreads;
   uint32_t x[kUnits][R][kWordsOf];
 
-  static __device__ __forceinline__ void place(int i, int& row, int& col) {
-    const int u = i * 256 + (int)threadIdx.x;
+  static __device__ __forceinline__ void place(int i, int thread, int& row, int& col) {
+    const int u = i * kThreads + thread;
     if constexpr (R == 1) {
-      row = u / (W / 8);
-      col = u % (W / 8) * 8;
+      row = u / (W / V);
+      col = u % (W / V) * V;
     } else {
       static_assert(kChunk / R == 16);
       row = ((u & 3) | (u >> 2 & 12)) * R;
-      col = ((u >> 2 & 3) | (u >> 6) * 4) * 8;
+      col = ((u >> 2 & 3) | (u >> 6) * 4) * V;
     }
   }
+  static __device__ __forceinline__ bool mine(int row, int col) { return kAll % kThreads == 0 || (row < kChunk && col < W); }
   // Rows of the chunk from `lo` to `hi`, `width` entries each; `first` is the row of the chunk's earliest step, which backwards is the
   // last row.
-  __device__ __forceinline__ void load(const In* first, int64_t step, bool back, int width, int lo, int hi) {
+  __device__ __forceinline__ void load(int thread, const In* first, int64_t step, bool back, int width, int lo, int hi) {
     const __amdgpu_buffer_rsrc_t buffer = __builtin_amdgcn_make_buffer_rsrc((void*)first, 0, kBufferBytes, 0x00027000);
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
       int row, col;
-      place(i, row, col);
+      place(i, thread, row, col);
 #pragma unroll
       for (int r = 0; r < R; ++r) {
-        const bool there = row + r >= lo && row + r < hi && col < W;
+        const bool there = row + r >= lo && row + r < hi && mine(row, col);
         const int t = back ? kChunk - 1 - row - r : row + r;
         const uint32_t at = ((uint32_t)t * (uint32_t)step + (uint32_t)col) * (uint32_t)sizeof(In);
         constexpr int kEach = 4 / sizeof(In);      // entries of a word
         if constexpr (WAY == kParts) {
+          if constexpr (kWordsOf == 2) {
+            const word2 v = __builtin_amdgcn_raw_buffer_load_b64(buffer, there && col < width ? at : ~0u, 0, 0);
+            x[i][r][0] = v.x;
+            x[i][r][1] = v.y;
+          } else {
 #pragma unroll
-          for (int w = 0; w < kWordsOf; w += 4) {
-            const word4 v = __builtin_amdgcn_raw_buffer_load_b128(buffer, there && col + w * kEach < width ? at + 4 * w : ~0u, 0, 0);
+            for (int w = 0; w < kWordsOf; w += 4) {
+              const word4 v = __builtin_amdgcn_raw_buffer_load_b128(buffer, there && col + w * kEach < width ? at + 4 * w : ~0u, 0, 0);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[i][r][w + e] = v[e];
+              for (int e = 0; e < 4; ++e) x[i][r][w + e] = v[e];
+            }
           }
         } else if constexpr (WAY == kWords) {
 #pragma unroll
@@ -337,34 +367,35 @@ struct Staged {
     else return entry<In>(x[i][r][e / 2], e & 1);
   }
   template <int STRIDE>
-  __device__ __forceinline__ void store(Core (&to)[kChunk][STRIDE]) const {
+  __device__ __forceinline__ void store(int thread, Core (&to)[kChunk][STRIDE]) const {
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
       int row, col;
-      place(i, row, col);
-      if (row >= kChunk || col >= W) continue;
+      place(i, thread, row, col);
+      if (!mine(row, col)) continue;
 #pragma unroll
       for (int r = 0; r < R; ++r) {
         if constexpr (sizeof(Core) == 2) {
-          *reinterpret_cast<uint4*>(&to[row + r][col]) = uint4{x[i][r][0], x[i][r][1], x[i][r][2], x[i][r][3]};
+          if constexpr (V == 8) *reinterpret_cast<uint4*>(&to[row + r][col]) = uint4{x[i][r][0], x[i][r][1], x[i][r][2], x[i][r][3]};
+          else *reinterpret_cast<uint2*>(&to[row + r][col]) = uint2{x[i][r][0], x[i][r][1]};
         } else {
-          *reinterpret_cast<f32x4*>(&to[row + r][col]) = f32x4{at(i, r, 0), at(i, r, 1), at(i, r, 2), at(i, r, 3)};
-          *reinterpret_cast<f32x4*>(&to[row + r][col + 4]) = f32x4{at(i, r, 4), at(i, r, 5), at(i, r, 6), at(i, r, 7)};
+#pragma unroll
+          for (int e = 0; e < V; e += 4) *reinterpret_cast<f32x4*>(&to[row + r][col + e]) = f32x4{at(i, r, e), at(i, r, e + 1), at(i, r, e + 2), at(i, r, e + 3)};
         }
       }
     }
   }
   // ... by columns: four steps of an entry are 8 bytes
   template <int STRIDE>
-  __device__ __forceinline__ void store_turned(Core (*to)[STRIDE]) const {
+  __device__ __forceinline__ void store_turned(int thread, Core (*to)[STRIDE]) const {
     static_assert(R == 4 && sizeof(Core) == 2);
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
       int row, col;
-      place(i, row, col);
-      if (col >= W) continue;
+      place(i, thread, row, col);
+      if (!mine(row, col)) continue;
 #pragma unroll
-      for (int e = 0; e < 8; e += 2) {
+      for (int e = 0; e < V; e += 2) {
         const uint32_t w0 = x[i][0][e / 2], w1 = x[i][1][e / 2], w2 = x[i][2][e / 2], w3 = x[i][3][e / 2];
         *reinterpret_cast<uint2*>(&to[col + e][row]) = uint2{__builtin_amdgcn_perm(w1, w0, 0x05040100u), __builtin_amdgcn_perm(w3, w2, 0x05040100u)};
         *reinterpret_cast<uint2*>(&to[col + e + 1][row]) = uint2{__builtin_amdgcn_perm(w1, w0, 0x07060302u), __builtin_amdgcn_perm(w3, w2, 0x07060302u)};
@@ -391,31 +422,40 @@ __device__ __forceinline__ double sums_to(double x) {
   return x;
 }
 
-// STATE: only the segments' own contributions to the state, and their logarithms' sums.
-// (workgroups of a compute unit: as its LDS holds, two at least where it holds them)
-template <class Core, int DA>
-constexpr int kChunkGroups = sizeof(ChunkShared<Core, DA>) * 2 > 163840 ? 1 : 2;
-template <class In, class Core, int DA, int N_OUT, int N_STATE, bool STATE, int WAY>
-__global__ __launch_bounds__(256, (kChunkGroups<Core, DA>)) void k_linear_chunks(LinearArgs A, LinearPass P, LinearChunks C) {
+// What a launch is for: the segments' own contributions to the state and their logarithms' sums; the result; the result and its
+// products with x.
+enum { kStates = 0, kResult = 1, kResultAndDots = 2 };
+// bf16 numbers that stand for one of fp32 where a result goes (one float otherwise)
+template <class Core, int MODE>
+constexpr int kPieces = std::is_same_v<Core, float> ? 1 : MODE == kResult ? 2 : 3;
+// Waves of a SIMD: as many workgroups as a compute unit's LDS holds, up to two of 8 waves or four of 4, and no less than 128 registers.
+template <class Core, int DA, int WAVES>
+constexpr int kChunkWaves = WAVES == 8 ? (sizeof(ChunkShared<Core, DA, WAVES>) * 2 > 163840 ? 2 : 4) : sizeof(ChunkShared<Core, DA, WAVES>) * 2 > 163840 ? 1 : 2;
+
+template <class In, class Core, int DA, int WAVES, int MODE, int WAY>
+__global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_linear_chunks(LinearArgs A, LinearPass P, LinearChunks C) {
+  typedef ChunkShared<Core, DA, WAVES> Shared;
+  constexpr bool STATE = MODE == kStates;
+  constexpr int N_OUT = kPieces<Core, MODE>, N_STATE = kPieces<Core, kStates>, kSlice = Shared::kSlice;
   typedef Operand<Core> Op;
   typedef typename Op::Frag Frag;
   constexpr int kJ = DA / Op::kInner, kT = Op::kTiles, kS = kChunk / Op::kInner;
   extern __shared__ __attribute__((aligned(16))) char lds[];
-  ChunkShared<Core, DA>& S = *reinterpret_cast<ChunkShared<Core, DA>*>(lds);
+  Shared& S = *reinterpret_cast<Shared*>(lds);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4;
   const uint32_t at = by_xcd(blockIdx.x, C.blocks);
   const int slice = at % C.slices, segment = at / C.slices % C.segments;
   const int64_t bh = at / C.slices / C.segments, b = bh / A.heads, entries = (int64_t)P.da * P.dc;
   const int64_t len = __builtin_amdgcn_readfirstlane((int)steps_of(A, b));      // (below 2^31)
-  const int h = (int)(bh % A.heads), col = slice * kLinearSlice + 16 * wave;     // the wave's first column
+  const int h = (int)(bh % A.heads), col = slice * kSlice + 16 * wave;     // the wave's first column
   const In* pa = (const In*)P.a + b * P.a_seq + (h / P.a_share) * P.a_head;
   const In* pb = (const In*)P.b + b * P.b_seq + (h / P.b_share) * P.b_head;
-  const In* pc = (const In*)P.c + b * P.c_seq + (h / P.c_share) * P.c_head + slice * kLinearSlice;
+  const In* pc = (const In*)P.c + b * P.c_seq + (h / P.c_share) * P.c_head + slice * kSlice;
   const In* px = (const In*)P.x + b * P.x_seq + (h / P.x_share) * P.x_head;
   const int64_t out = b * P.out_seq + h * P.out_head;
   const int64_t begin = (int64_t)segment * C.chunks * kChunk;
   const int64_t end = segment + 1 == C.segments ? A.steps : begin + (int64_t)C.chunks * kChunk;
-  const int in_slice = min(P.dc - slice * kLinearSlice, kLinearSlice);
+  const int in_slice = min(P.dc - slice * kSlice, kSlice);
 
   f32x4 state[kJ * kT];       // rows 16 j + 4 g + r of column `col + l`
   const float* from = STATE ? nullptr : C.states ? C.states + (bh * C.states_of + segment) * entries : P.first ? P.first + bh * P.first_of * entries : nullptr;
@@ -441,35 +481,38 @@ __global__ __launch_bounds__(256, (kChunkGroups<Core, DA>)) void k_linear_chunks
 
   const int64_t inside = min(end, len);       // steps of the segment that are in the sequence end here
   const int chunks = inside > begin ? (int)((inside - begin + kChunk - 1) / kChunk) : 0;
-  typedef ChunkShared<Core, DA> Shared;
-  Staged<In, Core, DA, 1, WAY> next_a;
-  Staged<In, Core, DA, Shared::kTurned ? 4 : 1, WAY> next_b;
-  Staged<In, Core, kLinearSlice, 1, WAY> next_c;
+  Staged<In, Core, DA, 1, WAVES, WAY> next_a;
+  Staged<In, Core, DA, Shared::kTurned ? 4 : 1, WAVES, WAY> next_b;
+  Staged<In, Core, kSlice, 1, WAVES, WAY> next_c;
   float next_g = 0.0f;
   const int64_t dir = P.back ? -1 : 1;
   const auto begin_of = [&](int i) { return begin + (int64_t)(P.back ? chunks - 1 - i : i) * kChunk; };
-  const auto ask = [&](int i) {
+  const auto ask = [&](int i, int thread) {
     const int64_t t0 = begin_of(i), first = t0 + (P.back ? kChunk - 1 : 0);      // the time of row 0
     const int there = (int)min((int64_t)kChunk, inside - t0), lo = P.back ? kChunk - there : 0, hi = P.back ? kChunk : there;
-    if (!STATE) next_a.load(pa + t0 * P.a_step, P.a_step, P.back, P.da, lo, hi);
-    next_b.load(pb + t0 * P.b_step, P.b_step, P.back, P.da, lo, hi);
-    next_c.load(pc + t0 * P.c_step, P.c_step, P.back, in_slice, lo, hi);
+    if (!STATE) next_a.load(thread, pa + t0 * P.a_step, P.a_step, P.back, P.da, lo, hi);
+    next_b.load(thread, pb + t0 * P.b_step, P.b_step, P.back, P.da, lo, hi);
+    next_c.load(thread, pc + t0 * P.c_step, P.c_step, P.back, in_slice, lo, hi);
     if (wave == 0) {
       const int64_t t = first + dir * lane + (P.back ? 1 : 0);
       next_g = lane >= lo && lane < hi && t < len ? log_gate(A, b, t, h) : 0.0f;
     }
   };
-  if (chunks > 0) ask(0);
+  if (chunks > 0) ask(0, threadIdx.x);
   for (int i = 0; i < chunks; ++i) {
+    // (threads' places are worked out anew for every chunk: kept over them, they would take more registers than there are)
+    int thread = threadIdx.x;
+    asm volatile("" : "+v"(thread));
+    const int lane = thread & 63, l = lane & 15, g = lane >> 4;
     const int64_t t0 = begin_of(i), first_time = t0 + (P.back ? kChunk - 1 : 0);
     // rows of the chunk that are in the sequence: forwards its first ones, backwards its last
     const int there = (int)min((int64_t)kChunk, inside - t0), lo = P.back ? kChunk - there : 0, hi = P.back ? kChunk : there;
     if (!STATE && P.kept && t0 % kLinearSave == 0) keep(P.kept + (bh * P.kept_of + t0 / kLinearSave) * entries, 1.0f);
     __syncthreads();
-    if (!STATE) next_a.store(S.a);
-    if constexpr (Shared::kTurned) next_b.store_turned(S.turned);
-    if (!STATE || !Shared::kTurned) next_b.store(S.b);
-    next_c.store(S.c);
+    if (!STATE) next_a.store(thread, S.a);
+    if constexpr (Shared::kTurned) next_b.store_turned(thread, S.turned);
+    if (!STATE || !Shared::kTurned) next_b.store(thread, S.b);
+    next_c.store(thread, S.c);
     if (wave == 0) {      // the logarithms' sums
       const double x = sums_to(next_g < kLinearLeast ? (double)kLog2Least : (double)next_g * 1.4426950408889634);
       const double all = __shfl(x, 63);
@@ -479,51 +522,19 @@ __global__ __launch_bounds__(256, (kChunkGroups<Core, DA>)) void k_linear_chunks
       total += all;
     }
     const int first = col + 4 * g;
-    float times[4][4];      // x
-    if (!STATE && P.dots) {
-      const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc((void*)(px + t0 * P.x_step), 0, kBufferBytes, 0x00027000);
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const int row = 16 * t + l, when = P.back ? kChunk - 1 - row : row;
-        const bool here = row >= lo && row < hi;
-        if constexpr (WAY != kEntries) {
-          const uint32_t at = here ? ((uint32_t)when * (uint32_t)P.x_step + (uint32_t)first) * (uint32_t)sizeof(In) : ~0u;
-          load_four<In>(from, at, P.dc - first, C.vec_x == 4, times[t]);
-        } else {
-#pragma unroll
-          for (int r = 0; r < 4; ++r) times[t][r] = here && first + r < P.dc ? to_float(px[(t0 + when) * P.x_step + first + r]) : 0.0f;
-        }
-      }
-    }
-    if (i + 1 < chunks) ask(i + 1);
+    if (i + 1 < chunks) ask(i + 1, thread);
     __syncthreads();
     const bool busy = 16 * wave < in_slice;      // (the others help with P only)
     Frag cf[kS];       // column l's entries, a lane's steps
+    const auto columns = [&](Frag (&cf)[kS]) {
 #pragma unroll
-    for (int s = 0; s < kS; ++s)
+      for (int s = 0; s < kS; ++s)
 #pragma unroll
-      for (int t = 0; t < kT; ++t)
+        for (int t = 0; t < kT; ++t)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) cf[s][4 * t + r] = S.c[16 * (s * kT + t) + 4 * g + r][16 * wave + l];
+          for (int r = 0; r < 4; ++r) cf[s][4 * t + r] = S.c[16 * (s * kT + t) + 4 * g + r][16 * wave + l];
+    };
     if constexpr (!STATE) {
-      // P^T by tiles of 16 x 16, three for a wave: rows s, columns t, s <= t, and two of zeros that complete an operand of two tiles
-      const uint32_t tiles = wave == 0 ? 0x300010u : wave == 1 ? 0x311101u : wave == 2 ? 0x322021u : 0x332223u;
-      f32x4 score[3];
-#pragma unroll
-      for (int n = 0; n < 3; ++n) {
-        const int t = tiles >> (20 - 8 * n) & 15, s = tiles >> (16 - 8 * n) & 15;
-        score[n] = f32x4{};
-        if (s > t || 16 * t >= hi || 16 * t + 15 < lo) continue;
-#pragma unroll
-        for (int j = 0; j < kJ; ++j) score[n] = Op::mma(Op::load(&S.b[16 * s + l][0], j, g), Op::load(&S.a[16 * t + l][0], j, g), score[n]);
-        const float high = S.c_high[16 * t + l], low = S.c_low[16 * t + l];
-        const f32x4 high_s = *(const f32x4*)&S.c_high[16 * s + 4 * g], low_s = *(const f32x4*)&S.c_low[16 * s + 4 * g];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float weighted = score[n][r] * __builtin_amdgcn_exp2f((high - high_s[r]) + (low - low_s[r]));
-          score[n][r] = s < t || 4 * g + r <= l ? weighted : 0.0f;
-        }
-      }
       // what comes of the state before the chunk
       f32x4 y[4] = {};
       if (busy) {
@@ -545,13 +556,39 @@ __global__ __launch_bounds__(256, (kChunkGroups<Core, DA>)) void k_linear_chunks
           for (int r = 0; r < 4; ++r) y[t][r] *= here;
         }
       }
+      // P^T by tiles of 16 x 16: rows s, columns t, s <= t, and two of zeros that complete an operand of two tiles.  A wave's are the
+      // pairs t, s in a word, three of them or two.
+      constexpr int kTiles = WAVES == 4 ? 3 : 2;
+      constexpr uint32_t kOfWaves[8] = {WAVES == 4 ? 0x300010u : 0x0010u, WAVES == 4 ? 0x311101u : 0x1101u, WAVES == 4 ? 0x322021u : 0x20FFu,
+                                        WAVES == 4 ? 0x332223u : 0x21FFu, 0x2223u, 0x3031u, 0x32FFu, 0x33FFu};
+      uint32_t tiles = kOfWaves[0];
+#pragma unroll
+      for (int w = 1; w < WAVES; ++w)
+        if (wave == w) tiles = kOfWaves[w];
+      f32x4 score[kTiles];
+#pragma unroll
+      for (int n = 0; n < kTiles; ++n) {
+        const int pair = tiles >> (8 * (kTiles - 1 - n)) & 255, t = pair >> 4, s = pair & 15;
+        score[n] = f32x4{};
+        if (s > t || 16 * t >= hi || 16 * t + 15 < lo) continue;
+#pragma unroll
+        for (int j = 0; j < kJ; ++j) score[n] = Op::mma(Op::load(&S.b[16 * s + l][0], j, g), Op::load(&S.a[16 * t + l][0], j, g), score[n]);
+        const float high = S.c_high[16 * t + l], low = S.c_low[16 * t + l];
+        const f32x4 high_s = *(const f32x4*)&S.c_high[16 * s + 4 * g], low_s = *(const f32x4*)&S.c_low[16 * s + 4 * g];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float weighted = score[n][r] * __builtin_amdgcn_exp2f((high - high_s[r]) + (low - low_s[r]));
+          score[n][r] = s < t || 4 * g + r <= l ? weighted : 0.0f;
+        }
+      }
       __syncthreads();
       // P by rows, over a (and b, which in 16 bits is needed by columns only from here on)
       Core (*const scores)[kChunk][Shared::kScoreRow] = reinterpret_cast<Core (*)[kChunk][Shared::kScoreRow]>(&S.a[0][0]);
       static_assert(Shared::kTurned ? N_OUT <= 3 : kChunk * Shared::kScoreRow * sizeof(Core) <= sizeof(S.a));
 #pragma unroll
-      for (int n = 0; n < 3; ++n) {
-        const int t = tiles >> (20 - 8 * n) & 15, s = tiles >> (16 - 8 * n) & 15;
+      for (int n = 0; n < kTiles; ++n) {
+        const int pair = tiles >> (8 * (kTiles - 1 - n)) & 255, t = pair >> 4, s = pair & 15;
+        if (t > 3) continue;
         float left[4] = {score[n][0], score[n][1], score[n][2], score[n][3]};
 #pragma unroll
         for (int k = 0; k < N_OUT; ++k) {
@@ -560,8 +597,24 @@ __global__ __launch_bounds__(256, (kChunkGroups<Core, DA>)) void k_linear_chunks
           for (int r = 0; r < 4; ++r) left[r] -= to_float((Core)left[r]);
         }
       }
+      Four<In> times[4];      // x
+      if constexpr (MODE == kResultAndDots) {
+        const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc((void*)(px + t0 * P.x_step), 0, kBufferBytes, 0x00027000);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const int row = 16 * t + l, when = P.back ? kChunk - 1 - row : row;
+          const bool here = row >= lo && row < hi;
+          if constexpr (WAY != kEntries) {
+            const uint32_t at = here ? ((uint32_t)when * (uint32_t)P.x_step + (uint32_t)first) * (uint32_t)sizeof(In) : ~0u;
+            times[t].load(from, at, P.dc - first, C.vec_x == 4);
+          } else {
+            times[t].load(px + (t0 + when) * P.x_step + first, here ? P.dc - first : 0);
+          }
+        }
+      }
       __syncthreads();
       if (busy) {
+        columns(cf);
         const uint32_t out_size = P.wide ? 4 : sizeof(In);
         char* const earliest = (char*)P.out + out_size * (out + t0 * P.out_step);
         const __amdgpu_buffer_rsrc_t to = __builtin_amdgcn_make_buffer_rsrc(earliest, 0, kBufferBytes, 0x00027000);
@@ -584,7 +637,7 @@ __global__ __launch_bounds__(256, (kChunkGroups<Core, DA>)) void k_linear_chunks
             for (int r = 0; r < 4; ++r)
               if (first + r < P.dc) store_result<In>(P, out + (t0 + when) * P.out_step + first + r, y[t][r]);
           }
-          if (P.dots) {
+          if constexpr (MODE == kResultAndDots) {
             float d = 0.0f;
 #pragma unroll
             for (int r = 0; r < 4; ++r) d = fmaf(y[t][r], times[t][r], d);      // (what is not there is zero)
@@ -594,7 +647,7 @@ __global__ __launch_bounds__(256, (kChunkGroups<Core, DA>)) void k_linear_chunks
           }
         }
       }
-      if (P.dots) {
+      if constexpr (MODE == kResultAndDots) {
         __syncthreads();
         if (wave == 0 && lane >= lo && lane < hi) {
           float d = S.dots[0][lane];
@@ -605,6 +658,7 @@ __global__ __launch_bounds__(256, (kChunkGroups<Core, DA>)) void k_linear_chunks
       if (i + 1 == chunks && (C.states || !P.last) && !P.kept) break;      // nobody reads the state
     }
     if (!busy) continue;
+    if constexpr (STATE) columns(cf);
     const float all = __builtin_amdgcn_exp2f(S.c_high[kChunk - 1] + S.c_low[kChunk - 1]);
 #pragma unroll
     for (int j = 0; j < kJ * kT; ++j)
@@ -643,8 +697,8 @@ __global__ __launch_bounds__(256, (kChunkGroups<Core, DA>)) void k_linear_chunks
   // zeros behind the sequence
   const int64_t zero = max(begin, len);
   const int width = in_slice;
-  for (int64_t e = threadIdx.x; e < (end - zero) * width; e += 256)
-    store_result<In>(P, out + (zero + e / width) * P.out_step + slice * kLinearSlice + e % width, 0.0f);
+  for (int64_t e = threadIdx.x; e < (end - zero) * width; e += 64 * WAVES)
+    store_result<In>(P, out + (zero + e / width) * P.out_step + slice * kSlice + e % width, 0.0f);
   if (P.kept && (len == 0 ? segment == 0 : begin < len && len <= end))
     keep(P.kept + (bh * P.kept_of + (len + kLinearSave - 1) / kLinearSave) * entries, 1.0f);
   if (P.last && !C.states) keep(P.last + bh * entries, P.back && len > 0 ? linear_decay(log_gate(A, b, 0, h)) : 1.0f);

@@ -51,7 +51,7 @@ bool strides_ok(const choco_linear_config& c, const int64_t s[3], int64_t heads,
 }
 
 int64_t pieces_of(const choco_linear_config& c) { return (c.steps + kLinearSave - 1) / kLinearSave; }
-int slices_of(int dim) { return (dim + kLinearSlice - 1) / kLinearSlice; }
+int slices_of(int dim, int slice = kLinearSlice) { return (dim + slice - 1) / slice; }
 int64_t rows_of(const choco_linear_config& c) { return c.batch * c.heads; }
 
 // Every launch of a call fits, and what it keeps stays far from 64 bits.
@@ -143,32 +143,41 @@ int width_of(const Rows& r, size_t size, int most, const choco_linear_config& c)
 // Up to so many steps are taken one by one.
 constexpr int64_t kStepByStep = 8;
 
-template <class In, class Core, int DA, int N_OUT, int N_STATE, bool STATE, int WAY>
-int launch_chunks(const choco_linear_config& c, const LinearArgs& A, const LinearPass& P, LinearChunks C) {
-  const size_t lds = sizeof(ChunkShared<Core, DA>);
-  const auto kernel = k_linear_chunks<In, Core, DA, N_OUT, N_STATE, STATE, WAY>;
+template <class In, int DA, int WAVES, int MODE, int WAY>
+int launch_chunks(const choco_linear_config& c, const LinearArgs& A, const LinearPass& P, const LinearChunks& C) {
+  typedef std::conditional_t<std::is_same_v<In, bf16_t>, bf16_t, float> Core;
+  const size_t lds = sizeof(ChunkShared<Core, DA, WAVES>);
+  const auto kernel = k_linear_chunks<In, Core, DA, WAVES, MODE, WAY>;
   if (lds > 65536) {
     static const hipError_t allowed = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     TRY_HIP(allowed);
   }
-  C.slices = slices_of(P.dc);
-  C.blocks = (uint32_t)(rows_of(c) * C.segments * C.slices);
-  kernel<<<dim3(C.blocks), 256, lds, (hipStream_t)c.stream>>>(A, P, C);
+  kernel<<<dim3(C.blocks), 64 * WAVES, lds, (hipStream_t)c.stream>>>(A, P, C);
   TRY_HIP(hipGetLastError());
   return CHOCO_OK;
 }
-// N_OUT: bf16 numbers for one of fp32 where the result goes
-template <class In, int N_OUT, bool STATE>
-int run_chunks(const choco_linear_config& c, const LinearArgs& A, const LinearPass& P, const LinearChunks& C) {
-  const auto with_way = [&](auto dim, auto way) -> int {
-    constexpr int DA = decltype(dim)::value, WAY = decltype(way)::value;
-    if constexpr (std::is_same_v<In, bf16_t>) return launch_chunks<In, bf16_t, DA, N_OUT, 3, STATE, WAY>(c, A, P, C);
-    else return launch_chunks<In, float, DA, 1, 1, STATE, WAY>(c, A, P, C);
+// Columns of a result that a workgroup takes: 16 a wave, four waves where that is enough, else eight (but four where eight's columns
+// leave no room in LDS).
+int slice_of(const choco_linear_config& c, const LinearPass& P) { return P.dc <= 64 || (c.type != CHOCO_BF16 && P.da > 128) ? 64 : 128; }
+
+template <class In, int MODE>
+int run_chunks(const choco_linear_config& c, const LinearArgs& A, const LinearPass& P, LinearChunks C) {
+  const int slice = slice_of(c, P);
+  C.slices = slices_of(P.dc, slice);
+  C.blocks = (uint32_t)(rows_of(c) * C.segments * C.slices);
+  const auto with_way = [&](auto dim, auto waves, auto way) -> int {
+    constexpr int DA = decltype(dim)::value, WAVES = decltype(waves)::value;
+    if constexpr (WAVES == 8 && DA > 128 && !std::is_same_v<In, bf16_t>) return CHOCO_E_UNSUPPORTED;     // (slice_of does not say so)
+    else return launch_chunks<In, DA, WAVES, MODE, decltype(way)::value>(c, A, P, C);
+  };
+  const auto with_waves = [&](auto dim, auto waves) -> int {
+    if (C.way == kParts) return with_way(dim, waves, std::integral_constant<int, kParts>{});
+    if (C.way == kWords) return with_way(dim, waves, std::integral_constant<int, kWords>{});
+    return with_way(dim, waves, std::integral_constant<int, kEntries>{});
   };
   const auto with_dim = [&](auto dim) -> int {
-    if (C.way == kParts) return with_way(dim, std::integral_constant<int, kParts>{});
-    if (C.way == kWords) return with_way(dim, std::integral_constant<int, kWords>{});
-    return with_way(dim, std::integral_constant<int, kEntries>{});
+    if (slice == 64) return with_waves(dim, std::integral_constant<int, 4>{});
+    return with_waves(dim, std::integral_constant<int, 8>{});
   };
   if (P.da <= 64) return with_dim(std::integral_constant<int, 64>{});
   if (P.da <= 128) return with_dim(std::integral_constant<int, 128>{});
@@ -209,7 +218,7 @@ LinearChunks chunks_of(const choco_linear_config& c, const LinearPass& P, const 
 // The states before all segments.
 template <class T>
 int run_states(const choco_linear_config& c, const LinearArgs& A, const LinearPass& P, const LinearChunks& C, const float* first, float* last) {
-  if (const int rc = run_chunks<T, 1, true>(c, A, P, C)) return rc;
+  if (const int rc = run_chunks<T, kStates>(c, A, P, C)) return rc;
   const int64_t entries = (int64_t)P.da * P.dc;
   const dim3 grid((uint32_t)std::min<int64_t>(65536, rows_of(c) * ((entries + 255) / 256)));
   k_linear_scan<<<grid, 256, 0, (hipStream_t)c.stream>>>(A, C.states, C.totals, C.segments, entries, first, last, P.back);
@@ -220,7 +229,7 @@ int run_states(const choco_linear_config& c, const LinearArgs& A, const LinearPa
 // Segments of a forward pass in chunks: as many as give so many workgroups, none shorter than kLinearSave steps.
 constexpr int64_t kWorkgroups = 1024;
 void segments_of(const choco_linear_config& c, int32_t& segments, int32_t& chunks) {
-  const int64_t all = (c.steps + kChunk - 1) / kChunk, alone = rows_of(c) * slices_of(c.dim_v), least = kLinearSave / kChunk;
+  const int64_t all = (c.steps + kChunk - 1) / kChunk, alone = rows_of(c) * slices_of(c.dim_v, 128), least = kLinearSave / kChunk;
   int64_t each = std::max(all, least);
   if (alone < kWorkgroups / 2 && all > least) each = std::max(least, (all * alone + kWorkgroups - 1) / kWorkgroups);
   each = (each + least - 1) / least * least;
@@ -240,7 +249,7 @@ int run_forward(const choco_linear_config& c, const LinearArgs& A, LinearPass P,
     C.states_of = C.segments;
     if (const int rc = run_states<T>(c, A, P, C, P.first, P.last)) return rc;
   }
-  return run_chunks<T, 2, false>(c, A, P, C);
+  return run_chunks<T, kResult>(c, A, P, C);
 }
 
 template <class T>
@@ -279,7 +288,7 @@ int run_backward(const choco_linear_config& c, const LinearArgs& A, const void* 
         C.states = const_cast<float*>(states);
         C.states_of = states_of;
       }
-      if (const int rc = P.dots ? run_chunks<T, 3, false>(c, A, P, C) : run_chunks<T, 2, false>(c, A, P, C)) return rc;
+      if (const int rc = P.dots ? run_chunks<T, kResultAndDots>(c, A, P, C) : run_chunks<T, kResult>(c, A, P, C)) return rc;
     }
     if (heads == c.heads) return CHOCO_OK;
     const int64_t count = c.batch * c.steps * heads * dim;
@@ -326,7 +335,10 @@ int run_backward(const choco_linear_config& c, const LinearArgs& A, const void* 
   G.q_dots = q_dots; G.k_dots = k_dots;
   G.saved = saved; G.later = later; G.dlast = dlast;
   G.saved_of = pieces + 1; G.later_of = pieces;
-  G.q_slices = G.k_slices = slices_of(c.dim_k);
+  LinearPass of_k{};
+  of_k.da = c.dim_v;
+  of_k.dc = c.dim_k;
+  G.q_slices = G.k_slices = slices_of(c.dim_k, stepwise ? kLinearSlice : slice_of(c, of_k));
   G.state = (int32_t)state;
   G.pieces = pieces;
   G.sums = !c.gate_steps;
