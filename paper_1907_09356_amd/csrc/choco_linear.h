@@ -203,10 +203,18 @@ struct LinearChunks {
   int32_t vec_out, vec_x;   // entries that a store, or a load of x, takes
 };
 
-// One XCD's workgroups take neighbouring parts of the work: slices of the same head share their a and b in its L2.
-__device__ __forceinline__ uint32_t by_xcd(uint32_t block, uint32_t blocks) {
-  const uint32_t x = block & 7, each = blocks >> 3, more = blocks & 7;
-  return x * each + min(x, more) + (block >> 3);
+// Workgroups go to the eight XCDs in turn: segments of a head one after the other, so that those a sequence does not reach are spread over all
+// of them, and slices of one segment eight apart, so that they share their a and b in an L2.  (2 x 32,768 x 16 x 128 in bf16 541 us;
+// neighbours on one XCD 540, but with lengths from a half on 496 | 494; heads one after the other 562 | 511.)
+struct ChunkPlace {
+  int64_t bh;
+  int segment, slice;
+  bool there;
+};
+__device__ __forceinline__ ChunkPlace chunk_place(const LinearArgs& A, const LinearChunks& C) {
+  const uint32_t rows = (uint32_t)(A.batch * A.heads), each = 8 * C.slices, in = blockIdx.x % each;
+  const uint32_t unit = blockIdx.x / each * 8 + (in & 7);
+  return {unit / C.segments, (int)(unit % C.segments), (int)(in >> 3), unit < rows * (uint32_t)C.segments};
 }
 
 template <class Core, int DA, int WAVES>
@@ -443,9 +451,10 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
   extern __shared__ __attribute__((aligned(16))) char lds[];
   Shared& S = *reinterpret_cast<Shared*>(lds);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4;
-  const uint32_t at = by_xcd(blockIdx.x, C.blocks);
-  const int slice = at % C.slices, segment = at / C.slices % C.segments;
-  const int64_t bh = at / C.slices / C.segments, b = bh / A.heads, entries = (int64_t)P.da * P.dc;
+  const ChunkPlace place = chunk_place(A, C);
+  if (!place.there) return;
+  const int slice = place.slice, segment = place.segment;
+  const int64_t bh = place.bh, b = bh / A.heads, entries = (int64_t)P.da * P.dc;
   const int64_t len = __builtin_amdgcn_readfirstlane((int)steps_of(A, b));      // (below 2^31)
   const int h = (int)(bh % A.heads), col = slice * kSlice + 16 * wave;     // the wave's first column
   const In* pa = (const In*)P.a + b * P.a_seq + (h / P.a_share) * P.a_head;
@@ -713,11 +722,22 @@ __global__ __launch_bounds__(256) void k_linear_scan(LinearArgs A, float* states
     if (e >= entries) continue;
     float s = first ? first[bh * entries + e] : 0.0f;
     float* p = states + bh * segments * entries + e;
-    for (int i = 0; i < segments; ++i) {
-      const int at = back ? segments - 1 - i : i;
-      const float own = p[at * entries];
-      p[at * entries] = s;
-      s = fmaf(s, __builtin_amdgcn_exp2f((float)totals[bh * segments + at]), own);
+    constexpr int kAhead = 16;      // (asked for together: a store may be of the next one's entry, for all that the compiler knows)
+    for (int i = 0; i < segments; i += kAhead) {
+      float own[kAhead], decay[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        if (i + k < segments) {
+          const int at = back ? segments - 1 - i - k : i + k;
+          own[k] = p[at * entries];
+          decay[k] = __builtin_amdgcn_exp2f((float)totals[bh * segments + at]);
+        }
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        if (i + k < segments) {
+          p[(back ? segments - 1 - i - k : i + k) * entries] = s;
+          s = fmaf(s, decay[k], own[k]);
+        }
     }
     if (last) last[bh * entries + e] = back && steps_of(A, b) > 0 ? s * linear_decay(log_gate(A, b, 0, (int)(bh % A.heads))) : s;
   }
@@ -762,7 +782,18 @@ __global__ __launch_bounds__(kLinearSave) void k_linear_gates(LinearArgs A, Line
   const float* later = whole ? G.later + (bh * G.later_of + piece) * G.state : G.dlast ? G.dlast + bh * G.state : nullptr;
   if (later && piece * kLinearSave < len) {
     const float* s = G.saved + (bh * G.saved_of + piece + 1) * G.state;
-    for (int i = threadIdx.x; i < G.state; i += kLinearSave) past += (double)later[i] * (double)s[i];
+    int i = threadIdx.x;
+    for (; i + 7 * kLinearSave < G.state; i += 8 * kLinearSave) {      // (eight at a time under way)
+      float x[8], y[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        x[k] = later[i + k * kLinearSave];
+        y[k] = s[i + k * kLinearSave];
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) past += (double)x[k] * (double)y[k];
+    }
+    for (; i < G.state; i += kLinearSave) past += (double)later[i] * (double)s[i];
     if (whole) past *= (double)linear_decay(log_gate(A, b, end, h));
   }
   past = wave_sum(past);

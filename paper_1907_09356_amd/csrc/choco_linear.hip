@@ -58,7 +58,7 @@ int64_t rows_of(const choco_linear_config& c) { return c.batch * c.heads; }
 bool linear_fits(const choco_linear_config& c) {
   const double rows = (double)rows_of(c), pieces = (double)pieces_of(c) + 1.0;
   if (rows * pieces * c.dim_k * c.dim_v > 1125899906842624.0 || rows * (double)c.steps * 512.0 > 1125899906842624.0) return false;
-  return launch_fits(rows * pieces * slices_of(CHOCO_LINEAR_MAX_DIM), 256);
+  return launch_fits((rows * pieces + 8.0) * slices_of(CHOCO_LINEAR_MAX_DIM), 512);
 }
 
 struct LinearLayout {
@@ -164,7 +164,7 @@ template <class In, int MODE>
 int run_chunks(const choco_linear_config& c, const LinearArgs& A, const LinearPass& P, LinearChunks C) {
   const int slice = slice_of(c, P);
   C.slices = slices_of(P.dc, slice);
-  C.blocks = (uint32_t)(rows_of(c) * C.segments * C.slices);
+  C.blocks = (uint32_t)((rows_of(c) * C.segments + 7) / 8 * 8 * C.slices);
   const auto with_way = [&](auto dim, auto waves, auto way) -> int {
     constexpr int DA = decltype(dim)::value, WAVES = decltype(waves)::value;
     if constexpr (WAVES == 8 && DA > 128 && !std::is_same_v<In, bf16_t>) return CHOCO_E_UNSUPPORTED;     // (slice_of does not say so)
@@ -226,7 +226,8 @@ int run_states(const choco_linear_config& c, const LinearArgs& A, const LinearPa
   return CHOCO_OK;
 }
 
-// Segments of a forward pass in chunks: as many as give so many workgroups, none shorter than kLinearSave steps.
+// Segments of a forward pass in chunks: as many as give so many workgroups, none shorter than kLinearSave steps.  (2 x 32,768 x 16 x 128
+// in bf16, us, with lengths from a half on: 512 580 | 519, 1024 572 | 519, 2048 594 | 551, 4096 680 | 611.)
 constexpr int64_t kWorkgroups = 1024;
 void segments_of(const choco_linear_config& c, int32_t& segments, int32_t& chunks) {
   const int64_t all = (c.steps + kChunk - 1) / kChunk, alone = rows_of(c) * slices_of(c.dim_v, 128), least = kLinearSave / kChunk;

@@ -205,6 +205,11 @@ __global__ __launch_bounds__(256) void k_muon_start(MuonArgs A) {
 }
 
 // ---- products ----
+// One XCD's workgroups make neighbouring tiles, whose operands its L2 then holds.
+__device__ __forceinline__ uint32_t by_xcd(uint32_t block, uint32_t blocks) {
+  const uint32_t x = block & 7, each = blocks >> 3, more = blocks & 7;
+  return x * each + min(x, more) + (block >> 3);
+}
 enum { kGram = 0, kSquare = 1, kApply = 2 };
 
 // Tile `at` of the lower triangle, row after row: its row and column.
@@ -220,17 +225,22 @@ __device__ __forceinline__ void to_lds(const void* from, void* to) {
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
 }
 
-// A workgroup makes a tile of TILE x TILE entries, a wave a quarter.  A step along the inner index takes 32 entries of TILE rows of both
-// operands, high and low, into one of two buffers while the other one's are multiplied.  In a buffer a row's four 16-byte
-// parts are exchanged by bits 2 and 3 of its number, so that 16 lanes that read one part of 16 rows meet 16 different banks.
+// A workgroup makes a tile of TILE x TILE entries.  A step along the inner index takes 32 entries of TILE rows of both operands, high and
+// low, into one of two buffers while the other one's are multiplied.  In a buffer a row's four 16-byte parts are exchanged by bits 2
+// and 3 of its number, so that 16 lanes that read one part of 16 rows meet 16 different banks.
+//   TILE 128: a wave makes a quarter of the tile, and loads one plane of the operands for all.
+//   TILE 64, where the tiles are too few to fill the card: every wave makes the whole tile, of every fourth step, from buffers of its own,
+// so that four steps are under way and nobody waits for anybody; the four sums are added up at the end.
 template <int KIND, int TILE>
-__global__ __launch_bounds__(256, 2) void k_muon_product(MuonArgs A) {
-  constexpr int W = TILE / 32;      // 16-row parts of a wave's side
-  constexpr int kLoads = TILE / 16; // of a wave, a step
-  __shared__ __attribute__((aligned(1024))) f16_t lds[2][4][TILE][32];    // left high, left low, right high, right low
+__global__ __launch_bounds__(256, TILE == 128 ? 2 : 1) void k_muon_product(MuonArgs A) {
+  constexpr bool ALONE = TILE == 64;
+  constexpr int W = 4;                                // 16-row parts of a wave's side
+  constexpr int kLoads = TILE / 16 * (ALONE ? 4 : 1); // of a wave, a step
+  __shared__ __attribute__((aligned(1024))) f16_t lds[2 * (ALONE ? 4 : 1)][4][TILE][32];    // left high, left low, right high, right low
   constexpr uint32_t MuonShape::*kBegin = KIND == kApply ? &MuonShape::apply_begin : &MuonShape::gram_begin;
-  const MuonShape S = shape_of<kBegin>(A, blockIdx.x);
-  const uint32_t at = blockIdx.x - S.*kBegin, tiles = KIND == kApply ? S.apply_tiles : S.gram_tiles, in = at % tiles;
+  const uint32_t tile_at = by_xcd(blockIdx.x, gridDim.x);
+  const MuonShape S = shape_of<kBegin>(A, tile_at);
+  const uint32_t at = tile_at - S.*kBegin, tiles = KIND == kApply ? S.apply_tiles : S.gram_tiles, in = at % tiles;
   const int which = (int)(at / tiles);
   const MuonPlanes P = planes_of(A, S, which);
   uint32_t ti, tj;
@@ -246,35 +256,38 @@ __global__ __launch_bounds__(256, 2) void k_muon_product(MuonArgs A) {
   const int64_t ld = KIND == kGram ? S.b_ld : S.a_ld;
   const int ms = S.a, ns = KIND == kApply ? S.b : S.a;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4;
-  const int m0 = ti * TILE, n0 = tj * TILE, mw = (wave & 1) * (TILE / 2), nw = (wave >> 1) * (TILE / 2);
+  const int m0 = ti * TILE, n0 = tj * TILE, mw = ALONE ? 0 : (wave & 1) * (TILE / 2), nw = ALONE ? 0 : (wave >> 1) * (TILE / 2);
 
-  // what a lane loads each step: wave w plane w's rows, 16 a load
-  const f16_t* from = (wave < 2 ? left : right) + (wave & 1) * (wave < 2 ? left_low : right_low);
-  const int first = wave < 2 ? m0 : n0, rows = wave < 2 ? ms : ns;
+  // what a lane loads each step, 16 rows a load: of plane `wave`, or of all four
   const f16_t* source[kLoads];
 #pragma unroll
   for (int i = 0; i < kLoads; ++i) {
-    const int row = 16 * i + (lane >> 2), part = (lane & 3) ^ ((row >> 2) & 3);
-    source[i] = from + (int64_t)min(first + row, rows - 1) * ld + 8 * part;
+    const int p = ALONE ? i / (TILE / 16) : wave, row = 16 * (i % (TILE / 16)) + (lane >> 2), part = (lane & 3) ^ ((row >> 2) & 3);
+    const f16_t* from = (p < 2 ? left : right) + (p & 1) * (p < 2 ? left_low : right_low);
+    source[i] = from + (int64_t)min((p < 2 ? m0 : n0) + row, (p < 2 ? ms : ns) - 1) * ld + 8 * part;
   }
+  const int buffers = ALONE ? 2 * wave : 0;
   const auto load = [&](int64_t k, int buffer) {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) to_lds(source[i] + k, &lds[buffer][wave][16 * i][0]);
+    for (int i = 0; i < kLoads; ++i)
+      to_lds(source[i] + k, &lds[buffers + buffer][ALONE ? i / (TILE / 16) : wave][16 * (i % (TILE / 16))][0]);
   };
   const int swap = 8 * (g ^ ((l >> 2) & 3));
+  constexpr int kStride = ALONE ? 128 : 32;
   float4_t acc[W][W] = {};
-  load(0, 0);
-  for (int64_t k = 0; k < ld; k += 32) {
-    const int buffer = (k >> 5) & 1;
-    // this step's parts are there for everybody, and everybody is done with the other buffer
+  int64_t k = ALONE ? 32 * wave : 0;
+  if (k < ld) load(k, 0);
+  for (int buffer = 0; k < ld; k += kStride, buffer ^= 1) {
+    // this step's parts are there (for everybody), and (everybody is) done with the other buffer
     __builtin_amdgcn_s_waitcnt(0);
-    __syncthreads();
+    if (ALONE) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    else __syncthreads();
     half8 f[4][W];
 #pragma unroll
     for (int p = 0; p < 4; ++p)
 #pragma unroll
-      for (int i = 0; i < W; ++i) f[p][i] = *(const half8*)&lds[buffer][p][(p < 2 ? mw : nw) + 16 * i + l][swap];
-    if (k + 32 < ld) load(k + 32, buffer ^ 1);
+      for (int i = 0; i < W; ++i) f[p][i] = *(const half8*)&lds[buffers + buffer][p][(p < 2 ? mw : nw) + 16 * i + l][swap];
+    if (k + kStride < ld) load(k + kStride, buffer ^ 1);
 #pragma unroll
     for (int i = 0; i < W; ++i)
 #pragma unroll
@@ -288,15 +301,23 @@ __global__ __launch_bounds__(256, 2) void k_muon_product(MuonArgs A) {
   // rows and by columns, 8 entries a lane.
   __syncthreads();
   float* const tile = (float*)&lds[0][0][0][0];
-  static_assert(sizeof(lds) >= TILE * TILE * sizeof(float));
+  static_assert(sizeof(lds) >= (ALONE ? 4 : 1) * TILE * TILE * sizeof(float));
   const auto place = [](int m, int n) { return m * TILE + (n ^ ((m >> 1) & (TILE / 2 - 4))); };
+  constexpr float kScale = KIND == kSquare ? kMuonDown * kMuonC : kMuonDown;
 #pragma unroll
   for (int i = 0; i < W; ++i)
 #pragma unroll
     for (int j = 0; j < W; ++j)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) tile[place(mw + 16 * i + 4 * g + r, nw + 16 * j + l)] = acc[i][j][r] * (KIND == kSquare ? kMuonDown * kMuonC : kMuonDown);
+      for (int r = 0; r < 4; ++r) tile[(ALONE ? wave * TILE * TILE : 0) + place(mw + 16 * i + 4 * g + r, nw + 16 * j + l)] = acc[i][j][r] * kScale;
   __syncthreads();
+  if (ALONE) {
+    for (int e = threadIdx.x * 4; e < TILE * TILE; e += 1024) {
+      float4_t* const sum = (float4_t*)(tile + e);
+      *sum = (*sum + sum[TILE * TILE / 4]) + (sum[2 * (TILE * TILE / 4)] + sum[3 * (TILE * TILE / 4)]);
+    }
+    __syncthreads();
+  }
   constexpr int kParts = TILE / 8;
   constexpr bool kAdds = KIND != kGram;     // a X or b P
   const bool last = KIND == kApply && A.last;
@@ -324,7 +345,7 @@ __global__ __launch_bounds__(256, 2) void k_muon_product(MuonArgs A) {
     float x[8];
     *(float4_t*)&x[0] = *(const float4_t*)&tile[place(i, j)];
     *(float4_t*)&x[4] = *(const float4_t*)&tile[place(i, j + 4)];
-    if (KIND != kApply && ti == tj) {     // the lower triangle's mirror image here too: a matrix's bits do not depend on the tiles' size
+    if (KIND != kApply && ti == tj) {     // the lower triangle's mirror image here too: P and Q are symmetric to the bit
 #pragma unroll
       for (int e = 0; e < 8; ++e)
         if (j + e > i) x[e] = tile[place(j + e, i)];

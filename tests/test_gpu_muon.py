@@ -286,7 +286,8 @@ def test_streams_and_graphs():
 
 
 def test_many_workers_of_a_large_matrix_in_rounds():
-    # operands of 130 workers are more than a round's: each worker's result is that of the worker alone
+    # operands of 130 workers are more than a round's: each worker's result is that of the worker alone (in tiles of another size, whose
+    # sums are in another order: both are off by what is allowed at most)
     n, r, c = 130, 700, 800
     X = torch.zeros((n, r * c), device="cuda")
     G = torch.empty((n, r * c), device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(4))
@@ -295,4 +296,7 @@ def test_many_workers_of_a_large_matrix_in_rounds():
     for w in (0, 64, n - 1):
         one = torch.zeros((1, r * c), device="cuda")
         T.Muon(one, r * c, ([0], [r], [c])).step(G[w:w + 1].contiguous(), 1.0)
-        assert torch.equal(one[0], X[w])
+        assert float((one[0] - X[w]).double().norm()) <= 2 * allowed(r, c, 5)
+        alike = torch.zeros((n, r * c), device="cuda")
+        T.Muon(alike, r * c, ([0], [r], [c])).step(G[w:w + 1].expand(n, -1).contiguous(), 1.0)
+        assert torch.equal(alike, X[w:w + 1].expand(n, -1))
