@@ -219,7 +219,7 @@ typedef struct {
   void* stream;
 } choco_orthogonalize_config;
 
-/* Bytes of device workspace (256-byte aligned). */
+/* Bytes of device workspace (256-byte aligned); may be 0. */
 int choco_orthogonalize_workspace_bytes(const choco_orthogonalize_config* cfg, size_t* bytes_host);
 /* x_dev is not written, and y_dev may not overlap it.  CHOCO_E_UNSUPPORTED: more work than one launch holds. */
 int choco_orthogonalize(const choco_orthogonalize_config* cfg, const void* x_dev, float* y_dev, void* workspace_dev,

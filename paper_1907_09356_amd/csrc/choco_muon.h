@@ -204,13 +204,53 @@ __global__ __launch_bounds__(256) void k_muon_start(MuonArgs A) {
   }
 }
 
-// ---- products ----
-// One XCD's workgroups make neighbouring tiles, whose operands its L2 then holds.
-__device__ __forceinline__ uint32_t by_xcd(uint32_t block, uint32_t blocks) {
-  const uint32_t x = block & 7, each = blocks >> 3, more = blocks & 7;
-  return x * each + min(x, more) + (block >> 3);
+// ---- small matrices ----
+// A workgroup takes a whole matrix, whose operands stay in LDS from the first iteration to the last: rows end on a multiple of 32 entries
+// and 8 more, which are 4 banks modulo 16, so that 16 lanes that read 16 bytes of 16 rows meet all banks.
+constexpr int kWholeWaves = 16;
+constexpr int64_t kWholeBytes = 160 * 1024 - 256;
+constexpr int kWholeTiles = 4;       // most 16 x 16 tiles of X that a wave makes
+inline __host__ __device__ int64_t whole_bytes(int64_t a, int64_t b) {
+  const int64_t ra = (a + 31) / 32 * 32, rb = (b + 31) / 32 * 32;
+  return 4 * (ra * (rb + 8) + rb * (ra + 8) + 2 * ra * (ra + 8));
 }
-enum { kGram = 0, kSquare = 1, kApply = 2 };
+// D tile of 16 x 16: rows m0 of one operand with rows n0 of another, both with their low planes so many entries behind.
+__device__ __forceinline__ float4_t whole_product(const f16_t* left, int64_t left_low, int left_ld, const f16_t* right, int64_t right_low, int right_ld,
+                                                  int m0, int n0, int inner, int l, int g) {
+  float4_t acc[3] = {};       // (apart, so that the instructions of a step do not wait for each other)
+  const f16_t *pl = left + (m0 + l) * left_ld + 8 * g, *pr = right + (n0 + l) * right_ld + 8 * g;
+#pragma unroll 2
+  for (int k = 0; k < inner; k += 32) {
+    const half8 lh = *(const half8*)(pl + k), ll = *(const half8*)(pl + left_low + k);
+    const half8 rh = *(const half8*)(pr + k), rl = *(const half8*)(pr + right_low + k);
+    acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ll, rh, acc[0], 0, 0, 0);
+    acc[1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lh, rl, acc[1], 0, 0, 0);
+    acc[2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lh, rh, acc[2], 0, 0, 0);
+  }
+  return (acc[0] + acc[1]) + acc[2];
+}
+typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+// Four entries that are next to one another.
+__device__ __forceinline__ void whole_place(f16_t* to, int64_t low, const float4_t& x) {
+  half4 high, less;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    high[r] = (f16_t)x[r];
+    less[r] = (f16_t)(x[r] - (float)high[r]);
+  }
+  *(half4*)to = high;
+  *(half4*)(to + low) = less;
+}
+__device__ __forceinline__ float4_t whole_entries(const f16_t* from, int64_t low) {
+  const half4 high = *(const half4*)from, less = *(const half4*)(from + low);
+  return float4_t{(float)high[0], (float)high[1], (float)high[2], (float)high[3]} + float4_t{(float)less[0], (float)less[1], (float)less[2], (float)less[3]};
+}
+__device__ __forceinline__ void whole_place(f16_t* to, int64_t low, float x) {
+  f16_t high, less;
+  split(x, high, less);
+  to[0] = high;
+  to[low] = less;
+}
 
 // Tile `at` of the lower triangle, row after row: its row and column.
 __device__ __forceinline__ void triangle(uint32_t at, uint32_t& i, uint32_t& j) {
@@ -219,6 +259,132 @@ __device__ __forceinline__ void triangle(uint32_t at, uint32_t& i, uint32_t& j) 
   while ((i + 1) * (i + 2) / 2 <= at) ++i;
   j = at - i * (i + 1) / 2;
 }
+
+template <class T, bool STEP>
+__global__ __launch_bounds__(64 * kWholeWaves) void k_muon_whole(MuonArgs A, int iterations) {
+  extern __shared__ __attribute__((aligned(16))) char whole_lds[];
+  __shared__ double part[kWholeWaves];
+  constexpr int kThreads = 64 * kWholeWaves;
+  const MuonShape S = shape_of<&MuonShape::start_begin>(A, blockIdx.x);
+  const int which = (int)(blockIdx.x - S.start_begin), worker = S.first + which;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4;
+  const int ra = (S.a + 31) / 32 * 32, rb = (S.b + 31) / 32 * 32, a_ld = ra + 8, b_ld = rb + 8;
+  f16_t* const x = (f16_t*)whole_lds;
+  const int64_t x_low = (int64_t)ra * b_ld, xt_low = (int64_t)rb * a_ld, p_low = (int64_t)ra * a_ld;
+  f16_t *const xt = x + 2 * x_low, *const p = xt + 2 * xt_low, *const q = p + 2 * p_low;
+  const bool tall = S.rows > S.cols;
+  const float scale = STEP && A.grad_scale ? A.grad_scale[worker] : 1.0f;
+  if (STEP && !__builtin_isfinite(scale)) return;
+  const int entries = S.rows * S.cols;
+  float* const moment = A.moments + S.moment + (int64_t)worker * entries;
+  // entry threadIdx.x and every kThreads-th from there, row and column counted on; all loads are under way together
+  constexpr int kEach = 256 * kWholeTiles / 64;      // (as many as a wave's part of X has for a lane)
+  const int step_rows = kThreads / S.cols, step_cols = kThreads % S.cols, r0 = (int)threadIdx.x / S.cols, c0 = (int)threadIdx.x % S.cols;
+  const auto for_entries = [&](auto&& fn) {
+    int r = r0, c = c0;
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      fn(k, (int)threadIdx.x + k * kThreads < entries, r, c);
+      c += step_cols;
+      r += step_rows;
+      if (c >= S.cols) {
+        c -= S.cols;
+        ++r;
+      }
+    }
+  };
+  float u[kEach], before[kEach];
+  for_entries([&](int k, bool there, int r, int c) {
+    u[k] = there ? source_entry<T>(A, S, which, r, c) : 0.0f;
+    if (STEP) before[k] = there ? moment[r * S.cols + c] : 0.0f;
+  });
+  for (int64_t e = threadIdx.x; e < (x_low + xt_low) / 4; e += kThreads) ((float4_t*)x)[e] = float4_t{};     // zeros behind the rows
+  double sum = 0.0;
+  for_entries([&](int k, bool there, int r, int c) {
+    if (STEP) {
+      const float grad = u[k] * scale, now = fmaf(A.momentum, before[k], grad);
+      if (there) moment[r * S.cols + c] = now;
+      u[k] = A.nesterov ? fmaf(A.momentum, now, grad) : now;
+    }
+    sum += (double)u[k] * (double)u[k];
+  });
+  for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
+  if (lane == 0) part[wave] = sum;
+  __syncthreads();
+  sum = 0.0;
+  for (int w = 0; w < kWholeWaves; ++w) sum += part[w];
+  const double up = sum == 0.0 ? 0.0 : (double)kMuonUp / sqrt(sum);
+  for_entries([&](int k, bool there, int r, int c) {
+    if (!there) return;
+    const int i = tall ? c : r, j = tall ? r : c;      // of the shorter side, of the longer
+    const float value = (float)((double)u[k] * up);
+    whole_place(x + i * b_ld + j, x_low, value);
+    whole_place(xt + j * a_ld + i, xt_low, value);
+  });
+  __syncthreads();
+  const int high = ra / 16, wide = rb / 16, triangles = high * (high + 1) / 2;
+  for (int round = 0; round < iterations; ++round) {
+    const bool last = round + 1 == iterations;
+    // a tile of P or Q by its columns, which is its mirror image by rows, and by rows where the tile is not its own mirror image
+    const auto mirrored = [&](f16_t* to, uint32_t i, uint32_t j, const float4_t& d) {
+      const int m = 16 * i + 4 * g, n = 16 * j + l;
+      whole_place(to + n * a_ld + m, p_low, d);
+      if (i != j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) whole_place(to + (m + r) * a_ld + n, p_low, d[r]);
+    };
+    for (int t = wave; t < triangles; t += kWholeWaves) {
+      uint32_t i, j;
+      triangle(t, i, j);
+      mirrored(p, i, j, whole_product(x, x_low, b_ld, x, x_low, b_ld, 16 * i, 16 * j, rb, l, g) * kMuonDown);
+    }
+    __syncthreads();
+    for (int t = wave; t < triangles; t += kWholeWaves) {
+      uint32_t i, j;
+      triangle(t, i, j);
+      const float4_t d = whole_product(p, p_low, a_ld, p, p_low, a_ld, 16 * i, 16 * j, ra, l, g);
+      mirrored(q, i, j, d * (kMuonDown * kMuonC) + whole_entries(p + (16 * j + l) * a_ld + 16 * i + 4 * g, p_low) * kMuonB);
+    }
+    __syncthreads();
+    float4_t made[kWholeTiles];
+#pragma unroll
+    for (int n = 0; n < kWholeTiles; ++n) {
+      const int t = wave + n * kWholeWaves;
+      if (t >= high * wide) continue;
+      const int i = t % high, j = t / high;
+      made[n] = whole_product(q, p_low, a_ld, xt, xt_low, a_ld, 16 * i, 16 * j, ra, l, g) * kMuonDown +
+                whole_entries(xt + (16 * j + l) * a_ld + 16 * i + 4 * g, xt_low) * kMuonA;
+    }
+    if (!last) __syncthreads();
+#pragma unroll
+    for (int n = 0; n < kWholeTiles; ++n) {
+      const int t = wave + n * kWholeWaves;
+      if (t >= high * wide) continue;
+      const int i = t % high, j = t / high;
+      if (!last) whole_place(xt + (16 * j + l) * a_ld + 16 * i + 4 * g, xt_low, made[n]);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int m = 16 * i + 4 * g + r, c = 16 * j + l;
+        if (!last) {
+          whole_place(x + m * b_ld + c, x_low, made[n][r]);
+        } else if (m < S.a && c < S.b) {
+          float* to = A.target + S.target + which * S.target_of + (int64_t)(tall ? c : m) * S.target_ld + (tall ? m : c);
+          const float o = made[n][r] * kMuonDown;
+          *to = STEP ? *to * (1.0f - A.lr * S.decay) - A.lr * S.rate * o : o;
+        }
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// ---- products ----
+// One XCD's workgroups make neighbouring tiles, whose operands its L2 then holds.
+__device__ __forceinline__ uint32_t by_xcd(uint32_t block, uint32_t blocks) {
+  const uint32_t x = block & 7, each = blocks >> 3, more = blocks & 7;
+  return x * each + min(x, more) + (block >> 3);
+}
+enum { kGram = 0, kSquare = 1, kApply = 2 };
 
 // 16 bytes for each lane of a wave, straight into LDS, where the lanes' lie one behind the other.
 __device__ __forceinline__ void to_lds(const void* from, void* to) {

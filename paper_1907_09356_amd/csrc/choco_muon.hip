@@ -26,7 +26,13 @@ constexpr int64_t kRoundBytes = (int64_t)1 << 30;
 int64_t padded(int64_t n) { return (n + kMuonPad - 1) / kMuonPad * kMuonPad; }
 int64_t tiles_of(int64_t n, int tile) { return (n + tile - 1) / tile; }
 
-// A shape's sides, operands and tiles; `count` and what is behind the begins are the caller's.
+// A matrix that a workgroup takes whole: what it holds fits LDS, and a wave's part of X its registers.
+bool whole(int64_t rows, int64_t cols) {
+  const int64_t a = std::min(rows, cols), b = std::max(rows, cols), ra = (a + 31) / 32 * 32, rb = (b + 31) / 32 * 32;
+  return whole_bytes(a, b) <= kWholeBytes && ra * rb <= 256 * kWholeTiles * kWholeWaves;
+}
+
+// A shape's sides, operands and tiles (tile = 0: taken whole); `count` and what is behind the begins are the caller's.
 MuonShape shape_from(int64_t rows, int64_t cols, int tile) {
   MuonShape S{};
   S.rows = (int32_t)rows;
@@ -37,6 +43,11 @@ MuonShape shape_from(int64_t rows, int64_t cols, int tile) {
   S.b_ld = (int32_t)padded(S.b);
   S.scratch_of = (muon_scratch(S.a, S.b, S.a_ld, S.b_ld) + 255) / 256 * 256;
   S.start_tiles = (uint32_t)(((rows + 63) / 64) * ((cols + 63) / 64));
+  if (tile == 0) {      // a workgroup takes all of it
+    S.start_tiles = 1;
+    S.scratch_of = 0;
+    return S;
+  }
   const int64_t high = tiles_of(S.a, tile);
   S.gram_tiles = (uint32_t)(high * (high + 1) / 2);
   S.apply_tiles = (uint32_t)(high * tiles_of(S.b, tile));
@@ -47,6 +58,7 @@ MuonShape shape_from(int64_t rows, int64_t cols, int tile) {
 struct Round {
   int32_t first, count;     // entries of the table
   uint32_t start_tiles, gram_tiles, apply_tiles;
+  int64_t lds;              // of matrices taken whole: the most that one needs
 };
 
 template <class T, bool STEP, int TILE>
@@ -69,6 +81,14 @@ int run_round(MuonArgs A, const Round& R, int iterations, hipStream_t stream) {
 }
 template <class T, bool STEP>
 int run_round(const MuonArgs& A, const Round& R, int iterations, int tile, hipStream_t stream) {
+  if (R.lds > 0) {
+    static const hipError_t allowed =
+        hipFuncSetAttribute((const void*)k_muon_whole<T, STEP>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kWholeBytes);
+    TRY_HIP(allowed);
+    k_muon_whole<T, STEP><<<dim3(R.start_tiles), 64 * kWholeWaves, (size_t)R.lds, stream>>>(A, iterations);
+    TRY_HIP(hipGetLastError());
+    return CHOCO_OK;
+  }
   return tile == 128 ? run_round<T, STEP, 128>(A, R, iterations, stream) : run_round<T, STEP, 64>(A, R, iterations, stream);
 }
 
@@ -99,15 +119,15 @@ struct StackLayout {
 int stack_layout(const choco_orthogonalize_config& c, StackLayout& L) {
   L = {};
   if (c.batch == 0 || c.rows == 0 || c.cols == 0) return CHOCO_OK;
-  L.tile = 128;
+  L.tile = whole(c.rows, c.cols) ? 0 : 128;
   L.shape = shape_from(c.rows, c.cols, L.tile);
-  if ((double)L.shape.apply_tiles * (double)c.batch < kFewTiles) L.shape = shape_from(c.rows, c.cols, L.tile = 64);
+  if (L.tile > 0 && (double)L.shape.apply_tiles * (double)c.batch < kFewTiles) L.shape = shape_from(c.rows, c.cols, L.tile = 64);
   const double most = std::max<double>(L.shape.start_tiles, std::max(L.shape.gram_tiles, L.shape.apply_tiles));
   if (!launch_fits(most, 256)) return CHOCO_E_UNSUPPORTED;
-  L.each = std::min<int64_t>(c.batch, std::max<int64_t>(1, kRoundBytes / L.shape.scratch_of));
-  while (L.each > 1 && !launch_fits(most * (double)L.each, 256)) L.each /= 2;
+  L.each = L.tile == 0 ? c.batch : std::min<int64_t>(c.batch, std::max<int64_t>(1, kRoundBytes / L.shape.scratch_of));
+  while (L.each > 1 && !launch_fits(most * (double)L.each, 512)) L.each /= 2;
   Parts parts;
-  L.partials = parts.take((size_t)L.each * L.shape.start_tiles * sizeof(double));
+  if (L.tile > 0) L.partials = parts.take((size_t)L.each * L.shape.start_tiles * sizeof(double));
   L.scratch = parts.take((size_t)L.each * (size_t)L.shape.scratch_of);
   L.total = parts.at;
   return CHOCO_OK;
@@ -148,7 +168,7 @@ int muon_layout(const choco_muon_config& c, std::vector<MuonShape>& table, std::
   Round now{};
   double tiles_in_all = 0.0;
   for (int32_t t = 0; t < c.ntensors; ++t)
-    if (c.rows_host[t] > 0 && c.cols_host[t] > 0) tiles_in_all += (double)c.n * shape_from(c.rows_host[t], c.cols_host[t], 128).apply_tiles;
+    if (c.rows_host[t] > 0 && c.cols_host[t] > 0 && !whole(c.rows_host[t], c.cols_host[t])) tiles_in_all += (double)c.n * shape_from(c.rows_host[t], c.cols_host[t], 128).apply_tiles;
   L.tile = tiles_in_all < kFewTiles ? 64 : 128;
   const auto close = [&] {
     if (now.count > 0) rounds.push_back(now);
@@ -156,26 +176,35 @@ int muon_layout(const choco_muon_config& c, std::vector<MuonShape>& table, std::
     now.first = (int32_t)table.size();
     scratch = partials = 0;
   };
+  std::vector<int64_t> moments((size_t)c.ntensors);
   for (int32_t t = 0; t < c.ntensors; ++t) {
+    moments[t] = moment;
+    moment += c.n * c.rows_host[t] * c.cols_host[t];
+  }
+  for (int32_t i = 0; i < 2 * c.ntensors; ++i) {      // those taken whole, then the others
+    const int32_t t = i % c.ntensors;
     const int64_t rows = c.rows_host[t], cols = c.cols_host[t], start = c.start_host[t];
-    if (rows == 0 || cols == 0) continue;
-    MuonShape S = shape_from(rows, cols, L.tile);
+    if (rows == 0 || cols == 0 || whole(rows, cols) != (i < c.ntensors)) continue;
+    const bool alone = i < c.ntensors;
+    if (!alone && now.lds > 0) close();
+    MuonShape S = shape_from(rows, cols, alone ? 0 : L.tile);
     S.source = S.target = start;
     S.source_of = S.target_of = ld;
     S.source_ld = S.target_ld = cols;
-    S.moment = moment;
-    moment += c.n * rows * cols;
+    S.moment = moments[t];
     S.decay = c.weight_decay_host ? c.weight_decay_host[t] : 0.0f;
     S.rate = c.lr_scale_host ? c.lr_scale_host[t] : std::sqrt(std::max(1.0f, (float)rows / (float)cols));
     const double tiles = std::max<double>(S.start_tiles, std::max(S.gram_tiles, S.apply_tiles));
-    if (!launch_fits(tiles, 256)) return CHOCO_E_UNSUPPORTED;
+    if (!launch_fits(tiles, 512)) return CHOCO_E_UNSUPPORTED;
+    if (alone) now.lds = std::max(now.lds, whole_bytes(S.a, S.b));
     for (int32_t w = 0; w < c.n;) {
       const double taken = std::max<double>(now.start_tiles, std::max(now.gram_tiles, now.apply_tiles));
-      int64_t count = std::min<int64_t>(c.n - w, (kRoundBytes - scratch) / S.scratch_of);
-      while (count > 0 && !launch_fits(taken + tiles * (double)count, 256)) count /= 2;
+      int64_t count = alone ? c.n - w : std::min<int64_t>(c.n - w, (kRoundBytes - scratch) / S.scratch_of);
+      while (count > 0 && !launch_fits(taken + tiles * (double)count, 512)) count /= 2;
       if (count < 1) {
         if (now.count > 0) {
           close();
+          if (alone) now.lds = whole_bytes(S.a, S.b);
           continue;
         }
         count = 1;
@@ -190,7 +219,7 @@ int muon_layout(const choco_muon_config& c, std::vector<MuonShape>& table, std::
       S.gram_begin = now.gram_tiles;
       S.apply_begin = now.apply_tiles;
       scratch += count * S.scratch_of;
-      partials += count * S.start_tiles;
+      partials += alone ? 0 : count * S.start_tiles;
       now.start_tiles += (uint32_t)count * S.start_tiles;
       now.gram_tiles += (uint32_t)count * S.gram_tiles;
       now.apply_tiles += (uint32_t)count * S.apply_tiles;
@@ -242,7 +271,7 @@ int choco_orthogonalize(const choco_orthogonalize_config* cfg, const void* x_dev
   if (!x_dev || !y_dev || !aligned_to(x_dev, type_bytes(c.type)) || !aligned_to(y_dev, 4)) return CHOCO_E_INVAL;
   StackLayout L;
   if (const int rc = stack_layout(c, L)) return rc;
-  if (!workspace_dev || !aligned_to(workspace_dev, 256)) return CHOCO_E_INVAL;
+  if (L.total > 0 && (!workspace_dev || !aligned_to(workspace_dev, 256))) return CHOCO_E_INVAL;
   if (L.total > workspace_bytes) return CHOCO_E_NOMEM;
   for (int64_t first = 0; first < c.batch; first += L.each) {
     MuonArgs A{};
@@ -259,7 +288,7 @@ int choco_orthogonalize(const choco_orthogonalize_config* cfg, const void* x_dev
     A.partials = (double*)((char*)workspace_dev + L.partials);
     A.scratch = (char*)workspace_dev + L.scratch;
     const uint32_t count = (uint32_t)A.one.count;
-    const Round R{0, 1, count * L.shape.start_tiles, count * L.shape.gram_tiles, count * L.shape.apply_tiles};
+    const Round R{0, 1, count * L.shape.start_tiles, count * L.shape.gram_tiles, count * L.shape.apply_tiles, L.tile > 0 ? 0 : whole_bytes(c.rows < c.cols ? c.rows : c.cols, c.rows < c.cols ? c.cols : c.rows)};
     int rc = CHOCO_OK;
     with_type(c.type, [&](auto x) { rc = run_round<decltype(x), false>(A, R, c.iterations, L.tile, (hipStream_t)c.stream); });
     if (rc) return rc;

@@ -136,7 +136,7 @@ def test_orthogonalize_refuses_bad_sizes(over):
 
 
 def test_orthogonalize_refuses_bad_pointers_and_does_nothing_where_nothing_is():
-    L, c, out = T.lib(), stack_cfg(), ctypes.c_size_t()
+    L, c, out = T.lib(), stack_cfg(rows=300, cols=400, x=(120_000, 400), y=(120_000, 400)), ctypes.c_size_t()
     assert L.choco_orthogonalize_workspace_bytes(ctypes.byref(c), ctypes.byref(out)) == B.OK and out.value > 0
     for x, y, ws in ((0, P, P), (P, 0, P), (P, P, 0), (P + 2, P, P), (P, P + 2, P), (P, P, P + 128)):
         assert L.choco_orthogonalize(ctypes.byref(c), x, y, ws, out.value) == B.E_INVAL
