@@ -2,14 +2,16 @@
 // result (device code).
 //
 // A matrix is taken with its shorter side first: a x b entries, a <= b.  Every product is of rows with rows, D[m][n] = sum over k of
-// L[m][k] R[n][k]:  P from X and X,  Q = b P + c P^2 from P and P (symmetric),  X' = a X + Q X from Q and X^T.  So X is held both
+// L[m][k] R[n][k]:  P from X and X,  Q = a I + b P + c P^2 from P and P (symmetric),  X' = Q X from Q and X^T.  So X is held both
 // ways, X^T twice (a launch reads one and writes the other).
 //
-// Operands are two fp16 numbers for one fp32, 2^13 x = high + low.  No entry of X, P or Q is beyond 3 (their singular
+// Operands are two fp16 numbers for one fp32, 2^13 x = high + low.  No entry of X, P or Q is beyond 3.5 (their singular
 // values are not), so high is below 2^15, and low keeps 11 bits more down to 2^-24: 22 bits of an entry above 2^-15, 2^-38 of a smaller
 // one.  A product takes high high + high low + low high on the matrix cores, where sums are fp32; the last, low low, is 2^-22 of the
 // first.
 #pragma once
+
+#include <type_traits>
 
 #include "choco_types.h"
 
@@ -343,7 +345,11 @@ __global__ __launch_bounds__(64 * kWholeWaves) void k_muon_whole(MuonArgs A, int
       uint32_t i, j;
       triangle(t, i, j);
       const float4_t d = whole_product(p, p_low, a_ld, p, p_low, a_ld, 16 * i, 16 * j, ra, l, g);
-      mirrored(q, i, j, d * (kMuonDown * kMuonC) + whole_entries(p + (16 * j + l) * a_ld + 16 * i + 4 * g, p_low) * kMuonB);
+      float4_t sum = d * (kMuonDown * kMuonC) + whole_entries(p + (16 * j + l) * a_ld + 16 * i + 4 * g, p_low) * kMuonB;
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (i == j && 4 * g + r == l) sum[r] += kMuonA * kMuonUp;
+      mirrored(q, i, j, sum);
     }
     __syncthreads();
     float4_t made[kWholeTiles];
@@ -352,8 +358,7 @@ __global__ __launch_bounds__(64 * kWholeWaves) void k_muon_whole(MuonArgs A, int
       const int t = wave + n * kWholeWaves;
       if (t >= high * wide) continue;
       const int i = t % high, j = t / high;
-      made[n] = whole_product(q, p_low, a_ld, xt, xt_low, a_ld, 16 * i, 16 * j, ra, l, g) * kMuonDown +
-                whole_entries(xt + (16 * j + l) * a_ld + 16 * i + 4 * g, xt_low) * kMuonA;
+      made[n] = whole_product(q, p_low, a_ld, xt, xt_low, a_ld, 16 * i, 16 * j, ra, l, g) * kMuonDown;
     }
     if (!last) __syncthreads();
 #pragma unroll
@@ -443,26 +448,35 @@ __global__ __launch_bounds__(256, TILE == 128 ? 2 : 1) void k_muon_product(MuonA
   float4_t acc[W][W] = {};
   int64_t k = ALONE ? 32 * wave : 0;
   if (k < ld) load(k, 0);
-  for (int buffer = 0; k < ld; k += kStride, buffer ^= 1) {
-    // this step's parts are there (for everybody), and (everybody is) done with the other buffer
-    __builtin_amdgcn_s_waitcnt(0);
-    if (ALONE) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    else __syncthreads();
-    half8 f[4][W];
+  // 16-row parts of the wave's sides that rows reach
+  const int m_parts = max(0, min(W, (ms - m0 - mw + 15) / 16)), n_parts = max(0, min(W, (ns - n0 - nw + 15) / 16));
+  const auto steps = [&](auto edges) {
+    constexpr bool EDGES = decltype(edges)::value;
+    for (int buffer = 0; k < ld; k += kStride, buffer ^= 1) {
+      // this step's parts are there (for everybody), and (everybody is) done with the other buffer
+      __builtin_amdgcn_s_waitcnt(0);
+      if (ALONE) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      else __syncthreads();
+      half8 f[4][W];
 #pragma unroll
-    for (int p = 0; p < 4; ++p)
+      for (int p = 0; p < 4; ++p)
 #pragma unroll
-      for (int i = 0; i < W; ++i) f[p][i] = *(const half8*)&lds[buffers + buffer][p][(p < 2 ? mw : nw) + 16 * i + l][swap];
-    if (k + kStride < ld) load(k + kStride, buffer ^ 1);
+        for (int i = 0; i < W; ++i) f[p][i] = *(const half8*)&lds[buffers + buffer][p][(p < 2 ? mw : nw) + 16 * i + l][swap];
+      if (k + kStride < ld) load(k + kStride, buffer ^ 1);
+      if (m_parts == 0 || n_parts == 0) continue;
 #pragma unroll
-    for (int i = 0; i < W; ++i)
+      for (int i = 0; i < W; ++i)
 #pragma unroll
-      for (int j = 0; j < W; ++j) {
-        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[1][i], f[2][j], acc[i][j], 0, 0, 0);
-        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[0][i], f[3][j], acc[i][j], 0, 0, 0);
-        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[0][i], f[2][j], acc[i][j], 0, 0, 0);
-      }
-  }
+        for (int j = 0; j < W; ++j) {
+          if (EDGES && (i >= m_parts || j >= n_parts)) continue;
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[1][i], f[2][j], acc[i][j], 0, 0, 0);
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[0][i], f[3][j], acc[i][j], 0, 0, 0);
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[0][i], f[2][j], acc[i][j], 0, 0, 0);
+        }
+    }
+  };
+  if (ms - m0 >= TILE && ns - n0 >= TILE) steps(std::false_type{});
+  else steps(std::true_type{});
   // The tile in LDS, fp32, columns exchanged by the rows' number so that reading down a column meets all banks, then out of it by
   // rows and by columns, 8 entries a lane.
   __syncthreads();
@@ -485,9 +499,8 @@ __global__ __launch_bounds__(256, TILE == 128 ? 2 : 1) void k_muon_product(MuonA
     __syncthreads();
   }
   constexpr int kParts = TILE / 8;
-  constexpr bool kAdds = KIND != kGram;     // a X or b P
+  constexpr bool kAdds = KIND == kSquare;     // a I + b P
   const bool last = KIND == kApply && A.last;
-  f16_t* const own = KIND == kApply ? P.x : P.p;
   f16_t* const made = KIND == kApply ? P.x : KIND == kGram ? P.p : P.q;
   f16_t* const turned = KIND == kApply ? P.xt[A.now ^ 1] : made;
   const int64_t low = KIND == kApply ? P.x_low : P.p_low, turned_low = KIND == kApply ? P.xt_low : P.p_low;
@@ -505,6 +518,7 @@ __global__ __launch_bounds__(256, TILE == 128 ? 2 : 1) void k_muon_product(MuonA
         to[e] = A.moments ? to[e] * (1.0f - A.lr * S.decay) - A.lr * S.rate * o : o;
       }
   };
+  if (!(last && tall))
   for (int u = threadIdx.x; u < TILE * kParts; u += 256) {
     const int i = u / kParts, j = u % kParts * 8, m = m0 + i, n = n0 + j;
     if (m >= ms || n >= n_ld) continue;
@@ -518,22 +532,21 @@ __global__ __launch_bounds__(256, TILE == 128 ? 2 : 1) void k_muon_product(MuonA
     }
     const int64_t at_row = (int64_t)m * n_ld + n;
     if (kAdds) {
-      const half8 high = *(const half8*)(own + at_row), less = *(const half8*)(own + at_row + low);
+      const half8 high = *(const half8*)(P.p + at_row), less = *(const half8*)(P.p + at_row + low);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] += (KIND == kApply ? kMuonA : kMuonB) * ((float)high[e] + (float)less[e]);
+      for (int e = 0; e < 8; ++e) x[e] += kMuonB * ((float)high[e] + (float)less[e]) + (m == n + e ? kMuonA * kMuonUp : 0.0f);
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e)
       if (n + e >= ns) x[e] = 0.0f;
-    if (last && !tall) {
+    if (last) {
       finish(m, n, x, ns - n);
       continue;
     }
-    if (kAdds && (KIND == kApply || ti != tj)) {
+    if (kAdds && ti != tj) {
       *(float4_t*)&tile[place(i, j)] = *(const float4_t*)&x[0];
       *(float4_t*)&tile[place(i, j + 4)] = *(const float4_t*)&x[4];
     }
-    if (last) continue;
     half8 high, less;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
