@@ -58,39 +58,55 @@ __device__ __forceinline__ void store_result(const LinearPass& P, int64_t at, fl
 }
 
 // ---- step by step ----
-// A workgroup takes a slice of columns, a lane a column, a wave a quarter of the state's rows.
+// A workgroup takes a slice of columns and holds the state in registers, V columns of every 4 V-th row a lane (V as the state in memory is
+// aligned).  Bound by the state, in and out once: for a step of D x D, 8 D^2 bytes against 5 D^2 operations.
 constexpr int kLinearStage = 8;     // steps whose a and b are in LDS at a time
 
-template <class T, int R>
+template <class T, int V, int D>
 __global__ __launch_bounds__(256) void k_linear_steps(LinearArgs A, LinearPass P) {
-  __shared__ float sa[kLinearStage][4 * R], sb[kLinearStage][4 * R], part[2][4][64];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  constexpr int kLanes = kLinearSlice / V, kRows = 256 / kLanes, R = D / kRows;
+  __shared__ float sa[kLinearStage][D], sb[kLinearStage][D];
+  __shared__ __attribute__((aligned(16))) float part[2][kRows][kLinearSlice];
+  const int row = threadIdx.x / kLanes, at = threadIdx.x % kLanes * V;
   const int slices = (P.dc + kLinearSlice - 1) / kLinearSlice, slice = blockIdx.x % slices;
   const int64_t bh = blockIdx.x / slices, b = bh / A.heads;
-  const int h = (int)(bh % A.heads), col = slice * kLinearSlice + lane, row = wave * R;
-  const bool in = col < P.dc;
+  const int h = (int)(bh % A.heads), col = slice * kLinearSlice + at;
+  const bool in = col < P.dc;      // (V divides the columns)
   const int64_t len = steps_of(A, b), state = (int64_t)P.da * P.dc;
   const T* pa = (const T*)P.a + b * P.a_seq + (h / P.a_share) * P.a_head;
   const T* pb = (const T*)P.b + b * P.b_seq + (h / P.b_share) * P.b_head;
-  const T* pc = (const T*)P.c + b * P.c_seq + (h / P.c_share) * P.c_head;
-  const int64_t out = b * P.out_seq + h * P.out_head + col;
-  float s[R];
+  const T* pc = (const T*)P.c + b * P.c_seq + (h / P.c_share) * P.c_head + col;
+  const int64_t out = b * P.out_seq + h * P.out_head + slice * kLinearSlice;
+  float s[R][V];
 #pragma unroll
-  for (int r = 0; r < R; ++r)
-    s[r] = P.first && in && row + r < P.da ? P.first[bh * P.first_of * state + (int64_t)(row + r) * P.state_a + (int64_t)col * P.state_c] : 0.0f;
+  for (int r = 0; r < R; ++r) {
+    const int i = row + r * kRows;
+#pragma unroll
+    for (int v = 0; v < V; ++v) s[r][v] = 0.0f;
+    if (P.first && in && i < P.da) {
+      const float* p = P.first + bh * P.first_of * state + (int64_t)i * P.state_a + (int64_t)col * P.state_c;
+      if (V > 1) load_floats<float, V>(p, s[r]);
+      else s[r][0] = *p;
+    }
+  }
   const auto keep = [&](float* to, float w) {
 #pragma unroll
-    for (int r = 0; r < R; ++r)
-      if (in && row + r < P.da) to[(int64_t)(row + r) * P.state_a + (int64_t)col * P.state_c] = s[r] * w;
+    for (int r = 0; r < R; ++r) {
+      const int i = row + r * kRows;
+      float x[V];
+#pragma unroll
+      for (int v = 0; v < V; ++v) x[v] = s[r][v] * w;
+      if (in && i < P.da) store_floats<float, V>(to + (int64_t)i * P.state_a + (int64_t)col * P.state_c, x);
+    }
   };
   for (int64_t i0 = 0; i0 < len; i0 += kLinearStage) {
     const int n = len - i0 < kLinearStage ? (int)(len - i0) : kLinearStage;
     __syncthreads();
-    for (int e = threadIdx.x; e < n * P.da; e += 256) {
-      const int i = e / P.da, j = e % P.da;
+    for (int e = threadIdx.x; e < n * D; e += 256) {
+      const int i = e / D, j = e % D;
       const int64_t t = P.back ? len - 1 - (i0 + i) : i0 + i;
-      sa[i][j] = to_float(pa[t * P.a_step + j]);
-      sb[i][j] = to_float(pb[t * P.b_step + j]);
+      sa[i][j] = j < P.da ? to_float(pa[t * P.a_step + j]) : 0.0f;
+      sb[i][j] = j < P.da ? to_float(pb[t * P.b_step + j]) : 0.0f;
     }
     __syncthreads();
     for (int i = 0; i < n; ++i) {
@@ -99,29 +115,37 @@ __global__ __launch_bounds__(256) void k_linear_steps(LinearArgs A, LinearPass P
       float w = 1.0f;
       if (!P.back) w = linear_decay(log_gate(A, b, t, h));
       else if (t + 1 < len) w = linear_decay(log_gate(A, b, t + 1, h));
-      const float c = in ? to_float(pc[t * P.c_step + col]) : 0.0f;
-      float sum = 0.0f;
+      float c[V], sum[V];
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        c[v] = in ? to_float(pc[t * P.c_step + v]) : 0.0f;
+        sum[v] = 0.0f;
+      }
 #pragma unroll
       for (int r = 0; r < R; ++r)
-        if (row + r < P.da) {
-          s[r] = fmaf(sb[i][row + r], c, s[r] * w);
-          sum = fmaf(sa[i][row + r], s[r], sum);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          s[r][v] = fmaf(sb[i][row + r * kRows], c[v], s[r][v] * w);
+          sum[v] = fmaf(sa[i][row + r * kRows], s[r][v], sum[v]);
         }
-      part[i & 1][wave][lane] = sum;
+      store_floats<float, V>(&part[i & 1][row][at], sum);
       __syncthreads();
-      if (wave == (i & 3)) {
-        const float y = (part[i & 1][0][lane] + part[i & 1][1][lane]) + (part[i & 1][2][lane] + part[i & 1][3][lane]);
-        if (in) store_result<T>(P, out + t * P.out_step, y);
+      if (threadIdx.x < kLinearSlice) {
+        const int mine = slice * kLinearSlice + (int)threadIdx.x;
+        float y = 0.0f;
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) y += part[i & 1][r][threadIdx.x];
+        if (mine < P.dc) store_result<T>(P, out + t * P.out_step + threadIdx.x, y);
         if (P.dots) {
-          float d = in ? y * to_float(((const T*)P.x)[b * P.x_seq + t * P.x_step + (h / P.x_share) * P.x_head + col]) : 0.0f;
+          float d = mine < P.dc ? y * to_float(((const T*)P.x)[b * P.x_seq + t * P.x_step + (h / P.x_share) * P.x_head + mine]) : 0.0f;
           for (int o = 32; o; o >>= 1) d += __shfl_xor(d, o);
-          if (lane == 0) P.dots[((int64_t)slice * A.batch * A.heads + bh) * A.steps + t] = d;
+          if (threadIdx.x == 0) P.dots[((int64_t)slice * A.batch * A.heads + bh) * A.steps + t] = d;
         }
       }
     }
   }
-  if (in)
-    for (int64_t t = len + wave; t < A.steps; t += 4) store_result<T>(P, out + t * P.out_step, 0.0f);
+  const int width = min(P.dc - slice * kLinearSlice, kLinearSlice);
+  for (int64_t e = threadIdx.x; e < (A.steps - len) * width; e += 256) store_result<T>(P, out + (len + e / width) * P.out_step + e % width, 0.0f);
   if (P.kept) keep(P.kept + (bh * P.kept_of + (len + kLinearSave - 1) / kLinearSave) * state, 1.0f);
   if (P.last) keep(P.last + bh * state, P.back && len > 0 ? linear_decay(log_gate(A, b, 0, h)) : 1.0f);
 }

@@ -187,10 +187,20 @@ int run_chunks(const choco_linear_config& c, const LinearArgs& A, const LinearPa
 template <class T>
 int run_steps(const choco_linear_config& c, const LinearArgs& A, const LinearPass& P) {
   const dim3 grid((uint32_t)(rows_of(c) * slices_of(P.dc)));
-  const hipStream_t stream = (hipStream_t)c.stream;
-  if (P.da <= 64) k_linear_steps<T, 16><<<grid, 256, 0, stream>>>(A, P);
-  else if (P.da <= 128) k_linear_steps<T, 32><<<grid, 256, 0, stream>>>(A, P);
-  else k_linear_steps<T, 64><<<grid, 256, 0, stream>>>(A, P);
+  const auto launch = [&](auto v, auto d) {
+    k_linear_steps<T, decltype(v)::value, decltype(d)::value><<<grid, 256, 0, (hipStream_t)c.stream>>>(A, P);
+  };
+  const auto with_dim = [&](auto v) {
+    if (P.da <= 64) launch(v, std::integral_constant<int, 64>{});
+    else if (P.da <= 128) launch(v, std::integral_constant<int, 128>{});
+    else launch(v, std::integral_constant<int, 256>{});
+  };
+  const auto wide = [&](int v) {      // columns of a state next to one another, on the border of as many
+    return P.state_c == 1 && P.dc % v == 0 && aligned_to(P.first, 4 * v) && aligned_to(P.last, 4 * v) && aligned_to(P.kept, 4 * v);
+  };
+  if (wide(4)) with_dim(std::integral_constant<int, 4>{});
+  else if (wide(2)) with_dim(std::integral_constant<int, 2>{});
+  else with_dim(std::integral_constant<int, 1>{});
   TRY_HIP(hipGetLastError());
   return CHOCO_OK;
 }
