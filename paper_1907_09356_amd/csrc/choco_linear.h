@@ -332,6 +332,10 @@ struct Staged {
   static constexpr int V = R == 1 ? 8 : 4;
   static constexpr int kWordsOf = V * sizeof(In) / 4;      // of V entries
   static constexpr int kThreads = 64 * WAVES, kAll = kChunk / R * (W / V), kUnits = (kAll + kThreads - 1) / kThreads;
+  // words of rows of their own: neighbouring lanes' are next to one another, a thread's in rows apart
+  static constexpr bool kByWords = WAY == kWords && R == 1;
+  static constexpr int kRowWords = W * sizeof(In) / 4, kEach = 4 / sizeof(In);      // entries of a word
+  static_assert(!kByWords || (kThreads % kRowWords == 0 && kUnits * kWordsOf * (kThreads / kRowWords) == kChunk));
   uint32_t x[kUnits][R][kWordsOf];
 
   static __device__ __forceinline__ void place(int i, int thread, int& row, int& col) {
@@ -350,6 +354,17 @@ struct Staged {
   // last row.
   __device__ __forceinline__ void load(int thread, const In* first, int64_t step, bool back, int width, int lo, int hi) {
     const __amdgpu_buffer_rsrc_t buffer = __builtin_amdgcn_make_buffer_rsrc((void*)first, 0, kBufferBytes, 0x00027000);
+    if constexpr (kByWords) {
+      const int col = thread % kRowWords * kEach;
+      const bool in = col < width;
+#pragma unroll
+      for (int i = 0; i < kUnits * kWordsOf; ++i) {
+        const int row = thread / kRowWords + i * (kThreads / kRowWords), t = back ? kChunk - 1 - row : row;
+        const uint32_t at = ((uint32_t)t * (uint32_t)step + (uint32_t)col) * (uint32_t)sizeof(In);
+        x[i / kWordsOf][0][i % kWordsOf] = __builtin_amdgcn_raw_buffer_load_b32(buffer, in && row >= lo && row < hi ? at : ~0u, 0, 0);
+      }
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
       int row, col;
@@ -359,7 +374,6 @@ struct Staged {
         const bool there = row + r >= lo && row + r < hi && mine(row, col);
         const int t = back ? kChunk - 1 - row - r : row + r;
         const uint32_t at = ((uint32_t)t * (uint32_t)step + (uint32_t)col) * (uint32_t)sizeof(In);
-        constexpr int kEach = 4 / sizeof(In);      // entries of a word
         if constexpr (WAY == kParts) {
           if constexpr (kWordsOf == 2) {
             const word2 v = __builtin_amdgcn_raw_buffer_load_b64(buffer, there && col < width ? at : ~0u, 0, 0);
@@ -400,6 +414,20 @@ struct Staged {
   }
   template <int STRIDE>
   __device__ __forceinline__ void store(int thread, Core (&to)[kChunk][STRIDE]) const {
+    if constexpr (kByWords) {
+#pragma unroll
+      for (int i = 0; i < kUnits * kWordsOf; ++i) {
+        const uint32_t word = x[i / kWordsOf][0][i % kWordsOf];
+        Core* p = &to[thread / kRowWords + i * (kThreads / kRowWords)][thread % kRowWords * kEach];
+        if constexpr (sizeof(In) == sizeof(Core)) {
+          *reinterpret_cast<uint32_t*>(p) = word;
+        } else {
+          p[0] = entry<In>(word, 0);
+          p[1] = entry<In>(word, 1);
+        }
+      }
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
       int row, col;

@@ -140,8 +140,10 @@ int width_of(const Rows& r, size_t size, int most, const choco_linear_config& c)
   return 1;
 }
 
-// Up to so many steps are taken one by one.
-constexpr int64_t kStepByStep = 8;
+// Up to so many steps are taken one by one.  us, one by one | in chunks, forward and backward: 160 x 10 heads of 64 in fp32, 4 steps 20 and 65 |
+// 35 and 104, 8 steps 31 and 94 | 36 and 107, 12 steps 41 and 127 | 38 and 110; 64 x 16 heads of 128 in bf16, 4 steps 35 and 113 | 34 and 99, 8 steps 48
+// and 159 | 34 and 100.
+int64_t step_by_step(const choco_linear_config& c) { return c.type == CHOCO_BF16 ? 3 : 8; }
 
 template <class In, int DA, int WAVES, int MODE, int WAY>
 int launch_chunks(const choco_linear_config& c, const LinearArgs& A, const LinearPass& P, const LinearChunks& C) {
@@ -250,7 +252,7 @@ void segments_of(const choco_linear_config& c, int32_t& segments, int32_t& chunk
 
 template <class T>
 int run_forward(const choco_linear_config& c, const LinearArgs& A, LinearPass P, const Rows& q, const Rows& k, const Rows& v, const Rows& y, char* ws) {
-  if (c.steps <= kStepByStep) return run_steps<T>(c, A, P);
+  if (c.steps <= step_by_step(c)) return run_steps<T>(c, A, P);
   LinearChunks C = chunks_of(c, P, q, k, v, y, nullptr);
   segments_of(c, C.segments, C.chunks);
   if (C.segments > 1) {
@@ -274,7 +276,7 @@ int run_backward(const choco_linear_config& c, const LinearArgs& A, const void* 
   float* const later = (float*)(ws + L.later);
   float* const q_dots = (float*)(ws + L.dots);
   float* const k_dots = q_dots + rows * c.steps * slices_of(c.dim_k);
-  const bool stepwise = c.steps <= kStepByStep, several = pieces > 1;
+  const bool stepwise = c.steps <= step_by_step(c), several = pieces > 1;
   // a pass on its own arrays; a gradient of heads that share one: of every head to the workspace, then added up
   const auto through = [&](LinearPass P, const Rows& ra, const Rows& rb, const Rows& rc_, Rows out, const Rows* x, const float* states,
                            int64_t states_of) -> int {
