@@ -128,8 +128,9 @@ typedef struct {
 int choco_linear_saved_bytes(const choco_linear_config* cfg, size_t* bytes_host);
 /* Bytes of device workspace that the forward (backward = 0) or the backward pass needs (16-byte aligned); may be 0. */
 int choco_linear_workspace_bytes(const choco_linear_config* cfg, int backward, size_t* bytes_host);
-/* Errors as above.  h0_dev (batch x heads x dim_k x dim_v fp32; zero without), lengths_dev (batch int32), h_last_dev (as h0)
-   and saved_dev may be NULL. */
+/* Errors as above; CHOCO_E_UNSUPPORTED: more than some 10^6 sequences' heads or a like number of their pieces of 256 steps.  h0_dev
+   (batch x heads x dim_k x dim_v fp32; zero without), lengths_dev (batch int32), h_last_dev (as h0) and saved_dev may be NULL.
+   Outputs may not overlap inputs, but for h_last and h0. */
 int choco_linear_forward(const choco_linear_config* cfg, const void* q_dev, const void* k_dev, const void* v_dev,
                          const float* g_dev, const float* h0_dev, const int32_t* lengths_dev, void* y_dev, float* h_last_dev,
                          float* saved_dev, void* workspace_dev, size_t workspace_bytes);
@@ -221,7 +222,7 @@ typedef struct {
 
 /* Bytes of device workspace (256-byte aligned); may be 0. */
 int choco_orthogonalize_workspace_bytes(const choco_orthogonalize_config* cfg, size_t* bytes_host);
-/* x_dev is not written, and y_dev may not overlap it.  CHOCO_E_UNSUPPORTED: more work than one launch holds. */
+/* y_dev may be x_dev (fp32, the same strides), else they may not overlap.  CHOCO_E_UNSUPPORTED: more work than one launch holds. */
 int choco_orthogonalize(const choco_orthogonalize_config* cfg, const void* x_dev, float* y_dev, void* workspace_dev,
                         size_t workspace_bytes);
 

@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "choco_train.h"
 #include "choco_types.h"
 
@@ -35,6 +37,17 @@ void with_type(int type, Fn&& fn) {
   if (type == CHOCO_F32) fn(float{});
   else if (type == CHOCO_BF16) fn(bf16_t{});
   else fn(f16_t{});
+}
+
+// A kernel's leave to take more than 64 KB of LDS at launch, asked for once on each device; `done`: where it has been.
+inline hipError_t allow_lds(const void* kernel, size_t bytes, std::atomic<uint64_t>& done) {
+  int device = 0;
+  if (const hipError_t e = hipGetDevice(&device)) return e;
+  const uint64_t bit = (uint64_t)1 << (device & 63);
+  if (device < 64 && (done.load(std::memory_order_relaxed) & bit)) return hipSuccess;
+  if (const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes)) return e;
+  if (device < 64) done.fetch_or(bit, std::memory_order_relaxed);
+  return hipSuccess;
 }
 
 // Parts of a workspace, one behind the other on multiples of 256 bytes.

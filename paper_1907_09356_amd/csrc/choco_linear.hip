@@ -151,8 +151,8 @@ int launch_chunks(const choco_linear_config& c, const LinearArgs& A, const Linea
   const size_t lds = sizeof(ChunkShared<Core, DA, WAVES>);
   const auto kernel = k_linear_chunks<In, Core, DA, WAVES, MODE, WAY>;
   if (lds > 65536) {
-    static const hipError_t allowed = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-    TRY_HIP(allowed);
+    static std::atomic<uint64_t> done{0};
+    TRY_HIP(allow_lds((const void*)kernel, lds, done));
   }
   kernel<<<dim3(C.blocks), 64 * WAVES, lds, (hipStream_t)c.stream>>>(A, P, C);
   TRY_HIP(hipGetLastError());

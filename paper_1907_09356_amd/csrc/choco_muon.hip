@@ -82,9 +82,8 @@ int run_round(MuonArgs A, const Round& R, int iterations, hipStream_t stream) {
 template <class T, bool STEP>
 int run_round(const MuonArgs& A, const Round& R, int iterations, int tile, hipStream_t stream) {
   if (R.lds > 0) {
-    static const hipError_t allowed =
-        hipFuncSetAttribute((const void*)k_muon_whole<T, STEP>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kWholeBytes);
-    TRY_HIP(allowed);
+    static std::atomic<uint64_t> done{0};
+    TRY_HIP(allow_lds((const void*)k_muon_whole<T, STEP>, kWholeBytes, done));
     k_muon_whole<T, STEP><<<dim3(R.start_tiles), 64 * kWholeWaves, (size_t)R.lds, stream>>>(A, iterations);
     TRY_HIP(hipGetLastError());
     return CHOCO_OK;

@@ -128,6 +128,13 @@ def test_strides():
     assert torch.equal(T.orthogonalize(x[:1].expand(3, -1, -1)), want[:1].expand(3, -1, -1))
 
 
+@pytest.mark.parametrize("shape", [(3, 20, 30), (2, 300, 120), (20, 700, 650)])
+def test_in_place(shape):
+    x = matrices(shape)
+    want = T.orthogonalize(x)
+    assert T.orthogonalize(x, out=x) is x and torch.equal(x, want)
+
+
 def test_tall_is_the_transposed_of_wide():
     x = matrices((2, 300, 120))
     a, b = T.orthogonalize(x), T.orthogonalize(x.transpose(1, 2).contiguous())
