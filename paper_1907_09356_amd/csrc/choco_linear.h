@@ -158,14 +158,16 @@ __global__ __launch_bounds__(256) void k_linear_steps(LinearArgs A, LinearPass P
 // That is how the cores take a left operand whose inner index is the row, so S does not go through LDS; P^T does, a wave makes
 // a quarter of it.  Differences of c are taken of c in two floats: a start-over leaves the steps behind it exact.
 //
-// Entries of 32 bits (and of fp16, taken as 32 bits) go to the fp32 matrix instruction.  Those of bf16 are operands as they are; what is fp32
-// by nature (P, S, weighted c) enters as a sum of bf16 numbers, two of them (2^-17) for a result of 16 bits, three (2^-25) for states
-// and wherever the result also goes into fp32 sums.
+// Entries of 32 bits go to the fp32 matrix instruction.  Those of 16 bits are operands as they are; what is fp32 by nature (P, S, weighted c)
+// enters as a sum of numbers of that type.  bf16: two of them (2^-17) for a result of 16 bits, three (2^-25) for states and wherever the
+// result also goes into fp32 sums.  fp16: two (2^-22), after a power of two has brought the largest into fp16's range.
 constexpr int kChunk = 64;
 constexpr float kLog2Least = -300.0f;     // stands for -infinity: less than any difference that counts
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 template <class Core>
@@ -191,6 +193,39 @@ struct Operand<bf16_t> {
   }
   static __device__ __forceinline__ f32x4 mma(Frag a, Frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 };
+template <>
+struct Operand<f16_t> {
+  typedef f16x8 Frag;
+  static constexpr int kInner = 32, kTiles = 2;
+  static __device__ __forceinline__ Frag load(const f16_t* row, int j, int g) {
+    const f16x4 lo = *(const f16x4*)(row + 32 * j + 4 * g), hi = *(const f16x4*)(row + 32 * j + 16 + 4 * g);
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+  static __device__ __forceinline__ f32x4 mma(Frag a, Frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+};
+// A power of two that brings numbers of a wave, the largest of them `most`, near the top of fp16's range, and back: up to 2^12, so that sums of
+// thousands stay in fp32's and what is 2^-36 of the largest still counts.
+struct Range {
+  float up, down;
+  __device__ __forceinline__ explicit Range(float most) {
+    const uint32_t e = max(__float_as_uint(most) >> 23, 12u);      // (not negative; infinite stays so)
+    up = __uint_as_float((265u - e) << 23);
+    down = __uint_as_float((e - 11u) << 23);
+  }
+};
+template <int CONTROL, int ROWS>
+__device__ __forceinline__ float larger_of(float x) {
+  return fmaxf(x, __uint_as_float(__builtin_amdgcn_update_dpp(__float_as_uint(x), __float_as_uint(x), CONTROL, ROWS, 15, false)));
+}
+__device__ __forceinline__ float largest_of_wave(float x) {
+  x = larger_of<0x111, 15>(x);
+  x = larger_of<0x112, 15>(x);
+  x = larger_of<0x114, 15>(x);
+  x = larger_of<0x118, 15>(x);
+  x = larger_of<0x142, 10>(x);
+  x = larger_of<0x143, 12>(x);
+  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), 63));
+}
 // fp32 numbers of an operand as so many operands that add up to it.
 template <class Core, int N>
 __device__ __forceinline__ void pieces_of(const f32x4 (&x)[Operand<Core>::kTiles], typename Operand<Core>::Frag (&p)[N]) {
@@ -199,17 +234,17 @@ __device__ __forceinline__ void pieces_of(const f32x4 (&x)[Operand<Core>::kTiles
     p[0] = x[0];
   } else {
     typedef float f32x2 __attribute__((ext_vector_type(2)));
-    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    typedef Core Two __attribute__((ext_vector_type(2)));
 #pragma unroll
     for (int e = 0; e < 8; e += 2) {
       f32x2 left = {x[e / 4][e % 4], x[e / 4][e % 4 + 1]};
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const bf16x2 two = __builtin_convertvector(left, bf16x2);
+        const Two two = __builtin_convertvector(left, Two);
         p[i][e] = two.x;
         p[i][e + 1] = two.y;
         const uint32_t word = __builtin_bit_cast(uint32_t, two);
-        if (i + 1 < N) left = f32x2{left.x - __uint_as_float(word << 16), left.y - __uint_as_float(word & 0xFFFF0000u)};
+        if (i + 1 < N) left = f32x2{left.x - entry<Core>(word, 0), left.y - entry<Core>(word, 1)};
       }
     }
   }
@@ -252,7 +287,7 @@ struct ChunkShared {
   Core more[kTurned && kScores > kRows ? kScores - kRows : 1];
   alignas(16) Core c[kChunk][kSlice + kPad];
   alignas(16) Core turned[kTurned ? DA : 1][kTurned ? kTurnedRow : 1];
-  alignas(16) float c_high[kChunk], c_low[kChunk], to_end[kChunk], dots[WAVES][kChunk];
+  alignas(16) float c_high[kChunk], c_low[kChunk], to_end[kChunk], dots[WAVES][kChunk], most[WAVES];
 };
 
 // How rows are read: parts of 16 bytes or words of 4 by offsets of 32 bits, where what is not there has one outside the buffer and comes
@@ -485,9 +520,9 @@ __device__ __forceinline__ double sums_to(double x) {
 // What a launch is for: the segments' own contributions to the state and their logarithms' sums; the result; the result and its
 // products with x.
 enum { kStates = 0, kResult = 1, kResultAndDots = 2 };
-// bf16 numbers that stand for one of fp32 where a result goes (one float otherwise)
+// numbers of 16 bits that stand for one of fp32 (one float otherwise)
 template <class Core, int MODE>
-constexpr int kPieces = std::is_same_v<Core, float> ? 1 : MODE == kResult ? 2 : 3;
+constexpr int kPieces = std::is_same_v<Core, float> ? 1 : std::is_same_v<Core, f16_t> || MODE == kResult ? 2 : 3;
 // Waves of a SIMD: as many workgroups as a compute unit's LDS holds, up to two of 8 waves or four of 4, and no less than 128 registers.
 template <class Core, int DA, int WAVES>
 constexpr int kChunkWaves = WAVES == 8 ? (sizeof(ChunkShared<Core, DA, WAVES>) * 2 > 163840 ? 2 : 4) : sizeof(ChunkShared<Core, DA, WAVES>) * 2 > 163840 ? 1 : 2;
@@ -496,6 +531,7 @@ template <class In, class Core, int DA, int WAVES, int MODE, int WAY>
 __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_linear_chunks(LinearArgs A, LinearPass P, LinearChunks C) {
   typedef ChunkShared<Core, DA, WAVES> Shared;
   constexpr bool STATE = MODE == kStates;
+  constexpr bool RANGED = std::is_same_v<Core, f16_t>;
   constexpr int N_OUT = kPieces<Core, MODE>, N_STATE = kPieces<Core, kStates>, kSlice = Shared::kSlice;
   typedef Operand<Core> Op;
   typedef typename Op::Frag Frag;
@@ -599,10 +635,24 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
       // what comes of the state before the chunk
       f32x4 y[4] = {};
       if (busy) {
+        float most = 0.0f;
+        if constexpr (RANGED) {
+#pragma unroll
+          for (int j = 0; j < kJ * kT; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) most = fmaxf(most, fabsf(state[j][r]));
+          most = largest_of_wave(most);
+        }
+        const Range range(most);
 #pragma unroll
         for (int j = 0; j < kJ; ++j) {
           Frag p[N_OUT];
-          pieces_of<Core, N_OUT>(*(const f32x4(*)[kT])&state[j * kT], p);
+          if constexpr (RANGED) {
+            const f32x4 ranged[2] = {state[j * kT] * range.up, state[j * kT + 1] * range.up};
+            pieces_of<Core, N_OUT>(ranged, p);
+          } else {
+            pieces_of<Core, N_OUT>(*(const f32x4(*)[kT])&state[j * kT], p);
+          }
 #pragma unroll
           for (int t = 0; t < 4; ++t) {
             const Frag q = Op::load(&S.a[16 * t + l][0], j, g);
@@ -614,7 +664,7 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
         for (int t = 0; t < 4; ++t) {
           const float here = __builtin_amdgcn_exp2f(S.c_high[16 * t + l] + S.c_low[16 * t + l]);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) y[t][r] *= here;
+          for (int r = 0; r < 4; ++r) y[t][r] *= RANGED ? here * range.down : here;
         }
       }
       // P^T by tiles of 16 x 16: rows s, columns t, s <= t, and two of zeros that complete an operand of two tiles.  A wave's are the
@@ -642,15 +692,31 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
           score[n][r] = s < t || 4 * g + r <= l ? weighted : 0.0f;
         }
       }
+      float most = 0.0f;
+      if constexpr (RANGED) {
+#pragma unroll
+        for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) most = fmaxf(most, fabsf(score[n][r]));
+        most = largest_of_wave(most);
+        if (lane == 0) S.most[wave] = most;
+      }
       __syncthreads();
       // P by rows, over a (and b, which in 16 bits is needed by columns only from here on)
       Core (*const scores)[kChunk][Shared::kScoreRow] = reinterpret_cast<Core (*)[kChunk][Shared::kScoreRow]>(&S.a[0][0]);
       static_assert(Shared::kTurned ? N_OUT <= 3 : kChunk * Shared::kScoreRow * sizeof(Core) <= sizeof(S.a));
+      if constexpr (RANGED)
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) most = fmaxf(most, S.most[w]);
+      const Range range(most);
 #pragma unroll
       for (int n = 0; n < kTiles; ++n) {
         const int pair = tiles >> (8 * (kTiles - 1 - n)) & 255, t = pair >> 4, s = pair & 15;
         if (t > 3) continue;
         float left[4] = {score[n][0], score[n][1], score[n][2], score[n][3]};
+        if constexpr (RANGED)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) left[r] *= range.up;
 #pragma unroll
         for (int k = 0; k < N_OUT; ++k) {
           store_floats<Core, 4>(&scores[k][16 * t + l][16 * s + 4 * g], left);
@@ -682,10 +748,12 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           if (16 * t >= hi || 16 * t + 15 < lo) continue;
+          f32x4 sum = RANGED ? f32x4{} : y[t];
 #pragma unroll
           for (int s = 0; s <= t / kT; ++s)
 #pragma unroll
-            for (int n = N_OUT - 1; n >= 0; --n) y[t] = Op::mma(cf[s], Op::load(&scores[n][16 * t + l][0], s, g), y[t]);
+            for (int n = N_OUT - 1; n >= 0; --n) sum = Op::mma(cf[s], Op::load(&scores[n][16 * t + l][0], s, g), sum);
+          y[t] = RANGED ? y[t] + sum * range.down : sum;
           // rows of the result: step 16 t + l, columns 4 g to 4 g + 3 of the wave's
           const int row = 16 * t + l, when = P.back ? kChunk - 1 - row : row;
           const bool here = row >= lo && row < hi;
@@ -721,32 +789,71 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
     if (!busy) continue;
     if constexpr (STATE) columns(cf);
     const float all = __builtin_amdgcn_exp2f(S.c_high[kChunk - 1] + S.c_low[kChunk - 1]);
-#pragma unroll
-    for (int j = 0; j < kJ * kT; ++j)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) state[j][r] *= all;
-#pragma unroll
-    for (int s = 0; s < kS; ++s) {
-      f32x4 w[kT];
+    const auto weighted = [&](int s, f32x4 (&w)[kT]) {
 #pragma unroll
       for (int t = 0; t < kT; ++t) {
         const f32x4 left = *(const f32x4*)&S.to_end[16 * (s * kT + t) + 4 * g];
 #pragma unroll
         for (int r = 0; r < 4; ++r) w[t][r] = (float)cf[s][4 * t + r] * left[r];
       }
-      Frag p[N_STATE];
-      pieces_of<Core, N_STATE>(w, p);
+    };
+    const auto rows_of_b = [&](int s, int j) {
+      Frag rows;
+      if constexpr (Shared::kTurned) {
+        rows = Op::load(&S.turned[16 * j + l][0], s, g);
+      } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) rows[r] = S.b[16 * s + 4 * g + r][16 * j + l];
+      }
+      return rows;
+    };
+    if constexpr (RANGED) {
+      f32x4 w[kS][kT];
+      float most = 0.0f;
+#pragma unroll
+      for (int s = 0; s < kS; ++s) {
+        weighted(s, w[s]);
+#pragma unroll
+        for (int t = 0; t < kT; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) most = fmaxf(most, fabsf(w[s][t][r]));
+      }
+      const Range range(largest_of_wave(most));
+      Frag p[kS][N_STATE];
+#pragma unroll
+      for (int s = 0; s < kS; ++s) {
+#pragma unroll
+        for (int t = 0; t < kT; ++t) w[s][t] = w[s][t] * range.up;
+        pieces_of<Core, N_STATE>(w[s], p[s]);
+      }
 #pragma unroll
       for (int j = 0; j < kJ * kT; ++j) {
-        Frag rows;
-        if constexpr (Shared::kTurned) {
-          rows = Op::load(&S.turned[16 * j + l][0], s, g);
-        } else {
+        f32x4 sum = {};
 #pragma unroll
-          for (int r = 0; r < 4; ++r) rows[r] = S.b[16 * s + 4 * g + r][16 * j + l];
+        for (int s = 0; s < kS; ++s) {
+          const Frag rows = rows_of_b(s, j);
+#pragma unroll
+          for (int n = N_STATE - 1; n >= 0; --n) sum = Op::mma(rows, p[s][n], sum);
         }
+        state[j] = state[j] * all + sum * range.down;
+      }
+    } else {
 #pragma unroll
-        for (int n = N_STATE - 1; n >= 0; --n) state[j] = Op::mma(rows, p[n], state[j]);
+      for (int j = 0; j < kJ * kT; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) state[j][r] *= all;
+#pragma unroll
+      for (int s = 0; s < kS; ++s) {
+        f32x4 w[kT];
+        weighted(s, w);
+        Frag p[N_STATE];
+        pieces_of<Core, N_STATE>(w, p);
+#pragma unroll
+        for (int j = 0; j < kJ * kT; ++j) {
+          const Frag rows = rows_of_b(s, j);
+#pragma unroll
+          for (int n = N_STATE - 1; n >= 0; --n) state[j] = Op::mma(rows, p[n], state[j]);
+        }
       }
     }
   }

@@ -143,11 +143,11 @@ int width_of(const Rows& r, size_t size, int most, const choco_linear_config& c)
 // Up to so many steps are taken one by one.  us, one by one | in chunks, forward and backward: 160 x 10 heads of 64 in fp32, 4 steps 20 and 65 |
 // 35 and 104, 8 steps 31 and 94 | 36 and 107, 12 steps 41 and 127 | 38 and 110; 64 x 16 heads of 128 in bf16, 4 steps 35 and 113 | 34 and 99, 8 steps 48
 // and 159 | 34 and 100.
-int64_t step_by_step(const choco_linear_config& c) { return c.type == CHOCO_BF16 ? 3 : 8; }
+int64_t step_by_step(const choco_linear_config& c) { return c.type == CHOCO_F32 ? 8 : 3; }
 
 template <class In, int DA, int WAVES, int MODE, int WAY>
 int launch_chunks(const choco_linear_config& c, const LinearArgs& A, const LinearPass& P, const LinearChunks& C) {
-  typedef std::conditional_t<std::is_same_v<In, bf16_t>, bf16_t, float> Core;
+  typedef In Core;
   const size_t lds = sizeof(ChunkShared<Core, DA, WAVES>);
   const auto kernel = k_linear_chunks<In, Core, DA, WAVES, MODE, WAY>;
   if (lds > 65536) {
@@ -160,7 +160,7 @@ int launch_chunks(const choco_linear_config& c, const LinearArgs& A, const Linea
 }
 // Columns of a result that a workgroup takes: 16 a wave, four waves where that is enough, else eight (but four where eight's columns
 // leave no room in LDS).
-int slice_of(const choco_linear_config& c, const LinearPass& P) { return P.dc <= 64 || (c.type != CHOCO_BF16 && P.da > 128) ? 64 : 128; }
+int slice_of(const choco_linear_config& c, const LinearPass& P) { return P.dc <= 64 || (c.type == CHOCO_F32 && P.da > 128) ? 64 : 128; }
 
 template <class In, int MODE>
 int run_chunks(const choco_linear_config& c, const LinearArgs& A, const LinearPass& P, LinearChunks C) {
@@ -169,7 +169,7 @@ int run_chunks(const choco_linear_config& c, const LinearArgs& A, const LinearPa
   C.blocks = (uint32_t)((rows_of(c) * C.segments + 7) / 8 * 8 * C.slices);
   const auto with_way = [&](auto dim, auto waves, auto way) -> int {
     constexpr int DA = decltype(dim)::value, WAVES = decltype(waves)::value;
-    if constexpr (WAVES == 8 && DA > 128 && !std::is_same_v<In, bf16_t>) return CHOCO_E_UNSUPPORTED;     // (slice_of does not say so)
+    if constexpr (WAVES == 8 && DA > 128 && std::is_same_v<In, float>) return CHOCO_E_UNSUPPORTED;     // (slice_of does not say so)
     else return launch_chunks<In, DA, WAVES, MODE, decltype(way)::value>(c, A, P, C);
   };
   const auto with_waves = [&](auto dim, auto waves) -> int {

@@ -88,8 +88,11 @@ def bound(exact, magnitude, dtype, terms):
 
 
 def check(got, exact, magnitude, terms, name):
-    off = (got.double() - exact).abs()
     allowed = bound(exact, magnitude, got.dtype, terms)
+    # what lies half a step or more beyond the type's largest number (fp16: 65504 + 16) rounds to infinity
+    limits = torch.finfo(got.dtype)
+    beyond = got.isinf() & (got.sign() == exact.sign()) & (exact.abs() + allowed >= limits.max * (1 + limits.eps / 4))
+    off = torch.where(beyond, 0.0, (got.double() - exact).abs())
     assert bool((off <= allowed).all()), (name, float((off / allowed).max()), off.max().item())
 
 
@@ -160,6 +163,16 @@ def test_gates_that_forget_nothing_and_gates_that_forget_all():
     q, k, v, g, h0, _, dy, dlast = make(2, 300, 2, 16, 16, F32)
     for value in (0.0, -1e-30, -50.0, -199.0, -1e4, -torch.inf):
         check_all(q, k, v, torch.full_like(g, value), h0, None, dy, dlast)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("size_q, size_k, size_v", [(2.0 ** -10, 256.0, 256.0), (2.0 ** -8, 2.0 ** -8, 2.0 ** -8), (64.0, 64.0, 2.0 ** -9), (1.0, 0.0, 1.0)])
+@pytest.mark.parametrize("N", [5, 200])
+def test_magnitudes(dtype, size_q, size_k, size_v, N):
+    # states and products of q and k beyond fp16's range, results within; values near its least; nothing at all
+    q, k, v, g, h0, _, dy, dlast = make(2, N, 2, 24, 40, dtype, seed=4, gate="head")
+    check_all(q * size_q, k * size_k, v * size_v, g, h0 * (size_k * size_v), None, dy * 2.0 ** -6 / max(size_k * size_v, size_q * size_v, 2.0 ** -6),
+              dlast * 2.0 ** -6)
 
 
 @pytest.mark.parametrize("N", [1, 30, 400])
