@@ -557,13 +557,21 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
   f32x4 state[kJ * kT];       // rows 16 j + 4 g + r of column `col + l`
   const float* from = STATE ? nullptr : C.states ? C.states + (bh * C.states_of + segment) * entries : P.first ? P.first + bh * P.first_of * entries : nullptr;
   const bool column = col + l < P.dc;
+  if (P.state_a == 1 && P.da % 4 == 0 && ((uintptr_t)from & 15) == 0) {      // four rows are next to one another (and so are on their border)
 #pragma unroll
-  for (int j = 0; j < kJ * kT; ++j)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int row = 16 * j + 4 * g + r;
-      state[j][r] = from && column && row < P.da ? from[(int64_t)row * P.state_a + (int64_t)(col + l) * P.state_c] : 0.0f;
+    for (int j = 0; j < kJ * kT; ++j) {
+      const int row = 16 * j + 4 * g;
+      state[j] = from && column && row < P.da ? *(const f32x4*)(from + (int64_t)(col + l) * P.state_c + row) : f32x4{};
     }
+  } else {
+#pragma unroll
+    for (int j = 0; j < kJ * kT; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int row = 16 * j + 4 * g + r;
+        state[j][r] = from && column && row < P.da ? from[(int64_t)row * P.state_a + (int64_t)(col + l) * P.state_c] : 0.0f;
+      }
+  }
   const auto keep = [&](float* to, float w) {
     int mine = 4 * g;
     asm volatile("" : "+v"(mine));      // (or its addresses would be kept in registers over the chunks)
