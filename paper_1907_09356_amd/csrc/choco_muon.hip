@@ -18,8 +18,20 @@ using namespace choco;
 namespace {
 
 constexpr int kMostIterations = 32;
-// Tiles of 128 x 128 entries where there are at least so many (of the largest product) to fill the card with, else of 64 x 64.
-constexpr double kFewTiles = 384;
+// Tiles of 128 x 128 entries where there are at least so many to fill the card with, of X' or of the lower triangles of P and Q, else of
+// 64 x 64.  us, all products in tiles of 64 | of 128 (so many of X', of a triangle): 333 x 1000 194 | 383 (24, 6); four of 650 x 650 373 | 490 (144,
+// 84), eight 518 | 478 (288, 168); two of 650 x 2600 462 | 768 (252, 42), four 753 | 816 (504, 84); 2048 x 2048 1198 | 1084 (256, 136); 64 of 256 x 256
+// 424 | 332 (256, 192); eight of 1024 x 1024 1201 | 798 (512, 288).
+constexpr double kFewTiles = 200, kFewOfTriangle = 128;
+struct Tiles {
+  int apply = 128, gram = 128;      // sides
+  double applies = 0.0, grams = 0.0;
+  void add(int64_t rows, int64_t cols, double count);
+  void choose() {
+    if (applies < kFewTiles) apply = 64;
+    if (grams < kFewOfTriangle) gram = 64;
+  }
+};
 // Matrices that a step takes at once: operands of so many bytes, or one matrix.
 constexpr int64_t kRoundBytes = (int64_t)1 << 30;
 
@@ -32,8 +44,8 @@ bool whole(int64_t rows, int64_t cols) {
   return whole_bytes(a, b) <= kWholeBytes && ra * rb <= 256 * kWholeTiles * kWholeWaves;
 }
 
-// A shape's sides, operands and tiles (tile = 0: taken whole); `count` and what is behind the begins are the caller's.
-MuonShape shape_from(int64_t rows, int64_t cols, int tile) {
+// A shape's sides, operands and tiles (null: taken whole); `count` and what is behind the begins are the caller's.
+MuonShape shape_from(int64_t rows, int64_t cols, const Tiles* tiles) {
   MuonShape S{};
   S.rows = (int32_t)rows;
   S.cols = (int32_t)cols;
@@ -43,15 +55,21 @@ MuonShape shape_from(int64_t rows, int64_t cols, int tile) {
   S.b_ld = (int32_t)padded(S.b);
   S.scratch_of = (muon_scratch(S.a, S.b, S.a_ld, S.b_ld) + 255) / 256 * 256;
   S.start_tiles = (uint32_t)(((rows + 63) / 64) * ((cols + 63) / 64));
-  if (tile == 0) {      // a workgroup takes all of it
+  if (!tiles) {      // a workgroup takes all of it
     S.start_tiles = 1;
     S.scratch_of = 0;
     return S;
   }
-  const int64_t high = tiles_of(S.a, tile);
+  const int64_t high = tiles_of(S.a, tiles->gram);
   S.gram_tiles = (uint32_t)(high * (high + 1) / 2);
-  S.apply_tiles = (uint32_t)(high * tiles_of(S.b, tile));
+  S.apply_tiles = (uint32_t)(tiles_of(S.a, tiles->apply) * tiles_of(S.b, tiles->apply));
   return S;
+}
+void Tiles::add(int64_t rows, int64_t cols, double count) {
+  const Tiles large;
+  const MuonShape S = shape_from(rows, cols, &large);
+  applies += S.apply_tiles * count;
+  grams += S.gram_tiles * count;
 }
 
 // Matrices that one set of launches takes.
@@ -61,8 +79,14 @@ struct Round {
   int64_t lds;              // of matrices taken whole: the most that one needs
 };
 
-template <class T, bool STEP, int TILE>
-int run_round(MuonArgs A, const Round& R, int iterations, hipStream_t stream) {
+template <int KIND>
+void launch_product(const MuonArgs& A, uint32_t tiles, int side, hipStream_t stream) {
+  if (side == 128) k_muon_product<KIND, 128><<<dim3(tiles), 256, 0, stream>>>(A);
+  else k_muon_product<KIND, 64><<<dim3(tiles), 256, 0, stream>>>(A);
+}
+
+template <class T, bool STEP>
+int run_tiles(MuonArgs A, const Round& R, int iterations, const Tiles& tiles, hipStream_t stream) {
   k_muon_squares<T, STEP><<<dim3(R.start_tiles), 256, 0, stream>>>(A);
   TRY_HIP(hipGetLastError());
   k_muon_start<T, STEP><<<dim3(R.start_tiles), 256, 0, stream>>>(A);
@@ -70,17 +94,17 @@ int run_round(MuonArgs A, const Round& R, int iterations, hipStream_t stream) {
   for (int i = 0; i < iterations; ++i) {
     A.now = i & 1;
     A.last = i + 1 == iterations;
-    k_muon_product<kGram, TILE><<<dim3(R.gram_tiles), 256, 0, stream>>>(A);
+    launch_product<kGram>(A, R.gram_tiles, tiles.gram, stream);
     TRY_HIP(hipGetLastError());
-    k_muon_product<kSquare, TILE><<<dim3(R.gram_tiles), 256, 0, stream>>>(A);
+    launch_product<kSquare>(A, R.gram_tiles, tiles.gram, stream);
     TRY_HIP(hipGetLastError());
-    k_muon_product<kApply, TILE><<<dim3(R.apply_tiles), 256, 0, stream>>>(A);
+    launch_product<kApply>(A, R.apply_tiles, tiles.apply, stream);
     TRY_HIP(hipGetLastError());
   }
   return CHOCO_OK;
 }
 template <class T, bool STEP>
-int run_round(const MuonArgs& A, const Round& R, int iterations, int tile, hipStream_t stream) {
+int run_round(const MuonArgs& A, const Round& R, int iterations, const Tiles& tiles, hipStream_t stream) {
   if (R.lds > 0) {
     static std::atomic<uint64_t> done{0};
     TRY_HIP(allow_lds((const void*)k_muon_whole<T, STEP>, kWholeBytes, done));
@@ -88,7 +112,7 @@ int run_round(const MuonArgs& A, const Round& R, int iterations, int tile, hipSt
     TRY_HIP(hipGetLastError());
     return CHOCO_OK;
   }
-  return tile == 128 ? run_round<T, STEP, 128>(A, R, iterations, stream) : run_round<T, STEP, 64>(A, R, iterations, stream);
+  return run_tiles<T, STEP>(A, R, iterations, tiles, stream);
 }
 
 // ---- a stack of matrices ----
@@ -111,22 +135,24 @@ int check_orthogonalize(const choco_orthogonalize_config* c) {
 
 struct StackLayout {
   MuonShape shape;
-  int tile;
+  Tiles tiles;
+  bool whole;
   int64_t each;       // matrices taken at once
   size_t partials, scratch, total;
 };
 int stack_layout(const choco_orthogonalize_config& c, StackLayout& L) {
   L = {};
   if (c.batch == 0 || c.rows == 0 || c.cols == 0) return CHOCO_OK;
-  L.tile = whole(c.rows, c.cols) ? 0 : 128;
-  L.shape = shape_from(c.rows, c.cols, L.tile);
-  if (L.tile > 0 && (double)L.shape.apply_tiles * (double)c.batch < kFewTiles) L.shape = shape_from(c.rows, c.cols, L.tile = 64);
+  L.whole = whole(c.rows, c.cols);
+  L.tiles.add(c.rows, c.cols, (double)c.batch);
+  L.tiles.choose();
+  L.shape = shape_from(c.rows, c.cols, L.whole ? nullptr : &L.tiles);
   const double most = std::max<double>(L.shape.start_tiles, std::max(L.shape.gram_tiles, L.shape.apply_tiles));
   if (!launch_fits(most, 256)) return CHOCO_E_UNSUPPORTED;
-  L.each = L.tile == 0 ? c.batch : std::min<int64_t>(c.batch, std::max<int64_t>(1, kRoundBytes / L.shape.scratch_of));
+  L.each = L.whole ? c.batch : std::min<int64_t>(c.batch, std::max<int64_t>(1, kRoundBytes / L.shape.scratch_of));
   while (L.each > 1 && !launch_fits(most * (double)L.each, 512)) L.each /= 2;
   Parts parts;
-  if (L.tile > 0) L.partials = parts.take((size_t)L.each * L.shape.start_tiles * sizeof(double));
+  if (!L.whole) L.partials = parts.take((size_t)L.each * L.shape.start_tiles * sizeof(double));
   L.scratch = parts.take((size_t)L.each * (size_t)L.shape.scratch_of);
   L.total = parts.at;
   return CHOCO_OK;
@@ -157,7 +183,7 @@ int check_muon(const choco_muon_config* c) {
 }
 
 struct MuonLayout {
-  int tile;
+  Tiles tiles;
   size_t state_end, table, partials, scratch, total;
 };
 // The matrices in rounds, and the workspace.  CHOCO_E_UNSUPPORTED: one that no launch holds.
@@ -165,10 +191,9 @@ int muon_layout(const choco_muon_config& c, std::vector<MuonShape>& table, std::
   const int64_t ld = resolve_ld(c);
   int64_t moment = 0, most_scratch = 0, most_partials = 0, scratch = 0, partials = 0;
   Round now{};
-  double tiles_in_all = 0.0;
   for (int32_t t = 0; t < c.ntensors; ++t)
-    if (c.rows_host[t] > 0 && c.cols_host[t] > 0 && !whole(c.rows_host[t], c.cols_host[t])) tiles_in_all += (double)c.n * shape_from(c.rows_host[t], c.cols_host[t], 128).apply_tiles;
-  L.tile = tiles_in_all < kFewTiles ? 64 : 128;
+    if (c.rows_host[t] > 0 && c.cols_host[t] > 0 && !whole(c.rows_host[t], c.cols_host[t])) L.tiles.add(c.rows_host[t], c.cols_host[t], (double)c.n);
+  L.tiles.choose();
   const auto close = [&] {
     if (now.count > 0) rounds.push_back(now);
     now = {};
@@ -186,7 +211,7 @@ int muon_layout(const choco_muon_config& c, std::vector<MuonShape>& table, std::
     if (rows == 0 || cols == 0 || whole(rows, cols) != (i < c.ntensors)) continue;
     const bool alone = i < c.ntensors;
     if (!alone && now.lds > 0) close();
-    MuonShape S = shape_from(rows, cols, alone ? 0 : L.tile);
+    MuonShape S = shape_from(rows, cols, alone ? nullptr : &L.tiles);
     S.source = S.target = start;
     S.source_of = S.target_of = ld;
     S.source_ld = S.target_ld = cols;
@@ -287,9 +312,9 @@ int choco_orthogonalize(const choco_orthogonalize_config* cfg, const void* x_dev
     A.partials = (double*)((char*)workspace_dev + L.partials);
     A.scratch = (char*)workspace_dev + L.scratch;
     const uint32_t count = (uint32_t)A.one.count;
-    const Round R{0, 1, count * L.shape.start_tiles, count * L.shape.gram_tiles, count * L.shape.apply_tiles, L.tile > 0 ? 0 : whole_bytes(c.rows < c.cols ? c.rows : c.cols, c.rows < c.cols ? c.cols : c.rows)};
+    const Round R{0, 1, count * L.shape.start_tiles, count * L.shape.gram_tiles, count * L.shape.apply_tiles, L.whole ? whole_bytes(L.shape.a, L.shape.b) : 0};
     int rc = CHOCO_OK;
-    with_type(c.type, [&](auto x) { rc = run_round<decltype(x), false>(A, R, c.iterations, L.tile, (hipStream_t)c.stream); });
+    with_type(c.type, [&](auto x) { rc = run_round<decltype(x), false>(A, R, c.iterations, L.tiles, (hipStream_t)c.stream); });
     if (rc) return rc;
   }
   return CHOCO_OK;
@@ -359,8 +384,8 @@ int choco_muon_step(choco_muon* a, const void* g_dev, int32_t grad_type, float l
     A.source = g_dev;
     A.grad_scale = grad_scale_dev;
     A.lr = lr;
-    const int rc = grad_type == CHOCO_F32 ? run_round<float, true>(A, R, a->iterations, a->layout.tile, a->stream)
-                                          : run_round<bf16_t, true>(A, R, a->iterations, a->layout.tile, a->stream);
+    const int rc = grad_type == CHOCO_F32 ? run_round<float, true>(A, R, a->iterations, a->layout.tiles, a->stream)
+                                          : run_round<bf16_t, true>(A, R, a->iterations, a->layout.tiles, a->stream);
     if (rc) return rc;
   }
   return CHOCO_OK;
