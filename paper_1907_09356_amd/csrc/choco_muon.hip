@@ -32,8 +32,9 @@ struct Tiles {
     if (grams < kFewOfTriangle) gram = 64;
   }
 };
-// Matrices that a step takes at once: operands of so many bytes, or one matrix.
-constexpr int64_t kRoundBytes = (int64_t)1 << 30;
+// Matrices that a step takes at once: operands of at most so many bytes, or one matrix.  (48 of 2600 x 650, whose operands are 1.2 GB: at once
+// 4.97 ms; in rounds of 1 GB 5.61, of 512 MB 5.69, of 256 MB, which stay in the last-level cache, 6.19.)
+constexpr int64_t kRoundBytes = (int64_t)1 << 31;
 
 int64_t padded(int64_t n) { return (n + kMuonPad - 1) / kMuonPad * kMuonPad; }
 int64_t tiles_of(int64_t n, int tile) { return (n + tile - 1) / tile; }
@@ -151,6 +152,8 @@ int stack_layout(const choco_orthogonalize_config& c, StackLayout& L) {
   if (!launch_fits(most, 256)) return CHOCO_E_UNSUPPORTED;
   L.each = L.whole ? c.batch : std::min<int64_t>(c.batch, std::max<int64_t>(1, kRoundBytes / L.shape.scratch_of));
   while (L.each > 1 && !launch_fits(most * (double)L.each, 512)) L.each /= 2;
+  const int64_t times = (c.batch + L.each - 1) / L.each;      // of like sizes
+  L.each = (c.batch + times - 1) / times;
   Parts parts;
   if (!L.whole) L.partials = parts.take((size_t)L.each * L.shape.start_tiles * sizeof(double));
   L.scratch = parts.take((size_t)L.each * (size_t)L.shape.scratch_of);
@@ -194,6 +197,12 @@ int muon_layout(const choco_muon_config& c, std::vector<MuonShape>& table, std::
   for (int32_t t = 0; t < c.ntensors; ++t)
     if (c.rows_host[t] > 0 && c.cols_host[t] > 0 && !whole(c.rows_host[t], c.cols_host[t])) L.tiles.add(c.rows_host[t], c.cols_host[t], (double)c.n);
   L.tiles.choose();
+  // rounds of like sizes, as many as it takes (a little more than their share each, as matrices are not divided)
+  double all = 0.0;
+  for (int32_t t = 0; t < c.ntensors; ++t)
+    if (c.rows_host[t] > 0 && c.cols_host[t] > 0 && !whole(c.rows_host[t], c.cols_host[t]))
+      all += (double)c.n * (double)shape_from(c.rows_host[t], c.cols_host[t], &L.tiles).scratch_of;
+  const int64_t most = (int64_t)std::min<double>(kRoundBytes, 1.02 * all / std::max(1.0, std::ceil(all / (double)kRoundBytes)));
   const auto close = [&] {
     if (now.count > 0) rounds.push_back(now);
     now = {};
@@ -223,7 +232,7 @@ int muon_layout(const choco_muon_config& c, std::vector<MuonShape>& table, std::
     if (alone) now.lds = std::max(now.lds, whole_bytes(S.a, S.b));
     for (int32_t w = 0; w < c.n;) {
       const double taken = std::max<double>(now.start_tiles, std::max(now.gram_tiles, now.apply_tiles));
-      int64_t count = alone ? c.n - w : std::min<int64_t>(c.n - w, (kRoundBytes - scratch) / S.scratch_of);
+      int64_t count = alone ? c.n - w : std::min<int64_t>(c.n - w, (most - scratch) / S.scratch_of);
       while (count > 0 && !launch_fits(taken + tiles * (double)count, 512)) count /= 2;
       if (count < 1) {
         if (now.count > 0) {

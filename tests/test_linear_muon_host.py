@@ -185,12 +185,12 @@ def test_muon_refuses_a_small_workspace_and_missing_handles():
 
 
 def test_muon_workspace_is_bounded_by_rounds():
-    # 64 workers' 4096 x 1024 matrices: operands of a round stay near 1 GB, the momenta are what grows
+    # 64 workers' 4096 x 1024 matrices: operands of a round stay below 2 GB, the momenta are what grows
     sizes = []
     for n in (32, 64):
         cfg, keep = T.make_muon_config(n, 4096 * 1024, 4096 * 1024, ([0], [4096], [1024]))
         out = ctypes.c_size_t()
         assert T.lib().choco_muon_workspace_bytes(ctypes.byref(cfg), ctypes.byref(out)) == B.OK
         sizes.append(out.value - n * 4096 * 1024 * 4)
-    assert sizes[0] <= 1.1 * 2 ** 30 and abs(sizes[1] - sizes[0]) <= 2 ** 20
+    assert sizes[0] <= 1.01 * 2 ** 31 and abs(sizes[1] - sizes[0]) <= 2 ** 20
     assert np.isfinite(sizes).all()
