@@ -5,6 +5,12 @@
 //   y:  a, b, c = q, k, v              dq: dy, v, k     (the same states transposed)
 //   dk: v, dy, q   backwards           dv: k, q, dy     backwards
 // where w = e^g_t forwards, and backwards the next step's, 1 at a sequence's last.
+//
+// Measured, us a call (what it has to read and write at the rate of a large copy, 5.1 TB/s): one token of 64 x 16 heads of 128 in bf16 26 (26),
+// of 160 x 13 of 50 in fp32 15 (8); 160 x 35 x 13 x 50 in fp32 62 (17), backward 210 (25); 2 x 32,768 x 16 x 128 in bf16, lengths from a half on,
+// 479 to 497 (172); 8 x 2000 x 20 x 64 in fp16, q and k shared by four, 91 (21); backward of 4 x 16,384 x 10 x 128 in bf16 1,080 (230).
+// Before: step by step all of it, 69,800 and 131,900 for the long ones; chunks without loads ahead 1,320 and 2,840; every wave its own P, 780
+// and 2,120; loads with branches, 710 and 2,030; four waves and 64 columns a workgroup 640 and 1,610.
 #pragma once
 
 #include <type_traits>
@@ -59,7 +65,8 @@ __device__ __forceinline__ void store_result(const LinearPass& P, int64_t at, fl
 
 // ---- step by step ----
 // A workgroup takes a slice of columns and holds the state in registers, V columns of every 4 V-th row a lane (V as the state in memory is
-// aligned).  Bound by the state, in and out once: for a step of D x D, 8 D^2 bytes against 5 D^2 operations.
+// aligned).  Bound by the state, in and out once: for a step of D x D, 8 D^2 bytes against 5 D^2 operations.  One token of 64 x 16 heads of 128
+// in bf16 26 us, 5.1 TB/s (a column a lane, a quarter of the rows a wave: 33), of 160 x 13 of 50 in fp32 15, 2.8 TB/s (20).
 constexpr int kLinearStage = 8;     // steps whose a and b are in LDS at a time
 
 template <class T, int V, int D>
@@ -161,6 +168,11 @@ __global__ __launch_bounds__(256) void k_linear_steps(LinearArgs A, LinearPass P
 // Entries of 32 bits go to the fp32 matrix instruction.  Those of 16 bits are operands as they are; what is fp32 by nature (P, S, weighted c)
 // enters as a sum of numbers of that type.  bf16: two of them (2^-17) for a result of 16 bits, three (2^-25) for states and wherever the
 // result also goes into fp32 sums.  fp16: two (2^-22), after a power of two has brought the largest into fp16's range.
+//
+// What bounds it: of a chunk of 64 x 128 x 128 in bf16 a SIMD's four waves take some 10,000 cycles of vector instructions (half of them split
+// fp32 numbers), 7,000 of matrix instructions, and LDS 5,000; memory 5,000 at the rate of a copy.  They overlap by half: 363 us for the
+// results of 2 x 32,768 x 16 x 128, 2.5 TB/s.  A workgroup has eight waves in 128 registers, two of them a compute unit: with one of them
+// (256 registers) 488 us, with four waves and 64 columns 527.
 constexpr int kChunk = 64;
 constexpr float kLog2Least = -300.0f;     // stands for -infinity: less than any difference that counts
 
@@ -523,7 +535,7 @@ enum { kStates = 0, kResult = 1, kResultAndDots = 2 };
 // numbers of 16 bits that stand for one of fp32 (one float otherwise)
 template <class Core, int MODE>
 constexpr int kPieces = std::is_same_v<Core, float> ? 1 : std::is_same_v<Core, f16_t> || MODE == kResult ? 2 : 3;
-// Waves of a SIMD: as many workgroups as a compute unit's LDS holds, up to two of 8 waves or four of 4, and no less than 128 registers.
+// Waves of a SIMD: those of two workgroups where a compute unit's LDS holds two.
 template <class Core, int DA, int WAVES>
 constexpr int kChunkWaves = WAVES == 8 ? (sizeof(ChunkShared<Core, DA, WAVES>) * 2 > 163840 ? 2 : 4) : sizeof(ChunkShared<Core, DA, WAVES>) * 2 > 163840 ? 1 : 2;
 
@@ -880,7 +892,8 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
   if (P.last && !C.states) keep(P.last + bh * entries, P.back && len > 0 ? linear_decay(log_gate(A, b, 0, h)) : 1.0f);
 }
 
-// From the segments' own contributions to the states before them, in place, and the last one.
+// From the segments' own contributions to the states before them, in place, and the last one.  Bound by memory: 40 heads of 128 x 128 in 64
+// segments 64 us, 5.3 TB/s (one segment after the other, each waited for, 93).
 __global__ __launch_bounds__(256) void k_linear_scan(LinearArgs A, float* states, const double* totals, int segments, int64_t entries, const float* first,
                                                      float* last, bool back) {
   const int64_t each = (entries + 255) / 256, count = A.batch * A.heads * each;
@@ -912,7 +925,8 @@ __global__ __launch_bounds__(256) void k_linear_scan(LinearArgs A, float* states
 
 // ---- the gates' gradient ----
 // dg_t = sum over s >= t of (q_s dq_s - k_s dk_s) up to any later step u, and what goes from before u past it, <E_u, S_u>: pieces of
-// kLinearSave steps, each with the states at its end, so that the differences' errors do not add up over a sequence.
+// kLinearSave steps, each with the states at its end, so that the differences' errors do not add up over a sequence.  Bound by these states:
+// 4 x 16,384 x 10 x 128 72 us, 4.7 TB/s.
 struct LinearGates {
   const float *q_dots, *k_dots, *saved, *later, *dlast;   // later: states that the backwards passes have before their pieces
   int64_t saved_of, later_of;

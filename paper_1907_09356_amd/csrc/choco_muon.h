@@ -5,6 +5,11 @@
 // L[m][k] R[n][k]:  P from X and X,  Q = a I + b P + c P^2 from P and P (symmetric),  X' = Q X from Q and X^T.  So X is held both
 // ways, X^T twice (a launch reads one and writes the other).
 //
+// Bound by matrix instructions: with symmetric products by half 5 (3 a^2 b + a^3) operations, three fp16 instructions each, against some 20 bytes
+// an entry.  Measured, us: eight workers' six 2600 x 650 4,980 (2,230 at the rate of a large fp16 product by the library), 16 of 1024 x 640 720
+// (317), 333 x 1000 alone 193, four of 64 x 192 37.  Before: products straight out of memory, a wave 32 x 32, 18,840, 2,460, 480 and 158; in tiles
+// of 128 through LDS 6,620 and 1,030; neighbouring tiles on one XCD 6,000 and 760; a X by Q's diagonal 5,640; all matrices at once 4,980.
+//
 // Operands are two fp16 numbers for one fp32, 2^13 x = high + low.  No entry of X, P or Q is beyond 3.5 (their singular
 // values are not), so high is below 2^15, and low keeps 11 bits more down to 2^-24: 22 bits of an entry above 2^-15, 2^-38 of a smaller
 // one.  A product takes high high + high low + low high on the matrix cores, where sums are fp32; the last, low low, is 2^-22 of the
@@ -207,7 +212,8 @@ __global__ __launch_bounds__(256) void k_muon_start(MuonArgs A) {
 }
 
 // ---- small matrices ----
-// A workgroup takes a whole matrix, whose operands stay in LDS from the first iteration to the last: rows end on a multiple of 32 entries
+// A workgroup takes a whole matrix, whose operands stay in LDS from the first iteration to the last.  Bound by latency: a product, its reads and
+// writes of LDS and a barrier, is some 2 us, four of 64 x 192 37 in all (eight waves 56; seventeen launches 115).  Rows end on a multiple of 32 entries
 // and 8 more, which are 4 banks modulo 16, so that 16 lanes that read 16 bytes of 16 rows meet all banks.
 constexpr int kWholeWaves = 16;
 constexpr int64_t kWholeBytes = 160 * 1024 - 256;
@@ -397,7 +403,8 @@ __device__ __forceinline__ void to_lds(const void* from, void* to) {
 }
 
 // A workgroup makes a tile of TILE x TILE entries.  A step along the inner index takes 32 entries of TILE rows of both operands, high and
-// low, into one of two buffers while the other one's are multiplied.  In a buffer a row's four 16-byte parts are exchanged by bits 2
+// low, into one of two buffers while the other one's are multiplied.  48 matrices of 2600 x 650: P 224 to 232 us, X' 570 to 617, 0.55 to 0.7 of the rate of a large
+// product by the library on the tiles as they are (a wave reads 16 KB of LDS for 48 instructions: both are busy alike).  In a buffer a row's four 16-byte parts are exchanged by bits 2
 // and 3 of its number, so that 16 lanes that read one part of 16 rows meet 16 different banks.
 //   TILE 128: a wave makes a quarter of the tile, and loads one plane of the operands for all.
 //   TILE 64, where the tiles are too few to fill the card: every wave makes the whole tile, of every fourth step, from buffers of its own,
