@@ -220,7 +220,7 @@ struct Operand<f16_t> {
 struct Range {
   float up, down;
   __device__ __forceinline__ explicit Range(float most) {
-    const uint32_t e = max(__float_as_uint(most) >> 23, 12u);      // (not negative; infinite stays so)
+    const uint32_t e = max(__float_as_uint(most) >> 23, 12u);      // (not negative, not infinite)
     up = __uint_as_float((265u - e) << 23);
     down = __uint_as_float((e - 11u) << 23);
   }
@@ -237,6 +237,20 @@ __device__ __forceinline__ float largest_of_wave(float x) {
   x = larger_of<0x142, 10>(x);
   x = larger_of<0x143, 12>(x);
   return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), 63));
+}
+// The largest magnitude of a wave's numbers, which `each` hands out; where one is infinite, of the others, which then keep their places.
+template <class Each>
+__device__ __forceinline__ float largest_of_wave(Each each) {
+  constexpr float kInfinite = __builtin_inff();
+  float most = 0.0f;
+  each([&](float x) { most = fmaxf(most, fabsf(x)); });
+  most = largest_of_wave(most);
+  if (most == kInfinite) {
+    most = 0.0f;
+    each([&](float x) { most = fmaxf(most, fabsf(x) < kInfinite ? fabsf(x) : 0.0f); });
+    most = largest_of_wave(most);
+  }
+  return most;
 }
 // fp32 numbers of an operand as so many operands that add up to it.
 template <class Core, int N>
@@ -656,13 +670,13 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
       f32x4 y[4] = {};
       if (busy) {
         float most = 0.0f;
-        if constexpr (RANGED) {
+        if constexpr (RANGED)
+          most = largest_of_wave([&](auto&& see) {
 #pragma unroll
-          for (int j = 0; j < kJ * kT; ++j)
+            for (int j = 0; j < kJ * kT; ++j)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) most = fmaxf(most, fabsf(state[j][r]));
-          most = largest_of_wave(most);
-        }
+              for (int r = 0; r < 4; ++r) see(state[j][r]);
+          });
         const Range range(most);
 #pragma unroll
         for (int j = 0; j < kJ; ++j) {
@@ -714,11 +728,12 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
       }
       float most = 0.0f;
       if constexpr (RANGED) {
+        most = largest_of_wave([&](auto&& see) {
 #pragma unroll
-        for (int n = 0; n < kTiles; ++n)
+          for (int n = 0; n < kTiles; ++n)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) most = fmaxf(most, fabsf(score[n][r]));
-        most = largest_of_wave(most);
+            for (int r = 0; r < 4; ++r) see(score[n][r]);
+        });
         if (lane == 0) S.most[wave] = most;
       }
       __syncthreads();
@@ -829,16 +844,16 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
     };
     if constexpr (RANGED) {
       f32x4 w[kS][kT];
-      float most = 0.0f;
 #pragma unroll
-      for (int s = 0; s < kS; ++s) {
-        weighted(s, w[s]);
+      for (int s = 0; s < kS; ++s) weighted(s, w[s]);
+      const Range range(largest_of_wave([&](auto&& see) {
 #pragma unroll
-        for (int t = 0; t < kT; ++t)
+        for (int s = 0; s < kS; ++s)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) most = fmaxf(most, fabsf(w[s][t][r]));
-      }
-      const Range range(largest_of_wave(most));
+          for (int t = 0; t < kT; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) see(w[s][t][r]);
+      }));
       Frag p[kS][N_STATE];
 #pragma unroll
       for (int s = 0; s < kS; ++s) {

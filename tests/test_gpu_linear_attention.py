@@ -203,6 +203,26 @@ def test_a_value_that_is_not_finite_stays_in_its_sequence_and_head():
         assert torch.equal(y[1, :max(0, at - 63)], y2[1, :max(0, at - 63)]) and bool(y2[1, at:, 0].isnan().all())
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("N", [2, 40, 200])
+def test_an_infinite_value_of_one_column_leaves_the_others(dtype, N):
+    # y's column depends on v's alone, and so does the state's
+    q, k, v, g, h0, _, _, _ = make(2, N, 2, 24, 40, dtype, seed=N)
+    n = whole(None, 2, N)
+    exact, size = reference(q, k, v, g, h0, n), reference(q.abs(), k.abs(), v.abs(), g, h0.abs(), n)
+    v = v.clone()
+    v[1, N // 3, 1, 5] = torch.inf
+    h0 = h0.clone()
+    h0[0, 0, 3, 17] = -torch.inf
+    y, last, _ = T.linear_attention(q, k, v, g, h0=h0)
+    assert not bool(y[1, N // 3:, 1, 5].isfinite().any()) and not bool(y[0, :, 0, 17].isfinite().any())
+    keep = torch.ones((2, 2, 40), dtype=torch.bool, device="cuda")
+    keep[1, 1, 5] = keep[0, 0, 17] = False
+    terms = 24 + 40 + N + 64
+    for name, got, at in (("y", y, keep[:, None].expand(y.shape)), ("last", last, keep[:, :, None].expand(last.shape))):
+        check(got[at], exact[name][at], size[name][at], terms, name)
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_without_a_first_state_and_without_a_gradient_of_the_last(dtype):
     for N in (1, 70, 600):

@@ -68,6 +68,12 @@ def test_against_64_bits(rows, cols, iterations):
     check(T.orthogonalize(x, iterations=iterations), iterate(x, iterations), iterations)
 
 
+@pytest.mark.parametrize("rows, cols", [(30, 500), (500, 30), (32, 512), (512, 32), (33, 512), (64, 224), (224, 64), (64, 256), (96, 128), (3, 512), (1, 600)])
+def test_about_where_one_workgroup_takes_a_matrix(rows, cols):
+    x = matrices((4, rows, cols), seed=rows)
+    check(T.orthogonalize(x), iterate(x, 5), 5)
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
 @pytest.mark.parametrize("scale", [1e-4, 1.0, 100.0])
 def test_types_and_magnitudes(dtype, scale):
