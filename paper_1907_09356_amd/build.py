@@ -4,7 +4,8 @@ import subprocess
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
-SRC = [os.path.join(HERE, "csrc", name) for name in ("choco.hip", "choco_train.hip", "choco_linear.hip", "choco_muon.hip")]
+SRC = [os.path.join(HERE, "csrc", name) for name in ("choco.hip", "choco_train.hip", "choco_linear.hip", "choco_linear_f32.hip",
+                                                       "choco_linear_bf16.hip", "choco_linear_f16.hip", "choco_muon.hip")]
 LIB = os.path.join(HERE, "libchoco.so")
 
 # -ffp-contract=off: every product and sum is rounded on its own, which the

@@ -907,6 +907,7 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
   if (P.last && !C.states) keep(P.last + bh * entries, P.back && len > 0 ? linear_decay(log_gate(A, b, 0, h)) : 1.0f);
 }
 
+#ifndef CHOCO_LINEAR_TYPE      // (where only one type's chunks are compiled)
 // From the segments' own contributions to the states before them, in place, and the last one.  Bound by memory: 40 heads of 128 x 128 in 64
 // segments 64 us, 5.3 TB/s (one segment after the other, each waited for, 93).
 __global__ __launch_bounds__(256) void k_linear_scan(LinearArgs A, float* states, const double* totals, int segments, int64_t entries, const float* first,
@@ -1022,6 +1023,8 @@ __global__ __launch_bounds__(256) void k_linear_gate_sums(const float* parts, in
   __syncthreads();
   if (threadIdx.x == 0) dg[blockIdx.x] = (float)((part[0] + part[1]) + (part[2] + part[3]));
 }
+
+#endif
 
 // A gradient of all heads, fp32 [batch][steps][heads][dim], added up over those that share one.
 template <class T>

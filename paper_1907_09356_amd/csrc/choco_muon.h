@@ -227,7 +227,6 @@ __device__ __forceinline__ float4_t whole_product(const f16_t* left, int64_t lef
                                                   int m0, int n0, int inner, int l, int g) {
   float4_t acc[3] = {};       // (apart, so that the instructions of a step do not wait for each other)
   const f16_t *pl = left + (m0 + l) * left_ld + 8 * g, *pr = right + (n0 + l) * right_ld + 8 * g;
-#pragma unroll 2
   for (int k = 0; k < inner; k += 32) {
     const half8 lh = *(const half8*)(pl + k), ll = *(const half8*)(pl + left_low + k);
     const half8 rh = *(const half8*)(pr + k), rl = *(const half8*)(pr + right_low + k);
