@@ -133,7 +133,7 @@ def test_lengths_and_types(N, dtype):
 
 @pytest.mark.parametrize("dk, dv", [(1, 1), (1, 64), (16, 1), (7, 5), (33, 65), (50, 50), (64, 64), (64, 130), (65, 64), (128, 96), (129, 31), (200, 256),
                                     (256, 256)])
-@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
 def test_sizes_of_heads(dk, dv, dtype):
     check_all(*make(2, 150, 2, dk, dv, dtype, seed=dk + dv, ragged=True))
 
