@@ -60,7 +60,6 @@ struct MuonArgs {
   bool last;
 };
 
-__device__ __forceinline__ int64_t plane(int64_t rows, int64_t ld) { return rows * ld; }
 // The operands of a matrix, high planes with the low ones behind them.
 struct MuonPlanes {
   f16_t *x, *xt[2], *p, *q;
