@@ -45,6 +45,10 @@ bool whole(int64_t rows, int64_t cols) {
   return whole_bytes(a, b) <= kWholeBytes && ra * rb <= 256 * kWholeTiles * kWholeWaves;
 }
 
+// Threads of a workgroup, of matrices taken whole and of the others.
+constexpr int kTileThreads = 256;
+int threads_of(bool whole) { return whole ? 64 * kWholeWaves : kTileThreads; }
+
 // A shape's sides, operands and tiles (null: taken whole); `count` and what is behind the begins are the caller's.
 MuonShape shape_from(int64_t rows, int64_t cols, const Tiles* tiles) {
   MuonShape S{};
@@ -82,15 +86,15 @@ struct Round {
 
 template <int KIND>
 void launch_product(const MuonArgs& A, uint32_t tiles, int side, hipStream_t stream) {
-  if (side == 128) k_muon_product<KIND, 128><<<dim3(tiles), 256, 0, stream>>>(A);
-  else k_muon_product<KIND, 64><<<dim3(tiles), 256, 0, stream>>>(A);
+  if (side == 128) k_muon_product<KIND, 128><<<dim3(tiles), kTileThreads, 0, stream>>>(A);
+  else k_muon_product<KIND, 64><<<dim3(tiles), kTileThreads, 0, stream>>>(A);
 }
 
 template <class T, bool STEP>
 int run_tiles(MuonArgs A, const Round& R, int iterations, const Tiles& tiles, hipStream_t stream) {
-  k_muon_squares<T, STEP><<<dim3(R.start_tiles), 256, 0, stream>>>(A);
+  k_muon_squares<T, STEP><<<dim3(R.start_tiles), kTileThreads, 0, stream>>>(A);
   TRY_HIP(hipGetLastError());
-  k_muon_start<T, STEP><<<dim3(R.start_tiles), 256, 0, stream>>>(A);
+  k_muon_start<T, STEP><<<dim3(R.start_tiles), kTileThreads, 0, stream>>>(A);
   TRY_HIP(hipGetLastError());
   for (int i = 0; i < iterations; ++i) {
     A.now = i & 1;
@@ -149,9 +153,10 @@ int stack_layout(const choco_orthogonalize_config& c, StackLayout& L) {
   L.tiles.choose();
   L.shape = shape_from(c.rows, c.cols, L.whole ? nullptr : &L.tiles);
   const double most = std::max<double>(L.shape.start_tiles, std::max(L.shape.gram_tiles, L.shape.apply_tiles));
-  if (!launch_fits(most, 256)) return CHOCO_E_UNSUPPORTED;
+  const int threads = threads_of(L.whole);
+  if (!launch_fits(most, threads)) return CHOCO_E_UNSUPPORTED;
   L.each = L.whole ? c.batch : std::min<int64_t>(c.batch, std::max<int64_t>(1, kRoundBytes / L.shape.scratch_of));
-  while (L.each > 1 && !launch_fits(most * (double)L.each, 512)) L.each /= 2;
+  while (L.each > 1 && !launch_fits(most * (double)L.each, threads)) L.each /= 2;
   const int64_t times = (c.batch + L.each - 1) / L.each;      // of like sizes
   L.each = (c.batch + times - 1) / times;
   Parts parts;
@@ -228,12 +233,12 @@ int muon_layout(const choco_muon_config& c, std::vector<MuonShape>& table, std::
     S.decay = c.weight_decay_host ? c.weight_decay_host[t] : 0.0f;
     S.rate = c.lr_scale_host ? c.lr_scale_host[t] : std::sqrt(std::max(1.0f, (float)rows / (float)cols));
     const double tiles = std::max<double>(S.start_tiles, std::max(S.gram_tiles, S.apply_tiles));
-    if (!launch_fits(tiles, 512)) return CHOCO_E_UNSUPPORTED;
+    if (!launch_fits(tiles, threads_of(alone))) return CHOCO_E_UNSUPPORTED;
     if (alone) now.lds = std::max(now.lds, whole_bytes(S.a, S.b));
     for (int32_t w = 0; w < c.n;) {
       const double taken = std::max<double>(now.start_tiles, std::max(now.gram_tiles, now.apply_tiles));
       int64_t count = alone ? c.n - w : std::min<int64_t>(c.n - w, (most - scratch) / S.scratch_of);
-      while (count > 0 && !launch_fits(taken + tiles * (double)count, 512)) count /= 2;
+      while (count > 0 && !launch_fits(taken + tiles * (double)count, threads_of(alone))) count /= 2;
       if (count < 1) {
         if (now.count > 0) {
           close();

@@ -97,6 +97,7 @@ int hipMemcpy2DAsync(void* d, size_t dp, const void* s, size_t sp, size_t w, siz
 }
 int hipMemsetAsync(void* d, int v, size_t n, void*) { return std::memset(d, v, n), 0; }
 int hipGetSymbolAddress(void** p, const void*) { return *p = symbol, 0; }
+int hipFuncSetAttribute(const void*, int, int) { return 0; }
 int hipGetDevice(int* d) { return *d = 0, 0; }
 int hipStreamCreateWithFlags(void** s, unsigned) { return *s = &handle, 0; }
 int hipStreamDestroy(void*) { return 0; }

@@ -1,0 +1,53 @@
+"""The launches of linear attention and of orthogonalised matrices, over a stand-in for the HIP runtime, without a GPU."""
+import pytest
+
+from tests.launches import recorded
+
+HEAD = """
+import ctypes
+from paper_1907_09356_amd import train as T
+P = 0x10000
+def launches(code):
+    assert code == B.OK, code
+    rows = [line.split() for line in stub.stub_launches().decode().splitlines()]
+    return [[name] + [[int(x) for x in dims.split("x")] for dims in (grid, block)] + [int(lds)] for name, grid, block, lds in rows]
+"""
+
+
+def run(code):
+    return recorded(HEAD + code)
+
+
+def fits(launch):
+    return launch[1][0] * launch[2][0] < 2 ** 32
+
+
+# ---- orthogonalised matrices ----
+@pytest.mark.parametrize("batch", [4_194_303, 4_194_304, 5_000_001, 16_777_215, 40_000_000])
+def test_stacks_of_small_matrices_are_divided_where_a_launch_ends(batch):
+    # a workgroup of 1024 threads takes a matrix, and a grid holds less than 2^32 threads
+    out = run("""
+c = T.OrthogonalizeConfig(batch=%d, rows=8, cols=8, type=T.F32, iterations=5, x_stride=(ctypes.c_int64 * 2)(64, 8), y_stride=(ctypes.c_int64 * 2)(64, 8))
+out = launches(T.lib().choco_orthogonalize(ctypes.byref(c), P, P, None, 0))
+""" % batch)
+    assert all(name == "k_muon_whole<float,false>" and block == [1024, 1, 1] for name, _, block, _ in out)
+    assert all(fits(launch) for launch in out)
+    assert sum(grid[0] for _, grid, _, _ in out) == batch
+    assert len(out) == 1 or len(out) <= 2 * -(-batch // (2 ** 22 - 1))
+
+
+def test_rounds_of_many_small_matrices_are_divided_where_a_launch_ends():
+    n, count = 65535, 70
+    out = run("""
+import numpy as np
+n, count = %d, %d
+cfg, keep = T.make_muon_config(n, 2 * count, 2 * count, (np.arange(count) * 2, [1] * count, [2] * count))
+need, a = ctypes.c_size_t(), ctypes.c_void_p()
+assert T.lib().choco_muon_workspace_bytes(ctypes.byref(cfg), ctypes.byref(need)) == B.OK
+ws = np.zeros(need.value + 256, dtype=np.uint8)
+base = (ws.ctypes.data + 255) // 256 * 256
+assert T.lib().choco_muon_init(ctypes.byref(cfg), P, base, need.value, ctypes.byref(a)) == B.OK
+out = launches(T.lib().choco_muon_step(a, P, T.F32, 0.1, None))
+""" % (n, count))
+    assert all(fits(launch) for launch in out)
+    assert sum(grid[0] for _, grid, _, _ in out) == n * count
