@@ -64,8 +64,8 @@ __device__ __forceinline__ void store_result(const LinearPass& P, int64_t at, fl
 }
 
 // ---- step by step ----
-// A workgroup takes a slice of columns and holds the state in registers, V columns of every 4 V-th row a lane (V as the state in memory is
-// aligned).  Bound by the state, in and out once: for a step of D x D, 8 D^2 bytes against 5 D^2 operations.  One token of 64 x 16 heads of 128
+// A workgroup takes a slice of columns and holds the state in registers, V columns of every 4 V-th row a lane (V as the state's rows divide;
+// one that lies on no border of V is read and written by entries, with the same sums).  Bound by the state, in and out once: for a step of D x D, 8 D^2 bytes against 5 D^2 operations.  One token of 64 x 16 heads of 128
 // in bf16 26 us, 5.1 TB/s (a column a lane, a quarter of the rows a wave: 33), of 160 x 13 of 50 in fp32 15, 2.8 TB/s (20).
 constexpr int kLinearStage = 8;     // steps whose a and b are in LDS at a time
 
@@ -86,24 +86,40 @@ __global__ __launch_bounds__(256) void k_linear_steps(LinearArgs A, LinearPass P
   const int64_t out = b * P.out_seq + h * P.out_head + slice * kLinearSlice;
   float s[R][V];
 #pragma unroll
-  for (int r = 0; r < R; ++r) {
-    const int i = row + r * kRows;
+  for (int r = 0; r < R; ++r)
 #pragma unroll
     for (int v = 0; v < V; ++v) s[r][v] = 0.0f;
-    if (P.first && in && i < P.da) {
-      const float* p = P.first + bh * P.first_of * state + (int64_t)i * P.state_a + (int64_t)col * P.state_c;
-      if (V > 1) load_floats<float, V>(p, s[r]);
-      else s[r][0] = *p;
+  const auto on_border = [](const float* p) { return V == 1 || ((uintptr_t)p & (4 * V - 1)) == 0; };
+  if (P.first) {
+    const float* p = P.first + bh * P.first_of * state + (int64_t)row * P.state_a + (int64_t)col * P.state_c;
+    if (on_border(P.first)) {
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+        if (in && row + r * kRows < P.da) load_floats<float, V>(p + (int64_t)r * kRows * P.state_a, s[r]);
+    } else {
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+          if (in && row + r * kRows < P.da) s[r][v] = p[(int64_t)r * kRows * P.state_a + v];
     }
   }
   const auto keep = [&](float* to, float w) {
+    float* p = to + (int64_t)row * P.state_a + (int64_t)col * P.state_c;
+    if (on_border(to)) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const int i = row + r * kRows;
-      float x[V];
+      for (int r = 0; r < R; ++r) {
+        float x[V];
 #pragma unroll
-      for (int v = 0; v < V; ++v) x[v] = s[r][v] * w;
-      if (in && i < P.da) store_floats<float, V>(to + (int64_t)i * P.state_a + (int64_t)col * P.state_c, x);
+        for (int v = 0; v < V; ++v) x[v] = s[r][v] * w;
+        if (in && row + r * kRows < P.da) store_floats<float, V>(p + (int64_t)r * kRows * P.state_a, x);
+      }
+    } else {
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+          if (in && row + r * kRows < P.da) p[(int64_t)r * kRows * P.state_a + v] = s[r][v] * w;
     }
   };
   for (int64_t i0 = 0; i0 < len; i0 += kLinearStage) {

@@ -155,9 +155,8 @@ int run_steps(const choco_linear_config& c, const LinearArgs& A, const LinearPas
     else if (P.da <= 128) launch(v, std::integral_constant<int, 128>{});
     else launch(v, std::integral_constant<int, 256>{});
   };
-  const auto wide = [&](int v) {      // columns of a state next to one another, on the border of as many
-    return P.state_c == 1 && P.dc % v == 0 && aligned_to(P.first, 4 * v) && aligned_to(P.last, 4 * v) && aligned_to(P.kept, 4 * v);
-  };
+  // columns of a state next to one another: by sizes alone, as it sets the order of sums (the kernel looks at the addresses)
+  const auto wide = [&](int v) { return P.state_c == 1 && P.dc % v == 0; };
   if (wide(4)) with_dim(std::integral_constant<int, 4>{});
   else if (wide(2)) with_dim(std::integral_constant<int, 2>{});
   else with_dim(std::integral_constant<int, 1>{});

@@ -325,6 +325,25 @@ def test_same_inputs_same_bits():
             assert all(torch.equal(a, b) for a, b in zip(runs[0], run))
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("N", [1, 3, 8, 70])
+def test_same_bits_wherever_the_states_lie(dtype, N):
+    def moved(x, by):      # the same numbers, so many entries behind a border of 256 bytes
+        wide = torch.empty(x.numel() + by, device="cuda")
+        wide[by:] = x.flatten()
+        return wide[by:].view(x.shape)
+
+    for dk, dv in ((16, 24), (50, 50), (7, 64), (130, 2), (8, 1)):
+        q, k, v, g, h0, _, dy, dlast = make(3, N, 2, dk, dv, dtype, seed=N)
+        runs = []
+        for a, b, c in ((0, 0, 0), (1, 0, 0), (0, 1, 0), (0, 0, 1), (2, 2, 2), (3, 1, 2)):
+            last = moved(torch.zeros_like(h0), b)
+            y, _, saved = T.linear_attention(q, k, v, g, h0=moved(h0, a), save=True, h_last=last)
+            runs.append((y, last, saved) + T.linear_attention_grad(q, k, v, g, moved(saved, b), dy, dlast=moved(dlast, c)))
+        for run in runs[1:]:
+            assert all(torch.equal(x, y) for x, y in zip(runs[0], run)), (dk, dv)
+
+
 def test_gradients_by_differences():
     # the loss is a sum of some thousand products of order one, differences over 2^-6 are good to 2^-24 x 1e3 x 2^6 of it
     q, k, v, g, h0, lengths, dy, dlast = make(2, 70, 2, 12, 12, F32, ragged=True)

@@ -22,6 +22,36 @@ def fits(launch):
     return launch[1][0] * launch[2][0] < 2 ** 32
 
 
+# ---- linear attention ----
+LINEAR = """
+def strides(steps, heads, dim):
+    return (ctypes.c_int64 * 3)(steps * heads * dim, heads * dim, dim)
+def linear(batch, steps, heads, dk, dv, kind, gate=1, q_heads=None, k_heads=None, v_heads=None):
+    hq, hk, hv = q_heads or heads, k_heads or heads, v_heads or heads
+    s = dict(q=(hq, dk), k=(hk, dk), v=(hv, dv), y=(heads, dv), g=(heads, 1), dq=(hq, dk), dk=(hk, dk), dv=(hv, dv))
+    return T.LinearConfig(batch=batch, steps=steps, heads=heads, q_heads=hq, k_heads=hk, v_heads=hv, dim_k=dk, dim_v=dv, type=kind,
+                          gate_steps=gate, **{name + "_stride": strides(steps, *v) for name, v in s.items()})
+def forward(c, h0=P, last=P, saved=P):
+    stub.stub_clear()
+    return launches(T.lib().choco_linear_forward(ctypes.byref(c), P, P, P, P, h0, None, P, last, saved, P, 1 << 50))
+def backward(c, saved=P, dlast=P, dg=P, dh0=P):
+    stub.stub_clear()
+    return launches(T.lib().choco_linear_backward(ctypes.byref(c), P, P, P, P, None, saved, P, dlast, P, P, P, dg, dh0, P, 1 << 50))
+"""
+
+
+@pytest.mark.parametrize("dk, dv", [(16, 24), (50, 50), (33, 7), (8, 1), (1, 8)])
+@pytest.mark.parametrize("steps", [1, 3, 100])
+def test_what_is_launched_depends_on_sizes_and_not_on_the_states_addresses(dk, dv, steps):
+    # lanes' columns set the order of sums, so they may not follow from where a state lies
+    out = run(LINEAR + """
+c = linear(2, %d, 3, %d, %d, T.F32)
+out = [[forward(c, P + a, P + b, P + e), backward(c, P + a, P + b, dh0=P + e)] for a, b, e in ((0, 0, 0), (4, 0, 0), (0, 4, 0), (0, 0, 4), (8, 8, 8))]
+""" % (steps, dk, dv))
+    for other in out[1:]:
+        assert other == out[0]
+
+
 # ---- orthogonalised matrices ----
 @pytest.mark.parametrize("batch", [4_194_303, 4_194_304, 5_000_001, 16_777_215, 40_000_000])
 def test_stacks_of_small_matrices_are_divided_where_a_launch_ends(batch):
