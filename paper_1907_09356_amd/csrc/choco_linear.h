@@ -35,7 +35,11 @@ struct LinearPass {
   float* last;              // state after its last step, backwards decayed by the first step's w: of S_0
   float* kept;              // forwards: states before every kLinearSave-th step and the last one, `kept_of` of each sequence and head
   int64_t kept_of, first_of;
+  // What a pass in chunks adds to the gates' gradient, or null:
   float* dots;              // [slices][batch * heads][steps]
+  const float* met;         // dq: states that the backwards passes have before their pieces; dk: what the forward pass kept
+  const float* met_last;    // dq: the gradient of the last states, or null
+  int64_t met_of;           // states of `met` from one head to the next
   bool back, wide;          // wide: out is fp32 whatever the inputs' type
 };
 
@@ -159,11 +163,6 @@ __global__ __launch_bounds__(256) void k_linear_steps(LinearArgs A, LinearPass P
 #pragma unroll
         for (int r = 0; r < kRows; ++r) y += part[i & 1][r][threadIdx.x];
         if (mine < P.dc) store_result<T>(P, out + t * P.out_step + threadIdx.x, y);
-        if (P.dots) {
-          float d = mine < P.dc ? y * to_float(((const T*)P.x)[b * P.x_seq + t * P.x_step + (h / P.x_share) * P.x_head + mine]) : 0.0f;
-          for (int o = 32; o; o >>= 1) d += __shfl_xor(d, o);
-          if (threadIdx.x == 0) P.dots[((int64_t)slice * A.batch * A.heads + bh) * A.steps + t] = d;
-        }
       }
     }
   }
@@ -197,6 +196,52 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+template <int CONTROL>
+__device__ __forceinline__ float moved_in_row(float x) {      // of 16 lanes; zero from beyond
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(x), CONTROL, 15, 15, false));
+}
+// Of 16 neighbouring lanes: sums from each on; the sum of all, everywhere.
+__device__ __forceinline__ float row_sums_from(float x) {
+  x += moved_in_row<0x101>(x);
+  x += moved_in_row<0x102>(x);
+  x += moved_in_row<0x104>(x);
+  return x + moved_in_row<0x108>(x);
+}
+__device__ __forceinline__ float row_sum(float x) {
+  x += moved_in_row<0x128>(x);
+  x += moved_in_row<0x124>(x);
+  x += moved_in_row<0x122>(x);
+  return x + moved_in_row<0x121>(x);
+}
+
+// The four rows of 16 lanes added up, in all of them; of numbers that are a row's own, the sum of the rows before.
+__device__ __forceinline__ float rows_summed(float x) {
+  const auto two = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(two[0]) + __uint_as_float(two[1]);
+  const auto four = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(four[0]) + __uint_as_float(four[1]);
+}
+template <int CONTROL, int ROWS>
+__device__ __forceinline__ float last_lane_of(float x) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(x), CONTROL, ROWS, 15, false));
+}
+__device__ __forceinline__ float rows_before(float x) {
+  x = last_lane_of<0x142, 14>(x);      // each row's, one row on; then the first's to the second's, the third's to the fourth's, the first half's
+  x += last_lane_of<0x142, 10>(x);
+  return x + last_lane_of<0x143, 12>(x);
+}
+// Sums over the lanes from each on, without its own where `own` is false.
+__device__ __forceinline__ float sums_from(float x, bool own, int row) {
+  x = row_sums_from(x);
+  float behind = 0.0f;
+#pragma unroll
+  for (int k = 3; k > 0; --k) {
+    const float sum = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), 16 * k));
+    behind += row < k ? sum : 0.0f;
+  }
+  return behind + (own ? x : moved_in_row<0x101>(x));
+}
 
 template <class Core>
 struct Operand;
@@ -323,13 +368,15 @@ struct ChunkShared {
   static constexpr int kPad = 16 / sizeof(Core), kSlice = 16 * WAVES;
   static constexpr bool kTurned = sizeof(Core) == 2;      // b by columns as well
   static constexpr int kTurnedRow = kChunk + 4, kScoreRow = kChunk + 4;
-  // (P, in 16 bits three pieces of it, lies over a, in 16 bits also over b, and what is missing)
-  static constexpr int kScores = 3 * kChunk * kScoreRow, kRows = 2 * kChunk * (DA + kPad);
+  // (P, in 16 bits three pieces of it, or two and x, lies over a, in 16 bits also over b, and what is missing)
+  static constexpr int kTwo = 2 * kChunk * kScoreRow, kScores = kTwo + kChunk * (kScoreRow > kSlice + kPad ? kScoreRow : kSlice + kPad), kRows = 2 * kChunk * (DA + kPad);
   Core a[kChunk][DA + kPad], b[kChunk][DA + kPad];
   Core more[kTurned && kScores > kRows ? kScores - kRows : 1];
   alignas(16) Core c[kChunk][kSlice + kPad];
   alignas(16) Core turned[kTurned ? DA : 1][kTurned ? kTurnedRow : 1];
   alignas(16) float c_high[kChunk], c_low[kChunk], to_end[kChunk], dots[WAVES][kChunk], most[WAVES];
+  alignas(16) float behind[10][16], before[10][16];      // sums over pairs of steps, of ten tiles
+  float met[WAVES], ahead[WAVES], weights[kChunk], ahead_all;
 };
 
 // How rows are read: parts of 16 bytes or words of 4 by offsets of 32 bits, where what is not there has one outside the buffer and comes
@@ -559,12 +606,12 @@ __device__ __forceinline__ double sums_to(double x) {
   return x;
 }
 
-// What a launch is for: the segments' own contributions to the state and their logarithms' sums; the result; the result and its
-// products with x.
-enum { kStates = 0, kResult = 1, kResultAndDots = 2 };
+// What a launch is for: the segments' own contributions to the state and their logarithms' sums; the result; dq or dk, and dv, with their parts of the
+// gates' gradient (dq and dk also without).
+enum { kStates = 0, kResult = 1, kOfStates = 2, kOfPairs = 3 };
 // numbers of 16 bits that stand for one of fp32 (one float otherwise)
 template <class Core, int MODE>
-constexpr int kPieces = std::is_same_v<Core, float> ? 1 : std::is_same_v<Core, f16_t> || MODE == kResult ? 2 : 3;
+constexpr int kPieces = std::is_same_v<Core, float> ? 1 : std::is_same_v<Core, f16_t> || MODE == kResult || MODE == kOfPairs ? 2 : 3;
 // Waves of a SIMD: those of two workgroups where a compute unit's LDS holds two.
 template <class Core, int DA, int WAVES>
 constexpr int kChunkWaves = WAVES == 8 ? (sizeof(ChunkShared<Core, DA, WAVES>) * 2 > 163840 ? 2 : 4) : sizeof(ChunkShared<Core, DA, WAVES>) * 2 > 163840 ? 1 : 2;
@@ -572,7 +619,7 @@ constexpr int kChunkWaves = WAVES == 8 ? (sizeof(ChunkShared<Core, DA, WAVES>) *
 template <class In, class Core, int DA, int WAVES, int MODE, int WAY>
 __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_linear_chunks(LinearArgs A, LinearPass P, LinearChunks C) {
   typedef ChunkShared<Core, DA, WAVES> Shared;
-  constexpr bool STATE = MODE == kStates;
+  constexpr bool STATE = MODE == kStates, DOTS = MODE == kOfStates, PAIRS = MODE == kOfPairs, X_IN_LDS = sizeof(Core) == 2;
   constexpr bool RANGED = std::is_same_v<Core, f16_t>;
   constexpr int N_OUT = kPieces<Core, MODE>, N_STATE = kPieces<Core, kStates>, kSlice = Shared::kSlice;
   typedef Operand<Core> Op;
@@ -626,6 +673,28 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
   };
   double total = 0.0;
 
+  // The state's products with one of the other direction, <E, S>: the sum over a wave's columns.
+  const auto meet = [&](const float* other, int thread) -> float {
+    const int l = thread & 15, row = (thread & 63) >> 4 << 2;
+    const float* p = other + (int64_t)(col + l) * P.state_c + (int64_t)row * P.state_a;
+    const bool together = P.state_a == 1 && P.da % 4 == 0 && ((uintptr_t)other & 15) == 0, in = col + l < P.dc;
+    float sum = 0.0f;
+#pragma unroll
+    for (int j = 0; j < kJ * kT; ++j) {
+      f32x4 x = {};
+      if (together) {
+        if (in && row + 16 * j < P.da) x = *(const f32x4*)(p + 16 * j);
+      } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (in && row + 16 * j + r < P.da) x[r] = p[(16 * j + r) * P.state_a];
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sum = fmaf(x[r], state[j][r], sum);
+    }
+    return rows_summed(row_sum(sum));
+  };
+
   const int64_t inside = min(end, len);       // steps of the segment that are in the sequence end here
   const int chunks = inside > begin ? (int)((inside - begin + kChunk - 1) / kChunk) : 0;
   Staged<In, Core, DA, 1, WAVES, WAY> next_a;
@@ -645,6 +714,34 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
       next_g = lane >= lo && lane < hi && t < len ? log_gate(A, b, t, h) : 0.0f;
     }
   };
+  // P^T by tiles of 16 x 16: rows s, columns t, s <= t, and two of zeros that complete an operand of two tiles.  A wave's are the
+  // pairs t, s in a word, three of them or two.
+  constexpr int kTiles = WAVES == 4 ? 3 : 2;
+  constexpr uint32_t kOfWaves[8] = {WAVES == 4 ? 0x300010u : 0x0010u, WAVES == 4 ? 0x311101u : 0x1101u, WAVES == 4 ? 0x322021u : 0x20FFu,
+                                    WAVES == 4 ? 0x332223u : 0x21FFu, 0x2223u, 0x3031u, 0x32FFu, 0x33FFu};
+  uint32_t tiles = kOfWaves[0];
+#pragma unroll
+  for (int w = 1; w < WAVES; ++w)
+    if (wave == w) tiles = kOfWaves[w];
+  // What a chunk's pairs put on its steps, those on either side of each, by one wave (backwards: a step's begin is its row's end).
+  const auto gather = [&](int i) {
+    const int64_t t0 = begin_of(i);
+    const int row = kChunk - 1 - lane, m = (row + 1) >> 4, e = (row + 1) & 15;
+    if (t0 + lane >= inside) return;
+    float sum = 0.0f;
+    if (m < 4) {
+      sum = S.behind[m * (m + 1) / 2 + m][e];
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int s = 0; s < t; ++s) {
+          if (t == m) sum += S.behind[t * (t + 1) / 2 + s][e];
+          if (s == m) sum += S.before[t * (t + 1) / 2 + s][e];
+          if (s < m && m < t) sum += S.behind[t * (t + 1) / 2 + s][0];
+        }
+    }
+    P.dots[((int64_t)slice * A.batch * A.heads + bh) * A.steps + t0 + lane] = sum;
+  };
   if (chunks > 0) ask(0, threadIdx.x);
   for (int i = 0; i < chunks; ++i) {
     // (threads' places are worked out anew for every chunk: kept over them, they would take more registers than there are)
@@ -656,10 +753,28 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
     const int there = (int)min((int64_t)kChunk, inside - t0), lo = P.back ? kChunk - there : 0, hi = P.back ? kChunk : there;
     if (!STATE && P.kept && t0 % kLinearSave == 0) keep(P.kept + (bh * P.kept_of + t0 / kLinearSave) * entries, 1.0f);
     __syncthreads();
+    if (PAIRS && i > 0 && wave == WAVES - 1) gather(i - 1);
     if (!STATE) next_a.store(thread, S.a);
     if constexpr (Shared::kTurned) next_b.store_turned(thread, S.turned);
     if (!STATE || !Shared::kTurned) next_b.store(thread, S.b);
     next_c.store(thread, S.c);
+    const bool busy = 16 * wave < in_slice;      // (the others help with P only)
+    // What goes through a whole chunk to the gates' gradient is <E, S> of its two ends.  In memory there are S at the begins and E at the ends of
+    // pieces of four chunks: dk's pass, which has E, does the first two, dq's, which has S, the last two.  Of these each does one with the
+    // next chunk "ahead": E reaches the piece's begin, or S its end, by way of that chunk's rows.
+    const int in_piece = (int)(t0 / kChunk) % (kLinearSave / kChunk);
+    const bool meets = DOTS && P.dots && (P.back ? in_piece < 2 : in_piece >= 2), ahead = meets && in_piece == (P.back ? 1 : 2) && i + 1 < chunks;
+    // the step whose logarithm the chunks' sums lack
+    const int64_t past = P.back ? t0 - (ahead ? kChunk : 0) : t0 + (ahead ? 2 : 1) * kChunk;
+    const float past_gate = meets && past < len ? log_gate(A, b, past, h) : 0.0f;
+    if constexpr (DOTS) {
+      if (meets && busy) {
+        const int64_t piece = t0 / kLinearSave;
+        const bool within = P.back || (piece + 1) * kLinearSave < len;
+        const float* other = within ? P.met + (bh * P.met_of + piece) * entries : P.met_last ? P.met_last + bh * entries : nullptr;
+        S.met[wave] = other ? meet(other, thread) : 0.0f;
+      }
+    }
     if (wave == 0) {      // the logarithms' sums
       const double x = sums_to(next_g < kLinearLeast ? (double)kLog2Least : (double)next_g * 1.4426950408889634);
       const double all = __shfl(x, 63);
@@ -670,8 +785,26 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
     }
     const int first = col + 4 * g;
     if (i + 1 < chunks) ask(i + 1, thread);
+    // four entries of a row of x from column `at` on, of which `width` are there
+    const auto entries_of_x = [&](int64_t t0, int lo, int hi, int row, int at, int width) {
+      Four<In> x;
+      const int when = P.back ? kChunk - 1 - row : row;
+      const bool here = row >= lo && row < hi;
+      if constexpr (WAY != kEntries) {
+        const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc((void*)(px + t0 * P.x_step), 0, kBufferBytes, 0x00027000);
+        x.load(from, here ? ((uint32_t)when * (uint32_t)P.x_step + (uint32_t)at) * (uint32_t)sizeof(In) : ~0u, width, C.vec_x == 4);
+      } else {
+        x.load(px + (t0 + when) * P.x_step + at, here ? width : 0);
+      }
+      return x;
+    };
+    constexpr int kXWide = X_IN_LDS || kSlice < DA ? kSlice : DA, kXParts = kSlice / kXWide;
+    Staged<In, Core, kXWide, 1, WAVES, WAY> now_x[kXParts];
+    if constexpr (PAIRS)
+#pragma unroll
+      for (int k = 0; k < kXParts; ++k)
+        now_x[k].load(thread, px + slice * kSlice + k * kXWide + t0 * P.x_step, P.x_step, P.back, in_slice - k * kXWide, lo, hi);
     __syncthreads();
-    const bool busy = 16 * wave < in_slice;      // (the others help with P only)
     Frag cf[kS];       // column l's entries, a lane's steps
     const auto columns = [&](Frag (&cf)[kS]) {
 #pragma unroll
@@ -684,7 +817,8 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
     if constexpr (!STATE) {
       // what comes of the state before the chunk
       f32x4 y[4] = {};
-      if (busy) {
+      // y += S^T a of the rows in LDS, in fp16 times a power of two that is taken back by the result
+      const auto by_state = [&](f32x4 (&y)[4]) -> float {
         float most = 0.0f;
         if constexpr (RANGED)
           most = largest_of_wave([&](auto&& see) {
@@ -710,23 +844,70 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
             for (int n = N_OUT - 1; n >= 0; --n) y[t] = Op::mma(p[n], q, y[t]);
           }
         }
+        return RANGED ? range.down : 1.0f;
+      };
+      const auto products_with = [&](const f32x4& y, const Four<In>& x) {      // of a row of the wave's columns (what is not there is zero)
+        float d = 0.0f;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) d = fmaf(y[r], x[r], d);
+        return rows_summed(d);
+      };
+      const auto from_state = [&] {
+        if (!busy) return;
+        Four<In> times[4];
+        if constexpr (DOTS)
+          if (P.dots)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) times[t] = entries_of_x(t0, lo, hi, 16 * t + l, first, P.dc - first);
+        const float down = by_state(y);
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           const float here = __builtin_amdgcn_exp2f(S.c_high[16 * t + l] + S.c_low[16 * t + l]);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) y[t][r] *= RANGED ? here * range.down : here;
+          for (int r = 0; r < 4; ++r) y[t][r] *= RANGED ? here * down : here;
+          if constexpr (DOTS)
+            if (P.dots) {
+              const float d = products_with(y[t], times[t]);
+              if (g == 0) S.dots[wave][16 * t + l] = d;
+            }
         }
-      }
-      // P^T by tiles of 16 x 16: rows s, columns t, s <= t, and two of zeros that complete an operand of two tiles.  A wave's are the
-      // pairs t, s in a word, three of them or two.
-      constexpr int kTiles = WAVES == 4 ? 3 : 2;
-      constexpr uint32_t kOfWaves[8] = {WAVES == 4 ? 0x300010u : 0x0010u, WAVES == 4 ? 0x311101u : 0x1101u, WAVES == 4 ? 0x322021u : 0x20FFu,
-                                        WAVES == 4 ? 0x332223u : 0x21FFu, 0x2223u, 0x3031u, 0x32FFu, 0x33FFu};
-      uint32_t tiles = kOfWaves[0];
-#pragma unroll
-      for (int w = 1; w < WAVES; ++w)
-        if (wave == w) tiles = kOfWaves[w];
+      };
+      from_state();
       f32x4 score[kTiles];
+      // x by rows: in 16 bits behind P's two pieces, in fp32 over P once that has been used, as many columns as there is room for
+      typedef Core XRows[kChunk][kXWide + Shared::kPad];
+      XRows& x_rows = *reinterpret_cast<XRows*>(&S.a[0][0] + (X_IN_LDS ? Shared::kTwo : 0));
+      const auto add_products_of_x = [&](f32x4& sum, int s, int t, int from) {      // of rows s of c with rows t of x
+#pragma unroll
+        for (int j = 0; j < kXWide / Op::kInner; ++j)
+          sum = Op::mma(Op::load(&S.c[16 * s + l][from], j, g), Op::load(&x_rows[16 * t + l][0], j, g), sum);
+      };
+      // Pairs of a row of tile s (4 g + r of its tile) and one of tile t (column l).  Their sums over those on either side of a row's begin: in one tile
+      // by row, of two tiles over t's rows from one on and over s's before it.
+      const auto sums_of_pairs = [&](const f32x4& pairs, int t, int s) {
+        const int tile = t * (t + 1) / 2 + s;
+        float behind = 0.0f;
+        if (s == t) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float from = row_sums_from(pairs[r]);
+            behind += 4 * g + r < l ? from : 0.0f;
+          }
+        } else {
+          behind = row_sums_from((pairs[0] + pairs[1]) + (pairs[2] + pairs[3]));
+          f32x4 before;
+          float sum = 0.0f;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            before[r] = sum;
+            sum += row_sum(pairs[r]);
+          }
+          const float rows = rows_before(sum);
+          if (l == 0) *(f32x4*)&S.before[tile][4 * g] = before + rows;
+        }
+        behind = rows_summed(behind);
+        if (g == 0) S.behind[tile][l] = behind;
+      };
 #pragma unroll
       for (int n = 0; n < kTiles; ++n) {
         const int pair = tiles >> (8 * (kTiles - 1 - n)) & 255, t = pair >> 4, s = pair & 15;
@@ -775,22 +956,27 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
           for (int r = 0; r < 4; ++r) left[r] -= to_float((Core)left[r]);
         }
       }
-      Four<In> times[4];      // x
-      if constexpr (MODE == kResultAndDots) {
-        const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc((void*)(px + t0 * P.x_step), 0, kBufferBytes, 0x00027000);
+      if constexpr (PAIRS && X_IN_LDS) now_x[0].store(thread, x_rows);
+      __syncthreads();
+      const auto all_pairs = [&] {
+        f32x4 sum[kTiles] = {};
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const int row = 16 * t + l, when = P.back ? kChunk - 1 - row : row;
-          const bool here = row >= lo && row < hi;
-          if constexpr (WAY != kEntries) {
-            const uint32_t at = here ? ((uint32_t)when * (uint32_t)P.x_step + (uint32_t)first) * (uint32_t)sizeof(In) : ~0u;
-            times[t].load(from, at, P.dc - first, C.vec_x == 4);
-          } else {
-            times[t].load(px + (t0 + when) * P.x_step + first, here ? P.dc - first : 0);
+        for (int k = 0; k < kXParts; ++k) {
+          if (!X_IN_LDS) {
+            __syncthreads();
+            now_x[k].store(thread, x_rows);
+            __syncthreads();
+          }
+#pragma unroll
+          for (int n = 0; n < kTiles; ++n) {
+            const int pair = tiles >> (8 * (kTiles - 1 - n)) & 255, t = pair >> 4, s = pair & 15;
+            if (s > t || 16 * t >= hi || 16 * t + 15 < lo) continue;
+            add_products_of_x(sum[n], s, t, k * kXWide);
+            if (k + 1 == kXParts) sums_of_pairs(score[n] * sum[n], t, s);
           }
         }
-      }
-      __syncthreads();
+      };
+      if constexpr (PAIRS && X_IN_LDS) all_pairs();
       if (busy) {
         columns(cf);
         const uint32_t out_size = P.wide ? 4 : sizeof(In);
@@ -817,24 +1003,58 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
             for (int r = 0; r < 4; ++r)
               if (first + r < P.dc) store_result<In>(P, out + (t0 + when) * P.out_step + first + r, y[t][r]);
           }
-          if constexpr (MODE == kResultAndDots) {
-            float d = 0.0f;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) d = fmaf(y[t][r], times[t][r], d);      // (what is not there is zero)
-            d += __shfl_xor(d, 16);
-            d += __shfl_xor(d, 32);
-            if (g == 0) S.dots[wave][row] = d;
+        }
+      }
+      if constexpr (DOTS) {
+        if (ahead) {      // the next chunk's rows with this one's state
+          const int64_t t1 = begin_of(i + 1);
+          const int there = (int)min((int64_t)kChunk, inside - t1), lo = P.back ? kChunk - there : 0, hi = P.back ? kChunk : there;
+          __syncthreads();
+          next_a.store(thread, S.a);
+          if (wave == 0) {
+            const double x = sums_to(next_g < kLinearLeast ? (double)kLog2Least : (double)next_g * 1.4426950408889634);
+            S.weights[lane] = __builtin_amdgcn_exp2f((float)x);
+            if (lane == 63) S.ahead_all = (float)x;
           }
+          __syncthreads();
+          if (busy) {
+            f32x4 z[4] = {};
+            const float down = by_state(z);
+            Four<In> times[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) times[t] = entries_of_x(t1, lo, hi, 16 * t + l, first, P.dc - first);
+            float sum = 0.0f;
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+              const int row = 16 * t + l;
+              const float d = products_with(z[t], times[t]);
+              sum += row >= lo && row < hi ? d * (RANGED ? down * S.weights[row] : S.weights[row]) : 0.0f;
+            }
+            S.ahead[wave] = row_sum(sum);
+            columns(cf);      // (anew: there are no registers to keep it)
+          }
+          __syncthreads();
+        }
+        if (P.dots && wave == WAVES - 1) {
+          // of a step: later steps of the chunk with what was before the chunk, or earlier ones with what comes behind it, and what goes
+          // through the whole chunk
+          const bool here = lane >= lo && lane < hi;
+          float d = 0.0f, met = 0.0f, beyond = 0.0f;
+          for (int w = 0; w < (in_slice + 15) / 16; ++w) {
+            d += S.dots[w][lane];
+            if (meets) met += S.met[w];
+            if (ahead) beyond += S.ahead[w];
+          }
+          d = sums_from(here ? d : 0.0f, !P.back, g);
+          if (meets) {
+            const float high = S.c_high[kChunk - 1], low = S.c_low[kChunk - 1], more = past_gate < kLinearLeast ? kLog2Least : past_gate * 1.44269504f;
+            met *= __builtin_amdgcn_exp2f(high + (low + (more + (ahead ? S.ahead_all : 0.0f))));
+            if (ahead) met = fmaf(beyond, __builtin_amdgcn_exp2f(high + low), met);
+          }
+          if (here) P.dots[((int64_t)slice * A.batch * A.heads + bh) * A.steps + first_time + dir * lane] = d + met;
         }
       }
-      if constexpr (MODE == kResultAndDots) {
-        __syncthreads();
-        if (wave == 0 && lane >= lo && lane < hi) {
-          float d = S.dots[0][lane];
-          for (int w = 1; w < (in_slice + 15) / 16; ++w) d += S.dots[w][lane];
-          P.dots[((int64_t)slice * A.batch * A.heads + bh) * A.steps + first_time + dir * lane] = d;
-        }
-      }
+      if constexpr (PAIRS && !X_IN_LDS) all_pairs();
       if (i + 1 == chunks && (C.states || !P.last) && !P.kept) break;      // nobody reads the state
     }
     if (!busy) continue;
@@ -913,6 +1133,10 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
     if (slice == 0 && threadIdx.x == 0) C.totals[bh * C.segments + segment] = total;
     return;
   }
+  if (PAIRS && chunks > 0) {
+    __syncthreads();
+    if (wave == WAVES - 1) gather(chunks - 1);
+  }
   // zeros behind the sequence
   const int64_t zero = max(begin, len);
   const int width = in_slice;
@@ -956,13 +1180,13 @@ __global__ __launch_bounds__(256) void k_linear_scan(LinearArgs A, float* states
 }
 
 // ---- the gates' gradient ----
-// dg_t = sum over s >= t of (q_s dq_s - k_s dk_s) up to any later step u, and what goes from before u past it, <E_u, S_u>: pieces of
-// kLinearSave steps, each with the states at its end, so that the differences' errors do not add up over a sequence.  Bound by these states:
-// 4 x 16,384 x 10 x 128 72 us, 4.7 TB/s.
+// dg_t = e^g_t <E_t, S_{t-1}> = the sum over pairs of steps s >= t > r of e^(c_s - c_r) (q_s k_r) (dy_s v_r), where r may also stand for the first state
+// and s for the last one's gradient: only what passes t is added up, so that a gate that hardly lets anything through has as many places right as
+// any other.  (By differences, sums of q dq - k dk, a gate of -10 beside open ones has two.)  In chunks, dv's pass has pairs
+// within a chunk, dq's and dk's those with what is before or behind it, by slices.
 struct LinearGates {
-  const float *q_dots, *k_dots, *saved, *later, *dlast;   // later: states that the backwards passes have before their pieces
-  int64_t saved_of, later_of;
-  int32_t q_slices, k_slices, state;
+  const float* dots;     // [slices of dq, dk and dv][batch * heads][steps]
+  int32_t slices;
   float* dg;       // [batch][steps][heads], or the pieces' sums [heads][batch * pieces]
   int64_t pieces;
   bool sums;
@@ -974,60 +1198,129 @@ __device__ __forceinline__ double wave_sum(double x) {
 }
 
 __global__ __launch_bounds__(kLinearSave) void k_linear_gates(LinearArgs A, LinearGates G) {
-  __shared__ double part[8];
-  const int64_t bh = blockIdx.x / G.pieces, piece = blockIdx.x % G.pieces, b = bh / A.heads;
+  __shared__ double part[4];
+  const int64_t bh = blockIdx.x / G.pieces, piece = blockIdx.x % G.pieces, b = bh / A.heads, t = piece * kLinearSave + threadIdx.x;
   const int h = (int)(bh % A.heads), wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int64_t len = steps_of(A, b), t = piece * kLinearSave + threadIdx.x, end = (piece + 1) * kLinearSave;
-  const bool in = t < len;
-  double x = 0.0;
-  if (in) {
-    const int64_t all = A.batch * A.heads;
-    for (int s = 0; s < G.q_slices; ++s) x += (double)G.q_dots[(s * all + bh) * A.steps + t];
-    for (int s = 0; s < G.k_slices; ++s) x -= (double)G.k_dots[(s * all + bh) * A.steps + t];
-  }
-  for (int o = 1; o < 64; o <<= 1) {      // from this step to the wave's last
-    const double y = __shfl_down(x, o);
-    if (lane + o < 64) x += y;
-  }
-  // what goes past the piece's end
-  double past = 0.0;
-  const bool whole = end < len;
-  const float* later = whole ? G.later + (bh * G.later_of + piece) * G.state : G.dlast ? G.dlast + bh * G.state : nullptr;
-  if (later && piece * kLinearSave < len) {
-    const float* s = G.saved + (bh * G.saved_of + piece + 1) * G.state;
-    int i = threadIdx.x;
-    for (; i + 7 * kLinearSave < G.state; i += 8 * kLinearSave) {      // (eight at a time under way)
-      float x[8], y[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        x[k] = later[i + k * kLinearSave];
-        y[k] = s[i + k * kLinearSave];
-      }
-#pragma unroll
-      for (int k = 0; k < 8; ++k) past += (double)x[k] * (double)y[k];
-    }
-    for (; i < G.state; i += kLinearSave) past += (double)later[i] * (double)s[i];
-    if (whole) past *= (double)linear_decay(log_gate(A, b, end, h));
-  }
-  past = wave_sum(past);
-  if (lane == 0) {
-    part[wave] = x;
-    part[4 + wave] = past;
-  }
-  __syncthreads();
-  x += (part[4] + part[5]) + (part[6] + part[7]);
-  for (int w = wave + 1; w < 4; ++w) x += part[w];
-  float dg = (float)x;
-  if (!in || log_gate(A, b, t, h) < kLinearLeast) dg = 0.0f;
+  float dg = 0.0f;
+  if (t < steps_of(A, b) && !(log_gate(A, b, t, h) < kLinearLeast))
+    for (int s = 0; s < G.slices; ++s) dg += G.dots[(s * A.batch * A.heads + bh) * A.steps + t];
   if (!G.sums) {
     if (t < A.steps) G.dg[(b * A.steps + t) * A.heads + h] = dg;
     return;
   }
-  __syncthreads();
   const double sum = wave_sum((double)dg);
   if (lane == 0) part[wave] = sum;
   __syncthreads();
   if (threadIdx.x == 0) G.dg[h * A.batch * G.pieces + b * G.pieces + piece] = (float)((part[0] + part[1]) + (part[2] + part[3]));
+}
+
+// ... of up to N steps, by one workgroup for a sequence and head: products of steps' rows, and of rows with the first state and the last one's gradient, both read
+// once.  P is dv's pass (a, b, c = k, q, dy) with x = v; P.first and P.met_last are the two states.
+constexpr int few_row(int n) { return 2 * n + 4; }       // floats of a row of LDS, of which four neighbours are read at a time
+template <class T, int N>
+__global__ __launch_bounds__(256) void k_linear_few_gates(LinearArgs A, LinearPass P, LinearGates G) {
+  constexpr int kRow = few_row(N);
+  extern __shared__ __attribute__((aligned(16))) char few_lds[];
+  float (*const qk)[kRow] = reinterpret_cast<float (*)[kRow]>(few_lds), (*const yv)[kRow] = qk + P.da;     // [entry][step of q or dy, step of k or v]
+  __shared__ float w[N], pairs[N][N], part[4][2 * N + 1];
+  const int64_t bh = blockIdx.x, b = bh / A.heads;
+  const int h = (int)(bh % A.heads), wave = threadIdx.x >> 6, lane = threadIdx.x & 63, n = (int)steps_of(A, b);
+  const T* pk = (const T*)P.a + b * P.a_seq + (h / P.a_share) * P.a_head;
+  const T* pq = (const T*)P.b + b * P.b_seq + (h / P.b_share) * P.b_head;
+  const T* py = (const T*)P.c + b * P.c_seq + (h / P.c_share) * P.c_head;
+  const T* pv = (const T*)P.x + b * P.x_seq + (h / P.x_share) * P.x_head;
+  static_assert(2 * N % 4 == 0);
+  const auto stage = [&](float (*to)[kRow], int dim, const T* x, int64_t x_step, const T* y, int64_t y_step) {
+    const int e = threadIdx.x;      // (256 entries at most)
+    if (e >= dim) return;
+    float all[2 * N];
+#pragma unroll
+    for (int s = 0; s < N; ++s) {
+      all[s] = s < n ? to_float(x[s * x_step + e]) : 0.0f;
+      all[N + s] = s < n ? to_float(y[s * y_step + e]) : 0.0f;
+    }
+#pragma unroll
+    for (int k = 0; k < 2 * N; k += 4) *(float4*)&to[e][k] = float4{all[k], all[k + 1], all[k + 2], all[k + 3]};
+  };
+  stage(qk, P.da, pq, P.b_step, pk, P.a_step);
+  stage(yv, P.dc, py, P.c_step, pv, P.x_step);
+  if (threadIdx.x < N) w[threadIdx.x] = (int)threadIdx.x < n ? linear_decay(log_gate(A, b, threadIdx.x, h)) : 1.0f;
+  __syncthreads();
+  {      // a pair of steps by so many threads
+    constexpr int kEach = 256 / (N * N);
+    const int s = threadIdx.x / (N * kEach), r = threadIdx.x / kEach % N;
+    float x = 0.0f, y = 0.0f;
+    if (r < s && s < n) {
+      for (int e = threadIdx.x % kEach; e < P.da; e += kEach) x = fmaf(qk[e][s], qk[e][N + r], x);
+      for (int e = threadIdx.x % kEach; e < P.dc; e += kEach) y = fmaf(yv[e][s], yv[e][N + r], y);
+    }
+    for (int o = kEach / 2; o; o >>= 1) {
+      x += __shfl_xor(x, o);
+      y += __shfl_xor(y, o);
+    }
+    x *= y;
+    for (int u = r + 1; u <= s; ++u) x *= w[u];
+    if (threadIdx.x % kEach == 0) pairs[s][r] = x;
+  }
+  float sums[2 * N + 1] = {};      // q_s S dy_s, k_r E v_r, <E, S>
+  const int64_t state = (int64_t)P.da * P.dc;
+  const float* first = P.first ? P.first + bh * P.first_of * state : nullptr;
+  const float* last = P.met_last ? P.met_last + bh * state : nullptr;
+  for (int col = lane; col < P.dc; col += 64) {
+    float column[2 * N] = {};
+    constexpr int kAhead = 8;      // rows under way
+    for (int i0 = wave; i0 < P.da; i0 += 4 * kAhead) {
+      float s[kAhead], e[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int i = i0 + 4 * u;
+        s[u] = first && i < P.da ? first[(int64_t)i * P.dc + col] : 0.0f;
+        e[u] = last && i < P.da ? last[(int64_t)i * P.dc + col] : 0.0f;
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const float* row = qk[min(i0 + 4 * u, P.da - 1)];      // (with zeros where there is none)
+#pragma unroll
+        for (int k = 0; k < 2 * N; ++k) column[k] = fmaf(row[k], k < N ? s[u] : e[u], column[k]);
+        sums[2 * N] = fmaf(s[u], e[u], sums[2 * N]);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 2 * N; ++k) sums[k] = fmaf(column[k], yv[col][k], sums[k]);
+  }
+#pragma unroll
+  for (int k = 0; k <= 2 * N; ++k) {
+    float x = sums[k];
+    for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
+    if (lane == 0) part[wave][k] = x;
+  }
+  __syncthreads();
+  const int t = threadIdx.x;
+  float dg = 0.0f;
+  if (t < n && !(log_gate(A, b, t, h) < kLinearLeast)) {
+    const auto sum = [&](int k) { return (part[0][k] + part[1][k]) + (part[2][k] + part[3][k]); };
+    float left = 1.0f;      // from the first state to step s
+    for (int s = 0; s < n; ++s) {
+      left *= w[s];
+      if (s >= t) dg = fmaf(left, sum(s), dg);
+    }
+    if (last) dg = fmaf(left, sum(2 * N), dg);
+    left = 1.0f;      // from step r to the last
+    for (int r = n - 1; last && r >= 0; --r) {
+      if (r < t) dg = fmaf(left, sum(N + r), dg);
+      left *= w[r];
+    }
+    for (int s = t; s < n; ++s)
+      for (int r = 0; r < t; ++r) dg += pairs[s][r];
+  }
+  if (!G.sums) {
+    if (t < A.steps) G.dg[(b * A.steps + t) * A.heads + h] = dg;
+    return;
+  }
+  if (wave == 0) {
+    const double all = wave_sum((double)dg);
+    if (lane == 0) G.dg[h * A.batch + b] = (float)all;
+  }
 }
 // One head's sum over all sequences and pieces.
 __global__ __launch_bounds__(256) void k_linear_gate_sums(const float* parts, int64_t count, float* dg) {

@@ -60,10 +60,15 @@ bool linear_fits(const choco_linear_config& c) {
   return launch_fits((rows * pieces + 8.0) * slices_of(CHOCO_LINEAR_MAX_DIM), 512);
 }
 
+// Slices of the passes in chunks of dq and dk, and of dv.
+int slices_by_k(const choco_linear_config& c) { return slices_of(c.dim_k, slice_of(c, c.dim_v, c.dim_k)); }
+int slices_by_v(const choco_linear_config& c) { return slices_of(c.dim_v, slice_of(c, c.dim_k, c.dim_v)); }
+
 struct LinearLayout {
   size_t later, totals, dots, sums, wide, total;
 };
 void segments_of(const choco_linear_config& c, int32_t& segments, int32_t& chunks);
+int64_t step_by_step(const choco_linear_config& c);
 LinearLayout linear_layout(const choco_linear_config& c, bool back) {
   LinearLayout L{};
   Parts parts;
@@ -80,7 +85,7 @@ LinearLayout linear_layout(const choco_linear_config& c, bool back) {
     L.totals = parts.take(rows * segments * sizeof(double));
   }
   if (back) {
-    L.dots = parts.take(rows * steps * 2 * slices_of(c.dim_k) * sizeof(float));
+    if (c.steps > step_by_step(c)) L.dots = parts.take(rows * steps * (2 * slices_by_k(c) + slices_by_v(c)) * sizeof(float));
     L.sums = parts.take(rows * (size_t)pieces_of(c) * sizeof(float));
     size_t most = 0;
     if (c.q_heads != c.heads || c.k_heads != c.heads) most = c.dim_k;
@@ -127,9 +132,9 @@ LinearArgs linear_args(const choco_linear_config& c, const float* g, const int32
   return A;
 }
 
-// Entries of rows that a load or store takes: as many as `most`, two or one, as the rows are aligned.
+// Entries of rows that a load or store takes: `most`, a power of two, or fewer, as the rows are aligned.
 int width_of(const Rows& r, size_t size, int most, const choco_linear_config& c) {
-  for (int v = most; v > 1; v = v > 2 ? 2 : 1) {
+  for (int v = most; v > 1; v /= 2) {
     const size_t bytes = v * size;
     bool ok = r.dim % v == 0 && aligned_to(r.p, bytes);
     const int64_t count[3] = {c.batch, c.steps, r.heads};
@@ -142,7 +147,8 @@ int width_of(const Rows& r, size_t size, int most, const choco_linear_config& c)
 // Up to so many steps are taken one by one.  us, one by one | in chunks, forward and backward: 160 x 10 heads of 64 in fp32, 4 steps 20 and 65 |
 // 35 and 104, 8 steps 31 and 94 | 36 and 107, 12 steps 41 and 127 | 38 and 110; 64 x 16 heads of 128 in bf16, 4 steps 35 and 113 | 34 and 99, 8 steps 48
 // and 159 | 34 and 100.
-int64_t step_by_step(const choco_linear_config& c) { return c.type == CHOCO_F32 ? 8 : 3; }
+constexpr int kFewOf32 = 8, kFewOf16 = 3;
+int64_t step_by_step(const choco_linear_config& c) { return c.type == CHOCO_F32 ? kFewOf32 : kFewOf16; }
 
 template <class T>
 int run_steps(const choco_linear_config& c, const LinearArgs& A, const LinearPass& P) {
@@ -173,8 +179,9 @@ LinearChunks chunks_of(const choco_linear_config& c, const LinearPass& P, const 
   };
   C.segments = 1;
   C.chunks = (int32_t)((c.steps + kChunk - 1) / kChunk);
-  C.way = far(out, out_size) || (x && far(*x, size)) ? kEntries : kParts;
-  for (const Rows* r : {&a, &b, &v}) {
+  C.way = far(out, out_size) ? kEntries : kParts;
+  for (const Rows* r : {&a, &b, &v, x}) {
+    if (!r) continue;
     const int v16 = (int)(16 / size), v4 = (int)(4 / size);
     if (width_of(*r, size, v16, c) != v16) C.way = std::min(C.way, (int)kWords);
     if (far(*r, size) || (v4 > 1 && width_of(*r, size, v4, c) != v4)) C.way = kEntries;
@@ -229,14 +236,15 @@ int run_backward(const choco_linear_config& c, const LinearArgs& A, const void* 
   const LinearLayout L = linear_layout(c, true);
   const Rows Q{q, c.q_stride, c.q_heads, c.dim_k}, K{k, c.k_stride, c.k_heads, c.dim_k}, V{v, c.v_stride, c.v_heads, c.dim_v},
       Y{dy, c.y_stride, c.heads, c.dim_v};
-  const int64_t rows = rows_of(c), pieces = pieces_of(c), state = (int64_t)c.dim_k * c.dim_v;
+  const int64_t rows = rows_of(c), pieces = pieces_of(c);
   float* const later = (float*)(ws + L.later);
   float* const q_dots = (float*)(ws + L.dots);
-  float* const k_dots = q_dots + rows * c.steps * slices_of(c.dim_k);
+  float* const k_dots = q_dots + rows * c.steps * slices_by_k(c);
+  float* const v_dots = k_dots + rows * c.steps * slices_by_k(c);
   const bool stepwise = c.steps <= step_by_step(c), several = pieces > 1;
   // a pass on its own arrays; a gradient of heads that share one: of every head to the workspace, then added up
   const auto through = [&](LinearPass P, const Rows& ra, const Rows& rb, const Rows& rc_, Rows out, const Rows* x, const float* states,
-                           int64_t states_of) -> int {
+                           int64_t states_of, int mode) -> int {
     const LinearPass given = P;
     const int32_t heads = out.heads, dim = out.dim;
     const int64_t wide_stride[3] = {(int64_t)c.heads * dim * c.steps, (int64_t)c.heads * dim, dim};
@@ -258,7 +266,8 @@ int run_backward(const choco_linear_config& c, const LinearArgs& A, const void* 
         C.states = const_cast<float*>(states);
         C.states_of = states_of;
       }
-      if (const int rc = P.dots ? run_chunks<T, kResultAndDots>(c, A, P, C) : run_chunks<T, kResult>(c, A, P, C)) return rc;
+      const int rc = mode == kOfStates ? run_chunks<T, kOfStates>(c, A, P, C) : mode == kOfPairs ? run_chunks<T, kOfPairs>(c, A, P, C) : run_chunks<T, kResult>(c, A, P, C);
+      if (rc) return rc;
     }
     if (heads == c.heads) return CHOCO_OK;
     const int64_t count = c.batch * c.steps * heads * dim;
@@ -269,13 +278,6 @@ int run_backward(const choco_linear_config& c, const LinearArgs& A, const void* 
     return CHOCO_OK;
   };
   const Rows DQ{dq, c.dq_stride, c.q_heads, c.dim_k}, DK{dk, c.dk_stride, c.k_heads, c.dim_k}, DV{dv, c.dv_stride, c.v_heads, c.dim_v};
-  LinearPass P = pass_of(c, Y, V, K, dq, c.dq_stride);
-  state_of(c, true, P);
-  P.first = saved;
-  P.first_of = pieces + 1;
-  P.x = q; P.x_seq = c.q_stride[0]; P.x_step = c.q_stride[1]; P.x_head = c.q_stride[2]; P.x_share = c.heads / c.q_heads;
-  P.dots = dg ? q_dots : nullptr;
-  if (const int rc = through(P, Y, V, K, DQ, dg ? &Q : nullptr, saved, pieces + 1)) return rc;
   LinearPass last = pass_of(c, K, Q, Y, dv, c.dv_stride);
   state_of(c, false, last);
   last.back = true;
@@ -291,29 +293,55 @@ int run_backward(const choco_linear_config& c, const LinearArgs& A, const void* 
     C.totals = (double*)(ws + L.totals);
     if (const int rc = run_states<T>(c, A, last, C, dlast, dh0)) return rc;
   }
+  const bool parts = dg && !stepwise;      // of the gates' gradient, by dq's pass and dk's
+  LinearPass P = pass_of(c, Y, V, K, dq, c.dq_stride);
+  state_of(c, true, P);
+  P.first = saved;
+  P.first_of = pieces + 1;
+  if (parts) {
+    P.x = q; P.x_seq = c.q_stride[0]; P.x_step = c.q_stride[1]; P.x_head = c.q_stride[2]; P.x_share = c.heads / c.q_heads;
+    P.dots = q_dots;
+    P.met = later;
+    P.met_of = pieces;
+    P.met_last = dlast;
+  }
+  if (const int rc = through(P, Y, V, K, DQ, parts ? &Q : nullptr, saved, pieces + 1, kOfStates)) return rc;
   P = pass_of(c, V, Y, Q, dk, c.dk_stride);
   state_of(c, true, P);
   P.back = true;
   P.first = dlast;
   P.first_of = 1;
-  P.x = k; P.x_seq = c.k_stride[0]; P.x_step = c.k_stride[1]; P.x_head = c.k_stride[2]; P.x_share = c.heads / c.k_heads;
-  P.dots = dg ? k_dots : nullptr;
-  if (const int rc = through(P, V, Y, Q, DK, dg ? &K : nullptr, later, pieces)) return rc;
-  if (const int rc = through(last, K, Q, Y, DV, nullptr, later, pieces)) return rc;
+  if (parts) {
+    P.x = k; P.x_seq = c.k_stride[0]; P.x_step = c.k_stride[1]; P.x_head = c.k_stride[2]; P.x_share = c.heads / c.k_heads;
+    P.dots = k_dots;
+    P.met = saved;
+    P.met_of = pieces + 1;
+  }
+  if (const int rc = through(P, V, Y, Q, DK, parts ? &K : nullptr, later, pieces, kOfStates)) return rc;
+  if (parts) {
+    last.x = v; last.x_seq = c.v_stride[0]; last.x_step = c.v_stride[1]; last.x_head = c.v_stride[2]; last.x_share = c.heads / c.v_heads;
+    last.dots = v_dots;
+  }
+  if (const int rc = through(last, K, Q, Y, DV, parts ? &V : nullptr, later, pieces, parts ? kOfPairs : kResult)) return rc;
   if (!dg) return CHOCO_OK;
   LinearGates G{};
-  G.q_dots = q_dots; G.k_dots = k_dots;
-  G.saved = saved; G.later = later; G.dlast = dlast;
-  G.saved_of = pieces + 1; G.later_of = pieces;
-  LinearPass of_k{};
-  of_k.da = c.dim_v;
-  of_k.dc = c.dim_k;
-  G.q_slices = G.k_slices = slices_of(c.dim_k, stepwise ? kLinearSlice : slice_of(c, of_k));
-  G.state = (int32_t)state;
+  G.dots = q_dots;
+  G.slices = 2 * slices_by_k(c) + slices_by_v(c);
   G.pieces = pieces;
   G.sums = !c.gate_steps;
   G.dg = G.sums ? (float*)(ws + L.sums) : dg;
-  if (pieces > 0) {
+  if (pieces > 0 && stepwise) {
+    LinearPass few = pass_of(c, K, Q, Y, nullptr, c.dv_stride);
+    few.x = v; few.x_seq = c.v_stride[0]; few.x_step = c.v_stride[1]; few.x_head = c.v_stride[2]; few.x_share = c.heads / c.v_heads;
+    few.first = saved;
+    few.first_of = pieces + 1;
+    few.met_last = dlast;
+    constexpr int kFew = std::is_same_v<T, float> ? kFewOf32 : kFewOf16;
+    const auto lds = [&](int n) { return (size_t)(c.dim_k + c.dim_v) * few_row(n) * sizeof(float); };
+    if (c.steps <= 4) k_linear_few_gates<T, 4><<<dim3((uint32_t)rows), 256, lds(4), stream>>>(A, few, G);
+    else if constexpr (kFew > 4) k_linear_few_gates<T, kFew><<<dim3((uint32_t)rows), 256, lds(kFew), stream>>>(A, few, G);
+    TRY_HIP(hipGetLastError());
+  } else if (pieces > 0) {
     k_linear_gates<<<dim3((uint32_t)(rows * pieces)), kLinearSave, 0, stream>>>(A, G);
     TRY_HIP(hipGetLastError());
   }

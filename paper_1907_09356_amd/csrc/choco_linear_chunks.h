@@ -13,10 +13,10 @@ inline int slices_of(int dim, int slice = kLinearSlice) { return (dim + slice - 
 inline int64_t rows_of(const choco_linear_config& c) { return c.batch * c.heads; }
 // Columns of a result that a workgroup takes: 16 a wave, four waves where that is enough, else eight (but four where eight's columns
 // leave no room in LDS).
-inline int slice_of(const choco_linear_config& c, const LinearPass& P) { return P.dc <= 64 || (c.type == CHOCO_F32 && P.da > 128) ? 64 : 128; }
+inline int slice_of(const choco_linear_config& c, int da, int dc) { return dc <= 64 || (c.type == CHOCO_F32 && da > 128) ? 64 : 128; }
+inline int rows_held(int da) { return da <= 64 ? 64 : da <= 128 ? 128 : 256; }      // rows of a state that a workgroup has registers for
 
-
-// A pass (MODE: kStates, kResult, kResultAndDots) over all segments.
+// A pass (MODE: kStates, kResult, kOfStates, kOfPairs) over all segments.
 template <class In, int MODE>
 int run_chunks(const choco_linear_config& c, const LinearArgs& A, const LinearPass& P, LinearChunks C);
 
@@ -36,7 +36,7 @@ int launch_chunks(const choco_linear_config& c, const LinearArgs& A, const Linea
 }
 template <class In, int MODE>
 int run_chunks(const choco_linear_config& c, const LinearArgs& A, const LinearPass& P, LinearChunks C) {
-  const int slice = slice_of(c, P);
+  const int slice = slice_of(c, P.da, P.dc);
   C.slices = slices_of(P.dc, slice);
   C.blocks = (uint32_t)((rows_of(c) * C.segments + 7) / 8 * 8 * C.slices);
   const auto with_way = [&](auto dim, auto waves, auto way) -> int {
@@ -53,15 +53,16 @@ int run_chunks(const choco_linear_config& c, const LinearArgs& A, const LinearPa
     if (slice == 64) return with_waves(dim, std::integral_constant<int, 4>{});
     return with_waves(dim, std::integral_constant<int, 8>{});
   };
-  if (P.da <= 64) return with_dim(std::integral_constant<int, 64>{});
-  if (P.da <= 128) return with_dim(std::integral_constant<int, 128>{});
+  if (rows_held(P.da) == 64) return with_dim(std::integral_constant<int, 64>{});
+  if (rows_held(P.da) == 128) return with_dim(std::integral_constant<int, 128>{});
   return with_dim(std::integral_constant<int, 256>{});
 }
 
 
 template int run_chunks<CHOCO_LINEAR_TYPE, kStates>(const choco_linear_config&, const LinearArgs&, const LinearPass&, LinearChunks);
 template int run_chunks<CHOCO_LINEAR_TYPE, kResult>(const choco_linear_config&, const LinearArgs&, const LinearPass&, LinearChunks);
-template int run_chunks<CHOCO_LINEAR_TYPE, kResultAndDots>(const choco_linear_config&, const LinearArgs&, const LinearPass&, LinearChunks);
+template int run_chunks<CHOCO_LINEAR_TYPE, kOfStates>(const choco_linear_config&, const LinearArgs&, const LinearPass&, LinearChunks);
+template int run_chunks<CHOCO_LINEAR_TYPE, kOfPairs>(const choco_linear_config&, const LinearArgs&, const LinearPass&, LinearChunks);
 #endif
 
 }  // namespace choco
