@@ -182,7 +182,7 @@ __global__ __launch_bounds__(256) void k_linear_steps(LinearArgs A, LinearPass P
 //
 // Entries of 32 bits go to the fp32 matrix instruction.  Those of 16 bits are operands as they are; what is fp32 by nature (P, S, weighted c)
 // enters as a sum of numbers of that type.  bf16: two of them (2^-17) for a result of 16 bits, three (2^-25) for states and wherever the
-// result also goes into fp32 sums.  fp16: two (2^-22), after a power of two has brought the largest into fp16's range.
+// result also goes into fp32 sums.  fp16: two (2^-22), after a power of two has brought the largest of a state's column, or of a step's P, into fp16's range.
 //
 // What bounds it: of a chunk of 64 x 128 x 128 in bf16 a SIMD's four waves take some 10,000 cycles of vector instructions (half of them split
 // fp32 numbers), 7,000 of matrix instructions, and LDS 5,000; memory 5,000 at the rate of a copy.  They overlap by half: 363 us for the
@@ -276,42 +276,31 @@ struct Operand<f16_t> {
   }
   static __device__ __forceinline__ f32x4 mma(Frag a, Frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 };
-// A power of two that brings numbers of a wave, the largest of them `most`, near the top of fp16's range, and back: up to 2^12, so that sums of
-// thousands stay in fp32's and what is 2^-36 of the largest still counts.
+// A power of two that brings numbers, the largest of them `most`, to the top of fp16's range, and back: below 2^15, so that what is 2^-39 of the
+// largest still counts.
 struct Range {
   float up, down;
   __device__ __forceinline__ explicit Range(float most) {
-    const uint32_t e = max(__float_as_uint(most) >> 23, 12u);      // (not negative, not infinite)
-    up = __uint_as_float((265u - e) << 23);
-    down = __uint_as_float((e - 11u) << 23);
+    const uint32_t e = max(__float_as_uint(most) >> 23, 15u);      // (not negative, not infinite)
+    up = __uint_as_float((268u - e) << 23);
+    down = __uint_as_float((e - 14u) << 23);
   }
 };
-template <int CONTROL, int ROWS>
-__device__ __forceinline__ float larger_of(float x) {
-  return fmaxf(x, __uint_as_float(__builtin_amdgcn_update_dpp(__float_as_uint(x), __float_as_uint(x), CONTROL, ROWS, 15, false)));
-}
-__device__ __forceinline__ float largest_of_wave(float x) {
-  x = larger_of<0x111, 15>(x);
-  x = larger_of<0x112, 15>(x);
-  x = larger_of<0x114, 15>(x);
-  x = larger_of<0x118, 15>(x);
-  x = larger_of<0x142, 10>(x);
-  x = larger_of<0x143, 12>(x);
-  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), 63));
-}
-// The largest magnitude of a wave's numbers, which `each` hands out; where one is infinite, of the others, which then keep their places.
+// The largest magnitude of a column's numbers, which are in a lane of each row of 16 and which `each` hands out; where one is infinite, of the others,
+// which then keep their places.
 template <class Each>
-__device__ __forceinline__ float largest_of_wave(Each each) {
+__device__ __forceinline__ float largest_of_column(Each each) {
   constexpr float kInfinite = __builtin_inff();
   float most = 0.0f;
   each([&](float x) { most = fmaxf(most, fabsf(x)); });
-  most = largest_of_wave(most);
-  if (most == kInfinite) {
+  if (__any(most == kInfinite)) {
     most = 0.0f;
     each([&](float x) { most = fmaxf(most, fabsf(x) < kInfinite ? fabsf(x) : 0.0f); });
-    most = largest_of_wave(most);
   }
-  return most;
+  const auto two = __builtin_amdgcn_permlane16_swap(__float_as_uint(most), __float_as_uint(most), false, false);
+  most = fmaxf(__uint_as_float(two[0]), __uint_as_float(two[1]));
+  const auto four = __builtin_amdgcn_permlane32_swap(__float_as_uint(most), __float_as_uint(most), false, false);
+  return fmaxf(__uint_as_float(four[0]), __uint_as_float(four[1]));
 }
 // fp32 numbers of an operand as so many operands that add up to it.
 template <class Core, int N>
@@ -374,7 +363,8 @@ struct ChunkShared {
   Core more[kTurned && kScores > kRows ? kScores - kRows : 1];
   alignas(16) Core c[kChunk][kSlice + kPad];
   alignas(16) Core turned[kTurned ? DA : 1][kTurned ? kTurnedRow : 1];
-  alignas(16) float c_high[kChunk], c_low[kChunk], to_end[kChunk], dots[WAVES][kChunk], most[WAVES];
+  alignas(16) float c_high[kChunk], c_low[kChunk], to_end[kChunk], dots[WAVES][kChunk];
+  uint32_t most[kChunk];
   alignas(16) float behind[10][16], before[10][16];      // sums over pairs of steps, of ten tiles
   float met[WAVES], ahead[WAVES], weights[kChunk], ahead_all;
 };
@@ -775,6 +765,7 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
         S.met[wave] = other ? meet(other, thread) : 0.0f;
       }
     }
+    if (!STATE && RANGED && wave == WAVES - 1) S.most[lane] = 0;
     if (wave == 0) {      // the logarithms' sums
       const double x = sums_to(next_g < kLinearLeast ? (double)kLog2Least : (double)next_g * 1.4426950408889634);
       const double all = __shfl(x, 63);
@@ -817,11 +808,11 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
     if constexpr (!STATE) {
       // what comes of the state before the chunk
       f32x4 y[4] = {};
-      // y += S^T a of the rows in LDS, in fp16 times a power of two that is taken back by the result
-      const auto by_state = [&](f32x4 (&y)[4]) -> float {
+      // y += S^T a of the rows in LDS, in fp16 times powers of two for each column of S that are taken back by the result
+      const auto by_state = [&](f32x4 (&y)[4]) -> f32x4 {
         float most = 0.0f;
         if constexpr (RANGED)
-          most = largest_of_wave([&](auto&& see) {
+          most = largest_of_column([&](auto&& see) {
 #pragma unroll
             for (int j = 0; j < kJ * kT; ++j)
 #pragma unroll
@@ -844,7 +835,11 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
             for (int n = N_OUT - 1; n >= 0; --n) y[t] = Op::mma(p[n], q, y[t]);
           }
         }
-        return RANGED ? range.down : 1.0f;
+        f32x4 down = {};      // of the columns that a lane has of y
+        if constexpr (RANGED)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) down[r] = __shfl(range.down, 4 * g + r);
+        return down;
       };
       const auto products_with = [&](const f32x4& y, const Four<In>& x) {      // of a row of the wave's columns (what is not there is zero)
         float d = 0.0f;
@@ -859,12 +854,12 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
           if (P.dots)
 #pragma unroll
             for (int t = 0; t < 4; ++t) times[t] = entries_of_x(t0, lo, hi, 16 * t + l, first, P.dc - first);
-        const float down = by_state(y);
+        const f32x4 down = by_state(y);
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           const float here = __builtin_amdgcn_exp2f(S.c_high[16 * t + l] + S.c_low[16 * t + l]);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) y[t][r] *= RANGED ? here * down : here;
+          for (int r = 0; r < 4; ++r) y[t][r] *= RANGED ? here * down[r] : here;
           if constexpr (DOTS)
             if (P.dots) {
               const float d = products_with(y[t], times[t]);
@@ -923,32 +918,32 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
           score[n][r] = s < t || 4 * g + r <= l ? weighted : 0.0f;
         }
       }
-      float most = 0.0f;
-      if constexpr (RANGED) {
-        most = largest_of_wave([&](auto&& see) {
+      if constexpr (RANGED)
 #pragma unroll
-          for (int n = 0; n < kTiles; ++n)
+        for (int n = 0; n < kTiles; ++n) {
+          const int pair = tiles >> (8 * (kTiles - 1 - n)) & 255, t = pair >> 4, s = pair & 15;
+          if (s > t || t > 3) continue;
+          const float most = largest_of_column([&](auto&& see) {
 #pragma unroll
             for (int r = 0; r < 4; ++r) see(score[n][r]);
-        });
-        if (lane == 0) S.most[wave] = most;
-      }
+          });
+          if (g == 0) atomicMax(&S.most[16 * t + l], __float_as_uint(most));      // (the order does not matter)
+        }
+      const auto range_of = [&](int t) { return Range(__uint_as_float(S.most[16 * t + l])); };      // of P's row
       __syncthreads();
       // P by rows, over a (and b, which in 16 bits is needed by columns only from here on)
       Core (*const scores)[kChunk][Shared::kScoreRow] = reinterpret_cast<Core (*)[kChunk][Shared::kScoreRow]>(&S.a[0][0]);
       static_assert(Shared::kTurned ? N_OUT <= 3 : kChunk * Shared::kScoreRow * sizeof(Core) <= sizeof(S.a));
-      if constexpr (RANGED)
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) most = fmaxf(most, S.most[w]);
-      const Range range(most);
 #pragma unroll
       for (int n = 0; n < kTiles; ++n) {
         const int pair = tiles >> (8 * (kTiles - 1 - n)) & 255, t = pair >> 4, s = pair & 15;
         if (t > 3) continue;
         float left[4] = {score[n][0], score[n][1], score[n][2], score[n][3]};
-        if constexpr (RANGED)
+        if constexpr (RANGED) {
+          const float up = range_of(t).up;
 #pragma unroll
-          for (int r = 0; r < 4; ++r) left[r] *= range.up;
+          for (int r = 0; r < 4; ++r) left[r] *= up;
+        }
 #pragma unroll
         for (int k = 0; k < N_OUT; ++k) {
           store_floats<Core, 4>(&scores[k][16 * t + l][16 * s + 4 * g], left);
@@ -990,7 +985,8 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
           for (int s = 0; s <= t / kT; ++s)
 #pragma unroll
             for (int n = N_OUT - 1; n >= 0; --n) sum = Op::mma(cf[s], Op::load(&scores[n][16 * t + l][0], s, g), sum);
-          y[t] = RANGED ? y[t] + sum * range.down : sum;
+          if constexpr (RANGED) y[t] += sum * range_of(t).down;
+          else y[t] = sum;
           // rows of the result: step 16 t + l, columns 4 g to 4 g + 3 of the wave's
           const int row = 16 * t + l, when = P.back ? kChunk - 1 - row : row;
           const bool here = row >= lo && row < hi;
@@ -1019,7 +1015,7 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
           __syncthreads();
           if (busy) {
             f32x4 z[4] = {};
-            const float down = by_state(z);
+            const f32x4 down = by_state(z);
             Four<In> times[4];
 #pragma unroll
             for (int t = 0; t < 4; ++t) times[t] = entries_of_x(t1, lo, hi, 16 * t + l, first, P.dc - first);
@@ -1027,8 +1023,8 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
               const int row = 16 * t + l;
-              const float d = products_with(z[t], times[t]);
-              sum += row >= lo && row < hi ? d * (RANGED ? down * S.weights[row] : S.weights[row]) : 0.0f;
+              const float d = products_with(RANGED ? z[t] * down : z[t], times[t]);
+              sum += row >= lo && row < hi ? d * S.weights[row] : 0.0f;
             }
             S.ahead[wave] = row_sum(sum);
             columns(cf);      // (anew: there are no registers to keep it)
@@ -1082,7 +1078,7 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
       f32x4 w[kS][kT];
 #pragma unroll
       for (int s = 0; s < kS; ++s) weighted(s, w[s]);
-      const Range range(largest_of_wave([&](auto&& see) {
+      const Range range(largest_of_column([&](auto&& see) {
 #pragma unroll
         for (int s = 0; s < kS; ++s)
 #pragma unroll

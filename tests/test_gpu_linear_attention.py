@@ -175,6 +175,29 @@ def test_magnitudes(dtype, size_q, size_k, size_v, N):
               dlast * 2.0 ** -6)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("N", [3, 64, 200, 700])
+def test_columns_and_steps_of_unlike_magnitudes(dtype, N):
+    # neighbouring columns of v and of the states 2^-26 apart, and steps' q likewise: a column's state and a step's result are as near as they would
+    # be alone (results that fp16 does not hold are infinite)
+    q, k, v, g, h0, _, dy, dlast = make(2, N, 2, 24, 40, dtype, seed=N, gate="head")
+    column = torch.where(torch.arange(40, device="cuda") % 3 == 0, 2.0 ** 12, 2.0 ** -14)
+    step = torch.where(torch.arange(N, device="cuda") % 5 == 0, 2.0 ** 11, 2.0 ** -13)[:, None, None]
+    for size_q, size_v, size_h in ((2.0 ** -6, column, column), (step, 2.0 ** 9, 2.0 ** 9)):
+        check_all(*((q * size_q).to(dtype), k, (v * size_v).to(dtype), g, h0 * size_h, None, dy, dlast), grad=False)
+    # the same backwards: the gradient of a state has dy's columns
+    column = column * 2.0 ** -6
+    cols, last = (dy * column).to(dtype), dlast * column
+    n = whole(None, 2, N)
+    exact = reference(q, k, v, g, h0, n, cols, last)
+    size = reference(q.abs(), k.abs(), v.abs(), g, h0.abs(), n, cols.abs(), last.abs())
+    saved = T.linear_attention(q, k, v, g, h0=h0, save=True)[2]
+    got = T.linear_attention_grad(q, k, v, g, saved, cols, dlast=last)
+    for name, x in zip(("dq", "dk", "dv", "dg", "dh0"), got):
+        if name != "dg":
+            check(x, exact[name], size[name], 24 + 40 + N + 64, name)
+
+
 @pytest.mark.parametrize("N", [1, 30, 400])
 def test_what_padding_holds_does_not_matter(N):
     q, k, v, g, h0, _, dy, dlast = make(4, N, 2, 32, 32, F32, seed=N)
