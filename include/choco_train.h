@@ -64,9 +64,10 @@ int choco_embed_backward(const choco_embed_config* cfg, const void* tokens_dev, 
  * A state that is infinite stays so or becomes NaN (where the product of the gates since is below fp32's range), in its channel of
  * its sequence only.  In long sequences workgroups wait for the states of earlier ones; a wait that does not end within some
  * seconds is given up and the states after it are NaN, without an error code.
- * In 16 bits more than a few steps are taken by 16-bit products of fp32 accuracy where states and the gates' gradient come of them, and of 2^-17 of what
- * is added up where y or dv does.  In CHOCO_F16 a number of a state, and a step's product of q and k, enters them relative to the largest of its column and of
- * its step within 64 steps: what is less than 2^-39 of that is lost.
+ * Inputs of 16 bits are multiplied by 16-bit matrix instructions, from a few steps on, with fp32 operands as sums of 16-bit numbers: to 2^-22 of what is added
+ * up or nearer in CHOCO_F16; in CHOCO_BF16 to 2^-25 for states, dq, dk and dg and to 2^-17 for y and dv, which are rounded to 2^-9 next.  In CHOCO_F16 an
+ * entry of a state counts relative to the largest of its column, and one step's product of q and k relative to the largest of its 64 steps': what is less than
+ * 2^-39 of that is lost.
  * Generation is steps = 1 with h0 = the last state; h_last may be h0's own buffer. */
 #define CHOCO_RECUR_SAVE_STEPS 8
 typedef struct {

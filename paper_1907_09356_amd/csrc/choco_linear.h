@@ -181,8 +181,9 @@ __global__ __launch_bounds__(256) void k_linear_steps(LinearArgs A, LinearPass P
 // a quarter of it.  Differences of c are taken of c in two floats: a start-over leaves the steps behind it exact.
 //
 // Entries of 32 bits go to the fp32 matrix instruction.  Those of 16 bits are operands as they are; what is fp32 by nature (P, S, weighted c)
-// enters as a sum of numbers of that type.  bf16: two of them (2^-17) for a result of 16 bits, three (2^-25) for states and wherever the
-// result also goes into fp32 sums.  fp16: two (2^-22), after a power of two has brought the largest of a state's column, or of a step's P, into fp16's range.
+// enters as a sum of numbers of that type.  bf16: three of them (2^-25) for states, and for dq and dk, whose products with what comes of states go into the
+// gates' gradient in fp32; two (2^-17) for y and dv, which are rounded to 16 bits next (dv of shared heads after their sum).  Which does not depend on
+// what is asked for.  fp16: two (2^-22), after a power of two has brought the largest of a state's column, or of a step's P, to the top of fp16's range.
 //
 // What bounds it: of a chunk of 64 x 128 x 128 in bf16 a SIMD's four waves take some 10,000 cycles of vector instructions (half of them split
 // fp32 numbers), 7,000 of matrix instructions, and LDS 5,000; memory 5,000 at the rate of a copy.  They overlap by half: 363 us for the

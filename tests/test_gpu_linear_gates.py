@@ -138,3 +138,20 @@ def test_values_that_are_not_finite_stay_in_their_sequence_and_head():
         keep = torch.ones_like(g, dtype=torch.bool)
         keep[1, :, 1] = False
         assert torch.equal(grads[0][keep], grads[1][keep]) and bool(grads[1][1, N // 2 + 1:, 1].isnan().all())
+
+
+@pytest.mark.parametrize("N", [2, 8, 70, 600])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("heads", [(4, 4, 4), (2, 1, 4), (4, 4, 1)])
+def test_the_other_gradients_do_not_depend_on_whether_the_gates_is_asked_for(heads, dtype, N):
+    q, k, v, g, h0, lengths, dy, dlast = make(3, N, 4, 40, 24, dtype, heads=heads, ragged=True)
+    saved = T.linear_attention(q, k, v, g, h0=h0, lengths=lengths, save=True)[2]
+    want = T.linear_attention_grad(q, k, v, g, saved, dy, lengths=lengths, dlast=dlast)
+    got = [torch.zeros_like(x) for x in (q.contiguous(), k.contiguous(), v.contiguous())]
+    dh0 = torch.zeros_like(h0)
+    cfg, nbytes, _ = T._linear_config(1, g, (q, k, v, dy, *got))
+    workspace = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+    T._enqueue(q, "choco_linear_backward", cfg, q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), lengths.data_ptr(), saved.data_ptr(),
+               dy.data_ptr(), dlast.data_ptr(), *(x.data_ptr() for x in got), None, dh0.data_ptr(), workspace.data_ptr(), nbytes)
+    for name, a, b in zip(("dq", "dk", "dv", "dh0"), got + [dh0], want[:3] + want[4:]):
+        assert torch.equal(a, b), name
