@@ -211,7 +211,7 @@ int choco_adamw_destroy(choco_adamw* a);
 /* ---- orthogonalised matrices, and an optimiser that steps along them -----------------------------------
  * The iteration on a matrix U, in fp32, from X = U / |U|_F (zero for a zero matrix):
  *   P = X X^T,   X <- a X + (b P + c P^2) X,   (a, b, c) = (3.4445, -4.7750, 2.0315)
- * brings the singular values that are not far below the largest near one (within 0.7 .. 1.2 after five).  Where U has more rows
+ * brings singular values near one: into 0.68 .. 1.21 after five, those from 1 / 500 of |U|_F on.  Smaller ones grow 3.4-fold each time.  Where U has more rows
  * than columns it is taken transposed, which gives the same matrix.  Products are of fp32 accuracy: operands are two fp16 numbers
  * each, 22 bits, and sums are fp32.  A matrix with an infinite or NaN entry becomes NaN. */
 typedef struct {
