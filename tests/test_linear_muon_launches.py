@@ -81,3 +81,20 @@ out = launches(T.lib().choco_muon_step(a, P, T.F32, 0.1, None))
 """ % (n, count))
     assert all(fits(launch) for launch in out)
     assert sum(grid[0] for _, grid, _, _ in out) == n * count
+
+
+def test_the_shapes_that_are_compared_with_64_bits_take_every_form():
+    from tests.test_gpu_newton_schulz import BOTH, LARGE, SIXTY_FOUR, WHOLE
+    out = run("""
+out = []
+for batch, rows, cols in %s:
+    c = T.OrthogonalizeConfig(batch=batch, rows=rows, cols=cols, type=T.F32, iterations=1, x_stride=(ctypes.c_int64 * 2)(rows * cols, cols),
+                              y_stride=(ctypes.c_int64 * 2)(rows * cols, cols))
+    stub.stub_clear()
+    out.append([launch[0] for launch in launches(T.lib().choco_orthogonalize(ctypes.byref(c), P, P, P, 1 << 50))])
+""" % (WHOLE + SIXTY_FOUR + LARGE + BOTH))
+    forms = [["k_muon_whole<float,false>"]] * len(WHOLE)
+    for shapes, gram, apply in ((SIXTY_FOUR, 64, 64), (LARGE, 128, 128), (BOTH, 64, 128)):
+        forms += [["k_muon_squares<float,false>", "k_muon_start<float,false>", "k_muon_product<0,%d>" % gram, "k_muon_product<1,%d>" % gram,
+                   "k_muon_product<2,%d>" % apply]] * len(shapes)
+    assert out == forms, [(a, b) for a, b in zip(out, forms) if a != b]
