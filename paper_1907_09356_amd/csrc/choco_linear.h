@@ -442,7 +442,7 @@ __device__ __forceinline__ void store_four(__amdgpu_buffer_rsrc_t buffer, uint32
 // A chunk's rows of one array on their way from memory to LDS, in the registers of WAVES waves: they are asked for while the chunk
 // before is worked on.  A thread takes R rows of V entries at a time: one of eight, or, for rows that are also laid out by
 // columns, four of four, 16 neighbouring lanes 4 x 4 of these, which meets all banks both ways.
-template <class In, class Core, int W, int R, int WAVES, int WAY>
+template <class In, int W, int R, int WAVES, int WAY>
 struct Staged {
   static constexpr int V = R == 1 ? 8 : 4;
   static constexpr int kWordsOf = V * sizeof(In) / 4;      // of V entries
@@ -523,23 +523,13 @@ struct Staged {
       }
     }
   }
-  __device__ __forceinline__ float at(int i, int r, int e) const {
-    if constexpr (sizeof(In) == 4) return __uint_as_float(x[i][r][e]);
-    else return entry<In>(x[i][r][e / 2], e & 1);
-  }
   template <int STRIDE>
-  __device__ __forceinline__ void store(int thread, Core (&to)[kChunk][STRIDE]) const {
+  __device__ __forceinline__ void store(int thread, In (&to)[kChunk][STRIDE]) const {
     if constexpr (kByWords) {
 #pragma unroll
       for (int i = 0; i < kUnits * kWordsOf; ++i) {
-        const uint32_t word = x[i / kWordsOf][0][i % kWordsOf];
-        Core* p = &to[thread / kRowWords + i * (kThreads / kRowWords)][thread % kRowWords * kEach];
-        if constexpr (sizeof(In) == sizeof(Core)) {
-          *reinterpret_cast<uint32_t*>(p) = word;
-        } else {
-          p[0] = entry<In>(word, 0);
-          p[1] = entry<In>(word, 1);
-        }
+        In* p = &to[thread / kRowWords + i * (kThreads / kRowWords)][thread % kRowWords * kEach];
+        *reinterpret_cast<uint32_t*>(p) = x[i / kWordsOf][0][i % kWordsOf];
       }
       return;
     }
@@ -550,20 +540,20 @@ struct Staged {
       if (!mine(row, col)) continue;
 #pragma unroll
       for (int r = 0; r < R; ++r) {
-        if constexpr (sizeof(Core) == 2) {
-          if constexpr (V == 8) *reinterpret_cast<uint4*>(&to[row + r][col]) = uint4{x[i][r][0], x[i][r][1], x[i][r][2], x[i][r][3]};
-          else *reinterpret_cast<uint2*>(&to[row + r][col]) = uint2{x[i][r][0], x[i][r][1]};
+        if constexpr (kWordsOf == 2) {
+          *reinterpret_cast<uint2*>(&to[row + r][col]) = uint2{x[i][r][0], x[i][r][1]};
         } else {
 #pragma unroll
-          for (int e = 0; e < V; e += 4) *reinterpret_cast<f32x4*>(&to[row + r][col + e]) = f32x4{at(i, r, e), at(i, r, e + 1), at(i, r, e + 2), at(i, r, e + 3)};
+          for (int w = 0; w < kWordsOf; w += 4)
+            *reinterpret_cast<uint4*>(&to[row + r][col + w * kEach]) = uint4{x[i][r][w], x[i][r][w + 1], x[i][r][w + 2], x[i][r][w + 3]};
         }
       }
     }
   }
   // ... by columns: four steps of an entry are 8 bytes
   template <int STRIDE>
-  __device__ __forceinline__ void store_turned(int thread, Core (*to)[STRIDE]) const {
-    static_assert(R == 4 && sizeof(Core) == 2);
+  __device__ __forceinline__ void store_turned(int thread, In (*to)[STRIDE]) const {
+    static_assert(R == 4 && sizeof(In) == 2);
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
       int row, col;
@@ -607,13 +597,13 @@ constexpr int kPieces = std::is_same_v<Core, float> ? 1 : std::is_same_v<Core, f
 template <class Core, int DA, int WAVES>
 constexpr int kChunkWaves = WAVES == 8 ? (sizeof(ChunkShared<Core, DA, WAVES>) * 2 > 163840 ? 2 : 4) : sizeof(ChunkShared<Core, DA, WAVES>) * 2 > 163840 ? 1 : 2;
 
-template <class In, class Core, int DA, int WAVES, int MODE, int WAY>
-__global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_linear_chunks(LinearArgs A, LinearPass P, LinearChunks C) {
-  typedef ChunkShared<Core, DA, WAVES> Shared;
-  constexpr bool STATE = MODE == kStates, DOTS = MODE == kOfStates, PAIRS = MODE == kOfPairs, X_IN_LDS = sizeof(Core) == 2;
-  constexpr bool RANGED = std::is_same_v<Core, f16_t>;
-  constexpr int N_OUT = kPieces<Core, MODE>, N_STATE = kPieces<Core, kStates>, kSlice = Shared::kSlice;
-  typedef Operand<Core> Op;
+template <class In, int DA, int WAVES, int MODE, int WAY>
+__global__ __launch_bounds__(64 * WAVES, (kChunkWaves<In, DA, WAVES>)) void k_linear_chunks(LinearArgs A, LinearPass P, LinearChunks C) {
+  typedef ChunkShared<In, DA, WAVES> Shared;
+  constexpr bool STATE = MODE == kStates, DOTS = MODE == kOfStates, PAIRS = MODE == kOfPairs, X_IN_LDS = sizeof(In) == 2;
+  constexpr bool RANGED = std::is_same_v<In, f16_t>;
+  constexpr int N_OUT = kPieces<In, MODE>, N_STATE = kPieces<In, kStates>, kSlice = Shared::kSlice;
+  typedef Operand<In> Op;
   typedef typename Op::Frag Frag;
   constexpr int kJ = DA / Op::kInner, kT = Op::kTiles, kS = kChunk / Op::kInner;
   extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -688,9 +678,9 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
 
   const int64_t inside = min(end, len);       // steps of the segment that are in the sequence end here
   const int chunks = inside > begin ? (int)((inside - begin + kChunk - 1) / kChunk) : 0;
-  Staged<In, Core, DA, 1, WAVES, WAY> next_a;
-  Staged<In, Core, DA, Shared::kTurned ? 4 : 1, WAVES, WAY> next_b;
-  Staged<In, Core, kSlice, 1, WAVES, WAY> next_c;
+  Staged<In, DA, 1, WAVES, WAY> next_a;
+  Staged<In, DA, Shared::kTurned ? 4 : 1, WAVES, WAY> next_b;
+  Staged<In, kSlice, 1, WAVES, WAY> next_c;
   float next_g = 0.0f;
   const int64_t dir = P.back ? -1 : 1;
   const auto begin_of = [&](int i) { return begin + (int64_t)(P.back ? chunks - 1 - i : i) * kChunk; };
@@ -791,7 +781,7 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
       return x;
     };
     constexpr int kXWide = X_IN_LDS || kSlice < DA ? kSlice : DA, kXParts = kSlice / kXWide;
-    Staged<In, Core, kXWide, 1, WAVES, WAY> now_x[kXParts];
+    Staged<In, kXWide, 1, WAVES, WAY> now_x[kXParts];
     if constexpr (PAIRS)
 #pragma unroll
       for (int k = 0; k < kXParts; ++k)
@@ -825,9 +815,9 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
           Frag p[N_OUT];
           if constexpr (RANGED) {
             const f32x4 ranged[2] = {state[j * kT] * range.up, state[j * kT + 1] * range.up};
-            pieces_of<Core, N_OUT>(ranged, p);
+            pieces_of<In, N_OUT>(ranged, p);
           } else {
-            pieces_of<Core, N_OUT>(*(const f32x4(*)[kT])&state[j * kT], p);
+            pieces_of<In, N_OUT>(*(const f32x4(*)[kT])&state[j * kT], p);
           }
 #pragma unroll
           for (int t = 0; t < 4; ++t) {
@@ -871,7 +861,7 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
       from_state();
       f32x4 score[kTiles];
       // x by rows: in 16 bits behind P's two pieces, in fp32 over P once that has been used, as many columns as there is room for
-      typedef Core XRows[kChunk][kXWide + Shared::kPad];
+      typedef In XRows[kChunk][kXWide + Shared::kPad];
       XRows& x_rows = *reinterpret_cast<XRows*>(&S.a[0][0] + (X_IN_LDS ? Shared::kTwo : 0));
       const auto add_products_of_x = [&](f32x4& sum, int s, int t, int from) {      // of rows s of c with rows t of x
 #pragma unroll
@@ -933,8 +923,8 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
       const auto range_of = [&](int t) { return Range(__uint_as_float(S.most[16 * t + l])); };      // of P's row
       __syncthreads();
       // P by rows, over a (and b, which in 16 bits is needed by columns only from here on)
-      Core (*const scores)[kChunk][Shared::kScoreRow] = reinterpret_cast<Core (*)[kChunk][Shared::kScoreRow]>(&S.a[0][0]);
-      static_assert(Shared::kTurned ? N_OUT <= 3 : kChunk * Shared::kScoreRow * sizeof(Core) <= sizeof(S.a));
+      In (*const scores)[kChunk][Shared::kScoreRow] = reinterpret_cast<In (*)[kChunk][Shared::kScoreRow]>(&S.a[0][0]);
+      static_assert(Shared::kTurned ? N_OUT <= 3 : kChunk * Shared::kScoreRow * sizeof(In) <= sizeof(S.a));
 #pragma unroll
       for (int n = 0; n < kTiles; ++n) {
         const int pair = tiles >> (8 * (kTiles - 1 - n)) & 255, t = pair >> 4, s = pair & 15;
@@ -947,9 +937,9 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
         }
 #pragma unroll
         for (int k = 0; k < N_OUT; ++k) {
-          store_floats<Core, 4>(&scores[k][16 * t + l][16 * s + 4 * g], left);
+          store_floats<In, 4>(&scores[k][16 * t + l][16 * s + 4 * g], left);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) left[r] -= to_float((Core)left[r]);
+          for (int r = 0; r < 4; ++r) left[r] -= to_float((In)left[r]);
         }
       }
       if constexpr (PAIRS && X_IN_LDS) now_x[0].store(thread, x_rows);
@@ -1092,7 +1082,7 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
       for (int s = 0; s < kS; ++s) {
 #pragma unroll
         for (int t = 0; t < kT; ++t) w[s][t] = w[s][t] * range.up;
-        pieces_of<Core, N_STATE>(w[s], p[s]);
+        pieces_of<In, N_STATE>(w[s], p[s]);
       }
 #pragma unroll
       for (int j = 0; j < kJ * kT; ++j) {
@@ -1115,7 +1105,7 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<Core, DA, WAVES>)) void k_
         f32x4 w[kT];
         weighted(s, w);
         Frag p[N_STATE];
-        pieces_of<Core, N_STATE>(w, p);
+        pieces_of<In, N_STATE>(w, p);
 #pragma unroll
         for (int j = 0; j < kJ * kT; ++j) {
           const Frag rows = rows_of_b(s, j);

@@ -23,9 +23,8 @@ int run_chunks(const choco_linear_config& c, const LinearArgs& A, const LinearPa
 #ifdef CHOCO_LINEAR_TYPE
 template <class In, int DA, int WAVES, int MODE, int WAY>
 int launch_chunks(const choco_linear_config& c, const LinearArgs& A, const LinearPass& P, const LinearChunks& C) {
-  typedef In Core;
-  const size_t lds = sizeof(ChunkShared<Core, DA, WAVES>);
-  const auto kernel = k_linear_chunks<In, Core, DA, WAVES, MODE, WAY>;
+  const size_t lds = sizeof(ChunkShared<In, DA, WAVES>);
+  const auto kernel = k_linear_chunks<In, DA, WAVES, MODE, WAY>;
   if (lds > 65536) {
     static std::atomic<uint64_t> done{0};
     TRY_HIP(allow_lds((const void*)kernel, lds, done));

@@ -30,7 +30,7 @@ constexpr int kMuonMost = 1 << 16;
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef float float4_t __attribute__((ext_vector_type(4)));
 
-// Matrices of one shape: one of each of `count` workers from `first` on.
+// Matrices of one shape: one of each of some workers from `first` on.
 struct MuonShape {
   int64_t source, source_of;      // entries from the source's begin to the first worker's matrix, and from there to the next's
   int64_t target, target_of;      // of x or of the result
@@ -38,7 +38,7 @@ struct MuonShape {
   int64_t source_ld, target_ld;
   int64_t scratch, scratch_of;    // bytes
   int64_t partials;               // sums of squares of the tiles, one matrix behind the other
-  int32_t rows, cols, a, b, a_ld, b_ld, first, count;
+  int32_t rows, cols, a, b, a_ld, b_ld, first;
   float decay, rate;
   uint32_t start_begin, gram_begin, apply_begin;    // tiles before these matrices'
   uint32_t start_tiles, gram_tiles, apply_tiles;    // of one of them

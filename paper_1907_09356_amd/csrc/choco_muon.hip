@@ -49,7 +49,7 @@ bool whole(int64_t rows, int64_t cols) {
 constexpr int kTileThreads = 256;
 int threads_of(bool whole) { return whole ? 64 * kWholeWaves : kTileThreads; }
 
-// A shape's sides, operands and tiles (null: taken whole); `count` and what is behind the begins are the caller's.
+// A shape's sides, operands and tiles (null: taken whole); where it lies and what is behind the begins are the caller's.
 MuonShape shape_from(int64_t rows, int64_t cols, const Tiles* tiles) {
   MuonShape S{};
   S.rows = (int32_t)rows;
@@ -248,7 +248,6 @@ int muon_layout(const choco_muon_config& c, std::vector<MuonShape>& table, std::
         count = 1;
       }
       S.first = w;
-      S.count = (int32_t)count;
       S.source = start + w * ld;
       S.target = S.source;
       S.scratch = scratch;
@@ -314,7 +313,6 @@ int choco_orthogonalize(const choco_orthogonalize_config* cfg, const void* x_dev
   for (int64_t first = 0; first < c.batch; first += L.each) {
     MuonArgs A{};
     A.one = L.shape;
-    A.one.count = (int32_t)std::min(L.each, c.batch - first);
     A.one.source = first * c.x_stride[0];
     A.one.source_of = c.x_stride[0];
     A.one.source_ld = c.x_stride[1];
@@ -325,7 +323,7 @@ int choco_orthogonalize(const choco_orthogonalize_config* cfg, const void* x_dev
     A.target = y_dev;
     A.partials = (double*)((char*)workspace_dev + L.partials);
     A.scratch = (char*)workspace_dev + L.scratch;
-    const uint32_t count = (uint32_t)A.one.count;
+    const uint32_t count = (uint32_t)std::min(L.each, c.batch - first);
     const Round R{0, 1, count * L.shape.start_tiles, count * L.shape.gram_tiles, count * L.shape.apply_tiles, L.whole ? whole_bytes(L.shape.a, L.shape.b) : 0};
     int rc = CHOCO_OK;
     with_type(c.type, [&](auto x) { rc = run_round<decltype(x), false>(A, R, c.iterations, L.tiles, (hipStream_t)c.stream); });
