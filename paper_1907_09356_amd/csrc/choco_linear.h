@@ -364,10 +364,17 @@ struct ChunkShared {
   Core more[kTurned && kScores > kRows ? kScores - kRows : 1];
   alignas(16) Core c[kChunk][kSlice + kPad];
   alignas(16) Core turned[kTurned ? DA : 1][kTurned ? kTurnedRow : 1];
-  alignas(16) float c_high[kChunk], c_low[kChunk], to_end[kChunk], dots[WAVES][kChunk];
-  uint32_t most[kChunk];
-  alignas(16) float behind[10][16], before[10][16];      // sums over pairs of steps, of ten tiles
-  float met[WAVES], ahead[WAVES], weights[kChunk], ahead_all;
+  alignas(16) float c_high[kChunk], c_low[kChunk], to_end[kChunk];
+  // for the gates' gradient, by one pass or the other (so that three workgroups of 64 x 64 in fp32 fit a compute unit)
+  union {
+    struct {
+      float dots[WAVES][kChunk], met[WAVES], ahead[WAVES], weights[kChunk], ahead_all;
+    };
+    struct {
+      alignas(16) float behind[10][16], before[10][16];      // sums over pairs of steps, of ten tiles
+    };
+  };
+  uint32_t most[std::is_same_v<Core, f16_t> ? kChunk : 1];
 };
 
 // How rows are read: parts of 16 bytes or words of 4 by offsets of 32 bits, where what is not there has one outside the buffer and comes
@@ -707,20 +714,20 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<In, DA, WAVES>)) void k_li
   // What a chunk's pairs put on its steps, those on either side of each, by one wave (backwards: a step's begin is its row's end).
   const auto gather = [&](int i) {
     const int64_t t0 = begin_of(i);
-    const int row = kChunk - 1 - lane, m = (row + 1) >> 4, e = (row + 1) & 15;
-    if (t0 + lane >= inside) return;
-    float sum = 0.0f;
-    if (m < 4) {
-      sum = S.behind[m * (m + 1) / 2 + m][e];
+    const int row = kChunk - lane, m = row >> 4, e = row & 15;      // (the row from whose begin on pairs count)
+    const auto tile = [](int t, int s) { return t * (t + 1) / 2 + s; };
+    const auto of = [](bool there, float x) { return there ? x : 0.0f; };
+    const int mine = m & 3;
+    float sum = S.behind[tile(mine, mine)][e];
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int s = 0; s < t; ++s) {
-          if (t == m) sum += S.behind[t * (t + 1) / 2 + s][e];
-          if (s == m) sum += S.before[t * (t + 1) / 2 + s][e];
-          if (s < m && m < t) sum += S.behind[t * (t + 1) / 2 + s][0];
-        }
+    for (int k = 0; k < 3; ++k) {
+      sum += of(k < mine, S.behind[tile(mine, k < mine ? k : 0)][e]);
+      sum += of(mine + k < 3, S.before[tile(mine + k < 3 ? mine + k + 1 : 3, mine + k < 3 ? mine : 0)][e]);
     }
+    if (mine == 1) sum += S.behind[tile(2, 0)][0] + S.behind[tile(3, 0)][0];
+    if (mine == 2) sum += S.behind[tile(3, 0)][0] + S.behind[tile(3, 1)][0];
+    if (m > 3) sum = 0.0f;
+    if (t0 + lane >= inside) return;
     P.dots[((int64_t)slice * A.batch * A.heads + bh) * A.steps + t0 + lane] = sum;
   };
   if (chunks > 0) ask(0, threadIdx.x);
@@ -1277,37 +1284,43 @@ __global__ __launch_bounds__(256) void k_linear_few_gates(LinearArgs A, LinearPa
   }
 #pragma unroll
   for (int k = 0; k <= 2 * N; ++k) {
-    float x = sums[k];
-    for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
+    const float x = rows_summed(row_sum(sums[k]));
     if (lane == 0) part[wave][k] = x;
   }
-  __syncthreads();
   const int t = threadIdx.x;
+  const bool counts = t < n && !(log_gate(A, b, t, h) < kLinearLeast);
+  __syncthreads();
+  if (wave > 0) return;
+  float all[2 * N + 1];
+  const float x = lane <= 2 * N ? (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]) : 0.0f;
+#pragma unroll
+  for (int k = 0; k <= 2 * N; ++k) all[k] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), k));
   float dg = 0.0f;
-  if (t < n && !(log_gate(A, b, t, h) < kLinearLeast)) {
-    const auto sum = [&](int k) { return (part[0][k] + part[1][k]) + (part[2][k] + part[3][k]); };
+  if (counts) {
     float left = 1.0f;      // from the first state to step s
-    for (int s = 0; s < n; ++s) {
+#pragma unroll
+    for (int s = 0; s < N; ++s) {      // (a step behind the sequence has a decay of one and rows of zeros)
       left *= w[s];
-      if (s >= t) dg = fmaf(left, sum(s), dg);
+      dg += s >= t ? left * all[s] : 0.0f;
     }
-    if (last) dg = fmaf(left, sum(2 * N), dg);
+    dg = last ? fmaf(left, all[2 * N], dg) : dg;
     left = 1.0f;      // from step r to the last
-    for (int r = n - 1; last && r >= 0; --r) {
-      if (r < t) dg = fmaf(left, sum(N + r), dg);
+#pragma unroll
+    for (int r = N - 1; r >= 0; --r) {
+      dg += last && r < t ? left * all[N + r] : 0.0f;
       left *= w[r];
     }
-    for (int s = t; s < n; ++s)
-      for (int r = 0; r < t; ++r) dg += pairs[s][r];
+#pragma unroll
+    for (int s = 1; s < N; ++s)
+#pragma unroll
+      for (int r = 0; r < s; ++r) dg += r < t && t <= s && s < n ? pairs[s][r] : 0.0f;
   }
   if (!G.sums) {
     if (t < A.steps) G.dg[(b * A.steps + t) * A.heads + h] = dg;
     return;
   }
-  if (wave == 0) {
-    const double all = wave_sum((double)dg);
-    if (lane == 0) G.dg[h * A.batch + b] = (float)all;
-  }
+  const double sum = wave_sum((double)dg);
+  if (lane == 0) G.dg[h * A.batch + b] = (float)sum;
 }
 // One head's sum over all sequences and pieces.
 __global__ __launch_bounds__(256) void k_linear_gate_sums(const float* parts, int64_t count, float* dg) {

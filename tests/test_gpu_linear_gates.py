@@ -20,7 +20,10 @@ def check_gates(q, k, v, g, h0, lengths, dy, dlast, relative=None):
     B, N, H = q.shape[0], q.shape[1], g.shape[-1]
     n = whole(lengths, B, N)
     exact = reference(q, k, v, g, h0, n, dy, dlast)
-    size = reference(q.abs(), k.abs(), v.abs(), g, h0.abs(), n, dy.abs(), dlast.abs())["steps_dg"]
+    if min(float(x.min()) for x in (q, k, v, h0, dy, dlast)) >= 0:
+        size = exact["steps_dg"]
+    else:
+        size = reference(q.abs(), k.abs(), v.abs(), g, h0.abs(), n, dy.abs(), dlast.abs())["steps_dg"]
     opened = reference(q.abs(), k.abs(), v.abs(), torch.zeros_like(g), h0.abs(), n, dy.abs(), dlast.abs())["steps_dg"]
     saved = T.linear_attention(q, k, v, g, h0=h0, lengths=lengths, save=True)[2]
     dg = T.linear_attention_grad(q, k, v, g, saved, dy, lengths=lengths, dlast=dlast)[3]
