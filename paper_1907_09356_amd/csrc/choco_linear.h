@@ -739,7 +739,7 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<In, DA, WAVES>)) void k_li
     const int64_t t0 = begin_of(i), first_time = t0 + (P.back ? kChunk - 1 : 0);
     // rows of the chunk that are in the sequence: forwards its first ones, backwards its last
     const int there = (int)min((int64_t)kChunk, inside - t0), lo = P.back ? kChunk - there : 0, hi = P.back ? kChunk : there;
-    if (!STATE && P.kept && t0 % kLinearSave == 0) keep(P.kept + (bh * P.kept_of + t0 / kLinearSave) * entries, 1.0f);
+    if (MODE == kResult && P.kept && t0 % kLinearSave == 0) keep(P.kept + (bh * P.kept_of + t0 / kLinearSave) * entries, 1.0f);
     __syncthreads();
     if (PAIRS && i > 0 && wave == WAVES - 1) gather(i - 1);
     if (!STATE) next_a.store(thread, S.a);
@@ -1001,6 +1001,9 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<In, DA, WAVES>)) void k_li
       }
       if constexpr (DOTS) {
         if (ahead) {      // the next chunk's rows with this one's state
+          int thread = threadIdx.x;      // (anew, for the registers)
+          asm volatile("" : "+v"(thread));
+          const int lane = thread & 63, l = lane & 15, g = lane >> 4, first = col + 4 * g;
           const int64_t t1 = begin_of(i + 1);
           const int there = (int)min((int64_t)kChunk, inside - t1), lo = P.back ? kChunk - there : 0, hi = P.back ? kChunk : there;
           __syncthreads();
@@ -1025,7 +1028,6 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<In, DA, WAVES>)) void k_li
               sum += row >= lo && row < hi ? d * S.weights[row] : 0.0f;
             }
             S.ahead[wave] = row_sum(sum);
-            columns(cf);      // (anew: there are no registers to keep it)
           }
           __syncthreads();
         }
@@ -1049,7 +1051,7 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<In, DA, WAVES>)) void k_li
         }
       }
       if constexpr (PAIRS && !X_IN_LDS) all_pairs();
-      if (i + 1 == chunks && (C.states || !P.last) && !P.kept) break;      // nobody reads the state
+      if (i + 1 == chunks && (C.states || !P.last) && !(MODE == kResult && P.kept)) break;      // nobody reads the state
     }
     if (!busy) continue;
     if constexpr (STATE) columns(cf);
@@ -1136,9 +1138,9 @@ __global__ __launch_bounds__(64 * WAVES, (kChunkWaves<In, DA, WAVES>)) void k_li
   const int width = in_slice;
   for (int64_t e = threadIdx.x; e < (end - zero) * width; e += 64 * WAVES)
     store_result<In>(P, out + (zero + e / width) * P.out_step + slice * kSlice + e % width, 0.0f);
-  if (P.kept && (len == 0 ? segment == 0 : begin < len && len <= end))
+  if (MODE == kResult && P.kept && (len == 0 ? segment == 0 : begin < len && len <= end))
     keep(P.kept + (bh * P.kept_of + (len + kLinearSave - 1) / kLinearSave) * entries, 1.0f);
-  if (P.last && !C.states) keep(P.last + bh * entries, P.back && len > 0 ? linear_decay(log_gate(A, b, 0, h)) : 1.0f);
+  if (!DOTS && P.last && !C.states) keep(P.last + bh * entries, P.back && len > 0 ? linear_decay(log_gate(A, b, 0, h)) : 1.0f);
 }
 
 #ifndef CHOCO_LINEAR_TYPE      // (where only one type's chunks are compiled)

@@ -158,3 +158,47 @@ def test_the_other_gradients_do_not_depend_on_whether_the_gates_is_asked_for(hea
                dy.data_ptr(), dlast.data_ptr(), *(x.data_ptr() for x in got), None, dh0.data_ptr(), workspace.data_ptr(), nbytes)
     for name, a, b in zip(("dq", "dk", "dv", "dh0"), got + [dh0], want[:3] + want[4:]):
         assert torch.equal(a, b), name
+
+
+@pytest.mark.parametrize("N", [5, 40, 300])
+@pytest.mark.parametrize("gate", ["step", "head"])
+def test_captured_and_replayed_beside_eager_calls(N, gate):
+    q, k, v, g, h0, lengths, dy, dlast = make(3, N, 2, 32, 64, F32, gate=gate, ragged=True)
+    other = make(3, N, 2, 32, 64, F32, gate=gate, seed=8)
+
+    def work(q, k, v, g, h0, lengths, dy, dlast):
+        saved = T.linear_attention(q, k, v, g, h0=h0, lengths=lengths, save=True)[2]
+        return T.linear_attention_grad(q, k, v, g, saved, dy, lengths=lengths, dlast=dlast)
+
+    want = [x.clone() for x in work(q, k, v, g, h0, lengths, dy, dlast)]
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        work(q, k, v, g, h0, lengths, dy, dlast)
+    torch.cuda.current_stream().wait_stream(stream)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = work(q, k, v, g, h0, lengths, dy, dlast)
+    for _ in range(3):
+        for x in got:
+            x.zero_()
+        work(*other)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_rows_far_apart():
+    # 2^26 entries: the last begins beyond 2^32 bytes
+    N, gap = 33, 1 << 26
+    flat = torch.zeros(N * gap, dtype=BF16, device="cuda")
+    q, k, v, g, h0, _, dy, dlast = make(1, N, 1, 16, 24, BF16)
+    saved = T.linear_attention(q, k, v, g, h0=h0, save=True)[2]
+    want = T.linear_attention_grad(q, k, v, g, saved, dy, dlast=dlast)
+    for i in range(4):
+        parts = [q, k, v, dy]
+        far = flat.as_strided(parts[i].shape, (0, gap, parts[i].shape[3], 1))
+        far.copy_(parts[i])
+        parts[i] = far
+        got = T.linear_attention_grad(*parts[:3], g, saved, parts[3], dlast=dlast)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
