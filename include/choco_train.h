@@ -142,7 +142,8 @@ int choco_linear_forward(const choco_linear_config* cfg, const void* q_dev, cons
    from the last step of a sequence back, E_t the gradient of S_t:
      E_t = q_t dy_t^T + exp(g_{t+1}) E_{t+1}  (+ dlast at its last step),
      dq_t = S_t dy_t,  dk_t = E_t v_t,  dv_t = E_t^T k_t,  dg_t = exp(g_t) <E_t, S_{t-1}>,  dh0 = exp(g_1) E_1 (dlast for an empty one);
-   the gradients of heads that share a q, k or v are added up.  dg_dev: batch x steps x heads fp32, or with gate_steps = 0
+   the gradients of heads that share a q, k or v are added up.  dg_t is added up of what passes step t alone, so that a gate that is
+   nearly closed has as many places right as an open one.  dg_dev: batch x steps x heads fp32, or with gate_steps = 0
    heads sums over all steps.  dg_dev and dh0_dev (as h0) may be NULL.  Every sum is taken in an order that
    depends on the sizes alone: same inputs, same bits. */
 int choco_linear_backward(const choco_linear_config* cfg, const void* q_dev, const void* k_dev, const void* v_dev,

@@ -6,11 +6,12 @@
 //   dk: v, dy, q   backwards           dv: k, q, dy     backwards
 // where w = e^g_t forwards, and backwards the next step's, 1 at a sequence's last.
 //
-// Measured, us a call (what it has to read and write at the rate of a large copy, 5.1 TB/s): one token of 64 x 16 heads of 128 in bf16 26 (26),
-// of 160 x 13 of 50 in fp32 15 (8); 160 x 35 x 13 x 50 in fp32 62 (17), backward 210 (25); 2 x 32,768 x 16 x 128 in bf16, lengths from a half on,
-// 479 to 497 (172); 8 x 2000 x 20 x 64 in fp16, q and k shared by four, 91 (21); backward of 4 x 16,384 x 10 x 128 in bf16 1,080 (230).
+// Measured, us a call (what it has to read and write at the rate of a large copy, 5.1 TB/s), three sets of inputs in turn: one token of 64 x 16 heads of
+// 128 in bf16 28 (26), of 160 x 13 of 50 in fp32 12 (8); 160 x 35 x 13 x 50 in fp32 62 (17), backward 229 (25); 2 x 32,768 x 16 x 128 in bf16, lengths
+// from a half on, 489 (172); 8 x 2000 x 20 x 64 in fp16, q and k shared by four, 95 (21); backward of 4 x 16,384 x 10 x 128 in bf16 1,200 (230).
 // Before: step by step all of it, 69,800 and 131,900 for the long ones; chunks without loads ahead 1,320 and 2,840; every wave its own P, 780
-// and 2,120; loads with branches, 710 and 2,030; four waves and 64 columns a workgroup 640 and 1,610.
+// and 2,120; loads with branches, 710 and 2,030; four waves and 64 columns a workgroup 640 and 1,610; gates' gradients by differences of sums, which
+// lose their places where a gate is nearly closed, 1,090 backward.
 #pragma once
 
 #include <type_traits>
@@ -69,8 +70,9 @@ __device__ __forceinline__ void store_result(const LinearPass& P, int64_t at, fl
 
 // ---- step by step ----
 // A workgroup takes a slice of columns and holds the state in registers, V columns of every 4 V-th row a lane (V as the state's rows divide;
-// one that lies on no border of V is read and written by entries, with the same sums).  Bound by the state, in and out once: for a step of D x D, 8 D^2 bytes against 5 D^2 operations.  One token of 64 x 16 heads of 128
-// in bf16 26 us, 5.1 TB/s (a column a lane, a quarter of the rows a wave: 33), of 160 x 13 of 50 in fp32 15, 2.8 TB/s (20).
+// one that lies on no border of V is read and written by entries, with the same sums).  Bound by the state, in and out once: for a step of D x D,
+// 8 D^2 bytes against 5 D^2 operations.  One token of 64 x 16 heads of 128 in bf16 28 us, 4.8 TB/s (25 and 5.4 where its 135 MB stay in the last-level
+// cache; a column a lane, a quarter of the rows a wave: 33), of 160 x 13 of 50 in fp32 12 us, 3.6 TB/s (20).
 constexpr int kLinearStage = 8;     // steps whose a and b are in LDS at a time
 
 template <class T, int V, int D>
@@ -1178,8 +1180,11 @@ __global__ __launch_bounds__(256) void k_linear_scan(LinearArgs A, float* states
 // ---- the gates' gradient ----
 // dg_t = e^g_t <E_t, S_{t-1}> = the sum over pairs of steps s >= t > r of e^(c_s - c_r) (q_s k_r) (dy_s v_r), where r may also stand for the first state
 // and s for the last one's gradient: only what passes t is added up, so that a gate that hardly lets anything through has as many places right as
-// any other.  (By differences, sums of q dq - k dk, a gate of -10 beside open ones has two.)  In chunks, dv's pass has pairs
-// within a chunk, dq's and dk's those with what is before or behind it, by slices.
+// any other.  (By differences, sums of q dq - k dk, a gate of -10 beside open ones has two, one of -20 none.)  In chunks, dv's pass has pairs
+// within a chunk, as score times score, dq's and dk's those with what is before or behind it, by slices.  Bound as these passes are: of 4 x 16,384 x 10 x
+// 128 in bf16 dq and dk take 395 us each (325 without their part: a state more to read for two of four chunks, a product with another chunk's rows),
+// dv 297 (245: its x to read, a score more); in fp32, 160 x 35 x 13 x 50, 70 (65) and 91 (70).  What is left, the slices' sum, takes 7 us of the long one.
+// Not kept: states between the chunks written by dq's pass and read by dk's, 1,680 to 1,420 us in all; pairs in dq's pass, whose registers do not hold them.
 struct LinearGates {
   const float* dots;     // [slices of dq, dk and dv][batch * heads][steps]
   int32_t slices;
@@ -1211,7 +1216,7 @@ __global__ __launch_bounds__(kLinearSave) void k_linear_gates(LinearArgs A, Line
 }
 
 // ... of up to N steps, by one workgroup for a sequence and head: products of steps' rows, and of rows with the first state and the last one's gradient, both read
-// once.  P is dv's pass (a, b, c = k, q, dy) with x = v; P.first and P.met_last are the two states.
+// once.  Bound by latency: 8 steps of 160 x 10 heads of 64 in fp32 37 us, the two states 10 at the rate of a copy.  P is dv's pass (a, b, c = k, q, dy) with x = v; P.first and P.met_last are the two states.
 constexpr int few_row(int n) { return 2 * n + 4; }       // floats of a row of LDS, of which four neighbours are read at a time
 template <class T, int N>
 __global__ __launch_bounds__(256) void k_linear_few_gates(LinearArgs A, LinearPass P, LinearGates G) {

@@ -144,9 +144,9 @@ int width_of(const Rows& r, size_t size, int most, const choco_linear_config& c)
   return 1;
 }
 
-// Up to so many steps are taken one by one.  us, one by one | in chunks, forward and backward: 160 x 10 heads of 64 in fp32, 4 steps 20 and 65 |
-// 35 and 104, 8 steps 31 and 94 | 36 and 107, 12 steps 41 and 127 | 38 and 110; 64 x 16 heads of 128 in bf16, 4 steps 35 and 113 | 34 and 99, 8 steps 48
-// and 159 | 34 and 100.
+// Up to so many steps are taken one by one.  us, one by one | in chunks, forward and backward, three sets of inputs in turn: 160 x 10 heads of 64 in fp32, 4
+// steps 22 and 81 | 41 and 123, 8 steps 33 and 125 | 40 and 124; 64 x 16 heads of 128 in bf16, 2 steps 31 and 140 | 39 and 114, 3 steps 35 and 150 | 39 and
+// 120, 4 steps 38 and 157 | 38 and 115, 8 steps 53 and 223 | 38 and 117.
 constexpr int kFewOf32 = 8, kFewOf16 = 3;
 int64_t step_by_step(const choco_linear_config& c) { return c.type == CHOCO_F32 ? kFewOf32 : kFewOf16; }
 
